@@ -519,6 +519,168 @@ int64_t lipcache_size(const lipcache_t* h);
  * for asynchronous inserts still running. NULL-safe. */
 void lipcache_destroy(lipcache_t* h);
 
+/* ------------------------------------------------------------------ heads
+ * Operators that train and serve the heads a cache certifies: logits under a
+ * shared head and each row's own low-rank adapter, their gradients, the
+ * cross-entropy loss, and orthogonalised optimiser steps (which keep a
+ * matrix's singular values, hence sigma_max of Eq. 17, level). None needs a
+ * cache handle. They share these conventions:
+ *
+ *  - The work is enqueued on `stream` of the current device and the call
+ *    returns; nothing synchronises and nothing is allocated, so calls can be
+ *    captured into a CUDA graph. Scratch is a caller's workspace (device
+ *    memory, 256-byte aligned, at least as many bytes as the matching
+ *    *_workspace function returns, -1 for sizes the operator refuses). One
+ *    workspace serves calls that follow one another on one stream; its
+ *    contents need not be kept between calls.
+ *  - Matrices are row-major; `ld` arguments are row strides in elements. Any
+ *    element alignment is taken; rows that start on 16-byte boundaries are
+ *    read fastest. Outputs must not overlap inputs unless stated.
+ *  - Tensors are LIPCACHE_F32 or LIPCACHE_BF16; sums and statistics are held
+ *    in FP32 or better, and each output is rounded once. FP32 products on the
+ *    tensor cores are taken as three FP16 products of operands split in two
+ *    (22 bits of each operand's row or matrix maximum).
+ *  - A bounded wait that expires on the device leaves the call's outputs
+ *    undefined and is counted (lipcache_operator_errors).
+ */
+#define LIPCACHE_F32 0
+#define LIPCACHE_BF16 1
+
+/* Limits of the operators (E_INVALID beyond them). */
+#define LIPCACHE_MAX_SIDE 65536        /* d, classes, and the smaller side of an orthogonalised matrix: 16384 */
+#define LIPCACHE_MAX_RANK 128
+#define LIPCACHE_MAX_ADAPTERS 4096
+#define LIPCACHE_MAX_TOKENS (1LL << 24)
+#define LIPCACHE_MAX_LOSS_CLASSES (1 << 24)
+#define LIPCACHE_MAX_NS_STEPS 32
+
+/* A shared head with low-rank adapters, and the rows it is applied to. */
+typedef struct lipcache_adapted {
+  int32_t type;            /* of x, W, A, B and of the outputs: LIPCACHE_F32 or LIPCACHE_BF16 */
+  int32_t d;               /* features of a row, 1 .. LIPCACHE_MAX_SIDE */
+  int32_t classes;         /* rows of W, 1 .. LIPCACHE_MAX_SIDE */
+  int32_t adapters;        /* G, 0 .. LIPCACHE_MAX_ADAPTERS */
+  int32_t rank;            /* r, 1 .. LIPCACHE_MAX_RANK (not read when adapters is 0) */
+  int32_t reserved;        /* 0 */
+  int64_t tokens;          /* rows of x, 0 .. LIPCACHE_MAX_TOKENS */
+  const void* x;           /* tokens x d, row stride ldx */
+  int64_t ldx;
+  const void* W;           /* classes x d, row stride ldw */
+  int64_t ldw;
+  const void* A;           /* G x rank x d, dense */
+  const void* B;           /* G x classes x rank, dense */
+  const int32_t* adapter;  /* tokens: each row's adapter; a value outside [0, G) means none */
+  const float* scales;     /* G, nullable (1): factor of each adapter's product */
+} lipcache_adapted;
+
+/* Workspace bytes of lipcache_adapted_logits (backward = 0) or
+ * lipcache_adapted_logits_backward (1) for the sizes in *p (pointers in it
+ * are not read); -1 if they are refused (no counterpart in the paper). */
+int64_t lipcache_adapted_workspace(const lipcache_adapted* p, int32_t backward);
+
+/*
+ * Logits of rows under a shared head and each row's adapter g = adapter[t]
+ * (the head of Eq. 5 with a low-rank term per tenant; no counterpart in the
+ * paper):
+ *   y_t = W x_t + bias + scales[g] B_g (A_g x_t)
+ *   bias  classes FP32, nullable
+ *   y     tokens x classes, row stride ldy
+ * Rows of one request may stand anywhere; rows whose adapters stand in
+ * non-decreasing order save a copy of x. tokens == 0 is a no-op.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_adapted_logits(const lipcache_adapted* p, const float* bias, void* y, int64_t ldy,
+                                        void* workspace, int64_t workspace_bytes, lipcache_stream_t stream);
+
+/*
+ * Gradients of lipcache_adapted_logits, W and bias being held fixed (no
+ * counterpart in the paper). With u_t = scales[g] A_g x_t and
+ * v_t = scales[g] B_g^T dy_t:
+ *   dx_t = W^T dy_t + A_g^T v_t             tokens x d, row stride lddx
+ *   dA_g = sum over g's rows of v_t x_t^T   G x rank x d
+ *   dB_g = sum over g's rows of dy_t u_t^T  G x classes x rank
+ * Each output is nullable (then not computed); gradients of adapters without
+ * rows are zero. Sums are taken in a fixed order: results repeat bit for bit.
+ *   dy    tokens x classes, row stride lddy
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_adapted_logits_backward(const lipcache_adapted* p, const void* dy, int64_t lddy, void* dx,
+                                                 int64_t lddx, void* dA, void* dB, void* workspace,
+                                                 int64_t workspace_bytes, lipcache_stream_t stream);
+
+/*
+ * Softmax cross entropy of each row and its gradient in one call (the L_CE of
+ * Eq. 7):
+ *   loss_t = w_t (log sum_j exp z_tj - z_{t,target_t})
+ *   dz_tj  = w_t (exp(z_tj) / sum_k exp(z_tk) - [j = target_t])
+ *   type     of logits and dlogits
+ *   logits   tokens x classes, row stride ldz; -inf masks a class
+ *   target   tokens; a value outside [0, classes) ignores the row: loss and
+ *            gradient 0 whatever its logits
+ *   weight   tokens FP32, nullable (1)
+ *   loss     tokens FP32, nullable
+ *   dlogits  tokens x classes, row stride ldd, nullable; may be `logits`
+ *            itself with ldd == ldz
+ * A masked target gives loss +inf (0 at weight 0); a row that is masked whole
+ * has loss +inf and gradient 0; a NaN or +inf logit makes its row NaN.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_cross_entropy(int32_t type, const void* logits, int64_t ldz, int64_t tokens, int32_t classes,
+                                       const int32_t* target, const float* weight, float* loss, void* dlogits,
+                                       int64_t ldd, lipcache_stream_t stream);
+
+/* Workspace bytes of lipcache_orthogonalize and lipcache_orthogonal_step for
+ * `batch` matrices of rows x cols (`type`: that of G, or of the weights); -1
+ * if the sizes are refused (no counterpart in the paper). */
+int64_t lipcache_orthogonalize_workspace(int32_t type, int64_t batch, int32_t rows, int32_t cols);
+
+/*
+ * Orthogonalise each of `batch` matrices by Newton-Schulz products (no
+ * counterpart in the paper; the result's singular values are those of
+ * G / ||G|| moved towards 1, so sigma_max of Eq. 17 is about 1):
+ *   X = G / (||G||_F + eps), of G^T where rows > cols
+ *   `steps` times, with (a, b, c) of that step:  S = X X^T,
+ *   X <- a X + (b S + c S S) X
+ *   G             batch x rows x cols, row stride ldg, matrix stride
+ *                 rows * ldg
+ *   coefficients  host, 3 * steps
+ *   out           batch x rows x cols dense, type of G; may be G if that is
+ *                 dense
+ * FP32 matrices are iterated as pairs of FP16 values (22 bits), BF16 ones as
+ * single FP16 values (11 bits, three more than the output's), with FP32
+ * sums. Intended for polynomials that keep singular values below 4; beyond
+ * 16 they overflow. A matrix with a NaN or an infinity comes out NaN.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_orthogonalize(int32_t type, const void* G, int64_t ldg, int64_t batch, int32_t rows,
+                                       int32_t cols, int32_t steps, const double* coefficients, double eps, void* out,
+                                       void* workspace, int64_t workspace_bytes, lipcache_stream_t stream);
+
+/*
+ * One optimiser step with an orthogonalised direction, for `batch` matrices
+ * of rows x cols, all dense (no counterpart in the paper):
+ *   M' = beta M + (1 - beta) grad
+ *   D  = nesterov ? beta M' + (1 - beta) grad : M'
+ *   W' = (1 - lr weight_decay) W - lr sqrt(max(1, rows / cols)) O(D)
+ * with O as lipcache_orthogonalize computes it (in FP32's precision where
+ * weight_type is LIPCACHE_F32).
+ *   weight, out_weight      weight_type; may be the same array
+ *   grad                    grad_type
+ *   momentum, out_momentum  FP32; may be the same array
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_orthogonal_step(int32_t weight_type, int32_t grad_type, const void* weight, const void* grad,
+                                         const float* momentum, void* out_weight, float* out_momentum, int64_t batch,
+                                         int32_t rows, int32_t cols, double lr, double beta, int32_t nesterov,
+                                         double weight_decay, int32_t steps, const double* coefficients, double eps,
+                                         void* workspace, int64_t workspace_bytes, lipcache_stream_t stream);
+
+/* Bounded waits of the operators above that expired on the current device
+ * since the library was loaded, in *count (host). Synchronises `stream`
+ * (error reporting of this library, no counterpart in the paper).
+ * Errors: E_INVALID, E_CUDA. */
+lipcache_status lipcache_operator_errors(int64_t* count, lipcache_stream_t stream);
+
 /* Message of the last failed call on this thread ("" if none; error
  * reporting of this library, no counterpart in the paper). */
 const char* lipcache_last_error(void);

@@ -17,6 +17,7 @@ STATUS_NAMES = {0: "OK", 1: "E_INVALID", 2: "E_STATE", 3: "E_DEGENERATE_HEAD", 4
 RADIUS_CONSERVATIVE, RADIUS_TIGHT = 0, 1
 INSERT_STREAMED_BIT = 1 << 3  # 1 << LIPCACHE_INSERT_STREAMED
 NOALLOC_SCRATCH_BYTES = 4259840  # LIPCACHE_NOALLOC_SCRATCH_BYTES
+F32, BF16 = 0, 1  # LIPCACHE_F32, LIPCACHE_BF16
 PROBE_AUTO, PROBE_TENSOR, PROBE_EXACT, PROBE_TENSOR_SINGLE, PROBE_TENSOR_PAIR = 0, 1, 2, 3, 4
 
 # Every symbol the header declares; tests check the library exports them all.
@@ -26,7 +27,10 @@ EXPORTS = ["lipcache_create", "lipcache_set_head", "lipcache_insert", "lipcache_
            "lipcache_set_probe_path", "lipcache_set_radius_scale", "lipcache_set_spectral_options",
            "lipcache_reserve", "lipcache_enable_timing", "lipcache_get_info",
            "lipcache_get_screen_info", "lipcache_insert_kernels", "lipcache_reset_stats",
-           "lipcache_size", "lipcache_destroy", "lipcache_last_error"]
+           "lipcache_size", "lipcache_destroy", "lipcache_last_error",
+           "lipcache_adapted_workspace", "lipcache_adapted_logits", "lipcache_adapted_logits_backward",
+           "lipcache_cross_entropy", "lipcache_orthogonalize_workspace", "lipcache_orthogonalize",
+           "lipcache_orthogonal_step", "lipcache_operator_errors"]
 
 
 class Info(C.Structure):
@@ -45,6 +49,13 @@ class Info(C.Structure):
 
 class ScreenInfo(C.Structure):
     _fields_ = [("unfit", C.c_int64), ("fp16_copy", C.c_int32), ("fp16", C.c_int32)]
+
+
+class Adapted(C.Structure):
+    _fields_ = [("type", C.c_int32), ("d", C.c_int32), ("classes", C.c_int32), ("adapters", C.c_int32),
+                ("rank", C.c_int32), ("reserved", C.c_int32), ("tokens", C.c_int64), ("x", C.c_void_p),
+                ("ldx", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64), ("A", C.c_void_p), ("B", C.c_void_p),
+                ("adapter", C.c_void_p), ("scales", C.c_void_p)]
 
 
 class LipCacheError(RuntimeError):
@@ -91,6 +102,15 @@ def load(path: str = LIB_PATH):
         "lipcache_size": ([vp], i64),
         "lipcache_destroy": ([vp], None),
         "lipcache_last_error": ([], C.c_char_p),
+        "lipcache_adapted_workspace": ([C.POINTER(Adapted), i32], i64),
+        "lipcache_adapted_logits": ([C.POINTER(Adapted), vp, vp, i64, vp, i64, vp], C.c_int),
+        "lipcache_adapted_logits_backward": ([C.POINTER(Adapted), vp, i64, vp, i64, vp, vp, vp, i64, vp], C.c_int),
+        "lipcache_cross_entropy": ([i32, vp, i64, i64, i32, vp, vp, vp, vp, i64, vp], C.c_int),
+        "lipcache_orthogonalize_workspace": ([i32, i64, i32, i32], i64),
+        "lipcache_orthogonalize": ([i32, vp, i64, i64, i32, i32, i32, vp, f64, vp, vp, i64, vp], C.c_int),
+        "lipcache_orthogonal_step": ([i32, i32, vp, vp, vp, vp, vp, i64, i32, i32, f64, f64, i32, f64, i32, vp, f64,
+                                      vp, i64, vp], C.c_int),
+        "lipcache_operator_errors": ([C.POINTER(i64), vp], C.c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
