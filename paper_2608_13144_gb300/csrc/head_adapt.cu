@@ -8,8 +8,6 @@
 namespace lc {
 namespace ops {
 
-__device__ unsigned long long g_errors;
-
 namespace {
 
 struct AdaptLayout {
@@ -164,13 +162,6 @@ void adapted_backward(const lipcache_adapted& p, const void* dy, int64_t lddy, v
   else
     backward<__nv_bfloat16>(p, static_cast<const __nv_bfloat16*>(dy), lddy, static_cast<__nv_bfloat16*>(dx), lddx,
                             static_cast<__nv_bfloat16*>(dA), static_cast<__nv_bfloat16*>(dB), l, s);
-}
-
-uint64_t operator_errors(cudaStream_t s) {
-  unsigned long long n = 0;
-  LC_CUDA(cudaMemcpyFromSymbolAsync(&n, g_errors, sizeof n, 0, cudaMemcpyDeviceToHost, s));
-  LC_CUDA(cudaStreamSynchronize(s));
-  return n;
 }
 
 }  // namespace ops

@@ -1,0 +1,535 @@
+// Tensor-core products for the operators of heads: D = sum over segments of
+// A_s B_s^T in tiles of 128 CG x BN, with an epilogue of the caller's.
+//
+// Operands are 16-bit (FP16 or BF16 in a segment) 3-D tensors read by TMA with
+// the 128-byte swizzle, zero-filled past their ends, each either K-major (the
+// contracted index is the innermost) or MN-major. tcgen05 MMAs accumulate in
+// FP32 in tensor memory, two accumulators taking turns. CG = 2: a CTA pair
+// works on one 256-row tile (cta_group::2), each CTA holding its 128 rows of A
+// and half the columns of B, so that a CTA's shared memory feeds the MMAs 128
+// bytes a clock instead of 192.
+//
+// Warps of a CTA: 0 TMA producer, 1 MMA issuer (of the pair's leader), 2-9
+// epilogue (tcgen05.ld, 32 columns at a time). CTAs are persistent: tiles are
+// dealt round robin. Every wait is bounded; a role that gives up raises the
+// CTA's abort flag, the kernel drains, and a counter of the device takes note.
+//
+// The tensor cores' FP32 sums are cut off, not rounded, at each addition, which
+// shows in long sums as a drift of one sign (K = 1003 .. 2048, FP32 operands:
+// 1.8e-5 of the result after five Newton-Schulz steps). DRAIN breaks a sum
+// into blocks of `block` stages per segment: the epilogue warps take each
+// block's sums out of tensor memory and add them in registers, rounded, while
+// the MMAs of the next block run into the other accumulator.
+//
+// A segment can be limited to some rows of the tile (`mask`): the MMA's
+// disabled output lanes keep what they hold, so that rows of other adapters
+// neither change nor turn NaN.
+#pragma once
+
+#include "operators.cuh"
+#include "tc_ptx.cuh"
+
+namespace lc {
+namespace ops {
+
+namespace mma {
+
+constexpr int kChunk = 64;           // contracted elements of a stage
+constexpr int kABytes = 128 * 128;   // 128 rows x 64 elements
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 32 * (2 + kEpiWarps);
+constexpr long long kWaitLimit = 1LL << 31;  // ~1 s at GB300 clocks
+constexpr int kSmem = 227 * 1024;
+constexpr int kMaxSegs = 4;
+
+// One product of the sum: `chunks` stages along the contracted index, the last
+// one of `last` MMAs (16 elements each).
+struct Seg {
+  int chunks, last;
+  int a_z, b_z;    // added to the tile's batch index
+  uint32_t idesc;
+};
+
+__host__ __device__ constexpr uint32_t idesc(int M, int N, bool bf16, bool a_mn, bool b_mn) {
+  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// Shared-memory descriptor of an operand stored with the 128-byte swizzle.
+// K-major: rows of 128 bytes (64 elements of K), 8-row groups 1024 bytes apart.
+// MN-major: blocks of 64 elements of MN (128 bytes) x 64 of K, 8192 bytes each;
+// groups of 8 along K are 1024 bytes apart, blocks along MN 8192.
+__device__ __forceinline__ uint64_t desc(uint32_t saddr, bool mn) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(mn ? 8192 >> 4 : 1) << 16) |
+         ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z,
+                                             uint32_t leader_bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+      "%4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(leader_bar)
+      : "memory");
+}
+
+// The MMA with a mask of output lanes (rows) to leave alone; `off` holds the
+// lanes of this CTA (CG = 1) or of both (CG = 2), 32 a word.
+template <int CG>
+__device__ __forceinline__ void mma_masked(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc,
+                                           const uint32_t (&off)[8]) {
+  if (CG == 1)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8}, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(id), "r"(acc), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3])
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %6, %7, %8, %9, %10, %11, %12}, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(id), "r"(acc), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3]), "r"(off[4]),
+        "r"(off[5]), "r"(off[6]), "r"(off[7])
+        : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+  if (CG == 1)
+    ptx::mma_f16(d, a, b, id, acc);
+  else
+    ptx::mma_f16_pair(d, a, b, id, acc);
+}
+
+// Runs of neighbouring rows that share an adapter (head_adapt.cu): run i is
+// rows [off[i], off[i + 1]), its adapter g[i] (outside [0, G): none).
+struct Runs {
+  const int* off;
+  const int* g;
+  const int* count;
+};
+
+// The low-rank segments of a tile: for each run in it and each of `pairs`
+// plane pairs, A rows of the run times B of the run's adapter.
+struct Low {
+  Runs runs;
+  int G = 0;          // 0: no low-rank segments
+  int chunks = 0, last = 0;
+  int pairs = 0;
+  int a_z[6], b_z[6];  // plane of each factor; B's z is b_z * G + adapter
+  uint32_t idesc;
+};
+
+struct Args {
+  int m_tiles, n_tiles, batches;
+  int sym;  // tiles on or above the diagonal only (m_tiles == n_tiles in units of the wider side)
+  int bn;   // columns of a tile
+  int stages;
+  int a_mn, b_mn, lb_mn;
+  int nseg;
+  int block;  // stages of each segment per block (DRAIN: all segments have the same stages)
+  Seg seg[kMaxSegs];
+  Low low;
+  unsigned long long* errors;  // expired waits, counted
+};
+
+// Tile `t`: its first row and column (in tiles) and batch index.
+__device__ __forceinline__ void tile_at(const Args& a, int t, int& mt, int& nt, int& z) {
+  if (a.sym) {
+    const int per = a.m_tiles * (a.m_tiles + 1) / 2;
+    z = t / per;
+    t -= z * per;
+    // column nt holds tiles 0..nt of the upper triangle
+    nt = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while (nt * (nt + 1) / 2 > t) --nt;
+    while ((nt + 1) * (nt + 2) / 2 <= t) ++nt;
+    mt = t - nt * (nt + 1) / 2;
+    return;
+  }
+  const int per = a.m_tiles * a.n_tiles;
+  z = t / per;
+  t -= z * per;
+  // bands of 8 row tiles, column by column: neighbours in time share operands in L2
+  const int band = t / (8 * a.n_tiles), rest = t - band * 8 * a.n_tiles;
+  const int high = min(8, a.m_tiles - band * 8);
+  nt = rest / high;
+  mt = band * 8 + rest - nt * high;
+}
+
+// The first run that reaches past row m0.
+__device__ __forceinline__ int first_run(const Runs& r, int n, int m0) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(r.off + mid + 1) > m0)
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
+}
+
+template <int CG, bool DRAIN, typename Epi>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_mma(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+          const __grid_constant__ CUtensorMap tmLA, const __grid_constant__ CUtensorMap tmLB, const Args a,
+          const Epi epi) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int b_bytes = a.bn / CG * 128, stage_bytes = kABytes + b_bytes;
+  const int nst = a.stages;
+  const uint32_t bars = base + nst * stage_bytes;
+  const uint32_t full = bars, empty = bars + 8 * nst, acc_full = empty + 8 * nst, acc_empty = acc_full + 16,
+                 drain = acc_empty + 16, misc = drain + 8;
+  unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
+  volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
+  volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? ptx::cluster_ctarank() : 0u;
+  const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+  constexpr int TM = 128 * CG;
+  const uint32_t cols = a.bn > 128 ? 512u : a.bn > 64 ? 256u : 128u;  // two accumulators
+  const uint32_t acc_stride = cols / 2;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < nst; ++s) {
+      ptx::mbar_init(full + 8 * s, 1);
+      ptx::mbar_init(empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(acc_full + 8 * b, 1);
+      ptx::mbar_init(acc_empty + 8 * b, CG * kEpiWarps);
+    }
+    ptx::mbar_init(drain, 1);
+    *abort_s = 0;
+    ptx::fence_mbar_init();
+    ptx::tma_prefetch_desc(&tmA);
+    ptx::tma_prefetch_desc(&tmB);
+  }
+  if (warp == 1) {
+    if (CG == 2) {
+      ptx::tmem_alloc_pair(misc, cols);
+      ptx::tmem_relinquish_pair();
+    } else {
+      ptx::tmem_alloc(misc, cols);
+      ptx::tmem_relinquish();
+    }
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  if (CG == 2) ptx::cluster_sync();
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const uint32_t tmem = *tmem_slot;
+  const int per = a.sym ? a.m_tiles * (a.m_tiles + 1) / 2 : a.m_tiles * a.n_tiles;
+  const int tiles = per * a.batches;
+  const int n_runs = a.low.G ? __ldg(a.low.runs.count) : 0;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer
+    if (lane == 0) {
+      const uint32_t lead_full = CG == 2 ? ptx::mapa(full, 0) : full;
+      int st = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      // one stage: the boxes of A at (row, k) and of B at (column, k)
+      auto load = [&](const CUtensorMap* ma, bool a_mn, int row, int ak, int az, const CUtensorMap* mb, bool b_mn,
+                      int col, int bk, int bz) {
+        ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, kWaitLimit);
+        if (!ok) return;
+        if (rank == 0) ptx::mbar_expect_tx(full + 8 * st, (uint32_t)(CG * stage_bytes));
+        const uint32_t sa = base + st * stage_bytes, sb = sa + kABytes, bar = lead_full + 8 * st;
+        auto box = [&](uint32_t dst, const CUtensorMap* m, int x, int y, int z) {
+          if (CG == 2)
+            load_3d_pair(dst, m, x, y, z, bar);
+          else
+            load_3d(dst, m, x, y, z, bar);
+        };
+        if (a_mn) {
+          box(sa, ma, row, ak, az);
+          box(sa + 8192, ma, row + 64, ak, az);
+        } else {
+          box(sa, ma, ak, row, az);
+        }
+        if (b_mn) {
+          for (int i = 0; i < a.bn / CG; i += 64) box(sb + i * 128, mb, col + i, bk, bz);
+        } else {
+          box(sb, mb, bk, col, bz);
+        }
+        if (++st == nst) st = 0, ph ^= 1u;
+      };
+      for (int t = worker; t < tiles && ok; t += workers) {
+        int mt, nt, z;
+        tile_at(a, t, mt, nt, z);
+        const int row = mt * TM + (int)rank * 128, col = nt * a.bn + (int)rank * (a.bn / CG);
+        for (int c0 = 0; c0 < a.seg[0].chunks && ok; c0 += a.block)
+          for (int s = 0; s < a.nseg && ok; ++s) {
+            const Seg& sg = a.seg[s];
+            const int c1 = min(c0 + a.block, sg.chunks);
+            for (int c = c0; c < c1 && ok; ++c)
+              load(&tmA, a.a_mn, row, c * kChunk, sg.a_z + z, &tmB, a.b_mn, col, c * kChunk, sg.b_z + z);
+          }
+        if (n_runs) {
+          const int m0 = mt * TM;
+          for (int i = first_run(a.low.runs, n_runs, m0); i < n_runs && ok; ++i) {
+            if (__ldg(a.low.runs.off + i) >= m0 + TM) break;
+            const int g = __ldg(a.low.runs.g + i);
+            if (g < 0 || g >= a.low.G) continue;
+            for (int q = 0; q < a.low.pairs && ok; ++q)
+              for (int c = 0; c < a.low.chunks && ok; ++c)
+                load(&tmLA, false, row, c * kChunk, a.low.a_z[q], &tmLB, a.lb_mn, col, c * kChunk,
+                     a.low.b_z[q] * a.low.G + g);
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    if (rank == 0) {
+      const bool lead = ptx::elect_one();
+      int st = 0, n = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int t = worker; t < tiles && ok; t += workers) {
+        int mt, nt, z;
+        tile_at(a, t, mt, nt, z);
+        uint32_t d = 0, acc = 0;
+        // the next accumulator, once both CTAs' epilogues are done with it
+        auto open = [&]() {
+          ok = ptx::mbar_wait_warp<CG == 2>(acc_empty + 8 * (n & 1), (uint32_t)((n >> 1) & 1) ^ 1u, abort_s, kWaitLimit);
+          if (!ok) return;
+          ptx::tc_fence_after();
+          d = tmem + (uint32_t)(n & 1) * acc_stride;
+          acc = 0;
+        };
+        auto close = [&]() {
+          if (ok && lead) {
+            if (CG == 2)
+              ptx::mma_commit_pair_multicast(acc_full + 8 * (n & 1), (uint16_t)3);
+            else
+              ptx::mma_commit(acc_full + 8 * (n & 1));
+          }
+          ++n;
+        };
+        // one stage of `steps` MMAs
+        auto chunk = [&](bool a_mn, bool b_mn, uint32_t id, int steps, const uint32_t* off) {
+          ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, kWaitLimit);
+          if (!ok) return;
+          ptx::tc_fence_after();
+          if (lead) {
+            uint64_t da = desc(base + st * stage_bytes, a_mn), db = desc(base + st * stage_bytes + kABytes, b_mn);
+            const uint64_t ia = a_mn ? 2048 >> 4 : 32 >> 4, ib = b_mn ? 2048 >> 4 : 32 >> 4;
+            for (int k = 0; k < steps; ++k, da += ia, db += ib) {
+              if (off) {
+                const uint32_t o[8] = {off[0], off[1], off[2], off[3], off[4], off[5], off[6], off[7]};
+                mma_masked<CG>(d, da, db, id, 1u, o);
+              } else {
+                mma<CG>(d, da, db, id, acc);
+              }
+              acc = 1;
+            }
+            if (CG == 2)
+              ptx::mma_commit_pair_multicast(empty + 8 * st, (uint16_t)3);
+            else
+              ptx::mma_commit(empty + 8 * st);
+          }
+          if (++st == nst) st = 0, ph ^= 1u;
+        };
+        for (int c0 = 0; c0 < a.seg[0].chunks && ok; c0 += a.block) {
+          if (c0) close();
+          open();
+          for (int s = 0; s < a.nseg && ok; ++s) {
+            const Seg& sg = a.seg[s];
+            const int c1 = min(c0 + a.block, sg.chunks);
+            for (int c = c0; c < c1 && ok; ++c)
+              chunk(a.a_mn, a.b_mn, sg.idesc, c == sg.chunks - 1 ? sg.last : 4, nullptr);
+          }
+        }
+        if (n_runs) {
+          const int m0 = mt * TM;
+          for (int i = first_run(a.low.runs, n_runs, m0); i < n_runs && ok; ++i) {
+            const int r0 = __ldg(a.low.runs.off + i) - m0, r1 = __ldg(a.low.runs.off + i + 1) - m0;
+            if (r0 >= TM) break;
+            const int g = __ldg(a.low.runs.g + i);
+            if (g < 0 || g >= a.low.G) continue;
+            uint32_t off[8];
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+              const int lo = min(max(r0 - 32 * w, 0), 32), hi = min(max(r1 - 32 * w, 0), 32);
+              const uint32_t on = (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~(lo == 32 ? 0xffffffffu : (1u << lo) - 1u);
+              off[w] = ~on;
+            }
+            for (int q = 0; q < a.low.pairs && ok; ++q)
+              for (int c = 0; c < a.low.chunks && ok; ++c)
+                chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, off);
+          }
+        }
+        close();
+      }
+      // every MMA has completed before tensor memory is given back
+      if (lead) {
+        volatile int never = 0;
+        if (CG == 2)
+          ptx::mma_commit_pair_multicast(drain, (uint16_t)1);
+        else
+          ptx::mma_commit(drain);
+        ptx::mbar_wait(drain, 0, &never, kWaitLimit);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ epilogue
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t lead_empty = CG == 2 ? ptx::mapa(acc_empty, 0) : acc_empty;
+    int n = 0;
+    bool ok = true;
+    for (int t = worker; t < tiles && ok; t += workers) {
+      int mt, nt, z;
+      tile_at(a, t, mt, nt, z);
+      const int row = mt * TM + (int)rank * 128 + quarter * 32;
+      uint32_t src = 0;
+      auto open = [&]() {
+        ok = ptx::mbar_wait(acc_full + 8 * (n & 1), (uint32_t)((n >> 1) & 1), abort_s, kWaitLimit);
+        ok = __all_sync(0xffffffffu, ok);
+        ptx::tc_fence_after();
+        src = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(n & 1) * acc_stride;
+      };
+      auto close = [&]() {
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (CG == 2)
+            ptx::mbar_arrive_cluster(lead_empty + 8 * (n & 1));
+          else
+            ptx::mbar_arrive(acc_empty + 8 * (n & 1));
+        }
+        ++n;
+      };
+      if (DRAIN) {
+        constexpr int kParts = CG == 2 ? 4 : 2;  // bn <= 128 CG
+        float sum[kParts][32];
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum[i][j] = 0.f;
+        for (int c0 = 0; c0 < a.seg[0].chunks; c0 += a.block) {
+          open();
+          if (!ok) break;
+#pragma unroll
+          for (int i = 0; i < kParts; ++i) {
+            if (half * 32 + 64 * i >= a.bn) break;
+            uint32_t v[32];
+            ptx::tmem_ld32(src + half * 32 + 64 * i, v);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sum[i][j] += __uint_as_float(v[j]);
+          }
+          close();
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+          const int c = half * 32 + 64 * i;
+          if (c >= a.bn) break;
+          uint32_t v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[i][j]);
+          epi.store(row, nt * a.bn + c, z, lane, v);
+        }
+      } else {
+        open();
+        if (!ok) break;
+        for (int c = half * 32; c < a.bn; c += 64) {
+          uint32_t v[32];
+          ptx::tmem_ld32(src + c, v);
+          ptx::tmem_wait_ld();
+          epi.store(row, nt * a.bn + c, z, lane, v);
+        }
+        close();
+      }
+    }
+  }
+  __syncthreads();
+  if (*abort_s) {
+    // copies this CTA has issued end long before this does
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1LL << 23)) {
+    }
+    if (threadIdx.x == 0) atomicAdd(a.errors, 1ull);
+    __syncthreads();
+  }
+  ptx::tc_fence_after();
+  if (CG == 2) ptx::cluster_sync();
+  if (warp == 1) {
+    if (CG == 2)
+      ptx::tmem_dealloc_pair(tmem, cols);
+    else
+      ptx::tmem_dealloc(tmem, cols);
+  }
+}
+
+// ---------------------------------------------------------------- host side
+EncodeTiledFn encoder();
+// Lets `kernel` use `bytes` of dynamic shared memory on the current device.
+void allow_smem(const void* kernel, int bytes);
+int num_sms();
+// The current device's counter of expired waits.
+unsigned long long* error_counter();
+
+// A 16-bit tensor of `planes` x rows x cols, row stride ld elements and plane
+// stride `plane` elements (both multiples of 8, the base 16-byte aligned).
+struct Tensor {
+  const void* base;
+  int64_t cols, rows, planes, ld, plane;
+};
+// Its map with a box of 64 x box_rows.
+CUtensorMap tensor_map(const Tensor& t, int box_rows);
+inline bool mappable(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+inline Seg segment(int64_t k, int a_z, int b_z, uint32_t id) {
+  const int chunks = (int)ceil_div(k, kChunk);
+  return Seg{chunks, (int)ceil_div(k - (int64_t)(chunks - 1) * kChunk, 16), a_z, b_z, id};
+}
+
+template <int CG, bool DRAIN, typename Epi>
+void launch(const CUtensorMap& A, const CUtensorMap& B, const CUtensorMap& LA, const CUtensorMap& LB, Args a,
+            const Epi& epi, cudaStream_t s) {
+  const int stage = kABytes + a.bn / CG * 128;
+  a.errors = error_counter();
+  if (!DRAIN) a.block = 1 << 30;
+  a.stages = std::min(8, (kSmem - 1024 - 512) / stage);
+  const int smem = 1024 + a.stages * stage + 512;
+  allow_smem(reinterpret_cast<const void*>(k_mma<CG, DRAIN, Epi>), kSmem);
+  const int64_t per = a.sym ? (int64_t)a.m_tiles * (a.m_tiles + 1) / 2 : (int64_t)a.m_tiles * a.n_tiles;
+  const int64_t tiles = per * a.batches;
+  LC_REQUIRE(tiles < (1LL << 31), LIPCACHE_E_INVALID, "too many tiles");
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(CG * std::min<int64_t>(tiles, num_sms() / CG)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = s;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CG;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CG == 2 ? 2 : 1;
+  LC_CUDA(cudaLaunchKernelEx(&cfg, k_mma<CG, DRAIN, Epi>, A, B, LA, LB, a, epi));
+  LC_LAUNCH_CHECK("k_mma");
+}
+
+}  // namespace mma
+}  // namespace ops
+}  // namespace lc
