@@ -121,6 +121,7 @@ struct Runs {
 // plane pairs, A rows of the run times B of the run's adapter.
 struct Low {
   Runs runs;
+  int from_a = 0;     // the rows' factor is A itself (no other segments; a run's first MMA overwrites)
   int G = 0;          // 0: no low-rank segments
   int chunks = 0, last = 0;
   int pairs = 0;
@@ -133,12 +134,20 @@ struct Args {
   int sym;  // tiles on or above the diagonal only (m_tiles == n_tiles in units of the wider side)
   int bn;   // columns of a tile
   int stages;
+  int a_rows;  // rows of A's box (K-major): 128, or fewer where the tile has no more
   int a_mn, b_mn, lb_mn;
   int nseg;
   int block;  // stages of each segment per block (DRAIN: all segments have the same stages)
   Seg seg[kMaxSegs];
   Low low;
+  const int* alt;              // nullable: where not 0, A is read by its second map
   unsigned long long* errors;  // expired waits, counted
+};
+
+// The operands' maps: A and what stands for it where *alt, B, the low-rank
+// segments' factors.
+struct Maps {
+  CUtensorMap a, a2, b, la, lb;
 };
 
 // Tile `t`: its first row and column (in tiles) and batch index.
@@ -179,9 +188,7 @@ __device__ __forceinline__ int first_run(const Runs& r, int n, int m0) {
 
 template <int CG, bool DRAIN, typename Epi>
 __global__ void __launch_bounds__(kThreads, 1)
-    k_mma(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-          const __grid_constant__ CUtensorMap tmLA, const __grid_constant__ CUtensorMap tmLB, const Args a,
-          const Epi epi) {
+    k_mma(const __grid_constant__ Maps maps, const Args a, const Epi epi) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const int b_bytes = a.bn / CG * 128, stage_bytes = kABytes + b_bytes;
@@ -211,8 +218,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     ptx::mbar_init(drain, 1);
     *abort_s = 0;
     ptx::fence_mbar_init();
-    ptx::tma_prefetch_desc(&tmA);
-    ptx::tma_prefetch_desc(&tmB);
+    ptx::tma_prefetch_desc(&maps.a);
+    ptx::tma_prefetch_desc(&maps.b);
   }
   if (warp == 1) {
     if (CG == 2) {
@@ -232,6 +239,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tmem_slot;
   const int per = a.sym ? a.m_tiles * (a.m_tiles + 1) / 2 : a.m_tiles * a.n_tiles;
   const int tiles = per * a.batches;
+  const int chunks = a.nseg ? a.seg[0].chunks : 0;
   const int n_runs = a.low.G ? __ldg(a.low.runs.count) : 0;
 
   if (warp == 0) {
@@ -241,12 +249,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       int st = 0;
       uint32_t ph = 0;
       bool ok = true;
+      const CUtensorMap* ma = a.alt && __ldg(a.alt) ? &maps.a2 : &maps.a;
+      const CUtensorMap* mla = a.low.from_a ? ma : &maps.la;
       // one stage: the boxes of A at (row, k) and of B at (column, k)
-      auto load = [&](const CUtensorMap* ma, bool a_mn, int row, int ak, int az, const CUtensorMap* mb, bool b_mn,
+      auto load = [&](const CUtensorMap* pa, bool a_mn, int row, int ak, int az, const CUtensorMap* pb, bool b_mn,
                       int col, int bk, int bz) {
         ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, kWaitLimit);
         if (!ok) return;
-        if (rank == 0) ptx::mbar_expect_tx(full + 8 * st, (uint32_t)(CG * stage_bytes));
+        if (rank == 0) ptx::mbar_expect_tx(full + 8 * st, (uint32_t)(CG * (a.a_rows * 128 + b_bytes)));
         const uint32_t sa = base + st * stage_bytes, sb = sa + kABytes, bar = lead_full + 8 * st;
         auto box = [&](uint32_t dst, const CUtensorMap* m, int x, int y, int z) {
           if (CG == 2)
@@ -255,15 +265,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             load_3d(dst, m, x, y, z, bar);
         };
         if (a_mn) {
-          box(sa, ma, row, ak, az);
-          box(sa + 8192, ma, row + 64, ak, az);
+          box(sa, pa, row, ak, az);
+          box(sa + 8192, pa, row + 64, ak, az);
         } else {
-          box(sa, ma, ak, row, az);
+          box(sa, pa, ak, row, az);
         }
         if (b_mn) {
-          for (int i = 0; i < a.bn / CG; i += 64) box(sb + i * 128, mb, col + i, bk, bz);
+          for (int i = 0; i < a.bn / CG; i += 64) box(sb + i * 128, pb, col + i, bk, bz);
         } else {
-          box(sb, mb, bk, col, bz);
+          box(sb, pb, bk, col, bz);
         }
         if (++st == nst) st = 0, ph ^= 1u;
       };
@@ -271,12 +281,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         int mt, nt, z;
         tile_at(a, t, mt, nt, z);
         const int row = mt * TM + (int)rank * 128, col = nt * a.bn + (int)rank * (a.bn / CG);
-        for (int c0 = 0; c0 < a.seg[0].chunks && ok; c0 += a.block)
+        for (int c0 = 0; c0 < chunks && ok; c0 += a.block)
           for (int s = 0; s < a.nseg && ok; ++s) {
             const Seg& sg = a.seg[s];
             const int c1 = min(c0 + a.block, sg.chunks);
             for (int c = c0; c < c1 && ok; ++c)
-              load(&tmA, a.a_mn, row, c * kChunk, sg.a_z + z, &tmB, a.b_mn, col, c * kChunk, sg.b_z + z);
+              load(ma, a.a_mn, row, c * kChunk, sg.a_z + z, &maps.b, a.b_mn, col, c * kChunk, sg.b_z + z);
           }
         if (n_runs) {
           const int m0 = mt * TM;
@@ -286,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (g < 0 || g >= a.low.G) continue;
             for (int q = 0; q < a.low.pairs && ok; ++q)
               for (int c = 0; c < a.low.chunks && ok; ++c)
-                load(&tmLA, false, row, c * kChunk, a.low.a_z[q], &tmLB, a.lb_mn, col, c * kChunk,
+                load(mla, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk,
                      a.low.b_z[q] * a.low.G + g);
           }
         }
@@ -331,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < steps; ++k, da += ia, db += ib) {
               if (off) {
                 const uint32_t o[8] = {off[0], off[1], off[2], off[3], off[4], off[5], off[6], off[7]};
-                mma_masked<CG>(d, da, db, id, 1u, o);
+                mma_masked<CG>(d, da, db, id, acc, o);
               } else {
                 mma<CG>(d, da, db, id, acc);
               }
@@ -344,9 +354,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           if (++st == nst) st = 0, ph ^= 1u;
         };
-        for (int c0 = 0; c0 < a.seg[0].chunks && ok; c0 += a.block) {
-          if (c0) close();
-          open();
+        open();
+        for (int c0 = 0; c0 < chunks && ok; c0 += a.block) {
+          if (c0) {
+            close();
+            open();
+          }
           for (int s = 0; s < a.nseg && ok; ++s) {
             const Seg& sg = a.seg[s];
             const int c1 = min(c0 + a.block, sg.chunks);
@@ -368,6 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const uint32_t on = (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~(lo == 32 ? 0xffffffffu : (1u << lo) - 1u);
               off[w] = ~on;
             }
+            if (a.low.from_a) acc = 0;
             for (int q = 0; q < a.low.pairs && ok; ++q)
               for (int c = 0; c < a.low.chunks && ok; ++c)
                 chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, off);
@@ -421,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < kParts; ++i)
 #pragma unroll
           for (int j = 0; j < 32; ++j) sum[i][j] = 0.f;
-        for (int c0 = 0; c0 < a.seg[0].chunks; c0 += a.block) {
+        for (int c0 = 0; c0 < max(chunks, 1); c0 += a.block) {
           open();
           if (!ok) break;
 #pragma unroll
@@ -501,8 +515,7 @@ inline Seg segment(int64_t k, int a_z, int b_z, uint32_t id) {
 }
 
 template <int CG, bool DRAIN, typename Epi>
-void launch(const CUtensorMap& A, const CUtensorMap& B, const CUtensorMap& LA, const CUtensorMap& LB, Args a,
-            const Epi& epi, cudaStream_t s) {
+void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
   const int stage = kABytes + a.bn / CG * 128;
   a.errors = error_counter();
   if (!DRAIN) a.block = 1 << 30;
@@ -526,7 +539,7 @@ void launch(const CUtensorMap& A, const CUtensorMap& B, const CUtensorMap& LA, c
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CG == 2 ? 2 : 1;
-  LC_CUDA(cudaLaunchKernelEx(&cfg, k_mma<CG, DRAIN, Epi>, A, B, LA, LB, a, epi));
+  LC_CUDA(cudaLaunchKernelEx(&cfg, k_mma<CG, DRAIN, Epi>, maps, a, epi));
   LC_LAUNCH_CHECK("k_mma");
 }
 

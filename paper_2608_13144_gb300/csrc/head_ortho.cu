@@ -354,6 +354,7 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
   a.n_tiles = (int)ceil_div(N, a.bn);
   a.sym = sym;
   a.block = kBlock;
+  a.a_rows = 128;
   const uint32_t id = mma::idesc(tm, a.bn, false, a_mn, b_mn);
   if (PLANES == 2) {
     a.seg[a.nseg++] = mma::segment(K, 0, batch, id);
@@ -363,23 +364,9 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
   const CUtensorMap ma = mma::tensor_map(A, a_mn ? 64 : 128);
   const CUtensorMap mb = mma::tensor_map(B, b_mn ? 64 : pair ? 128 : a.bn);
   if (pair)
-    mma::launch<2, PLANES == 2>(ma, mb, ma, mb, a, epi, s);
+    mma::launch<2, PLANES == 2>({ma, ma, mb, ma, mb}, a, epi, s);
   else
-    mma::launch<1, PLANES == 2>(ma, mb, ma, mb, a, epi, s);
-}
-
-template <typename K, typename... Args>
-void launch_pdl(K kernel, dim3 grid, cudaStream_t s, Args... args) {
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  LC_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+    mma::launch<1, PLANES == 2>({ma, ma, mb, ma, mb}, a, epi, s);
 }
 
 template <typename T, int VEC, int PLANES>
@@ -387,10 +374,10 @@ void normalise(const T* g, Direction a, int64_t batch, double eps, const OrthoLa
   a.units = a.cols / VEC;
   const int64_t n = (int64_t)a.rows * a.units;
   const unsigned parts = (unsigned)std::min<int64_t>(kParts, ceil_div(n, 256));
-  launch_pdl(k_squares<T, VEC>, dim3(parts, (unsigned)batch), s, g, a, l.part);
+  launch_pdl(k_squares<T, VEC>, dim3(parts, (unsigned)batch), 256, s, g, a, l.part);
   LC_LAUNCH_CHECK("k_squares");
   const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div(n, 512), 1024);
-  launch_pdl(k_planes<T, VEC, PLANES>, dim3(blocks, (unsigned)batch), s, g, a, (const double*)l.part, (int)parts, eps,
+  launch_pdl(k_planes<T, VEC, PLANES>, dim3(blocks, (unsigned)batch), 256, s, g, a, (const double*)l.part, (int)parts, eps,
              l.x[0], l.ld, batch * l.x_plane, l.t);
   LC_LAUNCH_CHECK("k_planes");
 }

@@ -34,8 +34,25 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) {
 }
 
 inline size_t elem(int type) { return type == LIPCACHE_F32 ? 4 : 2; }
+__device__ __forceinline__ int64_t ceil_div_dev(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+// A launch that may begin while the kernel before it ends; `kernel` waits for
+// that one's results itself (griddepcontrol.wait).
+template <typename K, typename... Args>
+void launch_pdl(K kernel, dim3 grid, int threads, cudaStream_t s, Args... args) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = s;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  LC_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+}
 
 // ---------------------------------------------------------------- launchers
 // head_adapt.cu
