@@ -814,7 +814,7 @@ struct Op {
           tc{a.c, l.ld_u, p.tokens, 2, l.ld_u, a.plane};
       const CUtensorMap m1 = mma::tensor_map(ti, 64), m2 = mma::tensor_map(ts, 64), mc = mma::tensor_map(tc, 64);
       const int smem = 1024 + 4 * (16384 + a.rb * 256) + 128;
-      mma::allow_smem(reinterpret_cast<const void*>(k_outer), 1024 + 4 * (16384 + 128 * 256) + 128);
+      allow_smem(reinterpret_cast<const void*>(k_outer), 1024 + 4 * (16384 + 128 * 256) + 128);
       cudaLaunchAttribute attr;
       attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
       attr.val.programmaticStreamSerializationAllowed = 1;

@@ -17,6 +17,18 @@ uint64_t operator_errors(cudaStream_t s) {
   return n;
 }
 
+void allow_smem(const void* kernel, int bytes) {
+  static std::mutex mu;
+  static std::set<std::pair<int, const void*>> done;
+  int dev = 0;
+  LC_CUDA(cudaGetDevice(&dev));
+  std::lock_guard<std::mutex> lock(mu);
+  if (!done.insert({dev, kernel}).second) return;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) done.erase({dev, kernel});
+  LC_CUDA(e);
+}
+
 namespace mma {
 
 EncodeTiledFn encoder() {
@@ -28,18 +40,6 @@ EncodeTiledFn encoder() {
   }();
   LC_REQUIRE(fn != nullptr, LIPCACHE_E_CUDA, "cuTensorMapEncodeTiled is unavailable from the driver");
   return fn;
-}
-
-void allow_smem(const void* kernel, int bytes) {
-  static std::mutex mu;
-  static std::set<std::pair<int, const void*>> done;
-  int dev = 0;
-  LC_CUDA(cudaGetDevice(&dev));
-  std::lock_guard<std::mutex> lock(mu);
-  if (!done.insert({dev, kernel}).second) return;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e != cudaSuccess) done.erase({dev, kernel});
-  LC_CUDA(e);
 }
 
 int num_sms() {

@@ -493,8 +493,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---------------------------------------------------------------- host side
 EncodeTiledFn encoder();
-// Lets `kernel` use `bytes` of dynamic shared memory on the current device.
-void allow_smem(const void* kernel, int bytes);
 int num_sms();
 // The current device's counter of expired waits.
 unsigned long long* error_counter();

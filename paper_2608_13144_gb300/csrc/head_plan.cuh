@@ -233,7 +233,7 @@ inline void make_plan(const int32_t* adapter, int64_t tokens, int G, const Plan&
   const int warps = G + 1 <= 1024 ? 32 : 8;
   const int ctas = tokens <= 2048 ? 1 : 8;
   const int smem = (warps + 1) * (G + 1) * 4;
-  mma::allow_smem(reinterpret_cast<const void*>(k_plan), 200 * 1024);
+  allow_smem(reinterpret_cast<const void*>(k_plan), 200 * 1024);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;

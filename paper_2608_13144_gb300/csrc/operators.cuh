@@ -41,18 +41,26 @@ inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 // A launch that may begin while the kernel before it ends; `kernel` waits for
 // that one's results itself (griddepcontrol.wait).
 template <typename K, typename... Args>
-void launch_pdl(K kernel, dim3 grid, int threads, cudaStream_t s, Args... args) {
+void launch_pdl_smem(K kernel, dim3 grid, int threads, int smem, cudaStream_t s, Args... args) {
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   LC_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
+template <typename K, typename... Args>
+void launch_pdl(K kernel, dim3 grid, int threads, cudaStream_t s, Args... args) {
+  launch_pdl_smem(kernel, grid, threads, 0, s, args...);
+}
+// head_mma.cu: lets `kernel` use `bytes` of dynamic shared memory on the
+// current device.
+void allow_smem(const void* kernel, int bytes);
 
 // ---------------------------------------------------------------- launchers
 // head_adapt.cu
