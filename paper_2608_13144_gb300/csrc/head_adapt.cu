@@ -4,21 +4,26 @@
 //   v_t = s_g B_g^T dy_t,  dx_t = W^T dy_t + A_g^T v_t
 //   dA_g = sum v_t x_t^T,  dB_g = sum dy_t u_t^T
 //
-// The shared product and the low-rank one of a tile are one sum in tensor
-// memory: after the stages of W come, for each run of rows in the tile with
-// the same adapter (head_plan.cuh), the few stages of that adapter's factor,
-// limited to the run's rows by the MMA's lane mask. u and v are kept to 16 bits
-// of mantissa or more (BF16 operands: two BF16 planes, hi + lo; FP32: three),
-// so the split costs less than the operands' own rounding.
+// Rows stay where they stand, in any order of adapters.
+// - The shared product runs on the tensor cores (head_mma.cuh). BF16: a tile
+//   with few adapters among its rows takes the low-rank product into the same
+//   sum, each adapter's few stages limited to its rows by the MMA's lane mask;
+//   a tile with many, and any FP32 tile, adds it in the epilogue, a thread a
+//   row, from u in FP32.
+// - u and v (shrink): BF16 on the tensor cores with the same lane masks, the
+//   rows loaded once for all adapters of a tile; FP32 a warp a row.
+// - dA and dB: the rows of an adapter, listed by the CTA that sums them, are
+//   gathered row by row, so that no other adapter's row is touched.
+// On the tensor cores u and v are two BF16 planes, hi + lo (16 bits): their
+// rounding stays below that of the operands.
 //
 // FP32 rows become two FP16 planes under a power of two of each row's own (rows
-// of W likewise), undone in the epilogue; u is divided by its row's before it
-// is split, and the factors of W's rows are folded into dy where W is
-// contracted over them, so each output keeps its precision relative to its own
-// terms. A few FP32 rows go through the CUDA cores instead.
+// of W likewise), undone in the epilogue; where W is contracted over its rows,
+// their powers are folded into dy: each output keeps its precision relative to
+// its own terms. A few rows go through the CUDA cores instead.
 #include <cuda_fp16.h>
 
-#include "head_plan.cuh"
+#include "head_mma.cuh"
 
 namespace lc {
 namespace ops {
@@ -29,213 +34,421 @@ typedef __nv_bfloat16 bf16;
 
 constexpr int kBlock = 4;  // stages of 64 the tensor cores sum before the sum is drained, FP32
 
-// ---------------------------------------------------------------- staging
-// The place's row of the input: `perm` where the plan sorted.
-__device__ __forceinline__ int64_t row_at(const int* flags, const int* perm, int64_t p) {
-  return flags && __ldg(flags + 1) ? (int64_t)__ldg(perm + p) : p;
-}
-
-struct Stage {
-  int64_t rows, ld;     // of the input
-  int cols;
-  const int* flags;     // nullable: rows in their own order
-  const int* perm;
-  int only_sorted;      // nothing to do where rows keep their order
-  const float* fold;    // FP32, nullable: a factor of each column
-  int64_t ldo, plane;
-  float* undo;          // FP32: what undoes each row's power of two
-  int most;             // the largest power used
-};
-
-// A warp a row. BF16 rows are copied, FP32 rows scaled and split.
-template <typename T>
-__global__ void __launch_bounds__(256) k_stage(const T* in, const Stage a, uint16_t* out) {
-  ptx::wait_prerequisites();
-  ptx::launch_dependents();
-  if (a.only_sorted && !__ldg(a.flags + 1)) return;
-  const int lane = threadIdx.x & 31;
-  for (int64_t p = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); p < a.rows; p += (int64_t)gridDim.x * 8) {
-    const T* r = in + row_at(a.flags, a.perm, p) * a.ld;
-    uint16_t* o = out + p * a.ldo;
-    if constexpr (sizeof(T) == 2) {
-      const uint16_t* w = reinterpret_cast<const uint16_t*>(r);
-      if ((((uintptr_t)w | (uintptr_t)(a.cols * 2)) & 15) == 0) {
-        for (int i = lane; i < a.cols / 8; i += 32) reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(w)[i];
-      } else {
-        for (int i = lane; i < a.cols; i += 32) o[i] = w[i];
-      }
-    } else {
-      auto value = [&](int i) { return a.fold ? to_f32<T>(r[i]) * __ldg(a.fold + i) : to_f32<T>(r[i]); };
-      float top = 0.f;
-      for (int i = lane; i < a.cols; i += 32) top = fmaxf(top, fabsf(value(i)));
-#pragma unroll
-      for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-      // the largest element lands in [2^14, 2^15)
-      int k = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-      k = max(-a.most, min(a.most, k));
-      const float f = ldexpf(1.f, k);
-      for (int i = lane; i < a.cols; i += 32) {
-        const float v = value(i) * f;
-        const __half hi = __float2half_rn(v), lo = __float2half_rn(v - __half2float(hi));
-        o[i] = __half_as_ushort(hi);
-        o[a.plane + i] = __half_as_ushort(lo);
-      }
-      if (lane == 0) a.undo[p] = ldexpf(1.f, -k);
-    }
-  }
-}
-
-// An adapter factor in rows of ldo: BF16 copied, FP32 (over its row's power of
-// two, nullable, one for `div_rows` rows in turn) as three BF16 planes.
-template <typename T>
+// ---------------------------------------------------------------- copies
+// A BF16 matrix whose rows TMA cannot read, in rows of ldo.
 __global__ void __launch_bounds__(256)
-    k_factor(const T* in, int64_t rows, int cols, int64_t ldo, int64_t plane, const float* undo, int div_rows,
-             uint16_t* out) {
+    k_copy_rows(const bf16* in, int64_t ld, int64_t rows, int cols, bf16* out, int64_t ldo) {
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int64_t n = rows * cols;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / cols;
-    uint16_t* o = out + r * ldo + (i - r * cols);
-    if constexpr (sizeof(T) == 2) {
-      *o = reinterpret_cast<const uint16_t*>(in)[i];
-    } else {
-      float v = in[i];
-      if (undo) v /= __ldg(undo + r % div_rows);  // a power of two
-#pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        const bf16 h = __float2bfloat16_rn(v);
-        o[q * plane] = __bfloat16_as_ushort(h);
-        v -= __bfloat162float(h);
-      }
-    }
-  }
+  const int lane = threadIdx.x & 31;
+  for (int64_t p = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); p < rows; p += (int64_t)gridDim.x * 8)
+    for (int i = lane; i < cols; i += 32) out[p * ldo + i] = in[p * ld + i];
 }
 
-// ---------------------------------------------------------------- shrink
-struct Shrink {
-  int64_t tokens, ld;
-  int width, r, G;
-  const int* flags;     // nullable, with perm: the plan's order
-  const int* perm;
+// ---------------------------------------------------------------- FP32 rows
+// A warp a row: its planes, and its low-rank product u (or v).
+struct RowJob {
+  const float* in = nullptr;
+  int64_t ld = 0, rows = 0;
+  int width = 0, vec = 0;       // vec: rows can be read 16 bytes at a time
+  const float* fold = nullptr;  // a factor of each column, in the planes only
+  __half* planes = nullptr;     // nullable
+  int64_t ldo = 0, plane = 0;
+  float* undo = nullptr;        // what undoes each row's power of two
+  int most = 0;                 // the largest power used
+  const float* F = nullptr;     // nullable: the factor
+  int64_t f_g = 0, f_j = 0, f_i = 0;
+  int f_vec = 0;                // factor and row can be read so together
+  float* u = nullptr;           // rows x r
+};
+struct RowJobs {
+  RowJob job[2];
   const int32_t* adapter;
   const float* scales;
-  int64_t f_g, f_j, f_i;  // strides of the factor
-  float* out;             // nullable: tokens x r
-  uint16_t* planes;       // nullable: BF16 planes of tokens x ldo
-  int64_t ldo, plane;
-  int n_planes;
-  const float* undo;      // nullable: over each row's power of two in the planes
+  int G, r;
 };
 
-// Four values' worth of rows a warp, eight columns at a time: the sums of 32
-// (row, j) pairs end on 32 lanes.
-template <typename T>
-__global__ void __launch_bounds__(128) k_shrink(const T* in, const T* F, const Shrink a) {
-  ptx::wait_prerequisites();
-  ptx::launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const int64_t p0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 5)) * 4;
-  if (p0 >= a.tokens) return;
-  const int j0 = blockIdx.y * 8, nj = min(8, a.r - j0);
-  const T* x[4];
-  int g[4];
+// Sums of eight values over a warp: lane l ends with the sum of value l & 7.
+__device__ __forceinline__ float sum8(float (&v)[8], int lane) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int64_t p = p0 + k;
-    const int64_t t = p < a.tokens ? row_at(a.flags, a.perm, p) : 0;
-    const int id = p < a.tokens ? __ldg(a.adapter + t) : -1;
-    g[k] = id >= 0 && id < a.G ? id : -1;
-    x[k] = in + t * a.ld;
-  }
-  float acc[32];
-#pragma unroll
-  for (int k = 0; k < 32; ++k) acc[k] = 0.f;
-  bool done[4] = {g[0] < 0, g[1] < 0, g[2] < 0, g[3] < 0};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (done[k]) continue;
-    bool in_g[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      in_g[q] = !done[q] && g[q] == g[k];
-      done[q] |= in_g[q];
-    }
-    const T* f = F + g[k] * a.f_g + j0 * a.f_j;
-#pragma unroll 2
-    for (int i = lane; i < a.width; i += 32) {
-      float xv[4], fv[8];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) xv[q] = in_g[q] ? to_f32<T>(x[q][i]) : 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) fv[j] = j < nj ? to_f32<T>(f[j * a.f_j + i * a.f_i]) : 0.f;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (in_g[q]) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[q * 8 + j] = fmaf(xv[q], fv[j], acc[q * 8 + j]);
-        }
-    }
-  }
-  // halve the values and double the lanes that share one, five times
-#pragma unroll
-  for (int s = 16; s > 0; s >>= 1) {
+  for (int s = 4; s > 0; s >>= 1) {
     const bool up = lane & s;
 #pragma unroll
     for (int k = 0; k < s; ++k) {
-      const float keep = up ? acc[k + s] : acc[k], give = up ? acc[k] : acc[k + s];
-      acc[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
+      const float keep = up ? v[k + s] : v[k], give = up ? v[k] : v[k + s];
+      v[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
     }
   }
-  const int q = lane >> 3, j = j0 + (lane & 7);
-  const int64_t p = p0 + q;
-  if (p >= a.tokens) return;
-  const int id = q == 0 ? g[0] : q == 1 ? g[1] : q == 2 ? g[2] : g[3];
-  float v = acc[0];
-  if (id < 0) v = 0.f;
-  else if (a.scales) v *= __ldg(a.scales + id);
-  if (a.out && j < a.r) a.out[p * a.r + j] = v;
-  if (a.planes && j < a.ldo) {
-    if (j >= a.r) v = 0.f;
-    if (a.undo) v /= __ldg(a.undo + p);
-    uint16_t* o = a.planes + p * a.ldo + j;
-    for (int k = 0; k < a.n_planes; ++k) {
-      const bf16 h = __float2bfloat16_rn(v);
-      o[k * a.plane] = __bfloat16_as_ushort(h);
-      v -= __bfloat162float(h);
+  float r = v[0];
+  r += __shfl_xor_sync(0xffffffffu, r, 8);
+  return r + __shfl_xor_sync(0xffffffffu, r, 16);
+}
+
+template <int VEC>
+__device__ __forceinline__ void row_planes(const RowJob& a, const float* r, int64_t row, int lane) {
+  auto get = [&](int i, float (&v)[VEC]) {
+    if (VEC == 4) {
+      const float4 q = *reinterpret_cast<const float4*>(r + i);
+      v[0] = q.x, v[1 % VEC] = q.y, v[2 % VEC] = q.z, v[3 % VEC] = q.w;
+    } else {
+      v[0] = r[i];
+    }
+    if (a.fold) {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) v[k] *= __ldg(a.fold + i + k);
+    }
+  };
+  float top = 0.f;
+  for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
+    float v[VEC];
+    get(i, v);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) top = fmaxf(top, fabsf(v[k]));
+  }
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  // the largest element lands in [2^14, 2^15)
+  int e = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
+  e = max(-a.most, min(a.most, e));
+  const float f = ldexpf(1.f, e);
+  __half* o = a.planes + row * a.ldo;
+  for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
+    float v[VEC];
+    get(i, v);
+    __align__(8) __half hi[VEC], lo[VEC];
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      v[k] *= f;
+      hi[k] = __float2half_rn(v[k]);
+      lo[k] = __float2half_rn(v[k] - __half2float(hi[k]));
+    }
+    if (VEC == 4) {
+      *reinterpret_cast<uint2*>(o + i) = *reinterpret_cast<uint2*>(hi);
+      *reinterpret_cast<uint2*>(o + a.plane + i) = *reinterpret_cast<uint2*>(lo);
+    } else {
+      o[i] = hi[0];
+      o[a.plane + i] = lo[0];
+    }
+  }
+  if (lane == 0) a.undo[row] = ldexpf(1.f, -e);
+}
+
+__global__ void __launch_bounds__(256) k_rows_f32(const RowJobs jobs) {
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int64_t all = jobs.job[0].rows + jobs.job[1].rows;
+  for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < all; w += (int64_t)gridDim.x * 8) {
+    const bool second = w >= jobs.job[0].rows;
+    const RowJob& a = jobs.job[second];
+    const int64_t row = second ? w - jobs.job[0].rows : w;
+    const float* r = a.in + row * a.ld;
+    if (a.planes) {
+      if (a.vec)
+        row_planes<4>(a, r, row, lane);
+      else
+        row_planes<1>(a, r, row, lane);
+    }
+    if (!a.F) continue;
+    const int g = __ldg(jobs.adapter + row);
+    const bool any = g >= 0 && g < jobs.G;
+    const float s = any && jobs.scales ? __ldg(jobs.scales + g) : 1.f;
+    for (int j0 = 0; j0 < jobs.r; j0 += 8) {
+      const int nj = min(8, jobs.r - j0);
+      float acc[8] = {};
+      if (any) {
+        const float* F = a.F + g * a.f_g + j0 * a.f_j;
+        if (nj == 8 && a.f_vec) {
+          for (int i = lane * 4; i < a.width; i += 128) {
+            const float4 x = *reinterpret_cast<const float4*>(r + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float4 f = __ldg(reinterpret_cast<const float4*>(F + j * a.f_j + i));
+              acc[j] = fmaf(x.x, f.x, fmaf(x.y, f.y, fmaf(x.z, f.z, fmaf(x.w, f.w, acc[j]))));
+            }
+          }
+        } else {
+#pragma unroll 4
+          for (int i = lane; i < a.width; i += 32) {
+            const float x = r[i];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (j < nj) acc[j] = fmaf(x, __ldg(F + j * a.f_j + i * a.f_i), acc[j]);
+          }
+        }
+      }
+      const float v = sum8(acc, lane);
+      if (lane < nj) a.u[row * jobs.r + j0 + lane] = any ? s * v : 0.f;
     }
   }
 }
 
-// The same product on the tensor cores (BF16): two planes.
-struct ShrinkEpi {
-  uint16_t* planes;
-  const int* row_g;
-  const float* scales;
-  int64_t ldo, plane, tokens;
-  int G;
-  __device__ __forceinline__ void store(int row0, int col0, int, int lane, const uint32_t (&acc)[32]) const {
-    const int64_t row = row0 + lane;
-    if (row >= tokens || col0 >= ldo) return;
-    const int g = __ldg(row_g + row);
-    const float s = g >= G ? 0.f : scales ? __ldg(scales + g) : 1.f;
-    uint16_t* o = planes + row * ldo + col0;
+// ---------------------------------------------------------------- shrink, few rows
+// u of one row (blockIdx.x), eight columns (blockIdx.y) in FP32.
+template <typename T>
+__global__ void __launch_bounds__(128)
+    k_shrink_few(const T* x, int64_t ldx, int width, const T* A, int vec, int G, int r, const int32_t* adapter,
+                 const float* scales, float* u) {
+  __shared__ float red[4][8];
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const int64_t t = blockIdx.x;
+  const int j0 = blockIdx.y * 8, nj = min(8, r - j0), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int g = __ldg(adapter + t);
+  const bool any = g >= 0 && g < G;
+  float acc[8] = {};
+  if (any) {
+    const T* row = x + t * ldx;
+    const T* F = A + ((int64_t)g * r + j0) * width;
+    constexpr int N = 16 / sizeof(T);
+    auto dot = [](const uint4& p, const uint4& q, float s) {
+      const uint32_t a[4] = {p.x, p.y, p.z, p.w}, b[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (col0 + q * 8 >= ldo) break;
-      uint16_t hi[8], lo[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float v = g >= G ? 0.f : s * __uint_as_float(acc[q * 8 + j]);
-        const bf16 h = __float2bfloat16_rn(v);
-        hi[j] = __bfloat16_as_ushort(h);
-        lo[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v - __bfloat162float(h)));
+      for (int k = 0; k < 4; ++k) {
+        if (sizeof(T) == 4) {
+          s = fmaf(__uint_as_float(a[k]), __uint_as_float(b[k]), s);
+        } else {
+          s = fmaf(__uint_as_float(a[k] << 16), __uint_as_float(b[k] << 16), s);
+          s = fmaf(__uint_as_float(a[k] & 0xffff0000u), __uint_as_float(b[k] & 0xffff0000u), s);
+        }
       }
-      *reinterpret_cast<uint4*>(o + q * 8) = *reinterpret_cast<uint4*>(hi);
-      *reinterpret_cast<uint4*>(o + plane + q * 8) = *reinterpret_cast<uint4*>(lo);
+      return s;
+    };
+    if (vec) {
+      for (int i = threadIdx.x * N; i < width; i += 128 * N) {
+        const uint4 xv = *reinterpret_cast<const uint4*>(row + i);
+        uint4 f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < nj) f[j] = __ldg(reinterpret_cast<const uint4*>(F + (int64_t)j * width + i));
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < nj) acc[j] = dot(xv, f[j], acc[j]);
+      }
+    } else {
+#pragma unroll 2
+      for (int i = threadIdx.x; i < width; i += 128) {
+        const float xv = to_f32<T>(row[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < nj) acc[j] = fmaf(xv, to_f32<T>(F[(int64_t)j * width + i]), acc[j]);
+      }
     }
   }
+  const float v = sum8(acc, lane);
+  if (lane < 8) red[warp][lane] = v;
+  __syncthreads();
+  if (threadIdx.x < nj) {
+    const int k = threadIdx.x;
+    const float s = ((red[0][k] + red[1][k]) + red[2][k]) + red[3][k];
+    u[t * r + j0 + k] = any ? (scales ? __ldg(scales + g) * s : s) : 0.f;
+  }
+}
+
+// ---------------------------------------------------------------- shrink, tensor cores
+// u of 128 rows: D[row, j] of each row's own adapter, the adapters of the tile
+// in groups whose factors share a stage with the rows. A cluster splits the
+// contracted width; its first CTA joins the parts in order. Bound by reading
+// the rows once.
+constexpr int kShrinkThreads = 192, kShrinkStages = 4, kShrinkStage = 48 * 1024;
+struct ShrinkJob {
+  CUtensorMap rows, factor;
+  int chunks, last;
+  int f_mn;       // the factor's contracted index is not its innermost
+  int f_bytes;    // of a factor's part of a stage
+  int per;        // factors in a stage
+  uint32_t idesc;
+  float* u;       // tokens x r
+  uint16_t* planes;
 };
+struct ShrinkJobs {
+  ShrinkJob job[2];
+  const int32_t* adapter;
+  const float* scales;
+  int64_t tokens, ldo, plane;
+  int G, r, rn;   // rn: r up to a multiple of 16, the columns of D
+  unsigned long long* errors;
+};
+
+__device__ __forceinline__ void store_cluster(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+__global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_constant__ ShrinkJobs a) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  float* part = reinterpret_cast<float*>(smem_raw + (base - ptx::smem_u32(smem_raw)));
+  const uint32_t full = base + kShrinkStages * kShrinkStage, empty = full + 8 * kShrinkStages,
+                 done = empty + 8 * kShrinkStages, misc = done + 8;
+  unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
+  volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
+  volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const ShrinkJob& job = a.job[blockIdx.z];
+  uint32_t splits;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(splits));
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int64_t m0 = (int64_t)(blockIdx.x / splits) * 128;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kShrinkStages; ++s) {
+      ptx::mbar_init(full + 8 * s, 1);
+      ptx::mbar_init(empty + 8 * s, 1);
+    }
+    ptx::mbar_init(done, 1);
+    *abort_s = 0;
+    ptx::fence_mbar_init();
+    ptx::tma_prefetch_desc(&job.rows);
+    ptx::tma_prefetch_desc(&job.factor);
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(misc, 128);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const uint32_t tmem = *tmem_slot;
+  const int c0 = (int)((int64_t)job.chunks * rank / splits), c1 = (int)((int64_t)job.chunks * (rank + 1) / splits);
+  if (warp <= 1) {
+    // producer and issuer walk the same groups of adapters and chunks
+    mma::Groups<128> gr;
+    gr.begin(a.adapter, a.tokens, a.G, m0, lane);
+    const bool lead = ptx::elect_one();
+    int st = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (;;) {
+      int g[8], n = 0;
+      uint32_t off[8][4];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (k >= job.per || n < k || !gr.next()) continue;
+        g[k] = gr.g;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) off[k][w] = ~gr.on[w];
+        n = k + 1;
+      }
+      if (n == 0 || !ok) break;
+      for (int c = c0; c < c1 && ok; ++c) {
+        if (warp == 0) {
+          ok = ptx::mbar_wait_warp(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
+          if (!ok) break;
+          if (lane == 0) {
+            const uint32_t sa = base + st * kShrinkStage, bar = full + 8 * st;
+            ptx::mbar_expect_tx(bar, (uint32_t)(16384 + n * job.f_bytes));
+            mma::load_3d(sa, &job.rows, c * 64, (int)m0, 0, bar);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              if (k >= n) break;
+              const uint32_t sb = sa + 16384 + k * job.f_bytes;
+              if (job.f_mn)
+                for (int j = 0; j * 8192 < job.f_bytes; ++j) mma::load_3d(sb + j * 8192, &job.factor, j * 64, c * 64, g[k], bar);
+              else
+                mma::load_3d(sb, &job.factor, c * 64, 0, g[k], bar);
+            }
+          }
+        } else {
+          ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, mma::kWaitLimit);
+          if (!ok) break;
+          ptx::tc_fence_after();
+          if (lead) {
+            const uint32_t sa = base + st * kShrinkStage;
+            const int steps = c == job.chunks - 1 ? job.last : 4;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              if (k >= n) break;
+              uint64_t da = mma::desc(sa, false), db = mma::desc(sa + 16384 + k * job.f_bytes, job.f_mn);
+              const uint32_t o[8] = {off[k][0], off[k][1], off[k][2], off[k][3], 0, 0, 0, 0};
+              for (int q = 0; q < steps; ++q, da += 32 >> 4, db += job.f_mn ? 2048 >> 4 : 32 >> 4)
+                mma::mma_masked<1>(tmem, da, db, job.idesc, c > c0 || q > 0, o);
+            }
+            ptx::mma_commit(empty + 8 * st);
+          }
+        }
+        if (++st == kShrinkStages) st = 0, ph ^= 1u;
+      }
+    }
+    if (warp == 1) {
+      if (lead) {
+        volatile int never = 0;
+        ptx::mma_commit(done);
+        ptx::mbar_wait(done, 0, &never, mma::kWaitLimit);
+      }
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+  bool ok = true;
+  if (warp >= 2) {
+    ok = ptx::mbar_wait(done, 0, abort_s, mma::kWaitLimit);
+    ok = __all_sync(0xffffffffu, ok);
+    ptx::tc_fence_after();
+  }
+  const int row = (warp & 3) * 32 + lane;
+  const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  if (splits > 1) {
+    // the first CTA's stages are free: its products are done
+    ptx::cluster_sync();
+    if (warp >= 2 && rank > 0) {
+      const uint32_t dst = ptx::mapa(base, 0) + (uint32_t)((rank - 1) * 128 * a.rn) * 4;
+      for (int j0 = 0; j0 < a.rn; j0 += 32) {
+        uint32_t v[32];
+        ptx::tmem_ld32(src + j0, v);
+        ptx::tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j0 + j < a.rn) store_cluster(dst + (uint32_t)((j0 + j) * 128 + row) * 4, __uint_as_float(v[j]));
+      }
+    }
+    ptx::cluster_sync();
+  }
+  if (warp >= 2 && rank == 0 && ok) {
+    const int64_t t = m0 + row;
+    const int id = t < a.tokens ? __ldg(a.adapter + t) : -1;
+    const bool any = id >= 0 && id < a.G;
+    const float s = any && a.scales ? __ldg(a.scales + id) : 1.f;
+    for (int j0 = 0; j0 < a.rn; j0 += 32) {
+      uint32_t v[32];
+      ptx::tmem_ld32(src + j0, v);
+      ptx::tmem_wait_ld();
+      if (t >= a.tokens) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        __align__(16) uint16_t hi[8], lo[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int j = j0 + q * 8 + k;
+          float f = __uint_as_float(v[q * 8 + k]);
+          if (j < a.rn)
+            for (uint32_t p = 1; p < splits; ++p) f += part[((p - 1) * a.rn + j) * 128 + row];
+          f = any && j < a.r ? s * f : 0.f;
+          if (j < a.r) job.u[t * a.r + j] = f;
+          const bf16 h = __float2bfloat16_rn(f);
+          hi[k] = __bfloat16_as_ushort(h);
+          lo[k] = __bfloat16_as_ushort(__float2bfloat16_rn(f - __bfloat162float(h)));
+        }
+        if (j0 + q * 8 < a.ldo) {
+          uint16_t* o = job.planes + t * a.ldo + j0 + q * 8;
+          *reinterpret_cast<uint4*>(o) = *reinterpret_cast<uint4*>(hi);
+          *reinterpret_cast<uint4*>(o + a.plane) = *reinterpret_cast<uint4*>(lo);
+        }
+      }
+    }
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (*abort_s) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1LL << 23)) {
+    }
+    if (threadIdx.x == 0) atomicAdd(a.errors, 1ull);
+    __syncthreads();
+  }
+  ptx::tc_fence_after();
+  if (warp == 1) ptx::tmem_dealloc(tmem, 128);
+}
 
 // ---------------------------------------------------------------- shared product
 template <typename T>
@@ -244,37 +457,83 @@ struct AdaptEpi {
   int64_t ldy, rows;
   int cols, vec;
   const float *bias, *undo_row, *undo_col;  // nullable
-  const int *flags, *perm;                  // nullable
-  // few rows: the low-rank product here, from FP32 u (B: G x cols x r)
+  // the low-rank product: u (tokens x r) times the factor of cols x r
+  // (f_col = r, f_j = 1) or r x cols (1, cols)
   const float* u;
-  const T* B;
+  const T* F;
   const int32_t* adapter;
-  int G, r;
-  __device__ __forceinline__ void store(int row0, int col0, int, int lane, const uint32_t (&acc)[32]) const {
-    const int left = cols - col0;
-    const int64_t p = row0 + lane;
-    if (left <= 0 || p >= rows) return;
-    float v[32];
-    const float f = undo_row ? __ldg(undo_row + p) : 1.f;
+  int G, r, f_vec, always;
+  int64_t f_col, f_j;
+
+  __device__ __forceinline__ void low(int64_t p, int col0, int left, float (&v)[32]) const {
+    constexpr int N = 16 / sizeof(T);
+    const int g = __ldg(adapter + p);
+    if (g < 0 || g >= G) return;
+    const T* f = F + (int64_t)g * cols * r + col0 * f_col;
+    const float* up = u + p * r;
+    if (f_vec && f_j == 1) {
+      for (int k = 0; k < r; k += N) {
+        float uk[N];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      v[j] = __uint_as_float(acc[j]) * f;
-      if (undo_col && j < left) v[j] *= __ldg(undo_col + col0 + j);
-      if (bias && j < left) v[j] += __ldg(bias + col0 + j);
-    }
-    if (u) {
-      const int g = __ldg(adapter + p);
-      if (g >= 0 && g < G) {
-        const T* b = B + ((int64_t)g * cols + col0) * r;
-        for (int k = 0; k < r; ++k) {
-          const float uk = __ldg(u + p * r + k);
+        for (int i = 0; i < N; ++i) uk[i] = __ldg(up + k + i);
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (j < left) v[j] = fmaf(uk, to_f32<T>(b[j * r + k]), v[j]);
+        for (int j = 0; j < 32; ++j) {
+          if (j >= left) break;
+          const uint4 q = __ldg(reinterpret_cast<const uint4*>(f + j * r + k));
+          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            v[j] = fmaf(uk[i], __uint_as_float(sizeof(T) == 4 ? w[i % 4] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16),
+                        v[j]);
         }
       }
+    } else if (f_vec) {
+#pragma unroll 2
+      for (int k = 0; k < r; ++k) {
+        const float uk = __ldg(up + k);
+#pragma unroll
+        for (int j = 0; j < 32; j += N) {
+          if (j >= left) break;  // (rows are whole vectors)
+          const uint4 q = __ldg(reinterpret_cast<const uint4*>(f + k * f_j + j));
+          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            v[j + i] = fmaf(uk, __uint_as_float(sizeof(T) == 4 ? w[i % 4] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16),
+                            v[j + i]);
+        }
+      }
+    } else {
+      for (int k = 0; k < r; ++k) {
+        const float uk = __ldg(up + k);
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+          if (j < left) v[j] = fmaf(uk, to_f32<T>(f[j * f_col + k * f_j]), v[j]);
+      }
     }
-    T* o = y + row_at(flags, perm, p) * ldy + col0;
+  }
+
+  __device__ __forceinline__ void store(int row0, int col0, int, int lane, bool many, const uint32_t (&acc)[32]) const {
+    const int left = cols - col0;
+    const int64_t p = row0 + lane;
+    if (left <= 0) return;
+    // what belongs to a column, a lane each
+    const float uc = undo_col && lane < left ? __ldg(undo_col + col0 + lane) : 1.f;
+    const float bc = bias && lane < left ? __ldg(bias + col0 + lane) : 0.f;
+    const float f = undo_row && p < rows ? __ldg(undo_row + p) : 1.f;
+    float v[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(acc[j]) * f;
+    if (undo_col) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] *= __shfl_sync(0xffffffffu, uc, j);
+    }
+    if (bias) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bc, j);
+    }
+    if (p >= rows) return;
+    if (u && (always || many)) low(p, col0, left, v);
+    T* o = y + p * ldy + col0;
     constexpr int kVec = 16 / sizeof(T);
 #pragma unroll
     for (int q = 0; q < 32 / kVec; ++q) {
@@ -348,49 +607,92 @@ __global__ void __launch_bounds__(128)
 }
 
 // ---------------------------------------------------------------- outer products
-// F_g[j, i] = sum over g's places p of c[p, j] in[row(p), i], on the tensor
-// cores: D^T, 128 of i x r of j (both planes of c side by side), one CTA each,
-// contracted over each run's whole groups of 16 rows; what is left of a run is
-// added in the epilogue, so that no row of another adapter is touched.
-struct Outer {
-  int r, width, rb;       // rb: columns of a plane in the tile, 64 or 128
-  const int* flags;
-  const int *off, *next, *first;
-  const bf16 *in, *in2;   // elements of the rows: in place, or staged where sorted
-  int64_t ld, ld2;
-  const uint16_t* c;      // planes of tokens x ldc
-  int64_t ldc, plane;
+// F_g[j, i] = sum over g's rows t of c[t, j] in[t, i]. A CTA lists the rows of
+// its adapter, a window of rows at a time, in order.
+constexpr int kWindow = 4096;  // (lists of 8 KB: two CTAs an SM)
+
+// The rows of `g` among [t0, t1), as offsets from t0, by THREADS threads;
+// returns their number. `count`: THREADS / 32 ints.
+template <int THREADS>
+__device__ __forceinline__ int list_rows(const int32_t* adapter, int64_t t0, int64_t t1, int g, uint16_t* list,
+                                         int* count, int tid) {
+  const int n = (int)(t1 - t0), per = (n + THREADS - 1) / THREADS;
+  const int a = min(tid * per, n), b = min(a + per, n);
+  int mine = 0;
+#pragma unroll 8
+  for (int i = a; i < b; ++i) mine += __ldg(adapter + t0 + i) == g;
+  int at = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, at, o);
+    if ((tid & 31) >= o) at += v;
+  }
+  if ((tid & 31) == 31) count[tid >> 5] = at;
+  asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+  int all = 0;
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w < tid >> 5) at += count[w];
+    all += count[w];
+  }
+  at -= mine;
+  if (mine)
+    for (int i = a; i < b; ++i)
+      if (__ldg(adapter + t0 + i) == g) list[at++] = (uint16_t)i;
+  asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+  return all;
+}
+
+// BF16, on the tensor cores: D^T, 128 of i x r of j (both planes of c side by
+// side). Four warps gather 64 rows a stage with 16-byte copies (past the list
+// and the width: zeros), one issues the MMAs.
+struct OuterJob {
+  const bf16* in;
+  int64_t ld;
+  int width;
+  const uint16_t* c;  // planes of tokens x ldc
   bf16* out;
   int64_t f_g, f_j, f_i;
+};
+struct OuterJobs {
+  OuterJob job[2];
+  const int32_t* adapter;
+  int64_t tokens, ldc, plane;
+  int r, rb;          // rb: columns of a plane in the tile, 64 or 128
   unsigned long long* errors;
 };
-constexpr int kOuterThreads = 192;
+constexpr int kOuterThreads = 160, kOuterStages = 3;
 
-__global__ void __launch_bounds__(kOuterThreads)
-    k_outer(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm2,
-            const __grid_constant__ CUtensorMap tmC, const Outer a) {
-  constexpr int kStages = 4;
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+__global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
   extern __shared__ unsigned char smem_raw[];
+  __shared__ int count[4];
+  const OuterJob& job = a.job[blockIdx.z];
+  const int i0 = blockIdx.x * 128, g = blockIdx.y;
+  if (i0 >= job.width) return;
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const int stage_bytes = 16384 + a.rb * 256;
-  const uint32_t full = base + kStages * stage_bytes, empty = full + 8 * kStages, done = empty + 8 * kStages,
-                 misc = done + 8;
+  const uint32_t lists = base + kOuterStages * stage_bytes, full = lists + 2 * kWindow, empty = full + 8 * kOuterStages,
+                 done = empty + 8 * kOuterStages, misc = done + 8;
+  uint16_t* list = reinterpret_cast<uint16_t*>(smem_raw + (lists - ptx::smem_u32(smem_raw)));
   unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
   volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
   volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
+  volatile int* total_s = reinterpret_cast<volatile int*>(misc_p + 8);  // chunks of the window, or -1
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int g = blockIdx.y, i0 = blockIdx.x * 128;
   const uint32_t cols = (uint32_t)a.rb * 2;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      ptx::mbar_init(full + 8 * s, 1);
+    for (int s = 0; s < kOuterStages; ++s) {
+      ptx::mbar_init(full + 8 * s, 128);
       ptx::mbar_init(empty + 8 * s, 1);
     }
     ptx::mbar_init(done, 1);
     *abort_s = 0;
     ptx::fence_mbar_init();
   }
-  if (warp == 1) {
+  if (warp == 4) {
     ptx::tmem_alloc(misc, cols);
     ptx::tmem_relinquish();
   }
@@ -400,54 +702,84 @@ __global__ void __launch_bounds__(kOuterThreads)
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   const uint32_t tmem = *tmem_slot;
-  const bool sorted = __ldg(a.flags + 1) != 0;
-  const int head = __ldg(a.first + g);
-  if (warp == 0) {
-    if (lane == 0) {
-      const CUtensorMap* m = sorted ? &tm2 : &tm;
-      int st = 0;
-      uint32_t ph = 0;
-      bool ok = true;
-      for (int i = head; i >= 0 && ok; i = __ldg(a.next + i)) {
-        const int r0 = __ldg(a.off + i), whole = (__ldg(a.off + i + 1) - r0) & ~15;
-        for (int k = 0; k < whole && ok; k += 64) {
-          ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
-          if (!ok) break;
-          ptx::mbar_expect_tx(full + 8 * st, (uint32_t)stage_bytes);
-          const uint32_t sa = base + st * stage_bytes, sb = sa + 16384;
-          mma::load_3d(sa, m, i0, r0 + k, 0, full + 8 * st);
-          mma::load_3d(sa + 8192, m, i0 + 64, r0 + k, 0, full + 8 * st);
-          for (int q = 0; q < 2; ++q)
-            for (int j = 0; j < a.rb; j += 64)
-              mma::load_3d(sb + (q * a.rb + j) * 128, &tmC, j, r0 + k, q, full + 8 * st);
-          if (++st == kStages) st = 0, ph ^= 1u;
-        }
-      }
+  const uint32_t id = mma::idesc(128, a.rb * 2, true, true, true);
+  int st = 0, issued = 0;  // stage and chunks so far, on every thread alike
+  uint32_t ph = 0, acc = 0;
+  bool ok = true;
+  const bool lead = warp == 4 && ptx::elect_one();
+  for (int64_t t0 = 0; t0 < a.tokens; t0 += kWindow) {
+    const int64_t t1 = min(t0 + kWindow, a.tokens);
+    if (warp < 4) {
+      const int n = list_rows<128>(a.adapter, t0, t1, g, list, count, threadIdx.x);
+      if (threadIdx.x == 0) *total_s = n;
     }
-  } else if (warp == 1) {
-    const bool lead = ptx::elect_one();
-    const uint32_t id = mma::idesc(128, a.rb * 2, true, true, true);
-    int st = 0;
-    uint32_t ph = 0, acc = 0;
-    bool ok = true;
-    for (int i = head; i >= 0 && ok; i = __ldg(a.next + i)) {
-      const int whole = (__ldg(a.off + i + 1) - __ldg(a.off + i)) & ~15;
-      for (int k = 0; k < whole && ok; k += 64) {
+    __syncthreads();
+    const int n = *total_s, chunks = (n + 63) / 64;
+    issued += chunks;
+    if (warp < 4) {
+      // 16-byte pieces of a stage: 64 rows x (16 of `in` + 2 x rb / 8 of c)
+      const int pieces = 16 + a.rb / 4;
+      auto arrive = [&](int s) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        ptx::mbar_arrive(full + 8 * s);
+      };
+      for (int k = 0; k < chunks && ok; ++k) {
+        ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
+        const uint32_t sa = base + st * stage_bytes;
+        // a warp takes a row at a time: its lanes the row's pieces
+        for (int r = warp; r < 64; r += 4) {
+          const bool row = k * 64 + r < n;
+          const int64_t t = row ? t0 + list[k * 64 + r] : t0;
+          for (int q = lane; q < pieces; q += 32) {
+            const void* src;
+            uint32_t dst;
+            int bytes;
+            if (q < 16) {
+              const int i = i0 + q * 8;
+              bytes = row ? max(0, min(16, (job.width - i) * 2)) : 0;
+              src = bytes ? job.in + t * job.ld + i : job.in;
+              dst = sa + (q >> 3) * 8192 + r * 128 + (((q & 7) ^ (r & 7)) << 4);
+            } else {
+              const int p = (q - 16) / (a.rb / 8), j = (q - 16 - p * (a.rb / 8));
+              bytes = row && j * 8 < a.ldc ? 16 : 0;
+              src = bytes ? a.plane * p + job.c + t * a.ldc + j * 8 : job.c;
+              dst = sa + 16384 + (p * a.rb + (j >> 3) * 64) * 128 + r * 128 + (((j & 7) ^ (r & 7)) << 4);
+            }
+            copy16(dst, src, bytes);
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        // the stage before this one has arrived
+        if (k > 0) {
+          asm volatile("cp.async.wait_group 1;" ::: "memory");
+          arrive(st == 0 ? kOuterStages - 1 : st - 1);
+        }
+        if (k == chunks - 1) {
+          asm volatile("cp.async.wait_group 0;" ::: "memory");
+          arrive(st);
+        }
+        if (++st == kOuterStages) st = 0, ph ^= 1u;
+      }
+    } else {
+      for (int k = 0; k < chunks && ok; ++k) {
         ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, mma::kWaitLimit);
         if (!ok) break;
         ptx::tc_fence_after();
         if (lead) {
           uint64_t da = mma::desc(base + st * stage_bytes, true), db = mma::desc(base + st * stage_bytes + 16384, true);
-          const int steps = min(4, (whole - k) / 16);
+          const int steps = min(4, (n - k * 64 + 15) / 16);
           for (int q = 0; q < steps; ++q, da += 2048 >> 4, db += 2048 >> 4) {
             ptx::mma_f16(tmem, da, db, id, acc);
             acc = 1;
           }
           ptx::mma_commit(empty + 8 * st);
         }
-        if (++st == kStages) st = 0, ph ^= 1u;
+        if (++st == kOuterStages) st = 0, ph ^= 1u;
       }
     }
+    __syncthreads();  // the list is free
+  }
+  if (warp == 4) {
     if (lead) {
       volatile int never = 0;
       ptx::mma_commit(done);
@@ -455,135 +787,135 @@ __global__ void __launch_bounds__(kOuterThreads)
     }
     __syncwarp();
   } else {
-    const int i = i0 + (warp & 3) * 32 + lane;
-    bool ok = ptx::mbar_wait(done, 0, abort_s, mma::kWaitLimit);
+    ok = ptx::mbar_wait(done, 0, abort_s, mma::kWaitLimit);
     ok = __all_sync(0xffffffffu, ok);
     ptx::tc_fence_after();
-    bool any = false;  // rows on the tensor cores
-    for (int q = head; q >= 0; q = __ldg(a.next + q)) any |= __ldg(a.off + q + 1) - __ldg(a.off + q) >= 16;
-    const bf16* in = sorted ? a.in2 : a.in;
-    const int64_t ld = sorted ? a.ld2 : a.ld;
-    bf16* out = a.out + g * a.f_g + (int64_t)i * a.f_i;
+    const int i = i0 + warp * 32 + lane;
+    bf16* out = job.out + g * job.f_g + (int64_t)i * job.f_i;
+    const bool vec = job.f_j == 1 && a.r % 8 == 0 && ((uintptr_t)job.out & 15) == 0;
     for (int j0 = 0; ok && j0 < a.r; j0 += 32) {
       uint32_t hi[32], lo[32];
-      float v[32];
-      const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16) + j0;
+      const uint32_t src = tmem + ((uint32_t)(warp * 32) << 16) + j0;
       ptx::tmem_ld32(src, hi);
       ptx::tmem_ld32(src + a.rb, lo);
       ptx::tmem_wait_ld();
+      if (i >= job.width) continue;
+      float v[32];
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = any ? __uint_as_float(hi[j]) + __uint_as_float(lo[j]) : 0.f;
-      for (int q = head; q >= 0; q = __ldg(a.next + q)) {
-        const int r0 = __ldg(a.off + q), r1 = __ldg(a.off + q + 1);
-        for (int p = r0 + ((r1 - r0) & ~15); p < r1; ++p) {
-          const float xv = i < a.width ? to_f32<bf16>(in[p * ld + i]) : 0.f;
-          const uint16_t* c = a.c + p * a.ldc + j0;
+      for (int j = 0; j < 32; ++j) v[j] = issued ? __uint_as_float(hi[j]) + __uint_as_float(lo[j]) : 0.f;
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (j0 + j < a.r)
-              v[j] = fmaf(xv, __uint_as_float((uint32_t)__ldg(c + j) << 16) +
-                                  __uint_as_float((uint32_t)__ldg(c + a.plane + j) << 16), v[j]);
+      for (int q = 0; q < 4; ++q) {
+        __align__(16) bf16 h[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = __float2bfloat16_rn(v[q * 8 + j]);
+        if (vec && j0 + q * 8 < a.r) {
+          *reinterpret_cast<uint4*>(out + j0 + q * 8) = *reinterpret_cast<uint4*>(h);
+        } else if (!vec) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j0 + q * 8 + j < a.r) out[(j0 + q * 8 + j) * job.f_j] = h[j];
         }
-      }
-      if (i < a.width) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j0 + j < a.r) out[(j0 + j) * a.f_j] = from_f32<bf16>(v[j]);
       }
     }
     ptx::tc_fence_before();
   }
   __syncthreads();
-  if (*abort_s) {
-    const long long t0 = clock64();
-    while (clock64() - t0 < (1LL << 23)) {
-    }
-    if (threadIdx.x == 0) atomicAdd(a.errors, 1ull);
-    __syncthreads();
-  }
+  if (threadIdx.x == 0 && *abort_s) atomicAdd(a.errors, 1ull);
   ptx::tc_fence_after();
-  if (warp == 1) ptx::tmem_dealloc(tmem, cols);
+  if (warp == 4) ptx::tmem_dealloc(tmem, cols);
 }
 
-// The same in FP32 on the CUDA cores: 128 of i, eight of j, the places dealt
-// over eight groups of threads.
-__global__ void __launch_bounds__(1024)
-    k_outer_f32(const float* in, int64_t ld, int width, const float* c, int r, const Plan p, float* out, int64_t f_g,
-                int64_t f_j, int64_t f_i) {
-  __shared__ float red[8][8][128];
+// FP32, on the CUDA cores: 128 of i, eight of j, the listed rows dealt over
+// eight groups of threads.
+struct OuterJobF32 {
+  const float* in;
+  int64_t ld;
+  int width;
+  const float* c;  // tokens x r
+  float* out;
+  int64_t f_g, f_j, f_i;
+};
+struct OuterJobsF32 {
+  OuterJobF32 job[2];
+  const int32_t* adapter;
+  int64_t tokens;
+  int r, groups;  // groups: of eight columns
+};
+
+__global__ void __launch_bounds__(1024) k_outer_f32(const OuterJobsF32 a) {
+  __shared__ float red[8][8][128];  // 32 KB; the list before it
+  __shared__ int count[32];
+  uint16_t* list = reinterpret_cast<uint16_t*>(red);
+  const OuterJobF32& job = a.job[blockIdx.z];
+  const int tile = blockIdx.x / a.groups, g = blockIdx.y, j0 = (blockIdx.x - tile * a.groups) * 8;
+  const int ti = threadIdx.x & 127, q = threadIdx.x >> 7, i = tile * 128 + ti;
+  if (tile * 128 >= job.width) return;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int g = blockIdx.z, j0 = blockIdx.y * 8, ti = threadIdx.x & 127, q = threadIdx.x >> 7;
-  const int i = blockIdx.x * 128 + ti;
-  const int nj = min(8, r - j0);
-  const bool sorted = __ldg(p.flags + 1) != 0;
+  const int nj = min(8, a.r - j0);
   float acc[8] = {};
-  for (int run = __ldg(p.first + g); run >= 0; run = __ldg(p.next + run)) {
-    const int r1 = __ldg(p.off + run + 1);
+  for (int64_t t0 = 0; t0 < a.tokens; t0 += kWindow) {
+    const int64_t t1 = min(t0 + kWindow, a.tokens);
+    const int n = list_rows<1024>(a.adapter, t0, t1, g, list, count, threadIdx.x);
 #pragma unroll 4
-    for (int at = __ldg(p.off + run) + q; at < r1; at += 8) {
-      const int64_t t = sorted ? __ldg(p.perm + at) : at;
-      const float x = i < width ? in[t * ld + i] : 0.f;
+    for (int k = q; k < n; k += 8) {
+      const int64_t t = t0 + list[k];
+      const float x = i < job.width ? __ldg(job.in + t * job.ld + i) : 0.f;
+      const float* c = job.c + t * a.r + j0;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (j < nj) acc[j] = fmaf(x, __ldg(c + (int64_t)at * r + j0 + j), acc[j]);
+        if (j < nj) acc[j] = fmaf(x, __ldg(c + j), acc[j]);
     }
+    __syncthreads();
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) red[q][j][ti] = acc[j];
   __syncthreads();
   for (int e = threadIdx.x; e < nj * 128; e += 1024) {
-    const int j = e >> 7, k = e & 127, at = blockIdx.x * 128 + k;
+    const int j = e >> 7, k = e & 127, at = tile * 128 + k;
     float s = red[0][j][k];
 #pragma unroll
     for (int w = 1; w < 8; ++w) s += red[w][j][k];
-    if (at < width) out[g * f_g + (j0 + j) * f_j + (int64_t)at * f_i] = s;
+    if (at < job.width) job.out[g * job.f_g + (j0 + j) * job.f_j + (int64_t)at * job.f_i] = s;
   }
 }
 
 // ---------------------------------------------------------------- host side
-constexpr int64_t kFewF32 = 64, kFewBf16 = 128;  // rows that need no plan
+constexpr int64_t kFewF32 = 64, kFewBf16 = 128;  // rows of the single-token form
 
-// What one product with the shared head needs: its rows' input (x or dy), its
-// contracted width and the factor its low-rank part shrinks by.
+// One product with the shared head: its rows' input (x or dy), its contracted
+// width, its columns and the strides of the factor that shrinks it.
 struct Side {
   const void* in;
   int64_t ld;
-  int width;       // contracted
-  int out;         // columns of the result
-  int64_t f_j, f_i;  // strides of the shrinking factor
+  int width, out;
+  int64_t f_j, f_i;
 };
 
 struct Layout {
-  Plan plan;
-  uint16_t* in[2];                       // staged rows: of x, of dy
-  uint16_t* w;                           // staged W
-  uint16_t *a, *b;                       // staged factors
-  float *undo_in, *undo_w, *u[2];        // u, v in FP32
-  uint16_t* up[2];                       // their planes
-  int64_t ld_in[2], ld_w, ld_a, ld_b, ld_u;
+  uint16_t* in[2];        // rows of x, of dy: planes (FP32), copies (BF16 that TMA cannot read)
+  uint16_t *w, *a, *b;    // the same of W and of the factors (BF16)
+  float *undo_in, *undo_w;
+  float* u[2];            // u, v: tokens x r
+  uint16_t* up[2];        // their planes (BF16)
+  int64_t ld_x, ld_y, ld_r;
   void take(Carve& c, const lipcache_adapted& p, bool backward) {
     const bool f32 = p.type == LIPCACHE_F32;
     const int64_t T = p.tokens, G = p.adapters, r = G ? p.rank : 1;
     const int planes = f32 ? 2 : 1;
-    ld_in[0] = round_up(p.d, 8);
-    ld_in[1] = round_up(p.classes, 8);
-    ld_w = round_up(p.d, 8);
-    ld_a = round_up(p.d, 8);
-    ld_b = ld_u = round_up(r, 8);
-    plan.take(c, G ? T : 0, p.adapters);
-    const bool stage_x = !(f32 && backward);
-    c.take(in[0], stage_x ? (size_t)(planes * T * ld_in[0]) : 0);
-    c.take(in[1], backward ? (size_t)(planes * T * ld_in[1]) : 0);
-    c.take(w, (size_t)(planes * p.classes * ld_w));
-    const int fp = f32 ? 3 : 1;
-    c.take(a, (size_t)(fp * G * r * ld_a));
-    c.take(b, (size_t)(fp * G * p.classes * ld_b));
+    ld_x = round_up(p.d, 8);
+    ld_y = round_up(p.classes, 8);
+    ld_r = round_up(r, 8);
+    c.take(in[0], f32 && backward ? 0 : (size_t)(planes * T * ld_x));
+    c.take(in[1], backward ? (size_t)(planes * T * ld_y) : 0);
+    c.take(w, (size_t)(planes * p.classes * ld_x));
+    c.take(a, f32 ? 0 : (size_t)(G * r * ld_x));
+    c.take(b, f32 ? 0 : (size_t)(G * p.classes * ld_r));
     c.take(undo_in, (size_t)T);
     c.take(undo_w, (size_t)p.classes);
     for (int i = 0; i < 2; ++i) {
       c.take(u[i], G ? (size_t)(T * r) : 0);
-      c.take(up[i], G ? (size_t)(3 * T * ld_u) : 0);
+      c.take(up[i], G && !f32 ? (size_t)(2 * T * ld_r) : 0);
     }
   }
 };
@@ -596,54 +928,118 @@ struct Op {
   cudaStream_t s;
   const T *x = static_cast<const T*>(p.x), *W = static_cast<const T*>(p.W), *A = static_cast<const T*>(p.A),
           *B = static_cast<const T*>(p.B);
-  const int* flags = p.adapters ? l.plan.flags : nullptr;
 
-  void stage(const T* in, int64_t ld, int64_t rows, int cols, bool sort, bool only_sorted, const float* fold,
-             uint16_t* out, int64_t ldo, float* undo) {
-    // (W's powers are folded into dy: less room)
-    Stage a{rows, ld, cols, sort ? flags : nullptr, l.plan.perm, only_sorted, fold, ldo, rows * ldo, undo, sort ? 100 : 60};
-    launch_pdl(k_stage<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows, 8), 1 << 16)), 256, s, in, a, out);
-    LC_LAUNCH_CHECK("k_stage");
+  // A BF16 tensor as TMA can read it: itself, or a copy.
+  Tensor readable(const void* in, int64_t ld, int64_t rows, int cols, int64_t planes, uint16_t* copy, int64_t ldo) {
+    if (mma::mappable(in, ld)) return Tensor{in, cols, rows, planes, ld, rows * ld};
+    const int64_t all = rows * planes;
+    launch_pdl(k_copy_rows, dim3((unsigned)std::min<int64_t>(ceil_div(all, 8), 1 << 16)), 256, s,
+               reinterpret_cast<const bf16*>(in), ld, all, cols, reinterpret_cast<bf16*>(copy), ldo);
+    LC_LAUNCH_CHECK("k_copy_rows");
+    return Tensor{copy, cols, rows, planes, ldo, rows * ldo};
   }
-  void factor(const T* in, int64_t rows, int cols, int64_t ldo, const float* undo, int div, uint16_t* out) {
-    launch_pdl(k_factor<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows * cols, 1024), 1 << 16)), 256, s, in, rows,
-               cols, ldo, rows * ldo, undo, div, out);
-    LC_LAUNCH_CHECK("k_factor");
+  Tensor rows_of(const Side& d, int i) {
+    return readable(d.in, d.ld, p.tokens, d.width, 1, l.in[i], i ? l.ld_y : l.ld_x);
   }
-  // u (i = 0) or v (1) of every row, in FP32 and/or planes.
-  void shrink(const Side& d, const T* F, int i, bool planned, bool want_f32, bool want_planes, const float* undo) {
-    Shrink a{p.tokens, d.ld, d.width, p.rank, p.adapters, planned ? flags : nullptr, l.plan.perm, p.adapter, p.scales,
-             (int64_t)p.rank * d.width, d.f_j, d.f_i, want_f32 ? l.u[i] : nullptr, want_planes ? l.up[i] : nullptr,
-             l.ld_u, p.tokens * l.ld_u, f32 ? 3 : 2, undo};
-    const dim3 grid((unsigned)ceil_div(p.tokens, 16), (unsigned)ceil_div(p.rank, 8));
-    launch_pdl(k_shrink<T>, grid, 128, s, static_cast<const T*>(d.in), F, a);
+  Tensor head() { return readable(W, p.ldw, p.classes, p.d, 1, l.w, l.ld_x); }
+  Tensor factor_a() { return readable(A, p.d, p.rank, p.d, p.adapters, l.a, l.ld_x); }
+  Tensor factor_b() { return readable(B, p.rank, p.classes, p.rank, p.adapters, l.b, l.ld_r); }
+
+  RowJob row_job(const void* in, int64_t ld, int64_t rows, int width) {
+    RowJob j;
+    j.in = static_cast<const float*>(in);
+    j.ld = ld;
+    j.rows = rows;
+    j.width = width;
+    j.vec = width % 4 == 0 && ld % 4 == 0 && ((uintptr_t)in & 15) == 0;
+    return j;
+  }
+  void to_planes(RowJob& j, uint16_t* out, int64_t ldo, float* undo, int most) {
+    j.planes = reinterpret_cast<__half*>(out);
+    j.ldo = ldo;
+    j.plane = j.rows * ldo;
+    j.undo = undo;
+    j.most = most;
+  }
+  void to_low(RowJob& j, const Side& d, const T* F, int i) {
+    if (!p.adapters) return;
+    j.F = reinterpret_cast<const float*>(F);
+    j.f_g = (int64_t)p.rank * d.width;
+    j.f_j = d.f_j;
+    j.f_i = d.f_i;
+    j.f_vec = j.vec && d.f_i == 1 && ((uintptr_t)F & 15) == 0;
+    j.u = l.u[i];
+  }
+  void run_rows(const RowJob& a, const RowJob& b) {
+    RowJobs j{{a, b}, p.adapter, p.scales, p.adapters, p.rank};
+    const int64_t all = a.rows + b.rows;
+    launch_pdl(k_rows_f32, dim3((unsigned)std::min<int64_t>(ceil_div(all, 8), 16 * mma::num_sms())), 256, s, j);
+    LC_LAUNCH_CHECK("k_rows_f32");
+  }
+
+  // u and/or v on the tensor cores.
+  struct Shrinking {
+    Tensor rows, factor;
+    bool f_mn;
+    int i;
+  };
+  void shrink(const Shrinking* jobs, int n) {
+    ShrinkJobs a = {};
+    int chunks = 1 << 30;
+    const int rn = (int)round_up(p.rank, 16), rb = p.rank <= 64 ? 64 : 128;
+    for (int k = 0; k < n; ++k) {
+      ShrinkJob& j = a.job[k];
+      const Shrinking& d = jobs[k];
+      j.rows = mma::tensor_map(d.rows, 128);
+      j.f_mn = d.f_mn;
+      const int cols = d.f_mn ? rb : rn;  // of D
+      j.factor = mma::tensor_map(d.factor, d.f_mn ? 64 : rn);
+      j.f_bytes = cols * 128;
+      j.per = std::min(8, 32768 / j.f_bytes);
+      const mma::Seg g = mma::segment(d.rows.cols, 0, 0, mma::idesc(128, cols, true, false, d.f_mn));
+      j.chunks = g.chunks;
+      j.last = g.last;
+      j.idesc = g.idesc;
+      j.u = l.u[d.i];
+      j.planes = l.up[d.i];
+      chunks = std::min(chunks, j.chunks);
+    }
+    a.adapter = p.adapter;
+    a.scales = p.scales;
+    a.tokens = p.tokens;
+    a.ldo = l.ld_r;
+    a.plane = p.tokens * l.ld_r;
+    a.G = p.adapters;
+    a.r = p.rank;
+    a.rn = rn;
+    a.errors = mma::error_counter();
+    const int64_t tiles = ceil_div(p.tokens, 128);
+    // the width split until the device is filled, four stages or more a CTA
+    int splits = 1;
+    while (splits < 4 && tiles * n * splits * 2 <= mma::num_sms() && chunks >= 8 * splits) splits *= 2;
+    const int smem = 1024 + kShrinkStages * kShrinkStage + 128;
+    allow_smem(reinterpret_cast<const void*>(k_shrink), smem);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)splits;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(splits * tiles), 1, (unsigned)n);
+    cfg.blockDim = dim3(kShrinkThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    LC_CUDA(cudaLaunchKernelEx(&cfg, k_shrink, a));
     LC_LAUNCH_CHECK("k_shrink");
   }
-  // The same on the tensor cores; rows: the maps of the input in place and staged.
-  void shrink_mma(const Side& d, const CUtensorMap& rows, const CUtensorMap& staged, const Tensor& F, bool f_mn, int i) {
-    mma::Args a = {};
-    a.m_tiles = (int)ceil_div(p.tokens, 128);
-    a.n_tiles = a.batches = 1;
-    a.bn = p.rank <= 64 ? 64 : 128;
-    a.a_rows = 128;
-    a.lb_mn = f_mn;
-    a.alt = flags + 1;
-    a.low.runs = l.plan.runs();
-    a.low.from_a = 1;
-    a.low.G = p.adapters;
-    a.low.pairs = 1;
-    const mma::Seg g = mma::segment(d.width, 0, 0, mma::idesc(128, a.bn, true, false, f_mn));
-    a.low.chunks = g.chunks;
-    a.low.last = g.last;
-    a.low.idesc = g.idesc;
-    const CUtensorMap f = mma::tensor_map(F, f_mn ? 64 : a.bn);
-    const ShrinkEpi e{l.up[i], l.plan.row_g, p.scales, l.ld_u, p.tokens * l.ld_u, p.tokens, p.adapters};
-    mma::launch<1, false>({rows, staged, f, rows, f}, a, e, s);
-  }
 
-  // out = rows . W (both as tensors) + low-rank: M tokens, N d.out, K d.width.
-  void product(const Side& d, const CUtensorMap& rows, const CUtensorMap& staged, const Tensor& w, bool w_mn, int a_rows,
-               int i, const Tensor* F, bool f_mn, AdaptEpi<T> e) {
+  // out = rows . W + low-rank: M tokens, N d.out, K d.width. F: the low-rank
+  // factor as the tensor cores read it (BF16), or null.
+  void product(const Side& d, const Tensor& rows, const Tensor& w, bool w_mn, int i, const Tensor* F, bool f_mn,
+               AdaptEpi<T> e) {
     mma::Args a = {};
     const int64_t tiles = ceil_div(p.tokens, 256) * ceil_div(d.out, 256);
     // CTA pairs where their tiles fill half the device; else single CTAs, the tile narrowed until they do
@@ -658,8 +1054,7 @@ struct Op {
     a.n_tiles = (int)ceil_div(d.out, a.bn);
     a.batches = 1;
     a.b_mn = w_mn;
-    a.a_rows = a_rows;
-    a.alt = flags ? flags + 1 : nullptr;
+    a.a_rows = (int)std::min<int64_t>(128, round_up(p.tokens, 8));
     a.block = kBlock;
     const uint32_t id = mma::idesc(tm, a.bn, !f32, false, w_mn);
     if (f32) {
@@ -667,26 +1062,25 @@ struct Op {
       a.seg[a.nseg++] = mma::segment(d.width, 1, 0, id);
     }
     a.seg[a.nseg++] = mma::segment(d.width, 0, 0, id);
-    const CUtensorMap mw = mma::tensor_map(w, w_mn ? 64 : a.bn / (pair ? 2 : 1));
-    CUtensorMap la = rows, lb = mw;
+    mma::Maps maps;
+    maps.a = mma::tensor_map(rows, a.a_rows);
+    maps.b = mma::tensor_map(w, w_mn ? 64 : a.bn / (pair ? 2 : 1));
+    maps.la = maps.a;
+    maps.lb = maps.b;
     if (F) {
       a.lb_mn = f_mn;
-      a.low.runs = l.plan.runs();
+      a.low.adapter = p.adapter;
+      a.low.tokens = p.tokens;
       a.low.G = p.adapters;
       const mma::Seg g = mma::segment(p.rank, 0, 0, mma::idesc(tm, a.bn, true, false, f_mn));
       a.low.chunks = g.chunks;
       a.low.last = g.last;
       a.low.idesc = g.idesc;
-      static const int pu[6] = {2, 0, 1, 1, 0, 0}, pf[6] = {0, 2, 1, 0, 1, 0};
-      a.low.pairs = f32 ? 6 : 2;
-      for (int k = 0; k < a.low.pairs; ++k) {
-        a.low.a_z[k] = f32 ? pu[k] : 1 - k;
-        a.low.b_z[k] = f32 ? pf[k] : 0;
-      }
-      la = mma::tensor_map(Tensor{l.up[i], l.ld_u, p.tokens, f32 ? 3 : 2, l.ld_u, p.tokens * l.ld_u}, 128);
-      lb = mma::tensor_map(*F, f_mn ? 64 : a.bn / (pair ? 2 : 1));
+      a.low.pairs = 2;  // lo, hi
+      a.low.a_z[0] = 1;
+      maps.la = mma::tensor_map(Tensor{l.up[i], l.ld_r, p.tokens, 2, l.ld_r, p.tokens * l.ld_r}, a.a_rows);
+      maps.lb = mma::tensor_map(*F, f_mn ? 64 : a.bn / (pair ? 2 : 1));
     }
-    const mma::Maps maps{rows, staged, mw, la, lb};
     if (pair)
       mma::launch<2, f32>(maps, a, e, s);
     else
@@ -700,63 +1094,39 @@ struct Op {
     e.rows = p.tokens;
     e.cols = cols;
     e.vec = ((uintptr_t)y & 15) == 0 && ldy * sizeof(T) % 16 == 0;
-    e.flags = flags;
-    e.perm = l.plan.perm;
     return e;
   }
-
-  // W's planes or its own rows; `undo_w` is set for FP32.
-  Tensor shared() {
-    if (f32 || !mma::mappable(W, p.ldw)) {
-      stage(W, p.ldw, p.classes, p.d, false, false, nullptr, l.w, l.ld_w, l.undo_w);
-      return Tensor{l.w, p.d, p.classes, f32 ? 2 : 1, l.ld_w, p.classes * l.ld_w};
-    }
-    return Tensor{W, p.d, p.classes, 1, p.ldw, 0};
+  // the low-rank product in the epilogue: F of cols x r (by_col) or r x cols
+  void epilogue_low(AdaptEpi<T>& e, int i, const T* F, bool by_col, bool always) {
+    if (!p.adapters) return;
+    constexpr int N = 16 / sizeof(T);
+    e.u = l.u[i];
+    e.F = F;
+    e.adapter = p.adapter;
+    e.G = p.adapters;
+    e.r = p.rank;
+    e.f_col = by_col ? p.rank : 1;
+    e.f_j = by_col ? 1 : e.cols;
+    e.f_vec = (by_col ? p.rank : e.cols) % N == 0 && ((uintptr_t)F & 15) == 0;
+    e.always = always;
   }
-  Tensor factor_a() {  // G x r x d
-    const int64_t rows = (int64_t)p.adapters * p.rank;
-    if (f32 || !mma::mappable(A, p.d)) {
-      factor(A, rows, p.d, l.ld_a, nullptr, 1, l.a);
-      return Tensor{l.a, p.d, p.rank, (f32 ? 3 : 1) * (int64_t)p.adapters, l.ld_a, p.rank * l.ld_a};
-    }
-    return Tensor{A, p.d, p.rank, p.adapters, p.d, (int64_t)p.rank * p.d};
-  }
-  Tensor factor_b(const float* undo) {  // G x classes x r
-    const int64_t rows = (int64_t)p.adapters * p.classes;
-    if (f32 || !mma::mappable(B, p.rank)) {
-      factor(B, rows, p.rank, l.ld_b, undo, p.classes, l.b);
-      return Tensor{l.b, p.rank, p.classes, (f32 ? 3 : 1) * (int64_t)p.adapters, l.ld_b, p.classes * l.ld_b};
-    }
-    return Tensor{B, p.rank, p.classes, p.adapters, p.rank, (int64_t)p.classes * p.rank};
-  }
-  // The maps of the rows of x (i = 0) or dy (1): in place, and staged in the plan's order.
-  void rows(const Side& d, int i, const float* fold, CUtensorMap& in, CUtensorMap& staged) {
-    const bool direct = !f32 && mma::mappable(d.in, d.ld);
-    staged = mma::tensor_map(Tensor{l.in[i], d.width, p.tokens, f32 ? 2 : 1, l.ld_in[i], p.tokens * l.ld_in[i]}, 128);
-    in = direct ? mma::tensor_map(Tensor{d.in, d.width, p.tokens, 1, d.ld, 0}, 128) : staged;
-    if (!direct || flags)
-      stage(static_cast<const T*>(d.in), d.ld, p.tokens, d.width, true, direct, fold, l.in[i], l.ld_in[i], l.undo_in);
-  }
-  // Whether an adapter has rows enough for its factor to be worth the tensor
-  // cores' stages (a factor's stages are loaded again for every run).
-  bool dense() const { return !f32 && p.tokens >= 16 * (int64_t)p.adapters; }
 
   void forward(const float* bias, T* y, int64_t ldy) {
     const Side d{x, p.ldx, p.d, p.classes, p.d, 1};
-    const bool tma = !f32 && mma::mappable(x, p.ldx) && mma::mappable(W, p.ldw);
+    const bool low = p.adapters > 0, tma = !f32 && mma::mappable(x, p.ldx) && mma::mappable(W, p.ldw);
     if (p.tokens <= (tma ? kFewBf16 : kFewF32)) {
-      if (p.adapters) shrink(d, A, 0, false, true, false, nullptr);
+      if (low) {
+        const int vec = ((uintptr_t)x & 15) == 0 && ((uintptr_t)A & 15) == 0 && p.ldx * sizeof(T) % 16 == 0 &&
+                        p.d * sizeof(T) % 16 == 0;
+        launch_pdl(k_shrink_few<T>, dim3((unsigned)p.tokens, (unsigned)ceil_div(p.rank, 8)), 128, s, x, p.ldx,
+                   (int)p.d, A, vec, (int)p.adapters, (int)p.rank, p.adapter, p.scales, l.u[0]);
+        LC_LAUNCH_CHECK("k_shrink_few");
+      }
       if (tma) {
         AdaptEpi<T> e = epilogue(y, ldy, p.classes);
         e.bias = bias;
-        e.flags = nullptr;
-        if (p.adapters) e.u = l.u[0], e.B = B, e.adapter = p.adapter, e.G = p.adapters, e.r = p.rank;
-        const int a_rows = (int)round_up(p.tokens, 8);
-        const CUtensorMap in = mma::tensor_map(Tensor{x, p.d, p.tokens, 1, p.ldx, 0}, a_rows);
-        const int* keep = flags;
-        flags = nullptr;
-        product(d, in, in, Tensor{W, p.d, p.classes, 1, p.ldw, 0}, false, a_rows, 0, nullptr, false, e);
-        flags = keep;
+        epilogue_low(e, 0, B, true, true);
+        product(d, rows_of(d, 0), head(), false, 0, nullptr, false, e);
       } else {
         launch_pdl(k_rows<T>, dim3((unsigned)ceil_div(p.classes, 16), (unsigned)ceil_div(p.tokens, 8)), 128, s, x,
                    p.ldx, p.tokens, W, p.ldw, (int)p.classes, (int)p.d, bias, (const float*)l.u[0], B, p.adapter,
@@ -765,108 +1135,108 @@ struct Op {
       }
       return;
     }
-    if (p.adapters) make_plan(p.adapter, p.tokens, p.adapters, l.plan, s);
-    CUtensorMap in, staged;
-    const Tensor w = shared();
-    rows(d, 0, nullptr, in, staged);
-    Tensor fb = {};
-    if (p.adapters) {
-      if (dense())
-        shrink_mma(d, in, staged, factor_a(), false, 0);
-      else
-        shrink(d, A, 0, true, false, true, f32 ? l.undo_in : nullptr);
-      fb = factor_b(f32 ? l.undo_w : nullptr);
-    }
     AdaptEpi<T> e = epilogue(y, ldy, p.classes);
     e.bias = bias;
-    if (f32) e.undo_row = l.undo_in, e.undo_col = l.undo_w;
-    product(d, in, staged, w, false, 128, 0, p.adapters ? &fb : nullptr, false, e);
-  }
-
-  void outer(const Side& d, int in_i, int c_i, T* out, const CUtensorMap& in, const CUtensorMap& staged) {
-    // d: the side whose rows are contracted; the factor's gradient has its strides
+    epilogue_low(e, 0, B, true, f32);
     if constexpr (f32) {
-      k_outer_f32_launch(d, c_i, out);
+      RowJob jx = row_job(x, p.ldx, p.tokens, p.d), jw = row_job(W, p.ldw, p.classes, p.d);
+      to_planes(jx, l.in[0], l.ld_x, l.undo_in, 100);
+      to_low(jx, d, A, 0);
+      to_planes(jw, l.w, l.ld_x, l.undo_w, 60);
+      run_rows(jx, jw);
+      e.undo_row = l.undo_in;
+      e.undo_col = l.undo_w;
+      product(d, Tensor{l.in[0], p.d, p.tokens, 2, l.ld_x, p.tokens * l.ld_x},
+              Tensor{l.w, p.d, p.classes, 2, l.ld_x, p.classes * l.ld_x}, false, 0, nullptr, false, e);
     } else {
-      Outer a = {};
-      a.r = p.rank;
-      a.width = d.width;
-      a.rb = p.rank <= 64 ? 64 : 128;
-      a.flags = flags;
-      a.off = l.plan.off;
-      a.next = l.plan.next;
-      a.first = l.plan.first;
-      const bool direct = mma::mappable(d.in, d.ld);
-      a.in2 = reinterpret_cast<const bf16*>(l.in[in_i]);
-      a.ld2 = l.ld_in[in_i];
-      a.in = direct ? static_cast<const bf16*>(d.in) : a.in2;
-      a.ld = direct ? d.ld : a.ld2;
-      a.c = l.up[c_i];
-      a.ldc = l.ld_u;
-      a.plane = p.tokens * l.ld_u;
-      a.out = out;
-      a.f_g = (int64_t)p.rank * d.width;
-      a.f_j = d.f_j;
-      a.f_i = d.f_i;
-      a.errors = mma::error_counter();
-      // boxes of 64 x 64: the rows are contracted
-      const Tensor ti{a.in, d.width, p.tokens, 1, a.ld, 0}, ts{a.in2, d.width, p.tokens, 1, a.ld2, 0},
-          tc{a.c, l.ld_u, p.tokens, 2, l.ld_u, a.plane};
-      const CUtensorMap m1 = mma::tensor_map(ti, 64), m2 = mma::tensor_map(ts, 64), mc = mma::tensor_map(tc, 64);
-      const int smem = 1024 + 4 * (16384 + a.rb * 256) + 128;
-      allow_smem(reinterpret_cast<const void*>(k_outer), 1024 + 4 * (16384 + 128 * 256) + 128);
-      cudaLaunchAttribute attr;
-      attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      attr.val.programmaticStreamSerializationAllowed = 1;
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3((unsigned)ceil_div(d.width, 128), (unsigned)p.adapters);
-      cfg.blockDim = dim3(kOuterThreads);
-      cfg.dynamicSmemBytes = (size_t)smem;
-      cfg.stream = s;
-      cfg.attrs = &attr;
-      cfg.numAttrs = 1;
-      LC_CUDA(cudaLaunchKernelEx(&cfg, k_outer, m1, m2, mc, a));
-      LC_LAUNCH_CHECK("k_outer");
+      const Tensor rows = rows_of(d, 0), w = head();
+      Tensor fb = {};
+      if (low) {
+        const Shrinking j{rows, factor_a(), false, 0};
+        shrink(&j, 1);
+        fb = factor_b();
+      }
+      product(d, rows, w, false, 0, low ? &fb : nullptr, false, e);
     }
-  }
-  void k_outer_f32_launch(const Side& d, int c_i, T* out) {
-    const dim3 grid((unsigned)ceil_div(d.width, 128), (unsigned)ceil_div(p.rank, 8), (unsigned)p.adapters);
-    launch_pdl(k_outer_f32, grid, 1024, s, reinterpret_cast<const float*>(d.in), d.ld, d.width, (const float*)l.u[c_i],
-               (int)p.rank, l.plan, reinterpret_cast<float*>(out), (int64_t)p.rank * d.width, d.f_j, d.f_i);
-    LC_LAUNCH_CHECK("k_outer_f32");
   }
 
   void backward(const T* dy, int64_t lddy, T* dx, int64_t lddx, T* dA, T* dB) {
     const Side sx{x, p.ldx, p.d, p.classes, p.d, 1}, sy{dy, lddy, p.classes, p.d, 1, p.rank};
-    const bool low = p.adapters > 0;
-    if (!low && !dx) return;
-    if (low) make_plan(p.adapter, p.tokens, p.adapters, l.plan, s);
-    CUtensorMap in_x, staged_x, in_y, staged_y;
-    Tensor w = {}, fa = {};
-    if (dx) w = shared();
-    // BF16 rows of x are read through the tensor cores for dA and u, those of dy for all else
-    if (!f32 && low && (dA || dB)) rows(sx, 0, nullptr, in_x, staged_x);
-    if (!f32 || dx) rows(sy, 1, f32 ? l.undo_w : nullptr, in_y, staged_y);
-    if (low && (dx || dA)) {
-      if (dense())
-        shrink_mma(sy, in_y, staged_y, factor_b(nullptr), true, 1);
-      else
-        shrink(sy, B, 1, true, f32, !f32 || dx != nullptr, f32 && dx ? l.undo_in : nullptr);
+    const bool low = p.adapters > 0, want_v = low && (dx || dA), want_u = low && dB;
+    if (!dx && !(low && (dA || dB))) return;
+    AdaptEpi<T> e = epilogue(dx, lddx, p.d);
+    if (dx) epilogue_low(e, 1, A, false, f32);
+    if constexpr (f32) {
+      RowJob jw = row_job(W, p.ldw, dx ? p.classes : 0, p.d), jx = row_job(x, p.ldx, want_u ? p.tokens : 0, p.d),
+             jy = row_job(dy, lddy, dx || want_v ? p.tokens : 0, p.classes);
+      if (dx) to_planes(jw, l.w, l.ld_x, l.undo_w, 60);
+      if (want_u) to_low(jx, sx, A, 0);
+      if (jx.rows + jw.rows) run_rows(jx, jw);
+      if (dx) {
+        to_planes(jy, l.in[1], l.ld_y, l.undo_in, 100);
+        jy.fold = l.undo_w;  // W's planes are W over these
+      }
+      if (want_v) to_low(jy, sy, B, 1);
+      if (jy.rows) run_rows(jy, RowJob{});
+      if (dx) {
+        e.undo_row = l.undo_in;
+        product(sy, Tensor{l.in[1], p.classes, p.tokens, 2, l.ld_y, p.tokens * l.ld_y},
+                Tensor{l.w, p.d, p.classes, 2, l.ld_x, p.classes * l.ld_x}, true, 1, nullptr, false, e);
+      }
+      if (low && (dA || dB)) {
+        OuterJobsF32 o = {};
+        int n = 0, wide = 0;
+        if (dA) o.job[n++] = OuterJobF32{x, p.ldx, p.d, l.u[1], dA, (int64_t)p.rank * p.d, p.d, 1}, wide = p.d;
+        if (dB)
+          o.job[n++] = OuterJobF32{dy, lddy, p.classes, l.u[0], dB, (int64_t)p.rank * p.classes, 1, p.rank},
+          wide = std::max(wide, p.classes);
+        o.adapter = p.adapter;
+        o.tokens = p.tokens;
+        o.r = p.rank;
+        o.groups = (int)ceil_div(p.rank, 8);
+        launch_pdl(k_outer_f32, dim3((unsigned)(ceil_div(wide, 128) * o.groups), (unsigned)p.adapters, (unsigned)n),
+                   1024, s, o);
+        LC_LAUNCH_CHECK("k_outer_f32");
+      }
+    } else {
+      Tensor rx = {}, ry = {}, w = {}, fa = {}, fb = {};
+      if (dx || want_v || want_u) ry = rows_of(sy, 1);
+      if (low && (dA || dB)) rx = rows_of(sx, 0);
+      if (dx) w = head();
+      if (low && (dx || want_u)) fa = factor_a();
+      if (want_v) fb = factor_b();
+      if (want_u || want_v) {
+        Shrinking j[2];
+        int n = 0;
+        if (want_v) j[n++] = Shrinking{ry, fb, true, 1};
+        if (want_u) j[n++] = Shrinking{rx, fa, false, 0};
+        shrink(j, n);
+      }
+      if (dx) product(sy, ry, w, true, 1, low ? &fa : nullptr, true, e);
+      if (low && (dA || dB)) {
+        OuterJobs o = {};
+        int n = 0, wide = 0;
+        if (dA)
+          o.job[n++] = OuterJob{static_cast<const bf16*>(rx.base), rx.ld, (int)p.d, l.up[1], dA, (int64_t)p.rank * p.d, p.d, 1},
+          wide = p.d;
+        if (dB)
+          o.job[n++] = OuterJob{static_cast<const bf16*>(ry.base), ry.ld, (int)p.classes, l.up[0], dB,
+                                (int64_t)p.rank * p.classes, 1, p.rank},
+          wide = std::max(wide, p.classes);
+        o.adapter = p.adapter;
+        o.tokens = p.tokens;
+        o.ldc = l.ld_r;
+        o.plane = p.tokens * l.ld_r;
+        o.r = p.rank;
+        o.rb = p.rank <= 64 ? 64 : 128;
+        o.errors = mma::error_counter();
+        const int smem = 1024 + kOuterStages * (16384 + o.rb * 256) + 2 * kWindow + 128;
+        allow_smem(reinterpret_cast<const void*>(k_outer), 1024 + kOuterStages * (16384 + 128 * 256) + 2 * kWindow + 128);
+        launch_pdl_smem(k_outer, dim3((unsigned)ceil_div(wide, 128), (unsigned)p.adapters, (unsigned)n), kOuterThreads,
+                        smem, s, o);
+        LC_LAUNCH_CHECK("k_outer");
+      }
     }
-    if (low && (dx || (dB && dense()))) fa = factor_a();
-    if (low && dB) {
-      if (dense())
-        shrink_mma(sx, in_x, staged_x, fa, false, 0);
-      else
-        shrink(sx, A, 0, true, f32, !f32, nullptr);
-    }
-    if (dx) {
-      AdaptEpi<T> e = epilogue(dx, lddx, p.d);
-      if (f32) e.undo_row = l.undo_in;
-      product(sy, in_y, staged_y, w, true, 128, 1, low ? &fa : nullptr, true, e);
-    }
-    if (low && dA) outer(sx, 0, 1, dA, in_x, staged_x);
-    if (low && dB) outer(sy, 1, 0, dB, in_y, staged_y);
   }
 };
 

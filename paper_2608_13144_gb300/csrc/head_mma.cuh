@@ -109,24 +109,70 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
     ptx::mma_f16_pair(d, a, b, id, acc);
 }
 
-// Runs of neighbouring rows that share an adapter (head_adapt.cu): run i is
-// rows [off[i], off[i + 1]), its adapter g[i] (outside [0, G): none).
-struct Runs {
-  const int* off;
-  const int* g;
-  const int* count;
-};
-
-// The low-rank segments of a tile: for each run in it and each of `pairs`
-// plane pairs, A rows of the run times B of the run's adapter.
+// The low-rank segments of a tile: for each adapter among the tile's rows and
+// each of `pairs` plane pairs, the rows' factor times the adapter's, limited to
+// the adapter's rows. Tiles with more than kFewAdapters leave it to the
+// epilogue (`many`), which costs as much for any number.
+constexpr int kFewAdapters = 8;
 struct Low {
-  Runs runs;
-  int from_a = 0;     // the rows' factor is A itself (no other segments; a run's first MMA overwrites)
-  int G = 0;          // 0: no low-rank segments
+  const int32_t* adapter = nullptr;  // of each row
+  int64_t tokens = 0;
+  int G = 0;                         // 0: no low-rank segments
   int chunks = 0, last = 0;
   int pairs = 0;
-  int a_z[6], b_z[6];  // plane of each factor; B's z is b_z * G + adapter
+  int a_z[2], b_z[2];                // plane of each factor; B's z is b_z * G + adapter
   uint32_t idesc;
+};
+
+// The adapters among TM rows, one after another: lane l holds the adapters of
+// rows 32 k + l, -1 for none.
+template <int TM>
+struct Groups {
+  int id[TM / 32];
+  uint32_t rest[TM / 32];  // rows of adapters still to come
+  uint32_t on[TM / 32];    // rows of adapter g
+  int g;
+  __device__ __forceinline__ void begin(const int32_t* adapter, int64_t tokens, int G, int64_t m0, int lane) {
+#pragma unroll
+    for (int k = 0; k < TM / 32; ++k) {
+      const int64_t t = m0 + 32 * k + lane;
+      const int a = t < tokens ? __ldg(adapter + t) : -1;
+      id[k] = a < G ? a : -1;
+    }
+    again();
+  }
+  __device__ __forceinline__ void again() {
+#pragma unroll
+    for (int k = 0; k < TM / 32; ++k) rest[k] = __ballot_sync(0xffffffffu, id[k] >= 0);
+  }
+  __device__ __forceinline__ bool next() {
+    int found = -1;
+#pragma unroll
+    for (int k = TM / 32 - 1; k >= 0; --k) {
+      const int a = __shfl_sync(0xffffffffu, id[k], (__ffs(rest[k]) - 1) & 31);
+      if (rest[k]) found = a;
+    }
+    if (found < 0) return false;
+    g = found;
+#pragma unroll
+    for (int k = 0; k < TM / 32; ++k) {
+      on[k] = __ballot_sync(0xffffffffu, id[k] == found);
+      rest[k] &= ~on[k];
+    }
+    return true;
+  }
+  // whether there are more than `most` of them
+  __device__ __forceinline__ bool more_than(int most) {
+    int n = 0;
+    bool more = false;
+    while (next())
+      if (++n > most) {
+        more = true;
+        break;
+      }
+    again();
+    return more;
+  }
 };
 
 struct Args {
@@ -140,14 +186,12 @@ struct Args {
   int block;  // stages of each segment per block (DRAIN: all segments have the same stages)
   Seg seg[kMaxSegs];
   Low low;
-  const int* alt;              // nullable: where not 0, A is read by its second map
   unsigned long long* errors;  // expired waits, counted
 };
 
-// The operands' maps: A and what stands for it where *alt, B, the low-rank
-// segments' factors.
+// The operands' maps: A, B and the low-rank segments' factors.
 struct Maps {
-  CUtensorMap a, a2, b, la, lb;
+  CUtensorMap a, b, la, lb;
 };
 
 // Tile `t`: its first row and column (in tiles) and batch index.
@@ -171,19 +215,6 @@ __device__ __forceinline__ void tile_at(const Args& a, int t, int& mt, int& nt, 
   const int high = min(8, a.m_tiles - band * 8);
   nt = rest / high;
   mt = band * 8 + rest - nt * high;
-}
-
-// The first run that reaches past row m0.
-__device__ __forceinline__ int first_run(const Runs& r, int n, int m0) {
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(r.off + mid + 1) > m0)
-      hi = mid;
-    else
-      lo = mid + 1;
-  }
-  return lo;
 }
 
 template <int CG, bool DRAIN, typename Epi>
@@ -240,24 +271,24 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int per = a.sym ? a.m_tiles * (a.m_tiles + 1) / 2 : a.m_tiles * a.n_tiles;
   const int tiles = per * a.batches;
   const int chunks = a.nseg ? a.seg[0].chunks : 0;
-  const int n_runs = a.low.G ? __ldg(a.low.runs.count) : 0;
 
   if (warp == 0) {
     // ------------------------------------------------------------ producer
-    if (lane == 0) {
+    {  // the whole warp, converged, for the adapters' sake; lane 0 copies
       const uint32_t lead_full = CG == 2 ? ptx::mapa(full, 0) : full;
       int st = 0;
       uint32_t ph = 0;
       bool ok = true;
-      const CUtensorMap* ma = a.alt && __ldg(a.alt) ? &maps.a2 : &maps.a;
-      const CUtensorMap* mla = a.low.from_a ? ma : &maps.la;
       // one stage: the boxes of A at (row, k) and of B at (column, k)
       auto load = [&](const CUtensorMap* pa, bool a_mn, int row, int ak, int az, const CUtensorMap* pb, bool b_mn,
                       int col, int bk, int bz) {
-        ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, kWaitLimit);
+        ok = ptx::mbar_wait_warp(empty + 8 * st, ph ^ 1u, abort_s, kWaitLimit);
         if (!ok) return;
-        if (rank == 0) ptx::mbar_expect_tx(full + 8 * st, (uint32_t)(CG * (a.a_rows * 128 + b_bytes)));
-        const uint32_t sa = base + st * stage_bytes, sb = sa + kABytes, bar = lead_full + 8 * st;
+        const uint32_t slot = st;
+        if (++st == nst) st = 0, ph ^= 1u;
+        if (lane != 0) return;
+        if (rank == 0) ptx::mbar_expect_tx(full + 8 * slot, (uint32_t)(CG * (a.a_rows * 128 + b_bytes)));
+        const uint32_t sa = base + slot * stage_bytes, sb = sa + kABytes, bar = lead_full + 8 * slot;
         auto box = [&](uint32_t dst, const CUtensorMap* m, int x, int y, int z) {
           if (CG == 2)
             load_3d_pair(dst, m, x, y, z, bar);
@@ -275,7 +306,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         } else {
           box(sb, pb, bk, col, bz);
         }
-        if (++st == nst) st = 0, ph ^= 1u;
       };
       for (int t = worker; t < tiles && ok; t += workers) {
         int mt, nt, z;
@@ -286,22 +316,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Seg& sg = a.seg[s];
             const int c1 = min(c0 + a.block, sg.chunks);
             for (int c = c0; c < c1 && ok; ++c)
-              load(ma, a.a_mn, row, c * kChunk, sg.a_z + z, &maps.b, a.b_mn, col, c * kChunk, sg.b_z + z);
+              load(&maps.a, a.a_mn, row, c * kChunk, sg.a_z + z, &maps.b, a.b_mn, col, c * kChunk, sg.b_z + z);
           }
-        if (n_runs) {
-          const int m0 = mt * TM;
-          for (int i = first_run(a.low.runs, n_runs, m0); i < n_runs && ok; ++i) {
-            if (__ldg(a.low.runs.off + i) >= m0 + TM) break;
-            const int g = __ldg(a.low.runs.g + i);
-            if (g < 0 || g >= a.low.G) continue;
-            for (int q = 0; q < a.low.pairs && ok; ++q)
-              for (int c = 0; c < a.low.chunks && ok; ++c)
-                load(mla, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk,
-                     a.low.b_z[q] * a.low.G + g);
-          }
+        if (a.low.G) {
+          Groups<TM> gr;
+          gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
+          if (!gr.more_than(kFewAdapters))
+            while (ok && gr.next())
+              for (int q = 0; q < a.low.pairs && ok; ++q)
+                for (int c = 0; c < a.low.chunks && ok; ++c)
+                  load(&maps.la, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk,
+                       a.low.b_z[q] * a.low.G + gr.g);
         }
       }
     }
+    __syncwarp();
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
     if (rank == 0) {
@@ -341,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int k = 0; k < steps; ++k, da += ia, db += ib) {
               if (off) {
                 const uint32_t o[8] = {off[0], off[1], off[2], off[3], off[4], off[5], off[6], off[7]};
-                mma_masked<CG>(d, da, db, id, acc, o);
+                mma_masked<CG>(d, da, db, id, 1u, o);
               } else {
                 mma<CG>(d, da, db, id, acc);
               }
@@ -367,25 +396,18 @@ __global__ void __launch_bounds__(kThreads, 1)
               chunk(a.a_mn, a.b_mn, sg.idesc, c == sg.chunks - 1 ? sg.last : 4, nullptr);
           }
         }
-        if (n_runs) {
-          const int m0 = mt * TM;
-          for (int i = first_run(a.low.runs, n_runs, m0); i < n_runs && ok; ++i) {
-            const int r0 = __ldg(a.low.runs.off + i) - m0, r1 = __ldg(a.low.runs.off + i + 1) - m0;
-            if (r0 >= TM) break;
-            const int g = __ldg(a.low.runs.g + i);
-            if (g < 0 || g >= a.low.G) continue;
-            uint32_t off[8];
+        if (a.low.G) {
+          Groups<TM> gr;
+          gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
+          if (!gr.more_than(kFewAdapters))
+            while (ok && gr.next()) {
+              uint32_t off[8] = {};
 #pragma unroll
-            for (int w = 0; w < 8; ++w) {
-              const int lo = min(max(r0 - 32 * w, 0), 32), hi = min(max(r1 - 32 * w, 0), 32);
-              const uint32_t on = (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~(lo == 32 ? 0xffffffffu : (1u << lo) - 1u);
-              off[w] = ~on;
+              for (int k = 0; k < TM / 32; ++k) off[k] = ~gr.on[k];
+              for (int q = 0; q < a.low.pairs && ok; ++q)
+                for (int c = 0; c < a.low.chunks && ok; ++c)
+                  chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, off);
             }
-            if (a.low.from_a) acc = 0;
-            for (int q = 0; q < a.low.pairs && ok; ++q)
-              for (int c = 0; c < a.low.chunks && ok; ++c)
-                chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, off);
-          }
         }
         close();
       }
@@ -410,6 +432,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       int mt, nt, z;
       tile_at(a, t, mt, nt, z);
       const int row = mt * TM + (int)rank * 128 + quarter * 32;
+      bool many = false;
+      if (a.low.G) {
+        Groups<TM> gr;
+        gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
+        many = gr.more_than(kFewAdapters);
+      }
       uint32_t src = 0;
       auto open = [&]() {
         ok = ptx::mbar_wait(acc_full + 8 * (n & 1), (uint32_t)((n >> 1) & 1), abort_s, kWaitLimit);
@@ -457,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[i][j]);
-          epi.store(row, nt * a.bn + c, z, lane, v);
+          epi.store(row, nt * a.bn + c, z, lane, many, v);
         }
       } else {
         open();
@@ -466,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t v[32];
           ptx::tmem_ld32(src + c, v);
           ptx::tmem_wait_ld();
-          epi.store(row, nt * a.bn + c, z, lane, v);
+          epi.store(row, nt * a.bn + c, z, lane, many, v);
         }
         close();
       }

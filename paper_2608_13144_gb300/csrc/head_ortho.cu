@@ -247,7 +247,7 @@ struct SymEpi {
   int m, tile;
   float f, b;
   const float* t;  // nullable: squared into f
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = m - col0;
     if (left <= 0) return;
     float g = f;
@@ -273,7 +273,7 @@ struct UpdateEpi {
   int rows, cols;
   float f, a;
   const float* t;
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
     const float u = t ? t[z] : 1.f, g = f * u;
@@ -296,7 +296,7 @@ struct LastEpi {
   int rows, cols, vec;
   float f, a, keep, rate;
   const float* t;
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
     const float u = t ? t[z] : 1.f, g = f * u;
@@ -364,9 +364,9 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
   const CUtensorMap ma = mma::tensor_map(A, a_mn ? 64 : 128);
   const CUtensorMap mb = mma::tensor_map(B, b_mn ? 64 : pair ? 128 : a.bn);
   if (pair)
-    mma::launch<2, PLANES == 2>({ma, ma, mb, ma, mb}, a, epi, s);
+    mma::launch<2, PLANES == 2>({ma, mb, ma, mb}, a, epi, s);
   else
-    mma::launch<1, PLANES == 2>({ma, ma, mb, ma, mb}, a, epi, s);
+    mma::launch<1, PLANES == 2>({ma, mb, ma, mb}, a, epi, s);
 }
 
 template <typename T, int VEC, int PLANES>
