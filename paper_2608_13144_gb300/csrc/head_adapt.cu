@@ -465,49 +465,66 @@ struct AdaptEpi {
   int G, r, f_vec, always;
   int64_t f_col, f_j;
 
+  // element i of a 16-byte vector
+  static __device__ __forceinline__ float part(const uint4& q, int i) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    return __uint_as_float(sizeof(T) == 4 ? w[i % 4] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+  // v += the row's low-rank product in 32 columns, `left` of them in the matrix
+  // (loads in groups of eight, all of a group in flight; past the matrix the
+  // last column is read again).
   __device__ __forceinline__ void low(int64_t p, int col0, int left, float (&v)[32]) const {
     constexpr int N = 16 / sizeof(T);
     const int g = __ldg(adapter + p);
     if (g < 0 || g >= G) return;
     const T* f = F + (int64_t)g * cols * r + col0 * f_col;
     const float* up = u + p * r;
+    const int last = min(left, 32) - 1;
     if (f_vec && f_j == 1) {
       for (int k = 0; k < r; k += N) {
         float uk[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) uk[i] = __ldg(up + k + i);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          if (j >= left) break;
-          const uint4 q = __ldg(reinterpret_cast<const uint4*>(f + j * r + k));
-          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        for (int j0 = 0; j0 < 32; j0 += 8) {
+          uint4 q[8];
 #pragma unroll
-          for (int i = 0; i < N; ++i)
-            v[j] = fmaf(uk[i], __uint_as_float(sizeof(T) == 4 ? w[i % 4] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16),
-                        v[j]);
+          for (int j = 0; j < 8; ++j) q[j] = __ldg(reinterpret_cast<const uint4*>(f + min(j0 + j, last) * r + k));
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[j0 + j] = fmaf(uk[i], part(q[j], i), v[j0 + j]);
         }
       }
     } else if (f_vec) {
-#pragma unroll 2
-      for (int k = 0; k < r; ++k) {
-        const float uk = __ldg(up + k);
+      const int end = last / N * N;  // (rows are whole vectors)
+      for (int k = 0; k < r; k += 2) {
+        const bool two = k + 1 < r;
+        const float u0 = __ldg(up + k), u1 = two ? __ldg(up + k + 1) : 0.f;
+        const T *f0 = f + k * f_j, *f1 = two ? f0 + f_j : f0;
+        uint4 q[2][32 / N];
 #pragma unroll
         for (int j = 0; j < 32; j += N) {
-          if (j >= left) break;  // (rows are whole vectors)
-          const uint4 q = __ldg(reinterpret_cast<const uint4*>(f + k * f_j + j));
-          const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+          q[0][j / N] = __ldg(reinterpret_cast<const uint4*>(f0 + min(j, end)));
+          q[1][j / N] = __ldg(reinterpret_cast<const uint4*>(f1 + min(j, end)));
+        }
 #pragma unroll
-          for (int i = 0; i < N; ++i)
-            v[j + i] = fmaf(uk, __uint_as_float(sizeof(T) == 4 ? w[i % 4] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16),
-                            v[j + i]);
+        for (int j = 0; j < 32; ++j) {
+          v[j] = fmaf(u0, part(q[0][j / N], j % N), v[j]);
+          if (two) v[j] = fmaf(u1, part(q[1][j / N], j % N), v[j]);
         }
       }
     } else {
       for (int k = 0; k < r; ++k) {
         const float uk = __ldg(up + k);
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j < left) v[j] = fmaf(uk, to_f32<T>(f[j * f_col + k * f_j]), v[j]);
+        for (int j0 = 0; j0 < 32; j0 += 8) {
+          float q[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) q[j] = to_f32<T>(f[min(j0 + j, last) * f_col + k * f_j]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j0 + j] = fmaf(uk, q[j], v[j0 + j]);
+        }
       }
     }
   }
@@ -535,6 +552,16 @@ struct AdaptEpi {
     if (u && (always || many)) low(p, col0, left, v);
     T* o = y + p * ldy + col0;
     constexpr int kVec = 16 / sizeof(T);
+    if (vec && left >= 32) {
+#pragma unroll
+      for (int q = 0; q < 32 / kVec; ++q) {
+        __align__(16) T h[kVec];
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) h[j] = from_f32<T>(v[q * kVec + j]);
+        *reinterpret_cast<uint4*>(o + q * kVec) = *reinterpret_cast<const uint4*>(h);
+      }
+      return;
+    }
 #pragma unroll
     for (int q = 0; q < 32 / kVec; ++q) {
       if (q * kVec >= left) break;
