@@ -115,19 +115,17 @@ __device__ __forceinline__ void row_planes(const RowJob& a, const float* r, int6
   for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
     float v[VEC];
     get(i, v);
-    __align__(8) __half hi[VEC], lo[VEC];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      v[k] *= f;
-      hi[k] = __float2half_rn(v[k]);
-      lo[k] = __float2half_rn(v[k] - __half2float(hi[k]));
-    }
-    if (VEC == 4) {
-      *reinterpret_cast<uint2*>(o + i) = *reinterpret_cast<uint2*>(hi);
-      *reinterpret_cast<uint2*>(o + a.plane + i) = *reinterpret_cast<uint2*>(lo);
+    for (int k = 0; k < VEC; ++k) v[k] *= f;
+    if constexpr (VEC == 4) {
+      uint32_t hi[2], lo[2];
+      split_f16(v, hi, lo);
+      *reinterpret_cast<uint2*>(o + i) = uint2{hi[0], hi[1]};
+      *reinterpret_cast<uint2*>(o + a.plane + i) = uint2{lo[0], lo[1]};
     } else {
-      o[i] = hi[0];
-      o[a.plane + i] = lo[0];
+      const __half hi = __float2half_rn(v[0]);
+      o[i] = hi;
+      o[a.plane + i] = __float2half_rn(v[0] - __half2float(hi));
     }
   }
   if (lane == 0) a.undo[row] = ldexpf(1.f, -e);
@@ -416,23 +414,22 @@ __global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_const
       if (t >= a.tokens) continue;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        __align__(16) uint16_t hi[8], lo[8];
+        float f[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const int j = j0 + q * 8 + k;
-          float f = __uint_as_float(v[q * 8 + k]);
+          f[k] = __uint_as_float(v[q * 8 + k]);
           if (j < a.rn)
-            for (uint32_t p = 1; p < splits; ++p) f += part[((p - 1) * a.rn + j) * 128 + row];
-          f = any && j < a.r ? s * f : 0.f;
-          if (j < a.r) job.u[t * a.r + j] = f;
-          const bf16 h = __float2bfloat16_rn(f);
-          hi[k] = __bfloat16_as_ushort(h);
-          lo[k] = __bfloat16_as_ushort(__float2bfloat16_rn(f - __bfloat162float(h)));
+            for (uint32_t p = 1; p < splits; ++p) f[k] += part[((p - 1) * a.rn + j) * 128 + row];
+          f[k] = any && j < a.r ? s * f[k] : 0.f;
+          if (j < a.r) job.u[t * a.r + j] = f[k];
         }
         if (j0 + q * 8 < a.ldo) {
+          uint32_t hi[4], lo[4];
+          split_bf16(f, hi, lo);
           uint16_t* o = job.planes + t * a.ldo + j0 + q * 8;
-          *reinterpret_cast<uint4*>(o) = *reinterpret_cast<uint4*>(hi);
-          *reinterpret_cast<uint4*>(o + a.plane) = *reinterpret_cast<uint4*>(lo);
+          *reinterpret_cast<uint4*>(o) = uint4{hi[0], hi[1], hi[2], hi[3]};
+          *reinterpret_cast<uint4*>(o + a.plane) = uint4{lo[0], lo[1], lo[2], lo[3]};
         }
       }
     }
@@ -553,13 +550,11 @@ struct AdaptEpi {
     T* o = y + p * ldy + col0;
     constexpr int kVec = 16 / sizeof(T);
     if (vec && left >= 32) {
+      uint32_t w[8 * sizeof(T)];
+      round_to<T>(v, w);
 #pragma unroll
-      for (int q = 0; q < 32 / kVec; ++q) {
-        __align__(16) T h[kVec];
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) h[j] = from_f32<T>(v[q * kVec + j]);
-        *reinterpret_cast<uint4*>(o + q * kVec) = *reinterpret_cast<const uint4*>(h);
-      }
+      for (int q = 0; q < 32 / kVec; ++q)
+        *reinterpret_cast<uint4*>(o + q * kVec) = uint4{w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]};
       return;
     }
 #pragma unroll

@@ -64,14 +64,15 @@ unsigned long long* error_counter() {
   return static_cast<unsigned long long*>(p);
 }
 
-CUtensorMap tensor_map(const Tensor& t, int box_rows) {
+CUtensorMap tensor_map(const Tensor& t, int box_rows, int box_cols) {
   CUtensorMap map;
   const cuuint64_t dims[3] = {(cuuint64_t)t.cols, (cuuint64_t)t.rows, (cuuint64_t)t.planes};
   const cuuint64_t strides[2] = {(cuuint64_t)t.ld * 2, (cuuint64_t)(t.planes > 1 ? t.plane : t.ld * t.rows) * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
   // (16-bit elements of either kind: the copy only moves them)
   const CUresult r = encoder()(&map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(t.base), dims, strides, box,
-                               step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                               step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   LC_REQUIRE(r == CUDA_SUCCESS, LIPCACHE_E_CUDA, "cuTensorMapEncodeTiled failed: " + std::to_string((int)r));
   return map;

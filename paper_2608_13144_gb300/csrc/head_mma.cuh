@@ -80,6 +80,33 @@ __device__ __forceinline__ void load_3d_pair(uint32_t dst, const CUtensorMap* ma
       : "memory");
 }
 
+__device__ __forceinline__ void store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                   reinterpret_cast<uint64_t>(map)),
+               "r"(x), "r"(y), "r"(z), "r"(src)
+               : "memory");
+}
+
+// Eight FP32 columns of this thread's lane, read and written.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+  ptx::tmem_wait_ld();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+               "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+               "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])),
+               "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+               : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // The MMA with a mask of output lanes (rows) to leave alone; `off` holds the
 // lanes of this CTA (CG = 1) or of both (CG = 2), 32 a word.
 template <int CG>
@@ -531,8 +558,9 @@ struct Tensor {
   const void* base;
   int64_t cols, rows, planes, ld, plane;
 };
-// Its map with a box of 64 x box_rows.
-CUtensorMap tensor_map(const Tensor& t, int box_rows);
+// Its map with a box of 64 x box_rows (128-byte swizzle), or of 32 x box_rows
+// (64-byte swizzle).
+CUtensorMap tensor_map(const Tensor& t, int box_rows, int box_cols = 64);
 inline bool mappable(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
 inline Seg segment(int64_t k, int a_z, int b_z, uint32_t id) {

@@ -24,13 +24,14 @@ namespace lc {
 namespace ops {
 namespace {
 
-constexpr int kParts = 128;      // partial sums of squares of a matrix, at most
+constexpr int kParts = 512;      // partial sums of squares of a matrix, at most
 constexpr float kXScale = 8192.f, kSScale = 1024.f;
 constexpr int kBlock = 4;  // stages of 64 summed on the tensor cores at a time, FP32 matrices
 
 struct OrthoLayout {
   __half *x[2], *s, *p;  // planes x batch x rows x ld
   float* t;              // batch: the rest of the normalisation
+  unsigned* phases;      // CTAs past each phase of k_iterate
   double* part;          // batch x kParts
   int64_t ld, sld, x_plane, s_plane;
   void take(Carve& c, int planes, int64_t batch, int rows, int cols) {
@@ -44,6 +45,7 @@ struct OrthoLayout {
     c.take(s, (size_t)(planes * batch * s_plane));
     c.take(p, (size_t)(planes * batch * s_plane));
     c.take(t, (size_t)batch);
+    c.take(phases, 1);
     c.take(part, (size_t)batch * kParts);
   }
 };
@@ -80,6 +82,7 @@ struct Direction {
   int rows, cols;
   int64_t ldg;
   int units;      // of VEC elements in a row
+  int tail;       // elements past the units (one row)
   OrthoStep st;
 };
 
@@ -103,6 +106,7 @@ __device__ __forceinline__ void direction(const Direction& a, const T* g, int64_
 
 // The new momentum, and each block's sum of squares of D (runs of eight to 64
 // in FP32, those in FP64, in a fixed order).
+// A dense matrix may be given as one row.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) k_squares(const T* g, const Direction a, double* part) {
   __shared__ double red[8];
@@ -130,6 +134,11 @@ __global__ void __launch_bounds__(256) k_squares(const T* g, const Direction a, 
     if ((++k & 7) == 0) sum += (double)run, run = 0.f;
   }
   sum += (double)run;
+  if (blockIdx.x == 0 && threadIdx.x < a.tail) {
+    float v[1];
+    direction<T, 1, true>(a, g, row0, a.units * VEC + threadIdx.x, v);
+    sum += (double)v[0] * v[0];
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
@@ -144,10 +153,11 @@ __global__ void __launch_bounds__(256) k_squares(const T* g, const Direction a, 
 template <typename T, int VEC, int PLANES>
 __global__ void __launch_bounds__(256)
     k_planes(const T* g, const Direction a, const double* part, int parts, double eps, __half* x,
-             int64_t ld, int64_t plane, float* t) {
+             int64_t ld, int64_t plane, float* t, unsigned* phases) {
   __shared__ float factor;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *phases = 0;
   if (threadIdx.x < 32) {
     double sum = 0.0;
     for (int i = threadIdx.x; i < parts; i += 32) sum += part[blockIdx.y * parts + i];
@@ -171,53 +181,55 @@ __global__ void __launch_bounds__(256)
     const int col = (int)(i - r * (uint32_t)a.units) * VEC;
     float v[VEC];
     direction<T, VEC, false>(a, g, row0 + r, col, v);
-    __half hi[VEC], lo[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      hi[j] = __float2half_rn(v[j] * f);
-      lo[j] = __float2half_rn(fmaf(v[j], f, -__half2float(hi[j])));
-    }
     __half* d = x + (row0 + r) * ld + col;
-    if (VEC == 8) {
-      *reinterpret_cast<uint4*>(d) = *reinterpret_cast<uint4*>(hi);
-      if (PLANES == 2) *reinterpret_cast<uint4*>(d + plane) = *reinterpret_cast<uint4*>(lo);
-    } else {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        d[j] = hi[j];
-        if (PLANES == 2) d[plane + j] = lo[j];
-      }
+    for (int j = 0; j < VEC; ++j) v[j] *= f;  // a power of two
+    if constexpr (VEC == 8) {
+      uint32_t hi[4], lo[4];
+      split_f16(v, hi, lo);
+      *reinterpret_cast<uint4*>(d) = uint4{hi[0], hi[1], hi[2], hi[3]};
+      if (PLANES == 2) *reinterpret_cast<uint4*>(d + plane) = uint4{lo[0], lo[1], lo[2], lo[3]};
+    } else {
+      const __half hi = __float2half_rn(v[0]);
+      d[0] = hi;
+      if (PLANES == 2) d[plane] = __float2half_rn(v[0] - __half2float(hi));
     }
   }
 }
 
 // ---------------------------------------------------------------- epilogues
-// 32 neighbouring values of a row as FP16 planes; columns past `cols` may be
-// written up to the row's stride.
+// 32 columns of a row (`left` of them in the matrix; up to the row's stride may
+// be written) as planes, and mirrored: down a column of stride ld, 32 lanes
+// side by side.
 template <int PLANES>
-__device__ __forceinline__ void store_planes(__half* d, int64_t plane, int left, const float (&v)[32]) {
+__device__ __forceinline__ void put_planes(__half* d, int64_t plane, __half* mirror, int64_t ld, int left,
+                                           const float (&v)[32]) {
+  uint32_t hi[16], lo[16];
+  split_f16(v, hi, lo);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     if (q * 8 >= left) break;
-    __half hi[8], lo[8];
+    *reinterpret_cast<uint4*>(d + q * 8) = uint4{hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]};
+    if (PLANES == 2)
+      *reinterpret_cast<uint4*>(d + plane + q * 8) = uint4{lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]};
+  }
+  if (mirror) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      hi[j] = __float2half_rn(v[q * 8 + j]);
-      lo[j] = __float2half_rn(v[q * 8 + j] - __half2float(hi[j]));
+    for (int j = 0; j < 32; ++j) {
+      if (j >= left) break;
+      mirror[j * ld] = __ushort_as_half((uint16_t)(hi[j / 2] >> (j & 1) * 16));
+      if (PLANES == 2) mirror[plane + j * ld] = __ushort_as_half((uint16_t)(lo[j / 2] >> (j & 1) * 16));
     }
-    *reinterpret_cast<uint4*>(d + q * 8) = *reinterpret_cast<uint4*>(hi);
-    if (PLANES == 2) *reinterpret_cast<uint4*>(d + plane + q * 8) = *reinterpret_cast<uint4*>(lo);
   }
 }
-// The same 32 values down a column (row stride ld): 32 lanes write neighbours.
-template <int PLANES>
-__device__ __forceinline__ void store_planes_t(__half* d, int64_t ld, int64_t plane, int left, const float (&v)[32]) {
+// v += f (eight FP16 values)
+__device__ __forceinline__ void add_f16(const uint4& w, float f, float* v) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    if (j >= left) break;
-    const __half hi = __float2half_rn(v[j]);
-    d[j * ld] = hi;
-    if (PLANES == 2) d[plane + j * ld] = __float2half_rn(v[j] - __half2float(hi));
+  for (int i = 0; i < 4; ++i) {
+    const float2 h = open_f16(x[i]);
+    v[2 * i] = fmaf(f, h.x, v[2 * i]);
+    v[2 * i + 1] = fmaf(f, h.y, v[2 * i + 1]);
   }
 }
 // v += f (the values of the planes)
@@ -226,15 +238,9 @@ __device__ __forceinline__ void add_planes(const __half* d, int64_t plane, int l
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     if (q * 8 >= left) break;
-    uint4 w = *reinterpret_cast<const uint4*>(d + q * 8);
-    const __half* h = reinterpret_cast<const __half*>(&w);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[q * 8 + j] = fmaf(f, __half2float(h[j]), v[q * 8 + j]);
-    if (PLANES == 2) {
-      w = *reinterpret_cast<const uint4*>(d + plane + q * 8);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[q * 8 + j] = fmaf(f, __half2float(h[j]), v[q * 8 + j]);
-    }
+    const uint4 w = __ldcg(reinterpret_cast<const uint4*>(d + q * 8));
+    add_f16(w, f, &v[q * 8]);
+    if (PLANES == 2) add_f16(__ldcg(reinterpret_cast<const uint4*>(d + plane + q * 8)), f, &v[q * 8]);
   }
 }
 
@@ -251,16 +257,15 @@ struct SymEpi {
     const int row = row0 + lane, left = m - col0;
     if (left <= 0) return;
     float g = f;
-    if (t) g *= t[z] * t[z];
+    if (t) g *= __ldcg(t + z) * __ldcg(t + z);
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = g * __uint_as_float(acc[j]);
     const int64_t at = z * mat + row * ld + col0;
-    if (row < m) {
-      if (of) add_planes<PLANES>(of + at, plane, left, b, v);
-      store_planes<PLANES>(d + at, plane, left, v);
-    }
-    if (row0 / tile != col0 / tile && row < m) store_planes_t<PLANES>(d + z * mat + col0 * ld + row, ld, plane, left, v);
+    if (row >= m) return;
+    if (of) add_planes<PLANES>(of + at, plane, left, b, v);
+    const bool off_diagonal = row0 / tile != col0 / tile;
+    put_planes<PLANES>(d + at, plane, off_diagonal ? d + z * mat + col0 * ld + row : nullptr, ld, left, v);
   }
 };
 
@@ -276,13 +281,13 @@ struct UpdateEpi {
   __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
-    const float u = t ? t[z] : 1.f, g = f * u;
+    const float u = t ? __ldcg(t + z) : 1.f, g = f * u;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = g * __uint_as_float(acc[j]);
     const int64_t at = z * mat + row * ld + col0;
     add_planes<PLANES>(x + at, plane, left, a * u, v);
-    store_planes<PLANES>(d + at, plane, left, v);
+    put_planes<PLANES>(d + at, plane, nullptr, 0, left, v);
   }
 };
 
@@ -299,7 +304,7 @@ struct LastEpi {
   __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
-    const float u = t ? t[z] : 1.f, g = f * u;
+    const float u = t ? __ldcg(t + z) : 1.f, g = f * u;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = g * __uint_as_float(acc[j]);
@@ -321,10 +326,8 @@ struct LastEpi {
         if (sizeof(T) == 4) {
           store_vec<8>(reinterpret_cast<float*>(d + at + q * 8), o);
         } else {
-          T h[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) h[j] = from_f32<T>(o[j]);
-          *reinterpret_cast<uint4*>(d + at + q * 8) = *reinterpret_cast<uint4*>(h);
+          *reinterpret_cast<uint4*>(d + at + q * 8) =
+              uint4{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7])};
         }
       } else {
 #pragma unroll
@@ -337,6 +340,660 @@ struct LastEpi {
     }
   }
 };
+
+// The power of two P carries: |P| <= 16 |b| + 256 |c| for singular values up
+// to 4 stays below 2^15.
+float poly_scale(float b, float c) {
+  const float bound = 16.f * fabsf(b) + 256.f * fabsf(c);
+  return exp2f(floorf(fminf(12.f, log2f(32768.f / fmaxf(bound, 1.f)))));
+}
+
+// ---------------------------------------------------------------- one launch
+// Matrices whose tiles do not fill the device several times over: all steps in
+// one cooperative launch, their products (phases) parted by a barrier over the
+// grid. 128 x 128 tiles, one CTA each; a stage holds 64 of the contracted
+// index of every plane of both operands, so that the three products of FP32
+// planes read each once. Where a phase has few tiles, a cluster of `split`
+// CTAs shares one: each sums a part of the contracted index, and the parts
+// meet in the shared memory of the CTA that writes that slice of the tile's
+// columns. The epilogue is a loop over eight columns, with its sums in tensor
+// memory: straight-line code for a whole tile is fetched anew in every phase
+// (it took 10 to 30 us a phase). Bound by the phases' latency (a barrier, the first loads, the join,
+// the writes: 4 to 6 us) until the products take longer.
+constexpr int kCluster = 4;
+constexpr int kTile = 128, kTileBytes = 128 * 128;
+// What a warp of the epilogue has to itself: others' parts of its 32 rows (three
+// of 32 + 4 columns, or one of 64 + 4), then what it sends to memory.
+constexpr int kPartBytes = 14 * 1024;
+
+struct IterateArgs {
+  CUtensorMap xk[2], xm[2], s, p;  // X's two buffers K-major and MN-major (boxes of 128 and 64 rows)
+  CUtensorMap to[4];               // X's buffers, S and P to write to (boxes of 32 x 32)
+  int tall, batch, m, n, steps;
+  int split[3];                    // of S, P and X' phases
+  float coef[3 * LIPCACHE_MAX_NS_STEPS], ps[LIPCACHE_MAX_NS_STEPS];
+  const float* t;
+  void* out;
+  const void* weight;
+  int rows, cols, vec;
+  float keep, rate;
+  unsigned* phases;
+  unsigned long long* errors;
+};
+
+__device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_release(unsigned* p) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
+}
+// Waits until `want` CTAs have passed; false when it gives up.
+__device__ __forceinline__ bool wait_phase(const unsigned* p, unsigned want, volatile int* abort) {
+  const long long t0 = clock64();
+  while (load_acquire(p) < want) {
+    if (*abort) return false;
+    if (clock64() - t0 > mma::kWaitLimit) {
+      *abort = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+// The same as the result, or the weights' update, in the caller's type.
+template <typename TO>
+__device__ __forceinline__ void put_result(const IterateArgs& a, int64_t at, int left, const float (&v)[32]) {
+  TO* o = static_cast<TO*>(a.out) + at;
+  const TO* w = a.weight ? static_cast<const TO*>(a.weight) + at : nullptr;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (q * 8 >= left) break;
+    float r[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = v[q * 8 + j];
+    if (a.vec) {
+      if (w) {
+        float old[8];
+        load_vec<TO, 8>(w + q * 8, old);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = fmaf(a.keep, old[j], -a.rate * r[j]);
+      }
+      if constexpr (sizeof(TO) == 4) {
+        store_vec<8>(reinterpret_cast<float*>(o + q * 8), r);
+      } else {
+        *reinterpret_cast<uint4*>(o + q * 8) =
+            uint4{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3]), pack_bf16(r[4], r[5]), pack_bf16(r[6], r[7])};
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (q * 8 + j < left) o[q * 8 + j] = from_f32<TO>(w ? fmaf(a.keep, to_f32<TO>(w[q * 8 + j]), -a.rate * r[j]) : r[j]);
+    }
+  }
+}
+
+// Counts the epilogue's warps as they pass; true for the eighth (nobody waits,
+// so that a warp that has given up holds up no other).
+__device__ __forceinline__ bool last_of_eight(uint32_t* count) {
+  __threadfence_block();
+  if (atomicAdd(count, 1u) + 1 < mma::kEpiWarps) return false;
+  *reinterpret_cast<volatile uint32_t*>(count) = 0;
+  __threadfence_block();
+  return true;
+}
+
+template <int PLANES, typename TO>
+__global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_constant__ IterateArgs a) {
+  constexpr int kStageBytes = 2 * PLANES * kTileBytes, kStages = PLANES == 2 ? 2 : 5;
+  constexpr int kSendBytes = 4096 * PLANES;  // a block of 32 x 32 and its mirror image, in planes
+  constexpr int kRegionBytes = 4 * kPartBytes > 8 * kSendBytes ? 4 * kPartBytes : 8 * kSendBytes;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t region = base + kStages * kStageBytes;
+  const uint32_t full = region + kRegionBytes, empty = full + 8 * kStages, acc_full = empty + 8 * kStages,
+                 acc_empty = acc_full + 16, ready = acc_empty + 16, got = ready + 8, drain = got + 8,
+                 go = drain + 8, misc = go + 8;
+  unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
+  volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
+  volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
+  uint32_t* counts = reinterpret_cast<uint32_t*>(misc_p + 8);  // warps done with what is added, with the phase
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)ptx::cluster_ctarank();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      ptx::mbar_init(full + 8 * s, 1);
+      ptx::mbar_init(empty + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(acc_full + 8 * b, 1);
+      ptx::mbar_init(acc_empty + 8 * b, mma::kEpiWarps);
+    }
+    // the join: every CTA is done with the parts of the join before; the others' parts are here
+    ptx::mbar_init(ready, kCluster * mma::kEpiWarps);
+    ptx::mbar_init(got, (kCluster - 1) * mma::kEpiWarps);
+    ptx::mbar_init(drain, 1);
+    ptx::mbar_init(go, 1);  // the producer has seen the barrier over the grid
+    *abort_s = 0;
+    counts[0] = counts[1] = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(misc, 512);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  ptx::cluster_sync();
+  ptx::wait_prerequisites();
+  const uint32_t tmem = *tmem_slot;
+  const int mt = (a.m + kTile - 1) / kTile, ntl = (a.n + kTile - 1) / kTile;
+  const int rows_t = a.tall ? ntl : mt, cols_t = a.tall ? mt : ntl;  // tiles of X as it is stored
+  const int sym = mt * (mt + 1) / 2;
+
+  // The work of a phase, the same for every role: `f(first block of 128 rows,
+  // of columns, z, first chunk, chunks)` for each of this CTA's tiles.
+  struct Work {
+    int kind, split, tiles, chunks, workers, me;
+  };
+  auto phase_of = [&](int i, int k) {
+    Work w;
+    w.kind = k == 2 ? (i == a.steps - 1 ? 3 : 2) : k;
+    w.split = a.split[k];
+    w.tiles = (k == 2 ? rows_t * cols_t : sym) * a.batch;
+    w.chunks = ((k == 0 ? a.n : a.m) + 63) / 64;
+    w.workers = w.split > 1 ? (int)gridDim.x / kCluster : (int)gridDim.x;
+    w.me = w.split > 1 ? (int)blockIdx.x / kCluster : (int)blockIdx.x;
+    return w;
+  };
+  // (a split of two uses half the cluster)
+  auto tile = [&](const Work& w, int t, int& r, int& c, int& z) {
+    if (w.kind < 2) {
+      z = t / sym;
+      t -= z * sym;
+      c = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+      while (c * (c + 1) / 2 > t) --c;
+      while ((c + 1) * (c + 2) / 2 <= t) ++c;
+      r = t - c * (c + 1) / 2;
+    } else {
+      const int per = rows_t * cols_t;
+      z = t / per;
+      t -= z * per;
+      r = t / cols_t;
+      c = t - r * cols_t;
+    }
+  };
+  auto range = [&](const Work& w, int& c0, int& c1) {
+    const int part = w.split > 1 ? rank : 0;
+    c0 = part >= w.split ? 0 : w.chunks * part / w.split;
+    c1 = part >= w.split ? 0 : w.chunks * (part + 1) / w.split;
+  };
+
+  // whether this CTA's tiles have something added to the product
+  auto adds = [&](const Work& w) { return w.kind > 0 && (w.split == 1 || rank < w.split); };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ producer
+    if (lane == 0) {
+      int st = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int i = 0; i < a.steps && ok; ++i)
+        for (int k = 0; k < 3 && ok; ++k) {
+          const Work w = phase_of(i, k);
+          const bool kx = i & 1;
+          ok = wait_phase(a.phases, (unsigned)(3 * i + k) * gridDim.x, abort_s);
+          if (!ok) break;
+          ptx::mbar_arrive(go);
+          asm volatile("fence.proxy.async.global;" ::: "memory");
+          const bool amn = k == 0 && a.tall, bmn = amn || (k == 2 && !a.tall);
+          const CUtensorMap* ma = k == 0 ? (a.tall ? &a.xm[kx] : &a.xk[kx]) : k == 1 ? &a.s : a.tall ? &a.xk[kx] : &a.p;
+          const CUtensorMap* mb = k == 0 ? ma : k == 1 ? &a.s : a.tall ? &a.p : &a.xm[kx];
+          int c0, c1;
+          range(w, c0, c1);
+          for (int t = w.me; t < w.tiles && ok; t += w.workers) {
+            int r, c, z;
+            tile(w, t, r, c, z);
+            for (int q = c0; q < c1 && ok; ++q) {
+              ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
+              if (!ok) break;
+              const uint32_t dst = base + st * kStageBytes, bar = full + 8 * st;
+              ptx::mbar_expect_tx(bar, (uint32_t)kStageBytes);
+              for (int pl = 0; pl < PLANES; ++pl) {
+                const int zz = pl * a.batch + z;
+                const uint32_t da = dst + pl * kTileBytes, db = dst + (PLANES + pl) * kTileBytes;
+                if (amn) {
+                  mma::load_3d(da, ma, r * kTile, q * 64, zz, bar);
+                  mma::load_3d(da + 8192, ma, r * kTile + 64, q * 64, zz, bar);
+                } else {
+                  mma::load_3d(da, ma, q * 64, r * kTile, zz, bar);
+                }
+                if (bmn) {
+                  mma::load_3d(db, mb, c * kTile, q * 64, zz, bar);
+                  mma::load_3d(db + 8192, mb, c * kTile + 64, q * 64, zz, bar);
+                } else {
+                  mma::load_3d(db, mb, q * 64, c * kTile, zz, bar);
+                }
+              }
+              if (++st == kStages) st = 0, ph ^= 1u;
+            }
+            if (ok && adds(w)) {
+              // what the epilogue adds to the product, a stage of its own: the halves of the tile this CTA writes
+              ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
+              if (!ok) break;
+              const uint32_t dst = base + st * kStageBytes, bar = full + 8 * st;
+              const CUtensorMap* mi = k == 1 ? &a.s : &a.xk[kx];
+              const int h0 = w.split == 1 ? 0 : w.split == 2 ? rank : rank >> 1, h1 = w.split == 1 ? 2 : h0 + 1;
+              ptx::mbar_expect_tx(bar, (uint32_t)((h1 - h0) * PLANES * kTileBytes));
+              for (int h = h0; h < h1; ++h)
+                for (int pl = 0; pl < PLANES; ++pl)
+                  mma::load_3d(dst + (h * PLANES + pl) * kTileBytes, mi, c * kTile + 64 * h, r * kTile, pl * a.batch + z, bar);
+              if (++st == kStages) st = 0, ph ^= 1u;
+            }
+          }
+        }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    const bool lead = ptx::elect_one();
+    int st = 0, n = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int i = 0; i < a.steps && ok; ++i)
+      for (int k = 0; k < 3 && ok; ++k) {
+        const Work w = phase_of(i, k);
+        const bool amn = k == 0 && a.tall, bmn = amn || (k == 2 && !a.tall);
+        const uint32_t id = mma::idesc(128, 128, false, amn, bmn);
+        int c0, c1;
+        range(w, c0, c1);
+        const int last_steps = ((k == 0 ? a.n : a.m) - (w.chunks - 1) * 64 + 15) / 16;
+        for (int t = w.me; t < w.tiles && ok; t += w.workers) {
+          for (int b0 = c0; b0 < c1 && ok; b0 += kBlock, ++n) {
+            ok = ptx::mbar_wait_warp(acc_empty + 8 * (n & 1), (uint32_t)((n >> 1) & 1) ^ 1u, abort_s, mma::kWaitLimit);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            const uint32_t d = tmem + (uint32_t)(n & 1) * 128u;
+            const int b1 = PLANES == 2 ? min(b0 + kBlock, c1) : c1;
+            for (int q = b0; q < b1 && ok; ++q) {
+              ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, mma::kWaitLimit);
+              if (!ok) break;
+              ptx::tc_fence_after();
+              if (lead) {
+                const uint32_t sa = base + st * kStageBytes, sb = sa + PLANES * kTileBytes;
+                const int steps = q == w.chunks - 1 ? last_steps : 4;
+                uint32_t acc = q > b0;
+                // lo hi, hi lo, hi hi
+                for (int pr = PLANES == 2 ? 0 : 2; pr < 3; ++pr) {
+                  uint64_t da = mma::desc(sa + (pr == 0 ? kTileBytes : 0), amn), db = mma::desc(sb + (pr == 1 ? kTileBytes : 0), bmn);
+                  for (int e = 0; e < steps; ++e, da += amn ? 2048 >> 4 : 32 >> 4, db += bmn ? 2048 >> 4 : 32 >> 4) {
+                    ptx::mma_f16(d, da, db, id, acc);
+                    acc = 1;
+                  }
+                }
+                ptx::mma_commit(empty + 8 * st);
+              }
+              if (++st == kStages) st = 0, ph ^= 1u;
+            }
+            if (ok && lead) ptx::mma_commit(acc_full + 8 * (n & 1));
+            if (PLANES == 1) b0 = c1;
+          }
+          if (adds(w) && ++st == kStages) st = 0, ph ^= 1u;
+        }
+      }
+    if (lead) {
+      volatile int never = 0;
+      ptx::mma_commit(drain);
+      ptx::mbar_wait(drain, 0, &never, mma::kWaitLimit);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ epilogue
+    // A warp: 32 rows, 64 columns as two blocks of 32 x 32. Blocks go to memory
+    // by way of shared memory and TMA, mirror images too: a store a row from
+    // registers takes a cycle for every 16 bytes (128 x 128 FP32 tiles: 9,000
+    // clocks of a phase).
+    const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * 64, sums = lanes + 256;
+    int n = 0, joins = 0, st = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int i = 0; i < a.steps && ok; ++i)
+      for (int k = 0; k < 3 && ok; ++k) {
+        const Work w = phase_of(i, k);
+        ok = ptx::mbar_wait_warp(go, (uint32_t)(3 * i + k) & 1u, abort_s, mma::kWaitLimit);
+        const float ps = a.ps[i];
+        const bool split = w.split > 1;
+        const int slice = 128 / w.split;
+        const int rows = k < 2 ? a.m : a.rows, cols = k < 2 ? a.m : a.cols;
+        const bool mine = !split || half * 64 / slice == rank || (half * 64 + 32) / slice == rank;
+        const uint32_t own = region + (split ? quarter * kPartBytes : (half * 4 + quarter) * kSendBytes);
+        const CUtensorMap* to = k == 0 ? &a.to[2] : k == 1 ? &a.to[3] : &a.to[(i & 1) ^ 1];
+        int c0, c1;
+        range(w, c0, c1);
+        for (int t = w.me; t < w.tiles && ok; t += w.workers) {
+          int r, c, z;
+          tile(w, t, r, c, z);
+          const float tn = i == 0 ? __ldcg(a.t + z) : 1.f;
+          float f, g = 0.f;
+          if (k == 0) {
+            f = tn * tn * (kSScale / (kXScale * kXScale));
+          } else if (k == 1) {
+            f = a.coef[3 * i + 2] * ps / (kSScale * kSScale);
+            g = a.coef[3 * i + 1] * ps / kSScale;
+          } else {
+            const float last = w.kind == 3 ? 1.f / kXScale : 1.f;
+            f = tn * last / ps;
+            g = tn * last * a.coef[3 * i];
+          }
+          const int row = r * kTile + quarter * 32 + lane, col = c * kTile + half * 64;
+          // blocks of the sum meet in tensor memory
+          uint32_t src = sums;
+          const int blocks = c1 <= c0 ? 0 : PLANES == 2 ? (c1 - c0 + kBlock - 1) / kBlock : 1;
+          for (int b = 0; b < blocks; ++b, ++n) {
+            ok = ptx::mbar_wait_warp(acc_full + 8 * (n & 1), (uint32_t)((n >> 1) & 1), abort_s, mma::kWaitLimit);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            src = lanes + (uint32_t)(n & 1) * 128u;
+            if (blocks == 1) break;
+#pragma unroll 1
+            for (int q = 0; q < 64; q += 8) {
+              float v[8];
+              mma::tmem_ld8(src + q, v);
+              if (b > 0) {
+                float s[8];
+                mma::tmem_ld8(sums + q, s);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += s[j];
+              }
+              mma::tmem_st8(sums + q, v);
+            }
+            mma::tmem_wait_st();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * (n & 1));
+            src = sums;
+          }
+          if (!ok) break;
+          st += c1 - c0;
+          while (st >= kStages) st -= kStages, ph ^= 1u;
+          if (split) {
+            // every CTA has read the parts of the join before
+            if (joins) ok = ptx::mbar_wait_warp<true>(ready, (uint32_t)(joins - 1) & 1u, abort_s, mma::kWaitLimit);
+            if (!ok) break;
+            // columns [slice o, + slice) go to CTA o, into the sender's slot there
+            if (blocks) {
+#pragma unroll 1
+              for (int p = 0; p < 2; ++p) {
+                const int first = half * 64 + p * 32, owner = first / slice;
+                if (owner == rank) continue;
+                uint32_t v[32];
+                ptx::tmem_ld32(src + p * 32, v);
+                ptx::tmem_wait_ld();
+                const int slot = rank < owner ? rank : rank - 1;
+                const uint32_t dst = ptx::mapa(region + quarter * kPartBytes, owner) +
+                                     (uint32_t)(((slot * 32 + lane) * (slice + 4) + first - owner * slice) * 4);
+#pragma unroll
+                for (int j = 0; j < 32; j += 4)
+                  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + j * 4), "r"(v[j]),
+                               "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3])
+                               : "memory");
+              }
+            }
+            __syncwarp();
+            if (lane < kCluster && lane != rank) ptx::mbar_arrive_cluster(ptx::mapa(got, lane));
+            ok = ptx::mbar_wait_warp<true>(got, (uint32_t)joins & 1u, abort_s, mma::kWaitLimit);
+            if (!ok) break;
+          }
+          const uint32_t in = base + st * kStageBytes + half * PLANES * kTileBytes + (quarter * 32 + lane) * 128;
+          if (adds(w)) {
+            ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, mma::kWaitLimit);
+            if (!ok) break;
+          }
+          float v[2][32];
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const int first = half * 64 + p * 32, owner = first / slice;
+            if (split && owner != rank) continue;
+            uint32_t bits[32];
+            ptx::tmem_ld32(src + p * 32, bits);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[p][j] = __uint_as_float(bits[j]);
+            if (split) {
+              // the parts in their order: those of lower CTAs, this one's, those of higher ones
+              float s[32];
+#pragma unroll
+              for (int j = 0; j < 32; ++j) s[j] = 0.f;
+#pragma unroll 1
+              for (int part = 0; part < w.split; ++part) {
+                if (part == rank) {
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) s[j] += v[p][j];
+                  continue;
+                }
+                const uint32_t o = own + (uint32_t)((((part < rank ? part : part - 1) * 32 + lane) * (slice + 4) + first -
+                                                     owner * slice) * 4);
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                  float e[4];
+                  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                               : "=f"(e[0]), "=f"(e[1]), "=f"(e[2]), "=f"(e[3])
+                               : "r"(o + j * 4)
+                               : "memory");
+#pragma unroll
+                  for (int q = 0; q < 4; ++q) s[j + q] += e[q];
+                }
+              }
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[p][j] = s[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[p][j] *= f;
+            if (k > 0) {
+#pragma unroll
+              for (int l = 0; l < PLANES; ++l)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  uint4 e;
+                  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                               : "=r"(e.x), "=r"(e.y), "=r"(e.z), "=r"(e.w)
+                               : "r"(in + l * kTileBytes + (((p * 4 + q) ^ (lane & 7)) << 4))
+                               : "memory");
+                  add_f16(e, g, &v[p][q * 8]);
+                }
+            }
+          }
+          if (adds(w)) {
+            // the last of the eight warps gives the stage back
+            __syncwarp();
+            if (lane == 0 && last_of_eight(counts)) ptx::mbar_arrive(empty + 8 * st);
+            if (++st == kStages) st = 0, ph ^= 1u;
+          }
+          if (blocks == 1) {
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * (n & 1));
+            ++n;
+          }
+          __syncwarp();  // the warp has read its parts
+          if (mine && w.kind < 3) {
+            const bool mirror = k < 2 && r != c;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const int first = half * 64 + p * 32;
+              if (split && first / slice != rank) continue;
+              uint32_t hl[2][16];
+              split_f16(v[p], hl[0], hl[1]);
+              // the block before has left
+              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+              __syncwarp();
+#pragma unroll
+              for (int l = 0; l < PLANES; ++l) {
+                const uint32_t at = own + l * 2048 + lane * 64;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((q ^ ((lane >> 1) & 3)) << 4)),
+                               "r"(hl[l][4 * q]), "r"(hl[l][4 * q + 1]), "r"(hl[l][4 * q + 2]), "r"(hl[l][4 * q + 3])
+                               : "memory");
+                if (mirror) {
+                  // lanes in pairs: the even one writes its and its neighbour's column 2 q, the odd one 2 q + 1
+                  const uint32_t to_m = own + (PLANES + l) * 2048 + ((lane & 7) >> 1) * 4;
+#pragma unroll
+                  for (int q = 0; q < 16; ++q) {
+                    const uint32_t other = __shfl_xor_sync(0xffffffffu, hl[l][q], 1);
+                    const int j = 2 * q + (lane & 1);
+                    const uint32_t word = lane & 1 ? __byte_perm(other, hl[l][q], 0x7632) : __byte_perm(hl[l][q], other, 0x5410);
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(to_m + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) << 4)), "r"(word)
+                                 : "memory");
+                  }
+                }
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) {
+                const int x = col + p * 32, y = r * kTile + quarter * 32;
+                for (int l = 0; l < PLANES; ++l) {
+                  if (x < cols && y < rows) mma::store_3d(to, x, y, l * a.batch + z, own + l * 2048);
+                  if (mirror && x < cols && y < rows) mma::store_3d(to, y, x, l * a.batch + z, own + (PLANES + l) * 2048);
+                }
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+              }
+            }
+          } else if (mine) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const int first = half * 64 + p * 32, left = cols - col - p * 32;
+              if ((split && first / slice != rank) || left <= 0 || row >= rows) continue;
+              put_result<TO>(a, ((int64_t)z * a.rows + row) * a.cols + col + p * 32, left, v[p]);
+            }
+          }
+          if (split) {
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
+            if (lane < kCluster) ptx::mbar_arrive_cluster(ptx::mapa(ready, lane));
+            ++joins;
+          }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        // written, and readable by copies of other CTAs; the last warp says so
+        asm volatile("fence.proxy.async.global;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          __threadfence();
+          if (last_of_eight(counts + 1)) add_release(a.phases);
+        }
+      }
+  }
+  __syncthreads();
+  if (*abort_s) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < (1LL << 23)) {
+    }
+    if (threadIdx.x == 0) atomicAdd(a.errors, 1ull);
+    __syncthreads();
+  }
+  ptx::tc_fence_after();
+  ptx::cluster_sync();
+  if (warp == 1) ptx::tmem_dealloc(tmem, 512);
+}
+
+template <int PLANES, typename TO>
+int iterate_ctas() {
+  static int known[64] = {};
+  int dev = 0;
+  LC_CUDA(cudaGetDevice(&dev));
+  if (dev < 64 && known[dev]) return known[dev];
+  allow_smem(reinterpret_cast<const void*>(k_iterate<PLANES, TO>), mma::kSmem);
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = kCluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(mma::num_sms() / kCluster * kCluster));
+  cfg.blockDim = dim3(mma::kThreads);
+  cfg.dynamicSmemBytes = mma::kSmem;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  LC_CUDA(cudaOccupancyMaxActiveClusters(&clusters, k_iterate<PLANES, TO>, &cfg));
+  LC_REQUIRE(clusters >= 1, LIPCACHE_E_CUDA, "no cluster of the iteration kernel fits on this device");
+  const int ctas = std::min(clusters, mma::num_sms() / kCluster) * kCluster;
+  if (dev < 64) known[dev] = ctas;
+  return ctas;
+}
+
+template <int PLANES, typename TO>
+void iterate_at_once(int batch, int rows, int cols, int steps, const double* co, void* out, const OrthoStep& st,
+                     const OrthoLayout& l, cudaStream_t s) {
+  const bool tall = rows > cols;
+  const int m = std::min(rows, cols), n = std::max(rows, cols);
+  IterateArgs a = {};
+  for (int i = 0; i < 2; ++i) {
+    const mma::Tensor X{l.x[i], cols, rows, (int64_t)PLANES * batch, l.ld, l.x_plane};
+    a.xk[i] = mma::tensor_map(X, 128);
+    a.xm[i] = mma::tensor_map(X, 64);
+    a.to[i] = mma::tensor_map(X, 32, 32);
+  }
+  const mma::Tensor S{l.s, m, m, (int64_t)PLANES * batch, l.sld, l.s_plane},
+      P{l.p, m, m, (int64_t)PLANES * batch, l.sld, l.s_plane};
+  a.s = mma::tensor_map(S, 128);
+  a.p = mma::tensor_map(P, 128);
+  a.to[2] = mma::tensor_map(S, 32, 32);
+  a.to[3] = mma::tensor_map(P, 32, 32);
+  a.tall = tall;
+  a.batch = batch;
+  a.m = m;
+  a.n = n;
+  a.steps = steps;
+  for (int i = 0; i < 3 * steps; ++i) a.coef[i] = (float)co[i];
+  for (int i = 0; i < steps; ++i) a.ps[i] = poly_scale(a.coef[3 * i + 1], a.coef[3 * i + 2]);
+  a.phases = l.phases;
+  a.errors = mma::error_counter();
+  const int ctas = iterate_ctas<PLANES, TO>();
+  // The split that ends first, in clocks: a stage's loads from L2 (64 bytes a
+  // clock and SM), the tile's epilogue, and the join (measured: 8,000 to 9,600
+  // for a tile's parts through the cluster, and the epilogue of a slice).
+  const int64_t mt = ceil_div(m, kTile), nt = ceil_div(n, kTile);
+  int64_t grid = 0;  // no more CTAs than have work: each takes part in every barrier
+  for (int k = 0; k < 3; ++k) {
+    const int64_t tiles = (k == 2 ? mt * nt : mt * (mt + 1) / 2) * batch, chunks = ceil_div(k == 0 ? n : m, 64);
+    int64_t best = -1;
+    for (int sp_ = 1; sp_ <= kCluster; sp_ *= 2) {
+      if (sp_ > chunks) break;
+      const int64_t workers = sp_ > 1 ? ctas / kCluster : ctas;
+      const int64_t cost = ceil_div(tiles, workers) * (ceil_div(chunks, sp_) * 512 * PLANES + (sp_ > 1 ? 14000 : 2000 + 1500 * PLANES));
+      if (best < 0 || cost < best) best = cost, a.split[k] = sp_;
+    }
+    grid = std::max(grid, tiles * (a.split[k] > 1 ? kCluster : 1));
+  }
+  grid = std::min<int64_t>(round_up(grid, kCluster), ctas);
+  a.t = l.t;
+  a.out = st.weight ? st.out_weight : out;
+  a.weight = st.weight;
+  a.rows = rows;
+  a.cols = cols;
+  a.vec = cols % 8 == 0 && ((uintptr_t)a.out & 15) == 0 && ((uintptr_t)a.weight & 15) == 0;
+  a.keep = st.keep;
+  a.rate = st.rate;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kCluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeCooperative;
+  attr[1].val.cooperative = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(mma::kThreads);
+  cfg.dynamicSmemBytes = mma::kSmem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  LC_CUDA(cudaLaunchKernelEx(&cfg, k_iterate<PLANES, TO>, a));
+  LC_LAUNCH_CHECK("k_iterate");
+}
 
 template <int PLANES, typename Epi>
 void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, int M, int N, int64_t K, int batch,
@@ -372,13 +1029,26 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
 template <typename T, int VEC, int PLANES>
 void normalise(const T* g, Direction a, int64_t batch, double eps, const OrthoLayout& l, cudaStream_t s) {
   a.units = a.cols / VEC;
-  const int64_t n = (int64_t)a.rows * a.units;
-  const unsigned parts = (unsigned)std::min<int64_t>(kParts, ceil_div(n, 256));
-  launch_pdl(k_squares<T, VEC>, dim3(parts, (unsigned)batch), 256, s, g, a, l.part);
+  const int64_t n = (int64_t)a.rows * a.units, per = (int64_t)a.rows * a.cols;
+  // dense matrices on 16-byte boundaries: eight elements at a time whatever the rows
+  const bool flat = VEC == 1 && a.ldg == a.cols && (batch == 1 || per % 8 == 0) && per < (1LL << 31) &&
+                    (((uintptr_t)g | (uintptr_t)a.st.momentum | (uintptr_t)a.st.out_momentum) & 15) == 0;
+  unsigned parts = (unsigned)std::min<int64_t>(kParts, ceil_div(flat ? per / 8 + 1 : n, 512));
+  if (flat) {
+    Direction f = a;
+    f.rows = 1;
+    f.cols = (int)per;
+    f.ldg = per;
+    f.units = (int)(per / 8);
+    f.tail = (int)(per % 8);
+    launch_pdl(k_squares<T, 8>, dim3(parts, (unsigned)batch), 256, s, g, f, l.part);
+  } else {
+    launch_pdl(k_squares<T, VEC>, dim3(parts, (unsigned)batch), 256, s, g, a, l.part);
+  }
   LC_LAUNCH_CHECK("k_squares");
   const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div(n, 512), 1024);
   launch_pdl(k_planes<T, VEC, PLANES>, dim3(blocks, (unsigned)batch), 256, s, g, a, (const double*)l.part, (int)parts, eps,
-             l.x[0], l.ld, batch * l.x_plane, l.t);
+             l.x[0], l.ld, batch * l.x_plane, l.t, l.phases);
   LC_LAUNCH_CHECK("k_planes");
 }
 
@@ -388,6 +1058,10 @@ void iterate(int batch, int rows, int cols, int steps, const double* co, void* o
   const bool tall = rows > cols;
   const int m = std::min(rows, cols), n = std::max(rows, cols);
   const int64_t xp = (int64_t)batch * l.x_plane, sp = (int64_t)batch * l.s_plane;
+  if (ceil_div(m, 256) * ceil_div(m, 256) * batch / 2 < mma::num_sms() / 4) {
+    iterate_at_once<PLANES, TO>(batch, rows, cols, steps, co, out, st, l, s);
+    return;
+  }
   const mma::Tensor S{l.s, m, m, (int64_t)PLANES * batch, l.sld, l.s_plane};
   const mma::Tensor P{l.p, m, m, (int64_t)PLANES * batch, l.sld, l.s_plane};
   const int tile = ceil_div(m, 256) * ceil_div(m, 256) * batch / 2 >= mma::num_sms() / 4 ? 256 : 128;
@@ -398,9 +1072,7 @@ void iterate(int batch, int rows, int cols, int steps, const double* co, void* o
     const mma::Tensor X{x, cols, rows, (int64_t)PLANES * batch, l.ld, l.x_plane};
     SymEpi<PLANES> gram{l.s, nullptr, l.sld, l.s_plane, sp, m, tile, kSScale / (kXScale * kXScale), 0.f, t};
     product<PLANES>(X, tall, X, tall, m, m, n, batch, true, gram, s);
-    // |P| <= 16 |b| + 256 |c| for singular values up to 4
-    const float bound = 16.f * fabsf(b) + 256.f * fabsf(c);
-    const float ps = exp2f(floorf(fminf(12.f, log2f(32768.f / fmaxf(bound, 1.f)))));
+    const float ps = poly_scale(b, c);
     SymEpi<PLANES> poly{l.p, l.s, l.sld, l.s_plane, sp, m, tile, c * ps / (kSScale * kSScale), b * ps / kSScale, nullptr};
     product<PLANES>(S, false, S, false, m, m, m, batch, true, poly, s);
     auto update = [&](auto epi) {
@@ -438,7 +1110,7 @@ void orthogonalize(int type, const void* G, int64_t ldg, int64_t batch, int rows
   OrthoLayout l;
   Carve c{ws, 0};
   l.take(c, planes, batch, rows, cols);
-  const Direction d{rows, cols, ldg, 0, st};
+  const Direction d{rows, cols, ldg, 0, 0, st};
   const bool vec = cols % 8 == 0 && ldg % 8 == 0 && ((uintptr_t)G & 15) == 0 && ((uintptr_t)st.momentum & 15) == 0 &&
                    ((uintptr_t)st.out_momentum & 15) == 0;
   auto go = [&](auto g) {

@@ -33,6 +33,48 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) {
   return __float2bfloat16_rn(v);
 }
 
+// Two values at a time: the conversions that pack run at several times the
+// rate of single ones.
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 open_f16(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// N values as two FP16 planes, hi + lo.
+template <int N>
+__device__ __forceinline__ void split_f16(const float (&v)[N], uint32_t (&hi)[N / 2], uint32_t (&lo)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    hi[i] = pack_f16(v[2 * i], v[2 * i + 1]);
+    const float2 h = open_f16(hi[i]);
+    lo[i] = pack_f16(v[2 * i] - h.x, v[2 * i + 1] - h.y);
+  }
+}
+// The same as BF16 planes.
+template <int N>
+__device__ __forceinline__ void split_bf16(const float (&v)[N], uint32_t (&hi)[N / 2], uint32_t (&lo)[N / 2]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    hi[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    lo[i] = pack_bf16(v[2 * i] - __uint_as_float(hi[i] << 16), v[2 * i + 1] - __uint_as_float(hi[i] & 0xffff0000u));
+  }
+}
+// N values (a multiple of 16 bytes) rounded to T, in 32-bit words.
+template <typename T, int N>
+__device__ __forceinline__ void round_to(const float (&v)[N], uint32_t (&w)[N * sizeof(T) / 4]) {
+#pragma unroll
+  for (int i = 0; i < (int)(N * sizeof(T) / 4); ++i) {
+    if constexpr (sizeof(T) == 4)
+      w[i] = __float_as_uint(v[i]);
+    else
+      w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+  }
+}
+
 inline size_t elem(int type) { return type == LIPCACHE_F32 ? 4 : 2; }
 __device__ __forceinline__ int64_t ceil_div_dev(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
