@@ -1106,6 +1106,7 @@ size_t ortho_bytes(int type, int64_t batch, int rows, int cols) {
 void orthogonalize(int type, const void* G, int64_t ldg, int64_t batch, int rows, int cols, int steps,
                    const double* coefficients, double eps, void* out, const OrthoStep& st, unsigned char* ws,
                    cudaStream_t s) {
+  if (ortho_small(type, G, ldg, batch, rows, cols, steps, coefficients, eps, out, st, s)) return;
   const int out_type = st.weight ? st.weight_type : type, planes = planes_of(out_type);
   OrthoLayout l;
   Carve c{ws, 0};

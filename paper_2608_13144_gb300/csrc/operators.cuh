@@ -126,6 +126,10 @@ struct OrthoStep {  // what a step adds to an orthogonalisation; null weight: no
   float beta = 0.f, keep = 1.f, rate = 0.f;  // W' = keep W - rate O
   bool nesterov = false;
 };
+// head_ortho_small.cu: false where the matrices are not its kind (a side of at
+// most 64, slices that fit)
+bool ortho_small(int type, const void* G, int64_t ldg, int64_t batch, int rows, int cols, int steps,
+                 const double* coefficients, double eps, void* out, const OrthoStep& st, cudaStream_t s);
 size_t ortho_bytes(int type, int64_t batch, int rows, int cols);
 void orthogonalize(int type, const void* G, int64_t ldg, int64_t batch, int rows, int cols, int steps,
                    const double* coefficients, double eps, void* out, const OrthoStep& st, unsigned char* ws,
