@@ -46,26 +46,36 @@ __global__ void __launch_bounds__(256)
 }
 
 // ---------------------------------------------------------------- FP32 rows
-// A warp a row: its planes, and its low-rank product u (or v).
+// A warp a row. Kinds of rows in a launch: planes of a row (of W, with the B of
+// all adapters for that class side by side); a row's low-rank product u or v,
+// and its planes at the place of the row's adapter among all of them (0
+// elsewhere); rows of A set side by side.
 struct RowJob {
+  int set_aside = 0;            // a row of A
   const float* in = nullptr;
   int64_t ld = 0, rows = 0;
   int width = 0, vec = 0;       // vec: rows can be read 16 bytes at a time
   const float* fold = nullptr;  // a factor of each column, in the planes only
-  __half* planes = nullptr;     // nullable
+  int most = 0;                 // the largest power used
+  __half* planes = nullptr;     // nullable: two FP16 planes under a power of two
   int64_t ldo = 0, plane = 0;
   float* undo = nullptr;        // what undoes each row's power of two
-  int most = 0;                 // the largest power used
-  const float* F = nullptr;     // nullable: the factor
-  int64_t f_g = 0, f_j = 0, f_i = 0;
-  int f_vec = 0;                // factor and row can be read so together
+  const float* F = nullptr;     // nullable: the factor of the row's adapter
+  int64_t f_g = 0, f_j = 0;
+  int f_vec = 0;                // elements of the factor a load: 4 along the row, or 1, 2, 4 along j
   float* u = nullptr;           // rows x r
+  bf16* wide = nullptr;         // nullable: three BF16 planes of all adapters' side by side
+  const float* side = nullptr;  // nullable: B, of which row c of every adapter is set side by side in `wide`
+  int64_t ldw = 0, wplane = 0;
+  int* odd = nullptr;           // whether a value set into `wide` was NaN or infinite (0 there instead)
 };
+constexpr int kRowJobs = 3;
 struct RowJobs {
-  RowJob job[2];
+  RowJob job[kRowJobs];
   const int32_t* adapter;
   const float* scales;
   int G, r;
+  int blocks[kRowJobs];
 };
 
 // Sums of eight values over a warp: lane l ends with the sum of value l & 7.
@@ -84,39 +94,65 @@ __device__ __forceinline__ float sum8(float (&v)[8], int lane) {
   return r + __shfl_xor_sync(0xffffffffu, r, 16);
 }
 
+// v as three BF16 planes (24 bits).
+__device__ __forceinline__ void put3(bf16* o, int64_t plane, float v) {
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    const bf16 h = __float2bfloat16_rn(v);
+    o[q * plane] = h;
+    v -= __bfloat162float(h);
+  }
+}
+
+// The exponent that takes the largest element of a row into [2^14, 2^15).
+__device__ __forceinline__ int row_power(float top, int most) {
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  const int e = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
+  return max(-most, min(most, e));
+}
+
+// The planes of a row; returns its factor.
 template <int VEC>
-__device__ __forceinline__ void row_planes(const RowJob& a, const float* r, int64_t row, int lane) {
+__device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int64_t row, int lane) {
+  constexpr int kHeld = 4;  // vectors that a lane keeps between the two passes
   auto get = [&](int i, float (&v)[VEC]) {
-    if (VEC == 4) {
-      const float4 q = *reinterpret_cast<const float4*>(r + i);
-      v[0] = q.x, v[1 % VEC] = q.y, v[2 % VEC] = q.z, v[3 % VEC] = q.w;
+    if constexpr (VEC == 4) {
+      const float4 q = __ldg(reinterpret_cast<const float4*>(r + i));
+      v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
     } else {
-      v[0] = r[i];
+      v[0] = __ldg(r + i);
     }
     if (a.fold) {
 #pragma unroll
       for (int k = 0; k < VEC; ++k) v[k] *= __ldg(a.fold + i + k);
     }
   };
+  float held[kHeld][VEC];
   float top = 0.f;
-  for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
-    float v[VEC];
-    get(i, v);
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) top = fmaxf(top, fabsf(v[k]));
+  for (int k = 0; k < kHeld; ++k) {
+    const int i = (k * 32 + lane) * VEC;
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) held[k][q] = 0.f;
+    if (i < a.width) get(i, held[k]);
   }
 #pragma unroll
-  for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-  // the largest element lands in [2^14, 2^15)
-  int e = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-  e = max(-a.most, min(a.most, e));
-  const float f = ldexpf(1.f, e);
-  __half* o = a.planes + row * a.ldo;
-  for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
+  for (int k = 0; k < kHeld; ++k)
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) top = fmaxf(top, fabsf(held[k][q]));
+#pragma unroll 4
+  for (int i = (kHeld * 32 + lane) * VEC; i < a.width; i += 32 * VEC) {
     float v[VEC];
     get(i, v);
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) v[k] *= f;
+    for (int q = 0; q < VEC; ++q) top = fmaxf(top, fabsf(v[q]));
+  }
+  const float f = ldexpf(1.f, row_power(top, a.most));
+  __half* o = a.planes + row * a.ldo;
+  auto put = [&](int i, float (&v)[VEC]) {
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) v[q] *= f;
     if constexpr (VEC == 4) {
       uint32_t hi[2], lo[2];
       split_f16(v, hi, lo);
@@ -127,56 +163,143 @@ __device__ __forceinline__ void row_planes(const RowJob& a, const float* r, int6
       o[i] = hi;
       o[a.plane + i] = __float2half_rn(v[0] - __half2float(hi));
     }
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int i = (k * 32 + lane) * VEC;
+    if (i < a.width) put(i, held[k]);
   }
-  if (lane == 0) a.undo[row] = ldexpf(1.f, -e);
+#pragma unroll 4
+  for (int i = (kHeld * 32 + lane) * VEC; i < a.width; i += 32 * VEC) {
+    float v[VEC];
+    get(i, v);
+    put(i, v);
+  }
+  if (lane == 0) a.undo[row] = 1.f / f;  // a power of two
+  return f;
 }
 
-__global__ void __launch_bounds__(256) k_rows_f32(const RowJobs jobs) {
+// A row's products with eight columns j of its adapter's factor. ALONG 0: the
+// row's index is the factor's innermost, VEC of it a load; 1: j is, VEC of it a
+// load.
+template <int ALONG, int VEC>
+__device__ __forceinline__ void row_dots(const RowJob& a, const float* r, const float* F, int nj, int R, int lane,
+                                         float (&acc)[8]) {
+  if constexpr (ALONG == 0) {
+#pragma unroll 1
+    for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
+      float x[VEC], f[8][VEC];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < nj) {
+          if constexpr (VEC == 4) {
+            const float4 q = __ldg(reinterpret_cast<const float4*>(F + j * a.f_j + i));
+            f[j][0] = q.x, f[j][1] = q.y, f[j][2] = q.z, f[j][3] = q.w;
+          } else {
+            f[j][0] = __ldg(F + j * a.f_j + i);
+          }
+        }
+      if constexpr (VEC == 4) {
+        const float4 q = __ldg(reinterpret_cast<const float4*>(r + i));
+        x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
+      } else {
+        x[0] = __ldg(r + i);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j < nj) {
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) acc[j] = fmaf(x[q], f[j][q], acc[j]);
+        }
+    }
+  } else {
+#pragma unroll 4
+    for (int i = lane; i < a.width; i += 32) {
+      const float x = __ldg(r + i);
+      const float* fp = F + (int64_t)i * R;
+#pragma unroll
+      for (int j = 0; j < 8; j += VEC)
+        if (j < nj) {
+          float f[VEC];
+          if constexpr (VEC == 4) {
+            const float4 q = __ldg(reinterpret_cast<const float4*>(fp + j));
+            f[0] = q.x, f[1] = q.y, f[2] = q.z, f[3] = q.w;
+          } else if constexpr (VEC == 2) {
+            const float2 q = __ldg(reinterpret_cast<const float2*>(fp + j));
+            f[0] = q.x, f[1] = q.y;
+          } else {
+            f[0] = __ldg(fp + j);
+          }
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) acc[j + q] = fmaf(x, f[q], acc[j + q]);
+        }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(128, 6) k_rows_f32(const __grid_constant__ RowJobs jobs) {
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const int64_t all = jobs.job[0].rows + jobs.job[1].rows;
-  for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < all; w += (int64_t)gridDim.x * 8) {
-    const bool second = w >= jobs.job[0].rows;
-    const RowJob& a = jobs.job[second];
-    const int64_t row = second ? w - jobs.job[0].rows : w;
+  const int lane = threadIdx.x & 31, R = jobs.r;
+  // a block has one kind of rows
+  const int b0 = jobs.blocks[0], b1 = b0 + jobs.blocks[1], b = blockIdx.x;
+  const int which = b < b0 ? 0 : b < b1 ? 1 : 2, first = b < b0 ? b : b < b1 ? b - b0 : b - b1;
+  const RowJob& a = jobs.job[which];
+  const int64_t step = (int64_t)jobs.blocks[which] * 4;
+  for (int64_t row = (int64_t)first * 4 + (threadIdx.x >> 5); row < a.rows; row += step) {
     const float* r = a.in + row * a.ld;
-    if (a.planes) {
-      if (a.vec)
-        row_planes<4>(a, r, row, lane);
-      else
-        row_planes<1>(a, r, row, lane);
+    float f = 1.f;
+    if (a.planes) f = a.vec ? row_planes<4>(a, r, row, lane) : row_planes<1>(a, r, row, lane);
+    if (a.side || a.set_aside) {
+      // B of this class, over the class's power of two; or a row of A
+      bool odd = false;
+      for (int i = lane; i < (a.side ? jobs.G * R : a.width); i += 32) {
+        const int h = i / R;
+        float v = __ldg(a.side ? a.side + ((int64_t)h * a.rows + row) * R + i - h * R : r + i);
+        if (!isfinite(v)) v = 0.f, odd = true;
+        put3(a.wide + row * a.ldw + i, a.wplane, v * f);
+      }
+      odd = __any_sync(0xffffffffu, odd);
+      if (lane == 0) a.odd[row] = odd;
     }
     if (!a.F) continue;
     const int g = __ldg(jobs.adapter + row);
     const bool any = g >= 0 && g < jobs.G;
-    const float s = any && jobs.scales ? __ldg(jobs.scales + g) : 1.f;
-    for (int j0 = 0; j0 < jobs.r; j0 += 8) {
-      const int nj = min(8, jobs.r - j0);
-      float acc[8] = {};
-      if (any) {
-        const float* F = a.F + g * a.f_g + j0 * a.f_j;
-        if (nj == 8 && a.f_vec) {
-          for (int i = lane * 4; i < a.width; i += 128) {
-            const float4 x = *reinterpret_cast<const float4*>(r + i);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float4 f = __ldg(reinterpret_cast<const float4*>(F + j * a.f_j + i));
-              acc[j] = fmaf(x.x, f.x, fmaf(x.y, f.y, fmaf(x.z, f.z, fmaf(x.w, f.w, acc[j]))));
-            }
-          }
-        } else {
-#pragma unroll 4
-          for (int i = lane; i < a.width; i += 32) {
-            const float x = r[i];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (j < nj) acc[j] = fmaf(x, __ldg(F + j * a.f_j + i * a.f_i), acc[j]);
-          }
-        }
+    bf16* o = a.wide ? a.wide + row * a.ldw : nullptr;
+    if (o) {  // 0 but at the row's own adapter (written after; rows are whole vectors)
+      const int n = (int)(a.ldw / 8);
+      for (int i = lane; i < 3 * n; i += 32) {
+        const int q = i >= 2 * n ? 2 : i >= n ? 1 : 0;
+        *reinterpret_cast<uint4*>(o + q * a.wplane + (i - q * n) * 8) = uint4{0, 0, 0, 0};
       }
-      const float v = sum8(acc, lane);
-      if (lane < nj) a.u[row * jobs.r + j0 + lane] = any ? s * v : 0.f;
+      __syncwarp();
+    }
+    if (!any) {
+      for (int j = lane; j < R; j += 32) a.u[row * R + j] = 0.f;
+      continue;
+    }
+    const float s = jobs.scales ? __ldg(jobs.scales + g) : 1.f;
+    for (int j0 = 0; j0 < R; j0 += 8) {
+      const int nj = min(8, R - j0);
+      const float* F = a.F + g * a.f_g + j0 * a.f_j;
+      float acc[8] = {};
+      if (a.f_j == 1) {
+        if (a.f_vec == 4)
+          row_dots<1, 4>(a, r, F, nj, R, lane, acc);
+        else if (a.f_vec == 2)
+          row_dots<1, 2>(a, r, F, nj, R, lane, acc);
+        else
+          row_dots<1, 1>(a, r, F, nj, R, lane, acc);
+      } else if (a.f_vec == 4) {
+        row_dots<0, 4>(a, r, F, nj, R, lane, acc);
+      } else {
+        row_dots<0, 1>(a, r, F, nj, R, lane, acc);
+      }
+      const float v = s * sum8(acc, lane);
+      if (lane < nj) {
+        a.u[row * R + j0 + lane] = v;
+        if (o) put3(o + g * R + j0 + lane, a.wplane, v * f);
+      }
     }
   }
 }
@@ -461,6 +584,33 @@ struct AdaptEpi {
   const int32_t* adapter;
   int G, r, f_vec, always;
   int64_t f_col, f_j;
+  // set-aside values of a dense low-rank product (NaN and infinities of the
+  // factor), a flag for each column (n_odd = 0) or for each of n_odd rows of A
+  const int* odd;
+  int n_odd;
+
+  __device__ __forceinline__ void odd_values(int64_t p, int col0, int left, int lane, float (&v)[32]) const {
+    bool flag = false;
+    if (n_odd == 0)
+      flag = lane < left && __ldg(odd + col0 + lane);
+    else
+      for (int i = lane; i < n_odd; i += 32) flag |= __ldg(odd + i) != 0;
+    if (!__any_sync(0xffffffffu, flag) || p >= rows) return;
+    const int g = __ldg(adapter + p);
+    if (g < 0 || g >= G) return;
+    const T* f = F + (int64_t)g * cols * r + col0 * f_col;
+    for (int k = 0; k < r; ++k) {
+      const float uk = __ldg(u + p * r + k);
+#pragma unroll 1
+      for (int j = 0; j < min(left, 32); ++j) {
+        const float q = to_f32<T>(f[j * f_col + k * f_j]);
+        if (isfinite(q)) continue;
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+          if (c == j) v[c] = fmaf(uk, q, v[c]);
+      }
+    }
+  }
 
   // element i of a 16-byte vector
   static __device__ __forceinline__ float part(const uint4& q, int i) {
@@ -545,8 +695,9 @@ struct AdaptEpi {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bc, j);
     }
+    if (odd) odd_values(p, col0, left, lane, v);
     if (p >= rows) return;
-    if (u && (always || many)) low(p, col0, left, v);
+    if (u && !odd && (always || many)) low(p, col0, left, v);
     T* o = y + p * ldy + col0;
     constexpr int kVec = 16 / sizeof(T);
     if (vec && left >= 32) {
@@ -638,11 +789,23 @@ constexpr int kWindow = 4096;  // (lists of 8 KB: two CTAs an SM)
 template <int THREADS>
 __device__ __forceinline__ int list_rows(const int32_t* adapter, int64_t t0, int64_t t1, int g, uint16_t* list,
                                          int* count, int tid) {
-  const int n = (int)(t1 - t0), per = (n + THREADS - 1) / THREADS;
-  const int a = min(tid * per, n), b = min(a + per, n);
-  int mine = 0;
+  constexpr int kPer = kWindow / THREADS;  // neighbouring rows a thread
+  static_assert(kPer <= 32 && kPer % 4 == 0, "a bit for each");
+  const int n = (int)(t1 - t0), first = tid * kPer;
+  uint32_t hits = 0;
+  if ((((uintptr_t)(adapter + t0)) & 15) == 0 && first + kPer <= n) {
+    int4 v[kPer / 4];
+#pragma unroll
+    for (int i = 0; i < kPer / 4; ++i) v[i] = __ldg(reinterpret_cast<const int4*>(adapter + t0 + first) + i);
+#pragma unroll
+    for (int i = 0; i < kPer / 4; ++i)
+      hits |= ((v[i].x == g ? 1u : 0u) | (v[i].y == g ? 2u : 0u) | (v[i].z == g ? 4u : 0u) | (v[i].w == g ? 8u : 0u)) << (4 * i);
+  } else {
 #pragma unroll 8
-  for (int i = a; i < b; ++i) mine += __ldg(adapter + t0 + i) == g;
+    for (int i = 0; i < kPer; ++i)
+      if (first + i < n && __ldg(adapter + t0 + first + i) == g) hits |= 1u << i;
+  }
+  const int mine = __popc(hits);
   int at = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -657,16 +820,19 @@ __device__ __forceinline__ int list_rows(const int32_t* adapter, int64_t t0, int
     all += count[w];
   }
   at -= mine;
-  if (mine)
-    for (int i = a; i < b; ++i)
-      if (__ldg(adapter + t0 + i) == g) list[at++] = (uint16_t)i;
+  while (hits) {
+    list[at++] = (uint16_t)(first + __ffs(hits) - 1);
+    hits &= hits - 1;
+  }
   asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
   return all;
 }
 
 // BF16, on the tensor cores: D^T, 128 of i x r of j (both planes of c side by
 // side). Four warps gather 64 rows a stage with 16-byte copies (past the list
-// and the width: zeros), one issues the MMAs.
+// and the width: zeros), one issues the MMAs. A cluster shares the rows of one
+// tile; its first CTA joins the parts in order. Bound by latency (the list, the
+// first rows) and by the adapter with the most rows.
 struct OuterJob {
   const bf16* in;
   int64_t ld;
@@ -692,8 +858,11 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ int count[4];
   const OuterJob& job = a.job[blockIdx.z];
-  const int i0 = blockIdx.x * 128, g = blockIdx.y;
-  if (i0 >= job.width) return;
+  uint32_t splits;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(splits));
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int i0 = (int)(blockIdx.x / splits) * 128, g = blockIdx.y;
+  if (i0 >= job.width) return;  // (the whole cluster)
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   const int stage_bytes = 16384 + a.rb * 256;
   const uint32_t lists = base + kOuterStages * stage_bytes, full = lists + 2 * kWindow, empty = full + 8 * kOuterStages,
@@ -736,48 +905,56 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
       if (threadIdx.x == 0) *total_s = n;
     }
     __syncthreads();
-    const int n = *total_s, chunks = (n + 63) / 64;
+    const int n = *total_s, all = (n + 63) / 64;
+    const int first = all * (int)rank / (int)splits, chunks = all * (int)(rank + 1) / (int)splits - first;
     issued += chunks;
     if (warp < 4) {
-      // 16-byte pieces of a stage: 64 rows x (16 of `in` + 2 x rb / 8 of c)
-      const int pieces = 16 + a.rb / 4;
       auto arrive = [&](int s) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         ptx::mbar_arrive(full + 8 * s);
       };
+      auto before = [&](int k) { return st >= k ? st - k : st - k + kOuterStages; };
       for (int k = 0; k < chunks && ok; ++k) {
         ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
         const uint32_t sa = base + st * stage_bytes;
-        // a warp takes a row at a time: its lanes the row's pieces
-        for (int r = warp; r < 64; r += 4) {
-          const bool row = k * 64 + r < n;
-          const int64_t t = row ? t0 + list[k * 64 + r] : t0;
-          for (int q = lane; q < pieces; q += 32) {
-            const void* src;
-            uint32_t dst;
-            int bytes;
-            if (q < 16) {
-              const int i = i0 + q * 8;
-              bytes = row ? max(0, min(16, (job.width - i) * 2)) : 0;
-              src = bytes ? job.in + t * job.ld + i : job.in;
-              dst = sa + (q >> 3) * 8192 + r * 128 + (((q & 7) ^ (r & 7)) << 4);
-            } else {
-              const int p = (q - 16) / (a.rb / 8), j = (q - 16 - p * (a.rb / 8));
-              bytes = row && j * 8 < a.ldc ? 16 : 0;
-              src = bytes ? a.plane * p + job.c + t * a.ldc + j * 8 : job.c;
-              dst = sa + 16384 + (p * a.rb + (j >> 3) * 64) * 128 + r * 128 + (((j & 7) ^ (r & 7)) << 4);
-            }
-            copy16(dst, src, bytes);
+        // 16-byte pieces of a row: 16 of `in`, rb / 8 of each plane of c; a lane
+        // has the same piece of all its warp's rows
+        for (int q = lane; q < 16 + a.rb / 4; q += 32) {
+          const char* src;
+          int64_t stride;
+          uint32_t dst;
+          int bytes, swz;
+          if (q < 16) {
+            const int i = i0 + q * 8;
+            bytes = max(0, min(16, (job.width - i) * 2));
+            src = reinterpret_cast<const char*>(job.in + (bytes ? i : 0));
+            stride = job.ld * 2;
+            dst = sa + (q >> 3) * 8192;
+            swz = q & 7;
+          } else {
+            const int p = (q - 16) / (a.rb / 8), j = (q - 16) - p * (a.rb / 8);
+            bytes = j * 8 < a.ldc ? 16 : 0;
+            src = reinterpret_cast<const char*>(job.c + a.plane * p + (bytes ? j * 8 : 0));
+            stride = a.ldc * 2;
+            dst = sa + 16384 + (p * a.rb + (j >> 3) * 64) * 128;
+            swz = j & 7;
           }
+          src += t0 * stride;
+          const uint16_t* rows = list + (first + k) * 64;
+          const int left = n - (first + k) * 64;
+#pragma unroll 4
+          for (int r = warp; r < 64; r += 4)
+            copy16(dst + r * 128 + ((swz ^ (r & 7)) << 4), src + (r < left ? rows[r] * stride : 0), r < left ? bytes : 0);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        // the stage before this one has arrived
-        if (k > 0) {
-          asm volatile("cp.async.wait_group 1;" ::: "memory");
-          arrive(st == 0 ? kOuterStages - 1 : st - 1);
+        // the stage two before this one has arrived; at the end, all have
+        if (k >= 2) {
+          asm volatile("cp.async.wait_group 2;" ::: "memory");
+          arrive(before(2));
         }
         if (k == chunks - 1) {
           asm volatile("cp.async.wait_group 0;" ::: "memory");
+          if (k >= 1) arrive(before(1));
           arrive(st);
         }
         if (++st == kOuterStages) st = 0, ph ^= 1u;
@@ -789,7 +966,7 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
         ptx::tc_fence_after();
         if (lead) {
           uint64_t da = mma::desc(base + st * stage_bytes, true), db = mma::desc(base + st * stage_bytes + 16384, true);
-          const int steps = min(4, (n - k * 64 + 15) / 16);
+          const int steps = min(4, (n - (first + k) * 64 + 15) / 16);
           for (int q = 0; q < steps; ++q, da += 2048 >> 4, db += 2048 >> 4) {
             ptx::mma_f16(tmem, da, db, id, acc);
             acc = 1;
@@ -812,30 +989,55 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
     ok = ptx::mbar_wait(done, 0, abort_s, mma::kWaitLimit);
     ok = __all_sync(0xffffffffu, ok);
     ptx::tc_fence_after();
-    const int i = i0 + warp * 32 + lane;
+  }
+  // hi + lo of 32 columns
+  auto sums = [&](int j0, float (&v)[32]) {
+    uint32_t hi[32], lo[32];
+    const uint32_t src = tmem + ((uint32_t)(warp * 32) << 16) + j0;
+    ptx::tmem_ld32(src, hi);
+    ptx::tmem_ld32(src + a.rb, lo);
+    ptx::tmem_wait_ld();
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = issued ? __uint_as_float(hi[j]) + __uint_as_float(lo[j]) : 0.f;
+  };
+  const int row = warp * 32 + lane;
+  if (splits > 1) {
+    ptx::cluster_sync();  // the first CTA's stages are free: its products are done
+    if (warp < 4 && rank > 0) {
+      const uint32_t dst = ptx::mapa(base, 0) + (rank - 1) * (uint32_t)(128 * a.rb * 4);
+      for (int j0 = 0; j0 < a.r; j0 += 32) {
+        float v[32];
+        sums(j0, v);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) store_cluster(dst + (uint32_t)((j0 + j) * 128 + row) * 4, v[j]);
+      }
+    }
+    ptx::cluster_sync();
+  }
+  if (warp < 4 && rank == 0) {
+    const float* part = reinterpret_cast<const float*>(smem_raw + (base - ptx::smem_u32(smem_raw)));
+    const int i = i0 + row;
     bf16* out = job.out + g * job.f_g + (int64_t)i * job.f_i;
     const bool vec = job.f_j == 1 && a.r % 8 == 0 && ((uintptr_t)job.out & 15) == 0;
     for (int j0 = 0; ok && j0 < a.r; j0 += 32) {
-      uint32_t hi[32], lo[32];
-      const uint32_t src = tmem + ((uint32_t)(warp * 32) << 16) + j0;
-      ptx::tmem_ld32(src, hi);
-      ptx::tmem_ld32(src + a.rb, lo);
-      ptx::tmem_wait_ld();
-      if (i >= job.width) continue;
       float v[32];
+      sums(j0, v);
+      for (uint32_t p = 1; p < splits; ++p) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] = issued ? __uint_as_float(hi[j]) + __uint_as_float(lo[j]) : 0.f;
+        for (int j = 0; j < 32; ++j) v[j] += part[(p - 1) * 128 * a.rb + (j0 + j) * 128 + row];
+      }
+      if (i >= job.width) continue;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        __align__(16) bf16 h[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[j] = __float2bfloat16_rn(v[q * 8 + j]);
-        if (vec && j0 + q * 8 < a.r) {
-          *reinterpret_cast<uint4*>(out + j0 + q * 8) = *reinterpret_cast<uint4*>(h);
-        } else if (!vec) {
+        if (j0 + q * 8 >= a.r) break;
+        if (vec) {
+          *reinterpret_cast<uint4*>(out + j0 + q * 8) =
+              uint4{pack_bf16(v[q * 8], v[q * 8 + 1]), pack_bf16(v[q * 8 + 2], v[q * 8 + 3]),
+                    pack_bf16(v[q * 8 + 4], v[q * 8 + 5]), pack_bf16(v[q * 8 + 6], v[q * 8 + 7])};
+        } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (j0 + q * 8 + j < a.r) out[(j0 + q * 8 + j) * job.f_j] = h[j];
+            if (j0 + q * 8 + j < a.r) out[(j0 + q * 8 + j) * job.f_j] = __float2bfloat16_rn(v[q * 8 + j]);
         }
       }
     }
@@ -847,8 +1049,8 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
   if (warp == 4) ptx::tmem_dealloc(tmem, cols);
 }
 
-// FP32, on the CUDA cores: 128 of i, eight of j, the listed rows dealt over
-// eight groups of threads.
+// FP32, on the CUDA cores: 64 of i, eight of j, the listed rows dealt over
+// sixteen groups of threads.
 struct OuterJobF32 {
   const float* in;
   int64_t ld;
@@ -865,13 +1067,13 @@ struct OuterJobsF32 {
 };
 
 __global__ void __launch_bounds__(1024) k_outer_f32(const OuterJobsF32 a) {
-  __shared__ float red[8][8][128];  // 32 KB; the list before it
+  __shared__ float red[16][8][64];  // 32 KB; the list before it
   __shared__ int count[32];
   uint16_t* list = reinterpret_cast<uint16_t*>(red);
   const OuterJobF32& job = a.job[blockIdx.z];
   const int tile = blockIdx.x / a.groups, g = blockIdx.y, j0 = (blockIdx.x - tile * a.groups) * 8;
-  const int ti = threadIdx.x & 127, q = threadIdx.x >> 7, i = tile * 128 + ti;
-  if (tile * 128 >= job.width) return;
+  const int ti = threadIdx.x & 63, q = threadIdx.x >> 6, i = tile * 64 + ti;
+  if (tile * 64 >= job.width) return;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   const int nj = min(8, a.r - j0);
@@ -879,8 +1081,8 @@ __global__ void __launch_bounds__(1024) k_outer_f32(const OuterJobsF32 a) {
   for (int64_t t0 = 0; t0 < a.tokens; t0 += kWindow) {
     const int64_t t1 = min(t0 + kWindow, a.tokens);
     const int n = list_rows<1024>(a.adapter, t0, t1, g, list, count, threadIdx.x);
-#pragma unroll 4
-    for (int k = q; k < n; k += 8) {
+#pragma unroll 8
+    for (int k = q; k < n; k += 16) {
       const int64_t t = t0 + list[k];
       const float x = i < job.width ? __ldg(job.in + t * job.ld + i) : 0.f;
       const float* c = job.c + t * a.r + j0;
@@ -893,11 +1095,11 @@ __global__ void __launch_bounds__(1024) k_outer_f32(const OuterJobsF32 a) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) red[q][j][ti] = acc[j];
   __syncthreads();
-  for (int e = threadIdx.x; e < nj * 128; e += 1024) {
-    const int j = e >> 7, k = e & 127, at = tile * 128 + k;
+  for (int e = threadIdx.x; e < nj * 64; e += 1024) {
+    const int j = e >> 6, k = e & 63, at = tile * 64 + k;
     float s = red[0][j][k];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) s += red[w][j][k];
+    for (int w = 1; w < 16; ++w) s += red[w][j][k];
     if (at < job.width) job.out[g * job.f_g + (j0 + j) * job.f_j + (int64_t)at * job.f_i] = s;
   }
 }
@@ -920,7 +1122,11 @@ struct Layout {
   float *undo_in, *undo_w;
   float* u[2];            // u, v: tokens x r
   uint16_t* up[2];        // their planes (BF16)
-  int64_t ld_x, ld_y, ld_r;
+  // FP32 with few adapters: u (or v) and the factor, every adapter's side by side, in three BF16 planes
+  bool dense;
+  bf16 *wide_u, *wide_f;
+  int* odd;
+  int64_t ld_x, ld_y, ld_r, ld_g;
   void take(Carve& c, const lipcache_adapted& p, bool backward) {
     const bool f32 = p.type == LIPCACHE_F32;
     const int64_t T = p.tokens, G = p.adapters, r = G ? p.rank : 1;
@@ -935,6 +1141,14 @@ struct Layout {
     c.take(b, f32 ? 0 : (size_t)(G * p.classes * ld_r));
     c.take(undo_in, (size_t)T);
     c.take(undo_w, (size_t)p.classes);
+    // up to 128 columns: two stages a pair of planes, twelve in all (in the
+    // epilogue, 65,536 x 200 with ten adapters of rank 8, the low-rank product
+    // took 100 of 138 us)
+    dense = f32 && G > 0 && G * r <= 128;
+    ld_g = round_up(G * r, 8);
+    c.take(wide_u, dense ? (size_t)(3 * T * ld_g) : 0);
+    c.take(wide_f, dense ? (size_t)(3 * (backward ? G * r * ld_x : p.classes * ld_g)) : 0);
+    c.take(odd, dense ? (size_t)(backward ? G * r : p.classes) : 0);
     for (int i = 0; i < 2; ++i) {
       c.take(u[i], G ? (size_t)(T * r) : 0);
       c.take(up[i], G && !f32 ? (size_t)(2 * T * ld_r) : 0);
@@ -976,26 +1190,40 @@ struct Op {
     j.vec = width % 4 == 0 && ld % 4 == 0 && ((uintptr_t)in & 15) == 0;
     return j;
   }
-  void to_planes(RowJob& j, uint16_t* out, int64_t ldo, float* undo, int most) {
+  RowJob planes_job(const void* in, int64_t ld, int64_t rows, int width, uint16_t* out, int64_t ldo, float* undo, int most) {
+    RowJob j = row_job(in, ld, rows, width);
     j.planes = reinterpret_cast<__half*>(out);
     j.ldo = ldo;
-    j.plane = j.rows * ldo;
+    j.plane = rows * ldo;
     j.undo = undo;
     j.most = most;
+    return j;
   }
-  void to_low(RowJob& j, const Side& d, const T* F, int i) {
+  // u (i = 0) or v (1) beside; with the job's planes, set side by side too
+  void add_low(RowJob& j, const Side& d, const T* F, int i) {
     if (!p.adapters) return;
     j.F = reinterpret_cast<const float*>(F);
     j.f_g = (int64_t)p.rank * d.width;
     j.f_j = d.f_j;
-    j.f_i = d.f_i;
-    j.f_vec = j.vec && d.f_i == 1 && ((uintptr_t)F & 15) == 0;
+    const uintptr_t at = (uintptr_t)F;
+    j.f_vec = d.f_j == 1 ? (p.rank % 4 == 0 && at % 16 == 0 ? 4 : p.rank % 2 == 0 && at % 8 == 0 ? 2 : 1)
+                         : (j.vec && at % 16 == 0 ? 4 : 1);
     j.u = l.u[i];
+    if (j.planes && l.dense) {
+      j.wide = l.wide_u;
+      j.ldw = l.ld_g;
+      j.wplane = j.rows * l.ld_g;
+    }
   }
-  void run_rows(const RowJob& a, const RowJob& b) {
-    RowJobs j{{a, b}, p.adapter, p.scales, p.adapters, p.rank};
-    const int64_t all = a.rows + b.rows;
-    launch_pdl(k_rows_f32, dim3((unsigned)std::min<int64_t>(ceil_div(all, 8), 16 * mma::num_sms())), 256, s, j);
+  void run_rows(const RowJob& a, const RowJob& b, const RowJob& c) {
+    RowJobs j{{a, b, c}, p.adapter, p.scales, p.adapters, p.rank, {}};
+    unsigned all = 0;
+    for (int k = 0; k < kRowJobs; ++k) {
+      j.blocks[k] = (int)std::min<int64_t>(ceil_div(j.job[k].rows, 4), 32 * mma::num_sms());
+      all += (unsigned)j.blocks[k];
+    }
+    if (!all) return;
+    launch_pdl(k_rows_f32, dim3(all), 128, s, j);
     LC_LAUNCH_CHECK("k_rows_f32");
   }
 
@@ -1059,7 +1287,8 @@ struct Op {
   }
 
   // out = rows . W + low-rank: M tokens, N d.out, K d.width. F: the low-rank
-  // factor as the tensor cores read it (BF16), or null.
+  // factor as the tensor cores read it, or null
+  // (FP32: as FP32 planes with every adapter's side by side).
   void product(const Side& d, const Tensor& rows, const Tensor& w, bool w_mn, int i, const Tensor* F, bool f_mn,
                AdaptEpi<T> e) {
     mma::Args a = {};
@@ -1094,13 +1323,21 @@ struct Op {
       a.low.adapter = p.adapter;
       a.low.tokens = p.tokens;
       a.low.G = p.adapters;
-      const mma::Seg g = mma::segment(p.rank, 0, 0, mma::idesc(tm, a.bn, true, false, f_mn));
+      a.low.dense = f32;
+      const int64_t k = f32 ? (int64_t)p.adapters * p.rank : p.rank;
+      const mma::Seg g = mma::segment(k, 0, 0, mma::idesc(tm, a.bn, true, false, f_mn));
       a.low.chunks = g.chunks;
       a.low.last = g.last;
       a.low.idesc = g.idesc;
-      a.low.pairs = 2;  // lo, hi
-      a.low.a_z[0] = 1;
-      maps.la = mma::tensor_map(Tensor{l.up[i], l.ld_r, p.tokens, 2, l.ld_r, p.tokens * l.ld_r}, a.a_rows);
+      // small products first
+      static const int pu[6] = {2, 0, 1, 1, 0, 0}, pf[6] = {0, 2, 1, 0, 1, 0};
+      a.low.pairs = f32 ? 6 : 2;
+      for (int q = 0; q < a.low.pairs; ++q) {
+        a.low.a_z[q] = f32 ? pu[q] : 1 - q;
+        a.low.b_z[q] = f32 ? pf[q] : 0;
+      }
+      maps.la = f32 ? mma::tensor_map(Tensor{l.wide_u, k, p.tokens, 3, l.ld_g, p.tokens * l.ld_g}, a.a_rows)
+                    : mma::tensor_map(Tensor{l.up[i], l.ld_r, p.tokens, 2, l.ld_r, p.tokens * l.ld_r}, a.a_rows);
       maps.lb = mma::tensor_map(*F, f_mn ? 64 : a.bn / (pair ? 2 : 1));
     }
     if (pair)
@@ -1161,15 +1398,23 @@ struct Op {
     e.bias = bias;
     epilogue_low(e, 0, B, true, f32);
     if constexpr (f32) {
-      RowJob jx = row_job(x, p.ldx, p.tokens, p.d), jw = row_job(W, p.ldw, p.classes, p.d);
-      to_planes(jx, l.in[0], l.ld_x, l.undo_in, 100);
-      to_low(jx, d, A, 0);
-      to_planes(jw, l.w, l.ld_x, l.undo_w, 60);
-      run_rows(jx, jw);
+      RowJob jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, 60);
+      if (l.dense) {
+        jw.side = B;
+        jw.wide = l.wide_f;
+        jw.ldw = l.ld_g;
+        jw.wplane = p.classes * l.ld_g;
+        jw.odd = l.odd;
+        e.odd = l.odd;
+      }
+      RowJob jx = planes_job(x, p.ldx, p.tokens, p.d, l.in[0], l.ld_x, l.undo_in, 100);
+      add_low(jx, d, A, 0);
+      run_rows(jw, jx, RowJob{});
       e.undo_row = l.undo_in;
       e.undo_col = l.undo_w;
+      const Tensor fb{l.wide_f, (int64_t)p.adapters * p.rank, p.classes, 3, l.ld_g, p.classes * l.ld_g};
       product(d, Tensor{l.in[0], p.d, p.tokens, 2, l.ld_x, p.tokens * l.ld_x},
-              Tensor{l.w, p.d, p.classes, 2, l.ld_x, p.classes * l.ld_x}, false, 0, nullptr, false, e);
+              Tensor{l.w, p.d, p.classes, 2, l.ld_x, p.classes * l.ld_x}, false, 0, l.dense ? &fb : nullptr, false, e);
     } else {
       const Tensor rows = rows_of(d, 0), w = head();
       Tensor fb = {};
@@ -1189,21 +1434,33 @@ struct Op {
     AdaptEpi<T> e = epilogue(dx, lddx, p.d);
     if (dx) epilogue_low(e, 1, A, false, f32);
     if constexpr (f32) {
-      RowJob jw = row_job(W, p.ldw, dx ? p.classes : 0, p.d), jx = row_job(x, p.ldx, want_u ? p.tokens : 0, p.d),
-             jy = row_job(dy, lddy, dx || want_v ? p.tokens : 0, p.classes);
-      if (dx) to_planes(jw, l.w, l.ld_x, l.undo_w, 60);
-      if (want_u) to_low(jx, sx, A, 0);
-      if (jx.rows + jw.rows) run_rows(jx, jw);
-      if (dx) {
-        to_planes(jy, l.in[1], l.ld_y, l.undo_in, 100);
-        jy.fold = l.undo_w;  // W's planes are W over these
+      RowJob jw, jx, ja, jy;
+      if (dx) jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, 60);
+      if (want_u) jx = row_job(x, p.ldx, p.tokens, p.d), add_low(jx, sx, A, 0);
+      if (dx && l.dense) {
+        ja = row_job(A, p.d, (int64_t)p.adapters * p.rank, p.d);
+        ja.set_aside = 1;
+        ja.wide = l.wide_f;
+        ja.ldw = l.ld_x;
+        ja.wplane = ja.rows * l.ld_x;
+        ja.odd = l.odd;
+        e.odd = l.odd;
+        e.n_odd = (int)ja.rows;
       }
-      if (want_v) to_low(jy, sy, B, 1);
-      if (jy.rows) run_rows(jy, RowJob{});
+      run_rows(jw, jx, ja);
+      if (dx) {
+        jy = planes_job(dy, lddy, p.tokens, p.classes, l.in[1], l.ld_y, l.undo_in, 100);
+        jy.fold = l.undo_w;  // W's planes are W over these
+      } else if (want_v) {
+        jy = row_job(dy, lddy, p.tokens, p.classes);
+      }
+      if (want_v) add_low(jy, sy, B, 1);
+      run_rows(jy, RowJob{}, RowJob{});
       if (dx) {
         e.undo_row = l.undo_in;
+        const Tensor fa{l.wide_f, p.d, (int64_t)p.adapters * p.rank, 3, l.ld_x, p.adapters * p.rank * l.ld_x};
         product(sy, Tensor{l.in[1], p.classes, p.tokens, 2, l.ld_y, p.tokens * l.ld_y},
-                Tensor{l.w, p.d, p.classes, 2, l.ld_x, p.classes * l.ld_x}, true, 1, nullptr, false, e);
+                Tensor{l.w, p.d, p.classes, 2, l.ld_x, p.classes * l.ld_x}, true, 1, l.dense ? &fa : nullptr, true, e);
       }
       if (low && (dA || dB)) {
         OuterJobsF32 o = {};
@@ -1216,7 +1473,7 @@ struct Op {
         o.tokens = p.tokens;
         o.r = p.rank;
         o.groups = (int)ceil_div(p.rank, 8);
-        launch_pdl(k_outer_f32, dim3((unsigned)(ceil_div(wide, 128) * o.groups), (unsigned)p.adapters, (unsigned)n),
+        launch_pdl(k_outer_f32, dim3((unsigned)(ceil_div(wide, 64) * o.groups), (unsigned)p.adapters, (unsigned)n),
                    1024, s, o);
         LC_LAUNCH_CHECK("k_outer_f32");
       }
@@ -1254,8 +1511,23 @@ struct Op {
         o.errors = mma::error_counter();
         const int smem = 1024 + kOuterStages * (16384 + o.rb * 256) + 2 * kWindow + 128;
         allow_smem(reinterpret_cast<const void*>(k_outer), 1024 + kOuterStages * (16384 + 128 * 256) + 2 * kWindow + 128);
-        launch_pdl_smem(k_outer, dim3((unsigned)ceil_div(wide, 128), (unsigned)p.adapters, (unsigned)n), kOuterThreads,
-                        smem, s, o);
+        // CTAs a tile: as long as an adapter has some four stages of rows for each, and a slot for its parts
+        unsigned splits = 1;
+        while (splits < (o.rb == 64 ? 4u : 2u) && p.tokens >= (int64_t)p.adapters * splits * 512) splits *= 2;
+        cudaLaunchAttribute attr[2];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = splits;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)ceil_div(wide, 128) * splits, (unsigned)p.adapters, (unsigned)n);
+        cfg.blockDim = dim3(kOuterThreads);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.stream = s;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        LC_CUDA(cudaLaunchKernelEx(&cfg, k_outer, o));
         LC_LAUNCH_CHECK("k_outer");
       }
     }

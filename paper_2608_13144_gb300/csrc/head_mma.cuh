@@ -147,7 +147,9 @@ struct Low {
   int G = 0;                         // 0: no low-rank segments
   int chunks = 0, last = 0;
   int pairs = 0;
-  int a_z[2], b_z[2];                // plane of each factor; B's z is b_z * G + adapter
+  int a_z[6], b_z[6];                // plane of each factor; B's z is b_z * G + adapter
+  int dense = 0;                     // every adapter's factor side by side, the rows' factors 0 but in their own:
+                                     // one product for all rows, B's z is b_z
   uint32_t idesc;
 };
 
@@ -345,7 +347,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int c = c0; c < c1 && ok; ++c)
               load(&maps.a, a.a_mn, row, c * kChunk, sg.a_z + z, &maps.b, a.b_mn, col, c * kChunk, sg.b_z + z);
           }
-        if (a.low.G) {
+        if (a.low.dense) {
+          for (int q = 0; q < a.low.pairs && ok; ++q)
+            for (int c = 0; c < a.low.chunks && ok; ++c)
+              load(&maps.la, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk, a.low.b_z[q]);
+        } else if (a.low.G) {
           Groups<TM> gr;
           gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
           if (!gr.more_than(kFewAdapters))
@@ -423,7 +429,11 @@ __global__ void __launch_bounds__(kThreads, 1)
               chunk(a.a_mn, a.b_mn, sg.idesc, c == sg.chunks - 1 ? sg.last : 4, nullptr);
           }
         }
-        if (a.low.G) {
+        if (a.low.dense) {
+          for (int q = 0; q < a.low.pairs && ok; ++q)
+            for (int c = 0; c < a.low.chunks && ok; ++c)
+              chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, nullptr);
+        } else if (a.low.G) {
           Groups<TM> gr;
           gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
           if (!gr.more_than(kFewAdapters))
@@ -460,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tile_at(a, t, mt, nt, z);
       const int row = mt * TM + (int)rank * 128 + quarter * 32;
       bool many = false;
-      if (a.low.G) {
+      if (a.low.G && !a.low.dense) {
         Groups<TM> gr;
         gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
         many = gr.more_than(kFewAdapters);
