@@ -47,24 +47,18 @@ __global__ void __launch_bounds__(256)
 
 // ---------------------------------------------------------------- FP32 rows
 // A warp a row. Kinds of rows in a launch: planes of a row (of W, with the B of
-// all adapters for that class side by side); a row's low-rank product u or v,
-// and its planes at the place of the row's adapter among all of them (0
-// elsewhere); rows of A set side by side.
+// all adapters for that class side by side); rows of A set side by side.
 struct RowJob {
   int set_aside = 0;            // a row of A
   const float* in = nullptr;
   int64_t ld = 0, rows = 0;
   int width = 0, vec = 0;       // vec: rows can be read 16 bytes at a time
-  const float* fold = nullptr;  // a factor of each column, in the planes only
+  const float* fold = nullptr;  // a factor of each column
   int most = 0;                 // the largest power used
-  __half* planes = nullptr;     // nullable: two FP16 planes under a power of two
+  __half* planes = nullptr;     // two FP16 planes under a power of two
   int64_t ldo = 0, plane = 0;
   float* undo = nullptr;        // what undoes each row's power of two
-  const float* F = nullptr;     // nullable: the factor of the row's adapter
-  int64_t f_g = 0, f_j = 0;
-  int f_vec = 0;                // elements of the factor a load: 4 along the row, or 1, 2, 4 along j
-  float* u = nullptr;           // rows x r
-  bf16* wide = nullptr;         // nullable: three BF16 planes of all adapters' side by side
+  bf16* wide = nullptr;         // three BF16 planes of what is set side by side
   const float* side = nullptr;  // nullable: B, of which row c of every adapter is set side by side in `wide`
   int64_t ldw = 0, wplane = 0;
   int* odd = nullptr;           // whether a value set into `wide` was NaN or infinite (0 there instead)
@@ -72,8 +66,6 @@ struct RowJob {
 constexpr int kRowJobs = 3;
 struct RowJobs {
   RowJob job[kRowJobs];
-  const int32_t* adapter;
-  const float* scales;
   int G, r;
   int blocks[kRowJobs];
 };
@@ -115,7 +107,7 @@ __device__ __forceinline__ int row_power(float top, int most) {
 // The planes of a row; returns its factor.
 template <int VEC>
 __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int64_t row, int lane) {
-  constexpr int kHeld = 4;  // vectors that a lane keeps between the two passes
+  constexpr int kHeld = 2;  // vectors that a lane keeps between the two passes
   auto get = [&](int i, float (&v)[VEC]) {
     if constexpr (VEC == 4) {
       const float4 q = __ldg(reinterpret_cast<const float4*>(r + i));
@@ -179,64 +171,6 @@ __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int
   return f;
 }
 
-// A row's products with eight columns j of its adapter's factor. ALONG 0: the
-// row's index is the factor's innermost, VEC of it a load; 1: j is, VEC of it a
-// load.
-template <int ALONG, int VEC>
-__device__ __forceinline__ void row_dots(const RowJob& a, const float* r, const float* F, int nj, int R, int lane,
-                                         float (&acc)[8]) {
-  if constexpr (ALONG == 0) {
-#pragma unroll 1
-    for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
-      float x[VEC], f[8][VEC];
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < nj) {
-          if constexpr (VEC == 4) {
-            const float4 q = __ldg(reinterpret_cast<const float4*>(F + j * a.f_j + i));
-            f[j][0] = q.x, f[j][1] = q.y, f[j][2] = q.z, f[j][3] = q.w;
-          } else {
-            f[j][0] = __ldg(F + j * a.f_j + i);
-          }
-        }
-      if constexpr (VEC == 4) {
-        const float4 q = __ldg(reinterpret_cast<const float4*>(r + i));
-        x[0] = q.x, x[1] = q.y, x[2] = q.z, x[3] = q.w;
-      } else {
-        x[0] = __ldg(r + i);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < nj) {
-#pragma unroll
-          for (int q = 0; q < VEC; ++q) acc[j] = fmaf(x[q], f[j][q], acc[j]);
-        }
-    }
-  } else {
-#pragma unroll 4
-    for (int i = lane; i < a.width; i += 32) {
-      const float x = __ldg(r + i);
-      const float* fp = F + (int64_t)i * R;
-#pragma unroll
-      for (int j = 0; j < 8; j += VEC)
-        if (j < nj) {
-          float f[VEC];
-          if constexpr (VEC == 4) {
-            const float4 q = __ldg(reinterpret_cast<const float4*>(fp + j));
-            f[0] = q.x, f[1] = q.y, f[2] = q.z, f[3] = q.w;
-          } else if constexpr (VEC == 2) {
-            const float2 q = __ldg(reinterpret_cast<const float2*>(fp + j));
-            f[0] = q.x, f[1] = q.y;
-          } else {
-            f[0] = __ldg(fp + j);
-          }
-#pragma unroll
-          for (int q = 0; q < VEC; ++q) acc[j + q] = fmaf(x, f[q], acc[j + q]);
-        }
-    }
-  }
-}
-
 __global__ void __launch_bounds__(128, 6) k_rows_f32(const __grid_constant__ RowJobs jobs) {
   ptx::wait_prerequisites();
   ptx::launch_dependents();
@@ -262,44 +196,164 @@ __global__ void __launch_bounds__(128, 6) k_rows_f32(const __grid_constant__ Row
       odd = __any_sync(0xffffffffu, odd);
       if (lane == 0) a.odd[row] = odd;
     }
-    if (!a.F) continue;
-    const int g = __ldg(jobs.adapter + row);
-    const bool any = g >= 0 && g < jobs.G;
-    bf16* o = a.wide ? a.wide + row * a.ldw : nullptr;
-    if (o) {  // 0 but at the row's own adapter (written after; rows are whole vectors)
-      const int n = (int)(a.ldw / 8);
-      for (int i = lane; i < 3 * n; i += 32) {
-        const int q = i >= 2 * n ? 2 : i >= n ? 1 : 0;
-        *reinterpret_cast<uint4*>(o + q * a.wplane + (i - q * n) * 8) = uint4{0, 0, 0, 0};
+  }
+}
+
+// u (or v) of FP32 rows. A block sorts its rows by adapter, so that a warp has
+// four rows of one adapter against eight columns of its factor: three loads for
+// eight multiplications of a lane, where a row alone takes nine. The products of
+// a row can be set side by side too (three BF16 planes, 0 but at its adapter's
+// place), over the row's power of two.
+struct LowJob {
+  const float* in;
+  int64_t ld;
+  int width, vec;
+  const float* F;
+  int64_t f_g, f_j, f_i;
+  float* u;
+  bf16* wide;         // nullable
+  const float* undo;
+};
+struct LowJobs {
+  LowJob job[2];
+  const int32_t* adapter;
+  const float* scales;
+  int64_t tokens, ldw;
+  int G, r, tile;
+};
+constexpr int kLowTile = 128;  // rows of a block, at most
+
+template <int VEC, bool J_INNER>
+__device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x)[4], const float* F, int nj, int lane,
+                                         float (&acc)[32]) {
+  for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
+    float v[4][VEC], f[8][VEC];
+    if constexpr (J_INNER) {  // eight neighbours of the factor (VEC = 1)
+      const float* fp = F + (int64_t)i * a.f_i;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j][0] = j < nj ? __ldg(fp + j) : 0.f;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (VEC == 4) {
+          const float4 q = j < nj ? __ldg(reinterpret_cast<const float4*>(F + j * a.f_j + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          f[j][0] = q.x, f[j][1] = q.y, f[j][2] = q.z, f[j][3] = q.w;
+        } else {
+          f[j][0] = j < nj ? __ldg(F + j * a.f_j + i) : 0.f;
+        }
       }
-      __syncwarp();
     }
-    if (!any) {
-      for (int j = lane; j < R; j += 32) a.u[row * R + j] = 0.f;
-      continue;
-    }
-    const float s = jobs.scales ? __ldg(jobs.scales + g) : 1.f;
-    for (int j0 = 0; j0 < R; j0 += 8) {
-      const int nj = min(8, R - j0);
-      const float* F = a.F + g * a.f_g + j0 * a.f_j;
-      float acc[8] = {};
-      if (a.f_j == 1) {
-        if (a.f_vec == 4)
-          row_dots<1, 4>(a, r, F, nj, R, lane, acc);
-        else if (a.f_vec == 2)
-          row_dots<1, 2>(a, r, F, nj, R, lane, acc);
-        else
-          row_dots<1, 1>(a, r, F, nj, R, lane, acc);
-      } else if (a.f_vec == 4) {
-        row_dots<0, 4>(a, r, F, nj, R, lane, acc);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (VEC == 4) {
+        const float4 q = __ldg(reinterpret_cast<const float4*>(x[k] + i));
+        v[k][0] = q.x, v[k][1] = q.y, v[k][2] = q.z, v[k][3] = q.w;
       } else {
-        row_dots<0, 1>(a, r, F, nj, R, lane, acc);
+        v[k][0] = __ldg(x[k] + i);
       }
-      const float v = s * sum8(acc, lane);
-      if (lane < nj) {
-        a.u[row * R + j0 + lane] = v;
-        if (o) put3(o + g * R + j0 + lane, a.wplane, v * f);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) acc[k * 8 + j] = fmaf(v[k][q], f[j][q], acc[k * 8 + j]);
+  }
+}
+
+__global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJobs a) {
+  __shared__ int id[kLowTile], order[kLowTile], starts[kLowTile + 1], sums[8];
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const LowJob& job = a.job[blockIdx.z];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.r;
+  const int64_t t0 = (int64_t)blockIdx.x * a.tile;
+  const int n = (int)min((int64_t)a.tile, a.tokens - t0);
+  const int j0 = blockIdx.y * 8, nj = min(8, R - j0);
+  int mine = a.G;  // rows without an adapter come last
+  if (tid < n) {
+    const int g = __ldg(a.adapter + t0 + tid);
+    mine = g >= 0 && g < a.G ? g : a.G;
+    id[tid] = mine;
+  }
+  __syncthreads();
+  if (tid < n) {
+    int rank = 0;
+    for (int k = 0; k < n; ++k) rank += id[k] < mine || (id[k] == mine && k < tid);
+    order[rank] = tid;
+  }
+  __syncthreads();
+  // groups: up to four neighbours in that order with one adapter
+  bool start = false;
+  if (tid < n) {
+    const int g = id[order[tid]];
+    int back = 0;
+    while (back < tid && id[order[tid - back - 1]] == g) ++back;
+    start = (back & 3) == 0;
+  }
+  const uint32_t m = __ballot_sync(0xffffffffu, start);
+  if (lane == 0) sums[warp] = __popc(m);
+  __syncthreads();
+  int at = __popc(m & ((1u << lane) - 1u)), groups = 0;
+  for (int w = 0; w < 8; ++w) {
+    if (w < warp) at += sums[w];
+    groups += sums[w];
+  }
+  if (start) starts[at] = tid;
+  if (tid == 0) starts[groups] = n;
+  __syncthreads();
+  for (int q = warp; q < groups; q += 8) {
+    const int first = starts[q], count = starts[q + 1] - first;
+    const int g = id[order[first]];
+    const bool any = g < a.G;
+    float acc[32];
+#pragma unroll
+    for (int k = 0; k < 32; ++k) acc[k] = 0.f;
+    if (any) {
+      const float* x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = job.in + (t0 + order[first + min(k, count - 1)]) * job.ld;
+      const float* F = job.F + g * job.f_g + j0 * job.f_j;
+      if (job.f_j == 1)
+        low_dots<1, true>(job, x, F, nj, lane, acc);
+      else if (job.vec)
+        low_dots<4, false>(job, x, F, nj, lane, acc);
+      else
+        low_dots<1, false>(job, x, F, nj, lane, acc);
+    }
+    // 32 sums on 32 lanes: halve the values, double the lanes that share one
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+      const bool up = lane & s;
+#pragma unroll
+      for (int k = 0; k < s; ++k) {
+        const float keep = up ? acc[k + s] : acc[k], give = up ? acc[k] : acc[k + s];
+        acc[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
       }
+    }
+    const int k = lane >> 3, j = lane & 7;
+    const int64_t t = t0 + order[first + min(k, count - 1)];
+    const float s = any && a.scales ? __ldg(a.scales + g) : 1.f;
+    const float v = any ? s * acc[0] : 0.f;
+    if (k < count && j < nj) job.u[t * R + j0 + j] = v;
+    if (job.wide) {
+      // the first of the blocks along j clears the rows' other places
+      if (blockIdx.y == 0) {
+        const int words = (int)(a.ldw / 8);
+        for (int e = lane; e < count * 3 * words; e += 32) {
+          const int row = e / (3 * words), rest = e - row * 3 * words, q3 = rest / words, w8 = rest - q3 * words;
+          // a word of eight columns may hold some of the adapter's own: left to those
+          bf16* o = job.wide + (t0 + order[first + row]) * a.ldw + q3 * a.tokens * a.ldw + w8 * 8;
+          const int c0 = w8 * 8, own0 = any ? g * R : 0, own1 = any ? own0 + R : 0;
+          if (c0 + 8 <= own0 || c0 >= own1)
+            *reinterpret_cast<uint4*>(o) = uint4{0, 0, 0, 0};
+          else
+            for (int c = 0; c < 8; ++c)
+              if (c0 + c < own0 || c0 + c >= own1) o[c] = __float2bfloat16_rn(0.f);
+        }
+      }
+      if (any && k < count && j < nj)
+        put3(job.wide + t * a.ldw + g * R + j0 + j, a.tokens * a.ldw, v / __ldg(job.undo + t));  // a power of two
     }
   }
 }
@@ -1141,10 +1195,10 @@ struct Layout {
     c.take(b, f32 ? 0 : (size_t)(G * p.classes * ld_r));
     c.take(undo_in, (size_t)T);
     c.take(undo_w, (size_t)p.classes);
-    // up to 128 columns: two stages a pair of planes, twelve in all (in the
+    // up to 256 columns: four stages a pair of planes, 24 in all (in the
     // epilogue, 65,536 x 200 with ten adapters of rank 8, the low-rank product
     // took 100 of 138 us)
-    dense = f32 && G > 0 && G * r <= 128;
+    dense = f32 && G > 0 && G * r <= 256;
     ld_g = round_up(G * r, 8);
     c.take(wide_u, dense ? (size_t)(3 * T * ld_g) : 0);
     c.take(wide_f, dense ? (size_t)(3 * (backward ? G * r * ld_x : p.classes * ld_g)) : 0);
@@ -1199,24 +1253,39 @@ struct Op {
     j.most = most;
     return j;
   }
-  // u (i = 0) or v (1) beside; with the job's planes, set side by side too
-  void add_low(RowJob& j, const Side& d, const T* F, int i) {
-    if (!p.adapters) return;
+  // u (i = 0) or v (1); `wide`: set side by side too, over the rows' powers of two
+  LowJob low_job(const Side& d, const T* F, int i, bool wide) {
+    LowJob j = {};
+    j.in = static_cast<const float*>(d.in);
+    j.ld = d.ld;
+    j.width = d.width;
+    j.vec = d.f_i == 1 && d.width % 4 == 0 && d.ld % 4 == 0 && (((uintptr_t)d.in | (uintptr_t)F) & 15) == 0;
     j.F = reinterpret_cast<const float*>(F);
     j.f_g = (int64_t)p.rank * d.width;
     j.f_j = d.f_j;
-    const uintptr_t at = (uintptr_t)F;
-    j.f_vec = d.f_j == 1 ? (p.rank % 4 == 0 && at % 16 == 0 ? 4 : p.rank % 2 == 0 && at % 8 == 0 ? 2 : 1)
-                         : (j.vec && at % 16 == 0 ? 4 : 1);
+    j.f_i = d.f_i;
     j.u = l.u[i];
-    if (j.planes && l.dense) {
-      j.wide = l.wide_u;
-      j.ldw = l.ld_g;
-      j.wplane = j.rows * l.ld_g;
-    }
+    j.wide = wide && l.dense ? l.wide_u : nullptr;
+    j.undo = l.undo_in;
+    return j;
+  }
+  void run_low(const LowJob* jobs, int n) {
+    if (!n) return;
+    LowJobs a = {};
+    for (int k = 0; k < n; ++k) a.job[k] = jobs[k];
+    a.adapter = p.adapter;
+    a.scales = p.scales;
+    a.tokens = p.tokens;
+    a.ldw = l.ld_g;
+    a.G = p.adapters;
+    a.r = p.rank;
+    // more rows a block leave fewer groups short; fewer fill the device
+    a.tile = p.tokens >= 64 * (int64_t)mma::num_sms() * 2 ? 128 : p.tokens >= 32 * (int64_t)mma::num_sms() ? 64 : 32;
+    launch_pdl(k_low_f32, dim3((unsigned)ceil_div(p.tokens, a.tile), (unsigned)ceil_div(p.rank, 8), (unsigned)n), 256, s, a);
+    LC_LAUNCH_CHECK("k_low_f32");
   }
   void run_rows(const RowJob& a, const RowJob& b, const RowJob& c) {
-    RowJobs j{{a, b, c}, p.adapter, p.scales, p.adapters, p.rank, {}};
+    RowJobs j{{a, b, c}, p.adapters, p.rank, {}};
     unsigned all = 0;
     for (int k = 0; k < kRowJobs; ++k) {
       j.blocks[k] = (int)std::min<int64_t>(ceil_div(j.job[k].rows, 4), 32 * mma::num_sms());
@@ -1407,9 +1476,9 @@ struct Op {
         jw.odd = l.odd;
         e.odd = l.odd;
       }
-      RowJob jx = planes_job(x, p.ldx, p.tokens, p.d, l.in[0], l.ld_x, l.undo_in, 100);
-      add_low(jx, d, A, 0);
-      run_rows(jw, jx, RowJob{});
+      run_rows(jw, planes_job(x, p.ldx, p.tokens, p.d, l.in[0], l.ld_x, l.undo_in, 100), RowJob{});
+      const LowJob ju = low_job(d, A, 0, true);
+      run_low(&ju, low ? 1 : 0);
       e.undo_row = l.undo_in;
       e.undo_col = l.undo_w;
       const Tensor fb{l.wide_f, (int64_t)p.adapters * p.rank, p.classes, 3, l.ld_g, p.classes * l.ld_g};
@@ -1434,28 +1503,29 @@ struct Op {
     AdaptEpi<T> e = epilogue(dx, lddx, p.d);
     if (dx) epilogue_low(e, 1, A, false, f32);
     if constexpr (f32) {
-      RowJob jw, jx, ja, jy;
-      if (dx) jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, 60);
-      if (want_u) jx = row_job(x, p.ldx, p.tokens, p.d), add_low(jx, sx, A, 0);
-      if (dx && l.dense) {
-        ja = row_job(A, p.d, (int64_t)p.adapters * p.rank, p.d);
-        ja.set_aside = 1;
-        ja.wide = l.wide_f;
-        ja.ldw = l.ld_x;
-        ja.wplane = ja.rows * l.ld_x;
-        ja.odd = l.odd;
-        e.odd = l.odd;
-        e.n_odd = (int)ja.rows;
-      }
-      run_rows(jw, jx, ja);
+      RowJob jw, ja, jy;
       if (dx) {
+        jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, 60);
+        if (l.dense) {
+          ja = row_job(A, p.d, (int64_t)p.adapters * p.rank, p.d);
+          ja.set_aside = 1;
+          ja.wide = l.wide_f;
+          ja.ldw = l.ld_x;
+          ja.wplane = ja.rows * l.ld_x;
+          ja.odd = l.odd;
+          e.odd = l.odd;
+          e.n_odd = (int)ja.rows;
+        }
+        run_rows(jw, ja, RowJob{});
         jy = planes_job(dy, lddy, p.tokens, p.classes, l.in[1], l.ld_y, l.undo_in, 100);
         jy.fold = l.undo_w;  // W's planes are W over these
-      } else if (want_v) {
-        jy = row_job(dy, lddy, p.tokens, p.classes);
+        run_rows(jy, RowJob{}, RowJob{});
       }
-      if (want_v) add_low(jy, sy, B, 1);
-      run_rows(jy, RowJob{}, RowJob{});
+      LowJob jl[2];
+      int nl = 0;
+      if (want_v) jl[nl++] = low_job(sy, B, 1, dx != nullptr);
+      if (want_u) jl[nl++] = low_job(sx, A, 0, false);
+      run_low(jl, nl);
       if (dx) {
         e.undo_row = l.undo_in;
         const Tensor fa{l.wide_f, p.d, (int64_t)p.adapters * p.rank, 3, l.ld_x, p.adapters * p.rank * l.ld_x};

@@ -27,6 +27,7 @@ namespace {
 constexpr int kParts = 512;      // partial sums of squares of a matrix, at most
 constexpr float kXScale = 8192.f, kSScale = 1024.f;
 constexpr int kBlock = 4;  // stages of 64 summed on the tensor cores at a time, FP32 matrices
+constexpr int kPairBlock = 2;  // the same where products with low parts share the sum
 
 struct OrthoLayout {
   __half *x[2], *s, *p;  // planes x batch x rows x ld
@@ -356,7 +357,9 @@ float poly_scale(float b, float c) {
 // planes read each once. Where a phase has few tiles, a cluster of `split`
 // CTAs shares one: each sums a part of the contracted index, and the parts
 // meet in the shared memory of the CTA that writes that slice of the tile's
-// columns. The epilogue is a loop over eight columns, with its sums in tensor
+// columns. Products with a low part have a sum of their own, 2^-11 of the other,
+// so that this is cut off a third as often (an addition in tensor memory is not
+// rounded). The epilogue is a loop over eight columns, with its sums in tensor
 // memory: straight-line code for a whole tile is fetched anew in every phase
 // (it took 10 to 30 us a phase). Bound by the phases' latency (a barrier, the first loads, the join,
 // the writes: 4 to 6 us) until the products take longer.
@@ -454,7 +457,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
   const uint32_t region = base + kStages * kStageBytes;
   const uint32_t full = region + kRegionBytes, empty = full + 8 * kStages, acc_full = empty + 8 * kStages,
                  acc_empty = acc_full + 16, ready = acc_empty + 16, got = ready + 8, drain = got + 8,
-                 go = drain + 8, misc = go + 8;
+                 go = drain + 8, low_empty = go + 8, misc = low_empty + 8;
   unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
   volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
   volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
@@ -475,6 +478,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
     ptx::mbar_init(got, (kCluster - 1) * mma::kEpiWarps);
     ptx::mbar_init(drain, 1);
     ptx::mbar_init(go, 1);  // the producer has seen the barrier over the grid
+    ptx::mbar_init(low_empty, mma::kEpiWarps);
     *abort_s = 0;
     counts[0] = counts[1] = 0;
     ptx::fence_mbar_init();
@@ -599,7 +603,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer
     const bool lead = ptx::elect_one();
-    int st = 0, n = 0;
+    int st = 0, n = 0, lows = 0;
     uint32_t ph = 0;
     bool ok = true;
     for (int i = 0; i < a.steps && ok; ++i)
@@ -611,6 +615,13 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
         range(w, c0, c1);
         const int last_steps = ((k == 0 ? a.n : a.m) - (w.chunks - 1) * 64 + 15) / 16;
         for (int t = w.me; t < w.tiles && ok; t += w.workers) {
+          uint32_t acc_low = 0;
+          if (PLANES == 2 && c1 > c0) {
+            // the tile's sum of products with low parts, read by the epilogue of the tile before
+            ok = ptx::mbar_wait_warp(low_empty, (uint32_t)(lows & 1) ^ 1u, abort_s, mma::kWaitLimit);
+            ptx::tc_fence_after();
+            ++lows;
+          }
           for (int b0 = c0; b0 < c1 && ok; b0 += kBlock, ++n) {
             ok = ptx::mbar_wait_warp(acc_empty + 8 * (n & 1), (uint32_t)((n >> 1) & 1) ^ 1u, abort_s, mma::kWaitLimit);
             if (!ok) break;
@@ -629,8 +640,13 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
                 for (int pr = PLANES == 2 ? 0 : 2; pr < 3; ++pr) {
                   uint64_t da = mma::desc(sa + (pr == 0 ? kTileBytes : 0), amn), db = mma::desc(sb + (pr == 1 ? kTileBytes : 0), bmn);
                   for (int e = 0; e < steps; ++e, da += amn ? 2048 >> 4 : 32 >> 4, db += bmn ? 2048 >> 4 : 32 >> 4) {
-                    ptx::mma_f16(d, da, db, id, acc);
-                    acc = 1;
+                    if (pr < 2) {
+                      ptx::mma_f16(tmem + 384u, da, db, id, acc_low);
+                      acc_low = 1;
+                    } else {
+                      ptx::mma_f16(d, da, db, id, acc);
+                      acc = 1;
+                    }
                   }
                 }
                 ptx::mma_commit(empty + 8 * st);
@@ -656,7 +672,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
     // registers takes a cycle for every 16 bytes (128 x 128 FP32 tiles: 9,000
     // clocks of a phase).
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * 64, sums = lanes + 256;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * 64, sums = lanes + 256, lows = lanes + 384;
     int n = 0, joins = 0, st = 0;
     uint32_t ph = 0;
     bool ok = true;
@@ -731,6 +747,13 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
                 if (owner == rank) continue;
                 uint32_t v[32];
                 ptx::tmem_ld32(src + p * 32, v);
+                if (PLANES == 2) {
+                  uint32_t low[32];
+                  ptx::tmem_ld32(lows + p * 32, low);
+                  ptx::tmem_wait_ld();
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
+                }
                 ptx::tmem_wait_ld();
                 const int slot = rank < owner ? rank : rank - 1;
                 const uint32_t dst = ptx::mapa(region + quarter * kPartBytes, owner) +
@@ -761,7 +784,13 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
             ptx::tmem_ld32(src + p * 32, bits);
             ptx::tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[p][j] = __uint_as_float(bits[j]);
+            for (int j = 0; j < 32; ++j) v[p][j] = blocks ? __uint_as_float(bits[j]) : 0.f;
+            if (PLANES == 2 && blocks) {
+              ptx::tmem_ld32(lows + p * 32, bits);
+              ptx::tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[p][j] += __uint_as_float(bits[j]);
+            }
             if (split) {
               // the parts in their order: those of lower CTAs, this one's, those of higher ones
               float s[32];
@@ -812,9 +841,10 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
             if (lane == 0 && last_of_eight(counts)) ptx::mbar_arrive(empty + 8 * st);
             if (++st == kStages) st = 0, ph ^= 1u;
           }
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (PLANES == 2 && blocks && lane == 0) ptx::mbar_arrive(low_empty);
           if (blocks == 1) {
-            ptx::tc_fence_before();
-            __syncwarp();
             if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * (n & 1));
             ++n;
           }
@@ -1010,7 +1040,7 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
   a.m_tiles = (int)ceil_div(M, tm);
   a.n_tiles = (int)ceil_div(N, a.bn);
   a.sym = sym;
-  a.block = kBlock;
+  a.block = kPairBlock;
   a.a_rows = 128;
   const uint32_t id = mma::idesc(tm, a.bn, false, a_mn, b_mn);
   if (PLANES == 2) {
