@@ -35,14 +35,21 @@ typedef __nv_bfloat16 bf16;
 constexpr int kBlock = 4;  // stages of 64 the tensor cores sum before the sum is drained, FP32
 
 // ---------------------------------------------------------------- copies
-// A BF16 matrix whose rows TMA cannot read, in rows of ldo.
+// A BF16 matrix whose rows TMA cannot read, in rows of ldo: 2048 columns of a
+// row a block.
 __global__ void __launch_bounds__(256)
-    k_copy_rows(const bf16* in, int64_t ld, int64_t rows, int cols, bf16* out, int64_t ldo) {
+    k_copy_rows(const uint16_t* in, int64_t ld, int cols, int parts, uint16_t* out, int64_t ldo) {
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int lane = threadIdx.x & 31;
-  for (int64_t p = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); p < rows; p += (int64_t)gridDim.x * 8)
-    for (int i = lane; i < cols; i += 32) out[p * ldo + i] = in[p * ld + i];
+  const int64_t row = blockIdx.x / parts;
+  const int c0 = (int)(blockIdx.x - row * parts) * 2048 + threadIdx.x;
+  uint16_t v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (c0 + k * 256 < cols) v[k] = in[row * ld + c0 + k * 256];
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (c0 + k * 256 < cols) out[row * ldo + c0 + k * 256] = v[k];
 }
 
 // ---------------------------------------------------------------- FP32 rows
@@ -52,7 +59,7 @@ struct RowJob {
   int set_aside = 0;            // a row of A
   const float* in = nullptr;
   int64_t ld = 0, rows = 0;
-  int width = 0, vec = 0;       // vec: rows can be read 16 bytes at a time
+  int width = 0, vec = 0;       // vec: elements of a row that can be read together, 4, 2 or 1
   const float* fold = nullptr;  // a factor of each column
   int most = 0;                 // the largest power used
   __half* planes = nullptr;     // two FP16 planes under a power of two
@@ -112,6 +119,9 @@ __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int
     if constexpr (VEC == 4) {
       const float4 q = __ldg(reinterpret_cast<const float4*>(r + i));
       v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+    } else if constexpr (VEC == 2) {
+      const float2 q = __ldg(reinterpret_cast<const float2*>(r + i));
+      v[0] = q.x, v[1] = q.y;
     } else {
       v[0] = __ldg(r + i);
     }
@@ -150,6 +160,11 @@ __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int
       split_f16(v, hi, lo);
       *reinterpret_cast<uint2*>(o + i) = uint2{hi[0], hi[1]};
       *reinterpret_cast<uint2*>(o + a.plane + i) = uint2{lo[0], lo[1]};
+    } else if constexpr (VEC == 2) {
+      uint32_t hi[1], lo[1];
+      split_f16(v, hi, lo);
+      *reinterpret_cast<uint32_t*>(o + i) = hi[0];
+      *reinterpret_cast<uint32_t*>(o + a.plane + i) = lo[0];
     } else {
       const __half hi = __float2half_rn(v[0]);
       o[i] = hi;
@@ -183,7 +198,10 @@ __global__ void __launch_bounds__(128, 6) k_rows_f32(const __grid_constant__ Row
   for (int64_t row = (int64_t)first * 4 + (threadIdx.x >> 5); row < a.rows; row += step) {
     const float* r = a.in + row * a.ld;
     float f = 1.f;
-    if (a.planes) f = a.vec ? row_planes<4>(a, r, row, lane) : row_planes<1>(a, r, row, lane);
+    if (a.planes)
+      f = a.vec == 4   ? row_planes<4>(a, r, row, lane)
+          : a.vec == 2 ? row_planes<2>(a, r, row, lane)
+                       : row_planes<1>(a, r, row, lane);
     if (a.side || a.set_aside) {
       // B of this class, over the class's power of two; or a row of A
       bool odd = false;
@@ -219,14 +237,15 @@ struct LowJobs {
   const int32_t* adapter;
   const float* scales;
   int64_t tokens, ldw;
-  int G, r, tile;
+  int G, r, tile, share;  // share: warps on a group, each a part of the width
 };
 constexpr int kLowTile = 128;  // rows of a block, at most
 
 template <int VEC, bool J_INNER>
-__device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x)[4], const float* F, int nj, int lane,
-                                         float (&acc)[32]) {
-  for (int i = lane * VEC; i < a.width; i += 32 * VEC) {
+__device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x)[4], const float* F, int nj, int at,
+                                         int step, float (&acc)[32]) {
+#pragma unroll(VEC == 4 ? 1 : 2)
+  for (int i = at * VEC; i < a.width; i += step * VEC) {
     float v[4][VEC], f[8][VEC];
     if constexpr (J_INNER) {  // eight neighbours of the factor (VEC = 1)
       const float* fp = F + (int64_t)i * a.f_i;
@@ -262,7 +281,9 @@ __device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x
 }
 
 __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJobs a) {
-  __shared__ int id[kLowTile], order[kLowTile], starts[kLowTile + 1], sums[8];
+  __shared__ __align__(16) int id[kLowTile];
+  __shared__ int order[kLowTile], starts[kLowTile + 1], sums[8];
+  __shared__ float parts[8][32];
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   const LowJob& job = a.job[blockIdx.z];
@@ -274,12 +295,16 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
   if (tid < n) {
     const int g = __ldg(a.adapter + t0 + tid);
     mine = g >= 0 && g < a.G ? g : a.G;
-    id[tid] = mine;
   }
+  if (tid < kLowTile) id[tid] = tid < n ? mine : 0x7fffffff;
   __syncthreads();
   if (tid < n) {
     int rank = 0;
-    for (int k = 0; k < n; ++k) rank += id[k] < mine || (id[k] == mine && k < tid);
+    for (int k = 0; k < n; k += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(id + k);
+      rank += (v.x < mine || (v.x == mine && k < tid)) + (v.y < mine || (v.y == mine && k + 1 < tid)) +
+              (v.z < mine || (v.z == mine && k + 2 < tid)) + (v.w < mine || (v.w == mine && k + 3 < tid));
+    }
     order[rank] = tid;
   }
   __syncthreads();
@@ -302,24 +327,28 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
   if (start) starts[at] = tid;
   if (tid == 0) starts[groups] = n;
   __syncthreads();
-  for (int q = warp; q < groups; q += 8) {
-    const int first = starts[q], count = starts[q + 1] - first;
+  const int share = a.share, part = warp % share;
+  for (int q0 = 0; q0 < groups; q0 += 8 / share) {
+    const int q = q0 + warp / share;
+    const bool live = q < groups;
+    const int first = live ? starts[q] : 0, count = live ? starts[q + 1] - first : 0;
     const int g = id[order[first]];
-    const bool any = g < a.G;
+    const bool any = live && g < a.G;
     float acc[32];
 #pragma unroll
     for (int k = 0; k < 32; ++k) acc[k] = 0.f;
     if (any) {
+      const int at = part * 32 + lane, step = share * 32;
       const float* x[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[k] = job.in + (t0 + order[first + min(k, count - 1)]) * job.ld;
       const float* F = job.F + g * job.f_g + j0 * job.f_j;
       if (job.f_j == 1)
-        low_dots<1, true>(job, x, F, nj, lane, acc);
+        low_dots<1, true>(job, x, F, nj, at, step, acc);
       else if (job.vec)
-        low_dots<4, false>(job, x, F, nj, lane, acc);
+        low_dots<4, false>(job, x, F, nj, at, step, acc);
       else
-        low_dots<1, false>(job, x, F, nj, lane, acc);
+        low_dots<1, false>(job, x, F, nj, at, step, acc);
     }
     // 32 sums on 32 lanes: halve the values, double the lanes that share one
 #pragma unroll
@@ -331,6 +360,14 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
         acc[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
       }
     }
+    if (share > 1) {  // the parts of the width, in order
+      __syncthreads();
+      parts[warp][lane] = acc[0];
+      __syncthreads();
+      if (part > 0) continue;
+      for (int o = 1; o < share; ++o) acc[0] += parts[warp + o][lane];
+    }
+    if (!live) continue;
     const int k = lane >> 3, j = lane & 7;
     const int64_t t = t0 + order[first + min(k, count - 1)];
     const float s = any && a.scales ? __ldg(a.scales + g) : 1.f;
@@ -627,6 +664,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_const
 // ---------------------------------------------------------------- shared product
 template <typename T>
 struct AdaptEpi {
+  static constexpr bool kTurns = true;
   T* y;
   int64_t ldy, rows;
   int cols, vec;
@@ -730,9 +768,10 @@ struct AdaptEpi {
     }
   }
 
-  __device__ __forceinline__ void store(int row0, int col0, int, int lane, bool many, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int, int lane, bool many, uint32_t turn,
+                                        const uint32_t (&acc)[32]) const {
     const int left = cols - col0;
-    const int64_t p = row0 + lane;
+    const int64_t p = (int64_t)row0 + lane;
     if (left <= 0) return;
     // what belongs to a column, a lane each
     const float uc = undo_col && lane < left ? __ldg(undo_col + col0 + lane) : 1.f;
@@ -750,30 +789,40 @@ struct AdaptEpi {
       for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bc, j);
     }
     if (odd) odd_values(p, col0, left, lane, v);
-    if (p >= rows) return;
-    if (u && !odd && (always || many)) low(p, col0, left, v);
-    T* o = y + p * ldy + col0;
-    constexpr int kVec = 16 / sizeof(T);
+    if (p < rows && u && !odd && (always || many)) low(p, col0, left, v);
+    // Turned in shared memory: a row from a thread would take a cycle for every
+    // 16 bytes, or for every element where rows are not whole vectors.
+    constexpr int kWords = 8 * sizeof(T), kStride = kWords + 1;  // 32-bit words of a row
+    uint32_t w[kWords];
+    round_to<T>(v, w);
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < kWords; ++q)
+      asm volatile("st.shared.b32 [%0], %1;" ::"r"(turn + (uint32_t)((lane * kStride + q) * 4)), "r"(w[q]) : "memory");
+    __syncwarp();
+    auto word = [&](int row, int q) {
+      uint32_t x;
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(turn + (uint32_t)((row * kStride + q) * 4)) : "memory");
+      return x;
+    };
+    const int have = (int)min((int64_t)32, rows - row0);
     if (vec && left >= 32) {
-      uint32_t w[8 * sizeof(T)];
-      round_to<T>(v, w);
+      constexpr int kLanes = kWords / 4;  // lanes a row
 #pragma unroll
-      for (int q = 0; q < 32 / kVec; ++q)
-        *reinterpret_cast<uint4*>(o + q * kVec) = uint4{w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]};
-      return;
-    }
-#pragma unroll
-    for (int q = 0; q < 32 / kVec; ++q) {
-      if (q * kVec >= left) break;
-      __align__(16) T h[kVec];
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) h[j] = from_f32<T>(v[q * kVec + j]);
-      if (vec && left >= (q + 1) * kVec) {
-        *reinterpret_cast<uint4*>(o + q * kVec) = *reinterpret_cast<const uint4*>(h);
-      } else {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j)
-          if (q * kVec + j < left) o[q * kVec + j] = h[j];
+      for (int r0 = 0; r0 < 32; r0 += 32 / kLanes) {
+        const int r = r0 + lane / kLanes, q = lane % kLanes * 4;
+        if (r < have)
+          *reinterpret_cast<uint4*>(y + ((int64_t)row0 + r) * ldy + col0 + q * (4 / sizeof(T))) =
+              uint4{word(r, q), word(r, q + 1), word(r, q + 2), word(r, q + 3)};
+      }
+    } else if (lane < left) {
+      T* o = y + (int64_t)row0 * ldy + col0 + lane;
+#pragma unroll 8
+      for (int r = 0; r < have; ++r) {
+        if constexpr (sizeof(T) == 4)
+          o[r * ldy] = __uint_as_float(word(r, lane));
+        else
+          reinterpret_cast<uint16_t*>(o)[r * ldy] = (uint16_t)(word(r, lane / 2) >> (lane & 1) * 16);
       }
     }
   }
@@ -1103,8 +1152,8 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
   if (warp == 4) ptx::tmem_dealloc(tmem, cols);
 }
 
-// FP32, on the CUDA cores: 64 of i, eight of j, the listed rows dealt over
-// sixteen groups of threads.
+// FP32, on the CUDA cores: 64 of i, eight of j at a time, the listed rows dealt
+// over GROUPS groups of threads (as many as an adapter has rows for).
 struct OuterJobF32 {
   const float* in;
   int64_t ld;
@@ -1117,44 +1166,51 @@ struct OuterJobsF32 {
   OuterJobF32 job[2];
   const int32_t* adapter;
   int64_t tokens;
-  int r, groups;  // groups: of eight columns
+  int r;
 };
 
-__global__ void __launch_bounds__(1024) k_outer_f32(const OuterJobsF32 a) {
-  __shared__ float red[16][8][64];  // 32 KB; the list before it
-  __shared__ int count[32];
-  uint16_t* list = reinterpret_cast<uint16_t*>(red);
+template <int GROUPS>
+__global__ void __launch_bounds__(64 * GROUPS) k_outer_f32(const __grid_constant__ OuterJobsF32 a) {
+  __shared__ float red[GROUPS][8][64];
+  __shared__ uint16_t list[kWindow];
+  __shared__ int count[2 * GROUPS];
   const OuterJobF32& job = a.job[blockIdx.z];
-  const int tile = blockIdx.x / a.groups, g = blockIdx.y, j0 = (blockIdx.x - tile * a.groups) * 8;
-  const int ti = threadIdx.x & 63, q = threadIdx.x >> 6, i = tile * 64 + ti;
-  if (tile * 64 >= job.width) return;
+  const int g = blockIdx.y;
+  const int ti = threadIdx.x & 63, q = threadIdx.x >> 6, i = blockIdx.x * 64 + ti;
+  if (blockIdx.x * 64 >= job.width) return;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int nj = min(8, a.r - j0);
-  float acc[8] = {};
-  for (int64_t t0 = 0; t0 < a.tokens; t0 += kWindow) {
-    const int64_t t1 = min(t0 + kWindow, a.tokens);
-    const int n = list_rows<1024>(a.adapter, t0, t1, g, list, count, threadIdx.x);
-#pragma unroll 8
-    for (int k = q; k < n; k += 16) {
-      const int64_t t = t0 + list[k];
-      const float x = i < job.width ? __ldg(job.in + t * job.ld + i) : 0.f;
-      const float* c = job.c + t * a.r + j0;
+  int n = 0;
+  int64_t t0 = 0;
+  const bool once = a.tokens <= kWindow;  // one list serves all j
+  if (once) n = list_rows<64 * GROUPS>(a.adapter, 0, a.tokens, g, list, count, threadIdx.x);
+  for (int j0 = 0; j0 < a.r; j0 += 8) {
+    const int nj = min(8, a.r - j0);
+    float acc[8] = {};
+    for (t0 = 0; t0 < a.tokens; t0 += kWindow) {
+      if (!once) n = list_rows<64 * GROUPS>(a.adapter, t0, min(t0 + kWindow, a.tokens), g, list, count, threadIdx.x);
+#pragma unroll 4
+      for (int k = q; k < n; k += GROUPS) {
+        const int64_t t = t0 + list[k];
+        const float x = i < job.width ? __ldg(job.in + t * job.ld + i) : 0.f;
+        const float* c = job.c + t * a.r + j0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < nj) acc[j] = fmaf(x, __ldg(c + j), acc[j]);
+        for (int j = 0; j < 8; ++j)
+          if (j < nj) acc[j] = fmaf(x, __ldg(c + j), acc[j]);
+      }
+      if (!once) __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) red[q][j][ti] = acc[j];
+    __syncthreads();
+    for (int e = threadIdx.x; e < nj * 64; e += 64 * GROUPS) {
+      const int j = e >> 6, k = e & 63, at = blockIdx.x * 64 + k;
+      float s = red[0][j][k];
+#pragma unroll
+      for (int w = 1; w < GROUPS; ++w) s += red[w][j][k];
+      if (at < job.width) job.out[g * job.f_g + (j0 + j) * job.f_j + (int64_t)at * job.f_i] = s;
     }
     __syncthreads();
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) red[q][j][ti] = acc[j];
-  __syncthreads();
-  for (int e = threadIdx.x; e < nj * 64; e += 1024) {
-    const int j = e >> 6, k = e & 63, at = tile * 64 + k;
-    float s = red[0][j][k];
-#pragma unroll
-    for (int w = 1; w < 16; ++w) s += red[w][j][k];
-    if (at < job.width) job.out[g * job.f_g + (j0 + j) * job.f_j + (int64_t)at * job.f_i] = s;
   }
 }
 
@@ -1223,8 +1279,9 @@ struct Op {
   Tensor readable(const void* in, int64_t ld, int64_t rows, int cols, int64_t planes, uint16_t* copy, int64_t ldo) {
     if (mma::mappable(in, ld)) return Tensor{in, cols, rows, planes, ld, rows * ld};
     const int64_t all = rows * planes;
-    launch_pdl(k_copy_rows, dim3((unsigned)std::min<int64_t>(ceil_div(all, 8), 1 << 16)), 256, s,
-               reinterpret_cast<const bf16*>(in), ld, all, cols, reinterpret_cast<bf16*>(copy), ldo);
+    const int parts = (int)ceil_div(cols, 2048);
+    launch_pdl(k_copy_rows, dim3((unsigned)(all * parts)), 256, s, reinterpret_cast<const uint16_t*>(in), ld, cols, parts,
+               copy, ldo);
     LC_LAUNCH_CHECK("k_copy_rows");
     return Tensor{copy, cols, rows, planes, ldo, rows * ldo};
   }
@@ -1241,7 +1298,9 @@ struct Op {
     j.ld = ld;
     j.rows = rows;
     j.width = width;
-    j.vec = width % 4 == 0 && ld % 4 == 0 && ((uintptr_t)in & 15) == 0;
+    j.vec = width % 4 == 0 && ld % 4 == 0 && ((uintptr_t)in & 15) == 0 ? 4
+            : width % 2 == 0 && ld % 2 == 0 && ((uintptr_t)in & 7) == 0 ? 2
+                                                                        : 1;
     return j;
   }
   RowJob planes_job(const void* in, int64_t ld, int64_t rows, int width, uint16_t* out, int64_t ldo, float* undo, int most) {
@@ -1279,8 +1338,10 @@ struct Op {
     a.ldw = l.ld_g;
     a.G = p.adapters;
     a.r = p.rank;
-    // more rows a block leave fewer groups short; fewer fill the device
-    a.tile = p.tokens >= 64 * (int64_t)mma::num_sms() * 2 ? 128 : p.tokens >= 32 * (int64_t)mma::num_sms() ? 64 : 32;
+    // more rows a block leave fewer groups short; fewer fill the device, and then warps share them
+    const int64_t sms = mma::num_sms();
+    a.tile = p.tokens >= 128 * sms ? 128 : p.tokens >= 32 * sms ? 32 : 8;
+    a.share = a.tile == 8 ? 4 : 1;
     launch_pdl(k_low_f32, dim3((unsigned)ceil_div(p.tokens, a.tile), (unsigned)ceil_div(p.rank, 8), (unsigned)n), 256, s, a);
     LC_LAUNCH_CHECK("k_low_f32");
   }
@@ -1315,7 +1376,7 @@ struct Op {
       j.factor = mma::tensor_map(d.factor, d.f_mn ? 64 : rn);
       j.f_bytes = cols * 128;
       j.per = std::min(8, 32768 / j.f_bytes);
-      const mma::Seg g = mma::segment(d.rows.cols, 0, 0, mma::idesc(128, cols, true, false, d.f_mn));
+      const mma::Seg g = mma::segment(d.rows.cols, mma::idesc(128, cols, true, false, d.f_mn));
       j.chunks = g.chunks;
       j.last = g.last;
       j.idesc = g.idesc;
@@ -1377,11 +1438,8 @@ struct Op {
     a.a_rows = (int)std::min<int64_t>(128, round_up(p.tokens, 8));
     a.block = kBlock;
     const uint32_t id = mma::idesc(tm, a.bn, !f32, false, w_mn);
-    if (f32) {
-      a.seg[a.nseg++] = mma::segment(d.width, 0, 1, id);
-      a.seg[a.nseg++] = mma::segment(d.width, 1, 0, id);
-    }
-    a.seg[a.nseg++] = mma::segment(d.width, 0, 0, id);
+    a.seg = mma::segment(d.width, id);
+    a.a_planes = a.b_planes = 1;
     mma::Maps maps;
     maps.a = mma::tensor_map(rows, a.a_rows);
     maps.b = mma::tensor_map(w, w_mn ? 64 : a.bn / (pair ? 2 : 1));
@@ -1394,7 +1452,7 @@ struct Op {
       a.low.G = p.adapters;
       a.low.dense = f32;
       const int64_t k = f32 ? (int64_t)p.adapters * p.rank : p.rank;
-      const mma::Seg g = mma::segment(k, 0, 0, mma::idesc(tm, a.bn, true, false, f_mn));
+      const mma::Seg g = mma::segment(k, mma::idesc(tm, a.bn, true, false, f_mn));
       a.low.chunks = g.chunks;
       a.low.last = g.last;
       a.low.idesc = g.idesc;
@@ -1410,9 +1468,9 @@ struct Op {
       maps.lb = mma::tensor_map(*F, f_mn ? 64 : a.bn / (pair ? 2 : 1));
     }
     if (pair)
-      mma::launch<2, f32>(maps, a, e, s);
+      mma::launch<2, f32 ? 2 : 1>(maps, a, e, s);
     else
-      mma::launch<1, f32>(maps, a, e, s);
+      mma::launch<1, f32 ? 2 : 1>(maps, a, e, s);
   }
 
   AdaptEpi<T> epilogue(T* y, int64_t ldy, int cols) {
@@ -1542,9 +1600,11 @@ struct Op {
         o.adapter = p.adapter;
         o.tokens = p.tokens;
         o.r = p.rank;
-        o.groups = (int)ceil_div(p.rank, 8);
-        launch_pdl(k_outer_f32, dim3((unsigned)(ceil_div(wide, 64) * o.groups), (unsigned)p.adapters, (unsigned)n),
-                   1024, s, o);
+        const dim3 grid((unsigned)ceil_div(wide, 64), (unsigned)p.adapters, (unsigned)n);
+        if (p.tokens >= 256 * (int64_t)p.adapters)
+          launch_pdl(k_outer_f32<16>, grid, 1024, s, o);
+        else
+          launch_pdl(k_outer_f32<4>, grid, 256, s, o);
         LC_LAUNCH_CHECK("k_outer_f32");
       }
     } else {

@@ -1,7 +1,7 @@
-// Tensor-core products for the operators of heads: D = sum over segments of
-// A_s B_s^T in tiles of 128 CG x BN, with an epilogue of the caller's.
+// Tensor-core products for the operators of heads: D = A B^T (+ low-rank
+// products) in tiles of 128 CG x BN, with an epilogue of the caller's.
 //
-// Operands are 16-bit (FP16 or BF16 in a segment) 3-D tensors read by TMA with
+// Operands are 16-bit (FP16 or BF16) 3-D tensors read by TMA with
 // the 128-byte swizzle, zero-filled past their ends, each either K-major (the
 // contracted index is the innermost) or MN-major. tcgen05 MMAs accumulate in
 // FP32 in tensor memory, two accumulators taking turns. CG = 2: a CTA pair
@@ -16,14 +16,16 @@
 //
 // The tensor cores' FP32 sums are cut off, not rounded, at each addition, which
 // shows in long sums as a drift of one sign (K = 1003 .. 2048, FP32 operands:
-// 1.8e-5 of the result after five Newton-Schulz steps). DRAIN breaks a sum
-// into blocks of `block` stages per segment: the epilogue warps take each
-// block's sums out of tensor memory and add them in registers, rounded, while
-// the MMAs of the next block run into the other accumulator.
+// 1.8e-5 of the result after five Newton-Schulz steps). PLANES = 2 (FP32: both
+// operands two planes, hi + lo, z apart by a_planes and b_planes; a stage holds
+// all four, for lo hi + hi lo + hi hi) breaks a sum into blocks of `block`
+// stages: the epilogue warps take each block's sums out of tensor memory and add
+// them in registers, rounded, while the MMAs of the next block run into the
+// other accumulator.
 //
-// A segment can be limited to some rows of the tile (`mask`): the MMA's
-// disabled output lanes keep what they hold, so that rows of other adapters
-// neither change nor turn NaN.
+// A low-rank product can be limited to some rows of the tile: the MMA's disabled
+// output lanes keep what they hold, so that rows of other adapters neither
+// change nor turn NaN.
 #pragma once
 
 #include "operators.cuh"
@@ -37,16 +39,15 @@ namespace mma {
 constexpr int kChunk = 64;           // contracted elements of a stage
 constexpr int kABytes = 128 * 128;   // 128 rows x 64 elements
 constexpr int kEpiWarps = 8;
+constexpr int kTurnBytes = 32 * 33 * 4;  // a warp's block of 32 x 32, turned for coalesced writes
 constexpr int kThreads = 32 * (2 + kEpiWarps);
 constexpr long long kWaitLimit = 1LL << 31;  // ~1 s at GB300 clocks
 constexpr int kSmem = 227 * 1024;
-constexpr int kMaxSegs = 4;
 
-// One product of the sum: `chunks` stages along the contracted index, the last
-// one of `last` MMAs (16 elements each).
+// A product: `chunks` stages along the contracted index, the last one of `last`
+// MMAs (16 elements each).
 struct Seg {
   int chunks, last;
-  int a_z, b_z;    // added to the tile's batch index
   uint32_t idesc;
 };
 
@@ -211,9 +212,9 @@ struct Args {
   int stages;
   int a_rows;  // rows of A's box (K-major): 128, or fewer where the tile has no more
   int a_mn, b_mn, lb_mn;
-  int nseg;
-  int block;  // stages of each segment per block (DRAIN: all segments have the same stages)
-  Seg seg[kMaxSegs];
+  int a_planes, b_planes;  // z from a plane to the next
+  int block;  // stages per block (DRAIN)
+  Seg seg;
   Low low;
   unsigned long long* errors;  // expired waits, counted
 };
@@ -246,16 +247,18 @@ __device__ __forceinline__ void tile_at(const Args& a, int t, int& mt, int& nt, 
   mt = band * 8 + rest - nt * high;
 }
 
-template <int CG, bool DRAIN, typename Epi>
+template <int CG, int PLANES, typename Epi>
 __global__ void __launch_bounds__(kThreads, 1)
     k_mma(const __grid_constant__ Maps maps, const Args a, const Epi epi) {
+  constexpr bool DRAIN = PLANES == 2;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  const int b_bytes = a.bn / CG * 128, stage_bytes = kABytes + b_bytes;
+  // a stage: A's planes, then B's
+  const int b_bytes = a.bn / CG * 128, stage_bytes = PLANES * (kABytes + b_bytes);
   const int nst = a.stages;
   const uint32_t bars = base + nst * stage_bytes;
   const uint32_t full = bars, empty = bars + 8 * nst, acc_full = empty + 8 * nst, acc_empty = acc_full + 16,
-                 drain = acc_empty + 16, misc = drain + 8;
+                 drain = acc_empty + 16, misc = drain + 8, turn = (misc + 16 + 127) & ~127u;
   unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
   volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
   volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
@@ -299,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = *tmem_slot;
   const int per = a.sym ? a.m_tiles * (a.m_tiles + 1) / 2 : a.m_tiles * a.n_tiles;
   const int tiles = per * a.batches;
-  const int chunks = a.nseg ? a.seg[0].chunks : 0;
+  const int chunks = a.seg.chunks;
 
   if (warp == 0) {
     // ------------------------------------------------------------ producer
@@ -308,49 +311,48 @@ __global__ void __launch_bounds__(kThreads, 1)
       int st = 0;
       uint32_t ph = 0;
       bool ok = true;
-      // one stage: the boxes of A at (row, k) and of B at (column, k)
+      // one stage: the boxes of A at (row, k) and of B at (column, k), of `planes` planes
       auto load = [&](const CUtensorMap* pa, bool a_mn, int row, int ak, int az, const CUtensorMap* pb, bool b_mn,
-                      int col, int bk, int bz) {
+                      int col, int bk, int bz, int planes) {
         ok = ptx::mbar_wait_warp(empty + 8 * st, ph ^ 1u, abort_s, kWaitLimit);
         if (!ok) return;
         const uint32_t slot = st;
         if (++st == nst) st = 0, ph ^= 1u;
         if (lane != 0) return;
-        if (rank == 0) ptx::mbar_expect_tx(full + 8 * slot, (uint32_t)(CG * (a.a_rows * 128 + b_bytes)));
-        const uint32_t sa = base + slot * stage_bytes, sb = sa + kABytes, bar = lead_full + 8 * slot;
+        if (rank == 0) ptx::mbar_expect_tx(full + 8 * slot, (uint32_t)(CG * planes * (a.a_rows * 128 + b_bytes)));
+        const uint32_t bar = lead_full + 8 * slot;
         auto box = [&](uint32_t dst, const CUtensorMap* m, int x, int y, int z) {
           if (CG == 2)
             load_3d_pair(dst, m, x, y, z, bar);
           else
             load_3d(dst, m, x, y, z, bar);
         };
-        if (a_mn) {
-          box(sa, pa, row, ak, az);
-          box(sa + 8192, pa, row + 64, ak, az);
-        } else {
-          box(sa, pa, ak, row, az);
-        }
-        if (b_mn) {
-          for (int i = 0; i < a.bn / CG; i += 64) box(sb + i * 128, pb, col + i, bk, bz);
-        } else {
-          box(sb, pb, bk, col, bz);
+        for (int p = 0; p < planes; ++p) {
+          const uint32_t sa = base + slot * stage_bytes + p * kABytes, sb = base + slot * stage_bytes + PLANES * kABytes + p * b_bytes;
+          const int za = az + p * a.a_planes, zb = bz + p * a.b_planes;
+          if (a_mn) {
+            box(sa, pa, row, ak, za);
+            box(sa + 8192, pa, row + 64, ak, za);
+          } else {
+            box(sa, pa, ak, row, za);
+          }
+          if (b_mn) {
+            for (int i = 0; i < a.bn / CG; i += 64) box(sb + i * 128, pb, col + i, bk, zb);
+          } else {
+            box(sb, pb, bk, col, zb);
+          }
         }
       };
       for (int t = worker; t < tiles && ok; t += workers) {
         int mt, nt, z;
         tile_at(a, t, mt, nt, z);
         const int row = mt * TM + (int)rank * 128, col = nt * a.bn + (int)rank * (a.bn / CG);
-        for (int c0 = 0; c0 < chunks && ok; c0 += a.block)
-          for (int s = 0; s < a.nseg && ok; ++s) {
-            const Seg& sg = a.seg[s];
-            const int c1 = min(c0 + a.block, sg.chunks);
-            for (int c = c0; c < c1 && ok; ++c)
-              load(&maps.a, a.a_mn, row, c * kChunk, sg.a_z + z, &maps.b, a.b_mn, col, c * kChunk, sg.b_z + z);
-          }
+        for (int c = 0; c < chunks && ok; ++c)
+          load(&maps.a, a.a_mn, row, c * kChunk, z, &maps.b, a.b_mn, col, c * kChunk, z, PLANES);
         if (a.low.dense) {
           for (int q = 0; q < a.low.pairs && ok; ++q)
             for (int c = 0; c < a.low.chunks && ok; ++c)
-              load(&maps.la, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk, a.low.b_z[q]);
+              load(&maps.la, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk, a.low.b_z[q], 1);
         } else if (a.low.G) {
           Groups<TM> gr;
           gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
@@ -359,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int q = 0; q < a.low.pairs && ok; ++q)
                 for (int c = 0; c < a.low.chunks && ok; ++c)
                   load(&maps.la, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk,
-                       a.low.b_z[q] * a.low.G + gr.g);
+                       a.low.b_z[q] * a.low.G + gr.g, 1);
         }
       }
     }
@@ -392,22 +394,26 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           ++n;
         };
-        // one stage of `steps` MMAs
-        auto chunk = [&](bool a_mn, bool b_mn, uint32_t id, int steps, const uint32_t* off) {
+        // one stage of `steps` MMAs (a product of planes each), the rows in `off` left alone
+        auto chunk = [&](bool a_mn, bool b_mn, uint32_t id, int steps, int planes, const uint32_t* off) {
           ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, kWaitLimit);
           if (!ok) return;
           ptx::tc_fence_after();
           if (lead) {
-            uint64_t da = desc(base + st * stage_bytes, a_mn), db = desc(base + st * stage_bytes + kABytes, b_mn);
+            const uint32_t sa = base + st * stage_bytes, sb = sa + PLANES * kABytes;
             const uint64_t ia = a_mn ? 2048 >> 4 : 32 >> 4, ib = b_mn ? 2048 >> 4 : 32 >> 4;
-            for (int k = 0; k < steps; ++k, da += ia, db += ib) {
-              if (off) {
-                const uint32_t o[8] = {off[0], off[1], off[2], off[3], off[4], off[5], off[6], off[7]};
-                mma_masked<CG>(d, da, db, id, 1u, o);
-              } else {
-                mma<CG>(d, da, db, id, acc);
+            // lo hi, hi lo, hi hi
+            for (int pr = planes == 2 ? 0 : 2; pr < 3; ++pr) {
+              uint64_t da = desc(sa + (pr == 0 ? kABytes : 0), a_mn), db = desc(sb + (pr == 1 ? b_bytes : 0), b_mn);
+              for (int k = 0; k < steps; ++k, da += ia, db += ib) {
+                if (off) {
+                  const uint32_t o[8] = {off[0], off[1], off[2], off[3], off[4], off[5], off[6], off[7]};
+                  mma_masked<CG>(d, da, db, id, 1u, o);
+                } else {
+                  mma<CG>(d, da, db, id, acc);
+                }
+                acc = 1;
               }
-              acc = 1;
             }
             if (CG == 2)
               ptx::mma_commit_pair_multicast(empty + 8 * st, (uint16_t)3);
@@ -422,17 +428,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             close();
             open();
           }
-          for (int s = 0; s < a.nseg && ok; ++s) {
-            const Seg& sg = a.seg[s];
-            const int c1 = min(c0 + a.block, sg.chunks);
-            for (int c = c0; c < c1 && ok; ++c)
-              chunk(a.a_mn, a.b_mn, sg.idesc, c == sg.chunks - 1 ? sg.last : 4, nullptr);
-          }
+          const int c1 = DRAIN ? min(c0 + a.block, chunks) : chunks;
+          for (int c = c0; c < c1 && ok; ++c)
+            chunk(a.a_mn, a.b_mn, a.seg.idesc, c == chunks - 1 ? a.seg.last : 4, PLANES, nullptr);
+          if (!DRAIN) c0 = chunks;
         }
         if (a.low.dense) {
           for (int q = 0; q < a.low.pairs && ok; ++q)
             for (int c = 0; c < a.low.chunks && ok; ++c)
-              chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, nullptr);
+              chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, 1, nullptr);
         } else if (a.low.G) {
           Groups<TM> gr;
           gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
@@ -443,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               for (int k = 0; k < TM / 32; ++k) off[k] = ~gr.on[k];
               for (int q = 0; q < a.low.pairs && ok; ++q)
                 for (int c = 0; c < a.low.chunks && ok; ++c)
-                  chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, off);
+                  chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, 1, off);
             }
         }
         close();
@@ -462,6 +466,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     // ------------------------------------------------------------ epilogue
     const int quarter = warp & 3, half = (warp - 2) >> 2;
+    const uint32_t mine = turn + (uint32_t)((warp - 2) * kTurnBytes);
     const uint32_t lead_empty = CG == 2 ? ptx::mapa(acc_empty, 0) : acc_empty;
     int n = 0;
     bool ok = true;
@@ -522,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[i][j]);
-          epi.store(row, nt * a.bn + c, z, lane, many, v);
+          epi.store(row, nt * a.bn + c, z, lane, many, mine, v);
         }
       } else {
         open();
@@ -531,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t v[32];
           ptx::tmem_ld32(src + c, v);
           ptx::tmem_wait_ld();
-          epi.store(row, nt * a.bn + c, z, lane, many, v);
+          epi.store(row, nt * a.bn + c, z, lane, many, mine, v);
         }
         close();
       }
@@ -573,19 +578,19 @@ struct Tensor {
 CUtensorMap tensor_map(const Tensor& t, int box_rows, int box_cols = 64);
 inline bool mappable(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
-inline Seg segment(int64_t k, int a_z, int b_z, uint32_t id) {
+inline Seg segment(int64_t k, uint32_t id) {
   const int chunks = (int)ceil_div(k, kChunk);
-  return Seg{chunks, (int)ceil_div(k - (int64_t)(chunks - 1) * kChunk, 16), a_z, b_z, id};
+  return Seg{chunks, (int)ceil_div(k - (int64_t)(chunks - 1) * kChunk, 16), id};
 }
 
-template <int CG, bool DRAIN, typename Epi>
+template <int CG, int PLANES, typename Epi>
 void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
-  const int stage = kABytes + a.bn / CG * 128;
+  const int stage = PLANES * (kABytes + a.bn / CG * 128);
   a.errors = error_counter();
-  if (!DRAIN) a.block = 1 << 30;
-  a.stages = std::min(8, (kSmem - 1024 - 512) / stage);
-  const int smem = 1024 + a.stages * stage + 512;
-  allow_smem(reinterpret_cast<const void*>(k_mma<CG, DRAIN, Epi>), kSmem);
+  const int turn = Epi::kTurns ? kEpiWarps * kTurnBytes + 128 : 0;
+  a.stages = std::min(8, (kSmem - 1024 - 512 - turn) / stage);
+  const int smem = 1024 + a.stages * stage + 512 + turn;
+  allow_smem(reinterpret_cast<const void*>(k_mma<CG, PLANES, Epi>), kSmem);
   const int64_t per = a.sym ? (int64_t)a.m_tiles * (a.m_tiles + 1) / 2 : (int64_t)a.m_tiles * a.n_tiles;
   const int64_t tiles = per * a.batches;
   LC_REQUIRE(tiles < (1LL << 31), LIPCACHE_E_INVALID, "too many tiles");
@@ -603,7 +608,7 @@ void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CG == 2 ? 2 : 1;
-  LC_CUDA(cudaLaunchKernelEx(&cfg, k_mma<CG, DRAIN, Epi>, maps, a, epi));
+  LC_CUDA(cudaLaunchKernelEx(&cfg, k_mma<CG, PLANES, Epi>, maps, a, epi));
   LC_LAUNCH_CHECK("k_mma");
 }
 

@@ -248,13 +248,14 @@ __device__ __forceinline__ void add_planes(const __half* d, int64_t plane, int l
 // S (of = null) or P = c S S + b S, both triangles.
 template <int PLANES>
 struct SymEpi {
+  static constexpr bool kTurns = false;
   __half* d;
   const __half* of;
   int64_t ld, mat, plane;  // row, matrix and plane strides
   int m, tile;
   float f, b;
   const float* t;  // nullable: squared into f
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = m - col0;
     if (left <= 0) return;
     float g = f;
@@ -273,13 +274,14 @@ struct SymEpi {
 // X' = a X + P X.
 template <int PLANES>
 struct UpdateEpi {
+  static constexpr bool kTurns = false;
   __half* d;
   const __half* x;
   int64_t ld, mat, plane;
   int rows, cols;
   float f, a;
   const float* t;
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
     const float u = t ? __ldcg(t + z) : 1.f, g = f * u;
@@ -295,6 +297,7 @@ struct UpdateEpi {
 // The last step: the result, or the weights' update, in the caller's type.
 template <int PLANES, typename T>
 struct LastEpi {
+  static constexpr bool kTurns = false;
   T* d;
   const T* w;  // null: the result itself
   const __half* x;
@@ -302,7 +305,7 @@ struct LastEpi {
   int rows, cols, vec;
   float f, a, keep, rate;
   const float* t;
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32]) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
     const float u = t ? __ldcg(t + z) : 1.f, g = f * u;
@@ -1043,17 +1046,14 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
   a.block = kPairBlock;
   a.a_rows = 128;
   const uint32_t id = mma::idesc(tm, a.bn, false, a_mn, b_mn);
-  if (PLANES == 2) {
-    a.seg[a.nseg++] = mma::segment(K, 0, batch, id);
-    a.seg[a.nseg++] = mma::segment(K, batch, 0, id);
-  }
-  a.seg[a.nseg++] = mma::segment(K, 0, 0, id);
+  a.seg = mma::segment(K, id);
+  a.a_planes = a.b_planes = batch;
   const CUtensorMap ma = mma::tensor_map(A, a_mn ? 64 : 128);
   const CUtensorMap mb = mma::tensor_map(B, b_mn ? 64 : pair ? 128 : a.bn);
   if (pair)
-    mma::launch<2, PLANES == 2>({ma, mb, ma, mb}, a, epi, s);
+    mma::launch<2, PLANES>({ma, mb, ma, mb}, a, epi, s);
   else
-    mma::launch<1, PLANES == 2>({ma, mb, ma, mb}, a, epi, s);
+    mma::launch<1, PLANES>({ma, mb, ma, mb}, a, epi, s);
 }
 
 template <typename T, int VEC, int PLANES>

@@ -77,23 +77,38 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
   __syncthreads();
   // neighbouring threads along memory: along j (wide) or i (tall)
   const int len = a.tall ? a.m : nj, lines = a.tall ? nj : a.m;
-  for (int e = tid; e < len * lines; e += kThreads) {
-    const int l = e / len, c = e - l * len;
-    const int i = a.tall ? c : l, j = a.tall ? l : c;
-    const int64_t src = a.tall ? (grow + j0 + j) * a.ldg + i : (grow + i) * a.ldg + j0 + j;
-    float v = to_f32<T>(g[src]);
-    if (a.st.weight) {
-      const int64_t o = at(i, j0 + j);
-      const float b = a.st.beta, m = fmaf(b, a.st.momentum[o], (1.f - b) * v);
-      a.st.out_momentum[o] = m;
-      v = a.st.nesterov ? fmaf(b, m, (1.f - b) * v) : m;
+  constexpr int kBatch = 8;  // elements of a thread whose loads are in flight together
+  for (int e0 = tid; e0 < len * lines; e0 += kThreads * kBatch) {
+    float v[kBatch], m[kBatch];
+    int at_x[kBatch];
+    int64_t o[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int e = e0 + q * kThreads;
+      v[q] = m[q] = 0.f;
+      at_x[q] = -1;
+      if (e >= len * lines) continue;
+      const int l = e / len, c = e - l * len, i = a.tall ? c : l, j = a.tall ? l : c;
+      v[q] = to_f32<T>(g[a.tall ? (grow + j0 + j) * a.ldg + i : (grow + i) * a.ldg + j0 + j]);
+      o[q] = at(i, j0 + j);
+      if (a.st.weight) m[q] = a.st.momentum[o[q]];
+      at_x[q] = i * a.stride + j;
     }
-    x[i * a.stride + j] = v;
-    const float w = fabsf(v);
-    if (w < 0x1p60f && (w > 0x1p-50f || w == 0.f))
-      run = fmaf(v, v, run);
-    else  // squares that FP32 does not hold
-      sum += (double)v * v;
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      if (at_x[q] < 0) continue;
+      if (a.st.weight) {
+        const float b = a.st.beta, n = fmaf(b, m[q], (1.f - b) * v[q]);
+        a.st.out_momentum[o[q]] = n;
+        v[q] = a.st.nesterov ? fmaf(b, n, (1.f - b) * v[q]) : n;
+      }
+      x[at_x[q]] = v[q];
+      const float w = fabsf(v[q]);
+      if (w < 0x1p60f && (w > 0x1p-50f || w == 0.f))
+        run = fmaf(v[q], v[q], run);
+      else  // squares that FP32 does not hold
+        sum += (double)v[q] * v[q];
+    }
   }
   sum += (double)run;
 #pragma unroll
@@ -207,12 +222,22 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
     }
     __syncthreads();
   }
-  for (int e = tid; e < len * lines; e += kThreads) {
-    const int l = e / len, c = e - l * len;
-    const int i = a.tall ? c : l, j = a.tall ? l : c;
-    const int64_t o = at(i, j0 + j);
-    const float v = x[i * a.stride + j];
-    out[o] = from_f32<TO>(a.st.weight ? fmaf(a.st.keep, to_f32<TO>(static_cast<const TO*>(a.st.weight)[o]), -a.st.rate * v) : v);
+  for (int e0 = tid; e0 < len * lines; e0 += kThreads * kBatch) {
+    float v[kBatch], w[kBatch];
+    int64_t o[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int e = e0 + q * kThreads;
+      o[q] = -1;
+      if (e >= len * lines) continue;
+      const int l = e / len, c = e - l * len, i = a.tall ? c : l, j = a.tall ? l : c;
+      o[q] = at(i, j0 + j);
+      v[q] = x[i * a.stride + j];
+      if (a.st.weight) w[q] = to_f32<TO>(static_cast<const TO*>(a.st.weight)[o[q]]);
+    }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q)
+      if (o[q] >= 0) out[o[q]] = from_f32<TO>(a.st.weight ? fmaf(a.st.keep, w[q], -a.st.rate * v[q]) : v[q]);
   }
   if (ctas > 1) cluster.sync();  // no CTA leaves while another reads its part
 }
