@@ -244,7 +244,7 @@ constexpr int kLowTile = 128;  // rows of a block, at most
 template <int VEC, bool J_INNER>
 __device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x)[4], const float* F, int nj, int at,
                                          int step, float (&acc)[32]) {
-#pragma unroll(VEC == 4 ? 1 : 2)
+#pragma unroll(VEC == 4 ? 1 : VEC == 2 ? 2 : 4)
   for (int i = at * VEC; i < a.width; i += step * VEC) {
     float v[4][VEC], f[8][VEC];
     if constexpr (J_INNER) {  // eight neighbours of the factor (VEC = 1)
@@ -257,6 +257,9 @@ __device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x
         if constexpr (VEC == 4) {
           const float4 q = j < nj ? __ldg(reinterpret_cast<const float4*>(F + j * a.f_j + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
           f[j][0] = q.x, f[j][1] = q.y, f[j][2] = q.z, f[j][3] = q.w;
+        } else if constexpr (VEC == 2) {
+          const float2 q = j < nj ? __ldg(reinterpret_cast<const float2*>(F + j * a.f_j + i)) : make_float2(0.f, 0.f);
+          f[j][0] = q.x, f[j][1] = q.y;
         } else {
           f[j][0] = j < nj ? __ldg(F + j * a.f_j + i) : 0.f;
         }
@@ -267,6 +270,9 @@ __device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x
       if constexpr (VEC == 4) {
         const float4 q = __ldg(reinterpret_cast<const float4*>(x[k] + i));
         v[k][0] = q.x, v[k][1] = q.y, v[k][2] = q.z, v[k][3] = q.w;
+      } else if constexpr (VEC == 2) {
+        const float2 q = __ldg(reinterpret_cast<const float2*>(x[k] + i));
+        v[k][0] = q.x, v[k][1] = q.y;
       } else {
         v[k][0] = __ldg(x[k] + i);
       }
@@ -345,8 +351,10 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
       const float* F = job.F + g * job.f_g + j0 * job.f_j;
       if (job.f_j == 1)
         low_dots<1, true>(job, x, F, nj, at, step, acc);
-      else if (job.vec)
+      else if (job.vec == 4)
         low_dots<4, false>(job, x, F, nj, at, step, acc);
+      else if (job.vec == 2)
+        low_dots<2, false>(job, x, F, nj, at, step, acc);
       else
         low_dots<1, false>(job, x, F, nj, at, step, acc);
     }
@@ -458,18 +466,19 @@ __global__ void __launch_bounds__(128)
 }
 
 // ---------------------------------------------------------------- shrink, tensor cores
-// u of 128 rows: D[row, j] of each row's own adapter, the adapters of the tile
-// in groups whose factors share a stage with the rows. A cluster splits the
-// contracted width; its first CTA joins the parts in order. Bound by reading
-// the rows once.
-constexpr int kShrinkThreads = 192, kShrinkStages = 4, kShrinkStage = 48 * 1024;
+// u of 128 rows. The factors of a tile's adapters stand side by side along N, so
+// that the rows are read, and the MMAs issued, once for all of them (up to 256
+// columns a pass); the epilogue takes each row's own columns. A cluster splits
+// the contracted width; its first CTA joins the parts in order. Bound by
+// reading the rows once, and by latency where they are few.
+constexpr int kShrinkThreads = 192, kShrinkStages = 3, kShrinkStage = 48 * 1024;
 struct ShrinkJob {
   CUtensorMap rows, factor;
   int chunks, last;
   int f_mn;       // the factor's contracted index is not its innermost
   int f_bytes;    // of a factor's part of a stage
   int per;        // factors in a stage
-  uint32_t idesc;
+  int cols;       // columns of D a factor
   float* u;       // tokens x r
   uint16_t* planes;
 };
@@ -489,9 +498,11 @@ __device__ __forceinline__ void store_cluster(uint32_t addr, float v) {
 __global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_constant__ ShrinkJobs a) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  float* part = reinterpret_cast<float*>(smem_raw + (base - ptx::smem_u32(smem_raw)));
-  const uint32_t full = base + kShrinkStages * kShrinkStage, empty = full + 8 * kShrinkStages,
-                 done = empty + 8 * kShrinkStages, misc = done + 8;
+  float* part = reinterpret_cast<float*>(smem_raw + (base - ptx::smem_u32(smem_raw)));  // others', in the stages
+  const uint32_t own_s = base + kShrinkStages * kShrinkStage;  // this CTA's u: [column][row]
+  float* own = part + kShrinkStages * kShrinkStage / 4;
+  const uint32_t full = own_s + 128 * 128 * 4, empty = full + 8 * kShrinkStages, acc_full = empty + 8 * kShrinkStages,
+                 acc_empty = acc_full + 16, misc = acc_empty + 16;
   unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
   volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
   volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
@@ -506,14 +517,17 @@ __global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_const
       ptx::mbar_init(full + 8 * s, 1);
       ptx::mbar_init(empty + 8 * s, 1);
     }
-    ptx::mbar_init(done, 1);
+    for (int b = 0; b < 2; ++b) {
+      ptx::mbar_init(acc_full + 8 * b, 1);
+      ptx::mbar_init(acc_empty + 8 * b, 4);
+    }
     *abort_s = 0;
     ptx::fence_mbar_init();
     ptx::tma_prefetch_desc(&job.rows);
     ptx::tma_prefetch_desc(&job.factor);
   }
   if (warp == 1) {
-    ptx::tmem_alloc(misc, 128);
+    ptx::tmem_alloc(misc, 512);
     ptx::tmem_relinquish();
   }
   ptx::tc_fence_before();
@@ -523,28 +537,29 @@ __global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_const
   ptx::launch_dependents();
   const uint32_t tmem = *tmem_slot;
   const int c0 = (int)((int64_t)job.chunks * rank / splits), c1 = (int)((int64_t)job.chunks * (rank + 1) / splits);
-  if (warp <= 1) {
-    // producer and issuer walk the same groups of adapters and chunks
+  const int cols = job.cols, row = (warp & 3) * 32 + lane;
+  bool ok = true;
+  {
+    // every role walks the same passes: up to `per` adapters of the tile each
     mma::Groups<128> gr;
     gr.begin(a.adapter, a.tokens, a.G, m0, lane);
     const bool lead = ptx::elect_one();
-    int st = 0;
+    const int my = gr.id[warp & 3];  // (epilogue) this thread's row's adapter
+    int st = 0, passes = 0;
     uint32_t ph = 0;
-    bool ok = true;
-    for (;;) {
+    for (bool more = gr.next(); more && ok; ++passes) {
       int g[8], n = 0;
-      uint32_t off[8][4];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        if (k >= job.per || n < k || !gr.next()) continue;
+        if (k >= job.per || !more) continue;
         g[k] = gr.g;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) off[k][w] = ~gr.on[w];
         n = k + 1;
+        more = gr.next();
       }
-      if (n == 0 || !ok) break;
-      for (int c = c0; c < c1 && ok; ++c) {
-        if (warp == 0) {
+      const int buf = passes & 1;
+      const uint32_t use = (uint32_t)(passes >> 1) & 1u;
+      if (warp == 0) {
+        for (int c = c0; c < c1 && ok; ++c) {
           ok = ptx::mbar_wait_warp(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
           if (!ok) break;
           if (lane == 0) {
@@ -561,110 +576,111 @@ __global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_const
                 mma::load_3d(sb, &job.factor, c * 64, 0, g[k], bar);
             }
           }
-        } else {
+          if (++st == kShrinkStages) st = 0, ph ^= 1u;
+        }
+      } else if (warp == 1) {
+        ok = ptx::mbar_wait_warp(acc_empty + 8 * buf, use ^ 1u, abort_s, mma::kWaitLimit);
+        ptx::tc_fence_after();
+        const uint32_t id = mma::idesc(128, n * cols, true, false, job.f_mn), d = tmem + (uint32_t)buf * 256u;
+        for (int c = c0; c < c1 && ok; ++c) {
           ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, mma::kWaitLimit);
           if (!ok) break;
           ptx::tc_fence_after();
           if (lead) {
             const uint32_t sa = base + st * kShrinkStage;
             const int steps = c == job.chunks - 1 ? job.last : 4;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              if (k >= n) break;
-              uint64_t da = mma::desc(sa, false), db = mma::desc(sa + 16384 + k * job.f_bytes, job.f_mn);
-              const uint32_t o[8] = {off[k][0], off[k][1], off[k][2], off[k][3], 0, 0, 0, 0};
-              for (int q = 0; q < steps; ++q, da += 32 >> 4, db += job.f_mn ? 2048 >> 4 : 32 >> 4)
-                mma::mma_masked<1>(tmem, da, db, job.idesc, c > c0 || q > 0, o);
-            }
+            uint64_t da = mma::desc(sa, false), db = mma::desc(sa + 16384, job.f_mn);
+            for (int q = 0; q < steps; ++q, da += 32 >> 4, db += job.f_mn ? 2048 >> 4 : 32 >> 4)
+              ptx::mma_f16(d, da, db, id, c > c0 || q > 0);
             ptx::mma_commit(empty + 8 * st);
           }
+          if (++st == kShrinkStages) st = 0, ph ^= 1u;
         }
-        if (++st == kShrinkStages) st = 0, ph ^= 1u;
+        if (ok && lead) ptx::mma_commit(acc_full + 8 * buf);
+      } else {
+        ok = ptx::mbar_wait_warp(acc_full + 8 * buf, use, abort_s, mma::kWaitLimit);
+        if (!ok) break;
+        ptx::tc_fence_after();
+        // each row's own columns, eight at a time
+        for (int k = 0; k < n; ++k) {
+          int gk = g[0];
+#pragma unroll
+          for (int q = 1; q < 8; ++q)
+            if (q == k) gk = g[q];
+          if (!__any_sync(0xffffffffu, my == gk)) continue;
+#pragma unroll 1
+          for (int j = 0; j < a.r; j += 8) {
+            float v[8];
+            mma::tmem_ld8(tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(buf * 256 + k * cols + j), v);
+            if (my == gk) {
+#pragma unroll
+              for (int q = 0; q < 8; ++q) own[(j + q) * 128 + row] = v[q];
+            }
+            __syncwarp();
+          }
+        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * buf);
       }
-    }
-    if (warp == 1) {
-      if (lead) {
-        volatile int never = 0;
-        ptx::mma_commit(done);
-        ptx::mbar_wait(done, 0, &never, mma::kWaitLimit);
-      }
-      __syncwarp();
     }
   }
   __syncwarp();
-  bool ok = true;
-  if (warp >= 2) {
-    ok = ptx::mbar_wait(done, 0, abort_s, mma::kWaitLimit);
-    ok = __all_sync(0xffffffffu, ok);
-    ptx::tc_fence_after();
-  }
-  const int row = (warp & 3) * 32 + lane;
-  const uint32_t src = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  const int64_t t = m0 + row;
+  const int id = t < a.tokens ? __ldg(a.adapter + t) : -1;
+  const bool any = id >= 0 && id < a.G;
   if (splits > 1) {
-    // the first CTA's stages are free: its products are done
+    // the first CTA's stages are free once all of them have their sums
     ptx::cluster_sync();
     if (warp >= 2 && rank > 0) {
-      const uint32_t dst = ptx::mapa(base, 0) + (uint32_t)((rank - 1) * 128 * a.rn) * 4;
-      for (int j0 = 0; j0 < a.rn; j0 += 32) {
-        uint32_t v[32];
-        ptx::tmem_ld32(src + j0, v);
-        ptx::tmem_wait_ld();
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-          if (j0 + j < a.rn) store_cluster(dst + (uint32_t)((j0 + j) * 128 + row) * 4, __uint_as_float(v[j]));
-      }
+      const uint32_t dst = ptx::mapa(base, 0) + (uint32_t)((rank - 1) * 128 * a.rn + row) * 4;
+#pragma unroll 8
+      for (int j = 0; j < a.r; ++j) store_cluster(dst + (uint32_t)(j * 128) * 4, own[j * 128 + row]);
     }
     ptx::cluster_sync();
   }
-  if (warp >= 2 && rank == 0 && ok) {
-    const int64_t t = m0 + row;
-    const int id = t < a.tokens ? __ldg(a.adapter + t) : -1;
-    const bool any = id >= 0 && id < a.G;
+  if (warp >= 2 && rank == 0 && ok && t < a.tokens) {
     const float s = any && a.scales ? __ldg(a.scales + id) : 1.f;
-    for (int j0 = 0; j0 < a.rn; j0 += 32) {
-      uint32_t v[32];
-      ptx::tmem_ld32(src + j0, v);
-      ptx::tmem_wait_ld();
-      if (t >= a.tokens) continue;
+#pragma unroll 1
+    for (int j0 = 0; j0 < a.ldo; j0 += 8) {
+      float f[8];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float f[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int j = j0 + q * 8 + k;
-          f[k] = __uint_as_float(v[q * 8 + k]);
-          if (j < a.rn)
-            for (uint32_t p = 1; p < splits; ++p) f[k] += part[((p - 1) * a.rn + j) * 128 + row];
-          f[k] = any && j < a.r ? s * f[k] : 0.f;
-          if (j < a.r) job.u[t * a.r + j] = f[k];
+      for (int k = 0; k < 8; ++k) {
+        const int j = j0 + k;
+        f[k] = 0.f;
+        if (any && j < a.r) {
+          f[k] = own[j * 128 + row];
+          for (uint32_t p = 1; p < splits; ++p) f[k] += part[((p - 1) * a.rn + j) * 128 + row];
+          f[k] *= s;
         }
-        if (j0 + q * 8 < a.ldo) {
-          uint32_t hi[4], lo[4];
-          split_bf16(f, hi, lo);
-          uint16_t* o = job.planes + t * a.ldo + j0 + q * 8;
-          *reinterpret_cast<uint4*>(o) = uint4{hi[0], hi[1], hi[2], hi[3]};
-          *reinterpret_cast<uint4*>(o + a.plane) = uint4{lo[0], lo[1], lo[2], lo[3]};
-        }
+        if (j < a.r) job.u[t * a.r + j] = f[k];
       }
+      uint32_t hi[4], lo[4];
+      split_bf16(f, hi, lo);
+      uint16_t* o = job.planes + t * a.ldo + j0;
+      *reinterpret_cast<uint4*>(o) = uint4{hi[0], hi[1], hi[2], hi[3]};
+      *reinterpret_cast<uint4*>(o + a.plane) = uint4{lo[0], lo[1], lo[2], lo[3]};
     }
   }
   ptx::tc_fence_before();
   __syncthreads();
   if (*abort_s) {
-    const long long t0 = clock64();
-    while (clock64() - t0 < (1LL << 23)) {
+    const long long t1 = clock64();
+    while (clock64() - t1 < (1LL << 23)) {
     }
     if (threadIdx.x == 0) atomicAdd(a.errors, 1ull);
     __syncthreads();
   }
   ptx::tc_fence_after();
-  if (warp == 1) ptx::tmem_dealloc(tmem, 128);
+  if (warp == 1) ptx::tmem_dealloc(tmem, 512);
 }
 
 // ---------------------------------------------------------------- shared product
-template <typename T>
+// EARLY: the few-rows form, whose epilogue takes the low-rank product of its
+// tile while the shared one is summed.
+template <typename T, bool EARLY = false>
 struct AdaptEpi {
-  static constexpr bool kTurns = true;
+  static constexpr bool kTurns = true, kEarly = EARLY;
   T* y;
   int64_t ldy, rows;
   int cols, vec;
@@ -674,7 +690,7 @@ struct AdaptEpi {
   const float* u;
   const T* F;
   const int32_t* adapter;
-  int G, r, f_vec, always;
+  int G, r, f_vec;
   int64_t f_col, f_j;
   // set-aside values of a dense low-rank product (NaN and infinities of the
   // factor), a flag for each column (n_odd = 0) or for each of n_odd rows of A
@@ -768,6 +784,15 @@ struct AdaptEpi {
     }
   }
 
+  // The low-rank product of 32 columns before the shared one is there (unscaled
+  // sums, every tile's: the few-rows form).
+  __device__ __forceinline__ bool ahead(int row0, int col0, int lane, float (&v)[32]) const {
+    if (!u) return false;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = 0.f;
+    if (row0 + lane < rows && col0 < cols) low(row0 + lane, col0, cols - col0, v);
+    return true;
+  }
   __device__ __forceinline__ void store(int row0, int col0, int, int lane, bool many, uint32_t turn,
                                         const uint32_t (&acc)[32]) const {
     const int left = cols - col0;
@@ -789,7 +814,7 @@ struct AdaptEpi {
       for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bc, j);
     }
     if (odd) odd_values(p, col0, left, lane, v);
-    if (p < rows && u && !odd && (always || many)) low(p, col0, left, v);
+    if (many && p < rows && u && !odd) low(p, col0, left, v);
     // Turned in shared memory: a row from a thread would take a cycle for every
     // 16 bytes, or for every element where rows are not whole vectors.
     constexpr int kWords = 8 * sizeof(T), kStride = kWords + 1;  // 32-bit words of a row
@@ -1203,8 +1228,9 @@ __global__ void __launch_bounds__(64 * GROUPS) k_outer_f32(const __grid_constant
 #pragma unroll
     for (int j = 0; j < 8; ++j) red[q][j][ti] = acc[j];
     __syncthreads();
+    // neighbouring threads along memory: along j or i
     for (int e = threadIdx.x; e < nj * 64; e += 64 * GROUPS) {
-      const int j = e >> 6, k = e & 63, at = blockIdx.x * 64 + k;
+      const int j = job.f_j == 1 ? e % nj : e >> 6, k = job.f_j == 1 ? e / nj : e & 63, at = blockIdx.x * 64 + k;
       float s = red[0][j][k];
 #pragma unroll
       for (int w = 1; w < GROUPS; ++w) s += red[w][j][k];
@@ -1318,7 +1344,8 @@ struct Op {
     j.in = static_cast<const float*>(d.in);
     j.ld = d.ld;
     j.width = d.width;
-    j.vec = d.f_i == 1 && d.width % 4 == 0 && d.ld % 4 == 0 && (((uintptr_t)d.in | (uintptr_t)F) & 15) == 0;
+    const uintptr_t both = (uintptr_t)d.in | (uintptr_t)F;
+    j.vec = d.width % 4 == 0 && d.ld % 4 == 0 && both % 16 == 0 ? 4 : d.width % 2 == 0 && d.ld % 2 == 0 && both % 8 == 0 ? 2 : 1;
     j.F = reinterpret_cast<const float*>(F);
     j.f_g = (int64_t)p.rank * d.width;
     j.f_j = d.f_j;
@@ -1372,14 +1399,13 @@ struct Op {
       const Shrinking& d = jobs[k];
       j.rows = mma::tensor_map(d.rows, 128);
       j.f_mn = d.f_mn;
-      const int cols = d.f_mn ? rb : rn;  // of D
+      j.cols = d.f_mn ? rb : rn;
       j.factor = mma::tensor_map(d.factor, d.f_mn ? 64 : rn);
-      j.f_bytes = cols * 128;
-      j.per = std::min(8, 32768 / j.f_bytes);
-      const mma::Seg g = mma::segment(d.rows.cols, mma::idesc(128, cols, true, false, d.f_mn));
+      j.f_bytes = j.cols * 128;
+      j.per = std::min(8, 256 / j.cols);
+      const mma::Seg g = mma::segment(d.rows.cols, 0);
       j.chunks = g.chunks;
       j.last = g.last;
-      j.idesc = g.idesc;
       j.u = l.u[d.i];
       j.planes = l.up[d.i];
       chunks = std::min(chunks, j.chunks);
@@ -1394,10 +1420,10 @@ struct Op {
     a.rn = rn;
     a.errors = mma::error_counter();
     const int64_t tiles = ceil_div(p.tokens, 128);
-    // the width split until the device is filled, four stages or more a CTA
+    // the width split until the device is filled, two stages or more a CTA
     int splits = 1;
-    while (splits < 4 && tiles * n * splits * 2 <= mma::num_sms() && chunks >= 8 * splits) splits *= 2;
-    const int smem = 1024 + kShrinkStages * kShrinkStage + 128;
+    while (splits < (rn <= 64 ? 4 : 2) && tiles * n * splits * 2 <= mma::num_sms() && chunks >= 4 * splits) splits *= 2;
+    const int smem = 1024 + kShrinkStages * kShrinkStage + 128 * 128 * 4 + 128;
     allow_smem(reinterpret_cast<const void*>(k_shrink), smem);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1419,12 +1445,13 @@ struct Op {
   // out = rows . W + low-rank: M tokens, N d.out, K d.width. F: the low-rank
   // factor as the tensor cores read it, or null
   // (FP32: as FP32 planes with every adapter's side by side).
+  template <bool EARLY>
   void product(const Side& d, const Tensor& rows, const Tensor& w, bool w_mn, int i, const Tensor* F, bool f_mn,
-               AdaptEpi<T> e) {
+               AdaptEpi<T, EARLY> e) {
     mma::Args a = {};
     const int64_t tiles = ceil_div(p.tokens, 256) * ceil_div(d.out, 256);
     // CTA pairs where their tiles fill half the device; else single CTAs, the tile narrowed until they do
-    const bool pair = tiles >= mma::num_sms() / 4;
+    const bool pair = !EARLY && tiles >= mma::num_sms() / 4;
     const int step = w_mn ? (pair ? 128 : 64) : 32;
     a.bn = (int)std::min<int64_t>(pair ? 256 : 128, round_up(d.out, step));
     if (!pair)
@@ -1440,6 +1467,7 @@ struct Op {
     const uint32_t id = mma::idesc(tm, a.bn, !f32, false, w_mn);
     a.seg = mma::segment(d.width, id);
     a.a_planes = a.b_planes = 1;
+    a.low_after = e.u && !F;
     mma::Maps maps;
     maps.a = mma::tensor_map(rows, a.a_rows);
     maps.b = mma::tensor_map(w, w_mn ? 64 : a.bn / (pair ? 2 : 1));
@@ -1467,14 +1495,19 @@ struct Op {
                     : mma::tensor_map(Tensor{l.up[i], l.ld_r, p.tokens, 2, l.ld_r, p.tokens * l.ld_r}, a.a_rows);
       maps.lb = mma::tensor_map(*F, f_mn ? 64 : a.bn / (pair ? 2 : 1));
     }
-    if (pair)
-      mma::launch<2, f32 ? 2 : 1>(maps, a, e, s);
-    else
-      mma::launch<1, f32 ? 2 : 1>(maps, a, e, s);
+    if constexpr (EARLY) {
+      mma::launch<1, 1>(maps, a, e, s);
+    } else {
+      if (pair)
+        mma::launch<2, f32 ? 2 : 1>(maps, a, e, s);
+      else
+        mma::launch<1, f32 ? 2 : 1>(maps, a, e, s);
+    }
   }
 
-  AdaptEpi<T> epilogue(T* y, int64_t ldy, int cols) {
-    AdaptEpi<T> e = {};
+  template <bool EARLY = false>
+  AdaptEpi<T, EARLY> epilogue(T* y, int64_t ldy, int cols) {
+    AdaptEpi<T, EARLY> e = {};
     e.y = y;
     e.ldy = ldy;
     e.rows = p.tokens;
@@ -1483,7 +1516,8 @@ struct Op {
     return e;
   }
   // the low-rank product in the epilogue: F of cols x r (by_col) or r x cols
-  void epilogue_low(AdaptEpi<T>& e, int i, const T* F, bool by_col, bool always) {
+  template <bool EARLY>
+  void epilogue_low(AdaptEpi<T, EARLY>& e, int i, const T* F, bool by_col) {
     if (!p.adapters) return;
     constexpr int N = 16 / sizeof(T);
     e.u = l.u[i];
@@ -1494,7 +1528,6 @@ struct Op {
     e.f_col = by_col ? p.rank : 1;
     e.f_j = by_col ? 1 : e.cols;
     e.f_vec = (by_col ? p.rank : e.cols) % N == 0 && ((uintptr_t)F & 15) == 0;
-    e.always = always;
   }
 
   void forward(const float* bias, T* y, int64_t ldy) {
@@ -1508,10 +1541,10 @@ struct Op {
                    (int)p.d, A, vec, (int)p.adapters, (int)p.rank, p.adapter, p.scales, l.u[0]);
         LC_LAUNCH_CHECK("k_shrink_few");
       }
-      if (tma) {
-        AdaptEpi<T> e = epilogue(y, ldy, p.classes);
+      if (!f32 && tma) {
+        AdaptEpi<T, true> e = epilogue<true>(y, ldy, p.classes);
         e.bias = bias;
-        epilogue_low(e, 0, B, true, true);
+        epilogue_low(e, 0, B, true);
         product(d, rows_of(d, 0), head(), false, 0, nullptr, false, e);
       } else {
         launch_pdl(k_rows<T>, dim3((unsigned)ceil_div(p.classes, 16), (unsigned)ceil_div(p.tokens, 8)), 128, s, x,
@@ -1523,7 +1556,7 @@ struct Op {
     }
     AdaptEpi<T> e = epilogue(y, ldy, p.classes);
     e.bias = bias;
-    epilogue_low(e, 0, B, true, f32);
+    epilogue_low(e, 0, B, true);
     if constexpr (f32) {
       RowJob jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, 60);
       if (l.dense) {
@@ -1559,7 +1592,7 @@ struct Op {
     const bool low = p.adapters > 0, want_v = low && (dx || dA), want_u = low && dB;
     if (!dx && !(low && (dA || dB))) return;
     AdaptEpi<T> e = epilogue(dx, lddx, p.d);
-    if (dx) epilogue_low(e, 1, A, false, f32);
+    if (dx) epilogue_low(e, 1, A, false);
     if constexpr (f32) {
       RowJob jw, ja, jy;
       if (dx) {

@@ -213,6 +213,7 @@ struct Args {
   int a_rows;  // rows of A's box (K-major): 128, or fewer where the tile has no more
   int a_mn, b_mn, lb_mn;
   int a_planes, b_planes;  // z from a plane to the next
+  int low_after;           // the epilogue adds the low-rank product of every tile
   int block;  // stages per block (DRAIN)
   Seg seg;
   Low low;
@@ -254,7 +255,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   // a stage: A's planes, then B's
-  const int b_bytes = a.bn / CG * 128, stage_bytes = PLANES * (kABytes + b_bytes);
+  // (A's rows past its box are whatever follows: their sums are not used)
+  const int a_bytes = a.a_rows * 128, b_bytes = a.bn / CG * 128, stage_bytes = PLANES * (a_bytes + b_bytes);
   const int nst = a.stages;
   const uint32_t bars = base + nst * stage_bytes;
   const uint32_t full = bars, empty = bars + 8 * nst, acc_full = empty + 8 * nst, acc_empty = acc_full + 16,
@@ -319,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t slot = st;
         if (++st == nst) st = 0, ph ^= 1u;
         if (lane != 0) return;
-        if (rank == 0) ptx::mbar_expect_tx(full + 8 * slot, (uint32_t)(CG * planes * (a.a_rows * 128 + b_bytes)));
+        if (rank == 0) ptx::mbar_expect_tx(full + 8 * slot, (uint32_t)(CG * planes * (a_bytes + b_bytes)));
         const uint32_t bar = lead_full + 8 * slot;
         auto box = [&](uint32_t dst, const CUtensorMap* m, int x, int y, int z) {
           if (CG == 2)
@@ -328,7 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             load_3d(dst, m, x, y, z, bar);
         };
         for (int p = 0; p < planes; ++p) {
-          const uint32_t sa = base + slot * stage_bytes + p * kABytes, sb = base + slot * stage_bytes + PLANES * kABytes + p * b_bytes;
+          const uint32_t sa = base + slot * stage_bytes + p * a_bytes, sb = base + slot * stage_bytes + PLANES * a_bytes + p * b_bytes;
           const int za = az + p * a.a_planes, zb = bz + p * a.b_planes;
           if (a_mn) {
             box(sa, pa, row, ak, za);
@@ -400,11 +402,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (!ok) return;
           ptx::tc_fence_after();
           if (lead) {
-            const uint32_t sa = base + st * stage_bytes, sb = sa + PLANES * kABytes;
+            const uint32_t sa = base + st * stage_bytes, sb = sa + PLANES * a_bytes;
             const uint64_t ia = a_mn ? 2048 >> 4 : 32 >> 4, ib = b_mn ? 2048 >> 4 : 32 >> 4;
             // lo hi, hi lo, hi hi
             for (int pr = planes == 2 ? 0 : 2; pr < 3; ++pr) {
-              uint64_t da = desc(sa + (pr == 0 ? kABytes : 0), a_mn), db = desc(sb + (pr == 1 ? b_bytes : 0), b_mn);
+              uint64_t da = desc(sa + (pr == 0 ? a_bytes : 0), a_mn), db = desc(sb + (pr == 1 ? b_bytes : 0), b_mn);
               for (int k = 0; k < steps; ++k, da += ia, db += ib) {
                 if (off) {
                   const uint32_t o[8] = {off[0], off[1], off[2], off[3], off[4], off[5], off[6], off[7]};
@@ -474,12 +476,17 @@ __global__ void __launch_bounds__(kThreads, 1)
       int mt, nt, z;
       tile_at(a, t, mt, nt, z);
       const int row = mt * TM + (int)rank * 128 + quarter * 32;
-      bool many = false;
+      bool many = a.low_after;
       if (a.low.G && !a.low.dense) {
         Groups<TM> gr;
         gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
         many = gr.more_than(kFewAdapters);
       }
+      // narrow tiles: the low-rank product while the MMAs run
+      float ahead[32];
+      bool have = false;
+      if constexpr (Epi::kEarly)
+        if (a.bn <= 64 && half * 32 < a.bn) have = epi.ahead(row, nt * a.bn + half * 32, lane, ahead);
       uint32_t src = 0;
       auto open = [&]() {
         ok = ptx::mbar_wait(acc_full + 8 * (n & 1), (uint32_t)((n >> 1) & 1), abort_s, kWaitLimit);
@@ -536,7 +543,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t v[32];
           ptx::tmem_ld32(src + c, v);
           ptx::tmem_wait_ld();
-          epi.store(row, nt * a.bn + c, z, lane, many, mine, v);
+          if constexpr (Epi::kEarly)
+            if (have) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ahead[j]);
+            }
+          epi.store(row, nt * a.bn + c, z, lane, many && !have, mine, v);
         }
         close();
       }
@@ -585,11 +597,13 @@ inline Seg segment(int64_t k, uint32_t id) {
 
 template <int CG, int PLANES, typename Epi>
 void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
-  const int stage = PLANES * (kABytes + a.bn / CG * 128);
+  const int stage = PLANES * (a.a_rows + a.bn / CG) * 128;
   a.errors = error_counter();
   const int turn = Epi::kTurns ? kEpiWarps * kTurnBytes + 128 : 0;
-  a.stages = std::min(8, (kSmem - 1024 - 512 - turn) / stage);
-  const int smem = 1024 + a.stages * stage + 512 + turn;
+  // (the MMAs read 128 rows of A's last stage)
+  const int past = std::max(0, kABytes - stage);
+  a.stages = std::min(16, (kSmem - 1024 - 640 - turn - past) / stage);
+  const int smem = 1024 + a.stages * stage + 640 + turn + past;
   allow_smem(reinterpret_cast<const void*>(k_mma<CG, PLANES, Epi>), kSmem);
   const int64_t per = a.sym ? (int64_t)a.m_tiles * (a.m_tiles + 1) / 2 : (int64_t)a.m_tiles * a.n_tiles;
   const int64_t tiles = per * a.batches;

@@ -248,7 +248,7 @@ __device__ __forceinline__ void add_planes(const __half* d, int64_t plane, int l
 // S (of = null) or P = c S S + b S, both triangles.
 template <int PLANES>
 struct SymEpi {
-  static constexpr bool kTurns = false;
+  static constexpr bool kTurns = false, kEarly = false;
   __half* d;
   const __half* of;
   int64_t ld, mat, plane;  // row, matrix and plane strides
@@ -274,7 +274,7 @@ struct SymEpi {
 // X' = a X + P X.
 template <int PLANES>
 struct UpdateEpi {
-  static constexpr bool kTurns = false;
+  static constexpr bool kTurns = false, kEarly = false;
   __half* d;
   const __half* x;
   int64_t ld, mat, plane;
@@ -297,7 +297,7 @@ struct UpdateEpi {
 // The last step: the result, or the weights' update, in the caller's type.
 template <int PLANES, typename T>
 struct LastEpi {
-  static constexpr bool kTurns = false;
+  static constexpr bool kTurns = false, kEarly = false;
   T* d;
   const T* w;  // null: the result itself
   const __half* x;
