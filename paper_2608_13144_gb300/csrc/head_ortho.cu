@@ -369,8 +369,9 @@ float poly_scale(float b, float c) {
 constexpr int kCluster = 4;
 constexpr int kTile = 128, kTileBytes = 128 * 128;
 // What a warp of the epilogue has to itself: others' parts of its 32 rows (three
-// of 32 + 4 columns, or one of 64 + 4), then what it sends to memory.
-constexpr int kPartBytes = 14 * 1024;
+// of 32 columns, or one of 64; four columns of the rows side by side), then what
+// it sends to memory.
+constexpr int kPartBytes = 12 * 1024;
 
 struct IterateArgs {
   CUtensorMap xk[2], xm[2], s, p;  // X's two buffers K-major and MN-major (boxes of 128 and 64 rows)
@@ -760,10 +761,10 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
                 ptx::tmem_wait_ld();
                 const int slot = rank < owner ? rank : rank - 1;
                 const uint32_t dst = ptx::mapa(region + quarter * kPartBytes, owner) +
-                                     (uint32_t)(((slot * 32 + lane) * (slice + 4) + first - owner * slice) * 4);
+                                     (uint32_t)(slot * slice * 128 + (first - owner * slice) * 128 + lane * 16);
 #pragma unroll
                 for (int j = 0; j < 32; j += 4)
-                  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + j * 4), "r"(v[j]),
+                  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + j * 128), "r"(v[j]),
                                "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3])
                                : "memory");
               }
@@ -806,14 +807,14 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
                   for (int j = 0; j < 32; ++j) s[j] += v[p][j];
                   continue;
                 }
-                const uint32_t o = own + (uint32_t)((((part < rank ? part : part - 1) * 32 + lane) * (slice + 4) + first -
-                                                     owner * slice) * 4);
+                const uint32_t o = own + (uint32_t)((part < rank ? part : part - 1) * slice * 128 +
+                                                    (first - owner * slice) * 128 + lane * 16);
 #pragma unroll
                 for (int j = 0; j < 32; j += 4) {
                   float e[4];
                   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
                                : "=f"(e[0]), "=f"(e[1]), "=f"(e[2]), "=f"(e[3])
-                               : "r"(o + j * 4)
+                               : "r"(o + j * 128)
                                : "memory");
 #pragma unroll
                   for (int q = 0; q < 4; ++q) s[j + q] += e[q];

@@ -50,11 +50,56 @@ __device__ __forceinline__ void dot16(const float* x, int stride, int ti, int tj
   }
 }
 
+// X <- a X + P X in the slice: columns in passes, ROWS rows x four columns a
+// thread.
+template <int ROWS>
+__device__ __forceinline__ void update(float* x, const float* p, int mp, int ss, int stride, int groups, float ca) {
+  const int rg = mp / ROWS, per = kThreads / rg;  // groups of rows; groups of columns a pass
+  const int r = threadIdx.x % rg, q0 = threadIdx.x / rg;
+  for (int c0 = 0; c0 < groups; c0 += per) {
+    const int c = c0 + q0;
+    const bool live = q0 < per && c < groups;
+    float4 acc[ROWS];
+    if (live) {
+      const float* xc = x + 4 * c;
+      const float* pr = p + ROWS * r;
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q) {
+        const float4 v = *reinterpret_cast<const float4*>(xc + (ROWS * r + q) * stride);
+        acc[q] = make_float4(ca * v.x, ca * v.y, ca * v.z, ca * v.w);
+      }
+#pragma unroll 4
+      for (int k = 0; k < mp; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(xc + k * stride);
+        float pk[ROWS];
+#pragma unroll
+        for (int q = 0; q < ROWS; q += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(pr + k * ss + q);
+          pk[q] = f.x, pk[q + 1] = f.y, pk[q + 2] = f.z, pk[q + 3] = f.w;
+        }
+#pragma unroll
+        for (int q = 0; q < ROWS; ++q) {
+          acc[q].x = fmaf(pk[q], v.x, acc[q].x);
+          acc[q].y = fmaf(pk[q], v.y, acc[q].y);
+          acc[q].z = fmaf(pk[q], v.z, acc[q].z);
+          acc[q].w = fmaf(pk[q], v.w, acc[q].w);
+        }
+      }
+    }
+    __syncthreads();  // the pass's columns have been read
+    if (live) {
+#pragma unroll
+      for (int q = 0; q < ROWS; ++q) *reinterpret_cast<float4*>(x + (ROWS * r + q) * stride + 4 * c) = acc[q];
+    }
+  }
+}
+
 template <typename T, typename TO>
 __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const SmallArgs a) {
   extern __shared__ float4 smem4[];
   __shared__ double norm_s;
   __shared__ double red[kThreads / 32];
+  __shared__ float factor_s[2];
   float* smem = reinterpret_cast<float*>(smem4);
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -120,13 +165,18 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
     norm_s = sum;
   }
   cluster.sync();
-  sum = 0.0;
-  for (int r = 0; r < ctas; ++r) sum += *cluster.map_shared_rank(&norm_s, r);
-  const double norm = sqrt(sum);
-  int e2 = 0;
-  frexp(norm > 0.0 ? norm : 1.0, &e2);
-  const bool fine = isfinite(norm) && e2 <= 126;
-  const float f1 = fine ? ldexpf(1.f, min(-e2, 126)) : NAN, f2 = fine ? (float)(ldexp(1.0, e2) / (norm + a.eps)) : NAN;
+  if (tid == 0) {  // (one thread: FP64 is slow)
+    sum = 0.0;
+    for (int r = 0; r < ctas; ++r) sum += *cluster.map_shared_rank(&norm_s, r);
+    const double norm = sqrt(sum);
+    int e2 = 0;
+    frexp(norm > 0.0 ? norm : 1.0, &e2);
+    const bool fine = isfinite(norm) && e2 <= 126;
+    factor_s[0] = fine ? ldexpf(1.f, min(-e2, 126)) : NAN;
+    factor_s[1] = fine ? (float)(ldexp(1.0, e2) / (norm + a.eps)) : NAN;
+  }
+  __syncthreads();
+  const float f1 = factor_s[0], f2 = factor_s[1];
   for (int e = tid; e < a.m * a.stride; e += kThreads) x[e] = x[e] * f1 * f2;
   __syncthreads();
 
@@ -145,6 +195,25 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
       while ((tj + 1) * (tj + 2) / 2 <= t) ++tj;
       const int ti = t - tj * (tj + 1) / 2;
       if (t < tiles) dot16(x, a.stride, ti, tj, nb, w & (ks - 1), ks, groups, acc);
+      if (ks >= 16) {
+        // 16 sums on 16 lanes: halve the values, double the lanes that share one
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) {
+          const bool up = w & o;
+#pragma unroll
+          for (int q = 0; q < o; ++q) {
+            const float keep = up ? acc[q + o] : acc[q], give = up ? acc[q] : acc[q + o];
+            acc[q] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+          }
+        }
+        if (ks == 32) acc[0] += __shfl_xor_sync(0xffffffffu, acc[0], 16);
+        if (t < tiles && (w & (ks - 1)) < 16) {
+          const int q = w & 15, i = ti + nb * (q >> 2), j = tj + nb * (q & 3);
+          mine[i * ss + j] = acc[0];
+          mine[j * ss + i] = acc[0];
+        }
+        continue;
+      }
       for (int o = ks / 2; o > 0; o >>= 1) {
 #pragma unroll
         for (int q = 0; q < 16; ++q) acc[q] += __shfl_xor_sync(0xffffffffu, acc[q], o);
@@ -171,6 +240,18 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
     }
     const float* sm = ctas > 1 ? s : mine;
     // P = b S + c S S (S is symmetric: rows against rows)
+    if (mp <= 32) {  // an element a thread: too few tiles for them
+      for (int e = tid; e < mp * mp; e += kThreads) {
+        const int i = e / mp, j = e - i * mp;
+        float acc = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < mp; k += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(sm + i * ss + k), v = *reinterpret_cast<const float4*>(sm + j * ss + k);
+          acc = fmaf(u.x, v.x, fmaf(u.y, v.y, fmaf(u.z, v.z, fmaf(u.w, v.w, acc))));
+        }
+        p[i * ss + j] = fmaf(cc, acc, cb * sm[i * ss + j]);
+      }
+    } else
     for (int w = tid; w < tiles; w += kThreads) {
       float acc[16] = {};
       int tj = 0;
@@ -186,40 +267,11 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
       }
     }
     __syncthreads();
-    // X <- a X + P X: columns in passes, eight rows x four columns a thread
-    const int rg = mp / 8, per = kThreads / rg;  // groups of rows; groups of columns a pass
-    for (int c0 = 0; c0 < groups; c0 += per) {
-      const int r = tid % rg, c = c0 + tid / rg;
-      const bool live = tid / rg < per && c < groups;
-      float4 acc[8];
-      if (live) {
-        const float* xc = x + 4 * c;
-        const float* pr = p + 8 * r;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const float4 v = *reinterpret_cast<const float4*>(xc + (8 * r + q) * a.stride);
-          acc[q] = make_float4(ca * v.x, ca * v.y, ca * v.z, ca * v.w);
-        }
-#pragma unroll 4
-        for (int k = 0; k < mp; ++k) {
-          const float4 v = *reinterpret_cast<const float4*>(xc + k * a.stride);
-          const float4 p0 = *reinterpret_cast<const float4*>(pr + k * ss), p1 = *reinterpret_cast<const float4*>(pr + k * ss + 4);
-          const float pk[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            acc[q].x = fmaf(pk[q], v.x, acc[q].x);
-            acc[q].y = fmaf(pk[q], v.y, acc[q].y);
-            acc[q].z = fmaf(pk[q], v.z, acc[q].z);
-            acc[q].w = fmaf(pk[q], v.w, acc[q].w);
-          }
-        }
-      }
-      __syncthreads();  // the pass's columns have been read
-      if (live) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) *reinterpret_cast<float4*>(x + (8 * r + q) * a.stride + 4 * c) = acc[q];
-      }
-    }
+    // X <- a X + P X: four rows a thread where eight leave threads idle
+    if (mp / 8 * groups < kThreads)
+      update<4>(x, p, mp, ss, a.stride, groups, ca);
+    else
+      update<8>(x, p, mp, ss, a.stride, groups, ca);
     __syncthreads();
   }
   for (int e0 = tid; e0 < len * lines; e0 += kThreads * kBatch) {
