@@ -454,7 +454,7 @@ __device__ __forceinline__ bool last_of_eight(uint32_t* count) {
 template <int PLANES, typename TO>
 __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_constant__ IterateArgs a) {
   constexpr int kStageBytes = 2 * PLANES * kTileBytes, kStages = PLANES == 2 ? 2 : 5;
-  constexpr int kSendBytes = 4096 * PLANES;  // a block of 32 x 32 and its mirror image, in planes
+  constexpr int kSendBytes = 6144 * PLANES;  // two blocks of 32 x 32 and a mirror image, in planes
   constexpr int kRegionBytes = 4 * kPartBytes > 8 * kSendBytes ? 4 * kPartBytes : 8 * kSendBytes;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -855,18 +855,22 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
           __syncwarp();  // the warp has read its parts
           if (mine && w.kind < 3) {
             const bool mirror = k < 2 && r != c;
+            bool busy = false;
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
               const int first = half * 64 + p * 32;
               if (split && first / slice != rank) continue;
               uint32_t hl[2][16];
               split_f16(v[p], hl[0], hl[1]);
-              // the block before has left
-              if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-              __syncwarp();
+              // what stood there has left: the tile before, or the mirror image before
+              if (!busy || (mirror && p == 1)) {
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();
+                busy = true;
+              }
 #pragma unroll
               for (int l = 0; l < PLANES; ++l) {
-                const uint32_t at = own + l * 2048 + lane * 64;
+                const uint32_t at = own + (p * PLANES + l) * 2048 + lane * 64;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((q ^ ((lane >> 1) & 3)) << 4)),
@@ -874,7 +878,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
                                : "memory");
                 if (mirror) {
                   // lanes in pairs: the even one writes its and its neighbour's column 2 q, the odd one 2 q + 1
-                  const uint32_t to_m = own + (PLANES + l) * 2048 + ((lane & 7) >> 1) * 4;
+                  const uint32_t to_m = own + (2 * PLANES + l) * 2048 + ((lane & 7) >> 1) * 4;
 #pragma unroll
                   for (int q = 0; q < 16; ++q) {
                     const uint32_t other = __shfl_xor_sync(0xffffffffu, hl[l][q], 1);
@@ -890,8 +894,8 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
               if (lane == 0) {
                 const int x = col + p * 32, y = r * kTile + quarter * 32;
                 for (int l = 0; l < PLANES; ++l) {
-                  if (x < cols && y < rows) mma::store_3d(to, x, y, l * a.batch + z, own + l * 2048);
-                  if (mirror && x < cols && y < rows) mma::store_3d(to, y, x, l * a.batch + z, own + (PLANES + l) * 2048);
+                  if (x < cols && y < rows) mma::store_3d(to, x, y, l * a.batch + z, own + (p * PLANES + l) * 2048);
+                  if (mirror && x < cols && y < rows) mma::store_3d(to, y, x, l * a.batch + z, own + (2 * PLANES + l) * 2048);
                 }
                 asm volatile("cp.async.bulk.commit_group;" ::: "memory");
               }
@@ -915,10 +919,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
         // written, and readable by copies of other CTAs; the last warp says so
         asm volatile("fence.proxy.async.global;" ::: "memory");
         __syncwarp();
-        if (lane == 0) {
-          __threadfence();
-          if (last_of_eight(counts + 1)) add_release(a.phases);
-        }
+        if (lane == 0 && last_of_eight(counts + 1)) add_release(a.phases);
       }
   }
   __syncthreads();
