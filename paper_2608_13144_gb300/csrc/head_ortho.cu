@@ -355,7 +355,7 @@ float poly_scale(float b, float c) {
 // ---------------------------------------------------------------- one launch
 // Matrices whose tiles do not fill the device several times over: all steps in
 // one cooperative launch, their products (phases) parted by a barrier over the
-// grid. 128 x 128 tiles, one CTA each; a stage holds 64 of the contracted
+// grid. Tiles of 128 x 128, or x 64 where those leave CTAs idle, one CTA each; a stage holds 64 of the contracted
 // index of every plane of both operands, so that the three products of FP32
 // planes read each once. Where a phase has few tiles, a cluster of `split`
 // CTAs shares one: each sums a part of the contracted index, and the parts
@@ -374,10 +374,10 @@ constexpr int kTile = 128, kTileBytes = 128 * 128;
 constexpr int kPartBytes = 12 * 1024;
 
 struct IterateArgs {
-  CUtensorMap xk[2], xm[2], s, p;  // X's two buffers K-major and MN-major (boxes of 128 and 64 rows)
+  CUtensorMap xk[2], xm[2], s, p, s64, p64;  // X's two buffers, S and P with boxes of 128 rows, and of 64
   CUtensorMap to[4];               // X's buffers, S and P to write to (boxes of 32 x 32)
   int tall, batch, m, n, steps;
-  int split[3];                    // of S, P and X' phases
+  int split[3], bn[3];             // of S, P and X' phases; bn: columns of a tile, 128 or (unsplit) 64
   float coef[3 * LIPCACHE_MAX_NS_STEPS], ps[LIPCACHE_MAX_NS_STEPS];
   const float* t;
   void* out;
@@ -387,6 +387,9 @@ struct IterateArgs {
   unsigned* phases;
   unsigned long long* errors;
 };
+
+// Tiles on or above the diagonal of rt x ct ones that are `wide` to a square.
+__host__ __device__ inline int upper_tiles(int rt, int ct, int wide) { return rt * ct - wide * (rt * (rt - 1) / 2); }
 
 __device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
   unsigned v;
@@ -497,20 +500,21 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
   ptx::cluster_sync();
   ptx::wait_prerequisites();
   const uint32_t tmem = *tmem_slot;
-  const int mt = (a.m + kTile - 1) / kTile, ntl = (a.n + kTile - 1) / kTile;
-  const int rows_t = a.tall ? ntl : mt, cols_t = a.tall ? mt : ntl;  // tiles of X as it is stored
-  const int sym = mt * (mt + 1) / 2;
+  const int rows_x = a.tall ? a.n : a.m, cols_x = a.tall ? a.m : a.n;  // of X as it is stored
 
-  // The work of a phase, the same for every role: `f(first block of 128 rows,
-  // of columns, z, first chunk, chunks)` for each of this CTA's tiles.
+  // The work of a phase, the same for every role.
   struct Work {
-    int kind, split, tiles, chunks, workers, me;
+    int kind, split, bn, rt, ct, per, tiles, chunks, workers, me;
   };
   auto phase_of = [&](int i, int k) {
     Work w;
     w.kind = k == 2 ? (i == a.steps - 1 ? 3 : 2) : k;
     w.split = a.split[k];
-    w.tiles = (k == 2 ? rows_t * cols_t : sym) * a.batch;
+    w.bn = a.bn[k];
+    w.rt = ((k == 2 ? rows_x : a.m) + kTile - 1) / kTile;
+    w.ct = ((k == 2 ? cols_x : a.m) + w.bn - 1) / w.bn;
+    w.per = k == 2 ? w.rt * w.ct : upper_tiles(w.rt, w.ct, kTile / w.bn);
+    w.tiles = w.per * a.batch;
     w.chunks = ((k == 0 ? a.n : a.m) + 63) / 64;
     w.workers = w.split > 1 ? (int)gridDim.x / kCluster : (int)gridDim.x;
     w.me = w.split > 1 ? (int)blockIdx.x / kCluster : (int)blockIdx.x;
@@ -518,19 +522,17 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
   };
   // (a split of two uses half the cluster)
   auto tile = [&](const Work& w, int t, int& r, int& c, int& z) {
+    z = t / w.per;
+    t -= z * w.per;
     if (w.kind < 2) {
-      z = t / sym;
-      t -= z * sym;
-      c = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-      while (c * (c + 1) / 2 > t) --c;
-      while ((c + 1) * (c + 2) / 2 <= t) ++c;
-      r = t - c * (c + 1) / 2;
+      // on or above the diagonal, row by row
+      const int wide = kTile / w.bn;
+      r = 0;
+      while (t >= w.ct - r * wide) t -= w.ct - r * wide, ++r;
+      c = r * wide + t;
     } else {
-      const int per = rows_t * cols_t;
-      z = t / per;
-      t -= z * per;
-      r = t / cols_t;
-      c = t - r * cols_t;
+      r = t / w.ct;
+      c = t - r * w.ct;
     }
   };
   auto range = [&](const Work& w, int& c0, int& c1) {
@@ -558,7 +560,8 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
           asm volatile("fence.proxy.async.global;" ::: "memory");
           const bool amn = k == 0 && a.tall, bmn = amn || (k == 2 && !a.tall);
           const CUtensorMap* ma = k == 0 ? (a.tall ? &a.xm[kx] : &a.xk[kx]) : k == 1 ? &a.s : a.tall ? &a.xk[kx] : &a.p;
-          const CUtensorMap* mb = k == 0 ? ma : k == 1 ? &a.s : a.tall ? &a.p : &a.xm[kx];
+          const bool half = w.bn == 64;  // B K-major: a box of 64 rows
+          const CUtensorMap* mb = bmn ? &a.xm[kx] : k == 0 ? (half ? &a.xm[kx] : &a.xk[kx]) : k == 1 ? (half ? &a.s64 : &a.s) : half ? &a.p64 : &a.p;
           int c0, c1;
           range(w, c0, c1);
           for (int t = w.me; t < w.tiles && ok; t += w.workers) {
@@ -568,7 +571,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
               ok = ptx::mbar_wait(empty + 8 * st, ph ^ 1u, abort_s, mma::kWaitLimit);
               if (!ok) break;
               const uint32_t dst = base + st * kStageBytes, bar = full + 8 * st;
-              ptx::mbar_expect_tx(bar, (uint32_t)kStageBytes);
+              ptx::mbar_expect_tx(bar, (uint32_t)(PLANES * (kTileBytes + w.bn * 128)));
               for (int pl = 0; pl < PLANES; ++pl) {
                 const int zz = pl * a.batch + z;
                 const uint32_t da = dst + pl * kTileBytes, db = dst + (PLANES + pl) * kTileBytes;
@@ -579,10 +582,10 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
                   mma::load_3d(da, ma, q * 64, r * kTile, zz, bar);
                 }
                 if (bmn) {
-                  mma::load_3d(db, mb, c * kTile, q * 64, zz, bar);
-                  mma::load_3d(db + 8192, mb, c * kTile + 64, q * 64, zz, bar);
+                  mma::load_3d(db, mb, c * w.bn, q * 64, zz, bar);
+                  if (!half) mma::load_3d(db + 8192, mb, c * w.bn + 64, q * 64, zz, bar);
                 } else {
-                  mma::load_3d(db, mb, q * 64, c * kTile, zz, bar);
+                  mma::load_3d(db, mb, q * 64, c * w.bn, zz, bar);
                 }
               }
               if (++st == kStages) st = 0, ph ^= 1u;
@@ -593,11 +596,11 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
               if (!ok) break;
               const uint32_t dst = base + st * kStageBytes, bar = full + 8 * st;
               const CUtensorMap* mi = k == 1 ? &a.s : &a.xk[kx];
-              const int h0 = w.split == 1 ? 0 : w.split == 2 ? rank : rank >> 1, h1 = w.split == 1 ? 2 : h0 + 1;
+              const int h0 = w.split == 1 ? 0 : w.split == 2 ? rank : rank >> 1, h1 = w.split == 1 ? w.bn / 64 : h0 + 1;
               ptx::mbar_expect_tx(bar, (uint32_t)((h1 - h0) * PLANES * kTileBytes));
               for (int h = h0; h < h1; ++h)
                 for (int pl = 0; pl < PLANES; ++pl)
-                  mma::load_3d(dst + (h * PLANES + pl) * kTileBytes, mi, c * kTile + 64 * h, r * kTile, pl * a.batch + z, bar);
+                  mma::load_3d(dst + (h * PLANES + pl) * kTileBytes, mi, c * w.bn + 64 * h, r * kTile, pl * a.batch + z, bar);
               if (++st == kStages) st = 0, ph ^= 1u;
             }
           }
@@ -614,7 +617,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
       for (int k = 0; k < 3 && ok; ++k) {
         const Work w = phase_of(i, k);
         const bool amn = k == 0 && a.tall, bmn = amn || (k == 2 && !a.tall);
-        const uint32_t id = mma::idesc(128, 128, false, amn, bmn);
+        const uint32_t id = mma::idesc(128, w.bn, false, amn, bmn);
         int c0, c1;
         range(w, c0, c1);
         const int last_steps = ((k == 0 ? a.n : a.m) - (w.chunks - 1) * 64 + 15) / 16;
@@ -671,12 +674,11 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
     __syncwarp();
   } else {
     // ------------------------------------------------------------ epilogue
-    // A warp: 32 rows, 64 columns as two blocks of 32 x 32. Blocks go to memory
+    // A warp: 32 rows, half the columns as blocks of 32 x 32. Blocks go to memory
     // by way of shared memory and TMA, mirror images too: a store a row from
     // registers takes a cycle for every 16 bytes (128 x 128 FP32 tiles: 9,000
     // clocks of a phase).
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * 64, sums = lanes + 256, lows = lanes + 384;
     int n = 0, joins = 0, st = 0;
     uint32_t ph = 0;
     bool ok = true;
@@ -686,9 +688,10 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
         ok = ptx::mbar_wait_warp(go, (uint32_t)(3 * i + k) & 1u, abort_s, mma::kWaitLimit);
         const float ps = a.ps[i];
         const bool split = w.split > 1;
-        const int slice = 128 / w.split;
+        const int slice = w.bn / w.split, hw = w.bn / 2;  // hw: this warp's columns
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + half * hw, sums = lanes + 256, lows = lanes + 384;
         const int rows = k < 2 ? a.m : a.rows, cols = k < 2 ? a.m : a.cols;
-        const bool mine = !split || half * 64 / slice == rank || (half * 64 + 32) / slice == rank;
+        const bool mine = !split || half * hw / slice == rank || (half * hw + 32) / slice == rank;
         const uint32_t own = region + (split ? quarter * kPartBytes : (half * 4 + quarter) * kSendBytes);
         const CUtensorMap* to = k == 0 ? &a.to[2] : k == 1 ? &a.to[3] : &a.to[(i & 1) ^ 1];
         int c0, c1;
@@ -708,7 +711,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
             f = tn * last / ps;
             g = tn * last * a.coef[3 * i];
           }
-          const int row = r * kTile + quarter * 32 + lane, col = c * kTile + half * 64;
+          const int row = r * kTile + quarter * 32 + lane, col = c * w.bn + half * hw;
           // blocks of the sum meet in tensor memory
           uint32_t src = sums;
           const int blocks = c1 <= c0 ? 0 : PLANES == 2 ? (c1 - c0 + kBlock - 1) / kBlock : 1;
@@ -719,7 +722,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
             src = lanes + (uint32_t)(n & 1) * 128u;
             if (blocks == 1) break;
 #pragma unroll 1
-            for (int q = 0; q < 64; q += 8) {
+            for (int q = 0; q < hw; q += 8) {
               float v[8];
               mma::tmem_ld8(src + q, v);
               if (b > 0) {
@@ -747,7 +750,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
             if (blocks) {
 #pragma unroll 1
               for (int p = 0; p < 2; ++p) {
-                const int first = half * 64 + p * 32, owner = first / slice;
+                const int first = half * hw + p * 32, owner = first / slice;
                 if (owner == rank) continue;
                 uint32_t v[32];
                 ptx::tmem_ld32(src + p * 32, v);
@@ -774,7 +777,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
             ok = ptx::mbar_wait_warp<true>(got, (uint32_t)joins & 1u, abort_s, mma::kWaitLimit);
             if (!ok) break;
           }
-          const uint32_t in = base + st * kStageBytes + half * PLANES * kTileBytes + (quarter * 32 + lane) * 128;
+          const uint32_t in = base + st * kStageBytes + (quarter * 32 + lane) * 128;
           if (adds(w)) {
             ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, mma::kWaitLimit);
             if (!ok) break;
@@ -782,8 +785,8 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
           float v[2][32];
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
-            const int first = half * 64 + p * 32, owner = first / slice;
-            if (split && owner != rank) continue;
+            const int first = half * hw + p * 32, owner = first / slice;
+            if (p * 32 >= hw || (split && owner != rank)) continue;
             uint32_t bits[32];
             ptx::tmem_ld32(src + p * 32, bits);
             ptx::tmem_wait_ld();
@@ -833,7 +836,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
                   uint4 e;
                   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                                : "=r"(e.x), "=r"(e.y), "=r"(e.z), "=r"(e.w)
-                               : "r"(in + l * kTileBytes + (((p * 4 + q) ^ (lane & 7)) << 4))
+                               : "r"(in + ((first >> 6) * PLANES + l) * kTileBytes + ((((first & 63) / 8 + q) ^ (lane & 7)) << 4))
                                : "memory");
                   add_f16(e, g, &v[p][q * 8]);
                 }
@@ -854,12 +857,12 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
           }
           __syncwarp();  // the warp has read its parts
           if (mine && w.kind < 3) {
-            const bool mirror = k < 2 && r != c;
+            const bool mirror = k < 2 && r != c * w.bn / kTile;
             bool busy = false;
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-              const int first = half * 64 + p * 32;
-              if (split && first / slice != rank) continue;
+              const int first = half * hw + p * 32;
+              if (p * 32 >= hw || (split && first / slice != rank)) continue;
               uint32_t hl[2][16];
               split_f16(v[p], hl[0], hl[1]);
               // what stood there has left: the tile before, or the mirror image before
@@ -903,8 +906,8 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
           } else if (mine) {
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-              const int first = half * 64 + p * 32, left = cols - col - p * 32;
-              if ((split && first / slice != rank) || left <= 0 || row >= rows) continue;
+              const int first = half * hw + p * 32, left = cols - col - p * 32;
+              if (p * 32 >= hw || (split && first / slice != rank) || left <= 0 || row >= rows) continue;
               put_result<TO>(a, ((int64_t)z * a.rows + row) * a.cols + col + p * 32, left, v[p]);
             }
           }
@@ -976,6 +979,8 @@ void iterate_at_once(int batch, int rows, int cols, int steps, const double* co,
       P{l.p, m, m, (int64_t)PLANES * batch, l.sld, l.s_plane};
   a.s = mma::tensor_map(S, 128);
   a.p = mma::tensor_map(P, 128);
+  a.s64 = mma::tensor_map(S, 64);
+  a.p64 = mma::tensor_map(P, 64);
   a.to[2] = mma::tensor_map(S, 32, 32);
   a.to[3] = mma::tensor_map(P, 32, 32);
   a.tall = tall;
@@ -988,21 +993,31 @@ void iterate_at_once(int batch, int rows, int cols, int steps, const double* co,
   a.phases = l.phases;
   a.errors = mma::error_counter();
   const int ctas = iterate_ctas<PLANES, TO>();
-  // The split that ends first, in clocks: a stage's loads from L2 (64 bytes a
-  // clock and SM), the tile's epilogue, and the join (measured: 8,000 to 9,600
-  // for a tile's parts through the cluster, and the epilogue of a slice).
-  const int64_t mt = ceil_div(m, kTile), nt = ceil_div(n, kTile);
+  // The tile and split that end first, in clocks: a stage's loads from L2 (64
+  // bytes a clock and SM; two stages of planes in flight take no less for 64
+  // columns), the tile's epilogue, the join (measured, 2001 x 1003
+  // FP32: 8,000 to 9,600 with the epilogue of a slice).
   int64_t grid = 0;  // no more CTAs than have work: each takes part in every barrier
   for (int k = 0; k < 3; ++k) {
-    const int64_t tiles = (k == 2 ? mt * nt : mt * (mt + 1) / 2) * batch, chunks = ceil_div(k == 0 ? n : m, 64);
-    int64_t best = -1;
-    for (int sp_ = 1; sp_ <= kCluster; sp_ *= 2) {
-      if (sp_ > chunks) break;
-      const int64_t workers = sp_ > 1 ? ctas / kCluster : ctas;
-      const int64_t cost = ceil_div(tiles, workers) * (ceil_div(chunks, sp_) * 512 * PLANES + (sp_ > 1 ? 14000 : 2000 + 1500 * PLANES));
-      if (best < 0 || cost < best) best = cost, a.split[k] = sp_;
+    const int64_t chunks = ceil_div(k == 0 ? n : m, 64);
+    int64_t best = -1, most = 0;
+    for (int c = 0; c < 4; ++c) {
+      const int bn = c == 0 ? 64 : 128, sp = c == 3 ? 4 : c == 2 ? 2 : 1;
+      if (sp > chunks) continue;
+      const int rt = (int)ceil_div(k == 2 ? rows : m, kTile), ct = (int)ceil_div(k == 2 ? cols : m, bn);
+      const int64_t tiles = (k == 2 ? (int64_t)rt * ct : upper_tiles(rt, ct, kTile / bn)) * (int64_t)batch;
+      const int64_t workers = sp > 1 ? ctas / kCluster : ctas;
+      const int stage = PLANES == 2 ? 1024 : 2 * (kTile + bn);
+      const int64_t cost = ceil_div(tiles, workers) * (ceil_div(chunks, sp) * stage +
+                                                       (sp > 1 ? 12000 : 2000 + 12 * PLANES * bn));
+      if (best < 0 || cost < best) {
+        best = cost;
+        a.split[k] = sp;
+        a.bn[k] = bn;
+        most = tiles * (sp > 1 ? kCluster : 1);
+      }
     }
-    grid = std::max(grid, tiles * (a.split[k] > 1 ? kCluster : 1));
+    grid = std::max(grid, most);
   }
   grid = std::min<int64_t>(round_up(grid, kCluster), ctas);
   a.t = l.t;
