@@ -24,6 +24,7 @@ namespace lc {
 namespace ops {
 namespace {
 
+constexpr int kBigTile = 256;  // rows and columns of a tile of a CTA pair
 constexpr int kParts = 512;      // partial sums of squares of a matrix, at most
 constexpr float kXScale = 8192.f, kSScale = 1024.f;
 constexpr int kBlock = 4;  // stages of 64 summed on the tensor cores at a time, FP32 matrices
@@ -252,7 +253,7 @@ struct SymEpi {
   __half* d;
   const __half* of;
   int64_t ld, mat, plane;  // row, matrix and plane strides
-  int m, tile;
+  int m;
   float f, b;
   const float* t;  // nullable: squared into f
   __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32]) const {
@@ -266,7 +267,7 @@ struct SymEpi {
     const int64_t at = z * mat + row * ld + col0;
     if (row >= m) return;
     if (of) add_planes<PLANES>(of + at, plane, left, b, v);
-    const bool off_diagonal = row0 / tile != col0 / tile;
+    const bool off_diagonal = row0 / kBigTile != col0 / kBigTile;
     put_planes<PLANES>(d + at, plane, off_diagonal ? d + z * mat + col0 * ld + row : nullptr, ld, left, v);
   }
 };
@@ -1045,6 +1046,7 @@ void iterate_at_once(int batch, int rows, int cols, int steps, const double* co,
   LC_LAUNCH_CHECK("k_iterate");
 }
 
+// Large matrices: tiles of 256 x 256 of CTA pairs.
 template <int PLANES, typename Epi>
 void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, int M, int N, int64_t K, int batch,
              bool sym, Epi epi, cudaStream_t s) {
@@ -1052,25 +1054,17 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
   a.batches = batch;
   a.a_mn = a_mn;
   a.b_mn = b_mn;
-  // 256 x 256 tiles of CTA pairs where they fill half the device, else 128 x 128 ones
-  const int64_t big = ceil_div(M, 256) * ceil_div(N, 256) * batch / (sym ? 2 : 1);
-  const bool pair = big >= mma::num_sms() / 4;
-  a.bn = pair ? 256 : 128;
-  const int tm = pair ? 256 : 128;
-  a.m_tiles = (int)ceil_div(M, tm);
-  a.n_tiles = (int)ceil_div(N, a.bn);
+  a.bn = kBigTile;
+  a.m_tiles = (int)ceil_div(M, kBigTile);
+  a.n_tiles = (int)ceil_div(N, kBigTile);
   a.sym = sym;
   a.block = kPairBlock;
   a.a_rows = 128;
-  const uint32_t id = mma::idesc(tm, a.bn, false, a_mn, b_mn);
-  a.seg = mma::segment(K, id);
+  a.seg = mma::segment(K, mma::idesc(kBigTile, kBigTile, false, a_mn, b_mn));
   a.a_planes = a.b_planes = batch;
   const CUtensorMap ma = mma::tensor_map(A, a_mn ? 64 : 128);
-  const CUtensorMap mb = mma::tensor_map(B, b_mn ? 64 : pair ? 128 : a.bn);
-  if (pair)
-    mma::launch<2, PLANES>({ma, mb, ma, mb}, a, epi, s);
-  else
-    mma::launch<1, PLANES>({ma, mb, ma, mb}, a, epi, s);
+  const CUtensorMap mb = mma::tensor_map(B, b_mn ? 64 : 128);
+  mma::launch<2, PLANES>({ma, mb, ma, mb}, a, epi, s);
 }
 
 template <typename T, int VEC, int PLANES>
@@ -1105,22 +1099,21 @@ void iterate(int batch, int rows, int cols, int steps, const double* co, void* o
   const bool tall = rows > cols;
   const int m = std::min(rows, cols), n = std::max(rows, cols);
   const int64_t xp = (int64_t)batch * l.x_plane, sp = (int64_t)batch * l.s_plane;
-  if (ceil_div(m, 256) * ceil_div(m, 256) * batch / 2 < mma::num_sms() / 4) {
+  if (ceil_div(m, kBigTile) * ceil_div(m, kBigTile) * batch / 2 < mma::num_sms() / 4) {
     iterate_at_once<PLANES, TO>(batch, rows, cols, steps, co, out, st, l, s);
     return;
   }
   const mma::Tensor S{l.s, m, m, (int64_t)PLANES * batch, l.sld, l.s_plane};
   const mma::Tensor P{l.p, m, m, (int64_t)PLANES * batch, l.sld, l.s_plane};
-  const int tile = ceil_div(m, 256) * ceil_div(m, 256) * batch / 2 >= mma::num_sms() / 4 ? 256 : 128;
   for (int i = 0; i < steps; ++i) {
     const float a = (float)co[3 * i], b = (float)co[3 * i + 1], c = (float)co[3 * i + 2];
     const float* t = i == 0 ? l.t : nullptr;
     __half *x = l.x[i & 1], *y = l.x[(i & 1) ^ 1];
     const mma::Tensor X{x, cols, rows, (int64_t)PLANES * batch, l.ld, l.x_plane};
-    SymEpi<PLANES> gram{l.s, nullptr, l.sld, l.s_plane, sp, m, tile, kSScale / (kXScale * kXScale), 0.f, t};
+    SymEpi<PLANES> gram{l.s, nullptr, l.sld, l.s_plane, sp, m, kSScale / (kXScale * kXScale), 0.f, t};
     product<PLANES>(X, tall, X, tall, m, m, n, batch, true, gram, s);
     const float ps = poly_scale(b, c);
-    SymEpi<PLANES> poly{l.p, l.s, l.sld, l.s_plane, sp, m, tile, c * ps / (kSScale * kSScale), b * ps / kSScale, nullptr};
+    SymEpi<PLANES> poly{l.p, l.s, l.sld, l.s_plane, sp, m, c * ps / (kSScale * kSScale), b * ps / kSScale, nullptr};
     product<PLANES>(S, false, S, false, m, m, m, batch, true, poly, s);
     auto update = [&](auto epi) {
       if (tall)
