@@ -697,16 +697,19 @@ struct AdaptEpi {
   const int* odd;
   int n_odd;
 
-  __device__ __forceinline__ void odd_values(int64_t p, int col0, int left, int lane, float (&v)[32]) const {
+  __device__ __forceinline__ bool any_odd(int col0, int left, int lane) const {
     bool flag = false;
     if (n_odd == 0)
       flag = lane < left && __ldg(odd + col0 + lane);
     else
       for (int i = lane; i < n_odd; i += 32) flag |= __ldg(odd + i) != 0;
-    if (!__any_sync(0xffffffffu, flag) || p >= rows) return;
+    return __any_sync(0xffffffffu, flag);
+  }
+  __device__ __forceinline__ void odd_values(int64_t p, int col0, int left, float (&v)[32]) const {
     const int g = __ldg(adapter + p);
     if (g < 0 || g >= G) return;
     const T* f = F + (int64_t)g * cols * r + col0 * f_col;
+#pragma unroll 1
     for (int k = 0; k < r; ++k) {
       const float uk = __ldg(u + p * r + k);
 #pragma unroll 1
@@ -784,6 +787,46 @@ struct AdaptEpi {
     }
   }
 
+  // x += the low-rank product of row p in the N columns from col on, `left` of
+  // them in the matrix.
+  template <int N>
+  __device__ __forceinline__ void low_part(int64_t p, int col, int left, float (&x)[N]) const {
+    const int g = __ldg(adapter + p);
+    if (g < 0 || g >= G) return;
+    const T* f = F + (int64_t)g * cols * r + col * f_col;
+    const float* up = u + p * r;
+    if (f_vec && f_j == 1 && N > 1) {
+#pragma unroll 1
+      for (int k = 0; k < r; k += N) {
+        float uk[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) uk[i] = __ldg(up + k + i);
+        uint4 q[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[i] = __ldg(reinterpret_cast<const uint4*>(f + min(i, left - 1) * r + k));
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+          for (int j = 0; j < N; ++j) x[i] = fmaf(uk[j], part(q[i], j), x[i]);
+      }
+    } else if (f_vec && N > 1) {
+#pragma unroll 4
+      for (int k = 0; k < r; ++k) {
+        const float uk = __ldg(up + k);
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(f + k * f_j));  // (rows are whole vectors)
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(uk, part(q, i), x[i]);
+      }
+    } else {
+#pragma unroll 4
+      for (int k = 0; k < r; ++k) {
+        const float uk = __ldg(up + k);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(uk, to_f32<T>(f[min(i, left - 1) * f_col + k * f_j]), x[i]);
+      }
+    }
+  }
+
   // The low-rank product of 32 columns before the shared one is there (unscaled
   // sums, every tile's: the few-rows form).
   __device__ __forceinline__ bool ahead(int row0, int col0, int lane, float (&v)[32]) const {
@@ -799,55 +842,72 @@ struct AdaptEpi {
     const int64_t p = (int64_t)row0 + lane;
     if (left <= 0) return;
     // what belongs to a column, a lane each
-    const float uc = undo_col && lane < left ? __ldg(undo_col + col0 + lane) : 1.f;
-    const float bc = bias && lane < left ? __ldg(bias + col0 + lane) : 0.f;
+    float uc = undo_col && lane < left ? __ldg(undo_col + col0 + lane) : 1.f;
+    float bc = bias && lane < left ? __ldg(bias + col0 + lane) : 0.f;
     const float f = undo_row && p < rows ? __ldg(undo_row + p) : 1.f;
+    const bool strange = odd && any_odd(col0, left, lane), after = many && u && !odd;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(acc[j]) * f;
-    if (undo_col) {
+    if (strange) {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] *= __shfl_sync(0xffffffffu, uc, j);
+      uc = 1.f;
+      if (p < rows) odd_values(p, col0, left, v);
     }
-    if (bias) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, bc, j);
-    }
-    if (odd) odd_values(p, col0, left, lane, v);
-    if (many && p < rows && u && !odd) low(p, col0, left, v);
-    // Turned in shared memory: a row from a thread would take a cycle for every
-    // 16 bytes, or for every element where rows are not whole vectors.
-    constexpr int kWords = 8 * sizeof(T), kStride = kWords + 1;  // 32-bit words of a row
-    uint32_t w[kWords];
-    round_to<T>(v, w);
+    // Turned in shared memory, 16 bytes at a time, places mixed by the row: a row
+    // from a thread would take a cycle for every 16 bytes, or for every element
+    // where rows are not whole vectors. Scales (powers of two) and biases of the
+    // columns come after, a few shuffles instead of 64, and so does the low-rank
+    // product of mixed rows, whose factors the lanes of a row then read side by side.
     __syncwarp();
 #pragma unroll
-    for (int q = 0; q < kWords; ++q)
-      asm volatile("st.shared.b32 [%0], %1;" ::"r"(turn + (uint32_t)((lane * kStride + q) * 4)), "r"(w[q]) : "memory");
+    for (int q = 0; q < 8; ++q)
+      asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (uint32_t)(lane * 128 + ((q ^ (lane & 7)) << 4))),
+                   "f"(v[4 * q]), "f"(v[4 * q + 1]), "f"(v[4 * q + 2]), "f"(v[4 * q + 3])
+                   : "memory");
     __syncwarp();
-    auto word = [&](int row, int q) {
-      uint32_t x;
-      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(turn + (uint32_t)((row * kStride + q) * 4)) : "memory");
-      return x;
-    };
     const int have = (int)min((int64_t)32, rows - row0);
-    if (vec && left >= 32) {
-      constexpr int kLanes = kWords / 4;  // lanes a row
+    constexpr int N = 16 / sizeof(T), kLanes = 32 / N;  // columns of a lane, lanes of a row
+    if (vec && (left >= 32 || left % N == 0)) {
+      const int first = lane / kLanes, q = lane % kLanes;
+      float cu[N], cb[N];
 #pragma unroll
-      for (int r0 = 0; r0 < 32; r0 += 32 / kLanes) {
-        const int r = r0 + lane / kLanes, q = lane % kLanes * 4;
-        if (r < have)
-          *reinterpret_cast<uint4*>(y + ((int64_t)row0 + r) * ldy + col0 + q * (4 / sizeof(T))) =
-              uint4{word(r, q), word(r, q + 1), word(r, q + 2), word(r, q + 3)};
+      for (int i = 0; i < N; ++i) {
+        cu[i] = __shfl_sync(0xffffffffu, uc, q * N + i);
+        cb[i] = __shfl_sync(0xffffffffu, bc, q * N + i);
+      }
+      T* o = y + ((int64_t)row0 + first) * ldy + col0 + q * N;
+      const bool inside = q * N < left;
+#pragma unroll
+      for (int r0 = 0; r0 < 32; r0 += N) {
+        const int r = r0 + first;
+        float x[N];
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(x[i]), "=f"(x[i + 1]), "=f"(x[i + 2]), "=f"(x[i + 3])
+                       : "r"(turn + (uint32_t)(r * 128 + (((q * N + i) / 4 ^ (r & 7)) << 4)))
+                       : "memory");
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaf(x[i], cu[i], cb[i]);
+        if (after && inside && r < have) low_part<N>((int64_t)row0 + r, col0 + q * N, left - q * N, x);
+        round_to<T>(x, w);
+        if (inside && r < have) *reinterpret_cast<uint4*>(o + r0 * ldy) = uint4{w[0], w[1], w[2], w[3]};
       }
     } else if (lane < left) {
       T* o = y + (int64_t)row0 * ldy + col0 + lane;
 #pragma unroll 8
       for (int r = 0; r < have; ++r) {
-        if constexpr (sizeof(T) == 4)
-          o[r * ldy] = __uint_as_float(word(r, lane));
-        else
-          reinterpret_cast<uint16_t*>(o)[r * ldy] = (uint16_t)(word(r, lane / 2) >> (lane & 1) * 16);
+        float x;
+        asm volatile("ld.shared.f32 %0, [%1];"
+                     : "=f"(x)
+                     : "r"(turn + (uint32_t)(r * 128 + ((lane >> 2 ^ (r & 7)) << 4) + (lane & 3) * 4))
+                     : "memory");
+        float z[1] = {fmaf(x, uc, bc)};
+        if (after) low_part<1>((int64_t)row0 + r, col0 + lane, 1, z);
+        o[r * ldy] = from_f32<T>(z[0]);
       }
     }
   }

@@ -39,7 +39,7 @@ namespace mma {
 constexpr int kChunk = 64;           // contracted elements of a stage
 constexpr int kABytes = 128 * 128;   // 128 rows x 64 elements
 constexpr int kEpiWarps = 8;
-constexpr int kTurnBytes = 32 * 33 * 4;  // a warp's block of 32 x 32, turned for coalesced writes
+constexpr int kTurnBytes = 32 * 32 * 4;  // a warp's block of 32 x 32, turned for coalesced writes
 constexpr int kThreads = 32 * (2 + kEpiWarps);
 constexpr long long kWaitLimit = 1LL << 31;  // ~1 s at GB300 clocks
 constexpr int kSmem = 227 * 1024;
@@ -505,14 +505,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         ++n;
       };
-      if (DRAIN) {
+      if (DRAIN && chunks > a.block) {
         constexpr int kParts = CG == 2 ? 4 : 2;  // bn <= 128 CG
         float sum[kParts][32];
 #pragma unroll
         for (int i = 0; i < kParts; ++i)
 #pragma unroll
           for (int j = 0; j < 32; ++j) sum[i][j] = 0.f;
-        for (int c0 = 0; c0 < max(chunks, 1); c0 += a.block) {
+        for (int c0 = 0; c0 < chunks; c0 += a.block) {
           open();
           if (!ok) break;
 #pragma unroll
@@ -539,6 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       } else {
         open();
         if (!ok) break;
+#pragma unroll 1
         for (int c = half * 32; c < a.bn; c += 64) {
           uint32_t v[32];
           ptx::tmem_ld32(src + c, v);
