@@ -102,9 +102,9 @@ def load(path: str = LIB_PATH):
         "lipcache_size": ([vp], i64),
         "lipcache_destroy": ([vp], None),
         "lipcache_last_error": ([], C.c_char_p),
-        "lipcache_adapted_workspace": ([C.POINTER(Adapted), i32], i64),
-        "lipcache_adapted_logits": ([C.POINTER(Adapted), vp, vp, i64, vp, i64, vp], C.c_int),
-        "lipcache_adapted_logits_backward": ([C.POINTER(Adapted), vp, i64, vp, i64, vp, vp, vp, i64, vp], C.c_int),
+        "lipcache_adapted_workspace": ([vp, i32], i64),
+        "lipcache_adapted_logits": ([vp, vp, vp, i64, vp, i64, vp], C.c_int),
+        "lipcache_adapted_logits_backward": ([vp, vp, i64, vp, i64, vp, vp, vp, i64, vp], C.c_int),
         "lipcache_cross_entropy": ([i32, vp, i64, i64, i32, vp, vp, vp, vp, i64, vp], C.c_int),
         "lipcache_orthogonalize_workspace": ([i32, i64, i32, i32], i64),
         "lipcache_orthogonalize": ([i32, vp, i64, i64, i32, i32, i32, vp, f64, vp, vp, i64, vp], C.c_int),

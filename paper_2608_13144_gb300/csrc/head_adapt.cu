@@ -290,6 +290,7 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
   __shared__ __align__(16) int id[kLowTile];
   __shared__ int order[kLowTile], starts[kLowTile + 1], sums[8];
   __shared__ float parts[8][32];
+  __shared__ __align__(16) bf16 own[3][kLowTile][8];
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   const LowJob& job = a.job[blockIdx.z];
@@ -381,24 +382,35 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
     const float s = any && a.scales ? __ldg(a.scales + g) : 1.f;
     const float v = any ? s * acc[0] : 0.f;
     if (k < count && j < nj) job.u[t * R + j0 + j] = v;
-    if (job.wide) {
-      // the first of the blocks along j clears the rows' other places
-      if (blockIdx.y == 0) {
-        const int words = (int)(a.ldw / 8);
-        for (int e = lane; e < count * 3 * words; e += 32) {
-          const int row = e / (3 * words), rest = e - row * 3 * words, q3 = rest / words, w8 = rest - q3 * words;
-          // a word of eight columns may hold some of the adapter's own: left to those
-          bf16* o = job.wide + (t0 + order[first + row]) * a.ldw + q3 * a.tokens * a.ldw + w8 * 8;
-          const int c0 = w8 * 8, own0 = any ? g * R : 0, own1 = any ? own0 + R : 0;
-          if (c0 + 8 <= own0 || c0 >= own1)
-            *reinterpret_cast<uint4*>(o) = uint4{0, 0, 0, 0};
-          else
-            for (int c = 0; c < 8; ++c)
-              if (c0 + c < own0 || c0 + c >= own1) o[c] = __float2bfloat16_rn(0.f);
+    // over a power of two
+    if (job.wide && any && k < count) put3(own[0][order[first + k]] + j, kLowTile * 8, j < nj ? v / __ldg(job.undo + t) : 0.f);
+  }
+  if (!job.wide) return;
+  __syncthreads();
+  // the rows set side by side: 16 bytes of a plane a lane
+  const int words = (int)(a.ldw / 8);
+  for (int row = warp; row < n; row += 8) {
+    const int g = id[row], low = g < a.G ? g * R : -R;  // the adapter's columns
+    bf16* o = job.wide + (t0 + row) * a.ldw;
+    for (int e = lane; e < 3 * words; e += 32) {
+      const int p = (e >= words) + (e >= 2 * words), w = e - p * words;
+      const bf16* from = own[p][row];
+      bf16* to = o + p * a.tokens * a.ldw + w * 8;
+      const int at = low + j0 - w * 8;  // of this block's columns in the word
+      if (w * 8 + 8 <= low || w * 8 >= low + R) {
+        if (blockIdx.y == 0) *reinterpret_cast<uint4*>(to) = uint4{0, 0, 0, 0};
+      } else if (at == 0 && nj == 8) {
+        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+      } else {
+        // the first of the blocks along j clears what is no block's
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          if (c >= at && c < at + nj)
+            to[c] = from[c - at];
+          else if (blockIdx.y == 0 && (w * 8 + c < low || w * 8 + c >= low + R))
+            to[c] = __float2bfloat16_rn(0.f);
         }
       }
-      if (any && k < count && j < nj)
-        put3(job.wide + t * a.ldw + g * R + j0 + j, a.tokens * a.ldw, v / __ldg(job.undo + t));  // a power of two
     }
   }
 }
@@ -697,13 +709,26 @@ struct AdaptEpi {
   const int* odd;
   int n_odd;
 
-  __device__ __forceinline__ bool any_odd(int col0, int left, int lane) const {
-    bool flag = false;
-    if (n_odd == 0)
-      flag = lane < left && __ldg(odd + col0 + lane);
-    else
-      for (int i = lane; i < n_odd; i += 32) flag |= __ldg(odd + i) != 0;
-    return __any_sync(0xffffffffu, flag);
+  // Of a row, and of a lane's columns in each of up to four blocks of 32, 64 apart.
+  struct Head {
+    float f, uc[4], bc[4];
+    bool odd;
+  };
+  __device__ __forceinline__ void load(int row0, int col0, int wide, int lane, Head& h) const {
+    const int64_t p = (int64_t)row0 + lane;
+    h.f = undo_row && p < rows ? __ldg(undo_row + p) : 1.f;
+    h.odd = false;
+    if (odd && n_odd)
+      for (int i = lane; i < n_odd; i += 32) h.odd |= __ldg(odd + i) != 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = col0 + 64 * i + lane;
+      const bool in = 64 * i < wide && c < cols;
+      h.uc[i] = undo_col && in ? __ldg(undo_col + c) : 1.f;
+      h.bc[i] = bias && in ? __ldg(bias + c) : 0.f;
+      if (odd && !n_odd && in) h.odd |= __ldg(odd + c) != 0;
+    }
+    h.odd = __any_sync(0xffffffffu, h.odd);
   }
   __device__ __forceinline__ void odd_values(int64_t p, int col0, int left, float (&v)[32]) const {
     const int g = __ldg(adapter + p);
@@ -837,15 +862,16 @@ struct AdaptEpi {
     return true;
   }
   __device__ __forceinline__ void store(int row0, int col0, int, int lane, bool many, uint32_t turn,
-                                        const uint32_t (&acc)[32]) const {
+                                        const uint32_t (&acc)[32], const Head& h, int block) const {
     const int left = cols - col0;
     const int64_t p = (int64_t)row0 + lane;
     if (left <= 0) return;
-    // what belongs to a column, a lane each
-    float uc = undo_col && lane < left ? __ldg(undo_col + col0 + lane) : 1.f;
-    float bc = bias && lane < left ? __ldg(bias + col0 + lane) : 0.f;
-    const float f = undo_row && p < rows ? __ldg(undo_row + p) : 1.f;
-    const bool strange = odd && any_odd(col0, left, lane), after = many && u && !odd;
+    const float f = h.f;
+    float uc = h.uc[0], bc = h.bc[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+      if (block == i) uc = h.uc[i], bc = h.bc[i];
+    const bool strange = h.odd, after = many && u && !odd;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(acc[j]) * f;

@@ -487,6 +487,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool have = false;
       if constexpr (Epi::kEarly)
         if (a.bn <= 64 && half * 32 < a.bn) have = epi.ahead(row, nt * a.bn + half * 32, lane, ahead);
+      // what the epilogue reads of the tile's rows and columns, before its sums are there
+      typename Epi::Head head;
+      epi.load(row, nt * a.bn + half * 32, a.bn - half * 32, lane, head);
       uint32_t src = 0;
       auto open = [&]() {
         ok = ptx::mbar_wait(acc_full + 8 * (n & 1), (uint32_t)((n >> 1) & 1), abort_s, kWaitLimit);
@@ -534,13 +537,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           uint32_t v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[i][j]);
-          epi.store(row, nt * a.bn + c, z, lane, many, mine, v);
+          epi.store(row, nt * a.bn + c, z, lane, many, mine, v, head, i);
         }
       } else {
         open();
         if (!ok) break;
 #pragma unroll 1
-        for (int c = half * 32; c < a.bn; c += 64) {
+        for (int i = 0, c = half * 32; c < a.bn; c += 64, ++i) {
           uint32_t v[32];
           ptx::tmem_ld32(src + c, v);
           ptx::tmem_wait_ld();
@@ -549,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + ahead[j]);
             }
-          epi.store(row, nt * a.bn + c, z, lane, many && !have, mine, v);
+          epi.store(row, nt * a.bn + c, z, lane, many && !have, mine, v, head, i);
         }
         close();
       }

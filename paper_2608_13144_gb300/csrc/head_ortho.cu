@@ -246,17 +246,21 @@ __device__ __forceinline__ void add_planes(const __half* d, int64_t plane, int l
   }
 }
 
+struct Nothing {};
+
 // S (of = null) or P = c S S + b S, both triangles.
 template <int PLANES>
 struct SymEpi {
   static constexpr bool kTurns = false, kEarly = false;
+  using Head = Nothing;
+  __device__ __forceinline__ void load(int, int, int, int, Nothing&) const {}
   __half* d;
   const __half* of;
   int64_t ld, mat, plane;  // row, matrix and plane strides
   int m;
   float f, b;
   const float* t;  // nullable: squared into f
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32], const Nothing&, int) const {
     const int row = row0 + lane, left = m - col0;
     if (left <= 0) return;
     float g = f;
@@ -276,13 +280,15 @@ struct SymEpi {
 template <int PLANES>
 struct UpdateEpi {
   static constexpr bool kTurns = false, kEarly = false;
+  using Head = Nothing;
+  __device__ __forceinline__ void load(int, int, int, int, Nothing&) const {}
   __half* d;
   const __half* x;
   int64_t ld, mat, plane;
   int rows, cols;
   float f, a;
   const float* t;
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32], const Nothing&, int) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
     const float u = t ? __ldcg(t + z) : 1.f, g = f * u;
@@ -299,6 +305,8 @@ struct UpdateEpi {
 template <int PLANES, typename T>
 struct LastEpi {
   static constexpr bool kTurns = false, kEarly = false;
+  using Head = Nothing;
+  __device__ __forceinline__ void load(int, int, int, int, Nothing&) const {}
   T* d;
   const T* w;  // null: the result itself
   const __half* x;
@@ -306,7 +314,7 @@ struct LastEpi {
   int rows, cols, vec;
   float f, a, keep, rate;
   const float* t;
-  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32]) const {
+  __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32], const Nothing&, int) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
     const float u = t ? __ldcg(t + z) : 1.f, g = f * u;

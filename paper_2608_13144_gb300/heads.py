@@ -16,6 +16,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import struct
 
 import torch
 
@@ -27,9 +28,21 @@ TYPES = {torch.float32: _lib.F32, torch.bfloat16: _lib.BF16}
 #: about 1 (0.7 to 1.2) within five steps.
 QUINTIC = (3.4445, -4.7750, 2.0315)
 
+I32, F32 = torch.int32, torch.float32
+#: struct lipcache_adapted, packed: half the time of filling ctypes' Adapted
+_ADAPTED = struct.Struct("@6i9q")
+assert _ADAPTED.size == C.sizeof(Adapted)
 
-def _stream(device: torch.device):
-    return torch.cuda.current_stream(device).cuda_stream
+
+def _call(at: int, fn, *args) -> None:
+    """fn on the current stream of GPU `at`, made current only where another one is."""
+    if torch._C._cuda_getDevice() == at:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(at))
+    else:
+        with torch.cuda.device(at):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(at))
+    if status:
+        check(status)
 
 
 def _type(t: torch.Tensor, name: str) -> int:
@@ -39,48 +52,31 @@ def _type(t: torch.Tensor, name: str) -> int:
         raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}") from None
 
 
-def _check(t: torch.Tensor, name: str, dims: int, device: torch.device, dtype: torch.dtype) -> None:
-    if t.dtype == dtype and t.dim() == dims and t.device == device:
+def _check(t: torch.Tensor, name: str, dims: int, at: int, dtype: torch.dtype) -> None:
+    if t.dtype == dtype and t.get_device() == at and t.dim() == dims:
         return
-    if t.device != device:
+    if t.get_device() != at:
         raise ValueError(f"{name} must be on one GPU with the other tensors, not on {t.device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     raise ValueError(f"{name} must have {dims} dimensions, not {t.dim()}")
 
 
-def _gpu(t: torch.Tensor, name: str) -> torch.device:
+def _gpu(t: torch.Tensor, name: str) -> int:
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU, not on {t.device}")
-    return t.device
+    return t.get_device()
 
 
-class _On:
-    """The device a call runs on, made current only where another one is."""
-
-    __slots__ = ("other",)
-
-    def __init__(self, device: torch.device):
-        self.other = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
-
-
-def _rows(t: torch.Tensor) -> torch.Tensor:
-    """`t` (2-D) with neighbours in a row next to each other in memory and rows that do not overlap."""
-    if t.shape[1] <= 1 or t.shape[0] <= 1:
-        return t if t.is_contiguous() else t.contiguous()
-    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
-
-
-def _ld(t: torch.Tensor) -> int:
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+def _rows(t: torch.Tensor):
+    """`t` (2-D) with neighbours in a row next to each other in memory and rows
+    that do not overlap, and its row stride."""
+    n, width = t.shape
+    if t.is_contiguous():
+        return t, width
+    if n > 1 and width > 1 and t.stride(1) == 1 and t.stride(0) >= width:
+        return t, t.stride(0)
+    return t.contiguous(), width
 
 
 def _workspace(nbytes: int, device: torch.device) -> torch.Tensor:
@@ -100,26 +96,33 @@ def _ortho_bytes(ty: int, batch: int, m: int, n: int) -> int:
     return _lib.load().lipcache_orthogonalize_workspace(ty, batch, m, n)
 
 
-def _describe(x, W, A, B, adapter, scales):
-    """The operator's description, and the tensors it points into."""
-    ty, dev, dt = _type(x, "x"), _gpu(x, "x"), x.dtype
-    _check(x, "x", 2, dev, dt)
-    _check(W, "W", 2, dev, dt)
-    _check(A, "A", 3, dev, dt)
-    _check(B, "B", 3, dev, dt)
-    _check(adapter, "adapter", 1, dev, torch.int32)
-    (n, d), classes, (G, r, _) = x.shape, W.shape[0], A.shape
-    if W.shape[1] != d or tuple(A.shape) != (G, r, d) or tuple(B.shape) != (G, classes, r) or adapter.shape[0] != n:
+def _describe(x, W, A, B, adapter, scales, backward):
+    """The operator's description, its sizes, scratch and device, and the tensors it points into."""
+    dt, at = x.dtype, x.get_device()
+    if not (dt in TYPES and at >= 0 and x.dim() == 2 and W.dtype == dt and W.get_device() == at and W.dim() == 2
+            and A.dtype == dt and A.get_device() == at and A.dim() == 3 and B.dtype == dt and B.get_device() == at
+            and B.dim() == 3 and adapter.dtype == I32 and adapter.get_device() == at and adapter.dim() == 1):
+        _type(x, "x")
+        _gpu(x, "x")
+        for t, name, dims, dtype in ((x, "x", 2, dt), (W, "W", 2, dt), (A, "A", 3, dt), (B, "B", 3, dt),
+                                     (adapter, "adapter", 1, I32)):
+            _check(t, name, dims, at, dtype)
+    (n, d), (classes, wide), (G, r, da) = x.shape, W.shape, A.shape
+    if wide != d or da != d or B.shape != (G, classes, r) or len(adapter) != n:
         raise ValueError("x must be n x d, W C x d, A G x r x d, B G x C x r and adapter must have n entries")
     if scales is not None:
-        _check(scales, "scales", 1, dev, torch.float32)
-        if scales.shape[0] != G:
+        _check(scales, "scales", 1, at, F32)
+        if len(scales) != G:
             raise ValueError("scales must have an entry per adapter")
         scales = scales.contiguous()
-    x, W, A, B, adapter = _rows(x), _rows(W), A.contiguous(), B.contiguous(), adapter.contiguous()
-    p = Adapted(ty, d, classes, G, r, 0, n, x.data_ptr(), _ld(x), W.data_ptr(), _ld(W), A.data_ptr(), B.data_ptr(),
-                adapter.data_ptr(), scales.data_ptr() if scales is not None else None)
-    return p, (x, W, A, B, adapter, scales)
+    x, ldx = _rows(x)
+    W, ldw = _rows(W)
+    A, B, adapter = A.contiguous(), B.contiguous(), adapter.contiguous()
+    ty, device = TYPES[dt], x.device
+    p = _ADAPTED.pack(ty, d, classes, G, r, 0, n, x.data_ptr(), ldx, W.data_ptr(), ldw, A.data_ptr(), B.data_ptr(),
+                      adapter.data_ptr(), 0 if scales is None else scales.data_ptr())
+    ws = _workspace(_adapted_bytes(ty, d, classes, G, r, n, backward), device)
+    return p, n, d, classes, ws, at, device, (x, W, A, B, adapter, scales)
 
 
 def adapted_logits(x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor, adapter: torch.Tensor,
@@ -129,23 +132,21 @@ def adapted_logits(x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
 
     x: n x d; W: C x d; A: G x r x d; B: G x C x r; adapter: n (int32; a value
     outside [0, G) means no adapter); bias: C (float32); scales: G (float32)."""
-    p, keep = _describe(x, W, A, B, adapter, scales)
+    p, n, _, classes, ws, at, device, keep = _describe(x, W, A, B, adapter, scales, 0)
     if bias is not None:
-        _check(bias, "bias", 1, x.device, torch.float32)
-        if bias.shape[0] != p.classes:
+        _check(bias, "bias", 1, at, F32)
+        if len(bias) != classes:
             raise ValueError("bias must have C entries")
         bias = bias.contiguous()
     if out is None:
-        out = torch.empty(p.tokens, p.classes, dtype=x.dtype, device=x.device)
+        out, ldy = torch.empty(n, classes, dtype=x.dtype, device=device), classes
     else:
-        _check(out, "out", 2, x.device, x.dtype)
-        if tuple(out.shape) != (p.tokens, p.classes) or _rows(out) is not out:
+        _check(out, "out", 2, at, x.dtype)
+        rows, ldy = _rows(out)
+        if out.shape != (n, classes) or rows is not out:
             raise ValueError("out must be n x C with dense rows")
-    L = _lib.load()
-    ws = _workspace(_adapted_bytes(p.type, p.d, p.classes, p.adapters, p.rank, p.tokens, 0), x.device)
-    with _On(x.device):
-        check(L.lipcache_adapted_logits(C.byref(p), bias.data_ptr() if bias is not None else None, out.data_ptr(),
-                                        _ld(out), ws.data_ptr(), ws.numel(), _stream(x.device)))
+    _call(at, _lib.load().lipcache_adapted_logits, p, None if bias is None else bias.data_ptr(), out.data_ptr(), ldy,
+          ws.data_ptr(), ws.numel())
     return out
 
 
@@ -154,22 +155,17 @@ def adapted_logits_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, 
                             need_dA: bool = True, need_dB: bool = True):
     """(dx, dA, dB) of adapted_logits for the gradient dy (n x C) of its
     result; W and bias are held fixed. An output that is not needed is None."""
-    p, keep = _describe(x, W, A, B, adapter, scales)
-    _check(dy, "dy", 2, x.device, x.dtype)
-    if tuple(dy.shape) != (p.tokens, p.classes):
+    p, n, d, classes, ws, at, device, keep = _describe(x, W, A, B, adapter, scales, 1)
+    dt = x.dtype
+    _check(dy, "dy", 2, at, dt)
+    if dy.shape != (n, classes):
         raise ValueError("dy must be n x C")
-    dy = _rows(dy)
-    dx = torch.empty(p.tokens, p.d, dtype=x.dtype, device=x.device) if need_dx else None
-    dA = torch.empty(A.shape, dtype=x.dtype, device=x.device) if need_dA else None
-    dB = torch.empty(B.shape, dtype=x.dtype, device=x.device) if need_dB else None
-    L = _lib.load()
-    ws = _workspace(_adapted_bytes(p.type, p.d, p.classes, p.adapters, p.rank, p.tokens, 1), x.device)
-    with _On(x.device):
-        check(L.lipcache_adapted_logits_backward(C.byref(p), dy.data_ptr(), _ld(dy),
-                                                 dx.data_ptr() if need_dx else None, p.d,
-                                                 dA.data_ptr() if need_dA else None,
-                                                 dB.data_ptr() if need_dB else None, ws.data_ptr(), ws.numel(),
-                                                 _stream(x.device)))
+    dy, lddy = _rows(dy)
+    dx = torch.empty(n, d, dtype=dt, device=device) if need_dx else None
+    dA = torch.empty(A.shape, dtype=dt, device=device) if need_dA else None
+    dB = torch.empty(B.shape, dtype=dt, device=device) if need_dB else None
+    _call(at, _lib.load().lipcache_adapted_logits_backward, p, dy.data_ptr(), lddy, dx.data_ptr() if need_dx else None, d,
+          dA.data_ptr() if need_dA else None, dB.data_ptr() if need_dB else None, ws.data_ptr(), ws.numel())
     return dx, dA, dB
 
 
@@ -181,30 +177,28 @@ def cross_entropy(logits: torch.Tensor, target: torch.Tensor, weight: torch.Tens
 
     logits: n x C; target: n (int32; a value outside [0, C) ignores the row);
     weight: n (float32)."""
-    ty, dev = _type(logits, "logits"), _gpu(logits, "logits")
-    _check(logits, "logits", 2, dev, logits.dtype)
-    _check(target, "target", 1, dev, torch.int32)
+    ty, at, dt = _type(logits, "logits"), _gpu(logits, "logits"), logits.dtype
+    _check(logits, "logits", 2, at, dt)
+    _check(target, "target", 1, at, I32)
     n, c = logits.shape
-    if target.shape[0] != n:
+    if len(target) != n:
         raise ValueError("target must have an entry per row of logits")
     if weight is not None:
-        _check(weight, "weight", 1, dev, torch.float32)
-        if weight.shape[0] != n:
+        _check(weight, "weight", 1, at, F32)
+        if len(weight) != n:
             raise ValueError("weight must have an entry per row of logits")
         weight = weight.contiguous()
-    z = _rows(logits)
+    z, ldz = _rows(logits)
     if in_place and z is not logits:
         raise ValueError("in_place needs logits with dense rows")
     target = target.contiguous()
-    loss = torch.empty(n, dtype=torch.float32, device=z.device)
-    dz = None
+    device = z.device
+    loss = torch.empty(n, dtype=F32, device=device)
+    dz, ldd = None, c
     if need_grad:
-        dz = z if in_place else torch.empty(n, c, dtype=z.dtype, device=z.device)
-    with _On(dev):
-        check(_lib.load().lipcache_cross_entropy(ty, z.data_ptr(), _ld(z), n, c, target.data_ptr(),
-                                                 weight.data_ptr() if weight is not None else None, loss.data_ptr(),
-                                                 dz.data_ptr() if need_grad else None, _ld(dz) if need_grad else c,
-                                                 _stream(z.device)))
+        dz, ldd = (z, ldz) if in_place else (torch.empty(n, c, dtype=dt, device=device), c)
+    _call(at, _lib.load().lipcache_cross_entropy, ty, z.data_ptr(), ldz, n, c, target.data_ptr(),
+          None if weight is None else weight.data_ptr(), loss.data_ptr(), None if dz is None else dz.data_ptr(), ldd)
     return loss, dz
 
 
@@ -242,7 +236,7 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=QUINTIC, eps: fl
     eps), X <- aX + (bS + cSS)X with S = XX^T (on the smaller side).
     coefficients: (a, b, c), or a triple for each step."""
     ty = _type(G, "G")
-    dev = _gpu(G, "G")
+    at, device = _gpu(G, "G"), G.device
     batch, m, n = _matrices(G, "G")
     coef = _polynomials(coefficients, steps)
     # rows of any stride, as long as the matrices follow one another in it
@@ -251,16 +245,14 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=QUINTIC, eps: fl
         G = G.contiguous()
         ld = n
     if out is None:
-        out = torch.empty(G.shape, dtype=G.dtype, device=G.device)
+        out = torch.empty(G.shape, dtype=G.dtype, device=device)
     else:
-        _check(out, "out", G.dim(), dev, G.dtype)
+        _check(out, "out", G.dim(), at, G.dtype)
         if out.shape != G.shape or not out.is_contiguous():
             raise ValueError("out must have G's shape and be contiguous")
-    L = _lib.load()
-    ws = _workspace(_ortho_bytes(ty, batch, m, n), dev)
-    with _On(dev):
-        check(L.lipcache_orthogonalize(ty, G.data_ptr(), ld, batch, m, n, int(steps), coef, float(eps),
-                                       out.data_ptr(), ws.data_ptr(), ws.numel(), _stream(G.device)))
+    ws = _workspace(_ortho_bytes(ty, batch, m, n), device)
+    _call(at, _lib.load().lipcache_orthogonalize, ty, G.data_ptr(), ld, batch, m, n, int(steps), coef, float(eps),
+          out.data_ptr(), ws.data_ptr(), ws.numel())
     return out
 
 
@@ -275,24 +267,22 @@ def orthogonal_step(weight: torch.Tensor, grad: torch.Tensor, momentum: torch.Te
     weight_decay) weight - lr sqrt(max(1, rows / cols)) O. weight and grad:
     float32 or bfloat16; momentum: float32; all rows x cols, or batch x rows x
     cols, contiguous."""
-    wt, gt, dev = _type(weight, "weight"), _type(grad, "grad"), _gpu(weight, "weight")
+    wt, gt, at = _type(weight, "weight"), _type(grad, "grad"), _gpu(weight, "weight")
     batch, m, n = _matrices(weight, "weight")
     ow, om = (weight, momentum) if out is None else out
+    shape, dims = weight.shape, weight.dim()
     for t, name, dtype in ((weight, "weight", weight.dtype), (grad, "grad", grad.dtype),
-                           (momentum, "momentum", torch.float32), (ow, "out[0]", weight.dtype),
-                           (om, "out[1]", torch.float32)):
-        _check(t, name, weight.dim(), dev, dtype)
-        if t.shape != weight.shape or (name != "grad" and not t.is_contiguous()):
+                           (momentum, "momentum", F32), (ow, "out[0]", weight.dtype),
+                           (om, "out[1]", F32)):
+        _check(t, name, dims, at, dtype)
+        if t.shape != shape or not (t.is_contiguous() or t is grad):
             raise ValueError(f"{name} must have the weight's shape and be contiguous")
     grad = grad.contiguous()
     coef = _polynomials(coefficients, steps)
-    L = _lib.load()
-    ws = _workspace(_ortho_bytes(wt, batch, m, n), dev)
-    with _On(dev):
-        check(L.lipcache_orthogonal_step(wt, gt, weight.data_ptr(), grad.data_ptr(), momentum.data_ptr(),
-                                         ow.data_ptr(), om.data_ptr(), batch, m, n, float(lr), float(beta),
-                                         int(bool(nesterov)), float(weight_decay), int(steps), coef, float(eps),
-                                         ws.data_ptr(), ws.numel(), _stream(weight.device)))
+    ws = _workspace(_ortho_bytes(wt, batch, m, n), weight.device)
+    _call(at, _lib.load().lipcache_orthogonal_step, wt, gt, weight.data_ptr(), grad.data_ptr(), momentum.data_ptr(),
+          ow.data_ptr(), om.data_ptr(), batch, m, n, float(lr), float(beta), int(bool(nesterov)), float(weight_decay),
+          int(steps), coef, float(eps), ws.data_ptr(), ws.numel())
     return ow, om
 
 
@@ -301,5 +291,5 @@ def operator_errors(device: torch.device | int | None = None) -> int:
     was loaded (synchronises the current stream)."""
     n = C.c_int64()
     with torch.cuda.device(device):
-        check(_lib.load().lipcache_operator_errors(C.byref(n), _stream(torch.device("cuda", torch.cuda.current_device()))))
+        check(_lib.load().lipcache_operator_errors(C.byref(n), torch.cuda.current_stream().cuda_stream))
     return n.value
