@@ -940,16 +940,20 @@ struct AdaptEpi {
 };
 
 // A few rows on the CUDA cores (FP32, or BF16 that TMA cannot read): a warp
-// takes four rows of W against eight of x.
+// takes four rows of W against eight of x. u: the rows' low-rank products, or
+// null where a block works them out itself, kRowsDots of them at most: as many
+// rows of A as the block has of W, where a launch of its own costs the call 3 us.
+constexpr int kRowsDots = 16;
 template <typename T>
 __global__ void __launch_bounds__(128)
     k_rows(const T* x, int64_t ldx, int64_t tokens, const T* W, int64_t ldw, int classes, int d, const float* bias,
-           const float* u, const T* B, const int32_t* adapter, int G, int r, T* y, int64_t ldy) {
+           const float* u, const T* A, const float* scales, const T* B, const int32_t* adapter, int G, int r, T* y,
+           int64_t ldy) {
+  __shared__ float own[kRowsDots];
   ptx::launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const int c0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c0 = (blockIdx.x * 4 + warp) * 4;
   const int64_t t0 = (int64_t)blockIdx.y * 8;
-  if (c0 >= classes) return;
   const T *w[4], *xr[8];
 #pragma unroll
   for (int k = 0; k < 4; ++k) w[k] = W + (int64_t)min(c0 + k, classes - 1) * ldw;
@@ -980,6 +984,33 @@ __global__ void __launch_bounds__(128)
       acc[k] = keep + __shfl_xor_sync(0xffffffffu, give, s);
     }
   }
+  if (G && !u) {
+    // four of the rows' low-rank products a warp
+    const T *xd[4], *ad[4];
+    const int dots = (int)min((int64_t)8, tokens - t0) * r;
+    float dot[4], scale[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = min(warp * 4 + k, dots - 1), row = e / r;
+      const int g = __ldg(adapter + t0 + row);
+      const bool any = g >= 0 && g < G;
+      xd[k] = x + (t0 + row) * ldx;
+      ad[k] = A + ((int64_t)(any ? g : 0) * r + e - row * r) * d;
+      scale[k] = any && scales ? __ldg(scales + g) : 1.f;
+      dot[k] = 0.f;
+    }
+#pragma unroll 2
+    for (int i = lane; i < d; i += 32)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) dot[k] = fmaf(to_f32<T>(xd[k][i]), to_f32<T>(ad[k][i]), dot[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) dot[k] += __shfl_xor_sync(0xffffffffu, dot[k], o);
+      if (lane == 0 && warp * 4 + k < dots) own[warp * 4 + k] = scale[k] * dot[k];
+    }
+    __syncthreads();
+  }
   const int c = c0 + (lane >> 3);
   const int64_t t = t0 + (lane & 7);
   if (c >= classes || t >= tokens) return;
@@ -988,7 +1019,8 @@ __global__ void __launch_bounds__(128)
   const int g = G ? __ldg(adapter + t) : -1;
   if (g >= 0 && g < G) {
     const T* b = B + ((int64_t)g * classes + c) * r;
-    for (int k = 0; k < r; ++k) v = fmaf(__ldg(u + t * r + k), to_f32<T>(b[k]), v);
+    const float* ut = u ? u + t * r : own + (lane & 7) * r;
+    for (int k = 0; k < r; ++k) v = fmaf(ut[k], to_f32<T>(b[k]), v);
   }
   y[t * ldy + c] = from_f32<T>(v);
 }
@@ -1620,7 +1652,8 @@ struct Op {
     const Side d{x, p.ldx, p.d, p.classes, p.d, 1};
     const bool low = p.adapters > 0, tma = !f32 && mma::mappable(x, p.ldx) && mma::mappable(W, p.ldw);
     if (p.tokens <= (tma ? kFewBf16 : kFewF32)) {
-      if (low) {
+      const bool own = !tma && p.tokens * p.rank <= kRowsDots;
+      if (low && !own) {
         const int vec = ((uintptr_t)x & 15) == 0 && ((uintptr_t)A & 15) == 0 && p.ldx * sizeof(T) % 16 == 0 &&
                         p.d * sizeof(T) % 16 == 0;
         launch_pdl(k_shrink_few<T>, dim3((unsigned)p.tokens, (unsigned)ceil_div(p.rank, 8)), 128, s, x, p.ldx,
@@ -1634,8 +1667,8 @@ struct Op {
         product(d, rows_of(d, 0), head(), false, 0, nullptr, false, e);
       } else {
         launch_pdl(k_rows<T>, dim3((unsigned)ceil_div(p.classes, 16), (unsigned)ceil_div(p.tokens, 8)), 128, s, x,
-                   p.ldx, p.tokens, W, p.ldw, (int)p.classes, (int)p.d, bias, (const float*)l.u[0], B, p.adapter,
-                   (int)p.adapters, (int)p.rank, y, ldy);
+                   p.ldx, p.tokens, W, p.ldw, (int)p.classes, (int)p.d, bias, own ? (const float*)nullptr : (const float*)l.u[0],
+                   A, p.scales, B, p.adapter, (int)p.adapters, (int)p.rank, y, ldy);
         LC_LAUNCH_CHECK("k_rows");
       }
       return;
