@@ -286,9 +286,13 @@ __device__ __forceinline__ void low_dots(const LowJob& a, const float* const (&x
   }
 }
 
+// A group of rows of one adapter: its place in the order, rows, adapter.
+__device__ __forceinline__ uint32_t group_of(int first, int count, int g) { return (uint32_t)(first | count << 8 | g << 16); }
+
 __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJobs a) {
-  __shared__ __align__(16) int id[kLowTile];
-  __shared__ int order[kLowTile], starts[kLowTile + 1], sums[8];
+  __shared__ int bins[LIPCACHE_MAX_ADAPTERS + 1];
+  __shared__ int id[kLowTile], order[kLowTile], total;
+  __shared__ uint32_t group[kLowTile];
   __shared__ float parts[8][32];
   __shared__ __align__(16) bf16 own[3][kLowTile][8];
   ptx::wait_prerequisites();
@@ -298,49 +302,55 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
   const int64_t t0 = (int64_t)blockIdx.x * a.tile;
   const int n = (int)min((int64_t)a.tile, a.tokens - t0);
   const int j0 = blockIdx.y * 8, nj = min(8, R - j0);
-  int mine = a.G;  // rows without an adapter come last
+  // Rows by adapter, those without one last: counted, the counts summed up, each
+  // row put in its place. (Which rows of an adapter share a group is left to
+  // chance; no row's sums depend on it.)
+  int mine = a.G, place = 0;
   if (tid < n) {
     const int g = __ldg(a.adapter + t0 + tid);
     mine = g >= 0 && g < a.G ? g : a.G;
   }
-  if (tid < kLowTile) id[tid] = tid < n ? mine : 0x7fffffff;
+  for (int i = tid; i <= a.G; i += 256) bins[i] = 0;
   __syncthreads();
-  if (tid < n) {
-    int rank = 0;
-    for (int k = 0; k < n; k += 4) {
-      const int4 v = *reinterpret_cast<const int4*>(id + k);
-      rank += (v.x < mine || (v.x == mine && k < tid)) + (v.y < mine || (v.y == mine && k + 1 < tid)) +
-              (v.z < mine || (v.z == mine && k + 2 < tid)) + (v.w < mine || (v.w == mine && k + 3 < tid));
+  if (tid < n) place = atomicAdd(&bins[mine], 1);
+  __syncthreads();
+  if (warp == 0) {
+    int rows = 0, groups = 0;
+    for (int i0 = 0; i0 <= a.G; i0 += 32) {
+      const int c = i0 + lane <= a.G ? bins[i0 + lane] : 0;
+      int sum = c | (c + 3) / 4 << 16;
+      const int one = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += v;
+      }
+      const int before = sum - one;  // rows and groups before this adapter's
+      if (i0 + lane <= a.G) bins[i0 + lane] = rows + (before & 0xffff) | (groups + (before >> 16)) << 8 | c << 16;
+      const int all = __shfl_sync(0xffffffffu, sum, 31);
+      rows += all & 0xffff;
+      groups += all >> 16;
     }
-    order[rank] = tid;
+    if (lane == 0) total = groups;
   }
   __syncthreads();
-  // groups: up to four neighbours in that order with one adapter
-  bool start = false;
   if (tid < n) {
-    const int g = id[order[tid]];
-    int back = 0;
-    while (back < tid && id[order[tid - back - 1]] == g) ++back;
-    start = (back & 3) == 0;
+    const int b = bins[mine], at = (b & 255) + place;
+    id[tid] = mine;
+    order[at] = tid;
+    if ((place & 3) == 0) group[(b >> 8 & 255) + place / 4] = group_of(at, min(4, (b >> 16) - place), mine);
   }
-  const uint32_t m = __ballot_sync(0xffffffffu, start);
-  if (lane == 0) sums[warp] = __popc(m);
   __syncthreads();
-  int at = __popc(m & ((1u << lane) - 1u)), groups = 0;
-  for (int w = 0; w < 8; ++w) {
-    if (w < warp) at += sums[w];
-    groups += sums[w];
-  }
-  if (start) starts[at] = tid;
-  if (tid == 0) starts[groups] = n;
-  __syncthreads();
-  const int share = a.share, part = warp % share;
+  const int groups = total, share = a.share, part = warp % share;
   for (int q0 = 0; q0 < groups; q0 += 8 / share) {
     const int q = q0 + warp / share;
     const bool live = q < groups;
-    const int first = live ? starts[q] : 0, count = live ? starts[q + 1] - first : 0;
-    const int g = id[order[first]];
+    const uint32_t it = live ? group[q] : 0u;
+    const int first = it & 255, count = it >> 8 & 255, g = it >> 16;
     const bool any = live && g < a.G;
+    const int64_t t = t0 + order[first + min(lane >> 3, max(count - 1, 0))];  // this lane's row of the results
+    const float scale = any && a.scales ? __ldg(a.scales + g) : 1.f;
+    const float over = any && job.wide ? __ldg(job.undo + t) : 1.f;
     float acc[32];
 #pragma unroll
     for (int k = 0; k < 32; ++k) acc[k] = 0.f;
@@ -348,7 +358,7 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
       const int at = part * 32 + lane, step = share * 32;
       const float* x[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = job.in + (t0 + order[first + min(k, count - 1)]) * job.ld;
+      for (int k = 0; k < 4; ++k) x[k] = job.in + __shfl_sync(0xffffffffu, t, k * 8) * job.ld;
       const float* F = job.F + g * job.f_g + j0 * job.f_j;
       if (job.f_j == 1)
         low_dots<1, true>(job, x, F, nj, at, step, acc);
@@ -378,12 +388,10 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
     }
     if (!live) continue;
     const int k = lane >> 3, j = lane & 7;
-    const int64_t t = t0 + order[first + min(k, count - 1)];
-    const float s = any && a.scales ? __ldg(a.scales + g) : 1.f;
-    const float v = any ? s * acc[0] : 0.f;
+    const float v = any ? scale * acc[0] : 0.f;
     if (k < count && j < nj) job.u[t * R + j0 + j] = v;
     // over a power of two
-    if (job.wide && any && k < count) put3(own[0][order[first + k]] + j, kLowTile * 8, j < nj ? v / __ldg(job.undo + t) : 0.f);
+    if (job.wide && any && k < count) put3(own[0][t - t0] + j, kLowTile * 8, j < nj ? v / over : 0.f);
   }
   if (!job.wide) return;
   __syncthreads();
@@ -399,8 +407,18 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
       const int at = low + j0 - w * 8;  // of this block's columns in the word
       if (w * 8 + 8 <= low || w * 8 >= low + R) {
         if (blockIdx.y == 0) *reinterpret_cast<uint4*>(to) = uint4{0, 0, 0, 0};
-      } else if (at == 0 && nj == 8) {
-        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+      } else if (R <= 8 || (at == 0 && nj == 8)) {
+        // the row's own columns (zeros past them), moved to their place in the word
+        ulonglong2 v = *reinterpret_cast<const ulonglong2*>(from);
+        const int up = at * 16;
+        if (up > 0) {
+          v.y = up < 64 ? v.y << up | v.x >> (64 - up) : v.x << (up - 64);
+          v.x = up < 64 ? v.x << up : 0;
+        } else if (up < 0) {
+          v.x = up > -64 ? v.x >> -up | v.y << (64 + up) : v.y >> (-up - 64);
+          v.y = up > -64 ? v.y >> -up : 0;
+        }
+        *reinterpret_cast<ulonglong2*>(to) = v;
       } else {
         // the first of the blocks along j clears what is no block's
 #pragma unroll
@@ -1793,9 +1811,9 @@ struct Op {
         o.errors = mma::error_counter();
         const int smem = 1024 + kOuterStages * (16384 + o.rb * 256) + 2 * kWindow + 128;
         allow_smem(reinterpret_cast<const void*>(k_outer), 1024 + kOuterStages * (16384 + 128 * 256) + 2 * kWindow + 128);
-        // CTAs a tile: as long as an adapter has some four stages of rows for each, and a slot for its parts
+        // CTAs a tile: as long as an adapter has some eight stages of rows for each (four: 37 us for 30 at 4,096 rows of 8), and a slot for its parts
         unsigned splits = 1;
-        while (splits < (o.rb == 64 ? 4u : 2u) && p.tokens >= (int64_t)p.adapters * splits * 512) splits *= 2;
+        while (splits < (o.rb == 64 ? 4u : 2u) && p.tokens >= (int64_t)p.adapters * splits * 1024) splits *= 2;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[0].val.programmaticStreamSerializationAllowed = 1;
