@@ -126,8 +126,13 @@ __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int
       v[0] = __ldg(r + i);
     }
     if (a.fold) {
+      if constexpr (VEC == 4) {
+        const float4 q = __ldg(reinterpret_cast<const float4*>(a.fold + i));
+        v[0] *= q.x, v[1] *= q.y, v[2] *= q.z, v[3] *= q.w;
+      } else {
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) v[k] *= __ldg(a.fold + i + k);
+        for (int k = 0; k < VEC; ++k) v[k] *= __ldg(a.fold + i + k);
+      }
     }
   };
   float held[kHeld][VEC];
@@ -1313,8 +1318,13 @@ __global__ void __launch_bounds__(kOuterThreads) k_outer(const OuterJobs a) {
   if (warp == 4) ptx::tmem_dealloc(tmem, cols);
 }
 
-// FP32, on the CUDA cores: 64 of i, eight of j at a time, the listed rows dealt
-// over GROUPS groups of threads (as many as an adapter has rows for).
+// FP32, on the CUDA cores: 64 COLS of i, eight of j at a time, the listed rows
+// dealt over GROUPS groups of threads. Where adapters have 256 rows or more, 16
+// groups and blocks of 64 columns, so that there are blocks enough (4,095 rows
+// of five, r = 6, widths 500 and 1,000: 24 us). With fewer, most blocks find few
+// rows or none, and eight groups of two columns a thread cost less (402 rows,
+// nearly all of one adapter of 36, r = 16, widths 384 and 3,520: 42 us; with
+// four groups of one column 80). Bound by the latency of a group's rows.
 struct OuterJobF32 {
   const float* in;
   int64_t ld;
@@ -1330,15 +1340,16 @@ struct OuterJobsF32 {
   int r;
 };
 
-template <int GROUPS>
+template <int GROUPS, int COLS>
 __global__ void __launch_bounds__(64 * GROUPS) k_outer_f32(const __grid_constant__ OuterJobsF32 a) {
-  __shared__ float red[GROUPS][8][64];
+  constexpr int kWide = 64 * COLS;
+  __shared__ float red[GROUPS][8][kWide];
   __shared__ uint16_t list[kWindow];
   __shared__ int count[2 * GROUPS];
   const OuterJobF32& job = a.job[blockIdx.z];
   const int g = blockIdx.y;
-  const int ti = threadIdx.x & 63, q = threadIdx.x >> 6, i = blockIdx.x * 64 + ti;
-  if (blockIdx.x * 64 >= job.width) return;
+  const int ti = threadIdx.x & 63, q = threadIdx.x >> 6, i = blockIdx.x * kWide + ti;
+  if (blockIdx.x * kWide >= job.width) return;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   int n = 0;
@@ -1347,30 +1358,42 @@ __global__ void __launch_bounds__(64 * GROUPS) k_outer_f32(const __grid_constant
   if (once) n = list_rows<64 * GROUPS>(a.adapter, 0, a.tokens, g, list, count, threadIdx.x);
   for (int j0 = 0; j0 < a.r; j0 += 8) {
     const int nj = min(8, a.r - j0);
-    float acc[8] = {};
+    float acc[COLS][8] = {};
     for (t0 = 0; t0 < a.tokens; t0 += kWindow) {
       if (!once) n = list_rows<64 * GROUPS>(a.adapter, t0, min(t0 + kWindow, a.tokens), g, list, count, threadIdx.x);
 #pragma unroll 4
       for (int k = q; k < n; k += GROUPS) {
         const int64_t t = t0 + list[k];
-        const float x = i < job.width ? __ldg(job.in + t * job.ld + i) : 0.f;
+        const float* in = job.in + t * job.ld + i;
         const float* c = job.c + t * a.r + j0;
+        float x[COLS], v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (j < nj) acc[j] = fmaf(x, __ldg(c + j), acc[j]);
+        for (int m = 0; m < COLS; ++m) x[m] = i + 64 * m < job.width ? __ldg(in + 64 * m) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < nj ? __ldg(c + j) : 0.f;
+#pragma unroll
+        for (int m = 0; m < COLS; ++m)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (j < nj) acc[m][j] = fmaf(x[m], v[j], acc[m][j]);
       }
       if (!once) __syncthreads();
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) red[q][j][ti] = acc[j];
+    for (int m = 0; m < COLS; ++m)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) red[q][j][ti + 64 * m] = acc[m][j];
     __syncthreads();
     // neighbouring threads along memory: along j or i
-    for (int e = threadIdx.x; e < nj * 64; e += 64 * GROUPS) {
-      const int j = job.f_j == 1 ? e % nj : e >> 6, k = job.f_j == 1 ? e / nj : e & 63, at = blockIdx.x * 64 + k;
+    float* out = job.out + g * job.f_g + j0 * job.f_j;
+    for (int e = threadIdx.x; e < nj * kWide; e += 64 * GROUPS) {
+      int j = e / kWide, k = e % kWide;
+      if (job.f_j == 1) j = nj == 8 ? e & 7 : e % nj, k = nj == 8 ? e >> 3 : e / nj;
+      const int at = blockIdx.x * kWide + k;
       float s = red[0][j][k];
 #pragma unroll
       for (int w = 1; w < GROUPS; ++w) s += red[w][j][k];
-      if (at < job.width) job.out[g * job.f_g + (j0 + j) * job.f_j + (int64_t)at * job.f_i] = s;
+      if (at < job.width) out[j * job.f_j + (int64_t)at * job.f_i] = s;
     }
     __syncthreads();
   }
@@ -1770,11 +1793,12 @@ struct Op {
         o.adapter = p.adapter;
         o.tokens = p.tokens;
         o.r = p.rank;
-        const dim3 grid((unsigned)ceil_div(wide, 64), (unsigned)p.adapters, (unsigned)n);
-        if (p.tokens >= 256 * (int64_t)p.adapters)
-          launch_pdl(k_outer_f32<16>, grid, 1024, s, o);
+        const bool many = p.tokens >= 256 * (int64_t)p.adapters;
+        const dim3 grid((unsigned)ceil_div(wide, many ? 64 : 128), (unsigned)p.adapters, (unsigned)n);
+        if (many)
+          launch_pdl(k_outer_f32<16, 1>, grid, 1024, s, o);
         else
-          launch_pdl(k_outer_f32<4>, grid, 256, s, o);
+          launch_pdl(k_outer_f32<8, 2>, grid, 512, s, o);
         LC_LAUNCH_CHECK("k_outer_f32");
       }
     } else {
