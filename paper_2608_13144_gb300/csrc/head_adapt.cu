@@ -1524,10 +1524,11 @@ struct Op {
     a.ldw = l.ld_g;
     a.G = p.adapters;
     a.r = p.rank;
-    // more rows a block leave fewer groups short; fewer fill the device, and then warps share them
+    // more rows a block leave fewer groups short; fewer fill the device, and then warps share them (4,095 rows of
+    // five adapters: 8 rows, four warps a group 41 us; 16, two 32; 32, two 40; 9,095 rows of one: 32, one 52; 16, two 58)
     const int64_t sms = mma::num_sms();
-    a.tile = p.tokens >= 128 * sms ? 128 : p.tokens >= 32 * sms ? 32 : 8;
-    a.share = a.tile == 8 ? 4 : 1;
+    a.tile = p.tokens >= 128 * sms ? 128 : p.tokens >= 32 * sms ? 32 : p.tokens >= 16 * sms ? 16 : 8;
+    a.share = a.tile == 8 ? 4 : a.tile == 16 ? 2 : 1;
     launch_pdl(k_low_f32, dim3((unsigned)ceil_div(p.tokens, a.tile), (unsigned)ceil_div(p.rank, 8), (unsigned)n), 256, s, a);
     LC_LAUNCH_CHECK("k_low_f32");
   }
