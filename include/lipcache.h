@@ -585,8 +585,7 @@ int64_t lipcache_adapted_workspace(const lipcache_adapted* p, int32_t backward);
  *   y_t = W x_t + bias + scales[g] B_g (A_g x_t)
  *   bias  classes FP32, nullable
  *   y     tokens x classes, row stride ldy
- * Rows of one request may stand anywhere; rows whose adapters stand in
- * non-decreasing order save a copy of x. tokens == 0 is a no-op.
+ * Rows may stand in any order of adapters. tokens == 0 is a no-op.
  * Errors: E_INVALID, E_CUDA.
  */
 lipcache_status lipcache_adapted_logits(const lipcache_adapted* p, const float* bias, void* y, int64_t ldy,
@@ -643,7 +642,8 @@ int64_t lipcache_orthogonalize_workspace(int32_t type, int64_t batch, int32_t ro
  *   X <- a X + (b S + c S S) X
  *   G             batch x rows x cols, row stride ldg, matrix stride
  *                 rows * ldg
- *   coefficients  host, 3 * steps
+ *   coefficients  host, 3 * steps, each finite and at most 64 in magnitude
+ *   eps           in [1e-30, 1]
  *   out           batch x rows x cols dense, type of G; may be G if that is
  *                 dense
  * FP32 matrices are iterated as pairs of FP16 values (22 bits), BF16 ones as

@@ -8,10 +8,12 @@
 // - The shared product runs on the tensor cores (head_mma.cuh). BF16: a tile
 //   with few adapters among its rows takes the low-rank product into the same
 //   sum, each adapter's few stages limited to its rows by the MMA's lane mask;
-//   a tile with many, and any FP32 tile, adds it in the epilogue, a thread a
-//   row, from u in FP32.
-// - u and v (shrink): BF16 on the tensor cores with the same lane masks, the
-//   rows loaded once for all adapters of a tile; FP32 a warp a row.
+//   a tile with many adds it in the epilogue from u in FP32. FP32: one more
+//   product, of u and of B with every adapter's side by side (zeros but in a
+//   row's own) as three BF16 planes each, up to 256 columns; in the epilogue
+//   beyond.
+// - u and v (shrink): BF16 on the tensor cores, a tile's adapters side by side,
+//   the rows loaded once for all of them; FP32 a warp for four rows of an adapter.
 // - dA and dB: the rows of an adapter, listed by the CTA that sums them, are
 //   gathered row by row, so that no other adapter's row is touched.
 // On the tensor cores u and v are two BF16 planes, hi + lo (16 bits): their
@@ -36,7 +38,7 @@ constexpr int kBlock = 4;  // stages of 64 the tensor cores sum before the sum i
 
 // ---------------------------------------------------------------- copies
 // A BF16 matrix whose rows TMA cannot read, in rows of ldo: 2048 columns of a
-// row a block.
+// row a block. Bound by memory.
 __global__ void __launch_bounds__(256)
     k_copy_rows(const uint16_t* in, int64_t ld, int cols, int parts, uint16_t* out, int64_t ldo) {
   ptx::wait_prerequisites();
@@ -53,8 +55,10 @@ __global__ void __launch_bounds__(256)
 }
 
 // ---------------------------------------------------------------- FP32 rows
-// A warp a row. Kinds of rows in a launch: planes of a row (of W, with the B of
-// all adapters for that class side by side); rows of A set side by side.
+// A warp a row, in registers between its maximum and its planes. Kinds of rows
+// in a launch: planes of a row (of W, with the B of all adapters for that class
+// side by side); rows of A set side by side. Bound by memory: 65,536 x 256 rows,
+// 134 MB, 26 us (5.2 TB/s).
 struct RowJob {
   int set_aside = 0;            // a row of A
   const float* in = nullptr;
@@ -226,7 +230,10 @@ __global__ void __launch_bounds__(128, 6) k_rows_f32(const __grid_constant__ Row
 // four rows of one adapter against eight columns of its factor: three loads for
 // eight multiplications of a lane, where a row alone takes nine. The products of
 // a row can be set side by side too (three BF16 planes, 0 but at its adapter's
-// place), over the row's power of two.
+// place), over the row's power of two. 65,536 x 256 rows, ten adapters of rank 8:
+// 43 us (67 MB read, 31 written; 24 of it outside the sums and the rows set side
+// by side), bound by the latency of a warp's groups, one after another, at 16
+// warps an SM: 128 registers hold four rows against eight columns.
 struct LowJob {
   const float* in;
   int64_t ld;
@@ -439,7 +446,8 @@ __global__ void __launch_bounds__(256, 2) k_low_f32(const __grid_constant__ LowJ
 }
 
 // ---------------------------------------------------------------- shrink, few rows
-// u of one row (blockIdx.x), eight columns (blockIdx.y) in FP32.
+// u of one row (blockIdx.x), eight columns (blockIdx.y) in FP32. Bound by
+// latency: 48 BF16 rows of 4,096, r = 16: 7.5 us.
 template <typename T>
 __global__ void __launch_bounds__(128)
     k_shrink_few(const T* x, int64_t ldx, int width, const T* A, int vec, int G, int r, const int32_t* adapter,
@@ -505,7 +513,9 @@ __global__ void __launch_bounds__(128)
 // that the rows are read, and the MMAs issued, once for all of them (up to 256
 // columns a pass); the epilogue takes each row's own columns. A cluster splits
 // the contracted width; its first CTA joins the parts in order. Bound by
-// reading the rows once, and by latency where they are few.
+// reading the rows once (8,192 x 4,096 BF16 rows, r = 16: 25 us, 5.5 TB/s after
+// 11 us that any size takes), and by latency where they are few. Twelve smaller
+// stages in place of three took no less.
 constexpr int kShrinkThreads = 192, kShrinkStages = 3, kShrinkStage = 48 * 1024;
 struct ShrinkJob {
   CUtensorMap rows, factor;
@@ -963,7 +973,8 @@ struct AdaptEpi {
 };
 
 // A few rows on the CUDA cores (FP32, or BF16 that TMA cannot read): a warp
-// takes four rows of W against eight of x. u: the rows' low-rank products, or
+// takes four rows of W against eight of x. Bound by latency, then by reading W
+// (4,096 x 4,096 FP32 for 16 rows: 70 us). u: the rows' low-rank products, or
 // null where a block works them out itself, kRowsDots of them at most: as many
 // rows of A as the block has of W, where a launch of its own costs the call 3 us.
 constexpr int kRowsDots = 16;
@@ -1101,7 +1112,8 @@ __device__ __forceinline__ int list_rows(const int32_t* adapter, int64_t t0, int
 // side). Four warps gather 64 rows a stage with 16-byte copies (past the list
 // and the width: zeros), one issues the MMAs. A cluster shares the rows of one
 // tile; its first CTA joins the parts in order. Bound by latency (the list, the
-// first rows) and by the adapter with the most rows.
+// first rows) and by the adapter with the most rows: 4,096 rows of eight adapters,
+// r = 32, widths 2,048 and 4,096: 30 us.
 struct OuterJob {
   const bf16* in;
   int64_t ld;

