@@ -1448,9 +1448,9 @@ struct Layout {
     c.take(b, f32 ? 0 : (size_t)(G * p.classes * ld_r));
     c.take(undo_in, (size_t)T);
     c.take(undo_w, (size_t)p.classes);
-    // up to 256 columns: four stages a pair of planes, 24 in all (in the
-    // epilogue, 65,536 x 200 with ten adapters of rank 8, the low-rank product
-    // took 100 of 138 us)
+    // up to 256 columns: eight stages of two planes each (in the epilogue,
+    // 65,536 x 200 with ten adapters of rank 8, the low-rank product took 100 of
+    // 138 us)
     dense = f32 && G > 0 && G * r <= 256;
     ld_g = round_up(G * r, 8);
     c.take(wide_u, dense ? (size_t)(3 * T * ld_g) : 0);
@@ -1656,13 +1656,6 @@ struct Op {
       a.low.chunks = g.chunks;
       a.low.last = g.last;
       a.low.idesc = g.idesc;
-      // small products first
-      static const int pu[6] = {2, 0, 1, 1, 0, 0}, pf[6] = {0, 2, 1, 0, 1, 0};
-      a.low.pairs = f32 ? 6 : 2;
-      for (int q = 0; q < a.low.pairs; ++q) {
-        a.low.a_z[q] = f32 ? pu[q] : 1 - q;
-        a.low.b_z[q] = f32 ? pf[q] : 0;
-      }
       maps.la = f32 ? mma::tensor_map(Tensor{l.wide_u, k, p.tokens, 3, l.ld_g, p.tokens * l.ld_g}, a.a_rows)
                     : mma::tensor_map(Tensor{l.up[i], l.ld_r, p.tokens, 2, l.ld_r, p.tokens * l.ld_r}, a.a_rows);
       maps.lb = mma::tensor_map(*F, f_mn ? 64 : a.bn / (pair ? 2 : 1));

@@ -146,20 +146,18 @@ __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t
     ptx::mma_f16_pair(d, a, b, id, acc);
 }
 
-// The low-rank segments of a tile: for each adapter among the tile's rows and
-// each of `pairs` plane pairs, the rows' factor times the adapter's, limited to
-// the adapter's rows. Tiles with more than kFewAdapters leave it to the
-// epilogue (`many`), which costs as much for any number.
+// The low-rank segments of a tile: for each adapter among the tile's rows the
+// rows' factor (two planes) times the adapter's, limited to the adapter's rows.
+// Tiles with more than kFewAdapters leave it to the epilogue (`many`), which
+// costs as much for any number.
 constexpr int kFewAdapters = 8;
 struct Low {
   const int32_t* adapter = nullptr;  // of each row
   int64_t tokens = 0;
   int G = 0;                         // 0: no low-rank segments
   int chunks = 0, last = 0;
-  int pairs = 0;
-  int a_z[6], b_z[6];                // plane of each factor; B's z is b_z * G + adapter
   int dense = 0;                     // every adapter's factor side by side, the rows' factors 0 but in their own:
-                                     // one product for all rows, B's z is b_z
+                                     // one product for all rows, three planes each (PLANES = 2)
   uint32_t idesc;
 };
 
@@ -257,6 +255,14 @@ __device__ __forceinline__ void tile_at(const Args& a, int t, int& mt, int& nt, 
   mt = band * 8 + rest - nt * high;
 }
 
+template <int CG>
+__device__ __forceinline__ void box_of(uint32_t dst, const CUtensorMap* m, int x, int y, int z, uint32_t bar) {
+  if (CG == 2)
+    load_3d_pair(dst, m, x, y, z, bar);
+  else
+    load_3d(dst, m, x, y, z, bar);
+}
+
 template <int CG, int PLANES, typename Epi>
 __global__ void __launch_bounds__(kThreads, 1)
     k_mma(const __grid_constant__ Maps maps, const Args a, const Epi epi) {
@@ -332,12 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane != 0) return;
         if (rank == 0) ptx::mbar_expect_tx(full + 8 * slot, (uint32_t)(CG * planes * (a_bytes + b_bytes)));
         const uint32_t bar = lead_full + 8 * slot;
-        auto box = [&](uint32_t dst, const CUtensorMap* m, int x, int y, int z) {
-          if (CG == 2)
-            load_3d_pair(dst, m, x, y, z, bar);
-          else
-            load_3d(dst, m, x, y, z, bar);
-        };
+        auto box = [&](uint32_t dst, const CUtensorMap* m, int x, int y, int z) { box_of<CG>(dst, m, x, y, z, bar); };
         for (int p = 0; p < planes; ++p) {
           const uint32_t sa = base + slot * stage_bytes + p * a_bytes, sb = base + slot * stage_bytes + PLANES * a_bytes + p * b_bytes;
           const int za = az + p * a.a_planes, zb = bz + p * a.b_planes;
@@ -354,25 +355,43 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       };
+      // a dense low-rank product's stage: two planes of the rows' factors and two of the adapters', at z0 and z1
+      auto load_planes = [&](int row, int col, int k, int z0, int z1) {
+        ok = ptx::mbar_wait_warp(empty + 8 * st, ph ^ 1u, abort_s, kWaitLimit);
+        if (!ok) return;
+        const uint32_t slot = st;
+        if (++st == nst) st = 0, ph ^= 1u;
+        if (lane != 0) return;
+        if (rank == 0) ptx::mbar_expect_tx(full + 8 * slot, (uint32_t)(CG * 2 * (a_bytes + b_bytes)));
+        const uint32_t bar = lead_full + 8 * slot, sa = base + slot * stage_bytes, sb = sa + 2 * a_bytes;
+        for (int p = 0; p < 2; ++p) {
+          const int z = p ? z1 : z0;
+          box_of<CG>(sa + p * a_bytes, &maps.la, k, row, z, bar);
+          if (a.lb_mn) {
+            for (int i = 0; i < a.bn / CG; i += 64) box_of<CG>(sb + p * b_bytes + i * 128, &maps.lb, col + i, k, z, bar);
+          } else {
+            box_of<CG>(sb + p * b_bytes, &maps.lb, k, col, z, bar);
+          }
+        }
+      };
       for (int t = worker; t < tiles && ok; t += workers) {
         int mt, nt, z;
         tile_at(a, t, mt, nt, z);
         const int row = mt * TM + (int)rank * 128, col = nt * a.bn + (int)rank * (a.bn / CG);
         for (int c = 0; c < chunks && ok; ++c)
           load(&maps.a, a.a_mn, row, c * kChunk, z, &maps.b, a.b_mn, col, c * kChunk, z, PLANES);
-        if (a.low.dense) {
-          for (int q = 0; q < a.low.pairs && ok; ++q)
+        if (PLANES == 2 && a.low.dense) {
+          for (int q = 0; q < 2 && ok; ++q)
             for (int c = 0; c < a.low.chunks && ok; ++c)
-              load(&maps.la, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk, a.low.b_z[q], 1);
+              load_planes(row, col, c * kChunk, 0, 2 - q);
         } else if (a.low.G) {
           Groups<TM> gr;
           gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
           if (!gr.more_than(kFewAdapters))
             while (ok && gr.next())
-              for (int q = 0; q < a.low.pairs && ok; ++q)
+              for (int q = 1; q >= 0 && ok; --q)
                 for (int c = 0; c < a.low.chunks && ok; ++c)
-                  load(&maps.la, false, row, c * kChunk, a.low.a_z[q], &maps.lb, a.lb_mn, col, c * kChunk,
-                       a.low.b_z[q] * a.low.G + gr.g, 1);
+                  load(&maps.la, false, row, c * kChunk, q, &maps.lb, a.lb_mn, col, c * kChunk, gr.g, 1);
         }
       }
     }
@@ -444,10 +463,30 @@ __global__ void __launch_bounds__(kThreads, 1)
             chunk(a.a_mn, a.b_mn, a.seg.idesc, c == chunks - 1 ? a.seg.last : 4, PLANES, nullptr);
           if (!DRAIN) c0 = chunks;
         }
-        if (a.low.dense) {
-          for (int q = 0; q < a.low.pairs && ok; ++q)
-            for (int c = 0; c < a.low.chunks && ok; ++c)
-              chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, 1, nullptr);
+        if (PLANES == 2 && a.low.dense) {
+          // u0 f2 and u2 f0 from stages of planes 0 and 2, then u1 f1, u0 f1, u1 f0 and u0 f0 from those of 0 and 1
+          for (int q = 0; q < 2 && ok; ++q)
+            for (int c = 0; c < a.low.chunks && ok; ++c) {
+              ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, kWaitLimit);
+              if (!ok) break;
+              ptx::tc_fence_after();
+              if (lead) {
+                const uint32_t sa = base + st * stage_bytes, sb = sa + 2 * a_bytes;
+                const int steps = c == a.low.chunks - 1 ? a.low.last : 4;
+                for (int pr = q == 0 ? 1 : 0; pr < (q == 0 ? 3 : 4); ++pr) {
+                  // pairs (plane of u, plane of f) of the stage: 11, 01, 10, 00
+                  uint64_t da = desc(sa + (pr == 0 || pr == 2 ? a_bytes : 0), false),
+                           db = desc(sb + (pr < 2 ? b_bytes : 0), a.lb_mn);
+                  for (int k = 0; k < steps; ++k, da += 32 >> 4, db += a.lb_mn ? 2048 >> 4 : 32 >> 4)
+                    mma<CG>(d, da, db, a.low.idesc, 1u);
+                }
+                if (CG == 2)
+                  ptx::mma_commit_pair_multicast(empty + 8 * st, (uint16_t)3);
+                else
+                  ptx::mma_commit(empty + 8 * st);
+              }
+              if (++st == nst) st = 0, ph ^= 1u;
+            }
         } else if (a.low.G) {
           Groups<TM> gr;
           gr.begin(a.low.adapter, a.low.tokens, a.low.G, (int64_t)mt * TM, lane);
@@ -456,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               uint32_t off[8] = {};
 #pragma unroll
               for (int k = 0; k < TM / 32; ++k) off[k] = ~gr.on[k];
-              for (int q = 0; q < a.low.pairs && ok; ++q)
+              for (int q = 0; q < 2 && ok; ++q)
                 for (int c = 0; c < a.low.chunks && ok; ++c)
                   chunk(false, a.lb_mn, a.low.idesc, c == a.low.chunks - 1 ? a.low.last : 4, 1, off);
             }
