@@ -255,6 +255,12 @@ __device__ __forceinline__ void tile_at(const Args& a, int t, int& mt, int& nt, 
   mt = band * 8 + rest - nt * high;
 }
 
+// Halves of a stage along the contracted index: the few-rows form's tiles are so
+// small that what a stage costs its producer and issuer sets the pace (450 clocks
+// for 64 of the index), so that theirs hold twice 64.
+template <typename Epi>
+constexpr int kHalves = Epi::kEarly ? 2 : 1;
+
 template <int CG>
 __device__ __forceinline__ void box_of(uint32_t dst, const CUtensorMap* m, int x, int y, int z, uint32_t bar) {
   if (CG == 2)
@@ -271,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   // a stage: A's planes, then B's
   // (A's rows past its box are whatever follows: their sums are not used)
-  const int a_bytes = a.a_rows * 128, b_bytes = a.bn / CG * 128, stage_bytes = PLANES * (a_bytes + b_bytes);
+  const int a_bytes = a.a_rows * 128, b_bytes = a.bn / CG * 128, stage_bytes = kHalves<Epi> * PLANES * (a_bytes + b_bytes);
   const int nst = a.stages;
   const uint32_t bars = base + nst * stage_bytes;
   const uint32_t full = bars, empty = bars + 8 * nst, acc_full = empty + 8 * nst, acc_empty = acc_full + 16,
@@ -378,8 +384,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         int mt, nt, z;
         tile_at(a, t, mt, nt, z);
         const int row = mt * TM + (int)rank * 128, col = nt * a.bn + (int)rank * (a.bn / CG);
-        for (int c = 0; c < chunks && ok; ++c)
-          load(&maps.a, a.a_mn, row, c * kChunk, z, &maps.b, a.b_mn, col, c * kChunk, z, PLANES);
+        if constexpr (Epi::kEarly) {
+          for (int c = 0; c < chunks && ok; c += 2) {
+            ok = ptx::mbar_wait_warp(empty + 8 * st, ph ^ 1u, abort_s, kWaitLimit);
+            if (!ok) break;
+            if (lane == 0) {
+              const int halves = min(2, chunks - c);
+              const uint32_t sa = base + st * stage_bytes, bar = full + 8 * st;
+              ptx::mbar_expect_tx(bar, (uint32_t)(halves * (a_bytes + b_bytes)));
+              for (int p = 0; p < halves; ++p) {
+                load_3d(sa + p * (a_bytes + b_bytes), &maps.a, (c + p) * kChunk, row, z, bar);
+                load_3d(sa + p * (a_bytes + b_bytes) + a_bytes, &maps.b, (c + p) * kChunk, col, z, bar);
+              }
+            }
+            if (++st == nst) st = 0, ph ^= 1u;
+          }
+        } else {
+          for (int c = 0; c < chunks && ok; ++c)
+            load(&maps.a, a.a_mn, row, c * kChunk, z, &maps.b, a.b_mn, col, c * kChunk, z, PLANES);
+        }
         if (PLANES == 2 && a.low.dense) {
           for (int q = 0; q < 2 && ok; ++q)
             for (int c = 0; c < a.low.chunks && ok; ++c)
@@ -453,15 +476,36 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (++st == nst) st = 0, ph ^= 1u;
         };
         open();
-        for (int c0 = 0; c0 < chunks && ok; c0 += a.block) {
-          if (c0) {
-            close();
-            open();
+        if constexpr (Epi::kEarly) {
+          for (int c = 0; c < chunks && ok; c += 2) {
+            ok = ptx::mbar_wait_warp(full + 8 * st, ph, abort_s, kWaitLimit);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            if (lead) {
+              const uint32_t sa = base + st * stage_bytes;
+              for (int p = 0; p < 2 && c + p < chunks; ++p) {
+                const int steps = c + p == chunks - 1 ? a.seg.last : 4;
+                uint64_t da = desc(sa + p * (a_bytes + b_bytes), false), db = desc(sa + p * (a_bytes + b_bytes) + a_bytes, false);
+                for (int k = 0; k < steps; ++k, da += 32 >> 4, db += 32 >> 4) {
+                  mma<CG>(d, da, db, a.seg.idesc, acc);
+                  acc = 1;
+                }
+              }
+              ptx::mma_commit(empty + 8 * st);
+            }
+            if (++st == nst) st = 0, ph ^= 1u;
           }
-          const int c1 = DRAIN ? min(c0 + a.block, chunks) : chunks;
-          for (int c = c0; c < c1 && ok; ++c)
-            chunk(a.a_mn, a.b_mn, a.seg.idesc, c == chunks - 1 ? a.seg.last : 4, PLANES, nullptr);
-          if (!DRAIN) c0 = chunks;
+        } else {
+          for (int c0 = 0; c0 < chunks && ok; c0 += a.block) {
+            if (c0) {
+              close();
+              open();
+            }
+            const int c1 = DRAIN ? min(c0 + a.block, chunks) : chunks;
+            for (int c = c0; c < c1 && ok; ++c)
+              chunk(a.a_mn, a.b_mn, a.seg.idesc, c == chunks - 1 ? a.seg.last : 4, PLANES, nullptr);
+            if (!DRAIN) c0 = chunks;
+          }
         }
         if (PLANES == 2 && a.low.dense) {
           // u0 f2 and u2 f0 from stages of planes 0 and 2, then u1 f1, u0 f1, u1 f0 and u0 f0 from those of 0 and 1
@@ -649,11 +693,11 @@ inline Seg segment(int64_t k, uint32_t id) {
 
 template <int CG, int PLANES, typename Epi>
 void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
-  const int stage = PLANES * (a.a_rows + a.bn / CG) * 128;
+  const int half = PLANES * (a.a_rows + a.bn / CG) * 128, stage = kHalves<Epi> * half;
   a.errors = error_counter();
   const int turn = Epi::kTurns ? kEpiWarps * kTurnBytes + 128 : 0;
   // (the MMAs read 128 rows of A's last stage)
-  const int past = std::max(0, kABytes - stage);
+  const int past = std::max(0, kABytes - half);
   a.stages = std::min(16, (kSmem - 1024 - 640 - turn - past) / stage);
   const int smem = 1024 + a.stages * stage + 640 + turn + past;
   allow_smem(reinterpret_cast<const void*>(k_mma<CG, PLANES, Epi>), kSmem);
