@@ -973,12 +973,17 @@ struct AdaptEpi {
 };
 
 // A few rows on the CUDA cores (FP32, or BF16 that TMA cannot read): a warp
-// takes four rows of W against eight of x. Bound by latency, then by reading W
-// (4,096 x 4,096 FP32 for 16 rows: 70 us). u: the rows' low-rank products, or
-// null where a block works them out itself, kRowsDots of them at most: as many
-// rows of A as the block has of W, where a launch of its own costs the call 3 us.
-constexpr int kRowsDots = 16;
-template <typename T>
+// takes four rows of W against eight of x; VEC: four FP32 columns a load. Bound by
+// the latency of the loads in flight (4,096 x 4,096 FP32, W from memory: eight rows
+// 32 us, 2.1 TB/s; 16 rows 51, one column a load 57; 48 rows 103, 157 by ones).
+// From 64 rows on the tensor cores are level or faster (64 rows, the shape above:
+// 128 us here, 106 there; 1,024 x 1,000: 13, 25).
+// u: the rows' low-rank products, or null where a block works them out itself,
+// kRowsDots of them at most (as many rows of A as the block has of W) of kRowsOwn
+// features: a launch of its own costs the host 3 us and the GPU under one, four
+// dots a warp of 4,096 features 14.
+constexpr int kRowsDots = 16, kRowsOwn = 512;
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(128)
     k_rows(const T* x, int64_t ldx, int64_t tokens, const T* W, int64_t ldw, int classes, int d, const float* bias,
            const float* u, const T* A, const float* scales, const T* B, const int32_t* adapter, int G, int r, T* y,
@@ -997,17 +1002,34 @@ __global__ void __launch_bounds__(128)
   float acc[32];
 #pragma unroll
   for (int k = 0; k < 32; ++k) acc[k] = 0.f;
+  if constexpr (VEC) {
 #pragma unroll 2
-  for (int i = lane; i < d; i += 32) {
-    float wv[4], xv[8];
+    for (int i = lane * 4; i < d; i += 128) {
+      float4 wv[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) wv[k] = to_f32<T>(w[k][i]);
+      for (int k = 0; k < 4; ++k) wv[k] = __ldg(reinterpret_cast<const float4*>(w[k] + i));
 #pragma unroll
-    for (int k = 0; k < 8; ++k) xv[k] = to_f32<T>(xr[k][i]);
+      for (int k = 0; k < 8; ++k) {
+        const float4 xv = __ldg(reinterpret_cast<const float4*>(xr[k] + i));
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 4; ++q)
+          acc[q * 8 + k] =
+              fmaf(wv[q].x, xv.x, fmaf(wv[q].y, xv.y, fmaf(wv[q].z, xv.z, fmaf(wv[q].w, xv.w, acc[q * 8 + k]))));
+      }
+    }
+  } else {
+#pragma unroll 2
+    for (int i = lane; i < d; i += 32) {
+      float wv[4], xv[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) acc[q * 8 + k] = fmaf(wv[q], xv[k], acc[q * 8 + k]);
+      for (int k = 0; k < 4; ++k) wv[k] = to_f32<T>(w[k][i]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) xv[k] = to_f32<T>(xr[k][i]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[q * 8 + k] = fmaf(wv[q], xv[k], acc[q * 8 + k]);
+    }
   }
 #pragma unroll
   for (int s = 16; s > 0; s >>= 1) {
@@ -1045,15 +1067,15 @@ __global__ void __launch_bounds__(128)
     }
     __syncthreads();
   }
-  const int c = c0 + (lane >> 3);
-  const int64_t t = t0 + (lane & 7);
+  const int c = c0 + lane / 8, row = lane % 8;
+  const int64_t t = t0 + row;
   if (c >= classes || t >= tokens) return;
   float v = acc[0];
   if (bias) v += __ldg(bias + c);
   const int g = G ? __ldg(adapter + t) : -1;
   if (g >= 0 && g < G) {
     const T* b = B + ((int64_t)g * classes + c) * r;
-    const float* ut = u ? u + t * r : own + (lane & 7) * r;
+    const float* ut = u ? u + t * r : own + row * r;
     for (int k = 0; k < r; ++k) v = fmaf(ut[k], to_f32<T>(b[k]), v);
   }
   y[t * ldy + c] = from_f32<T>(v);
@@ -1699,7 +1721,7 @@ struct Op {
     const Side d{x, p.ldx, p.d, p.classes, p.d, 1};
     const bool low = p.adapters > 0, tma = !f32 && mma::mappable(x, p.ldx) && mma::mappable(W, p.ldw);
     if (p.tokens <= (tma ? kFewBf16 : kFewF32)) {
-      const bool own = !tma && p.tokens * p.rank <= kRowsDots;
+      const bool own = !tma && p.tokens * p.rank <= kRowsDots && p.d <= kRowsOwn;
       if (low && !own) {
         const int vec = ((uintptr_t)x & 15) == 0 && ((uintptr_t)A & 15) == 0 && p.ldx * sizeof(T) % 16 == 0 &&
                         p.d * sizeof(T) % 16 == 0;
@@ -1713,9 +1735,11 @@ struct Op {
         epilogue_low(e, 0, B, true);
         product(d, rows_of(d, 0), head(), false, 0, nullptr, false, e);
       } else {
-        launch_pdl(k_rows<T>, dim3((unsigned)ceil_div(p.classes, 16), (unsigned)ceil_div(p.tokens, 8)), 128, s, x,
-                   p.ldx, p.tokens, W, p.ldw, (int)p.classes, (int)p.d, bias, own ? (const float*)nullptr : (const float*)l.u[0],
-                   A, p.scales, B, p.adapter, (int)p.adapters, (int)p.rank, y, ldy);
+        const bool wide = f32 && p.d % 4 == 0 && p.ldx % 4 == 0 && p.ldw % 4 == 0 && (((uintptr_t)x | (uintptr_t)W) & 15) == 0;
+        launch_pdl(wide ? k_rows<T, f32> : k_rows<T, false>,
+                   dim3((unsigned)ceil_div(p.classes, 16), (unsigned)ceil_div(p.tokens, 8)), 128, s, x, p.ldx, p.tokens,
+                   W, p.ldw, (int)p.classes, (int)p.d, bias, own ? (const float*)nullptr : (const float*)l.u[0], A,
+                   p.scales, B, p.adapter, (int)p.adapters, (int)p.rank, y, ldy);
         LC_LAUNCH_CHECK("k_rows");
       }
       return;
