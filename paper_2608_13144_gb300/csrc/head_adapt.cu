@@ -231,8 +231,8 @@ __global__ void __launch_bounds__(128, 6) k_rows_f32(const __grid_constant__ Row
 // eight multiplications of a lane, where a row alone takes nine. The products of
 // a row can be set side by side too (three BF16 planes, 0 but at its adapter's
 // place), over the row's power of two. 65,536 x 256 rows, ten adapters of rank 8:
-// 43 us (67 MB read, 31 written; 24 of it outside the sums and the rows set side
-// by side), bound by the latency of a warp's groups, one after another, at 16
+// 41 us (67 MB read, 31 written; half of it outside the sums and the rows set
+// side by side), bound by the latency of a warp's groups, one after another, at 16
 // warps an SM: 128 registers hold four rows against eight columns.
 struct LowJob {
   const float* in;

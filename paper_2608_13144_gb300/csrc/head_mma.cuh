@@ -270,10 +270,11 @@ __device__ __forceinline__ void box_of(uint32_t dst, const CUtensorMap* m, int x
     load_3d(dst, m, x, y, z, bar);
 }
 
-template <int CG, int PLANES, typename Epi>
+// DRAIN: a sum has more than one block (a kernel of its own: the registers that
+// hold sums between blocks leave too few for the epilogue, which then spills).
+template <int CG, int PLANES, bool DRAIN, typename Epi>
 __global__ void __launch_bounds__(kThreads, 1)
     k_mma(const __grid_constant__ Maps maps, const Args a, const Epi epi) {
-  constexpr bool DRAIN = PLANES == 2;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
   // a stage: A's planes, then B's
@@ -601,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         ++n;
       };
-      if (DRAIN && chunks > a.block) {
+      if constexpr (DRAIN) {
         constexpr int kParts = CG == 2 ? 4 : 2;  // bn <= 128 CG
         float sum[kParts][32];
 #pragma unroll
@@ -692,8 +693,8 @@ inline Seg segment(int64_t k, uint32_t id) {
   return Seg{chunks, (int)ceil_div(k - (int64_t)(chunks - 1) * kChunk, 16), id};
 }
 
-template <int CG, int PLANES, typename Epi>
-void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
+template <int CG, int PLANES, bool DRAIN, typename Epi>
+void launch_as(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
   const int half = PLANES * (a.a_rows + a.bn / CG) * 128, stage = kHalves<Epi> * half;
   a.errors = error_counter();
   const int turn = Epi::kTurns ? kEpiWarps * kTurnBytes + 128 : 0;
@@ -701,7 +702,7 @@ void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
   const int past = std::max(0, kABytes - half);
   a.stages = std::min(16, (kSmem - 1024 - 640 - turn - past) / stage);
   const int smem = 1024 + a.stages * stage + 640 + turn + past;
-  allow_smem(reinterpret_cast<const void*>(k_mma<CG, PLANES, Epi>), kSmem);
+  allow_smem(reinterpret_cast<const void*>(k_mma<CG, PLANES, DRAIN, Epi>), kSmem);
   const int64_t per = a.sym ? (int64_t)a.m_tiles * (a.m_tiles + 1) / 2 : (int64_t)a.m_tiles * a.n_tiles;
   const int64_t tiles = per * a.batches;
   LC_REQUIRE(tiles < (1LL << 31), LIPCACHE_E_INVALID, "too many tiles");
@@ -719,8 +720,15 @@ void launch(const Maps& maps, Args a, const Epi& epi, cudaStream_t s) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CG == 2 ? 2 : 1;
-  LC_CUDA(cudaLaunchKernelEx(&cfg, k_mma<CG, PLANES, Epi>, maps, a, epi));
+  LC_CUDA(cudaLaunchKernelEx(&cfg, k_mma<CG, PLANES, DRAIN, Epi>, maps, a, epi));
   LC_LAUNCH_CHECK("k_mma");
+}
+template <int CG, int PLANES, typename Epi>
+void launch(const Maps& maps, const Args& a, const Epi& epi, cudaStream_t s) {
+  if constexpr (PLANES == 2) {
+    if (a.seg.chunks > a.block) return launch_as<CG, PLANES, true>(maps, a, epi, s);
+  }
+  launch_as<CG, PLANES, false>(maps, a, epi, s);
 }
 
 }  // namespace mma
