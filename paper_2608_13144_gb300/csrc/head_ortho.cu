@@ -481,7 +481,8 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
   unsigned char* misc_p = smem_raw + (misc - ptx::smem_u32(smem_raw));
   volatile uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc_p);
   volatile int* abort_s = reinterpret_cast<volatile int*>(misc_p + 4);
-  uint32_t* counts = reinterpret_cast<uint32_t*>(misc_p + 8);  // warps done with what is added, with the phase
+  // warps done with what is added to even tiles and to odd ones, with the phase
+  uint32_t* counts = reinterpret_cast<uint32_t*>(misc_p + 8);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)ptx::cluster_ctarank();
   if (threadIdx.x == 0) {
@@ -500,7 +501,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
     ptx::mbar_init(go, 1);  // the producer has seen the barrier over the grid
     ptx::mbar_init(low_empty, mma::kEpiWarps);
     *abort_s = 0;
-    counts[0] = counts[1] = 0;
+    counts[0] = counts[1] = counts[2] = 0;
     ptx::fence_mbar_init();
   }
   if (warp == 1) {
@@ -692,7 +693,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
     // registers takes a cycle for every 16 bytes (128 x 128 FP32 tiles: 9,000
     // clocks of a phase).
     const int quarter = warp & 3, half = (warp - 2) >> 2;
-    int n = 0, joins = 0, st = 0;
+    int n = 0, joins = 0, st = 0, added = 0;
     uint32_t ph = 0;
     bool ok = true;
     for (int i = 0; i < a.steps && ok; ++i)
@@ -856,9 +857,12 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
             }
           }
           if (adds(w)) {
-            // the last of the eight warps gives the stage back
+            // The last of the eight warps gives the stage back. Tiles count apart by turns: with one
+            // sum a tile (one plane) a warp may be a tile ahead of another, but not two, since the
+            // accumulator of the tile after next waits for all eight, who count before they free it.
             __syncwarp();
-            if (lane == 0 && last_of_eight(counts)) ptx::mbar_arrive(empty + 8 * st);
+            if (lane == 0 && last_of_eight(counts + (added & 1))) ptx::mbar_arrive(empty + 8 * st);
+            ++added;
             if (++st == kStages) st = 0, ph ^= 1u;
           }
           ptx::tc_fence_before();
@@ -935,7 +939,7 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
         // written, and readable by copies of other CTAs; the last warp says so
         asm volatile("fence.proxy.async.global;" ::: "memory");
         __syncwarp();
-        if (lane == 0 && last_of_eight(counts + 1)) add_release(a.phases);
+        if (lane == 0 && last_of_eight(counts + 2)) add_release(a.phases);
       }
   }
   __syncthreads();
