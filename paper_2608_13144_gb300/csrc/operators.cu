@@ -21,6 +21,8 @@ bool known_type(int32_t t) { return t == LIPCACHE_F32 || t == LIPCACHE_BF16; }
 #define LC_ARG(cond, msg) LC_REQUIRE(cond, LIPCACHE_E_INVALID, msg)
 
 bool aligned(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % lc::ops::elem(type) == 0; }
+// of arrays of 32-bit values whatever the operator's type
+bool aligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 void check_adapted_sizes(const lipcache_adapted* p) {
   LC_ARG(p != nullptr, "NULL operator description");
@@ -45,7 +47,8 @@ void check_adapted(const lipcache_adapted* p) {
   LC_ARG(p->ldx >= p->d && p->ldw >= p->d, "a row stride is smaller than the row");
   LC_ARG(p->tokens == 0 || (p->x && p->W), "NULL x or W");
   LC_ARG(p->tokens == 0 || p->adapters == 0 || (p->A && p->B && p->adapter), "NULL A, B or adapter");
-  LC_ARG(aligned(p->x, p->type) && aligned(p->W, p->type) && aligned(p->A, p->type) && aligned(p->B, p->type),
+  LC_ARG(aligned(p->x, p->type) && aligned(p->W, p->type) && aligned(p->A, p->type) && aligned(p->B, p->type) &&
+             aligned4(p->adapter) && aligned4(p->scales),
          "a tensor is not aligned to its elements");
 }
 
@@ -66,6 +69,7 @@ LC_API lipcache_status lipcache_adapted_logits(const lipcache_adapted* p, const 
     check_adapted(p);
     if (p->tokens == 0) return;
     LC_ARG(y != nullptr && aligned(y, p->type), "y is NULL or not aligned to its elements");
+    LC_ARG(aligned4(bias), "a tensor is not aligned to its elements");
     LC_ARG(ldy >= p->classes, "a row stride is smaller than the row");
     check_workspace(workspace, workspace_bytes, lc::ops::adapted_bytes(*p, false));
     lc::ops::adapted_logits(*p, bias, y, ldy, static_cast<unsigned char*>(workspace), stream);
@@ -105,7 +109,8 @@ LC_API lipcache_status lipcache_cross_entropy(int32_t type, const void* logits, 
     LC_ARG(logits != nullptr && target != nullptr, "NULL logits or target");
     LC_ARG(ldz >= classes && (dlogits == nullptr || ldd >= classes), "a row stride is smaller than the row");
     LC_ARG(dlogits != logits || ldd == ldz, "gradients in place need the logits' row stride");
-    LC_ARG(aligned(logits, type) && aligned(dlogits, type), "a tensor is not aligned to its elements");
+    LC_ARG(aligned(logits, type) && aligned(dlogits, type) && aligned4(target) && aligned4(weight) && aligned4(loss),
+           "a tensor is not aligned to its elements");
     if (loss == nullptr && dlogits == nullptr) return;
     lc::ops::cross_entropy(type, logits, ldz, tokens, classes, target, weight, loss, dlogits, ldd, stream);
   });

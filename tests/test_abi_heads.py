@@ -92,6 +92,18 @@ def test_orthogonalize_arguments(lib):
         assert st(**bad) == 1, bad
 
 
+def test_arrays_of_32_bits_are_aligned(lib):
+    big = 1 << 40
+    for ty in (0, 1):
+        for bad in (dict(adapter=4098), dict(adapter=4097), dict(scales=4098)):
+            p = describe(type=ty, **bad)
+            assert lib.lipcache_adapted_logits(C.byref(p), None, 4096, 8, 4096, big, None) == 1, bad
+            assert lib.lipcache_adapted_logits_backward(C.byref(p), 4096, 8, 4096, 16, 4096, 4096, 4096, big, None) == 1, bad
+        assert lib.lipcache_adapted_logits(C.byref(describe(type=ty)), 4098, 4096, 8, 4096, big, None) == 1
+        for target, weight, loss in ((4098, None, 4096), (4096, 4098, 4096), (4096, None, 4097)):
+            assert lib.lipcache_cross_entropy(ty, 4096, 8, 2, 8, target, weight, loss, 8192, 8, None) == 1
+
+
 def test_operator_errors_argument(lib):
     assert lib.lipcache_operator_errors(None, None) == 1
 
