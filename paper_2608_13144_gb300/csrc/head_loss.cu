@@ -138,16 +138,20 @@ __device__ __forceinline__ RowResult finish(Run r, float zy, float w, float* los
   const float m_o = r.m, s_o = r.s;
   const bool bad = isnan(r.s) || !(zy < INFINITY);
   r.join(zy, zy == -INFINITY ? 0.f : 1.f);
+  const float others = s_o == 0.f ? 0.f : s_o * __expf(m_o - r.m);  // their share of r.s
   RowResult q;
   q.m = r.m;
   if (loss && write) {
-    const float l = zy == -INFINITY ? INFINITY : logf(r.s) + r.m - zy;
+    // Differences of logits first: the logarithm keeps its bits wherever the logits
+    // stand. A target that is the maximum has r.s = 1 + others, of which a sure
+    // row's loss would be the rounding.
+    const float l = zy == -INFINITY ? INFINITY : r.m == zy ? log1pf(others) : logf(r.s) + (r.m - zy);
     *loss = bad ? NAN : w == 0.f ? 0.f : w * l;
   }
   q.odd = bad || r.m == -INFINITY;
   q.fill = bad ? NAN : 0.f;
   q.inv = w / r.s;
-  q.at_target = s_o == 0.f ? 0.f : -w * (s_o * __expf(m_o - r.m) / r.s);
+  q.at_target = s_o == 0.f ? 0.f : -w * (others / r.s);
   return q;
 }
 
