@@ -94,7 +94,7 @@ __device__ __forceinline__ void direction(const Direction& a, const T* g, int64_
   load_vec<T, VEC>(g + row * a.ldg + col, v);
   if (!a.st.weight) return;
   const int64_t at = row * a.cols + col;
-  const float b = a.st.beta, r = 1.f - b;
+  const float b = a.st.beta, r = a.st.fresh;
   float m[VEC];
   load_vec<float, VEC>((FIRST ? a.st.momentum : a.st.out_momentum) + at, m);
   if (FIRST) {

@@ -143,9 +143,9 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
     for (int q = 0; q < kBatch; ++q) {
       if (at_x[q] < 0) continue;
       if (a.st.weight) {
-        const float b = a.st.beta, n = fmaf(b, m[q], (1.f - b) * v[q]);
+        const float b = a.st.beta, r = a.st.fresh * v[q], n = fmaf(b, m[q], r);
         a.st.out_momentum[o[q]] = n;
-        v[q] = a.st.nesterov ? fmaf(b, n, (1.f - b) * v[q]) : n;
+        v[q] = a.st.nesterov ? fmaf(b, n, r) : n;
       }
       x[at_x[q]] = v[q];
       const float w = fabsf(v[q]);

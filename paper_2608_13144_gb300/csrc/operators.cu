@@ -189,6 +189,7 @@ LC_API lipcache_status lipcache_orthogonal_step(int32_t weight_type, int32_t gra
     st.out_momentum = out_momentum;
     st.weight_type = weight_type;
     st.beta = (float)beta;
+    st.fresh = (float)(1.0 - beta);
     st.keep = (float)(1.0 - lr * weight_decay);
     st.rate = (float)(lr * std::sqrt(std::fmax(1.0, (double)rows / cols)));
     st.nesterov = nesterov != 0;

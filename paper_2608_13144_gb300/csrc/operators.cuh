@@ -123,7 +123,8 @@ struct OrthoStep {  // what a step adds to an orthogonalisation; null weight: no
   const float* momentum = nullptr;
   float* out_momentum = nullptr;
   int weight_type = 0;
-  float beta = 0.f, keep = 1.f, rate = 0.f;  // W' = keep W - rate O
+  float beta = 0.f, fresh = 1.f;  // fresh: 1 - beta, rounded once
+  float keep = 1.f, rate = 0.f;   // W' = keep W - rate O
   bool nesterov = false;
 };
 // head_ortho_small.cu: false where the matrices are not its kind (a side of at

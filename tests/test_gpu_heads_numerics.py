@@ -8,7 +8,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_heads import BF16, F32, UNIT, dev, f64, heads, within  # noqa: E402,F401
+from test_gpu_heads import BF16, F32, QUINTIC, UNIT, dev, f64, heads, ortho_exact, within  # noqa: E402,F401
 
 
 # ---------------------------------------------------------------- the loss's precision
@@ -38,3 +38,26 @@ def test_cross_entropy_of_confident_rows(dev, heads, dtype, c, offset):
     got, dz = heads.cross_entropy(z, y.to(dev))
     within(got, want, 2.0 ** -16 * want.abs() + 1e-37, "loss")
     within(dz, grad, 2 * UNIT[dtype] * grad.abs() + 2.0 ** -16 * grad.abs() + 1e-37, "grad")
+
+
+# ---------------------------------------------------------------- beta near one
+@pytest.mark.parametrize("shape", [(16, 200), (90, 130), (90, 128), (3, 70, 65)], ids=str)
+@pytest.mark.parametrize("gt", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("beta", [0.999, 0.9999, 0.999999])
+def test_orthogonal_step_with_beta_near_one(dev, heads, shape, gt, beta):
+    """1 - beta is that of the caller's beta, not of its rounding: momentum within four roundings."""
+    gen = torch.Generator().manual_seed(1)
+    grad, w = torch.randn(shape, generator=gen).to(gt), torch.randn(shape, generator=gen)
+    for mom in (torch.zeros(shape), 1e-4 * torch.randn(shape, generator=gen)):
+        for nesterov in (True, False):
+            _, om = heads.orthogonal_step(w.to(dev), grad.to(dev), mom.to(dev), 0.1, beta, nesterov)
+            new = beta * mom.double() + (1 - beta) * grad.double()
+            within(om, new, 4 * UNIT[F32] * (beta * mom.double().abs() + (1 - beta) * grad.double().abs()))
+            if shape == (90, 128):
+                ow, _ = heads.orthogonal_step(w.to(dev), grad.to(dev), mom.to(dev), 0.1, beta, nesterov)
+                d = beta * new + (1 - beta) * grad.double() if nesterov else new
+                o = ortho_exact(d, 5, QUINTIC, 1e-7)
+                noise = max(float(torch.linalg.vector_norm(ortho_exact(d, 5, QUINTIC, 1e-7, 2.0 ** -21, k) - o)) for k in range(3))
+                want = w.double() - 0.1 * o
+                assert float(torch.linalg.vector_norm(f64(ow) - want)) <= 0.8 * noise + 2 * UNIT[F32] * float(
+                    torch.linalg.vector_norm(want)) + 1e-7
