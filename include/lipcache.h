@@ -648,8 +648,10 @@ int64_t lipcache_orthogonalize_workspace(int32_t type, int64_t batch, int32_t ro
  *                 dense
  * FP32 matrices are iterated as pairs of FP16 values (22 bits), BF16 ones as
  * single FP16 values (11 bits, three more than the output's), with FP32
- * sums. Intended for polynomials that keep singular values below 4 (above, a
- * result may overflow). A matrix with a NaN or an infinity comes out NaN.
+ * sums, relative to the matrix's own size also while that is far below 1 (of
+ * a norm far below eps). Intended for polynomials that keep singular values
+ * below 4 (above, a result may overflow). A matrix with a NaN or an infinity
+ * comes out NaN.
  * Errors: E_INVALID, E_CUDA.
  */
 lipcache_status lipcache_orthogonalize(int32_t type, const void* G, int64_t ldg, int64_t batch, int32_t rows,

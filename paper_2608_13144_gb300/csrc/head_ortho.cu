@@ -12,6 +12,9 @@
 // normalisation is split into a power of two that takes ||D|| below 1, applied
 // exactly when the planes are written, and the rest t <= 2, which joins the
 // first step's epilogues, so that the first X of a BF16 matrix is exact.
+// A matrix far below eps stays far below 1 after that: it is kept as Y = 2^k X,
+// its largest singular value near 1, and each step takes from k what it lifts X
+// by (lift_steps), so that it keeps the bits of the planes all the way.
 //
 // S and P are symmetric: tiles on or above the diagonal are computed and
 // written twice. Nothing is transposed: a tall X is contracted over its rows,
@@ -33,6 +36,7 @@ constexpr int kPairBlock = 2;  // the same where products with low parts share t
 struct OrthoLayout {
   __half *x[2], *s, *p;  // planes x batch x rows x ld
   float* t;              // batch: the rest of the normalisation
+  float2* lift;          // batch x LIPCACHE_MAX_NS_STEPS: factors of each step (lift_steps)
   unsigned* phases;      // CTAs past each phase of k_iterate
   double* part;          // batch x kParts
   int64_t ld, sld, x_plane, s_plane;
@@ -47,6 +51,7 @@ struct OrthoLayout {
     c.take(s, (size_t)(planes * batch * s_plane));
     c.take(p, (size_t)(planes * batch * s_plane));
     c.take(t, (size_t)batch);
+    c.take(lift, (size_t)batch * LIPCACHE_MAX_NS_STEPS);
     c.take(phases, 1);
     c.take(part, (size_t)batch * kParts);
   }
@@ -151,11 +156,45 @@ __global__ void __launch_bounds__(256) k_squares(const T* g, const Direction a, 
   }
 }
 
+struct Steps {
+  int n;
+  float coef[3 * LIPCACHE_MAX_NS_STEPS];
+};
+
+// Y = 2^k X in step i: P = b S + c q S S and Y' = w (a Y + q P Y), S = Y Y^T, with
+// q = 4^-k and w = 2^(k' - k); the last step gives X itself (k' = 0). Once k = 0 it
+// stays there, and both factors are 1. While it is not, singular values of Y are
+// at most `top` (2 at first): p(s) / s is at most |a| + |b| q top^2 + |c| q^2 top^4,
+// and k' is what keeps the next ones in [1, 2) of that bound.
+__device__ __forceinline__ void lift_steps(double t, const Steps& st, float* rest, float2* lift) {
+  int x;
+  frexp(t, &x);
+  int k = max(0, 1 - x);
+  *rest = (float)ldexp(t, k);
+  float top = 2.f;
+  for (int i = 0; i < st.n; ++i) {
+    if (k == 0) {
+      lift[i] = make_float2(1.f, 1.f);
+      continue;
+    }
+    const float q = k < 75 ? ldexpf(1.f, -2 * k) : 0.f, s = q * top * top;
+    int r = k;
+    if (i + 1 < st.n) {
+      const float next = top * (fabsf(st.coef[3 * i]) + s * (fabsf(st.coef[3 * i + 1]) + s * fabsf(st.coef[3 * i + 2])));
+      frexpf(next, &r);
+      r = next > 0.f ? min(r - 1, k) : 0;
+      top = ldexpf(next, -r);
+    }
+    lift[i] = make_float2(q, ldexpf(1.f, -r));
+    k -= r;
+  }
+}
+
 // X's planes: D times 2^-e and kXScale, ||D|| < 2^e <= 2 ||D||.
 template <typename T, int VEC, int PLANES>
 __global__ void __launch_bounds__(256)
-    k_planes(const T* g, const Direction a, const double* part, int parts, double eps, __half* x,
-             int64_t ld, int64_t plane, float* t, unsigned* phases) {
+    k_planes(const T* g, const Direction a, const double* part, int parts, double eps, const Steps steps, __half* x,
+             int64_t ld, int64_t plane, float* t, float2* lift, unsigned* phases) {
   __shared__ float factor;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
@@ -171,7 +210,11 @@ __global__ void __launch_bounds__(256)
       frexp(norm > 0.0 ? norm : 1.0, &e);  // norm < 2^e
       const bool fine = isfinite(norm) && e <= 126;
       factor = fine ? ldexpf(kXScale, min(-e, 114)) : NAN;
-      if (blockIdx.x == 0) t[blockIdx.y] = fine ? (float)(ldexp(1.0, e) / (norm + eps)) : NAN;
+      if (blockIdx.x == 0) {
+        lift_steps(fine ? ldexp(1.0, e) / (norm + eps) : 1.0, steps, t + blockIdx.y,
+                   lift + (int64_t)blockIdx.y * LIPCACHE_MAX_NS_STEPS);
+        if (!fine) t[blockIdx.y] = NAN;
+      }
     }
   }
   __syncthreads();
@@ -248,7 +291,7 @@ __device__ __forceinline__ void add_planes(const __half* d, int64_t plane, int l
 
 struct Nothing {};
 
-// S (of = null) or P = c S S + b S, both triangles.
+// S (of = null) or P = c q S S + b S, both triangles.
 template <int PLANES>
 struct SymEpi {
   static constexpr bool kTurns = false, kEarly = false;
@@ -259,12 +302,14 @@ struct SymEpi {
   int64_t ld, mat, plane;  // row, matrix and plane strides
   int m;
   float f, b;
-  const float* t;  // nullable: squared into f
+  const float* t;      // nullable: squared into f
+  const float2* lift;  // of this step (P)
   __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32], const Nothing&, int) const {
     const int row = row0 + lane, left = m - col0;
     if (left <= 0) return;
     float g = f;
     if (t) g *= __ldcg(t + z) * __ldcg(t + z);
+    if (of) g *= __ldg(lift + (int64_t)z * LIPCACHE_MAX_NS_STEPS).x;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = g * __uint_as_float(acc[j]);
@@ -276,7 +321,7 @@ struct SymEpi {
   }
 };
 
-// X' = a X + P X.
+// X' = w (a X + q P X).
 template <int PLANES>
 struct UpdateEpi {
   static constexpr bool kTurns = false, kEarly = false;
@@ -288,10 +333,12 @@ struct UpdateEpi {
   int rows, cols;
   float f, a;
   const float* t;
+  const float2* lift;
   __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32], const Nothing&, int) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
-    const float u = t ? __ldcg(t + z) : 1.f, g = f * u;
+    const float2 qw = __ldg(lift + (int64_t)z * LIPCACHE_MAX_NS_STEPS);
+    const float u = (t ? __ldcg(t + z) : 1.f) * qw.y, g = f * u * qw.x;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = g * __uint_as_float(acc[j]);
@@ -314,10 +361,12 @@ struct LastEpi {
   int rows, cols, vec;
   float f, a, keep, rate;
   const float* t;
+  const float2* lift;
   __device__ __forceinline__ void store(int row0, int col0, int z, int lane, bool, uint32_t, const uint32_t (&acc)[32], const Nothing&, int) const {
     const int row = row0 + lane, left = cols - col0;
     if (left <= 0 || row >= rows) return;
-    const float u = t ? __ldcg(t + z) : 1.f, g = f * u;
+    const float2 qw = __ldg(lift + (int64_t)z * LIPCACHE_MAX_NS_STEPS);
+    const float u = (t ? __ldcg(t + z) : 1.f) * qw.y, g = f * u * qw.x;
     float v[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) v[j] = g * __uint_as_float(acc[j]);
@@ -393,6 +442,7 @@ struct IterateArgs {
   int split[3], bn[3];             // of S, P and X' phases; bn: columns of a tile, 128 or (unsplit) 64
   float coef[3 * LIPCACHE_MAX_NS_STEPS], ps[LIPCACHE_MAX_NS_STEPS];
   const float* t;
+  const float2* lift;
   void* out;
   const void* weight;
   int rows, cols, vec;
@@ -714,15 +764,16 @@ __global__ void __launch_bounds__(mma::kThreads, 1) k_iterate(const __grid_const
           int r, c, z;
           tile(w, t, r, c, z);
           const float tn = i == 0 ? __ldcg(a.t + z) : 1.f;
+          const float2 qw = __ldg(a.lift + (int64_t)z * LIPCACHE_MAX_NS_STEPS + i);
           float f, g = 0.f;
           if (k == 0) {
             f = tn * tn * (kSScale / (kXScale * kXScale));
           } else if (k == 1) {
-            f = a.coef[3 * i + 2] * ps / (kSScale * kSScale);
+            f = a.coef[3 * i + 2] * ps / (kSScale * kSScale) * qw.x;
             g = a.coef[3 * i + 1] * ps / kSScale;
           } else {
-            const float last = w.kind == 3 ? 1.f / kXScale : 1.f;
-            f = tn * last / ps;
+            const float last = w.kind == 3 ? qw.y / kXScale : qw.y;
+            f = tn * last / ps * qw.x;
             g = tn * last * a.coef[3 * i];
           }
           const int row = r * kTile + quarter * 32 + lane, col = c * w.bn + half * hw;
@@ -1038,6 +1089,7 @@ void iterate_at_once(int batch, int rows, int cols, int steps, const double* co,
   }
   grid = std::min<int64_t>(round_up(grid, kCluster), ctas);
   a.t = l.t;
+  a.lift = l.lift;
   a.out = st.weight ? st.out_weight : out;
   a.weight = st.weight;
   a.rows = rows;
@@ -1087,7 +1139,8 @@ void product(const mma::Tensor& A, bool a_mn, const mma::Tensor& B, bool b_mn, i
 }
 
 template <typename T, int VEC, int PLANES>
-void normalise(const T* g, Direction a, int64_t batch, double eps, const OrthoLayout& l, cudaStream_t s) {
+void normalise(const T* g, Direction a, int64_t batch, double eps, const Steps& steps, const OrthoLayout& l,
+               cudaStream_t s) {
   a.units = a.cols / VEC;
   const int64_t n = (int64_t)a.rows * a.units, per = (int64_t)a.rows * a.cols;
   // dense matrices on 16-byte boundaries: eight elements at a time whatever the rows
@@ -1108,7 +1161,7 @@ void normalise(const T* g, Direction a, int64_t batch, double eps, const OrthoLa
   LC_LAUNCH_CHECK("k_squares");
   const unsigned blocks = (unsigned)std::min<int64_t>(ceil_div(n, 512), 1024);
   launch_pdl(k_planes<T, VEC, PLANES>, dim3(blocks, (unsigned)batch), 256, s, g, a, (const double*)l.part, (int)parts, eps,
-             l.x[0], l.ld, batch * l.x_plane, l.t, l.phases);
+             steps, l.x[0], l.ld, batch * l.x_plane, l.t, l.lift, l.phases);
   LC_LAUNCH_CHECK("k_planes");
 }
 
@@ -1129,10 +1182,11 @@ void iterate(int batch, int rows, int cols, int steps, const double* co, void* o
     const float* t = i == 0 ? l.t : nullptr;
     __half *x = l.x[i & 1], *y = l.x[(i & 1) ^ 1];
     const mma::Tensor X{x, cols, rows, (int64_t)PLANES * batch, l.ld, l.x_plane};
-    SymEpi<PLANES> gram{l.s, nullptr, l.sld, l.s_plane, sp, m, kSScale / (kXScale * kXScale), 0.f, t};
+    const float2* lift = l.lift + i;
+    SymEpi<PLANES> gram{l.s, nullptr, l.sld, l.s_plane, sp, m, kSScale / (kXScale * kXScale), 0.f, t, lift};
     product<PLANES>(X, tall, X, tall, m, m, n, batch, true, gram, s);
     const float ps = poly_scale(b, c);
-    SymEpi<PLANES> poly{l.p, l.s, l.sld, l.s_plane, sp, m, c * ps / (kSScale * kSScale), b * ps / kSScale, nullptr};
+    SymEpi<PLANES> poly{l.p, l.s, l.sld, l.s_plane, sp, m, c * ps / (kSScale * kSScale), b * ps / kSScale, nullptr, lift};
     product<PLANES>(S, false, S, false, m, m, m, batch, true, poly, s);
     auto update = [&](auto epi) {
       if (tall)
@@ -1141,10 +1195,10 @@ void iterate(int batch, int rows, int cols, int steps, const double* co, void* o
         product<PLANES>(P, false, X, true, m, n, m, batch, false, epi, s);
     };
     if (i + 1 < steps) {
-      update(UpdateEpi<PLANES>{y, x, l.ld, l.x_plane, xp, rows, cols, 1.f / ps, a, t});
+      update(UpdateEpi<PLANES>{y, x, l.ld, l.x_plane, xp, rows, cols, 1.f / ps, a, t, lift});
     } else {
       LastEpi<PLANES, TO> e{static_cast<TO*>(st.weight ? st.out_weight : out), static_cast<const TO*>(st.weight), x,
-                            l.ld, l.x_plane, xp, rows, cols, 0, 1.f / (ps * kXScale), a / kXScale, st.keep, st.rate, t};
+                            l.ld, l.x_plane, xp, rows, cols, 0, 1.f / (ps * kXScale), a / kXScale, st.keep, st.rate, t, lift};
       e.vec = cols % 8 == 0 && ((uintptr_t)e.d & 15) == 0 && ((uintptr_t)e.w & 15) == 0;
       update(e);
     }
@@ -1173,12 +1227,14 @@ void orthogonalize(int type, const void* G, int64_t ldg, int64_t batch, int rows
   const Direction d{rows, cols, ldg, 0, 0, st};
   const bool vec = cols % 8 == 0 && ldg % 8 == 0 && ((uintptr_t)G & 15) == 0 && ((uintptr_t)st.momentum & 15) == 0 &&
                    ((uintptr_t)st.out_momentum & 15) == 0;
+  Steps poly = {steps, {}};
+  for (int i = 0; i < 3 * steps; ++i) poly.coef[i] = (float)coefficients[i];
   auto go = [&](auto g) {
     using T = std::remove_const_t<std::remove_pointer_t<decltype(g)>>;
     if (planes == 2)
-      vec ? normalise<T, 8, 2>(g, d, batch, eps, l, s) : normalise<T, 1, 2>(g, d, batch, eps, l, s);
+      vec ? normalise<T, 8, 2>(g, d, batch, eps, poly, l, s) : normalise<T, 1, 2>(g, d, batch, eps, poly, l, s);
     else
-      vec ? normalise<T, 8, 1>(g, d, batch, eps, l, s) : normalise<T, 1, 1>(g, d, batch, eps, l, s);
+      vec ? normalise<T, 8, 1>(g, d, batch, eps, poly, l, s) : normalise<T, 1, 1>(g, d, batch, eps, poly, l, s);
   };
   if (type == LIPCACHE_F32)
     go(static_cast<const float*>(G));

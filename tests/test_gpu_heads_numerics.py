@@ -8,7 +8,8 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_heads import BF16, F32, QUINTIC, UNIT, dev, f64, heads, ortho_exact, within  # noqa: E402,F401
+from test_gpu_heads import (  # noqa: E402,F401
+    BF16, F32, POLAR, QUINTIC, UNIT, check_ortho, dev, f64, heads, ortho_exact, within)
 
 
 # ---------------------------------------------------------------- the loss's precision
@@ -61,3 +62,28 @@ def test_orthogonal_step_with_beta_near_one(dev, heads, shape, gt, beta):
                 want = w.double() - 0.1 * o
                 assert float(torch.linalg.vector_norm(f64(ow) - want)) <= 0.8 * noise + 2 * UNIT[F32] * float(
                     torch.linalg.vector_norm(want)) + 1e-7
+
+
+# ---------------------------------------------------------------- norms below eps
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("batch,m,n", [(1, 40, 50), (1, 100, 130), (2, 300, 210), (5, 1030, 1100)])
+def test_orthogonalize_far_below_eps(dev, heads, dtype, batch, m, n):
+    """Norms of eps times 1 to 1e-20: the iteration keeps its precision while it
+    lifts them."""
+    gen = torch.Generator().manual_seed(m)
+    base = torch.randn(m, n, generator=gen)
+    base /= torch.linalg.vector_norm(base)
+    few = batch == 5
+    for eps in ((1e-7,) if few else (1e-7, 1.0)):
+        for ratios, steps, coef in (((1.0, 1e-2, 1e-4, 1e-7, 1e-10), 5, QUINTIC), ((0.3, 1e-3, 1e-5, 1e-12, 1e-20), 14, QUINTIC),
+                                    ((0.1, 1e-4, 1e-6, 1e-8, 1e-9), 4, [(0.5, 0.1, 0.1), POLAR, (8.0, -3.0, 1.0), (64.0, 1.0, -1.0)])):
+            if few and steps != 5:
+                continue
+            for k in range(0, len(ratios), batch):
+                r = ratios[k:k + batch]
+                g = torch.stack([base * (eps * v) for v in r]).to(dtype)
+                got = heads.orthogonalize(g.to(dev), steps=steps, coefficients=coef, eps=eps)
+                for i in range(len(r)):
+                    if few and i not in (0, 3):
+                        continue
+                    check_ortho(heads, got[i], g[i].double(), dtype, steps, coef, eps)
