@@ -195,7 +195,7 @@ template <typename T, int VEC, int PLANES>
 __global__ void __launch_bounds__(256)
     k_planes(const T* g, const Direction a, const double* part, int parts, double eps, const Steps steps, __half* x,
              int64_t ld, int64_t plane, float* t, float2* lift, unsigned* phases) {
-  __shared__ float factor;
+  __shared__ float factor[2];  // (2^-e alone can be past FP32's range)
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *phases = 0;
@@ -208,8 +208,9 @@ __global__ void __launch_bounds__(256)
       const double norm = sqrt(sum);
       int e = 0;
       frexp(norm > 0.0 ? norm : 1.0, &e);  // norm < 2^e
-      const bool fine = isfinite(norm) && e <= 126;
-      factor = fine ? ldexpf(kXScale, min(-e, 114)) : NAN;
+      const bool fine = isfinite(norm);
+      factor[0] = fine ? ldexpf(kXScale, min(-e, 100)) : NAN;
+      factor[1] = ldexpf(1.f, max(-e - 100, 0));
       if (blockIdx.x == 0) {
         lift_steps(fine ? ldexp(1.0, e) / (norm + eps) : 1.0, steps, t + blockIdx.y,
                    lift + (int64_t)blockIdx.y * LIPCACHE_MAX_NS_STEPS);
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(256)
     }
   }
   __syncthreads();
-  const float f = factor;
+  const float f = factor[0], f1 = factor[1];
   const uint32_t n = (uint32_t)a.rows * (uint32_t)a.units;
   const int64_t row0 = (int64_t)blockIdx.y * a.rows;
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(256)
     direction<T, VEC, false>(a, g, row0 + r, col, v);
     __half* d = x + (row0 + r) * ld + col;
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) v[j] *= f;  // a power of two
+    for (int j = 0; j < VEC; ++j) v[j] = v[j] * f * f1;  // powers of two
     if constexpr (VEC == 8) {
       uint32_t hi[4], lo[4];
       split_f16(v, hi, lo);

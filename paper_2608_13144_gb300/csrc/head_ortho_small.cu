@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
   extern __shared__ float4 smem4[];
   __shared__ double norm_s;
   __shared__ double red[kThreads / 32];
-  __shared__ float factor_s[2];
+  __shared__ float factor_s[3];
   float* smem = reinterpret_cast<float*>(smem4);
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -171,13 +171,15 @@ __global__ void __launch_bounds__(kThreads) k_small(const T* g, TO* out, const S
     const double norm = sqrt(sum);
     int e2 = 0;
     frexp(norm > 0.0 ? norm : 1.0, &e2);
-    const bool fine = isfinite(norm) && e2 <= 126;
-    factor_s[0] = fine ? ldexpf(1.f, min(-e2, 126)) : NAN;
-    factor_s[1] = fine ? (float)(ldexp(1.0, e2) / (norm + a.eps)) : NAN;
+    // 2^-e2 (past FP32's range for the smallest matrices, so in two), then the rest
+    const bool fine = isfinite(norm);
+    factor_s[0] = fine ? ldexpf(1.f, min(-e2, 100)) : NAN;
+    factor_s[1] = ldexpf(1.f, max(-e2 - 100, 0));
+    factor_s[2] = fine ? (float)(ldexp(1.0, e2) / (norm + a.eps)) : NAN;
   }
   __syncthreads();
-  const float f1 = factor_s[0], f2 = factor_s[1];
-  for (int e = tid; e < a.m * a.stride; e += kThreads) x[e] = x[e] * f1 * f2;
+  const float f0 = factor_s[0], f1 = factor_s[1], f2 = factor_s[2];
+  for (int e = tid; e < a.m * a.stride; e += kThreads) x[e] = x[e] * f0 * f1 * f2;
   __syncthreads();
 
   const int nb = mp / 4, tiles = nb * (nb + 1) / 2;

@@ -87,3 +87,17 @@ def test_orthogonalize_far_below_eps(dev, heads, dtype, batch, m, n):
                     if few and i not in (0, 3):
                         continue
                     check_ortho(heads, got[i], g[i].double(), dtype, steps, coef, eps)
+
+
+# ---------------------------------------------------------------- norms at the ends of the range
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(12, 40), (64, 9), (150, 90), (100, 128)])
+def test_orthogonalize_norms_at_the_ends_of_the_range(dev, heads, dtype, m, n):
+    """Matrices of the smallest and the largest finite numbers."""
+    gen = torch.Generator().manual_seed(n)
+    base = torch.randn(m, n, generator=gen)
+    for size, eps in ((1e-36, 1e-30), (1e-38, 1e-30), (1e-40, 1e-30), (2.0 ** -126, 1e-7), (1e36, 1e-7), (6e37, 1e-7), (6e37, 1.0)):
+        g = (base * size).to(dtype)
+        assert torch.isfinite(g).all()
+        got = heads.orthogonalize(g.to(dev), eps=eps)
+        check_ortho(heads, got, g.double(), dtype, 5, QUINTIC, eps)
