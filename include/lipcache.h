@@ -539,7 +539,9 @@ void lipcache_destroy(lipcache_t* h);
  *  - Tensors are LIPCACHE_F32 or LIPCACHE_BF16; sums and statistics are held
  *    in FP32 or better, and each output is rounded once. FP32 products on the
  *    tensor cores are taken as three FP16 products of operands split in two
- *    (22 bits of each operand's row or matrix maximum).
+ *    (22 bits of each operand's row or matrix maximum, at any size of the rows
+ *    of x and dy; of a head's rows down to a maximum of 2^-62, below which they
+ *    keep what 2^-84 leaves).
  *  - A bounded wait that expires on the device leaves the call's outputs
  *    undefined and is counted (lipcache_operator_errors).
  */

@@ -35,6 +35,11 @@ using mma::Tensor;
 typedef __nv_bfloat16 bf16;
 
 constexpr int kBlock = 4;  // stages of 64 the tensor cores sum before the sum is drained, FP32
+// Powers of two of FP32 rows, at most. Rows of x and dy: what FP32 can undo; their
+// smallest numbers still have the planes' bits. Rows of W: B stands beside them over the
+// same power, and so do rows of dy times its inverse, which have to stay in range; rows
+// of W below 2^-62 lose bits.
+constexpr int kRowPower = 126, kHeadPower = 60;
 
 // ---------------------------------------------------------------- copies
 // A BF16 matrix whose rows TMA cannot read, in rows of ldo: 2048 columns of a
@@ -107,12 +112,13 @@ __device__ __forceinline__ void put3(bf16* o, int64_t plane, float v) {
   }
 }
 
-// The exponent that takes the largest element of a row into [2^14, 2^15).
+// The exponent that takes the largest element of a row into [2^14, 2^15), at
+// most `most` (below, no finite row asks for less than -113).
 __device__ __forceinline__ int row_power(float top, int most) {
 #pragma unroll
   for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
   const int e = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-  return max(-most, min(most, e));
+  return min(most, e);
 }
 
 // The planes of a row; returns its factor.
@@ -726,6 +732,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1) k_shrink(const __grid_const
 template <typename T, bool EARLY = false>
 struct AdaptEpi {
   static constexpr bool kTurns = true, kEarly = EARLY;
+  static constexpr float kFar = 0x1p64f;
   T* y;
   int64_t ldy, rows;
   int cols, vec;
@@ -763,21 +770,28 @@ struct AdaptEpi {
     }
     h.odd = __any_sync(0xffffffffu, h.odd);
   }
-  __device__ __forceinline__ void odd_values(int64_t p, int col0, int left, float (&v)[32]) const {
-    const int g = __ldg(adapter + p);
-    if (g < 0 || g >= G) return;
-    const T* f = F + (int64_t)g * cols * r + col0 * f_col;
+  // Rare rows, in shared memory, a row a lane: the columns' factors, what is left of the row's
+  // (a sum times the whole of a large one may be past FP32's range before the column's), and what
+  // was set aside of the row's adapter.
+  __device__ __forceinline__ void strange(int64_t p, int col0, int left, int lane, uint32_t turn, float uc, float rest,
+                                          bool aside) const {
+    const int g = aside && p < rows ? __ldg(adapter + p) : -1;
+    const bool any = g >= 0 && g < G;
+    const T* f = any ? F + (int64_t)g * cols * r + col0 * f_col : nullptr;
 #pragma unroll 1
-    for (int k = 0; k < r; ++k) {
-      const float uk = __ldg(u + p * r + k);
+    for (int j = 0; j < 32; ++j) {
+      const uint32_t at = turn + (uint32_t)(lane * 128 + ((j >> 2 ^ (lane & 7)) << 4) + (j & 3) * 4);
+      float x;
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at) : "memory");
+      x = x * __shfl_sync(0xffffffffu, uc, j) * rest;
+      if (any && j < left) {
 #pragma unroll 1
-      for (int j = 0; j < min(left, 32); ++j) {
-        const float q = to_f32<T>(f[j * f_col + k * f_j]);
-        if (isfinite(q)) continue;
-#pragma unroll
-        for (int c = 0; c < 32; ++c)
-          if (c == j) v[c] = fmaf(uk, q, v[c]);
+        for (int k = 0; k < r; ++k) {
+          const float q = to_f32<T>(f[j * f_col + k * f_j]);
+          if (!isfinite(q)) x = fmaf(__ldg(u + p * r + k), q, x);
+        }
       }
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
     }
   }
 
@@ -904,16 +918,11 @@ struct AdaptEpi {
 #pragma unroll
     for (int i = 1; i < 4; ++i)
       if (block == i) uc = h.uc[i], bc = h.bc[i];
-    const bool strange = h.odd, after = many && u && !odd;
+    const bool after = many && u && !odd;
     float v[32];
+    const float near = sizeof(T) == 4 ? fminf(f, kFar) : f;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(acc[j]) * f;
-    if (strange) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) v[j] *= __shfl_sync(0xffffffffu, uc, j);
-      uc = 1.f;
-      if (p < rows) odd_values(p, col0, left, v);
-    }
+    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(acc[j]) * near;
     // Turned in shared memory, 16 bytes at a time, places mixed by the row: a row
     // from a thread would take a cycle for every 16 bytes, or for every element
     // where rows are not whole vectors. Scales (powers of two) and biases of the
@@ -925,6 +934,10 @@ struct AdaptEpi {
       asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (uint32_t)(lane * 128 + ((q ^ (lane & 7)) << 4))),
                    "f"(v[4 * q]), "f"(v[4 * q + 1]), "f"(v[4 * q + 2]), "f"(v[4 * q + 3])
                    : "memory");
+    if (sizeof(T) == 4 && (h.odd || __any_sync(0xffffffffu, f > kFar))) {
+      strange(p, col0, left, lane, turn, uc, f > kFar ? f / kFar : 1.f, h.odd);
+      uc = 1.f;
+    }
     __syncwarp();
     const int have = (int)min((int64_t)32, rows - row0);
     constexpr int N = 16 / sizeof(T), kLanes = 32 / N;  // columns of a lane, lanes of a row
@@ -1748,7 +1761,7 @@ struct Op {
     e.bias = bias;
     epilogue_low(e, 0, B, true);
     if constexpr (f32) {
-      RowJob jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, 60);
+      RowJob jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, kHeadPower);
       if (l.dense) {
         jw.side = B;
         jw.wide = l.wide_f;
@@ -1757,7 +1770,7 @@ struct Op {
         jw.odd = l.odd;
         e.odd = l.odd;
       }
-      run_rows(jw, planes_job(x, p.ldx, p.tokens, p.d, l.in[0], l.ld_x, l.undo_in, 100), RowJob{});
+      run_rows(jw, planes_job(x, p.ldx, p.tokens, p.d, l.in[0], l.ld_x, l.undo_in, kRowPower), RowJob{});
       const LowJob ju = low_job(d, A, 0, true);
       run_low(&ju, low ? 1 : 0);
       e.undo_row = l.undo_in;
@@ -1786,7 +1799,7 @@ struct Op {
     if constexpr (f32) {
       RowJob jw, ja, jy;
       if (dx) {
-        jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, 60);
+        jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, kHeadPower);
         if (l.dense) {
           ja = row_job(A, p.d, (int64_t)p.adapters * p.rank, p.d);
           ja.set_aside = 1;
@@ -1798,7 +1811,7 @@ struct Op {
           e.n_odd = (int)ja.rows;
         }
         run_rows(jw, ja, RowJob{});
-        jy = planes_job(dy, lddy, p.tokens, p.classes, l.in[1], l.ld_y, l.undo_in, 100);
+        jy = planes_job(dy, lddy, p.tokens, p.classes, l.in[1], l.ld_y, l.undo_in, kRowPower);
         jy.fold = l.undo_w;  // W's planes are W over these
         run_rows(jy, RowJob{}, RowJob{});
       }

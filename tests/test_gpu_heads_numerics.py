@@ -9,7 +9,8 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from test_gpu_heads import (  # noqa: E402,F401
-    BF16, F32, POLAR, QUINTIC, UNIT, check_ortho, dev, f64, heads, ortho_exact, within)
+    BF16, F32, POLAR, QUINTIC, UNIT, adapted_case, adapted_exact, check_ortho, dev, f64, heads, ortho_exact,
+    tolerance, within)
 
 
 # ---------------------------------------------------------------- the loss's precision
@@ -101,3 +102,25 @@ def test_orthogonalize_norms_at_the_ends_of_the_range(dev, heads, dtype, m, n):
         assert torch.isfinite(g).all()
         got = heads.orthogonalize(g.to(dev), eps=eps)
         check_ortho(heads, got, g.double(), dtype, 5, QUINTIC, eps)
+
+
+# ---------------------------------------------------------------- rows at the ends of the range
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 200])
+@pytest.mark.parametrize("g", [3, 80])
+@pytest.mark.parametrize("px,pw", [(118, -30), (100, 0), (0, 100), (0, 80), (-110, 30), (-100, 20), (-60, 100), (60, -40)])
+def test_adapted_rows_at_the_ends_of_the_range(dev, heads, dtype, n, g, px, pw):
+    """Rows of x, dy and W whose sizes are far from one, their products inside FP32's range."""
+    t, a, s, bias = adapted_case(dev, dtype, n, 72, 40, g, 4, "mixed", seed=11)
+    x, W = t["x"].clone(), t["W"].clone()
+    t["x"][::2] = (x[::2].float() * 2.0 ** px).to(dtype)
+    t["W"] = (W.float() * 2.0 ** pw).to(dtype)
+    t["B"] = (t["B"].float() * 2.0 ** min(pw, 0)).to(dtype)
+    y, ty = (v[0] for v in adapted_exact(t, a, s, None))
+    within(heads.adapted_logits(t["x"], t["W"], t["A"], t["B"], a, scales=s), y, tolerance(dtype, y, ty, 76), "y")
+    t["x"] = x
+    t["dy"][::2] = (t["dy"][::2].float() * 2.0 ** px).to(dtype)
+    t["A"] = (t["A"].float() * 2.0 ** min(pw, 0)).to(dtype)
+    dx, tdx = (v[1] for v in adapted_exact(t, a, s, None))
+    got = heads.adapted_logits_backward(t["dy"], t["x"], t["W"], t["A"], t["B"], a, scales=s, need_dA=False, need_dB=False)
+    within(got[0], dx, tolerance(dtype, dx, tdx, 44), "dx")
