@@ -540,8 +540,8 @@ void lipcache_destroy(lipcache_t* h);
  *    in FP32 or better, and each output is rounded once. FP32 products on the
  *    tensor cores are taken as three FP16 products of operands split in two
  *    (22 bits of each operand's row or matrix maximum, at any size of the rows
- *    of x and dy; of a head's rows down to a maximum of 2^-62, below which they
- *    keep what 2^-84 leaves).
+ *    of x and dy; of a head's rows down to a maximum of 2^-62 in gradients and
+ *    of 2^-92 in logits, with adapters times the class's largest value in B).
  *  - A bounded wait that expires on the device leaves the call's outputs
  *    undefined and is counted (lipcache_operator_errors).
  */

@@ -35,11 +35,17 @@ using mma::Tensor;
 typedef __nv_bfloat16 bf16;
 
 constexpr int kBlock = 4;  // stages of 64 the tensor cores sum before the sum is drained, FP32
-// Powers of two of FP32 rows, at most. Rows of x and dy: what FP32 can undo; their
-// smallest numbers still have the planes' bits. Rows of W: B stands beside them over the
-// same power, and so do rows of dy times its inverse, which have to stay in range; rows
-// of W below 2^-62 lose bits.
-constexpr int kRowPower = 126, kHeadPower = 60;
+// Powers of two of FP32 rows, at most. Rows of x, dy and (logits) W: what FP32 can undo;
+// the smallest numbers still have the planes' bits. Where W is contracted over its rows,
+// rows of dy are taken times the inverse, which has to leave them in range: rows of W
+// below 2^-62 lose bits there.
+constexpr int kRowPower = 126, kFoldPower = 60;
+// B set side by side stands over the power of its class's row of W: under 2^kSidePower
+// then, that sums of its products stay in range. Values of B and A that are not below
+// kAside, which a power would take out of range for the rows of other adapters too, are
+// set aside and added in the epilogue.
+constexpr int kSidePower = 92;
+constexpr float kAside = 0x1p32f;
 
 // ---------------------------------------------------------------- copies
 // A BF16 matrix whose rows TMA cannot read, in rows of ldo: 2048 columns of a
@@ -70,14 +76,14 @@ struct RowJob {
   int64_t ld = 0, rows = 0;
   int width = 0, vec = 0;       // vec: elements of a row that can be read together, 4, 2 or 1
   const float* fold = nullptr;  // a factor of each column
-  int most = 0;                 // the largest power used
+  int most = 0;                 // the largest power of two used
   __half* planes = nullptr;     // two FP16 planes under a power of two
   int64_t ldo = 0, plane = 0;
   float* undo = nullptr;        // what undoes each row's power of two
   bf16* wide = nullptr;         // three BF16 planes of what is set side by side
   const float* side = nullptr;  // nullable: B, of which row c of every adapter is set side by side in `wide`
   int64_t ldw = 0, wplane = 0;
-  int* odd = nullptr;           // whether a value set into `wide` was NaN or infinite (0 there instead)
+  int* odd = nullptr;           // whether a value set into `wide` was not below kAside (0 there instead)
 };
 constexpr int kRowJobs = 3;
 struct RowJobs {
@@ -112,18 +118,22 @@ __device__ __forceinline__ void put3(bf16* o, int64_t plane, float v) {
   }
 }
 
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, s));
+  return v;
+}
 // The exponent that takes the largest element of a row into [2^14, 2^15), at
 // most `most` (below, no finite row asks for less than -113).
 __device__ __forceinline__ int row_power(float top, int most) {
-#pragma unroll
-  for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+  top = warp_max(top);
   const int e = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
   return min(most, e);
 }
 
 // The planes of a row; returns its factor.
 template <int VEC>
-__device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int64_t row, int lane) {
+__device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int64_t row, int lane, int most) {
   constexpr int kHeld = 2;  // vectors that a lane keeps between the two passes
   auto get = [&](int i, float (&v)[VEC]) {
     if constexpr (VEC == 4) {
@@ -165,7 +175,7 @@ __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int
 #pragma unroll
     for (int q = 0; q < VEC; ++q) top = fmaxf(top, fabsf(v[q]));
   }
-  const float f = ldexpf(1.f, row_power(top, a.most));
+  const float f = ldexpf(1.f, row_power(top, most));
   __half* o = a.planes + row * a.ldo;
   auto put = [&](int i, float (&v)[VEC]) {
 #pragma unroll
@@ -213,17 +223,28 @@ __global__ void __launch_bounds__(128, 6) k_rows_f32(const __grid_constant__ Row
   for (int64_t row = (int64_t)first * 4 + (threadIdx.x >> 5); row < a.rows; row += step) {
     const float* r = a.in + row * a.ld;
     float f = 1.f;
+    int most = a.most;
+    if (a.side) {
+      float top = 0.f;
+      for (int i = lane; i < jobs.G * R; i += 32) {
+        const int h = i / R;
+        const float v = fabsf(__ldg(a.side + ((int64_t)h * a.rows + row) * R + i - h * R));
+        if (v < kAside) top = fmaxf(top, v);
+      }
+      top = warp_max(top);
+      if (top > 0.f) most = min(most, kSidePower - ilogbf(top));
+    }
     if (a.planes)
-      f = a.vec == 4   ? row_planes<4>(a, r, row, lane)
-          : a.vec == 2 ? row_planes<2>(a, r, row, lane)
-                       : row_planes<1>(a, r, row, lane);
+      f = a.vec == 4   ? row_planes<4>(a, r, row, lane, most)
+          : a.vec == 2 ? row_planes<2>(a, r, row, lane, most)
+                       : row_planes<1>(a, r, row, lane, most);
     if (a.side || a.set_aside) {
       // B of this class, over the class's power of two; or a row of A
       bool odd = false;
       for (int i = lane; i < (a.side ? jobs.G * R : a.width); i += 32) {
         const int h = i / R;
         float v = __ldg(a.side ? a.side + ((int64_t)h * a.rows + row) * R + i - h * R : r + i);
-        if (!isfinite(v)) v = 0.f, odd = true;
+        if (!(fabsf(v) < kAside)) v = 0.f, odd = true;
         put3(a.wide + row * a.ldw + i, a.wplane, v * f);
       }
       odd = __any_sync(0xffffffffu, odd);
@@ -744,8 +765,8 @@ struct AdaptEpi {
   const int32_t* adapter;
   int G, r, f_vec;
   int64_t f_col, f_j;
-  // set-aside values of a dense low-rank product (NaN and infinities of the
-  // factor), a flag for each column (n_odd = 0) or for each of n_odd rows of A
+  // set-aside values of a dense low-rank product (not below kAside, or NaN), a
+  // flag for each column (n_odd = 0) or for each of n_odd rows of A
   const int* odd;
   int n_odd;
 
@@ -788,7 +809,7 @@ struct AdaptEpi {
 #pragma unroll 1
         for (int k = 0; k < r; ++k) {
           const float q = to_f32<T>(f[j * f_col + k * f_j]);
-          if (!isfinite(q)) x = fmaf(__ldg(u + p * r + k), q, x);
+          if (!(fabsf(q) < kAside)) x = fmaf(__ldg(u + p * r + k), q, x);
         }
       }
       asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
@@ -1761,7 +1782,7 @@ struct Op {
     e.bias = bias;
     epilogue_low(e, 0, B, true);
     if constexpr (f32) {
-      RowJob jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, kHeadPower);
+      RowJob jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, kRowPower);
       if (l.dense) {
         jw.side = B;
         jw.wide = l.wide_f;
@@ -1799,7 +1820,7 @@ struct Op {
     if constexpr (f32) {
       RowJob jw, ja, jy;
       if (dx) {
-        jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, kHeadPower);
+        jw = planes_job(W, p.ldw, p.classes, p.d, l.w, l.ld_x, l.undo_w, kFoldPower);
         if (l.dense) {
           ja = row_job(A, p.d, (int64_t)p.adapters * p.rank, p.d);
           ja.set_aside = 1;

@@ -124,3 +124,34 @@ def test_adapted_rows_at_the_ends_of_the_range(dev, heads, dtype, n, g, px, pw):
     dx, tdx = (v[1] for v in adapted_exact(t, a, s, None))
     got = heads.adapted_logits_backward(t["dy"], t["x"], t["W"], t["A"], t["B"], a, scales=s, need_dA=False, need_dB=False)
     within(got[0], dx, tolerance(dtype, dx, tdx, 44), "dx")
+
+
+# ---------------------------------------------------------------- huge factors
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [4, 300])
+@pytest.mark.parametrize("size,pw", [(3.39e38, 0), (2.0 ** 75, -70), (2.0 ** 66, -40)])
+def test_adapted_large_factors_stay_apart(dev, heads, dtype, n, size, pw):
+    """Huge finite values in one adapter reach the outputs of its rows, and no other."""
+    t, a, s, _ = adapted_case(dev, dtype, n, 136, 88, 3, 8, "mixed", seed=9)
+    a[:3] = torch.tensor([0, 1, -1], dtype=torch.int32)
+    t["W"][5] = (t["W"][5].float() * 2.0 ** pw).to(dtype)
+    clean = heads.adapted_logits(t["x"], t["W"], t["A"], t["B"], a, scales=s)
+    back = heads.adapted_logits_backward(t["dy"], t["x"], t["W"], t["A"], t["B"], a, scales=s)
+    A, B = t["A"].clone(), t["B"].clone()
+    B[0, 5] = size
+    A[0, :, 7] = size
+    other = (a != 0).to(dev)
+    got = heads.adapted_logits(t["x"], t["W"], t["A"], B, a, scales=s)
+    assert torch.equal(got[other], clean[other])
+    keep = torch.arange(88, device=dev) != 5
+    assert torch.equal(got[:, keep], clean[:, keep])
+    dx, dA, dB = heads.adapted_logits_backward(t["dy"], t["x"], t["W"], A, t["B"], a, scales=s)
+    assert torch.equal(dx[other], back[0][other]) and torch.equal(dA, back[1]) and torch.equal(dB[1:], back[2][1:])
+    keep = torch.arange(136, device=dev) != 7
+    assert torch.equal(dx[:, keep], back[0][:, keep])
+    # and there, where FP32 holds it, the product itself
+    t2 = dict(t, B=B)
+    y, ty = (v[0] for v in adapted_exact(t2, a, s, None))
+    y, ty, got = y[:, 5], ty[:, 5], f64(got[:, 5])
+    fits = ty < 2.0 ** 127
+    within(got[fits], y[fits], tolerance(dtype, y, ty, 144)[fits], "y")
