@@ -127,7 +127,7 @@ __device__ __forceinline__ float warp_max(float v) {
 // most `most` (below, no finite row asks for less than -113).
 __device__ __forceinline__ int row_power(float top, int most) {
   top = warp_max(top);
-  const int e = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
+  const int e = top > 0.f ? 14 - ilogbf(top) : 0;
   return min(most, e);
 }
 
@@ -155,6 +155,8 @@ __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int
       }
     }
   };
+  // (infinities leave the others of their row their bits)
+  auto size = [](float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.f; };
   float held[kHeld][VEC];
   float top = 0.f;
 #pragma unroll
@@ -167,13 +169,13 @@ __device__ __forceinline__ float row_planes(const RowJob& a, const float* r, int
 #pragma unroll
   for (int k = 0; k < kHeld; ++k)
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) top = fmaxf(top, fabsf(held[k][q]));
+    for (int q = 0; q < VEC; ++q) top = fmaxf(top, size(held[k][q]));
 #pragma unroll 4
   for (int i = (kHeld * 32 + lane) * VEC; i < a.width; i += 32 * VEC) {
     float v[VEC];
     get(i, v);
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) top = fmaxf(top, fabsf(v[q]));
+    for (int q = 0; q < VEC; ++q) top = fmaxf(top, size(v[q]));
   }
   const float f = ldexpf(1.f, row_power(top, most));
   __half* o = a.planes + row * a.ldo;

@@ -3,6 +3,8 @@ numbers far from one, non-finite values and their neighbours, what a caller is
 told. Same 64-bit forms as test_gpu_heads.py; tolerances are derived at each
 test.
 """
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -155,3 +157,24 @@ def test_adapted_large_factors_stay_apart(dev, heads, dtype, n, size, pw):
     y, ty, got = y[:, 5], ty[:, 5], f64(got[:, 5])
     fits = ty < 2.0 ** 127
     within(got[fits], y[fits], tolerance(dtype, y, ty, 144)[fits], "y")
+
+
+# ---------------------------------------------------------------- a head that is not finite
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [4, 300])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_adapted_non_finite_head_stays_in_its_places(dev, heads, dtype, n, bad):
+    """An infinity or a NaN in W reaches its class's logits and its feature's gradient, and no other."""
+    t, a, s, _ = adapted_case(dev, dtype, n, 72, 40, 3, 4, "mixed", seed=13)
+    t["W"] = (t["W"].float() * 2.0 ** -30).to(dtype)
+    t["A"] = (t["A"].float() * 2.0 ** -30).to(dtype)
+    want = [v[:2] for v in adapted_exact(t, a, s, None)]
+    W = t["W"].clone()
+    W[3, 9] = bad
+    y = heads.adapted_logits(t["x"], W, t["A"], t["B"], a, scales=s)
+    dx = heads.adapted_logits_backward(t["dy"], t["x"], W, t["A"], t["B"], a, scales=s, need_dA=False, need_dB=False)[0]
+    for got, k, K, at in ((y, 0, 76, 3), (dx, 1, 44, 9)):
+        assert not torch.isfinite(got[:, at]).any()
+        w, terms = want[0][k], want[1][k]
+        keep = torch.arange(w.shape[1]) != at
+        within(got[:, keep.to(dev)], w[:, keep], tolerance(dtype, w, terms, K)[:, keep], str(k))
