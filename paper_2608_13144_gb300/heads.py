@@ -10,7 +10,9 @@ marshalling only; include/lipcache.h states the formulas).
 Tensors are float32 or bfloat16 on one GPU; the work runs on the current
 stream. Rows may be strided (a slice of a wider matrix); other layouts are
 copied first. Scratch comes from PyTorch's allocator, so calls can be captured
-into a CUDA graph.
+into a CUDA graph. Autograd does not see the operators: gradients are what
+adapted_logits_backward and cross_entropy return, and a tensor that requires
+gradients is refused while they are recorded (call under torch.no_grad()).
 """
 from __future__ import annotations
 
@@ -29,6 +31,7 @@ TYPES = {torch.float32: _lib.F32, torch.bfloat16: _lib.BF16}
 QUINTIC = (3.4445, -4.7750, 2.0315)
 
 I32, F32 = torch.int32, torch.float32
+_grads = torch.is_grad_enabled
 #: struct lipcache_adapted, packed: half the time of filling ctypes' Adapted
 _ADAPTED = struct.Struct("@6i9q")
 assert _ADAPTED.size == C.sizeof(Adapted)
@@ -60,6 +63,13 @@ def _check(t: torch.Tensor, name: str, dims: int, at: int, dtype: torch.dtype) -
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     raise ValueError(f"{name} must have {dims} dimensions, not {t.dim()}")
+
+
+def _recorded(**named) -> None:
+    """Refuses the tensor that asks for gradients which autograd would not find."""
+    for name, t in named.items():
+        if t is not None and t.requires_grad:
+            raise ValueError(f"{name} requires gradients, which autograd does not record here: call under torch.no_grad()")
 
 
 def _gpu(t: torch.Tensor, name: str) -> int:
@@ -107,6 +117,9 @@ def _describe(x, W, A, B, adapter, scales, backward):
         for t, name, dims, dtype in ((x, "x", 2, dt), (W, "W", 2, dt), (A, "A", 3, dt), (B, "B", 3, dt),
                                      (adapter, "adapter", 1, I32)):
             _check(t, name, dims, at, dtype)
+    if _grads() and (x.requires_grad or W.requires_grad or A.requires_grad or B.requires_grad
+                    or scales is not None and scales.requires_grad):
+        _recorded(x=x, W=W, A=A, B=B, scales=scales)
     (n, d), (classes, wide), (G, r, da) = x.shape, W.shape, A.shape
     if wide != d or da != d or B.shape != (G, classes, r) or len(adapter) != n:
         raise ValueError("x must be n x d, W C x d, A G x r x d, B G x C x r and adapter must have n entries")
@@ -135,6 +148,8 @@ def adapted_logits(x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
     p, n, _, classes, ws, at, device, keep = _describe(x, W, A, B, adapter, scales, 0)
     if bias is not None:
         _check(bias, "bias", 1, at, F32)
+        if bias.requires_grad and _grads():
+            _recorded(bias=bias)
         if len(bias) != classes:
             raise ValueError("bias must have C entries")
         bias = bias.contiguous()
@@ -142,6 +157,8 @@ def adapted_logits(x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
         out, ldy = torch.empty(n, classes, dtype=x.dtype, device=device), classes
     else:
         _check(out, "out", 2, at, x.dtype)
+        if out.requires_grad and _grads():
+            _recorded(out=out)
         rows, ldy = _rows(out)
         if out.shape != (n, classes) or rows is not out:
             raise ValueError("out must be n x C with dense rows")
@@ -158,6 +175,8 @@ def adapted_logits_backward(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, 
     p, n, d, classes, ws, at, device, keep = _describe(x, W, A, B, adapter, scales, 1)
     dt = x.dtype
     _check(dy, "dy", 2, at, dt)
+    if dy.requires_grad and _grads():
+        _recorded(dy=dy)
     if dy.shape != (n, classes):
         raise ValueError("dy must be n x C")
     dy, lddy = _rows(dy)
@@ -180,6 +199,8 @@ def cross_entropy(logits: torch.Tensor, target: torch.Tensor, weight: torch.Tens
     ty, at, dt = _type(logits, "logits"), _gpu(logits, "logits"), logits.dtype
     _check(logits, "logits", 2, at, dt)
     _check(target, "target", 1, at, I32)
+    if _grads() and (logits.requires_grad or weight is not None and weight.requires_grad):
+        _recorded(logits=logits, weight=weight)
     n, c = logits.shape
     if len(target) != n:
         raise ValueError("target must have an entry per row of logits")
@@ -237,6 +258,8 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=QUINTIC, eps: fl
     coefficients: (a, b, c), or a triple for each step."""
     ty = _type(G, "G")
     at, device = _gpu(G, "G"), G.device
+    if _grads() and (G.requires_grad or out is not None and out.requires_grad):
+        _recorded(G=G, out=out)
     batch, m, n = _matrices(G, "G")
     coef = _polynomials(coefficients, steps)
     # rows of any stride, as long as the matrices follow one another in it
@@ -270,6 +293,9 @@ def orthogonal_step(weight: torch.Tensor, grad: torch.Tensor, momentum: torch.Te
     wt, gt, at = _type(weight, "weight"), _type(grad, "grad"), _gpu(weight, "weight")
     batch, m, n = _matrices(weight, "weight")
     ow, om = (weight, momentum) if out is None else out
+    if _grads() and (weight.requires_grad or grad.requires_grad or momentum.requires_grad or ow.requires_grad
+                    or om.requires_grad):
+        _recorded(**{"weight": weight, "grad": grad, "momentum": momentum, "out[0]": ow, "out[1]": om})
     shape, dims = weight.shape, weight.dim()
     for t, name, dtype in ((weight, "weight", weight.dtype), (grad, "grad", grad.dtype),
                            (momentum, "momentum", F32), (ow, "out[0]", weight.dtype),

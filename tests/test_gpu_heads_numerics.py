@@ -178,3 +178,40 @@ def test_adapted_non_finite_head_stays_in_its_places(dev, heads, dtype, n, bad):
         w, terms = want[0][k], want[1][k]
         keep = torch.arange(w.shape[1]) != at
         within(got[:, keep.to(dev)], w[:, keep], tolerance(dtype, w, terms, K)[:, keep], str(k))
+
+
+# ---------------------------------------------------------------- autograd
+def test_tensors_that_require_gradients(dev, heads):
+    x, W = torch.randn(4, 16, device=dev), torch.randn(8, 16, device=dev)
+    A, B = torch.randn(2, 3, 16, device=dev), torch.randn(2, 8, 3, device=dev)
+    ids = torch.zeros(4, dtype=torch.int32, device=dev)
+    bias, scales, dy = torch.randn(8, device=dev), torch.rand(2, device=dev), torch.randn(4, 8, device=dev)
+    named = dict(x=x, W=W, A=A, B=B, bias=bias, scales=scales)
+    heads.adapted_logits(adapter=ids, **named)
+    for name, t in named.items():
+        leaf = dict(named, **{name: t.clone().requires_grad_()})
+        with pytest.raises(ValueError, match=name):
+            heads.adapted_logits(adapter=ids, **leaf)
+        with torch.no_grad():
+            heads.adapted_logits(adapter=ids, **leaf)
+        if name != "bias":
+            leaf.pop("bias")
+            with pytest.raises(ValueError, match=name):
+                heads.adapted_logits_backward(dy, adapter=ids, **leaf)
+    with pytest.raises(ValueError, match="out"):
+        heads.adapted_logits(adapter=ids, out=torch.empty(4, 8, device=dev).requires_grad_(), **named)
+    with pytest.raises(ValueError, match="dy"):
+        heads.adapted_logits_backward(dy.clone().requires_grad_(), x, W, A, B, ids)
+    with pytest.raises(ValueError, match="logits"):
+        heads.cross_entropy(x.clone().requires_grad_(), ids)
+    with pytest.raises(ValueError, match="weight"):
+        heads.cross_entropy(x, ids, torch.ones(4, device=dev).requires_grad_())
+    with pytest.raises(ValueError, match="G"):
+        heads.orthogonalize(x.clone().requires_grad_())
+    for k in range(3):
+        args = [x.clone(), x.clone(), x.clone()]
+        args[k].requires_grad_()
+        with pytest.raises(ValueError):
+            heads.orthogonal_step(*args, 0.1)
+        with torch.no_grad():
+            heads.orthogonal_step(*args, 0.1)
