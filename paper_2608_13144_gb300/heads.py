@@ -32,6 +32,8 @@ QUINTIC = (3.4445, -4.7750, 2.0315)
 
 I32, F32 = torch.int32, torch.float32
 _grads = torch.is_grad_enabled
+#: tells autograd that tensors were written to, so that a gradient that needs the old values raises
+_written = torch.autograd.graph.increment_version
 #: struct lipcache_adapted, packed: half the time of filling ctypes' Adapted
 _ADAPTED = struct.Struct("@6i9q")
 assert _ADAPTED.size == C.sizeof(Adapted)
@@ -153,7 +155,8 @@ def adapted_logits(x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
         if len(bias) != classes:
             raise ValueError("bias must have C entries")
         bias = bias.contiguous()
-    if out is None:
+    own = out is None
+    if own:
         out, ldy = torch.empty(n, classes, dtype=x.dtype, device=device), classes
     else:
         _check(out, "out", 2, at, x.dtype)
@@ -164,6 +167,8 @@ def adapted_logits(x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
             raise ValueError("out must be n x C with dense rows")
     _call(at, _lib.load().lipcache_adapted_logits, p, None if bias is None else bias.data_ptr(), out.data_ptr(), ldy,
           ws.data_ptr(), ws.numel())
+    if not own:
+        _written(out)
     return out
 
 
@@ -220,6 +225,8 @@ def cross_entropy(logits: torch.Tensor, target: torch.Tensor, weight: torch.Tens
         dz, ldd = (z, ldz) if in_place else (torch.empty(n, c, dtype=dt, device=device), c)
     _call(at, _lib.load().lipcache_cross_entropy, ty, z.data_ptr(), ldz, n, c, target.data_ptr(),
           None if weight is None else weight.data_ptr(), loss.data_ptr(), None if dz is None else dz.data_ptr(), ldd)
+    if in_place and need_grad:
+        _written(dz)
     return loss, dz
 
 
@@ -267,7 +274,8 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=QUINTIC, eps: fl
     if not (n == 1 or G.stride(-1) == 1) or ld < n or (batch > 1 and G.stride(0) != m * ld):
         G = G.contiguous()
         ld = n
-    if out is None:
+    own = out is None
+    if own:
         out = torch.empty(G.shape, dtype=G.dtype, device=device)
     else:
         _check(out, "out", G.dim(), at, G.dtype)
@@ -276,6 +284,8 @@ def orthogonalize(G: torch.Tensor, steps: int = 5, coefficients=QUINTIC, eps: fl
     ws = _workspace(_ortho_bytes(ty, batch, m, n), device)
     _call(at, _lib.load().lipcache_orthogonalize, ty, G.data_ptr(), ld, batch, m, n, int(steps), coef, float(eps),
           out.data_ptr(), ws.data_ptr(), ws.numel())
+    if not own:
+        _written(out)
     return out
 
 
@@ -309,6 +319,7 @@ def orthogonal_step(weight: torch.Tensor, grad: torch.Tensor, momentum: torch.Te
     _call(at, _lib.load().lipcache_orthogonal_step, wt, gt, weight.data_ptr(), grad.data_ptr(), momentum.data_ptr(),
           ow.data_ptr(), om.data_ptr(), batch, m, n, float(lr), float(beta), int(bool(nesterov)), float(weight_decay),
           int(steps), coef, float(eps), ws.data_ptr(), ws.numel())
+    _written((ow, om))
     return ow, om
 
 

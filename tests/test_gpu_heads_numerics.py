@@ -215,3 +215,35 @@ def test_tensors_that_require_gradients(dev, heads):
             heads.orthogonal_step(*args, 0.1)
         with torch.no_grad():
             heads.orthogonal_step(*args, 0.1)
+
+
+# ---------------------------------------------------------------- writes in place
+def test_writes_in_place_are_seen(dev, heads):
+    """What a call overwrites counts as changed, so that a gradient that needs the old values says so."""
+    x, W = torch.randn(4, 16, device=dev), torch.randn(8, 16, device=dev)
+    A, B = torch.randn(2, 3, 16, device=dev), torch.randn(2, 8, 3, device=dev)
+    ids, out = torch.zeros(4, dtype=torch.int32, device=dev), torch.empty(4, 8, device=dev)
+    heads.adapted_logits(x, W, A, B, ids, out=out)
+    assert out._version == 1
+    heads.cross_entropy(out, ids, in_place=True)
+    assert out._version == 2
+    heads.cross_entropy(out, ids)
+    assert out._version == 2
+    o = torch.empty_like(x)
+    heads.orthogonalize(x, out=o)
+    assert o._version == 1 and x._version == 0
+    w, m, g = x.clone(), x.clone(), x.clone()
+    was = [t._version for t in (w, m, g)]
+    heads.orthogonal_step(w, g, m, 0.1)
+    assert [t._version for t in (w, m, g)] == [was[0] + 1, was[1] + 1, was[2]]
+    heads.orthogonal_step(w, g, m, 0.1, out=(o, torch.empty_like(x)))
+    assert o._version == 2 and w._version == was[0] + 1
+    leaf = torch.nn.Parameter(x.clone())
+    y = (leaf * leaf).sum()
+    with torch.no_grad():
+        heads.orthogonal_step(leaf, g, m, 0.1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    with torch.inference_mode():
+        heads.orthogonal_step(w.clone(), g, m.clone(), 0.1)
+        heads.adapted_logits(x, W, A, B, ids, out=torch.empty(4, 8, device=dev))
