@@ -92,20 +92,25 @@ def _rows(t: torch.Tensor):
 
 
 def _workspace(nbytes: int, device: torch.device) -> torch.Tensor:
-    if nbytes < 0:
-        raise LipCacheError(_lib.E_INVALID, _lib.load().lipcache_last_error().decode())
     return torch.empty(nbytes if nbytes > 256 else 256, dtype=torch.uint8, device=device)
 
 
+def _taken(nbytes: int) -> int:
+    if nbytes < 0:
+        raise LipCacheError(_lib.E_INVALID, _lib.load().lipcache_last_error().decode())
+    return nbytes
+
+
+# (sizes that are refused are asked for anew each time, for the library's message)
 @functools.lru_cache(maxsize=1024)
 def _adapted_bytes(ty: int, d: int, classes: int, G: int, r: int, n: int, backward: int) -> int:
     p = Adapted(ty, d, classes, G, r, 0, n)
-    return _lib.load().lipcache_adapted_workspace(C.byref(p), backward)
+    return _taken(_lib.load().lipcache_adapted_workspace(C.byref(p), backward))
 
 
 @functools.lru_cache(maxsize=1024)
 def _ortho_bytes(ty: int, batch: int, m: int, n: int) -> int:
-    return _lib.load().lipcache_orthogonalize_workspace(ty, batch, m, n)
+    return _taken(_lib.load().lipcache_orthogonalize_workspace(ty, batch, m, n))
 
 
 def _describe(x, W, A, B, adapter, scales, backward):

@@ -247,3 +247,17 @@ def test_writes_in_place_are_seen(dev, heads):
     with torch.inference_mode():
         heads.orthogonal_step(w.clone(), g, m.clone(), 0.1)
         heads.adapted_logits(x, W, A, B, ids, out=torch.empty(4, 8, device=dev))
+
+
+# ---------------------------------------------------------------- messages of refusals
+def test_refusals_say_why_every_time(dev, heads):
+    from paper_2608_13144_gb300 import LipCacheError
+    x, W = torch.randn(4, 16, device=dev), torch.randn(8, 16, device=dev)
+    ids = torch.zeros(4, dtype=torch.int32, device=dev)
+    for _ in range(2):
+        with pytest.raises(LipCacheError, match="rank"):
+            heads.adapted_logits(x, W, x.new_zeros(2, 129, 16), x.new_zeros(2, 8, 129), ids)
+        with pytest.raises(LipCacheError, match="rank"):
+            heads.adapted_logits_backward(x.new_zeros(4, 8), x, W, x.new_zeros(2, 129, 16), x.new_zeros(2, 8, 129), ids)
+        with pytest.raises(LipCacheError, match="rows and cols"):
+            heads.orthogonalize(x.new_zeros(0, 8))
