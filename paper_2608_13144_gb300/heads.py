@@ -237,8 +237,8 @@ def cross_entropy(logits: torch.Tensor, target: torch.Tensor, weight: torch.Tens
 
 def _polynomials(coefficients, steps: int):
     """The 3 * steps coefficients: one triple for all steps, or one a step."""
-    if isinstance(coefficients, tuple):
-        return _triples(coefficients, int(steps))
+    if type(coefficients) is tuple and all(type(c) is float or type(c) is int for c in coefficients):
+        return _triples(coefficients, int(steps))  # (numbers alone: what is in a tensor or a list can change)
     return _flat(coefficients, steps)
 
 
@@ -248,7 +248,11 @@ def _triples(coefficients: tuple, steps: int):
 
 
 def _flat(coefficients, steps: int):
-    flat = [float(v) for c in coefficients for v in (c if hasattr(c, "__len__") else (c,))]
+    flat = []
+    for c in coefficients:
+        if hasattr(c, "tolist"):
+            c = c.tolist()
+        flat += [float(v) for v in (c if hasattr(c, "__len__") else (c,))]
     if len(flat) == 3:
         flat *= max(int(steps), 0)
     if len(flat) != 3 * steps:

@@ -261,3 +261,21 @@ def test_refusals_say_why_every_time(dev, heads):
             heads.adapted_logits_backward(x.new_zeros(4, 8), x, W, x.new_zeros(2, 129, 16), x.new_zeros(2, 8, 129), ids)
         with pytest.raises(LipCacheError, match="rows and cols"):
             heads.orthogonalize(x.new_zeros(0, 8))
+
+
+# ---------------------------------------------------------------- coefficients
+def test_coefficients_of_any_sequences(dev, heads):
+    g = torch.randn(20, 30, device=dev)
+    want = heads.orthogonalize(g, steps=2, coefficients=[QUINTIC, POLAR])
+    for co in ((QUINTIC, POLAR), ([*QUINTIC], [*POLAR]), [[*QUINTIC], [*POLAR]], (*QUINTIC, *POLAR),
+               torch.tensor([QUINTIC, POLAR], dtype=torch.float64)):
+        assert torch.equal(heads.orthogonalize(g, steps=2, coefficients=co), want)
+    one = heads.orthogonalize(g, steps=2, coefficients=QUINTIC)
+    for co in ([*QUINTIC], ([*QUINTIC],), (QUINTIC,), [QUINTIC] * 2, tuple(torch.tensor(QUINTIC, dtype=torch.float64))):
+        assert torch.equal(heads.orthogonalize(g, steps=2, coefficients=co), one)
+    # numbers in tensors that change between calls
+    co = tuple(torch.tensor(v, dtype=torch.float64) for v in QUINTIC)
+    assert torch.equal(heads.orthogonalize(g, steps=2, coefficients=co), one)
+    for c, v in zip(co, POLAR):
+        c.fill_(v)
+    assert torch.equal(heads.orthogonalize(g, steps=2, coefficients=co), heads.orthogonalize(g, steps=2, coefficients=POLAR))
