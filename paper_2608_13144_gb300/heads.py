@@ -80,6 +80,12 @@ def _gpu(t: torch.Tensor, name: str) -> int:
     return t.get_device()
 
 
+def _int32(*sizes: int) -> None:
+    """Sizes that the C ABI takes as int32 (ctypes would cut larger ones off)."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError(f"sizes must be at most {0x7fffffff}, not {max(sizes)}")
+
+
 def _rows(t: torch.Tensor):
     """`t` (2-D) with neighbours in a row next to each other in memory and rows
     that do not overlap, and its row stride."""
@@ -139,8 +145,12 @@ def _describe(x, W, A, B, adapter, scales, backward):
     W, ldw = _rows(W)
     A, B, adapter = A.contiguous(), B.contiguous(), adapter.contiguous()
     ty, device = TYPES[dt], x.device
-    p = _ADAPTED.pack(ty, d, classes, G, r, 0, n, x.data_ptr(), ldx, W.data_ptr(), ldw, A.data_ptr(), B.data_ptr(),
-                      adapter.data_ptr(), 0 if scales is None else scales.data_ptr())
+    try:
+        p = _ADAPTED.pack(ty, d, classes, G, r, 0, n, x.data_ptr(), ldx, W.data_ptr(), ldw, A.data_ptr(), B.data_ptr(),
+                          adapter.data_ptr(), 0 if scales is None else scales.data_ptr())
+    except struct.error:
+        _int32(d, classes, G, r)
+        raise
     ws = _workspace(_adapted_bytes(ty, d, classes, G, r, n, backward), device)
     return p, n, d, classes, ws, at, device, (x, W, A, B, adapter, scales)
 
@@ -212,6 +222,7 @@ def cross_entropy(logits: torch.Tensor, target: torch.Tensor, weight: torch.Tens
     if _grads() and (logits.requires_grad or weight is not None and weight.requires_grad):
         _recorded(logits=logits, weight=weight)
     n, c = logits.shape
+    _int32(c)
     if len(target) != n:
         raise ValueError("target must have an entry per row of logits")
     if weight is not None:
@@ -263,6 +274,7 @@ def _flat(coefficients, steps: int):
 def _matrices(t: torch.Tensor, name: str):
     if t.dim() not in (2, 3):
         raise ValueError(f"{name} must be rows x cols or batch x rows x cols")
+    _int32(*t.shape[-2:])
     return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
 
 

@@ -279,3 +279,17 @@ def test_coefficients_of_any_sequences(dev, heads):
     for c, v in zip(co, POLAR):
         c.fill_(v)
     assert torch.equal(heads.orthogonalize(g, steps=2, coefficients=co), heads.orthogonalize(g, steps=2, coefficients=POLAR))
+
+
+# ---------------------------------------------------------------- sizes past 32 bits
+def test_sizes_past_32_bits_are_refused(dev, heads):
+    """Not cut off to their lowest 32 bits (8 classes, 8 columns here)."""
+    one = torch.zeros(1, 1, dtype=BF16, device=dev)
+    wide = one.expand(1, 2 ** 32 + 8)
+    ids = torch.zeros(1, dtype=torch.int32, device=dev)
+    none = one.new_empty(0, 1, 1)
+    for call in (lambda: heads.cross_entropy(wide, ids), lambda: heads.orthogonalize(wide),
+                 lambda: heads.orthogonal_step(wide, wide, wide, 0.1),
+                 lambda: heads.adapted_logits(wide, wide, none.expand(0, 1, 2 ** 32 + 8), none, ids)):
+        with pytest.raises(ValueError, match="2147483647"):
+            call()
