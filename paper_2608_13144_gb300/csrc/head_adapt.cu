@@ -824,8 +824,8 @@ struct AdaptEpi {
     return __uint_as_float(sizeof(T) == 4 ? w[i % 4] : i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
   // v += the row's low-rank product in 32 columns, `left` of them in the matrix
-  // (loads in groups of eight, all of a group in flight; past the matrix the
-  // last column is read again).
+  // (few rows: a factor of cols x r; loads in groups, all of a group in flight;
+  // past the matrix the last column is read again).
   __device__ __forceinline__ void low(int64_t p, int col0, int left, float (&v)[32]) const {
     constexpr int N = 16 / sizeof(T);
     const int g = __ldg(adapter + p);
@@ -833,7 +833,7 @@ struct AdaptEpi {
     const T* f = F + (int64_t)g * cols * r + col0 * f_col;
     const float* up = u + p * r;
     const int last = min(left, 32) - 1;
-    if (f_vec && f_j == 1) {
+    if (f_vec) {
       for (int k = 0; k < r; k += N) {
         float uk[N];
 #pragma unroll
@@ -849,34 +849,16 @@ struct AdaptEpi {
             for (int i = 0; i < N; ++i) v[j0 + j] = fmaf(uk[i], part(q[j], i), v[j0 + j]);
         }
       }
-    } else if (f_vec) {
-      const int end = last / N * N;  // (rows are whole vectors)
-      for (int k = 0; k < r; k += 2) {
-        const bool two = k + 1 < r;
-        const float u0 = __ldg(up + k), u1 = two ? __ldg(up + k + 1) : 0.f;
-        const T *f0 = f + k * f_j, *f1 = two ? f0 + f_j : f0;
-        uint4 q[2][32 / N];
-#pragma unroll
-        for (int j = 0; j < 32; j += N) {
-          q[0][j / N] = __ldg(reinterpret_cast<const uint4*>(f0 + min(j, end)));
-          q[1][j / N] = __ldg(reinterpret_cast<const uint4*>(f1 + min(j, end)));
-        }
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          v[j] = fmaf(u0, part(q[0][j / N], j % N), v[j]);
-          if (two) v[j] = fmaf(u1, part(q[1][j / N], j % N), v[j]);
-        }
-      }
     } else {
       for (int k = 0; k < r; ++k) {
         const float uk = __ldg(up + k);
 #pragma unroll
-        for (int j0 = 0; j0 < 32; j0 += 8) {
-          float q[8];
+        for (int j0 = 0; j0 < 32; j0 += 16) {
+          float q[16];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) q[j] = to_f32<T>(f[min(j0 + j, last) * f_col + k * f_j]);
+          for (int j = 0; j < 16; ++j) q[j] = to_f32<T>(f[min(j0 + j, last) * r + k]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[j0 + j] = fmaf(uk, q[j], v[j0 + j]);
+          for (int j = 0; j < 16; ++j) v[j0 + j] = fmaf(uk, q[j], v[j0 + j]);
         }
       }
     }
@@ -1765,19 +1747,21 @@ struct Op {
                    (int)p.d, A, vec, (int)p.adapters, (int)p.rank, p.adapter, p.scales, l.u[0]);
         LC_LAUNCH_CHECK("k_shrink_few");
       }
-      if (!f32 && tma) {
-        AdaptEpi<T, true> e = epilogue<true>(y, ldy, p.classes);
-        e.bias = bias;
-        epilogue_low(e, 0, B, true);
-        product(d, rows_of(d, 0), head(), false, 0, nullptr, false, e);
-      } else {
-        const bool wide = f32 && p.d % 4 == 0 && p.ldx % 4 == 0 && p.ldw % 4 == 0 && (((uintptr_t)x | (uintptr_t)W) & 15) == 0;
-        launch_pdl(wide ? k_rows<T, f32> : k_rows<T, false>,
-                   dim3((unsigned)ceil_div(p.classes, 16), (unsigned)ceil_div(p.tokens, 8)), 128, s, x, p.ldx, p.tokens,
-                   W, p.ldw, (int)p.classes, (int)p.d, bias, own ? (const float*)nullptr : (const float*)l.u[0], A,
-                   p.scales, B, p.adapter, (int)p.adapters, (int)p.rank, y, ldy);
-        LC_LAUNCH_CHECK("k_rows");
+      if constexpr (!f32) {
+        if (tma) {
+          AdaptEpi<T, true> e = epilogue<true>(y, ldy, p.classes);
+          e.bias = bias;
+          epilogue_low(e, 0, B, true);
+          product(d, rows_of(d, 0), head(), false, 0, nullptr, false, e);
+          return;
+        }
       }
+      const bool wide = f32 && p.d % 4 == 0 && p.ldx % 4 == 0 && p.ldw % 4 == 0 && (((uintptr_t)x | (uintptr_t)W) & 15) == 0;
+      launch_pdl(wide ? k_rows<T, f32> : k_rows<T, false>,
+                 dim3((unsigned)ceil_div(p.classes, 16), (unsigned)ceil_div(p.tokens, 8)), 128, s, x, p.ldx, p.tokens, W,
+                 p.ldw, (int)p.classes, (int)p.d, bias, own ? (const float*)nullptr : (const float*)l.u[0], A, p.scales,
+                 B, p.adapter, (int)p.adapters, (int)p.rank, y, ldy);
+      LC_LAUNCH_CHECK("k_rows");
       return;
     }
     AdaptEpi<T> e = epilogue(y, ldy, p.classes);

@@ -76,7 +76,6 @@ __device__ __forceinline__ void round_to(const float (&v)[N], uint32_t (&w)[N * 
 }
 
 inline size_t elem(int type) { return type == LIPCACHE_F32 ? 4 : 2; }
-__device__ __forceinline__ int64_t ceil_div_dev(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
