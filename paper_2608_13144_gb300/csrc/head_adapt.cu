@@ -994,8 +994,8 @@ struct AdaptEpi {
 // takes four rows of W against eight of x; VEC: four FP32 columns a load. Bound by
 // the latency of the loads in flight (4,096 x 4,096 FP32, W from memory: eight rows
 // 32 us, 2.1 TB/s; 16 rows 51, one column a load 57; 48 rows 103, 157 by ones).
-// From 64 rows on the tensor cores are level or faster (64 rows, the shape above:
-// 128 us here, 106 there; 1,024 x 1,000: 13, 25).
+// Up to 64 rows stay here: at 64 the tensor cores take 106 us for 128 at the shape
+// above, but 25 for 13 at 1,024 x 1,000.
 // u: the rows' low-rank products, or null where a block works them out itself,
 // kRowsDots of them at most (as many rows of A as the block has of W) of kRowsOwn
 // features: a launch of its own costs the host 3 us and the GPU under one, four

@@ -1,13 +1,12 @@
 // Softmax cross entropy of each row and its gradient, the logits read once:
 //   loss_t = w_t (log sum_j exp z_tj - z_ty),  dz_tj = w_t (p_tj - [j = y])
-// Bound by memory (one read of z, one write of dz). Each thread keeps a running
-// maximum and sum of its part of the row, the parts join at the end, and the
-// row's values wait in registers (a warp a row) or shared memory (a block a
-// row) for the gradient. The target stands outside the sum: 1 - p_y is the
-// others' share, without cancellation. Measured: 65,536 x 200 FP32 (a warp a row)
-// 32 us, 3.3 TB/s; 4,096 x 50,001 BF16 (a block a row) 176 us, 4.7 TB/s; both
-// issue an instruction in three clocks of four, some twenty a value, most of them
-// for the two exponentials.
+// One read of z, one write of dz. Each thread keeps a running maximum and sum of
+// its part of the row, the parts join at the end, and the row's values wait in
+// registers (a warp a row) or shared memory (a block a row) for the gradient. The
+// target stands outside the sum: 1 - p_y is the others' share, without
+// cancellation. Bound by instructions: 65,536 x 200 FP32 (a warp a row) 32 us, 3.3
+// TB/s; 4,096 x 50,001 BF16 (a block a row) 176 us, 4.7 TB/s; both issue one in
+// three clocks of four, some twenty a value, most of them for the two exponentials.
 #include "head_mma.cuh"
 
 namespace lc {
@@ -30,9 +29,8 @@ __device__ __forceinline__ float exp2_of(float x) {
 }
 constexpr float kLog2e = 1.4426950408889634f;
 
-// A granule of 16 bytes: its values as pairs of FP32, their maximum (NaN
-// ignored), and FP32 pairs put back. The kernels do some eight instructions a
-// value; at twice that they, not memory, would be the bound.
+// A granule of 16 bytes: its values as pairs of FP32 (two values an
+// instruction), their maximum (NaN ignored), and FP32 pairs put back.
 template <typename T>
 struct Vec {
   static constexpr int N = 16 / sizeof(T);

@@ -7,7 +7,8 @@ marshalling only; include/lipcache.h states the formulas).
 * orthogonalize, orthogonal_step: Newton-Schulz orthogonalisation of a
   matrix, and the optimiser step that uses it.
 
-Tensors are float32 or bfloat16 on one GPU; the work runs on the current
+Tensors are float32 or bfloat16 on one GPU, up to 65,536 features and classes
+(a cache takes float32 heads of up to 1,024); the work runs on the current
 stream. Rows may be strided (a slice of a wider matrix); other layouts are
 copied first. Scratch comes from PyTorch's allocator, so calls can be captured
 into a CUDA graph. Autograd does not see the operators: gradients are what
@@ -161,7 +162,8 @@ def adapted_logits(x: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
     """y_t = W x_t + bias + scales[g] B_g (A_g x_t), g = adapter[t].
 
     x: n x d; W: C x d; A: G x r x d; B: G x C x r; adapter: n (int32; a value
-    outside [0, G) means no adapter); bias: C (float32); scales: G (float32)."""
+    outside [0, G) means no adapter); bias: C (float32); scales: G (float32);
+    out must not overlap the other tensors."""
     p, n, _, classes, ws, at, device, keep = _describe(x, W, A, B, adapter, scales, 0)
     if bias is not None:
         _check(bias, "bias", 1, at, F32)
