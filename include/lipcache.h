@@ -523,8 +523,10 @@ void lipcache_destroy(lipcache_t* h);
  * Operators that train and serve the heads a cache certifies: logits under a
  * shared head and each row's own low-rank adapter, their gradients, the
  * cross-entropy loss, and orthogonalised optimiser steps (which keep a
- * matrix's singular values, hence sigma_max of Eq. 17, level). None needs a
- * cache handle. They share these conventions:
+ * matrix's singular values, hence sigma_max of Eq. 17, level); what a head
+ * answers with its probabilities and most probable classes, distillation from
+ * such answers of a larger model, and the layer norm of the features that a
+ * head reads. None needs a cache handle. They share these conventions:
  *
  *  - The work is enqueued on `stream` of the current device and the call
  *    returns; nothing synchronises and nothing is allocated, so calls can be
@@ -555,6 +557,9 @@ void lipcache_destroy(lipcache_t* h);
 #define LIPCACHE_MAX_TOKENS (1LL << 24)
 #define LIPCACHE_MAX_LOSS_CLASSES (1 << 24)
 #define LIPCACHE_MAX_NS_STEPS 32
+#define LIPCACHE_MAX_TOP 128           /* most probable classes of a row */
+#define LIPCACHE_MIN_TEMPERATURE 1e-3
+#define LIPCACHE_MAX_TEMPERATURE 1e3
 
 /* A shared head with low-rank adapters, and the rows it is applied to. */
 typedef struct lipcache_adapted {
@@ -629,6 +634,123 @@ lipcache_status lipcache_adapted_logits_backward(const lipcache_adapted* p, cons
 lipcache_status lipcache_cross_entropy(int32_t type, const void* logits, int64_t ldz, int64_t tokens, int32_t classes,
                                        const int32_t* target, const float* weight, float* loss, void* dlogits,
                                        int64_t ldd, lipcache_stream_t stream);
+
+/*
+ * What a head answers for each row (the prediction of Eq. 6 with its
+ * probability; no counterpart in the paper). With m = max_j z_j, T the
+ * temperature and p = softmax(z / T):
+ *   logprob  tokens FP32, nullable: log p of the row's target class; 0 where
+ *            the target is outside [0, classes), -inf for a masked one
+ *   entropy  tokens FP32, nullable: -sum_j p_j log p_j
+ *   norm     tokens x 3 FP32 dense, nullable: m, log sum_j exp((z_j - m) / T),
+ *            sum_j p_j (m - z_j) / T; what lipcache_log_probs_backward needs
+ *   top      tokens x top_k FP32 dense: log p of the most probable classes in
+ *            falling order of their logits, the lower class first among equals
+ *   index    tokens x top_k dense: those classes
+ *   type     of logits
+ *   logits   tokens x classes, row stride ldz; -inf masks a class
+ *   target   tokens, nullable where logprob is
+ *   top_k    in [0, LIPCACHE_MAX_TOP]; top and index are not read where it is 0
+ *   temperature  in [LIPCACHE_MIN_TEMPERATURE, LIPCACHE_MAX_TEMPERATURE]
+ * Masked classes are not listed: places that no class fills hold -inf and
+ * index -1. A row that is masked whole has log-probabilities -inf, entropy 0
+ * and norm (-inf, 0, 0); one with a NaN or +inf logit has NaN in all outputs
+ * (logprob of an ignored target: 0) and index -1. Results repeat bit for bit.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_log_probs(int32_t type, const void* logits, int64_t ldz, int64_t tokens, int32_t classes,
+                                   const int32_t* target, int32_t top_k, double temperature, float* logprob,
+                                   float* entropy, float* norm, float* top, int32_t* index, lipcache_stream_t stream);
+
+/*
+ * Gradient of lipcache_log_probs' logprob and entropy for the gradients g =
+ * dlogprob and h = dentropy of them (no counterpart in the paper):
+ *   dz_c = (g ([c = target] - p_c) - h p_c (log p_c + entropy)) / T
+ *   norm                tokens x 3, as lipcache_log_probs left it for these
+ *                       logits and this temperature
+ *   dlogprob, dentropy  tokens FP32, each nullable (0); dlogprob needs target
+ *   dlogits             tokens x classes, row stride ldd; may be `logits`
+ *                       itself with ldd == ldz
+ * A row whose g (0 where its target is outside [0, classes)) and h are 0 has
+ * gradient 0 whatever its logits, and so has one that is masked whole; else a
+ * NaN or +inf logit makes its row NaN.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_log_probs_backward(int32_t type, const void* logits, int64_t ldz, int64_t tokens,
+                                            int32_t classes, const float* norm, const int32_t* target,
+                                            const float* dlogprob, const float* dentropy, double temperature,
+                                            void* dlogits, int64_t ldd, lipcache_stream_t stream);
+
+/*
+ * Distillation of each row from a teacher's most probable classes, and its
+ * gradient in one call (a proxy that learns from the main model's answers; no
+ * counterpart in the paper). With q the softmax of the row's top / T over the
+ * classes it names, 0 elsewhere, and p = softmax(z / T):
+ *   loss_t  = w_t T^2 sum_j q_j (log q_j - log p_j)
+ *   dz_tc   = w_t T (p_c - q_c)
+ *   type     of logits and dlogits
+ *   logits   tokens x classes, row stride ldz; -inf masks a class
+ *   top      tokens x top_k FP32 dense: logits, or log-probabilities at
+ *            temperature 1, of the classes that index names; -inf: no share
+ *   index    tokens x top_k dense; an entry outside [0, classes) is left out;
+ *            shares of a class that is named twice add up
+ *   top_k    in [1, LIPCACHE_MAX_TOP]
+ *   weight   tokens FP32, nullable (1)
+ *   loss     tokens FP32, nullable
+ *   dlogits  tokens x classes, row stride ldd, nullable; may be `logits`
+ *            itself with ldd == ldz
+ * A row of weight 0, or whose teacher names no class with a share, has loss
+ * and gradient 0 whatever its logits. A share of a masked class gives loss
+ * +inf; a row that is masked whole has loss +inf and gradient 0; a NaN or +inf
+ * logit, or such a value of the teacher, makes its row NaN.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_distill(int32_t type, const void* logits, int64_t ldz, int64_t tokens, int32_t classes,
+                                 int32_t top_k, const float* top, const int32_t* index, const float* weight,
+                                 double temperature, float* loss, void* dlogits, int64_t ldd,
+                                 lipcache_stream_t stream);
+
+/*
+ * Layer norm of feature rows (no counterpart in the paper):
+ *   y = (x - mean) / sqrt(var + eps) * weight + bias, mean and var (1 / d) of
+ *   the row
+ *   type    of x and y
+ *   x       tokens x d, row stride ldx; d in [1, LIPCACHE_MAX_SIDE]
+ *   weight  d FP32, nullable (1)
+ *   bias    d FP32, nullable (0)
+ *   eps     in [1e-30, 1]
+ *   y       tokens x d, row stride ldy
+ *   stats   tokens x 2 FP32 dense, nullable: mean, 1 / sqrt(var + eps)
+ * A row with a NaN or an infinity comes out NaN. Rows whose squared distances
+ * from their mean sum up beyond FP32 (features above about 2^60) are outside
+ * the operator's range.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_layer_norm(int32_t type, const void* x, int64_t ldx, int64_t tokens, int32_t d,
+                                    const float* weight, const float* bias, double eps, void* y, int64_t ldy,
+                                    float* stats, lipcache_stream_t stream);
+
+/* Workspace bytes of lipcache_layer_norm_backward; -1 if the sizes are refused
+ * (no counterpart in the paper). */
+int64_t lipcache_layer_norm_workspace(int32_t type, int64_t tokens, int32_t d);
+
+/*
+ * Gradients of lipcache_layer_norm for the gradient dy of its result (no
+ * counterpart in the paper). With xh = (x - mean) rstd and g = dy weight:
+ *   dx       = rstd (g - sum g / d - xh sum(g xh) / d)   tokens x d
+ *   dweight  = sum over rows of dy xh                    d FP32
+ *   dbias    = sum over rows of dy                       d FP32
+ * Each output is nullable (then not computed; no workspace is needed without
+ * dweight and dbias).
+ *   type   of dy, x and dx (row strides lddy, ldx, lddx)
+ *   stats  tokens x 2, as lipcache_layer_norm left it
+ * Sums are taken in a fixed order: results repeat bit for bit.
+ * Errors: E_INVALID, E_CUDA.
+ */
+lipcache_status lipcache_layer_norm_backward(int32_t type, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                             int64_t tokens, int32_t d, const float* stats, const float* weight,
+                                             void* dx, int64_t lddx, float* dweight, float* dbias, void* workspace,
+                                             int64_t workspace_bytes, lipcache_stream_t stream);
 
 /* Workspace bytes of lipcache_orthogonalize and lipcache_orthogonal_step for
  * `batch` matrices of rows x cols (`type`: that of G, or of the weights); -1

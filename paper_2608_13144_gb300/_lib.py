@@ -29,7 +29,9 @@ EXPORTS = ["lipcache_create", "lipcache_set_head", "lipcache_insert", "lipcache_
            "lipcache_get_screen_info", "lipcache_insert_kernels", "lipcache_reset_stats",
            "lipcache_size", "lipcache_destroy", "lipcache_last_error",
            "lipcache_adapted_workspace", "lipcache_adapted_logits", "lipcache_adapted_logits_backward",
-           "lipcache_cross_entropy", "lipcache_orthogonalize_workspace", "lipcache_orthogonalize",
+           "lipcache_cross_entropy", "lipcache_log_probs", "lipcache_log_probs_backward", "lipcache_distill",
+           "lipcache_layer_norm", "lipcache_layer_norm_workspace", "lipcache_layer_norm_backward",
+           "lipcache_orthogonalize_workspace", "lipcache_orthogonalize",
            "lipcache_orthogonal_step", "lipcache_operator_errors"]
 
 
@@ -106,6 +108,13 @@ def load(path: str = LIB_PATH):
         "lipcache_adapted_logits": ([vp, vp, vp, i64, vp, i64, vp], C.c_int),
         "lipcache_adapted_logits_backward": ([vp, vp, i64, vp, i64, vp, vp, vp, i64, vp], C.c_int),
         "lipcache_cross_entropy": ([i32, vp, i64, i64, i32, vp, vp, vp, vp, i64, vp], C.c_int),
+        "lipcache_log_probs": ([i32, vp, i64, i64, i32, vp, i32, f64, vp, vp, vp, vp, vp, vp], C.c_int),
+        "lipcache_log_probs_backward": ([i32, vp, i64, i64, i32, vp, vp, vp, vp, f64, vp, i64, vp], C.c_int),
+        "lipcache_distill": ([i32, vp, i64, i64, i32, i32, vp, vp, vp, f64, vp, vp, i64, vp], C.c_int),
+        "lipcache_layer_norm": ([i32, vp, i64, i64, i32, vp, vp, f64, vp, i64, vp, vp], C.c_int),
+        "lipcache_layer_norm_workspace": ([i32, i64, i32], i64),
+        "lipcache_layer_norm_backward": ([i32, vp, i64, vp, i64, i64, i32, vp, vp, vp, i64, vp, vp, vp, i64, vp],
+                                         C.c_int),
         "lipcache_orthogonalize_workspace": ([i32, i64, i32, i32], i64),
         "lipcache_orthogonalize": ([i32, vp, i64, i64, i32, i32, i32, vp, f64, vp, vp, i64, vp], C.c_int),
         "lipcache_orthogonal_step": ([i32, i32, vp, vp, vp, vp, vp, i64, i32, i32, f64, f64, i32, f64, i32, vp, f64,

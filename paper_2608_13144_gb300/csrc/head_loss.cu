@@ -8,6 +8,7 @@
 // TB/s; 4,096 x 50,001 BF16 (a block a row) 176 us, 4.7 TB/s; both issue one in
 // three clocks of four, some twenty a value, most of them for the two exponentials.
 #include "head_mma.cuh"
+#include "head_rows.cuh"
 
 namespace lc {
 namespace ops {
@@ -20,64 +21,6 @@ struct LossArgs {
   const float* weight;
   float* loss;
 };
-
-// exp(x) for x <= 0 on the special function unit: 2^(x log2 e).
-__device__ __forceinline__ float exp2_of(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-constexpr float kLog2e = 1.4426950408889634f;
-
-// A granule of 16 bytes: its values as pairs of FP32 (two values an
-// instruction), their maximum (NaN ignored), and FP32 pairs put back.
-template <typename T>
-struct Vec {
-  static constexpr int N = 16 / sizeof(T);
-  __device__ static __forceinline__ void open(const uint4& w, uint64_t (&v)[N / 2]) {
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i)
-      v[i] = sizeof(T) == 4 ? ptx::pack_f32x2(x[(2 * i) & 3], x[(2 * i + 1) & 3])
-                            : ptx::pack_f32x2(x[i & 3] << 16, x[i & 3] & 0xffff0000u);
-  }
-  __device__ static __forceinline__ float top(const uint4& w) {
-    if constexpr (sizeof(T) == 4) {
-      return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
-    } else {
-      const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
-      const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
-      return fmaxf(__low2float(m), __high2float(m));
-    }
-  }
-  __device__ static __forceinline__ uint4 close(const uint64_t (&v)[N / 2]) {
-    uint32_t x[4];
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      if constexpr (sizeof(T) == 4) {
-        x[2 * i] = (uint32_t)v[i];
-        x[2 * i + 1] = (uint32_t)(v[i] >> 32);
-      } else {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float((uint32_t)v[i]), __uint_as_float((uint32_t)(v[i] >> 32)));
-        x[i] = *reinterpret_cast<const uint32_t*>(&h);
-      }
-    }
-    return uint4{x[0], x[1], x[2], x[3]};
-  }
-  // element j of a granule
-  __device__ static __forceinline__ float at(const uint4& w, int j) {
-    return to_f32<T>(reinterpret_cast<const T*>(&w)[j]);
-  }
-};
-__device__ __forceinline__ uint64_t both(float f) {
-  return ptx::pack_f32x2(__float_as_uint(f), __float_as_uint(f));
-}
-// exp(v - m) of a pair
-__device__ __forceinline__ uint64_t exp_pair(uint64_t v, uint64_t minus_m) {
-  const uint64_t x = ptx::mul_f32x2(ptx::add_f32x2(v, minus_m), both(kLog2e));
-  return ptx::pack_f32x2(__float_as_uint(exp2_of(__uint_as_float((uint32_t)x))),
-                         __float_as_uint(exp2_of(__uint_as_float((uint32_t)(x >> 32)))));
-}
 
 // The running maximum m and sum s of exp(z - m) of a set; m = -inf, s = 0:
 // empty. A NaN or +inf among the values makes s NaN.

@@ -198,6 +198,143 @@ LC_API lipcache_status lipcache_orthogonal_step(int32_t weight_type, int32_t gra
   });
 }
 
+namespace {
+
+void check_rows(int32_t type, int64_t tokens, int32_t classes, int64_t ldz) {
+  LC_ARG(known_type(type), "unknown tensor type");
+  LC_ARG(tokens >= 0 && tokens <= LIPCACHE_MAX_TOKENS, "tokens must be in [0, LIPCACHE_MAX_TOKENS]");
+  LC_ARG(classes >= 1 && classes <= LIPCACHE_MAX_LOSS_CLASSES, "classes must be in [1, LIPCACHE_MAX_LOSS_CLASSES]");
+  LC_ARG(tokens == 0 || ldz >= classes, "a row stride is smaller than the row");
+}
+void check_temperature(double t) {
+  LC_ARG(t >= LIPCACHE_MIN_TEMPERATURE && t <= LIPCACHE_MAX_TEMPERATURE,
+         "temperature must be in [LIPCACHE_MIN_TEMPERATURE, LIPCACHE_MAX_TEMPERATURE]");
+}
+// A gradient's array: null, or rows of its own, or the logits themselves.
+void check_gradient(int32_t type, const void* logits, int64_t ldz, const void* dlogits, int64_t ldd, int32_t classes) {
+  LC_ARG(dlogits == nullptr || ldd >= classes, "a row stride is smaller than the row");
+  LC_ARG(dlogits != logits || ldd == ldz, "gradients in place need the logits' row stride");
+  LC_ARG(aligned(logits, type) && aligned(dlogits, type), "a tensor is not aligned to its elements");
+}
+
+}  // namespace
+
+LC_API lipcache_status lipcache_log_probs(int32_t type, const void* logits, int64_t ldz, int64_t tokens,
+                                          int32_t classes, const int32_t* target, int32_t top_k, double temperature,
+                                          float* logprob, float* entropy, float* norm, float* top, int32_t* index,
+                                          lipcache_stream_t stream) {
+  return guarded([&] {
+    check_rows(type, tokens, classes, ldz);
+    check_temperature(temperature);
+    LC_ARG(top_k >= 0 && top_k <= LIPCACHE_MAX_TOP, "top_k must be in [0, LIPCACHE_MAX_TOP]");
+    if (tokens == 0) return;
+    LC_ARG(logits != nullptr, "NULL logits");
+    LC_ARG(logprob == nullptr || target != nullptr, "log-probabilities need a target");
+    LC_ARG(top_k == 0 || (top != nullptr && index != nullptr), "NULL top or index");
+    LC_ARG(aligned(logits, type) && aligned4(target) && aligned4(logprob) && aligned4(entropy) && aligned4(norm) &&
+               aligned4(top) && aligned4(index),
+           "a tensor is not aligned to its elements");
+    if (!logprob && !entropy && !norm && top_k == 0) return;
+    lc::ops::log_probs(type, logits, ldz, tokens, classes, target, top_k, temperature, logprob, entropy, norm, top,
+                       index, stream);
+  });
+}
+
+LC_API lipcache_status lipcache_log_probs_backward(int32_t type, const void* logits, int64_t ldz, int64_t tokens,
+                                                   int32_t classes, const float* norm, const int32_t* target,
+                                                   const float* dlogprob, const float* dentropy, double temperature,
+                                                   void* dlogits, int64_t ldd, lipcache_stream_t stream) {
+  return guarded([&] {
+    check_rows(type, tokens, classes, ldz);
+    check_temperature(temperature);
+    if (tokens == 0) return;
+    LC_ARG(logits != nullptr && norm != nullptr && dlogits != nullptr, "NULL logits, norm or dlogits");
+    LC_ARG(dlogprob == nullptr || target != nullptr, "gradients of log-probabilities need a target");
+    check_gradient(type, logits, ldz, dlogits, ldd, classes);
+    LC_ARG(aligned4(norm) && aligned4(target) && aligned4(dlogprob) && aligned4(dentropy),
+           "a tensor is not aligned to its elements");
+    lc::ops::log_probs_backward(type, logits, ldz, tokens, classes, norm, target, dlogprob, dentropy, temperature,
+                                dlogits, ldd, stream);
+  });
+}
+
+LC_API lipcache_status lipcache_distill(int32_t type, const void* logits, int64_t ldz, int64_t tokens, int32_t classes,
+                                        int32_t top_k, const float* top, const int32_t* index, const float* weight,
+                                        double temperature, float* loss, void* dlogits, int64_t ldd,
+                                        lipcache_stream_t stream) {
+  return guarded([&] {
+    check_rows(type, tokens, classes, ldz);
+    check_temperature(temperature);
+    LC_ARG(top_k >= 1 && top_k <= LIPCACHE_MAX_TOP, "top_k must be in [1, LIPCACHE_MAX_TOP]");
+    if (tokens == 0) return;
+    LC_ARG(logits != nullptr && top != nullptr && index != nullptr, "NULL logits, top or index");
+    check_gradient(type, logits, ldz, dlogits, ldd, classes);
+    LC_ARG(aligned4(top) && aligned4(index) && aligned4(weight) && aligned4(loss),
+           "a tensor is not aligned to its elements");
+    if (loss == nullptr && dlogits == nullptr) return;
+    lc::ops::distill(type, logits, ldz, tokens, classes, top_k, top, index, weight, temperature, loss, dlogits, ldd,
+                     stream);
+  });
+}
+
+namespace {
+
+void check_norm_sizes(int32_t type, int64_t tokens, int32_t d) {
+  LC_ARG(known_type(type), "unknown tensor type");
+  LC_ARG(tokens >= 0 && tokens <= LIPCACHE_MAX_TOKENS, "tokens must be in [0, LIPCACHE_MAX_TOKENS]");
+  LC_ARG(d >= 1 && d <= LIPCACHE_MAX_SIDE, "d must be in [1, LIPCACHE_MAX_SIDE]");
+}
+
+}  // namespace
+
+LC_API lipcache_status lipcache_layer_norm(int32_t type, const void* x, int64_t ldx, int64_t tokens, int32_t d,
+                                           const float* weight, const float* bias, double eps, void* y, int64_t ldy,
+                                           float* stats, lipcache_stream_t stream) {
+  return guarded([&] {
+    check_norm_sizes(type, tokens, d);
+    LC_ARG(eps >= 1e-30 && eps <= 1.0, "eps must be in [1e-30, 1]");
+    if (tokens == 0) return;
+    LC_ARG(x != nullptr && y != nullptr, "NULL x or y");
+    LC_ARG(ldx >= d && ldy >= d, "a row stride is smaller than the row");
+    LC_ARG(aligned(x, type) && aligned(y, type) && aligned4(weight) && aligned4(bias) && aligned4(stats),
+           "a tensor is not aligned to its elements");
+    lc::ops::layer_norm(type, x, ldx, tokens, d, weight, bias, eps, y, ldy, stats, stream);
+  });
+}
+
+LC_API int64_t lipcache_layer_norm_workspace(int32_t type, int64_t tokens, int32_t d) {
+  int64_t bytes = -1;
+  guarded([&] {
+    check_norm_sizes(type, tokens, d);
+    bytes = (int64_t)lc::ops::layer_norm_bytes(tokens, d);
+  });
+  return bytes;
+}
+
+LC_API lipcache_status lipcache_layer_norm_backward(int32_t type, const void* dy, int64_t lddy, const void* x,
+                                                    int64_t ldx, int64_t tokens, int32_t d, const float* stats,
+                                                    const float* weight, void* dx, int64_t lddx, float* dweight,
+                                                    float* dbias, void* workspace, int64_t workspace_bytes,
+                                                    lipcache_stream_t stream) {
+  return guarded([&] {
+    check_norm_sizes(type, tokens, d);
+    LC_ARG(aligned(dy, type) && aligned(x, type) && aligned(dx, type) && aligned4(stats) && aligned4(weight) &&
+               aligned4(dweight) && aligned4(dbias),
+           "a tensor is not aligned to its elements");
+    if (tokens == 0) {
+      if (dweight) LC_CUDA(cudaMemsetAsync(dweight, 0, (size_t)d * 4, stream));
+      if (dbias) LC_CUDA(cudaMemsetAsync(dbias, 0, (size_t)d * 4, stream));
+      return;
+    }
+    LC_ARG(dy != nullptr && x != nullptr && stats != nullptr, "NULL dy, x or stats");
+    LC_ARG(lddy >= d && ldx >= d && (dx == nullptr || lddx >= d), "a row stride is smaller than the row");
+    if (!dx && !dweight && !dbias) return;
+    if (dweight || dbias) check_workspace(workspace, workspace_bytes, lc::ops::layer_norm_bytes(tokens, d));
+    lc::ops::layer_norm_backward(type, dy, lddy, x, ldx, tokens, d, stats, weight, dx, lddx, dweight, dbias,
+                                 static_cast<unsigned char*>(workspace), stream);
+  });
+}
+
 LC_API lipcache_status lipcache_operator_errors(int64_t* count, lipcache_stream_t stream) {
   return guarded([&] {
     LC_ARG(count != nullptr, "count is NULL");

@@ -115,6 +115,24 @@ uint64_t operator_errors(cudaStream_t s);
 // head_loss.cu
 void cross_entropy(int type, const void* z, int64_t ldz, int64_t tokens, int classes, const int32_t* target,
                    const float* weight, float* loss, void* dz, int64_t ldd, cudaStream_t s);
+// head_probs.cu
+void log_probs(int type, const void* z, int64_t ldz, int64_t tokens, int classes, const int32_t* target, int k,
+               double temperature, float* logprob, float* entropy, float* norm, float* top, int32_t* index,
+               cudaStream_t s);
+void log_probs_backward(int type, const void* z, int64_t ldz, int64_t tokens, int classes, const float* norm,
+                        const int32_t* target, const float* dlogprob, const float* dentropy, double temperature,
+                        void* dz, int64_t ldd, cudaStream_t s);
+// head_distill.cu
+void distill(int type, const void* z, int64_t ldz, int64_t tokens, int classes, int k, const float* top,
+             const int32_t* index, const float* weight, double temperature, float* loss, void* dz, int64_t ldd,
+             cudaStream_t s);
+// head_norm.cu
+size_t layer_norm_bytes(int64_t tokens, int d);
+void layer_norm(int type, const void* x, int64_t ldx, int64_t tokens, int d, const float* weight, const float* bias,
+                double eps, void* y, int64_t ldy, float* stats, cudaStream_t s);
+void layer_norm_backward(int type, const void* dy, int64_t lddy, const void* x, int64_t ldx, int64_t tokens, int d,
+                         const float* stats, const float* weight, void* dx, int64_t lddx, float* dweight, float* dbias,
+                         unsigned char* ws, cudaStream_t s);
 // head_ortho.cu
 struct OrthoStep {  // what a step adds to an orthogonalisation; null weight: none
   const void* weight = nullptr;

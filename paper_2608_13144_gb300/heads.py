@@ -4,6 +4,12 @@ marshalling only; include/lipcache.h states the formulas).
 * adapted_logits, adapted_logits_backward: logits of rows under a shared head
   and each row's own low-rank adapter, and their gradients;
 * cross_entropy: per-row losses and the gradient of the logits in one call;
+* log_probs, log_probs_backward: log-probabilities of given classes, entropies
+  and the most probable classes of each row, and the gradient of the first two;
+* distill: the divergence of rows of logits from a teacher's most probable
+  classes (as log_probs returns them), and its gradient, in one call;
+* layer_norm, layer_norm_backward: layer norm of the features that a head
+  reads, and its gradients;
 * orthogonalize, orthogonal_step: Newton-Schulz orthogonalisation of a
   matrix, and the optimiser step that uses it.
 
@@ -12,7 +18,7 @@ Tensors are float32 or bfloat16 on one GPU, up to 65,536 features and classes
 stream. Rows may be strided (a slice of a wider matrix); other layouts are
 copied first. Scratch comes from PyTorch's allocator, so calls can be captured
 into a CUDA graph. Autograd does not see the operators: gradients are what
-adapted_logits_backward and cross_entropy return, and a tensor that requires
+the operators named so, cross_entropy and distill return, and a tensor that requires
 gradients is refused while they are recorded (call under torch.no_grad()).
 """
 from __future__ import annotations
@@ -20,6 +26,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import struct
+from typing import NamedTuple
 
 import torch
 
@@ -118,6 +125,11 @@ def _adapted_bytes(ty: int, d: int, classes: int, G: int, r: int, n: int, backwa
 @functools.lru_cache(maxsize=1024)
 def _ortho_bytes(ty: int, batch: int, m: int, n: int) -> int:
     return _taken(_lib.load().lipcache_orthogonalize_workspace(ty, batch, m, n))
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_bytes(ty: int, n: int, d: int) -> int:
+    return _taken(_lib.load().lipcache_layer_norm_workspace(ty, n, d))
 
 
 def _describe(x, W, A, B, adapter, scales, backward):
@@ -246,6 +258,202 @@ def cross_entropy(logits: torch.Tensor, target: torch.Tensor, weight: torch.Tens
     if in_place and need_grad:
         _written(dz)
     return loss, dz
+
+
+class LogProbs(NamedTuple):
+    """What log_probs returns; None: not asked for."""
+    logprob: torch.Tensor | None  #: n: log-probability of the target
+    entropy: torch.Tensor  #: n
+    norm: torch.Tensor  #: n x 3: what log_probs_backward needs
+    top: torch.Tensor | None  #: n x k: log-probabilities of the most probable classes
+    index: torch.Tensor | None  #: n x k (int32): those classes
+
+
+def _logits(logits: torch.Tensor, target: torch.Tensor | None):
+    """The type, device and sizes of rows of logits, and their classes' check."""
+    ty, at = _type(logits, "logits"), _gpu(logits, "logits")
+    _check(logits, "logits", 2, at, logits.dtype)
+    n, c = logits.shape
+    _int32(c)
+    if target is not None:
+        _check(target, "target", 1, at, I32)
+        if len(target) != n:
+            raise ValueError("target must have an entry per row of logits")
+        target = target.contiguous()
+    return ty, at, n, c, target
+
+
+def _per_row(t: torch.Tensor | None, name: str, n: int, at: int):
+    if t is None:
+        return None
+    _check(t, name, 1, at, F32)
+    if len(t) != n:
+        raise ValueError(f"{name} must have an entry per row")
+    return t.contiguous()
+
+
+def _gradient(logits: torch.Tensor, in_place: bool):
+    """Rows of logits, their stride, and where their gradient goes."""
+    z, ldz = _rows(logits)
+    if not in_place:
+        return z, ldz, torch.empty(logits.shape, dtype=logits.dtype, device=logits.device), logits.shape[1]
+    if z is not logits:
+        raise ValueError("in_place needs logits with dense rows")
+    return z, ldz, z, ldz
+
+
+def log_probs(logits: torch.Tensor, target: torch.Tensor | None = None, top: int = 0,
+              temperature: float = 1.0) -> LogProbs:
+    """What each row's softmax(z / temperature) says: the log-probability of its
+    target, its entropy and its `top` most probable classes, the lower class
+    first among equal logits (at most 128; masked classes, at -inf, are not
+    listed: -inf and index -1 where no class is left).
+
+    logits: n x C; target: n (int32; a value outside [0, C) has log-probability
+    0)."""
+    ty, at, n, c, target = _logits(logits, target)
+    if logits.requires_grad and _grads():
+        _recorded(logits=logits)
+    top = int(top)
+    if not 0 <= top <= 128:
+        raise ValueError("top must be in [0, 128]")
+    z, ldz = _rows(logits)
+    device, k = z.device, top > 0
+    entropy, norm = torch.empty(n, dtype=F32, device=device), torch.empty(n, 3, dtype=F32, device=device)
+    logprob = None if target is None else torch.empty(n, dtype=F32, device=device)
+    best = torch.empty(n, top, dtype=F32, device=device) if k else None
+    index = torch.empty(n, top, dtype=I32, device=device) if k else None
+    _call(at, _lib.load().lipcache_log_probs, ty, z.data_ptr(), ldz, n, c, None if target is None else target.data_ptr(),
+          top, float(temperature), None if logprob is None else logprob.data_ptr(), entropy.data_ptr(), norm.data_ptr(),
+          best.data_ptr() if k else None, index.data_ptr() if k else None)
+    return LogProbs(logprob, entropy, norm, best, index)
+
+
+def log_probs_backward(logits: torch.Tensor, norm: torch.Tensor, target: torch.Tensor | None = None,
+                       dlogprob: torch.Tensor | None = None, dentropy: torch.Tensor | None = None,
+                       temperature: float = 1.0, in_place: bool = False) -> torch.Tensor:
+    """The gradient of the logits for the gradients dlogprob and dentropy (n,
+    float32; None: 0) of log_probs' results; norm, target and temperature are
+    that call's. Overwrites logits with in_place."""
+    ty, at, n, c, target = _logits(logits, target)
+    _check(norm, "norm", 2, at, F32)
+    if _grads():
+        _recorded(logits=logits, norm=norm, dlogprob=dlogprob, dentropy=dentropy)
+    if norm.shape != (n, 3):
+        raise ValueError("norm must be n x 3")
+    if dlogprob is not None and target is None:
+        raise ValueError("dlogprob needs a target")
+    norm = norm.contiguous()
+    dlogprob, dentropy = _per_row(dlogprob, "dlogprob", n, at), _per_row(dentropy, "dentropy", n, at)
+    z, ldz, dz, ldd = _gradient(logits, in_place)
+    _call(at, _lib.load().lipcache_log_probs_backward, ty, z.data_ptr(), ldz, n, c, norm.data_ptr(),
+          None if target is None else target.data_ptr(), None if dlogprob is None else dlogprob.data_ptr(),
+          None if dentropy is None else dentropy.data_ptr(), float(temperature), dz.data_ptr(), ldd)
+    if in_place:
+        _written(dz)
+    return dz
+
+
+def distill(logits: torch.Tensor, top: torch.Tensor, index: torch.Tensor, weight: torch.Tensor | None = None,
+            temperature: float = 1.0, need_grad: bool = True, in_place: bool = False):
+    """(loss, dlogits): loss_t = weight_t T^2 sum_j q_j (log q_j - log p_j) with
+    p = softmax(z / T) and q the softmax of the teacher's top / T over the
+    classes in index, and the gradient of the losses' sum; dlogits is None
+    without need_grad, and overwrites logits with in_place.
+
+    logits: n x C; top: n x k (float32: the teacher's logits, or
+    log-probabilities at temperature 1); index: n x k (int32; an entry outside
+    [0, C) is left out, a row without any has loss 0); weight: n (float32)."""
+    ty, at, n, c, _ = _logits(logits, None)
+    _check(top, "top", 2, at, F32)
+    _check(index, "index", 2, at, I32)
+    if _grads() and (logits.requires_grad or top.requires_grad or weight is not None and weight.requires_grad):
+        _recorded(logits=logits, top=top, weight=weight)
+    k = top.shape[1]
+    if top.shape != (n, k) or index.shape != (n, k) or not 1 <= k <= 128:
+        raise ValueError("top and index must be n x k, k in [1, 128]")
+    top, index, weight = top.contiguous(), index.contiguous(), _per_row(weight, "weight", n, at)
+    dz, ldd = None, c
+    if need_grad:
+        z, ldz, dz, ldd = _gradient(logits, in_place)
+    else:
+        z, ldz = _rows(logits)
+    loss = torch.empty(n, dtype=F32, device=z.device)
+    _call(at, _lib.load().lipcache_distill, ty, z.data_ptr(), ldz, n, c, k, top.data_ptr(), index.data_ptr(),
+          None if weight is None else weight.data_ptr(), float(temperature), loss.data_ptr(),
+          dz.data_ptr() if need_grad else None, ldd)
+    if in_place and need_grad:
+        _written(dz)
+    return loss, dz
+
+
+def _columns(t: torch.Tensor | None, name: str, d: int, at: int):
+    if t is None:
+        return None
+    _check(t, name, 1, at, F32)
+    if len(t) != d:
+        raise ValueError(f"{name} must have an entry per feature")
+    return t.contiguous()
+
+
+def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+               eps: float = 1e-5, out: torch.Tensor | None = None):
+    """(y, stats): y = (x - mean) / sqrt(var + eps) * weight + bias for each row
+    of x (n x d), and the rows' mean and 1 / sqrt(var + eps) (n x 2, float32),
+    which layer_norm_backward needs. weight, bias: d (float32); out must not
+    overlap the other tensors."""
+    ty, at = _type(x, "x"), _gpu(x, "x")
+    _check(x, "x", 2, at, x.dtype)
+    n, d = x.shape
+    _int32(d)
+    if _grads():
+        _recorded(x=x, weight=weight, bias=bias, out=out)
+    weight, bias = _columns(weight, "weight", d, at), _columns(bias, "bias", d, at)
+    x, ldx = _rows(x)
+    own = out is None
+    if own:
+        out, ldy = torch.empty(n, d, dtype=x.dtype, device=x.device), d
+    else:
+        _check(out, "out", 2, at, x.dtype)
+        rows, ldy = _rows(out)
+        if out.shape != (n, d) or rows is not out:
+            raise ValueError("out must be n x d with dense rows")
+    stats = torch.empty(n, 2, dtype=F32, device=x.device)
+    _call(at, _lib.load().lipcache_layer_norm, ty, x.data_ptr(), ldx, n, d, None if weight is None else weight.data_ptr(),
+          None if bias is None else bias.data_ptr(), float(eps), out.data_ptr(), ldy, stats.data_ptr())
+    if not own:
+        _written(out)
+    return out, stats
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, weight: torch.Tensor | None = None,
+                        need_dx: bool = True, need_dweight: bool = True, need_dbias: bool = True):
+    """(dx, dweight, dbias) of layer_norm for the gradient dy (n x d) of its
+    result; stats are that call's. dx has x's type, dweight and dbias are
+    float32; an output that is not needed is None."""
+    ty, at = _type(x, "x"), _gpu(x, "x")
+    _check(x, "x", 2, at, x.dtype)
+    _check(dy, "dy", 2, at, x.dtype)
+    _check(stats, "stats", 2, at, F32)
+    n, d = x.shape
+    _int32(d)
+    if _grads():
+        _recorded(dy=dy, x=x, stats=stats, weight=weight)
+    if dy.shape != (n, d) or stats.shape != (n, 2):
+        raise ValueError("dy must be n x d and stats n x 2")
+    weight, stats = _columns(weight, "weight", d, at), stats.contiguous()
+    x, ldx = _rows(x)
+    dy, lddy = _rows(dy)
+    device = x.device
+    dx = torch.empty(n, d, dtype=x.dtype, device=device) if need_dx else None
+    dweight = torch.empty(d, dtype=F32, device=device) if need_dweight else None
+    dbias = torch.empty(d, dtype=F32, device=device) if need_dbias else None
+    ws = _workspace(_norm_bytes(ty, n, d), device)
+    _call(at, _lib.load().lipcache_layer_norm_backward, ty, dy.data_ptr(), lddy, x.data_ptr(), ldx, n, d,
+          stats.data_ptr(), None if weight is None else weight.data_ptr(), dx.data_ptr() if need_dx else None, d,
+          dweight.data_ptr() if need_dweight else None, dbias.data_ptr() if need_dbias else None, ws.data_ptr(),
+          ws.numel())
+    return dx, dweight, dbias
 
 
 def _polynomials(coefficients, steps: int):
