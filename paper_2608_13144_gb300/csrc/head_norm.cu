@@ -53,40 +53,90 @@ template <typename T, int B, int G, int P>
 struct Columns {
   static constexpr int E = B / (int)sizeof(T), U = P / E;  // values of a unit, units
   using Word = typename Unit<B>::type;
-  struct Raw {
-    Word w[U];
-  };
-  __device__ static __forceinline__ int column(int u, int rank) { return (u * G + rank) * E; }
-  __device__ static __forceinline__ Raw load(const T* p, int d, int rank) {
-    Raw r{};
+  int d, rank;
+  __device__ __forceinline__ int column(int u) const { return (u * G + rank) * E; }
+  __device__ __forceinline__ bool inside(int u) const { return column(u) < d; }
+  // f(index of a value, its column) for the thread's values
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (column(u, rank) < d) r.w[u] = *reinterpret_cast<const Word*>(p + column(u, rank));
-    return r;
+      if (inside(u)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) f(u * E + e, column(u) + e);
+      }
   }
-  __device__ static __forceinline__ void open(const Raw& r, float (&v)[P]) {
+  __device__ __forceinline__ void store(T* p, const float (&v)[P]) const {
 #pragma unroll
     for (int u = 0; u < U; ++u)
+      if (inside(u)) {
+        float part[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[u * E + e] = to_f32<T>(reinterpret_cast<const T*>(&r.w[u])[e]);
+        for (int e = 0; e < E; ++e) part[e] = v[u * E + e];
+        Word w;
+        if constexpr (sizeof(T) == 2 && E >= 2)
+          round_to<T, E>(part, reinterpret_cast<uint32_t(&)[E / 2]>(w));
+        else
+#pragma unroll
+          for (int e = 0; e < E; ++e) reinterpret_cast<T*>(&w)[e] = from_f32<T>(part[e]);
+        *reinterpret_cast<Word*>(p + column(u)) = w;
+      }
   }
-  __device__ static __forceinline__ void store(T* p, int d, int rank, const float (&v)[P]) {
+  // an FP32 array's values, `other` without one
+  __device__ __forceinline__ void floats(const float* p, float other, float (&v)[P]) const {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      Word w;
-#pragma unroll
-      for (int e = 0; e < E; ++e) reinterpret_cast<T*>(&w)[e] = from_f32<T>(v[u * E + e]);
-      if (column(u, rank) < d) *reinterpret_cast<Word*>(p + column(u, rank)) = w;
-    }
-  }
-  // an FP32 array's values at the thread's columns, `other` past d
-  __device__ static __forceinline__ void floats(const float* p, int d, int rank, float other, float (&v)[P]) {
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[u * E + e] = p && column(u, rank) < d ? __ldg(p + column(u, rank) + e) : other;
+    for (int i = 0; i < P; ++i) v[i] = other;
+    if (p) each([&](int i, int c) { v[i] = __ldg(p + c); });
   }
 };
+
+// Rows on their way to a thread: asynchronous copies of its columns into its own
+// places of a ring in shared memory, D rows ahead, or one row ahead in registers
+// (units of two bytes, which cannot be copied so).
+template <typename T, int B, int G, int P, int D>
+struct Feed {
+  using Cols = Columns<T, B, G, P>;
+  using Word = typename Cols::Word;
+  static constexpr int U = Cols::U, E = Cols::E;
+  static constexpr bool kRing = B >= 4;
+  static constexpr int kDepth = kRing ? D : 1;
+  static constexpr int kBytes = kRing ? D * P * G * (int)sizeof(T) : 0;  // of a group
+  Word* ring;
+  Word next[kRing ? 1 : U];
+  __device__ __forceinline__ void issue(const Cols& at, int slot, const T* p) {
+    if constexpr (kRing) {
+      if (p) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (at.inside(u)) {
+            const uint32_t to = ptx::smem_u32(ring + (slot * U + u) * G + at.rank);
+            if constexpr (B == 16)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p + at.column(u)) : "memory");
+            else
+              asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p + at.column(u)), "n"(B) : "memory");
+          }
+      }
+    } else if (p) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (at.inside(u)) next[u] = *reinterpret_cast<const Word*>(p + at.column(u));
+    }
+  }
+  __device__ __forceinline__ void take(const Cols& at, int slot, float (&v)[P]) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at.inside(u)) {
+        const Word w = kRing ? ring[(slot * U + u) * G + at.rank] : next[kRing ? 0 : u];
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[u * E + e] = to_f32<T>(reinterpret_cast<const T*>(&w)[e]);
+      }
+  }
+};
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 // Sums over a group of a cluster's blocks, on every thread. `turn`: this thread's
 // count of sums, whose two buffers take turns: with one barrier between, a slow
@@ -99,14 +149,17 @@ struct GroupSum {
 #pragma unroll
     for (int i = 0; i < K; ++i) v[i] = warp_sum(v[i]);
     if constexpr (G > 32) {
-      const int lane = threadIdx.x & 31;
-      if (lane == 0) {
+      if ((threadIdx.x & 31) == 0) {
 #pragma unroll
         for (int i = 0; i < K; ++i) warps[turn][i][threadIdx.x >> 5] = v[i];
       }
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < K; ++i) v[i] = warp_sum(lane < G / 32 ? warps[turn][i][lane] : 0.f);
+      for (int i = 0; i < K; ++i) {
+        v[i] = warps[turn][i][0];
+#pragma unroll
+        for (int j = 1; j < G / 32; ++j) v[i] += warps[turn][i][j];
+      }
       if constexpr (CL > 1) {
         if (threadIdx.x == 0) {
 #pragma unroll
@@ -136,56 +189,67 @@ struct GroupSum {
 template <int G>
 constexpr int kBlock = G == 32 ? 256 : G;
 
-// Whose rows a group takes: `first`, then every `step`-th; and where its columns
-// begin. A cluster of CL blocks shares a row.
-template <int G, int P, int CL>
+// Whose rows a group takes: `first`, then every `step`-th; and its columns, from
+// `base` on. A cluster of CL blocks shares a row.
+template <typename T, int B, int G, int P, int CL>
 struct Share {
   int64_t first, step;
-  int base, d, rank;
-  __device__ __forceinline__ explicit Share(int all) {
+  int base, slot;
+  Columns<T, B, G, P> cols;
+  __device__ __forceinline__ explicit Share(int d) {
     constexpr int kGroups = kBlock<G> / G;
-    const int block = (int)(blockIdx.x / CL);
-    first = (int64_t)block * kGroups + (G == 32 ? threadIdx.x >> 5 : 0);
+    slot = G == 32 ? threadIdx.x >> 5 : 0;
+    first = (int64_t)(blockIdx.x / CL) * kGroups + slot;
     step = (int64_t)(gridDim.x / CL) * kGroups;
     base = CL > 1 ? (int)ptx::cluster_ctarank() * G * P : 0;
-    d = min(max(all - base, 0), CL > 1 ? G * P : all);
-    rank = group_rank<G>();
+    cols.d = CL > 1 ? min(max(d - base, 0), G * P) : d;
+    cols.rank = group_rank<G>();
   }
 };
 
+constexpr int kNormDepth = 4, kGradDepth = 3;
+
 template <typename T, int B, int G, int P, int CL>
 __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const NormArgs a) {
-  using Cols = Columns<T, B, G, P>;
+  extern __shared__ uint4 ring_s[];
   __shared__ GroupSum<G, 1, CL> sum1;
   __shared__ GroupSum<G, 2, CL> sum2;
+  using Rows = Feed<T, B, G, P, kNormDepth>;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const Share<G, P, CL> at(a.d);
+  const Share<T, B, G, P, CL> at(a.d);
+  Rows feed;
+  feed.ring = reinterpret_cast<typename Rows::Word*>(reinterpret_cast<char*>(ring_s) + at.slot * Rows::kBytes);
+  auto row = [&](int64_t t) { return t < a.tokens ? x + t * a.ldx + at.base : nullptr; };
+#pragma unroll
+  for (int i = 0; i < Rows::kDepth; ++i) {
+    feed.issue(at.cols, i, row(at.first + i * at.step));
+    commit_copies();
+  }
   float w[P], b[P];
-  Cols::floats(a.weight ? a.weight + at.base : nullptr, at.d, at.rank, 1.f, w);
-  Cols::floats(a.bias ? a.bias + at.base : nullptr, at.d, at.rank, 0.f, b);
+  at.cols.floats(a.weight ? a.weight + at.base : nullptr, 1.f, w);
+  at.cols.floats(a.bias ? a.bias + at.base : nullptr, 0.f, b);
   const float over = 1.f / (float)a.d;
-  int turn1 = 0, turn2 = 0;
-  typename Cols::Raw next = {};
-  if (at.first < a.tokens) next = Cols::load(x + at.first * a.ldx + at.base, at.d, at.rank);
+  int turn1 = 0, turn2 = 0, slot = 0;
   for (int64_t t = at.first; t < a.tokens; t += at.step) {
     float v[P];
-    Cols::open(next, v);
-    if (t + at.step < a.tokens) next = Cols::load(x + (t + at.step) * a.ldx + at.base, at.d, at.rank);
+    wait_copies<Rows::kDepth - 1>();
+    feed.take(at.cols, slot, v);
+    feed.issue(at.cols, slot, row(t + Rows::kDepth * at.step));
+    commit_copies();
+    slot = slot + 1 == Rows::kDepth ? 0 : slot + 1;
     float s1[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < P; ++i) s1[0] += v[i];
+    at.cols.each([&](int i, int) { s1[0] += v[i]; });
     sum1(s1, turn1);
     float mean = s1[0] * over, off = mean, var = 0.f;
     // once, but for rows whose spread is lost in the first mean's rounding
-    for (int round = 0; round < 8; ++round) {
+    for (int again = 0; again < 8; ++again) {
       float s2[2] = {0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        v[i] = Cols::column(i / Cols::E, at.rank) < at.d ? v[i] - off : 0.f;
+      at.cols.each([&](int i, int) {
+        v[i] -= off;
         s2[0] += v[i];
         s2[1] += v[i] * v[i];
-      }
+      });
       sum2(s2, turn2);
       off = s2[0] * over;
       var = s2[1] * over - off * off;
@@ -193,97 +257,97 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const Norm
       mean += off;
     }
     const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + a.eps);
-    if (a.stats && at.rank == 0 && at.base == 0) {
+    if (a.stats && at.cols.rank == 0 && at.base == 0) {
       a.stats[2 * t] = mean + off;
       a.stats[2 * t + 1] = rstd;
     }
-#pragma unroll
-    for (int i = 0; i < P; ++i) v[i] = (v[i] - off) * rstd * w[i] + b[i];
-    Cols::store(y + t * a.ldy + at.base, at.d, at.rank, v);
+    at.cols.each([&](int i, int) { v[i] = (v[i] - off) * rstd * w[i] + b[i]; });
+    at.cols.store(y + t * a.ldy + at.base, v);
   }
   if (CL > 1) ptx::cluster_sync();  // (others may still read this block's sums)
 }
 
 template <typename T, int B, int G, int P, int CL>
 __global__ void __launch_bounds__(kBlock<G>) k_norm_grad(const T* dy, const T* x, T* dx, const NormArgs a) {
-  using Cols = Columns<T, B, G, P>;
   constexpr int kGroups = kBlock<G> / G;
+  extern __shared__ uint4 ring_s[];  // the rows' rings; after them G == 32's warps' columns, 2 x d each
   __shared__ GroupSum<G, 3, CL> sum;
-  extern __shared__ float cols_s[];  // G == 32: the warps' columns, 2 x d each
+  using Rows = Feed<T, B, G, P, kGradDepth>;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const Share<G, P, CL> at(a.d);
+  const Share<T, B, G, P, CL> at(a.d);
+  Rows feed_x, feed_dy;
+  feed_x.ring = reinterpret_cast<typename Rows::Word*>(reinterpret_cast<char*>(ring_s) + at.slot * 2 * Rows::kBytes);
+  feed_dy.ring = feed_x.ring + Rows::kBytes / B;
+  float2 ahead[2] = {};  // the statistics of the next two rows
+  auto issue = [&](int64_t t, int slot) {
+    const bool is = t < a.tokens;
+    feed_x.issue(at.cols, slot, is ? x + t * a.ldx + at.base : nullptr);
+    feed_dy.issue(at.cols, slot, is ? dy + t * a.lddy + at.base : nullptr);
+    commit_copies();
+  };
+  auto stats_of = [&](int64_t t) { return t < a.tokens ? float2{__ldg(a.stats + 2 * t), __ldg(a.stats + 2 * t + 1)} : float2{}; };
+#pragma unroll
+  for (int i = 0; i < Rows::kDepth; ++i) issue(at.first + i * at.step, i);
+  ahead[0] = stats_of(at.first);
+  ahead[1] = stats_of(at.first + at.step);
   float w[P], dw[P], db[P];
-  Cols::floats(a.weight ? a.weight + at.base : nullptr, at.d, at.rank, 1.f, w);
+  at.cols.floats(a.weight ? a.weight + at.base : nullptr, 1.f, w);
 #pragma unroll
   for (int i = 0; i < P; ++i) dw[i] = db[i] = 0.f;
   const float over = 1.f / (float)a.d;
-  int turn = 0;
-  typename Cols::Raw next_x = {}, next_dy = {};
-  float next_mean = 0.f, next_rstd = 0.f;
-  auto load = [&](int64_t t) {
-    if (t >= a.tokens) return;
-    next_x = Cols::load(x + t * a.ldx + at.base, at.d, at.rank);
-    next_dy = Cols::load(dy + t * a.lddy + at.base, at.d, at.rank);
-    next_mean = __ldg(a.stats + 2 * t);
-    next_rstd = __ldg(a.stats + 2 * t + 1);
-  };
-  load(at.first);
+  int turn = 0, slot = 0;
   for (int64_t t = at.first; t < a.tokens; t += at.step) {
     float v[P], g[P];
-    Cols::open(next_x, v);
-    Cols::open(next_dy, g);
-    const float mean = next_mean, rstd = next_rstd;
-    load(t + at.step);
+    wait_copies<Rows::kDepth - 1>();
+    feed_x.take(at.cols, slot, v);
+    feed_dy.take(at.cols, slot, g);
+    issue(t + Rows::kDepth * at.step, slot);
+    slot = slot + 1 == Rows::kDepth ? 0 : slot + 1;
+    const float mean = ahead[0].x, rstd = ahead[0].y;
+    ahead[0] = ahead[1];
+    ahead[1] = stats_of(t + 2 * at.step);
     float s[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      v[i] = Cols::column(i / Cols::E, at.rank) < at.d ? (v[i] - mean) * rstd : 0.f;
+    at.cols.each([&](int i, int) {
+      v[i] = (v[i] - mean) * rstd;
+      const float gw = g[i] * w[i];
       s[0] += v[i];
-      s[1] += g[i] * w[i];
-      s[2] += g[i] * w[i] * v[i];
-    }
+      s[1] += gw;
+      s[2] += gw * v[i];
+    });
     sum(s, turn);
     // xh is v less `off`, what the rounded mean leaves
     const float off = s[0] * over, mean_g = s[1] * over, mean_gx = s[2] * over - off * mean_g;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
+    at.cols.each([&](int i, int) {
       const float xh = v[i] - off;
       dw[i] += g[i] * xh;
       db[i] += g[i];
       g[i] = rstd * (g[i] * w[i] - mean_g - xh * mean_gx);
-    }
-    if (dx) Cols::store(dx + t * a.lddx + at.base, at.d, at.rank, g);
+    });
+    if (dx) at.cols.store(dx + t * a.lddx + at.base, g);
   }
   if (CL > 1) ptx::cluster_sync();
   if (!a.parts) return;
   float* out = a.parts + (int64_t)(blockIdx.x / CL) * 2 * a.d + at.base;
   if constexpr (G == 32) {
-    float* own = cols_s + (threadIdx.x >> 5) * 2 * a.d;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int c = Cols::column(i / Cols::E, at.rank) + i % Cols::E;
-      if (c < at.d) {
-        own[c] = dw[i];
-        own[a.d + c] = db[i];
-      }
-    }
+    float* all = reinterpret_cast<float*>(reinterpret_cast<char*>(ring_s) + kGroups * 2 * Rows::kBytes);
+    float* own = all + at.slot * 2 * a.d;
+    at.cols.each([&](int i, int c) {
+      own[c] = dw[i];
+      own[a.d + c] = db[i];
+    });
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * a.d; c += kBlock<G>) {
       float t = 0.f;
 #pragma unroll
-      for (int r = 0; r < kGroups; ++r) t += cols_s[r * 2 * a.d + c];
+      for (int r = 0; r < kGroups; ++r) t += all[r * 2 * a.d + c];
       out[c] = t;
     }
   } else {
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int c = Cols::column(i / Cols::E, at.rank) + i % Cols::E;
-      if (c < at.d) {
-        out[c] = dw[i];
-        out[a.d + c] = db[i];
-      }
-    }
+    at.cols.each([&](int i, int c) {
+      out[c] = dw[i];
+      out[a.d + c] = db[i];
+    });
   }
 }
 
@@ -313,11 +377,14 @@ __global__ void __launch_bounds__(512) k_norm_columns(const float* parts, int bl
   }
 }
 
-// Blocks (clusters) that take rows in turn: as many as a GB300's 152 SMs hold.
-int norm_blocks(int64_t tokens, int d) {
-  const int groups = d <= 512 ? 8 : 1;
-  const int most = d <= 2048 ? 608 : d <= 8192 ? 304 : d <= 16384 ? 76 : d <= 32768 ? 38 : 19;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(tokens, groups), most));
+// Blocks (clusters of CL) that take rows in turn: what a GB300's 152 SMs hold at once
+// of the kernel, whose rows are then dealt evenly.
+constexpr int kSms = 152, kMostOnSm = 4;
+template <typename K>
+int resident_blocks(K kernel, int threads, int smem) {
+  int n = 0;
+  LC_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, (size_t)smem));
+  return std::max(1, std::min(n, kMostOnSm)) * kSms;
 }
 
 template <int CL, typename K, typename... Args>
@@ -379,9 +446,12 @@ void launch_norm(const T* x, T* y, const NormArgs& a, cudaStream_t s) {
                          (uintptr_t)(a.d * sizeof(T));
   by_width(a.d, [&](auto g, auto p, auto cl) {
     by_alignment<T>(bits, [&](auto b) {
-      constexpr int G = decltype(g)::value, CL = decltype(cl)::value;
-      launch_cluster<CL>(k_norm<T, decltype(b)::value, G, decltype(p)::value, CL>, norm_blocks(a.tokens, a.d), kBlock<G>, 0,
-                         s, x, y, a);
+      constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value, B = decltype(b)::value;
+      constexpr int kSmem = kBlock<G> / G * Feed<T, B, G, P, kNormDepth>::kBytes;
+      if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(k_norm<T, B, G, P, CL>), kSmem);
+      static const int kResident = resident_blocks(k_norm<T, B, G, P, CL>, kBlock<G>, kSmem);
+      const int blocks = (int)std::min<int64_t>(ceil_div(a.tokens, kBlock<G> / G), kResident / CL);
+      launch_cluster<CL>(k_norm<T, B, G, P, CL>, blocks, kBlock<G>, kSmem, s, x, y, a);
     });
   });
   LC_LAUNCH_CHECK("k_norm");
@@ -392,12 +462,15 @@ void launch_norm_grad(const T* dy, const T* x, T* dx, const NormArgs& a, float* 
   const uintptr_t bits = (uintptr_t)x | (uintptr_t)dy | (uintptr_t)dx | (uintptr_t)(a.ldx * sizeof(T)) |
                          (uintptr_t)(a.lddy * sizeof(T)) | (uintptr_t)(dx ? a.lddx * sizeof(T) : 0) |
                          (uintptr_t)(a.d * sizeof(T));
-  const int blocks = norm_blocks(a.tokens, a.d);
+  int blocks = 0;
   by_width(a.d, [&](auto g, auto p, auto cl) {
     by_alignment<T>(bits, [&](auto b) {
-      constexpr int G = decltype(g)::value, CL = decltype(cl)::value;
-      launch_cluster<CL>(k_norm_grad<T, decltype(b)::value, G, decltype(p)::value, CL>, blocks, kBlock<G>,
-                         G == 32 ? 8 * 2 * a.d * 4 : 0, s, dy, x, dx, a);
+      constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value, B = decltype(b)::value;
+      constexpr int kSmem = kBlock<G> / G * (2 * Feed<T, B, G, P, kGradDepth>::kBytes + (G == 32 ? 2 * G * P * 4 : 0));
+      if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(k_norm_grad<T, B, G, P, CL>), kSmem);
+      static const int kResident = resident_blocks(k_norm_grad<T, B, G, P, CL>, kBlock<G>, kSmem);
+      blocks = (int)std::min<int64_t>(ceil_div(a.tokens, kBlock<G> / G), kResident / CL);
+      launch_cluster<CL>(k_norm_grad<T, B, G, P, CL>, blocks, kBlock<G>, kSmem, s, dy, x, dx, a);
     });
   });
   LC_LAUNCH_CHECK("k_norm_grad");
@@ -410,7 +483,7 @@ void launch_norm_grad(const T* dy, const T* x, T* dx, const NormArgs& a, float* 
 }  // namespace
 
 size_t layer_norm_bytes(int64_t tokens, int d) {
-  return tokens == 0 ? 0 : (size_t)norm_blocks(tokens, d) * 2 * d * 4;
+  return (size_t)std::min<int64_t>(tokens, kSms * kMostOnSm) * 2 * d * 4;
 }
 
 void layer_norm(int type, const void* x, int64_t ldx, int64_t tokens, int d, const float* weight, const float* bias,
