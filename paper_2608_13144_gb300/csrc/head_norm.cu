@@ -6,9 +6,9 @@
 // turn, so that weight, bias and the columns' sums stay with their thread. Columns'
 // sums are written once a block and joined by a second kernel, in a fixed order.
 //
-// Sums are taken about a first mean, and what that mean is off by is taken out
-// again: a row far from 0 loses nothing. The gradient does the same about the
-// rounded mean that it is given.
+// A row's moments are taken by warps about the warp's own mean and joined by their
+// distances, which are small: a row far from 0 loses nothing, and one barrier a row
+// is enough. The gradient takes out what the rounded mean that it is given is off by.
 #include "head_mma.cuh"
 #include "head_rows.cuh"
 
@@ -48,56 +48,125 @@ struct Unit<2> {
 };
 
 // The columns of a thread: units of B bytes, unit u at G u + rank, so that
-// neighbours read next to each other.
-template <typename T, int B, int G, int P>
+// neighbours read next to each other. Values are held in pairs, for instructions
+// that take two.
+// FULL: the row is as wide as its threads' places.
+template <typename T, int B, int G, int P, bool FULL>
 struct Columns {
   static constexpr int E = B / (int)sizeof(T), U = P / E;  // values of a unit, units
   using Word = typename Unit<B>::type;
   int d, rank;
   __device__ __forceinline__ int column(int u) const { return (u * G + rank) * E; }
-  __device__ __forceinline__ bool inside(int u) const { return column(u) < d; }
-  // f(index of a value, its column) for the thread's values
+  __device__ __forceinline__ bool inside(int u) const { return FULL || column(u) < d; }
+  // f(pair) for each pair with a column; `whole`: both have one
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (inside(u)) {
+    for (int k = 0; k < P / 2; ++k)
+      if (inside(2 * k / E)) f(k);
+  }
+  __device__ __forceinline__ bool whole(int pair) const { return E > 1 || inside(2 * pair + 1); }
+  // a pair's values, 0 for what has no column
+  __device__ __forceinline__ uint64_t masked(uint64_t v, int pair) const {
+    return whole(pair) ? v : v & 0xffffffffull;
+  }
+  // values of T, as units
+  __device__ static __forceinline__ void open(const Word& w, int u, uint64_t (&v)[P / 2]) {
+    if constexpr (E == 1) {
+      const uint32_t f = __float_as_uint(to_f32<T>(*reinterpret_cast<const T*>(&w)));
+      v[u / 2] = u & 1 ? (v[u / 2] & 0xffffffffull) | (uint64_t)f << 32 : (uint64_t)f;
+    } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) f(u * E + e, column(u) + e);
+      for (int k = 0; k < E / 2; ++k) {
+        if constexpr (sizeof(T) == 4) {
+          const uint32_t* x = reinterpret_cast<const uint32_t*>(&w) + 2 * k;
+          v[u * E / 2 + k] = ptx::pack_f32x2(x[0], x[1]);
+        } else {
+          const uint32_t x = reinterpret_cast<const uint32_t*>(&w)[k];
+          v[u * E / 2 + k] = ptx::pack_f32x2(x << 16, x & 0xffff0000u);
+        }
+      }
+    }
+  }
+  // The compiler takes units for new ones from here on.
+  __device__ static __forceinline__ void forget(Word (&w)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if constexpr (B == 16)
+        asm volatile("" : "+r"(w[u].x), "+r"(w[u].y), "+r"(w[u].z), "+r"(w[u].w));
+      else if constexpr (B == 4)
+        asm volatile("" : "+r"(w[u]));
+      else
+        asm volatile("" : "+h"(w[u]));
+    }
+  }
+  // a pair of the thread's units
+  __device__ static __forceinline__ uint64_t pair(const Word (&w)[U], int k) {
+    if constexpr (E == 1) {
+      return ptx::pack_f32x2(__float_as_uint(to_f32<T>(*reinterpret_cast<const T*>(&w[2 * k]))),
+                             __float_as_uint(to_f32<T>(*reinterpret_cast<const T*>(&w[2 * k + 1]))));
+    } else if constexpr (sizeof(T) == 4) {
+      const uint32_t* x = reinterpret_cast<const uint32_t*>(&w[2 * k / E]) + 2 * k % E;
+      return ptx::pack_f32x2(x[0], x[1]);
+    } else {
+      const uint32_t x = reinterpret_cast<const uint32_t*>(&w[2 * k / E])[k % (E / 2)];
+      return ptx::pack_f32x2(x << 16, x & 0xffff0000u);
+    }
+  }
+  // To a row: f(pair)'s values, a unit (or two of one value) at a time.
+  template <typename F>
+  __device__ __forceinline__ void put(T* p, F&& f) const {
+    constexpr int S = E > 1 ? 1 : 2;  // units of a step
+#pragma unroll
+    for (int u = 0; u < U; u += S)
+      if (inside(u)) {
+        Word w[S];
+#pragma unroll
+        for (int k = 0; k < E * S / 2; ++k) {
+          const uint64_t x = f(u * E / 2 + k);
+          if constexpr (E == 1) {
+            *reinterpret_cast<T*>(&w[0]) = from_f32<T>(lo_f32(x));
+            *reinterpret_cast<T*>(&w[1]) = from_f32<T>(hi_f32(x));
+          } else if constexpr (sizeof(T) == 4) {
+            reinterpret_cast<uint32_t*>(&w[0])[2 * k] = (uint32_t)x;
+            reinterpret_cast<uint32_t*>(&w[0])[2 * k + 1] = (uint32_t)(x >> 32);
+          } else {
+            reinterpret_cast<uint32_t*>(&w[0])[k] = pack_bf16(lo_f32(x), hi_f32(x));
+          }
+        }
+        *reinterpret_cast<Word*>(p + column(u)) = w[0];
+        if constexpr (S == 2)
+          if (inside(u + 1)) *reinterpret_cast<Word*>(p + column(u + 1)) = w[1];
       }
   }
-  __device__ __forceinline__ void store(T* p, const float (&v)[P]) const {
+  // f(value of the pair array, column) for each value
+  template <typename F>
+  __device__ __forceinline__ void each_value(const uint64_t (&v)[P / 2], F&& f) const {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (inside(u)) {
-        float part[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) part[e] = v[u * E + e];
-        Word w;
-        if constexpr (sizeof(T) == 2 && E >= 2)
-          round_to<T, E>(part, reinterpret_cast<uint32_t(&)[E / 2]>(w));
-        else
-#pragma unroll
-          for (int e = 0; e < E; ++e) reinterpret_cast<T*>(&w)[e] = from_f32<T>(part[e]);
-        *reinterpret_cast<Word*>(p + column(u)) = w;
-      }
+    for (int i = 0; i < P; ++i)
+      if (inside(i / E)) f(i & 1 ? hi_f32(v[i / 2]) : lo_f32(v[i / 2]), column(i / E) + i % E);
   }
   // an FP32 array's values, `other` without one
-  __device__ __forceinline__ void floats(const float* p, float other, float (&v)[P]) const {
+  __device__ __forceinline__ void floats(const float* p, float other, uint64_t (&v)[P / 2]) const {
 #pragma unroll
-    for (int i = 0; i < P; ++i) v[i] = other;
-    if (p) each([&](int i, int c) { v[i] = __ldg(p + c); });
+    for (int k = 0; k < P / 2; ++k) {
+      float x[2] = {other, other};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (p && inside((2 * k + h) / E)) x[h] = __ldg(p + column((2 * k + h) / E) + (2 * k + h) % E);
+      v[k] = ptx::pack_f32x2(__float_as_uint(x[0]), __float_as_uint(x[1]));
+    }
   }
 };
 
 // Rows on their way to a thread: asynchronous copies of its columns into its own
 // places of a ring in shared memory, D rows ahead, or one row ahead in registers
 // (units of two bytes, which cannot be copied so).
-template <typename T, int B, int G, int P, int D>
+template <typename T, int B, int G, int P, bool FULL, int D>
 struct Feed {
-  using Cols = Columns<T, B, G, P>;
+  using Cols = Columns<T, B, G, P, FULL>;
   using Word = typename Cols::Word;
-  static constexpr int U = Cols::U, E = Cols::E;
+  static constexpr int U = Cols::U;
   static constexpr bool kRing = B >= 4;
   static constexpr int kDepth = kRing ? D : 1;
   static constexpr int kBytes = kRing ? D * P * G * (int)sizeof(T) : 0;  // of a group
@@ -122,14 +191,13 @@ struct Feed {
         if (at.inside(u)) next[u] = *reinterpret_cast<const Word*>(p + at.column(u));
     }
   }
-  __device__ __forceinline__ void take(const Cols& at, int slot, float (&v)[P]) const {
+  __device__ __forceinline__ Word word(const Cols& at, int slot, int u) const {
+    return kRing ? ring[(slot * U + u) * G + at.rank] : next[kRing ? 0 : u];
+  }
+  __device__ __forceinline__ void take(const Cols& at, int slot, uint64_t (&v)[P / 2]) const {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (at.inside(u)) {
-        const Word w = kRing ? ring[(slot * U + u) * G + at.rank] : next[kRing ? 0 : u];
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[u * E + e] = to_f32<T>(reinterpret_cast<const T*>(&w)[e]);
-      }
+      if (at.inside(u)) Cols::open(word(at, slot, u), u, v);
   }
 };
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -138,86 +206,92 @@ __device__ __forceinline__ void wait_copies() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Sums over a group of a cluster's blocks, on every thread. `turn`: this thread's
-// count of sums, whose two buffers take turns: with one barrier between, a slow
-// thread's reading is safe from the sum after next.
-template <int G, int K, int CL>
-struct GroupSum {
-  float warps[2][K][G == 32 ? 1 : G / 32];
-  float blocks[2][K];
-  __device__ __forceinline__ void operator()(float (&v)[K], int& turn) {
+__device__ __forceinline__ float sum_of(uint64_t v) { return lo_f32(v) + hi_f32(v); }
+__device__ __forceinline__ float xor_sum(float v, int lanes) { return v + __shfl_xor_sync(kAll, v, lanes); }
+// Two sums at once over a warp: a's on lanes below 16, b's on the others.
+__device__ __forceinline__ float warp_sum2(float a, float b) {
+  const bool high = threadIdx.x & 16;
+  float v = (high ? b : a) + __shfl_xor_sync(kAll, high ? a : b, 16);
 #pragma unroll
-    for (int i = 0; i < K; ++i) v[i] = warp_sum(v[i]);
-    if constexpr (G > 32) {
-      if ((threadIdx.x & 31) == 0) {
+  for (int o = 8; o > 0; o >>= 1) v = xor_sum(v, o);
+  return v;
+}
+// Three: a's on lane 0, b's on lane 16, c's on lanes 8 and 24 (and those after them).
+__device__ __forceinline__ float warp_sum3(float a, float b, float c) {
+  const bool high = threadIdx.x & 16, odd = threadIdx.x & 8;
+  const float ab = (high ? b : a) + __shfl_xor_sync(kAll, high ? a : b, 16);
+  c = xor_sum(c, 16);
+  float v = (odd ? c : ab) + __shfl_xor_sync(kAll, odd ? ab : c, 8);
 #pragma unroll
-        for (int i = 0; i < K; ++i) warps[turn][i][threadIdx.x >> 5] = v[i];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < K; ++i) {
-        v[i] = warps[turn][i][0];
-#pragma unroll
-        for (int j = 1; j < G / 32; ++j) v[i] += warps[turn][i][j];
-      }
-      if constexpr (CL > 1) {
-        if (threadIdx.x == 0) {
-#pragma unroll
-          for (int i = 0; i < K; ++i) blocks[turn][i] = v[i];
-        }
-        ptx::cluster_sync();
-#pragma unroll
-        for (int i = 0; i < K; ++i) {
-          float s = 0.f;
-#pragma unroll
-          for (int b = 0; b < CL; ++b) {
-            float o;
-            asm volatile("ld.shared::cluster.f32 %0, [%1];"
-                         : "=f"(o)
-                         : "r"(ptx::mapa(ptx::smem_u32(&blocks[turn][i]), b))
-                         : "memory");
-            s += o;
-          }
-          v[i] = s;
-        }
-      }
-      turn ^= 1;
-    }
-  }
+  for (int o = 4; o > 0; o >>= 1) v = xor_sum(v, o);
+  return v;
+}
+
+// What joins the warps of a row, and the blocks of a cluster. Two buffers take
+// turns: with one barrier between, a slow thread's reading is safe from the join
+// after next.
+template <int G, int CL>
+struct NormShared {
+  float4 warp[2][G == 32 ? 1 : G / 32];
+  float4 block[2];
 };
+// Every block's `mine` of the cluster, in order, to f(rank, value).
+template <int CL, typename F>
+__device__ __forceinline__ void over_cluster(float4& place, const float4& mine, F&& f) {
+  if (threadIdx.x == 0) place = mine;
+  ptx::cluster_sync();
+#pragma unroll
+  for (int b = 0; b < CL; ++b) {
+    float4 o;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(o.x), "=f"(o.y), "=f"(o.z), "=f"(o.w)
+                 : "r"(ptx::mapa(ptx::smem_u32(&place), b))
+                 : "memory");
+    f(b, o);
+  }
+}
 
 template <int G>
 constexpr int kBlock = G == 32 ? 256 : G;
+// The barrier of a group of G threads among the block's GROUPS.
+template <int G, int GROUPS>
+__device__ __forceinline__ void group_barrier(int group) {
+  if constexpr (GROUPS == 1)
+    __syncthreads();
+  else
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(G) : "memory");
+}
 
 // Whose rows a group takes: `first`, then every `step`-th; and its columns, from
 // `base` on. A cluster of CL blocks shares a row.
-template <typename T, int B, int G, int P, int CL>
+template <typename T, int B, int G, int P, bool FULL, int CL, int GROUPS>
 struct Share {
   int64_t first, step;
   int base, slot;
-  Columns<T, B, G, P> cols;
+  Columns<T, B, G, P, FULL> cols;
   __device__ __forceinline__ explicit Share(int d) {
-    constexpr int kGroups = kBlock<G> / G;
-    slot = G == 32 ? threadIdx.x >> 5 : 0;
-    first = (int64_t)(blockIdx.x / CL) * kGroups + slot;
-    step = (int64_t)(gridDim.x / CL) * kGroups;
+    slot = GROUPS == 1 ? 0 : threadIdx.x / G;
+    first = (int64_t)(blockIdx.x / CL) * GROUPS + slot;
+    step = (int64_t)(gridDim.x / CL) * GROUPS;
     base = CL > 1 ? (int)ptx::cluster_ctarank() * G * P : 0;
     cols.d = CL > 1 ? min(max(d - base, 0), G * P) : d;
-    cols.rank = group_rank<G>();
+    cols.rank = threadIdx.x % G;
   }
 };
 
-constexpr int kNormDepth = 4, kGradDepth = 3;
+// Rows ahead of a group (what shared memory holds of the widest).
+template <typename T, int G, int P>
+constexpr int kNormDepth = G * P * (int)sizeof(T) > 48 * 1024 ? 3 : 4;
+constexpr int kGradDepth = 3;
 
-template <typename T, int B, int G, int P, int CL>
+template <typename T, int B, int G, int P, bool FULL, int CL>
 __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const NormArgs a) {
   extern __shared__ uint4 ring_s[];
-  __shared__ GroupSum<G, 1, CL> sum1;
-  __shared__ GroupSum<G, 2, CL> sum2;
-  using Rows = Feed<T, B, G, P, kNormDepth>;
+  __shared__ NormShared<G, CL> shared;
+  using Rows = Feed<T, B, G, P, FULL, kNormDepth<T, G, P>>;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const Share<T, B, G, P, CL> at(a.d);
+  const Share<T, B, G, P, FULL, CL, kBlock<G> / G> at(a.d);
   Rows feed;
   feed.ring = reinterpret_cast<typename Rows::Word*>(reinterpret_cast<char*>(ring_s) + at.slot * Rows::kBytes);
   auto row = [&](int64_t t) { return t < a.tokens ? x + t * a.ldx + at.base : nullptr; };
@@ -226,58 +300,113 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const Norm
     feed.issue(at.cols, i, row(at.first + i * at.step));
     commit_copies();
   }
-  float w[P], b[P];
+  uint64_t w[P / 2], b[P / 2];
   at.cols.floats(a.weight ? a.weight + at.base : nullptr, 1.f, w);
   at.cols.floats(a.bias ? a.bias + at.base : nullptr, 0.f, b);
-  const float over = 1.f / (float)a.d;
-  int turn1 = 0, turn2 = 0, slot = 0;
-  for (int64_t t = at.first; t < a.tokens; t += at.step) {
-    float v[P];
+  constexpr int W = G / 32;
+  const int warp = G == 32 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int mine = 0;  // the warp's columns
+  at.cols.each([&](int k) { mine += at.cols.whole(k) ? 2 : 1; });
+  mine = __reduce_add_sync(kAll, mine);
+  const float n = (float)mine, over_n = mine ? 1.f / n : 0.f, over = 1.f / (float)a.d;
+  int turn = 0, slot = 0;
+  T* out = y + at.first * a.ldy + at.base;
+  for (int64_t t = at.first; t < a.tokens; t += at.step, out += at.step * a.ldy) {
+    uint64_t v[P / 2];
     wait_copies<Rows::kDepth - 1>();
     feed.take(at.cols, slot, v);
     feed.issue(at.cols, slot, row(t + Rows::kDepth * at.step));
     commit_copies();
     slot = slot + 1 == Rows::kDepth ? 0 : slot + 1;
-    float s1[1] = {0.f};
-    at.cols.each([&](int i, int) { s1[0] += v[i]; });
-    sum1(s1, turn1);
-    float mean = s1[0] * over, off = mean, var = 0.f;
-    // once, but for rows whose spread is lost in the first mean's rounding
-    for (int again = 0; again < 8; ++again) {
-      float s2[2] = {0.f, 0.f};
-      at.cols.each([&](int i, int) {
-        v[i] -= off;
-        s2[0] += v[i];
-        s2[1] += v[i] * v[i];
+    // the warp's mean c, and its sums s and m2 of x - c and their squares
+    uint64_t p = 0;
+    at.cols.each([&](int k) { p = ptx::add_f32x2(p, at.cols.masked(v[k], k)); });
+    float c = warp_sum(sum_of(p)) * over_n, off = c, s, m2;
+    // once, but for rows whose spread is lost in the mean's rounding
+    for (int again = 0;; ++again) {
+      uint64_t s2 = 0, q2 = 0;
+      at.cols.each([&](int k) {
+        v[k] = at.cols.masked(ptx::add_f32x2(v[k], both(-off)), k);
+        s2 = ptx::add_f32x2(s2, v[k]);
+        q2 = ptx::fma_f32x2(v[k], v[k], q2);
       });
-      sum2(s2, turn2);
-      off = s2[0] * over;
-      var = s2[1] * over - off * off;
-      if (!(off * off > var * 0.00390625f)) break;
-      mean += off;
+      const float sq = warp_sum2(sum_of(s2), sum_of(q2)), other = __shfl_xor_sync(kAll, sq, 16);
+      s = lane < 16 ? sq : other;
+      m2 = lane < 16 ? other : sq;
+      if (!(s * s > m2 * n * 0.00390625f) || again == 7) break;
+      off = s * over_n;
+      c += off;
+    }
+    // e: the warp's c less the row's mean
+    float mean, e, var;
+    if constexpr (W == 1) {
+      e = -s * over_n;
+      mean = c - e;
+      var = (m2 + e * (2.f * s + n * e)) * over;
+    } else {
+      if (lane == 0) shared.warp[turn][warp] = float4{c, s, m2, n};
+      __syncthreads();
+      const float4 o = shared.warp[turn][lane % W];
+      const float first = __shfl_sync(kAll, o.x, 0), away = o.x - first;
+      float sum = away * o.w + o.y, count = o.w;
+#pragma unroll
+      for (int l = 1; l < W; l <<= 1) {
+        sum = xor_sum(sum, l);
+        if (CL > 1) count = xor_sum(count, l);
+      }
+      const float middle = sum * (CL > 1 ? (count > 0.f ? 1.f / count : 0.f) : over);
+      const float apart = o.w > 0.f ? away - middle : 0.f;
+      float q = o.z + apart * (2.f * o.y + o.w * apart);
+#pragma unroll
+      for (int l = 1; l < W; l <<= 1) q = xor_sum(q, l);
+      e = __shfl_sync(kAll, apart, warp);
+      mean = first + middle;
+      if constexpr (CL > 1) {
+        float4 part[CL];
+        over_cluster<CL>(shared.block[turn], float4{first, middle, q, count}, [&](int r, const float4& o) { part[r] = o; });
+        float all = 0.f;
+#pragma unroll
+        for (int r = 0; r < CL; ++r) all += ((part[r].x - part[0].x) + part[r].y) * part[r].w;
+        const float centre = all * over;
+        q = 0.f;
+#pragma unroll
+        for (int r = 0; r < CL; ++r) {
+          const float apart = (part[r].x - part[0].x) + part[r].y - centre;
+          q += part[r].w > 0.f ? part[r].z + part[r].w * apart * apart : 0.f;
+        }
+        e += (first - part[0].x) + middle - centre;
+        mean = part[0].x + centre;
+      }
+      var = q * over;
+      turn ^= 1;
     }
     const float rstd = 1.f / sqrtf((var < 0.f ? 0.f : var) + a.eps);
     if (a.stats && at.cols.rank == 0 && at.base == 0) {
-      a.stats[2 * t] = mean + off;
+      a.stats[2 * t] = mean;
       a.stats[2 * t + 1] = rstd;
     }
-    at.cols.each([&](int i, int) { v[i] = (v[i] - off) * rstd * w[i] + b[i]; });
-    at.cols.store(y + t * a.ldy + at.base, v);
+    at.cols.put(out, [&](int k) {
+      return ptx::fma_f32x2(ptx::mul_f32x2(ptx::add_f32x2(v[k], both(e)), both(rstd)), w[k], b[k]);
+    });
   }
   if (CL > 1) ptx::cluster_sync();  // (others may still read this block's sums)
 }
 
-template <typename T, int B, int G, int P, int CL>
-__global__ void __launch_bounds__(kBlock<G>) k_norm_grad(const T* dy, const T* x, T* dx, const NormArgs a) {
-  constexpr int kGroups = kBlock<G> / G;
-  extern __shared__ uint4 ring_s[];  // the rows' rings; after them G == 32's warps' columns, 2 x d each
-  __shared__ GroupSum<G, 3, CL> sum;
-  using Rows = Feed<T, B, G, P, kGradDepth>;
+// Values wait as they were loaded, not as FP32, between the row's sums and its
+// gradient; GROUPS groups of G threads a block, whose columns' sums join there.
+template <typename T, int B, int G, int P, bool FULL, int CL, int GROUPS>
+__global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x, T* dx, const NormArgs a) {
+  extern __shared__ uint4 ring_s[];  // the rows' rings; in the end the groups' columns, 2 x d each
+  __shared__ NormShared<G, CL> shared_s[GROUPS];
+  using Rows = Feed<T, B, G, P, FULL, kGradDepth>;
+  using Cols = typename Rows::Cols;
+  using Word = typename Rows::Word;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const Share<T, B, G, P, CL> at(a.d);
+  const Share<T, B, G, P, FULL, CL, GROUPS> at(a.d);
+  NormShared<G, CL>& shared = shared_s[at.slot];
   Rows feed_x, feed_dy;
-  feed_x.ring = reinterpret_cast<typename Rows::Word*>(reinterpret_cast<char*>(ring_s) + at.slot * 2 * Rows::kBytes);
+  feed_x.ring = reinterpret_cast<Word*>(reinterpret_cast<char*>(ring_s) + at.slot * 2 * Rows::kBytes);
   feed_dy.ring = feed_x.ring + Rows::kBytes / B;
   float2 ahead[2] = {};  // the statistics of the next two rows
   auto issue = [&](int64_t t, int slot) {
@@ -291,63 +420,111 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm_grad(const T* dy, const T* x
   for (int i = 0; i < Rows::kDepth; ++i) issue(at.first + i * at.step, i);
   ahead[0] = stats_of(at.first);
   ahead[1] = stats_of(at.first + at.step);
-  float w[P], dw[P], db[P];
-  at.cols.floats(a.weight ? a.weight + at.base : nullptr, 1.f, w);
+  // Weights in registers; where a thread holds 32 columns, in shared memory, a
+  // thread's pairs G apart (each thread reads what a thread of its place wrote).
+  constexpr bool kSharedWeight = P >= 32;
+  __shared__ uint64_t weight_s[kSharedWeight ? P / 2 * G : 1];
+  uint64_t w[P / 2], dw[P / 2], db[P / 2];
+  if (!kSharedWeight || at.slot == 0) at.cols.floats(a.weight ? a.weight + at.base : nullptr, 1.f, w);
+  if (kSharedWeight) {
+    if (at.slot == 0) {
 #pragma unroll
-  for (int i = 0; i < P; ++i) dw[i] = db[i] = 0.f;
+      for (int k = 0; k < P / 2; ++k) weight_s[k * G + at.cols.rank] = w[k];
+    }
+    __syncthreads();
+  }
+  auto weight = [&](int k) { return kSharedWeight ? weight_s[k * G + at.cols.rank] : w[k]; };
+#pragma unroll
+  for (int k = 0; k < P / 2; ++k) dw[k] = db[k] = 0;
+  constexpr int W = G / 32;
+  const int warp = (threadIdx.x % G) >> 5, lane = threadIdx.x & 31;
   const float over = 1.f / (float)a.d;
   int turn = 0, slot = 0;
   for (int64_t t = at.first; t < a.tokens; t += at.step) {
-    float v[P], g[P];
+    Word raw_x[Cols::U], raw_dy[Cols::U];
     wait_copies<Rows::kDepth - 1>();
-    feed_x.take(at.cols, slot, v);
-    feed_dy.take(at.cols, slot, g);
+#pragma unroll
+    for (int u = 0; u < Cols::U; ++u)
+      if (at.cols.inside(u)) {
+        raw_x[u] = feed_x.word(at.cols, slot, u);
+        raw_dy[u] = feed_dy.word(at.cols, slot, u);
+      }
     issue(t + Rows::kDepth * at.step, slot);
     slot = slot + 1 == Rows::kDepth ? 0 : slot + 1;
     const float mean = ahead[0].x, rstd = ahead[0].y;
     ahead[0] = ahead[1];
     ahead[1] = stats_of(t + 2 * at.step);
-    float s[3] = {0.f, 0.f, 0.f};
-    at.cols.each([&](int i, int) {
-      v[i] = (v[i] - mean) * rstd;
-      const float gw = g[i] * w[i];
-      s[0] += v[i];
-      s[1] += gw;
-      s[2] += gw * v[i];
+    const uint64_t minus_mean = both(-mean), r = both(rstd);
+    uint64_t s0 = 0, s1 = 0, s2 = 0;
+    at.cols.each([&](int k) {
+      const uint64_t xh = at.cols.masked(ptx::mul_f32x2(ptx::add_f32x2(Cols::pair(raw_x, k), minus_mean), r), k);
+      const uint64_t gw = ptx::mul_f32x2(at.cols.masked(Cols::pair(raw_dy, k), k), weight(k));
+      s0 = ptx::add_f32x2(s0, xh);
+      s1 = ptx::add_f32x2(s1, gw);
+      s2 = ptx::fma_f32x2(gw, xh, s2);
     });
-    sum(s, turn);
-    // xh is v less `off`, what the rounded mean leaves
-    const float off = s[0] * over, mean_g = s[1] * over, mean_gx = s[2] * over - off * mean_g;
-    at.cols.each([&](int i, int) {
-      const float xh = v[i] - off;
-      dw[i] += g[i] * xh;
-      db[i] += g[i];
-      g[i] = rstd * (g[i] * w[i] - mean_g - xh * mean_gx);
-    });
-    if (dx) at.cols.store(dx + t * a.lddx + at.base, g);
+    float sum[3];
+    const float part = warp_sum3(sum_of(s0), sum_of(s1), sum_of(s2));
+    if constexpr (W == 1) {
+      sum[0] = __shfl_sync(kAll, part, 0);
+      sum[1] = __shfl_sync(kAll, part, 16);
+      sum[2] = __shfl_sync(kAll, part, 8);
+    } else {
+      if ((lane & 7) == 0 && lane != 24) reinterpret_cast<float*>(&shared.warp[turn][warp])[lane == 8 ? 2 : lane >> 4] = part;
+      group_barrier<G, GROUPS>(at.slot);
+      const float4 o = shared.warp[turn][lane % W];
+      sum[0] = o.x, sum[1] = o.y, sum[2] = o.z;
+#pragma unroll
+      for (int l = 1; l < W; l <<= 1)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) sum[i] = xor_sum(sum[i], l);
+      if constexpr (CL > 1) {
+        float all[3] = {0.f, 0.f, 0.f};
+        over_cluster<CL>(shared.block[turn], float4{sum[0], sum[1], sum[2], 0.f}, [&](int, const float4& o) {
+          all[0] += o.x, all[1] += o.y, all[2] += o.z;
+        });
+        sum[0] = all[0], sum[1] = all[1], sum[2] = all[2];
+      }
+      turn ^= 1;
+    }
+    // (opened anew below: kept as FP32 since above, the values would take twice the registers)
+    Cols::forget(raw_x);
+    Cols::forget(raw_dy);
+    // xh less `off`, what the rounded mean leaves
+    const float off = sum[0] * over, mean_g = sum[1] * over, mean_gx = sum[2] * over - off * mean_g;
+    const uint64_t less = both(-off), down = both(-mean_g * rstd), along = both(-mean_gx * rstd);
+    auto step = [&](int k) {
+      const uint64_t g = Cols::pair(raw_dy, k);
+      const uint64_t xh = ptx::add_f32x2(ptx::mul_f32x2(ptx::add_f32x2(Cols::pair(raw_x, k), minus_mean), r), less);
+      dw[k] = ptx::fma_f32x2(g, xh, dw[k]);
+      db[k] = ptx::add_f32x2(db[k], g);
+      return ptx::fma_f32x2(xh, along, ptx::fma_f32x2(ptx::mul_f32x2(g, weight(k)), r, down));
+    };
+    if (dx)
+      at.cols.put(dx + t * a.lddx + at.base, step);
+    else
+      at.cols.each(step);
   }
   if (CL > 1) ptx::cluster_sync();
   if (!a.parts) return;
-  float* out = a.parts + (int64_t)(blockIdx.x / CL) * 2 * a.d + at.base;
-  if constexpr (G == 32) {
-    float* all = reinterpret_cast<float*>(reinterpret_cast<char*>(ring_s) + kGroups * 2 * Rows::kBytes);
-    float* own = all + at.slot * 2 * a.d;
-    at.cols.each([&](int i, int c) {
-      own[c] = dw[i];
-      own[a.d + c] = db[i];
-    });
+  float* parts = a.parts + (int64_t)(blockIdx.x / CL) * 2 * a.d + at.base;
+  if constexpr (GROUPS > 1) {
+    // (all copies have arrived: the last rows' were waited for, the others are empty)
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * a.d; c += kBlock<G>) {
+    float* all = reinterpret_cast<float*>(ring_s);
+    float* own = all + at.slot * 2 * a.d;
+    at.cols.each_value(dw, [&](float v, int c) { own[c] = v; });
+    at.cols.each_value(db, [&](float v, int c) { own[a.d + c] = v; });
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.d; c += G * GROUPS) {
       float t = 0.f;
 #pragma unroll
-      for (int r = 0; r < kGroups; ++r) t += all[r * 2 * a.d + c];
-      out[c] = t;
+      for (int r = 0; r < GROUPS; ++r) t += all[r * 2 * a.d + c];
+      parts[c] = t;
     }
   } else {
-    at.cols.each([&](int i, int c) {
-      out[c] = dw[i];
-      out[a.d + c] = db[i];
-    });
+    at.cols.each_value(dw, [&](float v, int c) { parts[c] = v; });
+    at.cols.each_value(db, [&](float v, int c) { parts[a.d + c] = v; });
   }
 }
 
@@ -406,52 +583,102 @@ void launch_cluster(K kernel, int blocks, int threads, int smem, cudaStream_t s,
   LC_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
-// f(G, P, CL) for rows of d columns.
+template <int V>
+using Int = std::integral_constant<int, V>;
+// f(G, P, CL) for rows of d columns: as many columns a thread as registers hold
+// (sums over threads cost more than values), more threads beyond, then blocks.
 template <typename F>
 void by_width(int d, F&& f) {
-  using std::integral_constant;
-  auto with = [&](auto g, auto p, auto cl) { f(g, p, cl); };
-  integral_constant<int, 1> one;
   if (d <= 256)
-    with(integral_constant<int, 32>{}, integral_constant<int, 8>{}, one);
+    f(Int<32>{}, Int<8>{}, Int<1>{});
   else if (d <= 512)
-    with(integral_constant<int, 32>{}, integral_constant<int, 16>{}, one);
+    f(Int<32>{}, Int<16>{}, Int<1>{});
+  else if (d <= 1024)
+    f(Int<32>{}, Int<32>{}, Int<1>{});
   else if (d <= 2048)
-    with(integral_constant<int, 128>{}, integral_constant<int, 16>{}, one);
+    f(Int<64>{}, Int<32>{}, Int<1>{});
   else if (d <= 4096)
-    with(integral_constant<int, 256>{}, integral_constant<int, 16>{}, one);
+    f(Int<128>{}, Int<32>{}, Int<1>{});
   else if (d <= 8192)
-    with(integral_constant<int, 512>{}, integral_constant<int, 16>{}, one);
+    f(Int<256>{}, Int<32>{}, Int<1>{});
   else if (d <= 16384)
-    with(integral_constant<int, 512>{}, integral_constant<int, 16>{}, integral_constant<int, 2>{});
+    f(Int<512>{}, Int<32>{}, Int<1>{});
   else if (d <= 32768)
-    with(integral_constant<int, 512>{}, integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    f(Int<512>{}, Int<32>{}, Int<2>{});
   else
-    with(integral_constant<int, 512>{}, integral_constant<int, 16>{}, integral_constant<int, 8>{});
+    f(Int<512>{}, Int<32>{}, Int<4>{});
 }
-// f(B) with the largest unit that divides every address and row.
+// f(G, P, CL, GROUPS) of the gradient, which holds a thread's columns four times over
+// (FP32 values; packed BF16 ones, not those of single units, take half the
+// registers).
+template <typename T, int B, typename F>
+void by_width_grad(int d, F&& f) {
+  constexpr bool kPacked = sizeof(T) == 2 && B > 2;
+  if (d <= 256) {
+    f(Int<32>{}, Int<8>{}, Int<1>{}, Int<8>{});
+  } else if (d <= 512) {
+    f(Int<32>{}, Int<16>{}, Int<1>{}, Int<8>{});
+  } else if (d <= 1024) {
+    if constexpr (kPacked)
+      f(Int<32>{}, Int<32>{}, Int<1>{}, Int<12>{});
+    else
+      f(Int<64>{}, Int<16>{}, Int<1>{}, Int<8>{});
+  } else if (d <= 2048) {
+    if constexpr (kPacked)
+      f(Int<64>{}, Int<32>{}, Int<1>{}, Int<6>{});
+    else
+      f(Int<128>{}, Int<16>{}, Int<1>{}, Int<4>{});
+  } else if (d <= 4096) {
+    if constexpr (kPacked)
+      f(Int<128>{}, Int<32>{}, Int<1>{}, Int<3>{});
+    else
+      f(Int<256>{}, Int<16>{}, Int<1>{}, Int<2>{});
+  } else if (d <= 8192) {
+    f(Int<512>{}, Int<16>{}, Int<1>{}, Int<1>{});
+  } else if (d <= 16384) {
+    f(Int<512>{}, Int<16>{}, Int<2>{}, Int<1>{});
+  } else if (d <= 32768) {
+    f(Int<512>{}, Int<16>{}, Int<4>{}, Int<1>{});
+  } else {
+    f(Int<512>{}, Int<16>{}, Int<8>{}, Int<1>{});
+  }
+}
+// f(B) with the largest unit that divides every address and row; f(FULL), which has
+// kernels of its own for the largest unit.
 template <typename T, typename F>
 void by_alignment(uintptr_t bits, F&& f) {
   if (bits % 16 == 0)
-    f(std::integral_constant<int, 16>{});
+    f(Int<16>{});
   else if (sizeof(T) == 2 && bits % 4 == 0)
-    f(std::integral_constant<int, 4>{});
+    f(Int<4>{});
   else
-    f(std::integral_constant<int, (int)sizeof(T)>{});
+    f(Int<(int)sizeof(T)>{});
+}
+template <int B, typename F>
+void by_fullness(bool full, F&& f) {
+  if constexpr (B == 16) {
+    if (full) return f(std::true_type{});
+  }
+  f(std::false_type{});
 }
 
 template <typename T>
 void launch_norm(const T* x, T* y, const NormArgs& a, cudaStream_t s) {
   const uintptr_t bits = (uintptr_t)x | (uintptr_t)y | (uintptr_t)(a.ldx * sizeof(T)) | (uintptr_t)(a.ldy * sizeof(T)) |
                          (uintptr_t)(a.d * sizeof(T));
-  by_width(a.d, [&](auto g, auto p, auto cl) {
-    by_alignment<T>(bits, [&](auto b) {
-      constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value, B = decltype(b)::value;
-      constexpr int kSmem = kBlock<G> / G * Feed<T, B, G, P, kNormDepth>::kBytes;
-      if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(k_norm<T, B, G, P, CL>), kSmem);
-      static const int kResident = resident_blocks(k_norm<T, B, G, P, CL>, kBlock<G>, kSmem);
-      const int blocks = (int)std::min<int64_t>(ceil_div(a.tokens, kBlock<G> / G), kResident / CL);
-      launch_cluster<CL>(k_norm<T, B, G, P, CL>, blocks, kBlock<G>, kSmem, s, x, y, a);
+  by_alignment<T>(bits, [&](auto b) {
+    by_width(a.d, [&](auto g, auto p, auto cl) {
+      constexpr int B = decltype(b)::value;
+       by_fullness<B>(a.d == g * p * cl, [&](auto full) {
+          constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value;
+          constexpr bool FULL = decltype(full)::value;
+          constexpr int kSmem = kBlock<G> / G * Feed<T, B, G, P, FULL, kNormDepth<T, G, P>>::kBytes;
+          const auto kernel = k_norm<T, B, G, P, FULL, CL>;
+          if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
+          static const int kResident = resident_blocks(kernel, kBlock<G>, kSmem);
+          const int blocks = (int)std::min<int64_t>(ceil_div(a.tokens, kBlock<G> / G), kResident / CL);
+          launch_cluster<CL>(kernel, blocks, kBlock<G>, kSmem, s, x, y, a);
+        });
     });
   });
   LC_LAUNCH_CHECK("k_norm");
@@ -463,14 +690,21 @@ void launch_norm_grad(const T* dy, const T* x, T* dx, const NormArgs& a, float* 
                          (uintptr_t)(a.lddy * sizeof(T)) | (uintptr_t)(dx ? a.lddx * sizeof(T) : 0) |
                          (uintptr_t)(a.d * sizeof(T));
   int blocks = 0;
-  by_width(a.d, [&](auto g, auto p, auto cl) {
-    by_alignment<T>(bits, [&](auto b) {
-      constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value, B = decltype(b)::value;
-      constexpr int kSmem = kBlock<G> / G * (2 * Feed<T, B, G, P, kGradDepth>::kBytes + (G == 32 ? 2 * G * P * 4 : 0));
-      if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(k_norm_grad<T, B, G, P, CL>), kSmem);
-      static const int kResident = resident_blocks(k_norm_grad<T, B, G, P, CL>, kBlock<G>, kSmem);
-      blocks = (int)std::min<int64_t>(ceil_div(a.tokens, kBlock<G> / G), kResident / CL);
-      launch_cluster<CL>(k_norm_grad<T, B, G, P, CL>, blocks, kBlock<G>, kSmem, s, dy, x, dx, a);
+  by_alignment<T>(bits, [&](auto b) {
+    constexpr int B = decltype(b)::value;
+    by_width_grad<T, B>(a.d, [&](auto g, auto p, auto cl, auto groups) {
+      by_fullness<B>(a.d == g * p * cl, [&](auto full) {
+        constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value;
+        constexpr int GROUPS = decltype(groups)::value;
+        constexpr bool FULL = decltype(full)::value;
+        constexpr int kRing = GROUPS * 2 * Feed<T, B, G, P, FULL, kGradDepth>::kBytes;
+        constexpr int kSums = GROUPS > 1 ? GROUPS * 2 * G * P * 4 : 0, kSmem = kRing > kSums ? kRing : kSums;
+        const auto kernel = k_norm_grad<T, B, G, P, FULL, CL, GROUPS>;
+        if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
+        static const int kResident = resident_blocks(kernel, G * GROUPS, kSmem);
+        blocks = (int)std::min<int64_t>(ceil_div(a.tokens, GROUPS), kResident / CL);
+        launch_cluster<CL>(kernel, blocks, G * GROUPS, kSmem, s, dy, x, dx, a);
+      });
     });
   });
   LC_LAUNCH_CHECK("k_norm_grad");
