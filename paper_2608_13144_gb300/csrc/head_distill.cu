@@ -2,8 +2,9 @@
 // gradient in the same call:
 //   q = softmax of the teacher's values / T over the classes it names,
 //   loss = w T^2 sum_j q_j (log q_j - log p_j),  dz = w T (p - q)
-// A row's sums first, then its values again for the gradient: from shared memory
-// where a block has the row in it, else from the caches. The gradient is written as
+// A row's sums first, then its values again for the gradient: small rows wait in the
+// registers of a few lanes, larger ones in shared memory (of a cluster where one
+// block's does not hold them), the largest are read twice. The gradient is written as
 // w T p everywhere, and at the teacher's classes once more.
 #include "head_mma.cuh"
 #include "head_rows.cuh"
@@ -22,179 +23,366 @@ struct DistillArgs {
   float* loss;
 };
 
-constexpr int kMostTop = LIPCACHE_MAX_TOP;
-constexpr int kTopRegs = kMostTop / 32;
+constexpr uint32_t kAll = 0xffffffffu;
 
-// The teacher's answers of one row, entry 32 i + lane in a warp's registers. rest:
-// the sum of the shares of other classes than the entry's; same: of its own class;
-// first: no entry before it names its class.
+// The teacher's answers of one row on L lanes, entry L i + lane in a lane's
+// registers. rest: the sum of the shares of other classes than the entry's; same: of
+// its own; first: no entry before it names its class.
+template <int L, int R>
 struct Teacher {
-  int index[kTopRegs];
-  float q[kTopRegs], log_q[kTopRegs], same[kTopRegs], rest[kTopRegs];
-  bool first[kTopRegs], bad, any;
+  int index[R];
+  float q[R], log_q[R], same[R], rest[R];
+  bool first[R], bad, any;
 
-  __device__ __forceinline__ void load(const DistillArgs& a, int64_t row, int lane) {
-    constexpr uint32_t kAll = 0xffffffffu;
-    float v[kTopRegs];
-    float best = -INFINITY;
+  __device__ __forceinline__ void load(const DistillArgs& a, int64_t row, int lane, bool live) {
+    float v[R], best = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kTopRegs; ++i) {
-      const int j = 32 * i + lane;
+    for (int i = 0; i < R; ++i) {
+      const int j = L * i + lane;
       index[i] = -1;
       v[i] = -INFINITY;
-      if (j < a.k) {
-        index[i] = a.index[row * a.k + j];
-        if (index[i] < 0 || index[i] >= a.classes) index[i] = -1;
-        if (index[i] >= 0) v[i] = a.top[row * a.k + j];
+      if (j < a.k && live) {
+        index[i] = __ldg(a.index + row * a.k + j);
+        const float x = __ldg(a.top + row * a.k + j);
+        if (index[i] < 0 || index[i] >= a.classes)
+          index[i] = -1;
+        else
+          v[i] = x;
       }
       best = max_nan(best, v[i]);
     }
-    const uint32_t top = __reduce_max_sync(kAll, key_of(best));
+    const uint32_t top = lanes_max<L>(key_of(best));
     any = top >= kUnmasked;
     bad = top >= kNanKey;
-    if (!any || bad) return;
-    best = value_of(top);
+    best = any && !bad ? value_of(top) : 0.f;
     // the largest stands outside the sum: a sure teacher's logarithms keep their bits
+    const int base = threadIdx.x & 31 & ~(L - 1);
     float others = 0.f;
-    bool out = false;
+    bool out = false, own[R];
 #pragma unroll
-    for (int i = 0; i < kTopRegs; ++i) {
-      const uint32_t b = __ballot_sync(kAll, v[i] == best);
-      const bool own = !out && b && (__ffs(b) - 1) == lane;
+    for (int i = 0; i < R; ++i) {
+      const uint32_t b = (__ballot_sync(kAll, v[i] == best) >> base) & (L == 32 ? kAll : (1u << (L & 31)) - 1);
+      own[i] = !out && b && __ffs(b) - 1 == lane;
       out = out || b;
       log_q[i] = (v[i] - best) / a.temperature;
       q[i] = v[i] == -INFINITY ? 0.f : expf(log_q[i]);
-      if (!own) others += q[i];
+      if (!own[i]) others += q[i];
     }
-    others = warp_sum(others);
-    const float log_sum = log1pf(others);
+    others = lanes_sum<L>(others);
+    const float log_sum = log1pf(others), over = 1.f / (1.f + others);
 #pragma unroll
-    for (int i = 0; i < kTopRegs; ++i) {
+    for (int i = 0; i < R; ++i) {
       log_q[i] -= log_sum;
-      q[i] /= 1.f + others;
-      same[i] = rest[i] = 0.f;
+      q[i] *= over;
+      same[i] = q[i];
+      rest[i] = own[i] ? others * over : 1.f - q[i];
       first[i] = index[i] >= 0;
     }
+  }
+  // Where a class may be named twice.
+  __device__ __forceinline__ void join_same(int k, int lane) {
+    const int base = threadIdx.x & 31 & ~(L - 1);
 #pragma unroll
-    for (int i = 0; i < kTopRegs; ++i) {
-      if (32 * i >= a.k) break;
-      for (int l = 0; l < 32 && 32 * i + l < a.k; ++l) {
-        const int other = __shfl_sync(kAll, index[i], l);
-        const float share = __shfl_sync(kAll, q[i], l);
+    for (int i = 0; i < R; ++i) same[i] = rest[i] = 0.f;
 #pragma unroll
-        for (int e = 0; e < kTopRegs; ++e) {
+    for (int i = 0; i < R; ++i)
+      for (int l = 0; l < L && L * i + l < k; ++l) {
+        const int other = __shfl_sync(kAll, index[i], base + l);
+        const float share = __shfl_sync(kAll, q[i], base + l);
+#pragma unroll
+        for (int e = 0; e < R; ++e) {
           const bool mine = other == index[e];
           same[e] += mine ? share : 0.f;
           rest[e] += mine ? 0.f : share;
-          if (mine && 32 * i + l < 32 * e + lane) first[e] = false;
+          if (mine && L * i + l < L * e + lane) first[e] = false;
         }
       }
+  }
+  // This lane's part of the divergence; at: what the gradient is at the entries'
+  // classes; zj: their logits.
+  __device__ __forceinline__ float divergence(const DistillArgs& a, const RowSums& sums, float w, const float (&zj)[R],
+                                              float (&at)[R]) const {
+    const float log_sum = log1pf(sums.others);
+    float loss = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const float lp = sums.none || zj[i] == -INFINITY ? -INFINITY : (zj[i] - sums.m) / a.temperature - log_sum;
+      if (q[i] > 0.f) loss += q[i] * (log_q[i] - lp);
+      // p - q; where both are near 1, the difference of what they leave to others
+      const float p = exp2_of(lp * kLog2e);
+      at[i] = w * a.temperature * (p > 0.5f && same[i] > 0.5f ? rest[i] + expm1f(lp) : p - same[i]);
     }
+    return loss;
   }
 };
 
-template <int G>
-struct DistillShared {
-  JoinShared<G> join;
-  int live;
-};
+// The gradient w T p of a granule (factor = w T / sum), or `fill`.
+template <typename T>
+__device__ __forceinline__ uint4 gradient_of(const uint4& w, bool live, uint64_t minus_m, uint64_t c, uint64_t factor,
+                                             float fill) {
+  constexpr int N = Vec<T>::N;
+  uint64_t v[N / 2];
+  if (live) {
+    Vec<T>::open(w, v);
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) v[j] = ptx::mul_f32x2(exp2_pair(shifted(v[j], minus_m, c)), factor);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) v[j] = both(fill);
+  }
+  return Vec<T>::close(v);
+}
 
-// G threads a row: 32, of which a block holds four rows, or a block. RESIDENT: the
-// row waits in shared memory for its second reading.
-template <typename T, int G, bool RESIDENT>
-__global__ void __launch_bounds__(G == 32 ? 128 : G) k_distill(const T* z, T* dz, const DistillArgs a) {
-  constexpr int kRows = G == 32 ? 4 : 1, N = Vec<T>::N;
-  extern __shared__ uint4 row_s[];
-  __shared__ DistillShared<G> shared[kRows];
+// Small rows: L lanes each, U granules a lane, up to 2 L classes of the teacher.
+template <typename T, int L, int U>
+__global__ void __launch_bounds__(128) k_distill_lanes(const T* z, T* dz, const DistillArgs a) {
+  constexpr int kRows = 32 / L, R = 2;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int slot = G == 32 ? threadIdx.x >> 5 : 0, rank = group_rank<G>(), lane = threadIdx.x & 31;
-  const int64_t t = (int64_t)blockIdx.x * kRows + slot;
-  if (t >= a.tokens) return;
+  const int lane = threadIdx.x & (L - 1);
+  const int64_t t = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 5)) * kRows + (threadIdx.x & 31) / L;
+  const bool is = t < a.tokens;
+  const T* zr = z + (is ? t : 0) * a.ldz;
+  const RowSpan<T> row(zr, a.classes);
+  LaneRow<T, L, U> r;
+  r.load(row, a.classes, lane, is);
+  const float w = !is ? 0.f : a.weight ? __ldg(a.weight + t) : 1.f;
+  Teacher<L, R> teacher;
+  teacher.load(a, t, lane, is);
+  float zj[R], at[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) zj[i] = teacher.index[i] >= 0 ? to_f32<T>(zr[teacher.index[i]]) : 0.f;
+  teacher.join_same(a.k, lane);
+  uint32_t mine;
+  const RowSums sums = sum_lanes<T, L, U, false>(r, lane, a.c, mine);
+  const bool taught = teacher.any && w != 0.f, bad = taught && (teacher.bad || isnan(sums.m));
+  float loss = lanes_sum<L>(teacher.divergence(a, sums, w, zj, at));
+  loss = bad ? NAN : taught ? w * a.temperature * a.temperature * loss : 0.f;
+  if (is && a.loss && lane == 0) a.loss[t] = loss;
+  if (!dz) return;
+  T* dr = dz + t * a.ldd;
+  const bool live = taught && !bad && !sums.none, same_place = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
+  const uint64_t minus_m = both(-sums.m), c = both(a.c), factor = both(w * a.temperature / (1.f + sums.others));
+  if (is) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u * L + lane < row.count)
+        put_granule<T>(dr, same_place, gradient_of<T>(r.w[u], live, minus_m, c, factor, bad ? NAN : 0.f),
+                       row.first(u * L + lane), a.classes);
+  }
+  __syncwarp();  // (the row's lanes have written what is written over here)
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (live && teacher.first[i]) dr[teacher.index[i]] = from_f32<T>(at[i]);
+}
+
+// Larger rows: a block of G threads each, or a cluster of CL blocks that split it.
+// RESIDENT: a thread copies its granules (16 at most) to shared memory, four at a
+// time, and reads them there twice.
+template <typename T, int G, int CL, bool RESIDENT>
+__global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(const T* z, T* dz, const DistillArgs a) {
+  constexpr int R = LIPCACHE_MAX_TOP / 32, U = 4;
+  extern __shared__ uint4 row_s[];
+  __shared__ JoinShared<G> join;
+  __shared__ int index_s[LIPCACHE_MAX_TOP], live_s, twice_s;
+  __shared__ float2 part_s;
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const int rank = threadIdx.x, lane = rank & 31, block = CL > 1 ? (int)ptx::cluster_ctarank() : 0;
+  const int64_t t = blockIdx.x / CL;
   const T* zr = z + t * a.ldz;
   T* dr = dz ? dz + t * a.ldd : nullptr;
   const RowSpan<T> row(zr, a.classes);
+  const int share = (row.count + CL - 1) / CL, begin = min(block * share, row.count), end = min(begin + share, row.count);
+  const Slice at(row, begin, end, a.classes);
   auto get = [&](int i) { return row.granules[i]; };
-  auto keep = [&](int i) {
-    const uint4 w = row.granules[i];
-    if (RESIDENT) row_s[i] = w;
-    return w;
-  };
-  auto again = [&](int i) { return RESIDENT ? row_s[i] : row.granules[i]; };
-  const float w = a.weight ? a.weight[t] : 1.f;
-  const bool first_warp = rank < 32;
-  Teacher teacher;
-  float zj[kTopRegs];
-  int live = 0;  // 1: a row with a teacher, 2: its values are NaN
-  if (first_warp) {
-    teacher.load(a, t, lane);
-    live = w == 0.f || !teacher.any ? 0 : teacher.bad ? 2 : 1;
+  if constexpr (RESIDENT) {
 #pragma unroll
-    for (int i = 0; i < kTopRegs; ++i) zj[i] = live == 1 && teacher.index[i] >= 0 ? to_f32<T>(zr[teacher.index[i]]) : 0.f;
-    if (G > 32 && lane == 0) shared[slot].live = live;
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = at.first + (k * U + u) * G + rank;
+        if (i < at.last) {
+          const uint32_t to = ptx::smem_u32(row_s + (i - begin));
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row.granules + i) : "memory");
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
   }
-  group_sync<G>();
-  if (G > 32) live = shared[slot].live;
-  float fill = 0.f, loss = 0.f, factor = 0.f;
+  const float w = a.weight ? __ldg(a.weight + t) : 1.f;
+  const bool first_warp = rank < 32;
+  Teacher<32, R> teacher;
+  float zj[R], grad[R];
+  if (first_warp) {
+    teacher.load(a, t, lane, true);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      zj[i] = teacher.index[i] >= 0 ? to_f32<T>(zr[teacher.index[i]]) : 0.f;
+      if (32 * i + lane < a.k) index_s[32 * i + lane] = teacher.index[i];
+    }
+    if (lane == 0) {
+      live_s = w == 0.f || !teacher.any ? 0 : teacher.bad ? 2 : 1;
+      twice_s = 0;
+    }
+  }
+  __syncthreads();
+  int live = live_s;  // 1: a row with a teacher, 2: its results are NaN
+  // whether a class is named twice: four threads an entry
+  for (int e = rank; e < 4 * a.k; e += G) {
+    const int entry = e >> 2, mine = index_s[entry];
+    if (mine >= 0)
+      for (int j = e & 3; j < entry; j += 4)
+        if (index_s[j] == mine) twice_s = 1;
+  }
   RowSums sums{};
   if (live == 1) {
-    const auto part = sum_part<T, G, false, 4>(row, 0, row.count, a.classes, rank, a.c, keep);
-    sums = join_group<T, G, false>(part, row, 0, row.count, a.classes, a.c, get, shared[slot].join);
-    if (isnan(sums.m)) live = 2;
-  }
-  if (live == 2) fill = loss = NAN;
-  float at[kTopRegs];
-  if (first_warp && live == 1) {
-    const float log_sum = sums.none ? 0.f : log1pf(sums.others);
+    RowPart<T, false> part;
+    if constexpr (RESIDENT) {
 #pragma unroll
-    for (int i = 0; i < kTopRegs; ++i) {
-      const float lp = sums.none || zj[i] == -INFINITY ? -INFINITY : (zj[i] - sums.m) / a.temperature - log_sum;
-      if (teacher.q[i] > 0.f && teacher.index[i] >= 0) loss += teacher.q[i] * (teacher.log_q[i] - lp);
-      // p - q; where both are near 1, the difference of what is left of them
-      const float p = exp2_of(lp * kLog2e);
-      at[i] = w * a.temperature * (p > 0.5f && teacher.same[i] > 0.5f ? teacher.rest[i] + expm1f(lp) : p - teacher.same[i]);
-    }
-    loss = w * a.temperature * a.temperature * warp_sum(loss);
-  }
-  if (a.loss && rank == 0) a.loss[t] = loss;
-  if (!dr) return;
-  if (live == 1 && sums.none) live = 0;  // masked whole
-  if (live == 1) factor = w * a.temperature / (1.f + sums.others);
-  const uint64_t minus_m = both(-sums.m), c = both(a.c), f = both(factor);
-  const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
-  for (int i = rank; i < row.count; i += G) {
-    uint64_t v[N / 2];
-    if (live == 1) {
-      Vec<T>::open(again(i), v);
+      for (int k = 0; k < 4; ++k) {
+        if (k == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        if (k == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        if (k == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (k == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        int i = at.first + k * U * G + rank;
+        if (i + (U - 1) * G < at.last) {
+          uint4 x[U];
 #pragma unroll
-      for (int j = 0; j < N / 2; ++j) v[j] = ptx::mul_f32x2(exp2_pair(shifted(v[j], minus_m, c)), f);
+          for (int u = 0; u < U; ++u) x[u] = row_s[i + u * G - begin];
+          part.add(x, a.c);
+        } else {
+          for (; i < at.last && i < at.first + (k + 1) * U * G; i += G) {
+            const uint4 x[1] = {row_s[i - begin]};
+            part.add(x, a.c);
+          }
+        }
+      }
+      const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
+      if (edge >= 0) {
+        const uint4 x[1] = {masked_outside<T>(get(edge), row.first(edge), a.classes)};
+        part.add(x, a.c);
+      }
     } else {
-#pragma unroll
-      for (int j = 0; j < N / 2; ++j) v[j] = both(fill);
+      part = sum_part<T, G, false, U>(row, at, a.classes, rank, a.c, get);
     }
-    put_granule<T>(dr, same, Vec<T>::close(v), row.first(i), a.classes);
+    sums = join_block<T, G, false>(part, row, at, a.classes, a.c, get, join, [] {});
+  } else {
+    if constexpr (RESIDENT) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
   }
-  if (live != 1) return;
-  group_sync<G>();
-  if (first_warp) {
+  if constexpr (CL > 1) {
+    if (rank == 0) part_s = float2{sums.m, sums.others};
+    ptx::cluster_sync();
+    if (live == 1) {
+      float m[CL], others[CL];
+      uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < kTopRegs; ++i)
-      if (teacher.index[i] >= 0 && teacher.first[i]) dr[teacher.index[i]] = from_f32<T>(at[i]);
+      for (int b = 0; b < CL; ++b) {
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];"
+                     : "=f"(m[b]), "=f"(others[b])
+                     : "r"(ptx::mapa(ptx::smem_u32(&part_s), b))
+                     : "memory");
+        top = max(top, m[b] == -INFINITY ? 0u : isnan(m[b]) ? kNanKey : key_of(m[b]));
+      }
+      sums.none = top == 0;
+      sums.m = sums.none ? -INFINITY : top >= kNanKey ? NAN : value_of(top);
+      sums.others = 0.f;
+      bool out = false;  // one block's maximum stands outside the others
+#pragma unroll
+      for (int b = 0; b < CL; ++b) {
+        if (m[b] == -INFINITY) continue;
+        const bool own = !out && m[b] == sums.m;
+        out = out || own;
+        sums.others += exp2_of(fmaxf((m[b] - sums.m) * a.c, kLeast)) * (own ? others[b] : 1.f + others[b]);
+      }
+    }
   }
+  float fill = 0.f, loss = 0.f;
+  if (live == 1 && isnan(sums.m)) live = 2;
+  if (live == 2) fill = loss = NAN;
+  if (first_warp && live == 1) {
+    if (twice_s) teacher.join_same(a.k, lane);
+    loss = w * a.temperature * a.temperature * warp_sum(teacher.divergence(a, sums, w, zj, grad));
+  }
+  if (a.loss && rank == 0 && block == 0) a.loss[t] = loss;
+  if (dr) {
+    if (live == 1 && sums.none) live = 0;  // masked whole
+    const uint64_t minus_m = both(-sums.m), c = both(a.c), factor = both(w * a.temperature / (1.f + sums.others));
+    const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
+    auto put = [&](int i, const uint4& x) {
+      put_granule<T>(dr, same, gradient_of<T>(x, live == 1, minus_m, c, factor, fill), row.first(i), a.classes);
+    };
+    for (int i = at.first + rank; i < at.last; i += G) put(i, RESIDENT ? row_s[i - begin] : get(i));
+    const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
+    if (edge >= 0) put(edge, get(edge));
+    __syncthreads();
+    // (each block those of its own classes)
+    const int low = row.first(begin), high = row.first(end);
+    if (first_warp && live == 1) {
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (teacher.first[i] && teacher.index[i] >= low && teacher.index[i] < high) dr[teacher.index[i]] = from_f32<T>(grad[i]);
+    }
+  }
+  if (CL > 1) ptx::cluster_sync();  // (until all have read part_s)
+}
+
+template <typename T, int L>
+bool distill_lanes(const T* z, T* dz, const DistillArgs& a, int granules, cudaStream_t s) {
+  constexpr int kMost = sizeof(T) == 4 ? 8 : 4;  // 32 values a lane
+  if (granules > L * kMost || a.k > 2 * L) return false;
+  const dim3 grid((unsigned)ceil_div(a.tokens, 4 * (32 / L)));
+  if (granules <= L)
+    launch_pdl(k_distill_lanes<T, L, 1>, grid, 128, s, z, dz, a);
+  else if (granules <= 2 * L)
+    launch_pdl(k_distill_lanes<T, L, 2>, grid, 128, s, z, dz, a);
+  else if (granules <= 4 * L)
+    launch_pdl(k_distill_lanes<T, L, 4>, grid, 128, s, z, dz, a);
+  else
+    launch_pdl(k_distill_lanes<T, L, kMost>, grid, 128, s, z, dz, a);
+  return true;
+}
+
+constexpr int kResidentBytes = 111 * 1024;  // twice on an SM, beside what is static
+
+template <typename T, int G, int CL, bool RESIDENT>
+void launch_blocks(const T* z, T* dz, const DistillArgs& a, int granules, cudaStream_t s) {
+  const auto kernel = k_distill<T, G, CL, RESIDENT>;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CL;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.tokens * CL));
+  cfg.blockDim = dim3(G);
+  cfg.dynamicSmemBytes = RESIDENT ? (size_t)ceil_div(granules, CL) * 16 : 0;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = CL > 1 ? 2 : 1;
+  if (cfg.dynamicSmemBytes > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kResidentBytes);
+  LC_CUDA(cudaLaunchKernelEx(&cfg, kernel, z, dz, a));
 }
 
 template <typename T>
 void launch_distill(const T* z, T* dz, const DistillArgs& a, cudaStream_t s) {
-  const int granules = (int)ceil_div(a.classes, Vec<T>::N) + 1;
-  if (granules <= 257) {
-    launch_pdl(k_distill<T, 32, false>, dim3((unsigned)ceil_div(a.tokens, 4)), 128, s, z, dz, a);
+  const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
+  constexpr int kMost = kResidentBytes / 16;
+  if (distill_lanes<T, 8>(z, dz, a, granules, s) || distill_lanes<T, 16>(z, dz, a, granules, s) ||
+      distill_lanes<T, 32>(z, dz, a, granules, s)) {
   } else if (granules <= 2048) {
-    launch_pdl_smem(k_distill<T, 128, true>, dim3((unsigned)a.tokens), 128, granules * 16, s, z, dz, a);
-  } else if (granules * 16 <= 112 * 1024 - 512) {
-    allow_smem(reinterpret_cast<const void*>(k_distill<T, 512, true>), 112 * 1024);
-    launch_pdl_smem(k_distill<T, 512, true>, dim3((unsigned)a.tokens), 512, granules * 16, s, z, dz, a);
+    launch_blocks<T, 128, 1, true>(z, dz, a, granules, s);
+  } else if (granules <= kMost && a.tokens > 32) {
+    launch_blocks<T, 512, 1, true>(z, dz, a, granules, s);
+  } else if (granules <= 4 * kMost && a.tokens > 32) {
+    launch_blocks<T, 512, 4, true>(z, dz, a, granules, s);
+  } else if (granules <= 8 * kMost) {
+    launch_blocks<T, 512, 8, true>(z, dz, a, granules, s);
   } else {
-    launch_pdl(k_distill<T, 512, false>, dim3((unsigned)a.tokens), 512, s, z, dz, a);
+    launch_blocks<T, 512, 8, false>(z, dz, a, granules, s);
   }
   LC_LAUNCH_CHECK("k_distill");
 }

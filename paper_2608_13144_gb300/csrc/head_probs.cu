@@ -27,18 +27,77 @@ struct ProbArgs {
 };
 
 constexpr float kLn2 = 0.6931471805599453f;
+using ops::key_of;
 
 // ---------------------------------------------------------------- the k largest
+// A candidate: a value's key, and below it the complement of its index, so that the
+// larger candidate stands first.
+using Found = unsigned long long;
+__device__ __forceinline__ Found candidate(uint32_t key, int index) { return (Found)key << 32 | (uint32_t)~index; }
+__device__ __forceinline__ uint32_t key_of(Found f) { return (uint32_t)(f >> 32); }
+__device__ __forceinline__ int index_of(Found f) { return (int)~(uint32_t)f; }
+
+// G threads, a warp or a block, whose maxima say where the k largest are.
 template <int G>
 struct SelectShared {
-  static constexpr int kCap = G == 32 ? 128 : G == 128 ? 512 : 1024;
+  static constexpr int kCap = G == 32 ? 128 : 4 * G;
   uint32_t key[G];
   uint16_t live[G];
   uint32_t tau;
   int n_live, n;
   int total[G / 32];
-  unsigned long long found[kCap];
+  Found found[kCap];
 };
+
+// One warp: tau, a key that at least k of the threads' maxima reach (or the lowest
+// there is), and which threads reach it.
+template <int G>
+__device__ __forceinline__ void find_threshold(SelectShared<G>& sh, int k) {
+  constexpr uint32_t kAll = 0xffffffffu;
+  constexpr int R = G / 32;
+  const int lane = threadIdx.x & 31;
+  uint32_t v[R], high = 0, low = kAll;
+  int some = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    v[i] = sh.key[i * 32 + lane];
+    high = max(high, v[i]);
+    if (v[i]) low = min(low, v[i]), ++some;
+  }
+  some = __reduce_add_sync(kAll, some);
+  uint32_t lo = kUnmasked;
+  if (some >= k) {
+    // [lo, hi): k maxima or more reach lo, fewer hi
+    lo = __reduce_min_sync(kAll, low);
+    uint32_t hi = __reduce_max_sync(kAll, high) + 1;
+    const int enough = k + k / 4 + 4;
+    while (some > enough && hi > lo + 1) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) c += v[i] >= mid;
+      c = __reduce_add_sync(kAll, c);
+      if (c >= k) {
+        lo = mid;
+        some = c;
+      } else {
+        hi = mid;
+      }
+    }
+  }
+  int live = 0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const uint32_t b = __ballot_sync(kAll, v[i] >= lo);
+    if (v[i] >= lo) sh.live[live + __popc(b & ((1u << lane) - 1))] = (uint16_t)(i * 32 + lane);
+    live += __popc(b);
+  }
+  if (lane == 0) {
+    sh.tau = lo;
+    sh.n_live = live;
+    sh.n = 0;
+  }
+}
 
 // Sum over the group, on every thread.
 template <int G>
@@ -54,85 +113,35 @@ __device__ __forceinline__ int group_count(int v, int (&total)[G / 32]) {
   return v;
 }
 
-// How many of a granule's values inside the row have a key of at least `tau`.
-template <typename T>
-__device__ __forceinline__ int count_from(const uint4& w, int first, int n, uint32_t tau) {
-  int c = 0;
-#pragma unroll
-  for (int j = 0; j < Vec<T>::N; ++j) c += first + j >= 0 && first + j < n && key_of(Vec<T>::at(w, j)) >= tau;
-  return c;
-}
-
 // The group's k largest unmasked values in granules [begin, end) of a row without
-// NaN or +inf, to emit(rank, key, index), each rank from one thread; returns how
-// many there are (at most k). `mine`: the key of this thread's own maximum, 0 if it
-// holds none.
+// NaN or +inf, after find_threshold and a barrier, to emit(rank, candidate), each rank
+// from one thread; returns how many there are (at most k).
 template <typename T, int G, typename Get, typename Emit>
-__device__ __forceinline__ int select_largest(const RowSpan<T>& row, int begin, int end, int n, int k, uint32_t mine,
+__device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice& at, int begin, int end, int n, int k,
                                               Get get, SelectShared<G>& sh, Emit emit) {
   constexpr uint32_t kAll = 0xffffffffu;
-  constexpr int N = Vec<T>::N, R = G / 32, kCap = SelectShared<G>::kCap;
-  const int rank = group_rank<G>(), lane = threadIdx.x & 31;
-  sh.key[rank] = mine;
-  group_sync<G>();
-  if (G == 32 || threadIdx.x < 32) {
-    uint32_t v[R];
-    uint32_t high = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      v[i] = sh.key[i * 32 + lane];
-      high = max(high, v[i]);
-    }
-    // [lo, hi): k threads or more reach lo (or it is the lowest there is), fewer hi
-    uint32_t lo = kUnmasked, hi = __reduce_max_sync(kAll, high) + 1;
-    while (hi > lo + 1) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      int c = 0;
-#pragma unroll
-      for (int i = 0; i < R; ++i) c += v[i] >= mid;
-      c = __reduce_add_sync(kAll, c);
-      if (c >= k) {
-        lo = mid;
-        if (c <= k + k / 4 + 4) break;
-      } else {
-        hi = mid;
-      }
-    }
-    int live = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const uint32_t b = __ballot_sync(kAll, v[i] >= lo);
-      if (v[i] >= lo) sh.live[live + __popc(b & ((1u << lane) - 1))] = (uint16_t)(i * 32 + lane);
-      live += __popc(b);
-    }
-    if (lane == 0) {
-      sh.tau = lo;
-      sh.n_live = live;
-      sh.n = 0;
-    }
-  }
-  group_sync<G>();
-  const uint32_t tau = sh.tau;
-  const int live = sh.n_live;
+  constexpr int N = Vec<T>::N, kCap = SelectShared<G>::kCap;
+  const int rank = group_rank<G>(), lane = threadIdx.x & 31, warp = G == 32 ? 0 : threadIdx.x >> 5;
   auto collect = [&](int granule, uint32_t from) {
     const uint4 w = get(granule);
     const int first = row.first(granule);
+    const float least = value_of(from);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const uint32_t key = key_of(Vec<T>::at(w, j));
-      if (key >= from && first + j >= 0 && first + j < n) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < kCap) sh.found[at] = (unsigned long long)key << 32 | (uint32_t)~(first + j);
+      const float z = Vec<T>::at(w, j);
+      if (z >= least && first + j >= 0 && first + j < n) {
+        const int to = atomicAdd(&sh.n, 1);
+        if (to < kCap) sh.found[to] = candidate(key_of(z), first + j);
       }
     }
   };
-  if (live > 0) {
-    const int rounds = (end - begin + G - 1) / G;
-    for (int i = rank; i < rounds * live; i += G) {
-      const int granule = begin + i / live * G + sh.live[i % live];
-      if (granule < end) collect(granule, tau);
-    }
-  }
+  // a warp reads a live thread's granules; those at the row's ends are read by all
+  const int live = sh.n_live;
+  const uint32_t tau = sh.tau;
+  for (int l = warp; l < live; l += G / 32)
+    for (int i = at.first + sh.live[l] + lane * G; i < at.last; i += 32 * G) collect(i, tau);
+  if (rank == 0 && at.head >= 0) collect(at.head, tau);
+  if (rank == 1 && at.tail >= 0) collect(at.tail, tau);
   group_sync<G>();
   int found = sh.n, ties = 0;
   uint32_t equal = 0;
@@ -140,21 +149,29 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, int begin, 
     // Many equal values, or large ones crowded into few threads: halve over the whole
     // row until the values from lo up fit, or those above lo are fewer than k and the
     // rest of the k are ties at lo.
-    uint32_t lo = tau, hi = 0xff800000u;
-    int at_lo = found;
-    while (hi > lo + 1 && at_lo > kCap) {
+    uint32_t lo = tau, hi = kNanKey;
+    int from_lo = found;
+    auto count = [&](int i, uint32_t from) {
+      const uint4 w = get(i);
+      const int first = row.first(i);
+      int c = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) c += first + j >= 0 && first + j < n && key_of(Vec<T>::at(w, j)) >= from;
+      return c;
+    };
+    while (hi > lo + 1 && from_lo > kCap) {
       const uint32_t mid = lo + (hi - lo) / 2;
       int c = 0;
-      for (int i = begin + rank; i < end; i += G) c += count_from<T>(get(i), row.first(i), n, mid);
+      for (int i = begin + rank; i < end; i += G) c += count(i, mid);
       c = group_count<G>(c, sh.total);
       if (c >= k) {
         lo = mid;
-        at_lo = c;
+        from_lo = c;
       } else {
         hi = mid;
       }
     }
-    const bool tied = at_lo > kCap;
+    const bool tied = from_lo > kCap;
     group_sync<G>();
     if (rank == 0) sh.n = 0;
     group_sync<G>();
@@ -167,10 +184,10 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, int begin, 
     }
   }
   for (int i = rank; i < found; i += G) {
-    const unsigned long long own = sh.found[i];
+    const Found own = sh.found[i];
     int r = 0;
     for (int j = 0; j < found; ++j) r += sh.found[j] > own;
-    if (r < k) emit(r, (uint32_t)(own >> 32), (int)~(uint32_t)own);
+    if (r < k) emit(r, own);
   }
   // ties in the order of their indices
   for (int i = begin, done = 0; done < ties && i < end; i += G) {
@@ -193,10 +210,10 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, int begin, 
     before -= c;
     if constexpr (G > 32) {
       group_sync<G>();
-      if (lane == 0) sh.total[threadIdx.x >> 5] = all;
+      if (lane == 0) sh.total[warp] = all;
       group_sync<G>();
       const int t = lane < G / 32 ? sh.total[lane] : 0;
-      before += __reduce_add_sync(kAll, lane < (int)(threadIdx.x >> 5) ? t : 0);
+      before += __reduce_add_sync(kAll, lane < warp ? t : 0);
       all = __reduce_add_sync(kAll, t);
     }
     if (c) {
@@ -204,7 +221,7 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, int begin, 
 #pragma unroll
       for (int j = 0; j < N; ++j)
         if (first + j >= 0 && first + j < n && key_of(Vec<T>::at(w, j)) == equal) {
-          if (done + before < ties) emit(found + done + before, equal, first + j);
+          if (done + before < ties) emit(found + done + before, candidate(equal, first + j));
           ++before;
         }
     }
@@ -214,86 +231,320 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, int begin, 
 }
 
 // ---------------------------------------------------------------- log-probabilities
-// What a row's sums say, and its outputs of one value.
+// What a row's sums say.
 struct RowSays {
-  float m, log_sum;
-  bool bad;
-};
-__device__ __forceinline__ RowSays write_row(const ProbArgs& a, int64_t row, const RowSums& r, float zy, bool write) {
-  const bool bad = isnan(r.m);
-  const float total = 1.f + r.others;
-  float log_sum = r.none ? 0.f : log1pf(r.others), mean = r.none ? 0.f : -kLn2 * r.q / total;
-  if (bad) log_sum = mean = NAN;
-  if (write) {
-    if (a.norm) {
-      float* o = a.norm + 3 * row;
-      o[0] = r.m;
-      o[1] = log_sum;
-      o[2] = mean;
-    }
-    if (a.entropy) a.entropy[row] = log_sum + mean;
-    if (a.logprob) {
-      const int y = a.target[row];
-      const bool live = y >= 0 && y < a.classes;
-      const float lp = r.none || zy == -INFINITY ? -INFINITY : (zy - r.m) / a.temperature - log_sum;
-      a.logprob[row] = !live ? 0.f : bad ? NAN : lp;
-    }
+  float m, log_sum, mean;
+  bool bad, none;
+  __device__ __forceinline__ explicit RowSays(const RowSums& r) {
+    m = r.m;
+    none = r.none;
+    bad = isnan(r.m);
+    log_sum = bad ? NAN : none ? 0.f : log1pf(r.others);
+    mean = bad ? NAN : none ? 0.f : __fdividef(-kLn2 * r.q, 1.f + r.others);
   }
-  return RowSays{r.m, log_sum, bad};
+  // log p of a value
+  __device__ __forceinline__ float log_p(const ProbArgs& a, float z) const {
+    return z == -INFINITY ? -INFINITY : (z - m) / a.temperature - log_sum;
+  }
+};
+// The row's outputs of one value; zy: the target's logit.
+__device__ __forceinline__ void put_row(const ProbArgs& a, int64_t row, const RowSays& says, int y, float zy) {
+  if (a.norm) {
+    float* o = a.norm + 3 * row;
+    o[0] = says.m;
+    o[1] = says.log_sum;
+    o[2] = says.mean;
+  }
+  if (a.entropy) a.entropy[row] = says.log_sum + says.mean;
+  if (a.logprob) a.logprob[row] = y < 0 || y >= a.classes ? 0.f : says.bad ? NAN : says.none ? -INFINITY : says.log_p(a, zy);
 }
-__device__ __forceinline__ void put_top(const ProbArgs& a, int64_t row, const RowSays& says, int r, uint32_t key, int i) {
-  a.top[row * a.k + r] = (value_of(key) - says.m) / a.temperature - says.log_sum;
-  a.index[row * a.k + r] = i;
+__device__ __forceinline__ void put_top(const ProbArgs& a, int64_t row, const RowSays& says, int r, Found f) {
+  a.top[row * a.k + r] = says.log_p(a, value_of(key_of(f)));
+  a.index[row * a.k + r] = index_of(f);
 }
 // places that no class fills
-__device__ __forceinline__ void fill_top(const ProbArgs& a, int64_t row, int from, float with, int rank, int G) {
+__device__ __forceinline__ void fill_top(const ProbArgs& a, int64_t row, int from, bool bad, int rank, int G) {
   for (int i = from + rank; i < a.k; i += G) {
-    a.top[row * a.k + i] = with;
+    a.top[row * a.k + i] = bad ? NAN : -INFINITY;
     a.index[row * a.k + i] = -1;
   }
 }
 
-// G threads a row: 32, of which a block holds four rows, or a block.
-template <typename T, int G>
-__global__ void __launch_bounds__(G == 32 ? 128 : G) k_probs(const T* z, const ProbArgs a) {
-  constexpr int kRows = G == 32 ? 4 : 1;
-  __shared__ SelectShared<G> select_s[kRows];
-  __shared__ JoinShared<G> join_s[kRows];
+// Small rows: L lanes each, all of a row in registers. The k-th of the lanes' sorted
+// maxima is the threshold; what reaches it is ranked as in select_largest, which also
+// takes the rows of which too much does. k <= L.
+template <typename T, int L, int U>
+__global__ void __launch_bounds__(128) k_probs_lanes(const T* z, const ProbArgs a) {
+  constexpr int N = Vec<T>::N, kRows = 32 / L, kCap = 64;
+  constexpr uint32_t kAll = 0xffffffffu;
+  __shared__ Found found_s[4 * kRows][kCap];
+  __shared__ SelectShared<32> select_s[4];
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int slot = G == 32 ? threadIdx.x >> 5 : 0, rank = group_rank<G>();
-  const int64_t t = (int64_t)blockIdx.x * kRows + slot;
-  if (t >= a.tokens) return;
+  const int warp = threadIdx.x >> 5, slot = (threadIdx.x & 31) / L, lane = threadIdx.x & (L - 1);
+  const int64_t base = ((int64_t)blockIdx.x * 4 + warp) * kRows, t = base + slot;
+  const bool live = t < a.tokens;
+  const RowSpan<T> row(z + (live ? t : 0) * a.ldz, a.classes);
+  LaneRow<T, L, U> r;
+  r.load(row, a.classes, lane, live);
+  int y = -1;
+  float zy = 0.f;
+  if (live && lane == 0 && a.logprob) {
+    y = __ldg(a.target + t);
+    if (y >= 0 && y < a.classes) zy = to_f32<T>(z[t * a.ldz + y]);
+  }
+  uint32_t mine;
+  const RowSums sums = sum_lanes<T, L, U, true>(r, lane, a.c, mine);
+  const RowSays says(sums);
+  if (live && lane == 0) put_row(a, t, says, y, zy);
+  if (a.k == 0) return;
+  // the lanes' maxima in falling order
+  uint32_t v = mine;
+#pragma unroll
+  for (int size = 2; size <= L; size <<= 1)
+#pragma unroll
+    for (int step = size / 2; step > 0; step >>= 1) {
+      const uint32_t other = __shfl_xor_sync(kAll, v, step);
+      v = ((lane & step) == 0) == ((lane & size) == 0) ? max(v, other) : min(v, other);
+    }
+  const float least = value_of(max(__shfl_sync(kAll, v, slot * L + a.k - 1), kUnmasked));
+  const bool select = live && !says.bad && !says.none;
+  int count = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int j = 0; j < N; ++j) count += r.at(u, j) >= least;
+  int to = count;
+#pragma unroll
+  for (int o = 1; o < L; o <<= 1) {
+    const int p = __shfl_up_sync(kAll, to, o);
+    if (lane >= o) to += p;
+  }
+  int all = __shfl_sync(kAll, to, slot * L + L - 1);
+  if (!select) all = 0;
+  Found* found = found_s[warp * kRows + slot];
+  to -= count;
+  if (count && all && all <= kCap) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float x = r.at(u, j);
+        if (x >= least) found[to++] = candidate(key_of(x), row.first(u * L + lane) + j);
+      }
+  }
+  __syncwarp();
+  if (live && all <= kCap) {
+    for (int i = lane; i < all; i += L) {
+      const Found own = found[i];
+      int before = 0;
+      for (int j = 0; j < all; ++j) before += found[j] > own;
+      if (before < a.k) put_top(a, t, says, before, own);
+    }
+    fill_top(a, t, min(all, a.k), says.bad, lane, L);
+  }
+  // rows with too many: the whole warp, one after another
+  for (uint32_t over = __ballot_sync(kAll, all > kCap); over;) {
+    const int from = __ffs(over) - 1;
+    const int64_t tt = base + from / L;
+    over &= L == 32 ? 0u : ~(((1u << (L & 31)) - 1) << from);
+    const RowSpan<T> wide(z + tt * a.ldz, a.classes);
+    auto get = [&](int i) { return wide.granules[i]; };
+    const Slice at(wide, 0, wide.count, a.classes);
+    uint32_t key = 0;
+    for (int i = at.first + (int)(threadIdx.x & 31); i < at.last; i += 32) {
+      const float top = top_nan<T>(get(i));
+      if (top > -INFINITY) key = max(key, ops::key_of(top));
+    }
+    __syncwarp();
+    select_s[warp].key[threadIdx.x & 31] = key;
+    __syncwarp();
+    find_threshold<32>(select_s[warp], a.k);
+    __syncwarp();
+    RowSays other = says;
+    other.m = __shfl_sync(kAll, says.m, from);
+    other.log_sum = __shfl_sync(kAll, says.log_sum, from);
+    const int have = select_largest<T, 32>(wide, at, 0, wide.count, a.classes, a.k, get, select_s[warp],
+                                           [&](int r, Found f) { put_top(a, tt, other, r, f); });
+    fill_top(a, tt, have, false, threadIdx.x & 31, 32);
+    __syncwarp();
+  }
+}
+
+// Large rows: a block of G threads each, or a cluster of CL blocks that split it.
+template <typename T, int G, int CL>
+__global__ void __launch_bounds__(G) k_probs(const T* z, const ProbArgs a) {
+  __shared__ SelectShared<G> select;
+  __shared__ JoinShared<G> join;
+  __shared__ RowSums part_s;
+  __shared__ int have_s;
+  static_assert(CL * LIPCACHE_MAX_TOP <= SelectShared<G>::kCap || CL == 1, "a cluster's candidates side by side");
+  __shared__ Found best_s[CL > 1 ? LIPCACHE_MAX_TOP : 1];
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const int64_t t = blockIdx.x / CL;
+  const int block = CL > 1 ? (int)ptx::cluster_ctarank() : 0, rank = threadIdx.x;
   const T* zr = z + t * a.ldz;
   const RowSpan<T> row(zr, a.classes);
+  const int share = (row.count + CL - 1) / CL, begin = min(block * share, row.count), end = min(begin + share, row.count);
+  const Slice at(row, begin, end, a.classes);
   auto get = [&](int i) { return row.granules[i]; };
+  int y = -1;
   float zy = 0.f;
-  if (a.logprob && rank == 0) {
-    const int y = a.target[t];
+  if (a.logprob && rank == 0 && block == 0) {
+    y = __ldg(a.target + t);
     if (y >= 0 && y < a.classes) zy = to_f32<T>(zr[y]);
   }
-  const auto part = sum_part<T, G, true, 4>(row, 0, row.count, a.classes, rank, a.c, get);
-  const RowSums sums = join_group<T, G, true>(part, row, 0, row.count, a.classes, a.c, get, join_s[slot]);
-  const RowSays says = write_row(a, t, sums, zy, rank == 0);
-  if (a.k == 0) return;
-  int have = 0;
-  if (!says.bad && !sums.none) {
-    const uint32_t mine = part.s == 0 ? 0u : key_of(part.m);
-    have = select_largest<T, G>(row, 0, row.count, a.classes, a.k, mine, get, select_s[slot],
-                                [&](int r, uint32_t key, int i) { put_top(a, t, says, r, key, i); });
+  const auto part = sum_part<T, G, true, 4>(row, at, a.classes, rank, a.c, get);
+  select.key[rank] = part.key();
+  RowSums sums = join_block<T, G, true>(part, row, at, a.classes, a.c, get, join, [&] {
+    if (a.k) find_threshold<G>(select, a.k);
+  });
+  if constexpr (CL == 1) {
+    const RowSays says(sums);
+    if (rank == 0) put_row(a, t, says, y, zy);
+    if (a.k == 0) return;
+    int have = 0;
+    if (!says.bad && !says.none)
+      have = select_largest<T, G>(row, at, begin, end, a.classes, a.k, get, select,
+                                  [&](int r, Found f) { put_top(a, t, says, r, f); });
+    fill_top(a, t, have, says.bad, rank, G);
+  } else {
+    // each block's best, which the first one ranks against each other
+    int have = 0;
+    if (a.k && !isnan(sums.m) && !sums.none)
+      have = select_largest<T, G>(row, at, begin, end, a.classes, a.k, get, select, [&](int r, Found f) { best_s[r] = f; });
+    if (rank == 0) {
+      part_s = sums;
+      have_s = have;
+    }
+    ptx::cluster_sync();
+    if (block == 0) {
+      auto far = [](const void* p, int b) { return ptx::mapa(ptx::smem_u32(p), b); };
+      auto load = [](uint32_t p) {
+        uint32_t v;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(p) : "memory");
+        return v;
+      };
+      RowSums of[CL];
+      int n[CL], all = 0;
+      uint32_t top = 0;
+#pragma unroll
+      for (int b = 0; b < CL; ++b) {
+        of[b].m = __uint_as_float(load(far(&part_s.m, b)));
+        of[b].others = __uint_as_float(load(far(&part_s.others, b)));
+        of[b].q = __uint_as_float(load(far(&part_s.q, b)));
+        n[b] = (int)load(far(&have_s, b));
+        all += n[b];
+        of[b].none = of[b].m == -INFINITY;
+        top = max(top, of[b].none ? 0u : isnan(of[b].m) ? kNanKey : ops::key_of(of[b].m));
+      }
+      sums.none = top == 0;
+      sums.m = sums.none ? -INFINITY : top >= kNanKey ? NAN : value_of(top);
+      sums.others = sums.q = 0.f;
+      bool out = false;  // one block's maximum stands outside the others
+#pragma unroll
+      for (int b = 0; b < CL; ++b) {
+        if (of[b].none) continue;
+        const float delta = fmaxf((of[b].m - sums.m) * a.c, kLeast), f = exp2_of(delta);
+        const bool own = !out && of[b].m == sums.m;
+        out = out || own;
+        sums.others += f * (own ? of[b].others : 1.f + of[b].others);
+        sums.q += f * (of[b].q + delta * (1.f + of[b].others));
+      }
+      const RowSays says(sums);
+      if (rank == 0) put_row(a, t, says, y, zy);
+      if (says.bad) all = 0;
+      // the blocks' lists side by side, each in falling order
+      if (all) {
+#pragma unroll
+        for (int b = 0; b < CL; ++b)
+          for (int i = rank; i < n[b]; i += G) {
+            Found f;
+            asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(f) : "r"(far(best_s + i, b)) : "memory");
+            select.found[b * LIPCACHE_MAX_TOP + i] = f;
+          }
+        __syncthreads();
+        for (int i = rank; i < CL * a.k; i += G) {
+          const int b = i / a.k, j = i - b * a.k;
+          int count = 0;
+#pragma unroll
+          for (int o = 0; o < CL; ++o)
+            if (o == b) count = n[o];
+          if (j >= count) continue;
+          const Found own = select.found[b * LIPCACHE_MAX_TOP + j];
+          int r = j;
+#pragma unroll
+          for (int o = 0; o < CL; ++o) {
+            if (o == b) continue;
+            int lo = 0, hi = n[o];  // of the other list, those above
+            while (lo < hi) {
+              const int mid = (lo + hi) / 2;
+              if (select.found[o * LIPCACHE_MAX_TOP + mid] > own)
+                lo = mid + 1;
+              else
+                hi = mid;
+            }
+            r += lo;
+          }
+          if (r < a.k) put_top(a, t, says, r, own);
+        }
+      }
+      if (a.k) fill_top(a, t, min(all, a.k), says.bad, rank, G);
+    }
+    ptx::cluster_sync();  // (until the first one has read)
   }
-  fill_top(a, t, have, says.bad ? NAN : -INFINITY, rank, G);
+}
+
+template <typename T, int L, int U>
+void launch_lanes(const T* z, const ProbArgs& a, cudaStream_t s) {
+  launch_pdl(k_probs_lanes<T, L, U>, dim3((unsigned)ceil_div(a.tokens, 4 * (32 / L))), 128, s, z, a);
+}
+template <typename T, int L>
+bool probs_lanes(const T* z, const ProbArgs& a, int granules, cudaStream_t s) {
+  constexpr int kMost = sizeof(T) == 4 ? 8 : 4;  // 32 values a lane
+  if (granules > L * kMost || 4 * a.k > 3 * L) return false;
+  if (granules <= L)
+    launch_lanes<T, L, 1>(z, a, s);
+  else if (granules <= 2 * L)
+    launch_lanes<T, L, 2>(z, a, s);
+  else if (granules <= 4 * L)
+    launch_lanes<T, L, 4>(z, a, s);
+  else
+    launch_lanes<T, L, kMost>(z, a, s);
+  return true;
+}
+
+template <typename T, int G, int CL>
+void launch_blocks(const T* z, const ProbArgs& a, cudaStream_t s) {
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CL;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.tokens * CL));
+  cfg.blockDim = dim3(G);
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = CL > 1 ? 2 : 1;
+  LC_CUDA(cudaLaunchKernelEx(&cfg, k_probs<T, G, CL>, z, a));
 }
 
 template <typename T>
 void launch_probs(const T* z, const ProbArgs& a, cudaStream_t s) {
-  const int granules = (int)ceil_div(a.classes, Vec<T>::N) + 1;
-  if (granules <= 257 && a.k <= 32)
-    launch_pdl(k_probs<T, 32>, dim3((unsigned)ceil_div(a.tokens, 4)), 128, s, z, a);
-  else if (granules <= 2048)
-    launch_pdl(k_probs<T, 128>, dim3((unsigned)a.tokens), 128, s, z, a);
-  else
-    launch_pdl(k_probs<T, 512>, dim3((unsigned)a.tokens), 512, s, z, a);
+  // granules of a row, one more where rows start inside one
+  const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
+  if (probs_lanes<T, 8>(z, a, granules, s) || probs_lanes<T, 16>(z, a, granules, s) || probs_lanes<T, 32>(z, a, granules, s)) {
+  } else if (granules >= 2048 && a.tokens <= 48) {
+    launch_blocks<T, 256, 8>(z, a, s);
+  } else if (granules <= 2048 && a.k <= 64) {
+    launch_blocks<T, 128, 1>(z, a, s);
+  } else {
+    launch_blocks<T, 256, 1>(z, a, s);
+  }
   LC_LAUNCH_CHECK("k_probs");
 }
 

@@ -164,14 +164,6 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 
 // ---------------------------------------------------------------- softmax sums
-// What a group leaves for its threads between two barriers.
-template <int G>
-struct JoinShared {
-  static constexpr int W = G / 32;
-  uint32_t top[W];
-  float s[W], q[W], own[W];
-};
-
 // Of a set of logits with t = (z - m) / T, in units of log 2: m its maximum,
 // 1 + others the sum of exp2(t), q the sum of exp2(t) t (<= 0). One of the values
 // that are m stands outside `others`, so that a sure row's logarithm is
@@ -199,128 +191,266 @@ __device__ __forceinline__ uint64_t bounded(uint64_t t) {
 template <typename T, bool MEAN>
 struct RowPart {
   static constexpr int N = Vec<T>::N;
+  // BF16 values are raised to `floor` two at a time, before they are opened: a
+  // value that far below m whose t is finite. Maxima of 2^100 or more have none.
+  static constexpr bool kFloor = MEAN && sizeof(T) == 2;
   float m = -3.402823466e38f;
   uint64_t s = 0, q = 0;
+  uint32_t floor = 0;
+  bool wide = true;
+  template <int U>
+  __device__ __forceinline__ float top_of(const uint4 (&w)[U]) const {
+    if constexpr (sizeof(T) == 4) {
+      float top = top_nan<T>(w[0]);
+#pragma unroll
+      for (int u = 1; u < U; ++u) top = max_nan(top, top_nan<T>(w[u]));
+      return top;
+    } else {
+      __nv_bfloat162 m = *reinterpret_cast<const __nv_bfloat162*>(&w[0].x);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w[u]);
+        m = __hmax2_nan(m, __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3])));
+      }
+      return max_nan(__low2float(m), __high2float(m));
+    }
+  }
   template <int U>
   __device__ __forceinline__ void add(const uint4 (&w)[U], float c) {
-    float top = top_nan<T>(w[0]);
-#pragma unroll
-    for (int u = 1; u < U; ++u) top = max_nan(top, top_nan<T>(w[u]));
-    top = max_nan(top, m);
+    const float top = max_nan(top_of(w), m);
     if (top != m) {
-      const float delta = fmaxf((m - top) * c, kLeast);
-      const uint64_t f = both(exp2_of(delta));
-      if (MEAN) q = ptx::mul_f32x2(f, ptx::fma_f32x2(both(delta), s, q));
-      s = ptx::mul_f32x2(f, s);
+      const float delta = fmaxf((m - top) * c, kLeast), f = exp2_of(delta);
+      if (MEAN) q = ptx::mul_f32x2(both(f), ptx::fma_f32x2(both(delta), s, q));
+      s = ptx::mul_f32x2(both(f), s);
       m = top;
+      if (kFloor) {
+        wide = !(fabsf(m) < 1.2676506e30f);
+        const uint32_t bits = __float_as_uint(m - 500.f / c - fabsf(m) * 0.015625f);
+        // (rounded down: two steps of BF16 below m at least)
+        const uint32_t low = (bits >> 31 ? bits + 0xffffu : bits) >> 16;
+        floor = low | low << 16;
+      }
     }
+    if (wide)
+      accumulate<U, false>(w, c);
+    else
+      accumulate<U, kFloor>(w, c);
+  }
+  template <int U, bool FLOOR>
+  __device__ __forceinline__ void accumulate(const uint4 (&w)[U], float c) {
     const uint64_t minus_m = both(-m), cc = both(c);
+    const __nv_bfloat162 low = *reinterpret_cast<const __nv_bfloat162*>(&floor);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      uint4 x = w[u];
+      if constexpr (FLOOR) {
+        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __hmax2(h[i], low);
+      }
       uint64_t v[N / 2];
-      Vec<T>::open(w[u], v);
+      Vec<T>::open(x, v);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
         uint64_t t = shifted(v[i], minus_m, cc);
-        if (MEAN) t = bounded(t);
+        if (MEAN && !FLOOR) t = bounded(t);
         const uint64_t e = exp2_pair(t);
         s = ptx::add_f32x2(s, e);
         if (MEAN) q = ptx::fma_f32x2(e, t, q);
       }
     }
   }
+  // 0: nothing above -inf (s is 0; of a part that saw NaN it may be, too)
+  __device__ __forceinline__ uint32_t key() const {
+    return s == 0 && m <= 3.402823466e38f ? 0u : key_of(m);
+  }
 };
 
-// The part of thread `rank` of G in granules [begin, end) of a row: U at a time.
+// Which granules of [begin, end) of a row are a thread's: those inside the row go
+// round robin, the first and last one, if they reach outside, are thread 0's and 1's.
+struct Slice {
+  int first, last;  // granules inside the row, from first up to last
+  int head, tail;   // the others, -1: none
+  template <typename T>
+  __device__ __forceinline__ Slice(const RowSpan<T>& row, int begin, int end, int n) : first(begin), last(end), head(-1), tail(-1) {
+    if (begin < end && row.edge(begin, n)) head = first++;
+    if (first < last && row.edge(last - 1, n)) tail = --last;
+  }
+};
+
+// The part of thread `rank` of G: U granules at a time.
 template <typename T, int G, bool MEAN, int U, typename Get>
-__device__ __forceinline__ RowPart<T, MEAN> sum_part(const RowSpan<T>& row, int begin, int end, int n, int rank, float c,
+__device__ __forceinline__ RowPart<T, MEAN> sum_part(const RowSpan<T>& row, const Slice& at, int n, int rank, float c,
                                                      Get get) {
   RowPart<T, MEAN> part;
-  const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
-  for (int i = begin + rank; i < end; i += U * G) {
+  int i = at.first + rank;
+  for (; i + (U - 1) * G < at.last; i += U * G) {
     uint4 w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = i + u * G < end ? get(i + u * G) : uint4{none, none, none, none};
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * G < end && row.edge(i + u * G, n)) w[u] = masked_outside<T>(w[u], row.first(i + u * G), n);
+    for (int u = 0; u < U; ++u) w[u] = get(i + u * G);
+    part.add(w, c);
+  }
+  for (; i < at.last; i += G) {
+    const uint4 w[1] = {get(i)};
+    part.add(w, c);
+  }
+  const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
+  if (edge >= 0) {
+    const uint4 w[1] = {masked_outside<T>(get(edge), row.first(edge), n)};
     part.add(w, c);
   }
   return part;
 }
 
-// The group's sums from its threads'. Where the row is nearly sure, the sum of the
+// What a group's warps leave for each other between barriers.
+template <int G>
+struct JoinShared {
+  static constexpr int W = G / 32;
+  uint32_t top[W];
+  float s[W], q[W], own, again;
+};
+
+// The block's sums from its threads'. Where the row is nearly sure, the sum of the
 // thread that holds the maximum has lost the others' last bits beside it: its warp
-// takes that thread's granules again.
-template <typename T, int G, bool MEAN, typename Get>
-__device__ __forceinline__ RowSums join_group(const RowPart<T, MEAN>& part, const RowSpan<T>& row, int begin, int end,
-                                              int n, float c, Get get, JoinShared<G>& sh) {
+// takes that thread's granules again. meanwhile(): what warp 0 does between the two
+// barriers.
+template <typename T, int G, bool MEAN, typename Get, typename F>
+__device__ __forceinline__ RowSums join_block(const RowPart<T, MEAN>& part, const RowSpan<T>& row, const Slice& at, int n,
+                                              float c, Get get, JoinShared<G>& sh, F&& meanwhile) {
   constexpr int W = G / 32;
   constexpr uint32_t kAll = 0xffffffffu;
-  const int lane = threadIdx.x & 31, warp = G == 32 ? 0 : threadIdx.x >> 5;
-  float s = lo_f32(part.s) + hi_f32(part.s), q = MEAN ? lo_f32(part.q) + hi_f32(part.q) : 0.f;
-  // (a thread that saw nothing above -inf has s = 0; one that saw NaN may have)
-  const uint32_t key = s == 0.f && part.m <= 3.402823466e38f ? 0u : key_of(part.m);
-  const uint32_t warp_key = __reduce_max_sync(kAll, key);
-  uint32_t top = warp_key;
-  int winner_warp = 0;
-  if (W > 1) {
-    if (lane == 0) sh.top[warp] = warp_key;
-    __syncthreads();
-    const uint32_t other = sh.top[lane % W];
-    top = __reduce_max_sync(kAll, other);
-    winner_warp = __ffs(__ballot_sync(kAll, other == top)) - 1;
-  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t key = part.key(), warp_key = __reduce_max_sync(kAll, key);
+  if (lane == 0) sh.top[warp] = warp_key;
+  __syncthreads();
+  const uint32_t other = sh.top[lane % W], top = __reduce_max_sync(kAll, other);
+  const int winner_warp = __ffs(__ballot_sync(kAll, other == top)) - 1;
   RowSums r;
   r.none = top == 0;
-  r.m = r.none ? -INFINITY : value_of(top);
-  if (top >= kNanKey) r.m = NAN;
+  r.m = r.none ? -INFINITY : top >= kNanKey ? NAN : value_of(top);
   const float delta = fmaxf((part.m - r.m) * c, kLeast), f = exp2_of(delta);
-  if (MEAN) q = s == 0.f ? 0.f : f * (q + delta * s);
+  float s = lo_f32(part.s) + hi_f32(part.s), q = 0.f;
+  if (MEAN) q = s == 0.f ? 0.f : f * (lo_f32(part.q) + hi_f32(part.q) + delta * s);
   s = s == 0.f ? 0.f : f * s;
-  const int winner = warp == winner_warp ? __ffs(__ballot_sync(kAll, key == top)) - 1 : -1;
-  float own = 0.f;
-  if (lane == winner) {
-    own = s - 1.f;
-    s = 0.f;
+  int winner = -1;
+  if (warp == winner_warp) {
+    winner = __ffs(__ballot_sync(kAll, key == top)) - 1;
+    if (lane == winner) {
+      sh.own = s - 1.f;
+      s = 0.f;
+    }
   }
   s = warp_sum(s);
   if (MEAN) q = warp_sum(q);
-  if (winner >= 0) own = __shfl_sync(kAll, own, winner);
-  if (W > 1) {
-    if (lane == 0) {
-      sh.s[warp] = s;
-      sh.q[warp] = q;
-      if (warp == winner_warp) sh.own[0] = own;
-    }
-    __syncthreads();
-    s = warp_sum(lane < W ? sh.s[lane % W] : 0.f);
-    if (MEAN) q = warp_sum(lane < W ? sh.q[lane % W] : 0.f);
-    own = sh.own[0];
+  if (lane == 0) {
+    sh.s[warp] = s;
+    sh.q[warp] = q;
   }
-  if (s + own < 0.0625f && !r.none) {  // (the same for the whole group)
+  if (warp == 0) meanwhile();
+  __syncthreads();
+  s = sh.s[0];
+  q = sh.q[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) {
+    s += sh.s[i];
+    if (MEAN) q += sh.q[i];
+  }
+  float own = sh.own;
+  if (s + own < 0.0625f && !r.none) {  // (the same for the whole block)
     if (warp == winner_warp) {
       const int thread = warp * 32 + winner;
       float again = 0.f;
-      for (int i = begin + thread + lane * G; i < end; i += 32 * G) {
+      auto take = [&](int i, bool edge) {
         uint4 w = get(i);
-        if (row.edge(i, n)) w = masked_outside<T>(w, row.first(i), n);
+        if (edge) w = masked_outside<T>(w, row.first(i), n);
 #pragma unroll
         for (int j = 0; j < Vec<T>::N; ++j) {
           const float z = Vec<T>::at(w, j);
           if (z < r.m) again += exp2_of((z - r.m) * c);
         }
-      }
-      own = warp_sum(again);
-      if (W > 1 && lane == 0) sh.own[1] = own;
+      };
+      for (int i = at.first + thread + lane * G; i < at.last; i += 32 * G) take(i, false);
+      const int edge = thread == 0 ? at.head : thread == 1 ? at.tail : -1;
+      if (lane == 0 && edge >= 0) take(edge, true);
+      again = warp_sum(again);
+      if (lane == 0) sh.again = again;
     }
-    if (W > 1) {
-      __syncthreads();
-      own = sh.own[1];
-    }
+    __syncthreads();
+    own = sh.again;
   }
   r.others = s + own;
   r.q = q;
+  return r;
+}
+
+// ---------------------------------------------------------------- rows on a few lanes
+// A row on L lanes of a warp, all of it in their registers: U granules a lane, granule
+// u L + lane. What lies outside the row is -inf.
+template <typename T, int L, int U>
+struct LaneRow {
+  static constexpr int N = Vec<T>::N;
+  uint4 w[U];
+  __device__ __forceinline__ void load(const RowSpan<T>& row, int n, int lane, bool live) {
+    const uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      w[u] = live && u * L + lane < row.count ? row.granules[u * L + lane] : uint4{none, none, none, none};
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u * L + lane < row.count && row.edge(u * L + lane, n)) w[u] = masked_outside<T>(w[u], row.first(u * L + lane), n);
+  }
+  __device__ __forceinline__ float at(int u, int j) const { return Vec<T>::at(w[u], j); }
+};
+// Sum, and maximum of keys, over the L lanes.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <int L>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  if constexpr (L == 32) {
+    return __reduce_max_sync(0xffffffffu, v);
+  } else {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  }
+}
+// Its sums, on all of its lanes; `mine`: the lane's own maximum's key.
+template <typename T, int L, int U, bool MEAN>
+__device__ __forceinline__ RowSums sum_lanes(const LaneRow<T, L, U>& row, int lane, float c, uint32_t& mine) {
+  constexpr int N = Vec<T>::N;
+  RowPart<T, MEAN> part;
+  const float own = part.top_of(row.w);
+  mine = own == -INFINITY ? 0u : key_of(own);
+  const uint32_t top = lanes_max<L>(mine);
+  RowSums r;
+  r.none = top == 0;
+  r.m = r.none ? 0.f : top >= kNanKey ? NAN : value_of(top);
+  part.m = r.m;
+  part.template accumulate<U, false>(row.w, c);
+  float s = lo_f32(part.s) + hi_f32(part.s), q = MEAN ? lo_f32(part.q) + hi_f32(part.q) : 0.f;
+  const uint32_t holders = __ballot_sync(0xffffffffu, mine == top) >> (threadIdx.x & 31 & ~(L - 1));
+  const bool holds = mine == top && !(holders & ((1u << lane) - 1));
+  if (holds) s -= 1.f;
+  r.others = lanes_sum<L>(s);
+  if (__any_sync(0xffffffffu, r.others < 0.0625f && !r.none)) {
+    // a nearly sure row: beside its maximum the lane's sum has lost the others' last bits
+    float again = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float z = row.at(u, j);
+        if (z < r.m) again += exp2_of((z - r.m) * c);
+      }
+    const float anew = lanes_sum<L>(holds ? again : s);
+    if (r.others < 0.0625f) r.others = anew;
+  }
+  r.q = MEAN ? lanes_sum<L>(q) : 0.f;
+  if (r.none) r.m = -INFINITY;
   return r;
 }
 
