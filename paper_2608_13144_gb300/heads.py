@@ -40,6 +40,7 @@ QUINTIC = (3.4445, -4.7750, 2.0315)
 
 I32, F32 = torch.int32, torch.float32
 _grads = torch.is_grad_enabled
+_empty = torch.empty
 #: tells autograd that tensors were written to, so that a gradient that needs the old values raises
 _written = torch.autograd.graph.increment_version
 #: struct lipcache_adapted, packed: half the time of filling ctypes' Adapted
@@ -269,37 +270,26 @@ class LogProbs(NamedTuple):
     index: torch.Tensor | None  #: n x k (int32): those classes
 
 
-def _logits(logits: torch.Tensor, target: torch.Tensor | None):
-    """The type, device and sizes of rows of logits, and their classes' check."""
-    ty, at = _type(logits, "logits"), _gpu(logits, "logits")
-    _check(logits, "logits", 2, at, logits.dtype)
+def _logits(logits: torch.Tensor):
+    """The type, device, and shape of rows of logits."""
+    dt, at = logits.dtype, logits.get_device()
+    if dt not in TYPES or at < 0 or logits.dim() != 2:
+        _type(logits, "logits")
+        _gpu(logits, "logits")
+        _check(logits, "logits", 2, at, dt)
     n, c = logits.shape
-    _int32(c)
-    if target is not None:
-        _check(target, "target", 1, at, I32)
-        if len(target) != n:
-            raise ValueError("target must have an entry per row of logits")
-        target = target.contiguous()
-    return ty, at, n, c, target
+    if c > 0x7fffffff:
+        _int32(c)
+    return TYPES[dt], at, n, c
 
 
-def _per_row(t: torch.Tensor | None, name: str, n: int, at: int):
-    if t is None:
-        return None
-    _check(t, name, 1, at, F32)
-    if len(t) != n:
-        raise ValueError(f"{name} must have an entry per row")
-    return t.contiguous()
-
-
-def _gradient(logits: torch.Tensor, in_place: bool):
-    """Rows of logits, their stride, and where their gradient goes."""
-    z, ldz = _rows(logits)
-    if not in_place:
-        return z, ldz, torch.empty(logits.shape, dtype=logits.dtype, device=logits.device), logits.shape[1]
-    if z is not logits:
-        raise ValueError("in_place needs logits with dense rows")
-    return z, ldz, z, ldz
+def _entries(t: torch.Tensor, name: str, n: int, at: int, dtype: torch.dtype, what: str) -> torch.Tensor:
+    """A contiguous vector of n entries."""
+    if t.dtype != dtype or t.get_device() != at or t.dim() != 1:
+        _check(t, name, 1, at, dtype)
+    if t.shape[0] != n:
+        raise ValueError(f"{name} must have an entry per {what}")
+    return t if t.is_contiguous() else t.contiguous()
 
 
 def log_probs(logits: torch.Tensor, target: torch.Tensor | None = None, top: int = 0,
@@ -311,22 +301,36 @@ def log_probs(logits: torch.Tensor, target: torch.Tensor | None = None, top: int
 
     logits: n x C; target: n (int32; a value outside [0, C) has log-probability
     0)."""
-    ty, at, n, c, target = _logits(logits, target)
+    ty, at, n, c = _logits(logits)
     if logits.requires_grad and _grads():
         _recorded(logits=logits)
-    top = int(top)
     if not 0 <= top <= 128:
         raise ValueError("top must be in [0, 128]")
     z, ldz = _rows(logits)
-    device, k = z.device, top > 0
-    entropy, norm = torch.empty(n, dtype=F32, device=device), torch.empty(n, 3, dtype=F32, device=device)
-    logprob = None if target is None else torch.empty(n, dtype=F32, device=device)
-    best = torch.empty(n, top, dtype=F32, device=device) if k else None
-    index = torch.empty(n, top, dtype=I32, device=device) if k else None
-    _call(at, _lib.load().lipcache_log_probs, ty, z.data_ptr(), ldz, n, c, None if target is None else target.data_ptr(),
-          top, float(temperature), None if logprob is None else logprob.data_ptr(), entropy.data_ptr(), norm.data_ptr(),
-          best.data_ptr() if k else None, index.data_ptr() if k else None)
+    device = z.device
+    logprob = best = index = y = lp = bp = ip = None
+    if target is not None:
+        target = _entries(target, "target", n, at, I32, "row of logits")
+        y = target.data_ptr()
+        logprob = _empty(n, dtype=F32, device=device)
+        lp = logprob.data_ptr()
+    entropy, norm = _empty(n, dtype=F32, device=device), _empty((n, 3), dtype=F32, device=device)
+    if top:
+        best, index = _empty((n, top), dtype=F32, device=device), _empty((n, top), dtype=I32, device=device)
+        bp, ip = best.data_ptr(), index.data_ptr()
+    _call(at, _lib.load().lipcache_log_probs, ty, z.data_ptr(), ldz, n, c, y, top, temperature, lp, entropy.data_ptr(),
+          norm.data_ptr(), bp, ip)
     return LogProbs(logprob, entropy, norm, best, index)
+
+
+def _gradient(logits: torch.Tensor, in_place: bool):
+    """Rows of logits, their stride, and where their gradient goes."""
+    z, ldz = _rows(logits)
+    if not in_place:
+        return z, ldz, _empty(logits.shape, dtype=logits.dtype, device=logits.device), logits.shape[1]
+    if z is not logits:
+        raise ValueError("in_place needs logits with dense rows")
+    return z, ldz, z, ldz
 
 
 def log_probs_backward(logits: torch.Tensor, norm: torch.Tensor, target: torch.Tensor | None = None,
@@ -335,20 +339,29 @@ def log_probs_backward(logits: torch.Tensor, norm: torch.Tensor, target: torch.T
     """The gradient of the logits for the gradients dlogprob and dentropy (n,
     float32; None: 0) of log_probs' results; norm, target and temperature are
     that call's. Overwrites logits with in_place."""
-    ty, at, n, c, target = _logits(logits, target)
+    ty, at, n, c = _logits(logits)
     _check(norm, "norm", 2, at, F32)
-    if _grads():
-        _recorded(logits=logits, norm=norm, dlogprob=dlogprob, dentropy=dentropy)
     if norm.shape != (n, 3):
         raise ValueError("norm must be n x 3")
-    if dlogprob is not None and target is None:
-        raise ValueError("dlogprob needs a target")
+    if _grads() and (logits.requires_grad or norm.requires_grad or dlogprob is not None and dlogprob.requires_grad
+                    or dentropy is not None and dentropy.requires_grad):
+        _recorded(logits=logits, norm=norm, dlogprob=dlogprob, dentropy=dentropy)
     norm = norm.contiguous()
-    dlogprob, dentropy = _per_row(dlogprob, "dlogprob", n, at), _per_row(dentropy, "dentropy", n, at)
+    y = g = h = None
+    if target is not None:
+        target = _entries(target, "target", n, at, I32, "row of logits")
+        y = target.data_ptr()
+    if dlogprob is not None:
+        if target is None:
+            raise ValueError("dlogprob needs a target")
+        dlogprob = _entries(dlogprob, "dlogprob", n, at, F32, "row of logits")
+        g = dlogprob.data_ptr()
+    if dentropy is not None:
+        dentropy = _entries(dentropy, "dentropy", n, at, F32, "row of logits")
+        h = dentropy.data_ptr()
     z, ldz, dz, ldd = _gradient(logits, in_place)
-    _call(at, _lib.load().lipcache_log_probs_backward, ty, z.data_ptr(), ldz, n, c, norm.data_ptr(),
-          None if target is None else target.data_ptr(), None if dlogprob is None else dlogprob.data_ptr(),
-          None if dentropy is None else dentropy.data_ptr(), float(temperature), dz.data_ptr(), ldd)
+    _call(at, _lib.load().lipcache_log_probs_backward, ty, z.data_ptr(), ldz, n, c, norm.data_ptr(), y, g, h, temperature,
+          dz.data_ptr(), ldd)
     if in_place:
         _written(dz)
     return dz
@@ -364,7 +377,7 @@ def distill(logits: torch.Tensor, top: torch.Tensor, index: torch.Tensor, weight
     logits: n x C; top: n x k (float32: the teacher's logits, or
     log-probabilities at temperature 1); index: n x k (int32; an entry outside
     [0, C) is left out, a row without any has loss 0); weight: n (float32)."""
-    ty, at, n, c, _ = _logits(logits, None)
+    ty, at, n, c = _logits(logits)
     _check(top, "top", 2, at, F32)
     _check(index, "index", 2, at, I32)
     if _grads() and (logits.requires_grad or top.requires_grad or weight is not None and weight.requires_grad):
@@ -372,28 +385,35 @@ def distill(logits: torch.Tensor, top: torch.Tensor, index: torch.Tensor, weight
     k = top.shape[1]
     if top.shape != (n, k) or index.shape != (n, k) or not 1 <= k <= 128:
         raise ValueError("top and index must be n x k, k in [1, 128]")
-    top, index, weight = top.contiguous(), index.contiguous(), _per_row(weight, "weight", n, at)
-    dz, ldd = None, c
+    top, index = top.contiguous(), index.contiguous()
+    w = dz = dp = None
+    if weight is not None:
+        weight = _entries(weight, "weight", n, at, F32, "row of logits")
+        w = weight.data_ptr()
     if need_grad:
         z, ldz, dz, ldd = _gradient(logits, in_place)
+        dp = dz.data_ptr()
     else:
         z, ldz = _rows(logits)
-    loss = torch.empty(n, dtype=F32, device=z.device)
-    _call(at, _lib.load().lipcache_distill, ty, z.data_ptr(), ldz, n, c, k, top.data_ptr(), index.data_ptr(),
-          None if weight is None else weight.data_ptr(), float(temperature), loss.data_ptr(),
-          dz.data_ptr() if need_grad else None, ldd)
+        ldd = c
+    loss = _empty(n, dtype=F32, device=z.device)
+    _call(at, _lib.load().lipcache_distill, ty, z.data_ptr(), ldz, n, c, k, top.data_ptr(), index.data_ptr(), w,
+          temperature, loss.data_ptr(), dp, ldd)
     if in_place and need_grad:
         _written(dz)
     return loss, dz
 
 
-def _columns(t: torch.Tensor | None, name: str, d: int, at: int):
-    if t is None:
-        return None
-    _check(t, name, 1, at, F32)
-    if len(t) != d:
-        raise ValueError(f"{name} must have an entry per feature")
-    return t.contiguous()
+def _features(x: torch.Tensor):
+    dt, at = x.dtype, x.get_device()
+    if dt not in TYPES or at < 0 or x.dim() != 2:
+        _type(x, "x")
+        _gpu(x, "x")
+        _check(x, "x", 2, at, dt)
+    n, d = x.shape
+    if d > 0x7fffffff:
+        _int32(d)
+    return dt, at, n, d
 
 
 def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
@@ -402,28 +422,32 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     of x (n x d), and the rows' mean and 1 / sqrt(var + eps) (n x 2, float32),
     which layer_norm_backward needs. weight, bias: d (float32); out must not
     overlap the other tensors."""
-    ty, at = _type(x, "x"), _gpu(x, "x")
-    _check(x, "x", 2, at, x.dtype)
-    n, d = x.shape
-    _int32(d)
-    if _grads():
+    dt, at, n, d = _features(x)
+    if _grads() and (x.requires_grad or weight is not None and weight.requires_grad or bias is not None
+                    and bias.requires_grad or out is not None and out.requires_grad):
         _recorded(x=x, weight=weight, bias=bias, out=out)
-    weight, bias = _columns(weight, "weight", d, at), _columns(bias, "bias", d, at)
+    w = b = None
+    if weight is not None:
+        weight = _entries(weight, "weight", d, at, F32, "feature")
+        w = weight.data_ptr()
+    if bias is not None:
+        bias = _entries(bias, "bias", d, at, F32, "feature")
+        b = bias.data_ptr()
     x, ldx = _rows(x)
-    own = out is None
-    if own:
-        out, ldy = torch.empty(n, d, dtype=x.dtype, device=x.device), d
+    device = x.device
+    if out is None:
+        y, ldy = _empty((n, d), dtype=dt, device=device), d
     else:
-        _check(out, "out", 2, at, x.dtype)
-        rows, ldy = _rows(out)
-        if out.shape != (n, d) or rows is not out:
+        _check(out, "out", 2, at, dt)
+        y, ldy = _rows(out)
+        if out.shape != (n, d) or y is not out:
             raise ValueError("out must be n x d with dense rows")
-    stats = torch.empty(n, 2, dtype=F32, device=x.device)
-    _call(at, _lib.load().lipcache_layer_norm, ty, x.data_ptr(), ldx, n, d, None if weight is None else weight.data_ptr(),
-          None if bias is None else bias.data_ptr(), float(eps), out.data_ptr(), ldy, stats.data_ptr())
-    if not own:
+    stats = _empty((n, 2), dtype=F32, device=device)
+    _call(at, _lib.load().lipcache_layer_norm, TYPES[dt], x.data_ptr(), ldx, n, d, w, b, eps, y.data_ptr(), ldy,
+          stats.data_ptr())
+    if out is not None:
         _written(out)
-    return out, stats
+    return y, stats
 
 
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, weight: torch.Tensor | None = None,
@@ -431,28 +455,38 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, 
     """(dx, dweight, dbias) of layer_norm for the gradient dy (n x d) of its
     result; stats are that call's. dx has x's type, dweight and dbias are
     float32; an output that is not needed is None."""
-    ty, at = _type(x, "x"), _gpu(x, "x")
-    _check(x, "x", 2, at, x.dtype)
-    _check(dy, "dy", 2, at, x.dtype)
+    dt, at, n, d = _features(x)
+    _check(dy, "dy", 2, at, dt)
     _check(stats, "stats", 2, at, F32)
-    n, d = x.shape
-    _int32(d)
-    if _grads():
+    if _grads() and (dy.requires_grad or x.requires_grad or stats.requires_grad or weight is not None
+                    and weight.requires_grad):
         _recorded(dy=dy, x=x, stats=stats, weight=weight)
     if dy.shape != (n, d) or stats.shape != (n, 2):
         raise ValueError("dy must be n x d and stats n x 2")
-    weight, stats = _columns(weight, "weight", d, at), stats.contiguous()
+    ty, device = TYPES[dt], x.device
+    dx = dweight = dbias = ws = w = dxp = dwp = dbp = wsp = None
+    nbytes = 0
+    if weight is not None:
+        weight = _entries(weight, "weight", d, at, F32, "feature")
+        w = weight.data_ptr()
+    stats = stats.contiguous()
     x, ldx = _rows(x)
     dy, lddy = _rows(dy)
-    device = x.device
-    dx = torch.empty(n, d, dtype=x.dtype, device=device) if need_dx else None
-    dweight = torch.empty(d, dtype=F32, device=device) if need_dweight else None
-    dbias = torch.empty(d, dtype=F32, device=device) if need_dbias else None
-    ws = _workspace(_norm_bytes(ty, n, d), device)
+    if need_dx:
+        dx = _empty((n, d), dtype=dt, device=device)
+        dxp = dx.data_ptr()
+    if need_dweight:
+        dweight = _empty(d, dtype=F32, device=device)
+        dwp = dweight.data_ptr()
+    if need_dbias:
+        dbias = _empty(d, dtype=F32, device=device)
+        dbp = dbias.data_ptr()
+    if need_dweight or need_dbias:
+        nbytes = _norm_bytes(ty, n, d)
+        ws = _workspace(nbytes, device)
+        wsp = ws.data_ptr()
     _call(at, _lib.load().lipcache_layer_norm_backward, ty, dy.data_ptr(), lddy, x.data_ptr(), ldx, n, d,
-          stats.data_ptr(), None if weight is None else weight.data_ptr(), dx.data_ptr() if need_dx else None, d,
-          dweight.data_ptr() if need_dweight else None, dbias.data_ptr() if need_dbias else None, ws.data_ptr(),
-          ws.numel())
+          stats.data_ptr(), w, dxp, d, dwp, dbp, wsp, nbytes)
     return dx, dweight, dbias
 
 
