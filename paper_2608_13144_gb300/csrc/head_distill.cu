@@ -116,20 +116,27 @@ struct Teacher {
   }
 };
 
-// The gradient w T p of a granule (factor = w T / sum), or `fill`.
-template <typename T>
-__device__ __forceinline__ uint4 gradient_of(const uint4& w, bool live, uint64_t minus_m, uint64_t c, uint64_t factor,
-                                             float fill) {
-  constexpr int N = Vec<T>::N;
-  uint64_t v[N / 2];
-  if (live) {
+// The gradient w T p of a row's granules.
+struct RowGradient {
+  uint64_t minus_m, c, factor;
+  __device__ __forceinline__ RowGradient(const DistillArgs& a, const RowSums& sums, float w)
+      : minus_m(both(-sums.m)), c(both(a.c)), factor(both(w * a.temperature / (1.f + sums.others))) {}
+  template <typename T>
+  __device__ __forceinline__ uint4 of(const uint4& w) const {
+    constexpr int N = Vec<T>::N;
+    uint64_t v[N / 2];
     Vec<T>::open(w, v);
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) v[j] = ptx::mul_f32x2(exp2_pair(shifted(v[j], minus_m, c)), factor);
-  } else {
-#pragma unroll
-    for (int j = 0; j < N / 2; ++j) v[j] = both(fill);
+    return Vec<T>::close(v);
   }
+};
+// A granule of `fill` (0 or NaN).
+template <typename T>
+__device__ __forceinline__ uint4 granule_of(float fill) {
+  uint64_t v[Vec<T>::N / 2];
+#pragma unroll
+  for (int j = 0; j < Vec<T>::N / 2; ++j) v[j] = both(fill);
   return Vec<T>::close(v);
 }
 
@@ -162,12 +169,12 @@ __global__ void __launch_bounds__(128) k_distill_lanes(const T* z, T* dz, const 
   if (!dz) return;
   T* dr = dz + t * a.ldd;
   const bool live = taught && !bad && !sums.none, same_place = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
-  const uint64_t minus_m = both(-sums.m), c = both(a.c), factor = both(w * a.temperature / (1.f + sums.others));
+  const RowGradient gradient(a, sums, w);
   if (is) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (u * L + lane < row.count)
-        put_granule<T>(dr, same_place, gradient_of<T>(r.w[u], live, minus_m, c, factor, bad ? NAN : 0.f),
+        put_granule<T>(dr, same_place, live ? gradient.of<T>(r.w[u]) : granule_of<T>(bad ? NAN : 0.f),
                        row.first(u * L + lane), a.classes);
   }
   __syncwarp();  // (the row's lanes have written what is written over here)
@@ -226,51 +233,51 @@ __global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(con
       twice_s = 0;
     }
   }
-  __syncthreads();
-  int live = live_s;  // 1: a row with a teacher, 2: its results are NaN
-  // whether a class is named twice: four threads an entry
-  for (int e = rank; e < 4 * a.k; e += G) {
-    const int entry = e >> 2, mine = index_s[entry];
-    if (mine >= 0)
-      for (int j = e & 3; j < entry; j += 4)
-        if (index_s[j] == mine) twice_s = 1;
-  }
-  RowSums sums{};
-  if (live == 1) {
-    RowPart<T, false> part;
-    if constexpr (RESIDENT) {
+  // the sums of any row: which have a teacher the other warps know from the join on
+  const Scale k{a.c, 0.f};
+  RowPart<T, false> part;
+  if constexpr (RESIDENT) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (k == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
-        if (k == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
-        if (k == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-        if (k == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
-        int i = at.first + k * U * G + rank;
-        if (i + (U - 1) * G < at.last) {
-          uint4 x[U];
+    for (int b = 0; b < 4; ++b) {
+      if (b == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      if (b == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
+      if (b == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      if (b == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      int i = at.first + b * U * G + rank;
+      const bool whole = i + (U - 1) * G < at.last;
+      uint4 x[U];
+      if (whole) {
 #pragma unroll
-          for (int u = 0; u < U; ++u) x[u] = row_s[i + u * G - begin];
-          part.add(x, a.c);
-        } else {
-          for (; i < at.last && i < at.first + (k + 1) * U * G; i += G) {
-            const uint4 x[1] = {row_s[i - begin]};
-            part.add(x, a.c);
-          }
+        for (int u = 0; u < U; ++u) x[u] = row_s[i + u * G - begin];
+      }
+      if (b == 0) part.start(whole ? part.top_of(x) : -INFINITY, k);
+      if (whole) {
+        part.add(x, k);
+      } else {
+        for (; i < at.last && i < at.first + (b + 1) * U * G; i += G) {
+          const uint4 one[1] = {row_s[i - begin]};
+          part.add(one, k);
         }
       }
-      const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
-      if (edge >= 0) {
-        const uint4 x[1] = {masked_outside<T>(get(edge), row.first(edge), a.classes)};
-        part.add(x, a.c);
-      }
-    } else {
-      part = sum_part<T, G, false, U>(row, at, a.classes, rank, a.c, get);
     }
-    sums = join_block<T, G, false>(part, row, at, a.classes, a.c, get, join, [] {});
+    const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
+    if (edge >= 0) {
+      const uint4 one[1] = {masked_outside<T>(get(edge), row.first(edge), a.classes)};
+      part.add(one, k);
+    }
   } else {
-    if constexpr (RESIDENT) asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncthreads();
+    part = sum_part<T, G, false, U>(row, at, a.classes, rank, k, get);
   }
+  RowSums sums = join_block<T, G, false>(part, row, at, a.classes, a.c, get, join, [&] {
+    // whether a class is named twice: four threads an entry
+    for (int e = rank; e < 4 * a.k; e += G) {
+      const int entry = e >> 2, mine = index_s[entry];
+      if (mine >= 0)
+        for (int j = e & 3; j < entry; j += 4)
+          if (index_s[j] == mine) twice_s = 1;
+    }
+  });
+  int live = live_s;  // 1: a row with a teacher, 2: its results are NaN
   if constexpr (CL > 1) {
     if (rank == 0) part_s = float2{sums.m, sums.others};
     ptx::cluster_sync();
@@ -308,14 +315,22 @@ __global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(con
   if (a.loss && rank == 0 && block == 0) a.loss[t] = loss;
   if (dr) {
     if (live == 1 && sums.none) live = 0;  // masked whole
-    const uint64_t minus_m = both(-sums.m), c = both(a.c), factor = both(w * a.temperature / (1.f + sums.others));
+    const RowGradient gradient(a, sums, w);
     const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
-    auto put = [&](int i, const uint4& x) {
-      put_granule<T>(dr, same, gradient_of<T>(x, live == 1, minus_m, c, factor, fill), row.first(i), a.classes);
-    };
-    for (int i = at.first + rank; i < at.last; i += G) put(i, RESIDENT ? row_s[i - begin] : get(i));
+    if (live == 1 && same) {
+      uint4* out = reinterpret_cast<uint4*>(dr + row.first(at.first));
+#pragma unroll 4
+      for (int i = rank; i < at.last - at.first; i += G)
+        out[i] = gradient.of<T>(RESIDENT ? row_s[at.first - begin + i] : get(at.first + i));
+    } else {
+      for (int i = at.first + rank; i < at.last; i += G) {
+        const uint4 x = RESIDENT ? row_s[i - begin] : get(i);
+        put_granule<T>(dr, same, live == 1 ? gradient.of<T>(x) : granule_of<T>(fill), row.first(i), a.classes);
+      }
+    }
     const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
-    if (edge >= 0) put(edge, get(edge));
+    if (edge >= 0)
+      put_granule<T>(dr, same, live == 1 ? gradient.of<T>(get(edge)) : granule_of<T>(fill), row.first(edge), a.classes);
     __syncthreads();
     // (each block those of its own classes)
     const int low = row.first(begin), high = row.first(end);

@@ -20,7 +20,7 @@ namespace {
 struct ProbArgs {
   int64_t ldz, tokens;
   int classes, k;
-  float temperature, c;  // c = log2(e) / temperature
+  float temperature, c, reach;  // c = log2(e) / temperature, reach = 500 / c
   const int32_t* target;
   float *logprob, *entropy, *norm, *top;
   int32_t* index;
@@ -395,10 +395,10 @@ __global__ void __launch_bounds__(G) k_probs(const T* z, const ProbArgs a) {
     y = __ldg(a.target + t);
     if (y >= 0 && y < a.classes) zy = to_f32<T>(zr[y]);
   }
-  const auto part = sum_part<T, G, true, 4>(row, at, a.classes, rank, a.c, get);
+  const auto part = sum_part<T, G, true, 4>(row, at, a.classes, rank, Scale{a.c, a.reach}, get);
   select.key[rank] = part.key();
   RowSums sums = join_block<T, G, true>(part, row, at, a.classes, a.c, get, join, [&] {
-    if (a.k) find_threshold<G>(select, a.k);
+    if (rank < 32 && a.k) find_threshold<G>(select, a.k);
   });
   if constexpr (CL == 1) {
     const RowSays says(sums);
@@ -552,7 +552,7 @@ void launch_probs(const T* z, const ProbArgs& a, cudaStream_t s) {
 struct ProbGradArgs {
   int64_t ldz, ldd, tokens;
   int classes, parts;  // parts: warps a row
-  float temperature, c;
+  float temperature, c, reach;
   const float *norm, *dlogprob, *dentropy;
   const int32_t* target;
 };
@@ -581,6 +581,8 @@ __global__ void __launch_bounds__(256) k_probs_grad(const T* z, T* dz, const Pro
   const float scale = exp2_of(-log_sum * kLog2e) / a.temperature;
   const uint64_t alpha = both(-(g + h * mean) * scale), beta = both(-h * kLn2 * scale);
   const uint64_t minus_m = both(-m), c = both(a.c);
+  const bool raise = sizeof(T) == 2 && has_floor(m);
+  const uint32_t floor = floor_below(m, a.reach);
   const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
   uint4 w[kGradVecs];
   const int from = part * 32 * kGradVecs + lane;
@@ -596,7 +598,7 @@ __global__ void __launch_bounds__(256) k_probs_grad(const T* z, T* dz, const Pro
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) v[j] = 0;
     } else {
-      Vec<T>::open(w[u], v);
+      Vec<T>::open(raise ? raised(w[u], floor) : w[u], v);
       float at_y = 0.f;
       if ((uint32_t)(y - first) < (uint32_t)N) {
         const float ty = (Vec<T>::at(w[u], y - first) - m) / a.temperature, p = __expf(ty - log_sum);
@@ -604,7 +606,8 @@ __global__ void __launch_bounds__(256) k_probs_grad(const T* z, T* dz, const Pro
       }
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
-        const uint64_t x = bounded(shifted(v[j], minus_m, c));
+        uint64_t x = shifted(v[j], minus_m, c);
+        if (!raise) x = bounded(x);
         v[j] = ptx::mul_f32x2(exp2_pair(x), ptx::fma_f32x2(beta, x, alpha));
       }
       if ((uint32_t)(y - first) < (uint32_t)N) {
@@ -637,7 +640,7 @@ void log_probs(int type, const void* z, int64_t ldz, int64_t tokens, int classes
                double temperature, float* logprob, float* entropy, float* norm, float* top, int32_t* index,
                cudaStream_t s) {
   const ProbArgs a{ldz, tokens, classes, k, (float)temperature, (float)(1.4426950408889634 / temperature),
-                   target, logprob, entropy, norm, top, index};
+                   (float)(500.0 / 1.4426950408889634 * temperature), target, logprob, entropy, norm, top, index};
   if (type == LIPCACHE_F32)
     launch_probs(static_cast<const float*>(z), a, s);
   else
@@ -648,7 +651,7 @@ void log_probs_backward(int type, const void* z, int64_t ldz, int64_t tokens, in
                         const int32_t* target, const float* dlogprob, const float* dentropy, double temperature,
                         void* dz, int64_t ldd, cudaStream_t s) {
   const ProbGradArgs a{ldz, ldd, tokens, classes, 0, (float)temperature, (float)(1.4426950408889634 / temperature),
-                       norm, dlogprob, dentropy, target};
+                       (float)(500.0 / 1.4426950408889634 * temperature), norm, dlogprob, dentropy, target};
   if (type == LIPCACHE_F32)
     launch_probs_grad(static_cast<const float*>(z), static_cast<float*>(dz), a, s);
   else

@@ -173,6 +173,22 @@ struct RowSums {
   bool none;
 };
 
+// BF16 values, for which bounding t costs less before they are opened: a value twice,
+// so far below m that its t is at most -500 (reach = 500 / c) but finite, for
+// |m| < 2^100.
+__device__ __forceinline__ uint32_t floor_below(float m, float reach) {
+  const uint32_t bits = __float_as_uint(m - reach - fabsf(m) * 0.015625f);
+  // (rounded down: two steps of BF16 below m at least)
+  const uint32_t low = (bits >> 31 ? bits + 0xffffu : bits) >> 16;
+  return low | low << 16;
+}
+__device__ __forceinline__ bool has_floor(float m) { return fabsf(m) < 1.2676506e30f; }
+__device__ __forceinline__ uint4 raised(uint4 w, uint32_t floor) {
+  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&w);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __hmax2(h[i], *reinterpret_cast<const __nv_bfloat162*>(&floor));
+  return w;
+}
 // t of a pair: differences first, so that logits may stand at any offset.
 __device__ __forceinline__ uint64_t shifted(uint64_t v, uint64_t minus_m, uint64_t c) {
   return ptx::mul_f32x2(ptx::add_f32x2(v, minus_m), c);
@@ -186,20 +202,23 @@ __device__ __forceinline__ uint64_t bounded(uint64_t t) {
   return ptx::pack_f32x2(__float_as_uint(fmaxf(lo_f32(t), kLeast)), __float_as_uint(fmaxf(hi_f32(t), kLeast)));
 }
 
-// A thread's part of a row: the running maximum (from the lowest finite value up),
-// and the sums relative to it; with MEAN, q too. NaN or +inf: m is.
+// What t and its bounds go by: c = log2(e) / T.
+struct Scale {
+  float c, reach;  // reach = 500 / c
+};
+
+// A thread's part of a row: the largest value, and the sums relative to m, which is
+// at least that (the warp's largest at the start, so that few of a thread's later
+// values move it); with MEAN, q too. NaN or +inf: top is.
 template <typename T, bool MEAN>
 struct RowPart {
   static constexpr int N = Vec<T>::N;
-  // BF16 values are raised to `floor` two at a time, before they are opened: a
-  // value that far below m whose t is finite. Maxima of 2^100 or more have none.
   static constexpr bool kFloor = MEAN && sizeof(T) == 2;
-  float m = -3.402823466e38f;
+  float top = -INFINITY, m = -3.402823466e38f;
   uint64_t s = 0, q = 0;
   uint32_t floor = 0;
-  bool wide = true;
   template <int U>
-  __device__ __forceinline__ float top_of(const uint4 (&w)[U]) const {
+  __device__ __forceinline__ static float top_of(const uint4 (&w)[U]) {
     if constexpr (sizeof(T) == 4) {
       float top = top_nan<T>(w[0]);
 #pragma unroll
@@ -215,41 +234,35 @@ struct RowPart {
       return max_nan(__low2float(m), __high2float(m));
     }
   }
+  // m before anything is added, by the whole warp; `first`: the thread's first value,
+  // or -inf
+  __device__ __forceinline__ void start(float first, const Scale& k) {
+    m = fmaxf(value_of(__reduce_max_sync(0xffffffffu, key_of(first))), -3.402823466e38f);
+    if (kFloor) floor = floor_below(m, k.reach);
+  }
   template <int U>
-  __device__ __forceinline__ void add(const uint4 (&w)[U], float c) {
-    const float top = max_nan(top_of(w), m);
-    if (top != m) {
-      const float delta = fmaxf((m - top) * c, kLeast), f = exp2_of(delta);
+  __device__ __forceinline__ void add(const uint4 (&w)[U], const Scale& k) {
+    const float here = top_of(w);
+    top = max_nan(top, here);
+    if (!(here <= m)) {
+      const float delta = fmaxf((m - here) * k.c, kLeast), f = exp2_of(delta);
       if (MEAN) q = ptx::mul_f32x2(both(f), ptx::fma_f32x2(both(delta), s, q));
       s = ptx::mul_f32x2(both(f), s);
-      m = top;
-      if (kFloor) {
-        wide = !(fabsf(m) < 1.2676506e30f);
-        const uint32_t bits = __float_as_uint(m - 500.f / c - fabsf(m) * 0.015625f);
-        // (rounded down: two steps of BF16 below m at least)
-        const uint32_t low = (bits >> 31 ? bits + 0xffffu : bits) >> 16;
-        floor = low | low << 16;
-      }
+      m = here;
+      if (kFloor) floor = floor_below(m, k.reach);
     }
-    if (wide)
-      accumulate<U, false>(w, c);
+    if (!kFloor || has_floor(m))
+      accumulate<kFloor>(w, k.c);
     else
-      accumulate<U, kFloor>(w, c);
+      accumulate<false>(w, k.c);
   }
-  template <int U, bool FLOOR>
+  template <bool FLOOR, int U>
   __device__ __forceinline__ void accumulate(const uint4 (&w)[U], float c) {
     const uint64_t minus_m = both(-m), cc = both(c);
-    const __nv_bfloat162 low = *reinterpret_cast<const __nv_bfloat162*>(&floor);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      uint4 x = w[u];
-      if constexpr (FLOOR) {
-        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&x);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = __hmax2(h[i], low);
-      }
       uint64_t v[N / 2];
-      Vec<T>::open(x, v);
+      Vec<T>::open(FLOOR ? raised(w[u], floor) : w[u], v);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
         uint64_t t = shifted(v[i], minus_m, cc);
@@ -260,10 +273,8 @@ struct RowPart {
       }
     }
   }
-  // 0: nothing above -inf (s is 0; of a part that saw NaN it may be, too)
-  __device__ __forceinline__ uint32_t key() const {
-    return s == 0 && m <= 3.402823466e38f ? 0u : key_of(m);
-  }
+  // 0: nothing above -inf
+  __device__ __forceinline__ uint32_t key() const { return top == -INFINITY ? 0u : key_of(top); }
 };
 
 // Which granules of [begin, end) of a row are a thread's: those inside the row go
@@ -280,24 +291,35 @@ struct Slice {
 
 // The part of thread `rank` of G: U granules at a time.
 template <typename T, int G, bool MEAN, int U, typename Get>
-__device__ __forceinline__ RowPart<T, MEAN> sum_part(const RowSpan<T>& row, const Slice& at, int n, int rank, float c,
-                                                     Get get) {
+__device__ __forceinline__ RowPart<T, MEAN> sum_part(const RowSpan<T>& row, const Slice& at, int n, int rank,
+                                                     const Scale& k, Get get) {
   RowPart<T, MEAN> part;
   int i = at.first + rank;
-  for (; i + (U - 1) * G < at.last; i += U * G) {
-    uint4 w[U];
+  const bool whole = i + (U - 1) * G < at.last;
+  uint4 w[U];
+  float first = -INFINITY;
+  if (whole) {
 #pragma unroll
     for (int u = 0; u < U; ++u) w[u] = get(i + u * G);
-    part.add(w, c);
+    first = RowPart<T, MEAN>::top_of(w);
+  }
+  part.start(first, k);
+  if (whole) {
+    part.add(w, k);
+    for (i += U * G; i + (U - 1) * G < at.last; i += U * G) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) w[u] = get(i + u * G);
+      part.add(w, k);
+    }
   }
   for (; i < at.last; i += G) {
-    const uint4 w[1] = {get(i)};
-    part.add(w, c);
+    const uint4 one[1] = {get(i)};
+    part.add(one, k);
   }
   const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
   if (edge >= 0) {
-    const uint4 w[1] = {masked_outside<T>(get(edge), row.first(edge), n)};
-    part.add(w, c);
+    const uint4 one[1] = {masked_outside<T>(get(edge), row.first(edge), n)};
+    part.add(one, k);
   }
   return part;
 }
@@ -312,8 +334,8 @@ struct JoinShared {
 
 // The block's sums from its threads'. Where the row is nearly sure, the sum of the
 // thread that holds the maximum has lost the others' last bits beside it: its warp
-// takes that thread's granules again. meanwhile(): what warp 0 does between the two
-// barriers.
+// takes that thread's granules again. meanwhile(): what warps do besides, between the
+// two barriers.
 template <typename T, int G, bool MEAN, typename Get, typename F>
 __device__ __forceinline__ RowSums join_block(const RowPart<T, MEAN>& part, const RowSpan<T>& row, const Slice& at, int n,
                                               float c, Get get, JoinShared<G>& sh, F&& meanwhile) {
@@ -346,7 +368,7 @@ __device__ __forceinline__ RowSums join_block(const RowPart<T, MEAN>& part, cons
     sh.s[warp] = s;
     sh.q[warp] = q;
   }
-  if (warp == 0) meanwhile();
+  meanwhile();
   __syncthreads();
   s = sh.s[0];
   q = sh.q[0];
@@ -423,14 +445,14 @@ template <typename T, int L, int U, bool MEAN>
 __device__ __forceinline__ RowSums sum_lanes(const LaneRow<T, L, U>& row, int lane, float c, uint32_t& mine) {
   constexpr int N = Vec<T>::N;
   RowPart<T, MEAN> part;
-  const float own = part.top_of(row.w);
+  const float own = RowPart<T, MEAN>::top_of(row.w);
   mine = own == -INFINITY ? 0u : key_of(own);
   const uint32_t top = lanes_max<L>(mine);
   RowSums r;
   r.none = top == 0;
   r.m = r.none ? 0.f : top >= kNanKey ? NAN : value_of(top);
   part.m = r.m;
-  part.template accumulate<U, false>(row.w, c);
+  part.template accumulate<false>(row.w, c);
   float s = lo_f32(part.s) + hi_f32(part.s), q = MEAN ? lo_f32(part.q) + hi_f32(part.q) : 0.f;
   const uint32_t holders = __ballot_sync(0xffffffffu, mine == top) >> (threadIdx.x & 31 & ~(L - 1));
   const bool holds = mine == top && !(holders & ((1u << lane) - 1));
