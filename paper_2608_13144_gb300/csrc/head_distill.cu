@@ -118,16 +118,17 @@ struct Teacher {
 
 // The gradient w T p of a row's granules.
 struct RowGradient {
-  uint64_t minus_m, c, factor;
+  float m;
+  uint64_t c, factor;
   __device__ __forceinline__ RowGradient(const DistillArgs& a, const RowSums& sums, float w)
-      : minus_m(both(-sums.m)), c(both(a.c)), factor(both(w * a.temperature / (1.f + sums.others))) {}
+      : m(sums.m), c(both(a.c)), factor(both(w * a.temperature / (1.f + sums.others))) {}
   template <typename T>
   __device__ __forceinline__ uint4 of(const uint4& w) const {
     constexpr int N = Vec<T>::N;
     uint64_t v[N / 2];
-    Vec<T>::open(w, v);
+    differences<T>(w, m, v);
 #pragma unroll
-    for (int j = 0; j < N / 2; ++j) v[j] = ptx::mul_f32x2(exp2_pair(shifted(v[j], minus_m, c)), factor);
+    for (int j = 0; j < N / 2; ++j) v[j] = ptx::mul_f32x2(exp2_pair(ptx::mul_f32x2(v[j], c)), factor);
     return Vec<T>::close(v);
   }
 };

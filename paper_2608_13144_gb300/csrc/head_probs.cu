@@ -46,7 +46,7 @@ struct SelectShared {
   uint32_t tau;
   int n_live, n;
   int total[G / 32];
-  Found found[kCap];
+  __align__(16) Found found[kCap];
 };
 
 // One warp: tau, a key that at least k of the threads' maxima reach (or the lowest
@@ -113,6 +113,41 @@ __device__ __forceinline__ int group_count(int v, int (&total)[G / 32]) {
   return v;
 }
 
+// Which of a granule's values reach `least`: a bit each.
+template <typename T>
+struct Reach;
+template <>
+struct Reach<float> {
+  float least;
+  __device__ __forceinline__ explicit Reach(float least) : least(least) {}
+  __device__ __forceinline__ uint32_t of(const uint4& w) const {
+    return (__uint_as_float(w.x) >= least ? 1u : 0u) | (__uint_as_float(w.y) >= least ? 2u : 0u) |
+           (__uint_as_float(w.z) >= least ? 4u : 0u) | (__uint_as_float(w.w) >= least ? 8u : 0u);
+  }
+  __device__ __forceinline__ int index(int bit) const { return bit; }
+  __device__ __forceinline__ float value(const uint4& w, int j) const {
+    return __uint_as_float(j & 2 ? (j & 1 ? w.w : w.z) : (j & 1 ? w.y : w.x));
+  }
+};
+template <>
+struct Reach<__nv_bfloat16> {
+  __nv_bfloat162 least;  // rounded up
+  __device__ __forceinline__ explicit Reach(float x) {
+    const uint32_t bits = __float_as_uint(x), up = (bits >> 31 ? bits : bits + 0xffffu) >> 16, two = up | up << 16;
+    least = *reinterpret_cast<const __nv_bfloat162*>(&two);
+  }
+  __device__ __forceinline__ uint32_t of(const uint4& w) const {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
+    return (__hge2_mask(h[0], least) & 0x00010001u) | (__hge2_mask(h[1], least) & 0x00020002u) |
+           (__hge2_mask(h[2], least) & 0x00040004u) | (__hge2_mask(h[3], least) & 0x00080008u);
+  }
+  __device__ __forceinline__ int index(int bit) const { return bit < 16 ? 2 * bit : 2 * (bit - 16) + 1; }
+  __device__ __forceinline__ float value(const uint4& w, int j) const {
+    const uint32_t x = j & 4 ? (j & 2 ? w.w : w.z) : (j & 2 ? w.y : w.x);
+    return __uint_as_float(j & 1 ? x & 0xffff0000u : x << 16);
+  }
+};
+
 // The group's k largest unmasked values in granules [begin, end) of a row without
 // NaN or +inf, after find_threshold and a barrier, to emit(rank, candidate), each rank
 // from one thread; returns how many there are (at most k).
@@ -122,6 +157,10 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice
   constexpr uint32_t kAll = 0xffffffffu;
   constexpr int N = Vec<T>::N, kCap = SelectShared<G>::kCap;
   const int rank = group_rank<G>(), lane = threadIdx.x & 31, warp = G == 32 ? 0 : threadIdx.x >> 5;
+  auto keep = [&](float z, int index) {
+    const int to = atomicAdd(&sh.n, 1);
+    if (to < kCap) sh.found[to] = candidate(key_of(z), index);
+  };
   auto collect = [&](int granule, uint32_t from) {
     const uint4 w = get(granule);
     const int first = row.first(granule);
@@ -129,17 +168,22 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const float z = Vec<T>::at(w, j);
-      if (z >= least && first + j >= 0 && first + j < n) {
-        const int to = atomicAdd(&sh.n, 1);
-        if (to < kCap) sh.found[to] = candidate(key_of(z), first + j);
-      }
+      if (z >= least && first + j >= 0 && first + j < n) keep(z, first + j);
     }
   };
-  // a warp reads a live thread's granules; those at the row's ends are read by all
+  // a warp reads a live thread's granules, all inside the row; those at the row's
+  // ends are read by all
   const int live = sh.n_live;
   const uint32_t tau = sh.tau;
+  const Reach<T> reach(value_of(tau));
   for (int l = warp; l < live; l += G / 32)
-    for (int i = at.first + sh.live[l] + lane * G; i < at.last; i += 32 * G) collect(i, tau);
+    for (int i = at.first + sh.live[l] + lane * G; i < at.last; i += 32 * G) {
+      const uint4 w = get(i);
+      for (uint32_t hits = reach.of(w); hits; hits &= hits - 1) {
+        const int j = reach.index(__ffs(hits) - 1);
+        keep(reach.value(w, j), row.first(i) + j);
+      }
+    }
   if (rank == 0 && at.head >= 0) collect(at.head, tau);
   if (rank == 1 && at.tail >= 0) collect(at.tail, tau);
   group_sync<G>();
@@ -183,10 +227,20 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice
       ties = k - found;
     }
   }
+  if ((found & 1) && found < kCap) {  // (an even number: they are read in pairs)
+    if (rank == 0) sh.found[found] = 0;
+    if (G == 32 || found < 32)
+      __syncwarp();
+    else
+      __syncthreads();
+  }
   for (int i = rank; i < found; i += G) {
     const Found own = sh.found[i];
     int r = 0;
-    for (int j = 0; j < found; ++j) r += sh.found[j] > own;
+    for (int j = 0; j < found; j += 2) {
+      const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(sh.found + j);
+      r += (two.x > own) + (two.y > own);
+    }
     if (r < k) emit(r, own);
   }
   // ties in the order of their indices
@@ -401,14 +455,14 @@ __global__ void __launch_bounds__(G) k_probs(const T* z, const ProbArgs a) {
     if (rank < 32 && a.k) find_threshold<G>(select, a.k);
   });
   if constexpr (CL == 1) {
-    const RowSays says(sums);
-    if (rank == 0) put_row(a, t, says, y, zy);
+    if (rank == 0) put_row(a, t, RowSays(sums), y, zy);
     if (a.k == 0) return;
     int have = 0;
-    if (!says.bad && !says.none)
+    const bool bad = isnan(sums.m);
+    if (!bad && !sums.none)
       have = select_largest<T, G>(row, at, begin, end, a.classes, a.k, get, select,
-                                  [&](int r, Found f) { put_top(a, t, says, r, f); });
-    fill_top(a, t, have, says.bad, rank, G);
+                                  [&](int r, Found f) { put_top(a, t, RowSays(sums), r, f); });
+    if (have < a.k) fill_top(a, t, have, bad, rank, G);
   } else {
     // each block's best, which the first one ranks against each other
     int have = 0;
@@ -551,86 +605,159 @@ void launch_probs(const T* z, const ProbArgs& a, cudaStream_t s) {
 // ---------------------------------------------------------------- their gradient
 struct ProbGradArgs {
   int64_t ldz, ldd, tokens;
-  int classes, parts;  // parts: warps a row
+  int classes;
   float temperature, c, reach;
   const float *norm, *dlogprob, *dentropy;
   const int32_t* target;
 };
-constexpr int kGradVecs = 4;  // granules a lane takes
-
-// A warp takes 32 kGradVecs granules of a row. With t in units of log 2:
-// dz = exp2(t) (alpha + beta t), alpha = -(g + h mean) / (T sum), beta = -h ln 2 /
-// (T sum); the target's own 1 - p is -expm1(logprob), without cancellation.
+// A row's gradient. With t in units of log 2: dz = exp2(t) (alpha + beta t), alpha =
+// -(g + h mean) / (T sum), beta = -h ln 2 / (T sum); at the target's class 1 - p is
+// -expm1(logprob), without cancellation.
 template <typename T>
-__global__ void __launch_bounds__(256) k_probs_grad(const T* z, T* dz, const ProbGradArgs a) {
-  constexpr int N = Vec<T>::N;
+struct ProbGradient {
+  static constexpr int N = Vec<T>::N;
+  float g, h, m, log_sum, mean;
+  uint64_t alpha, beta, c;
+  uint32_t floor;
+  int y;  // the target, kNone: none (far before any row)
+  static constexpr int kNone = -(1 << 30);
+  bool zero, raise, nan;
+  __device__ __forceinline__ ProbGradient(const ProbGradArgs& a, int64_t t) : c(both(a.c)) {
+    y = a.target ? __ldg(a.target + t) : kNone;
+    if (y < 0 || y >= a.classes) y = kNone;
+    g = y >= 0 && a.dlogprob ? __ldg(a.dlogprob + t) : 0.f;
+    h = a.dentropy ? __ldg(a.dentropy + t) : 0.f;
+    m = __ldg(a.norm + 3 * t);
+    log_sum = __ldg(a.norm + 3 * t + 1);
+    mean = __ldg(a.norm + 3 * t + 2);
+    if (g == 0.f) y = kNone;  // (its gradient is like the others')
+    zero = (g == 0.f && h == 0.f) || m == -INFINITY;
+    nan = isnan(m);
+    const float scale = exp2_of(-log_sum * kLog2e) / a.temperature;
+    alpha = both(-(g + h * mean) * scale);
+    beta = both(-h * kLn2 * scale);
+    raise = sizeof(T) == 2 && has_floor(m);
+    floor = floor_below(m, a.reach);
+  }
+  template <bool RAISE>
+  __device__ __forceinline__ uint4 of(const uint4& w) const {
+    uint64_t v[N / 2];
+    differences<T>(RAISE ? raised(w, floor) : w, m, v);
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+      uint64_t x = ptx::mul_f32x2(v[j], c);
+      if (!RAISE) x = bounded(x);
+      v[j] = ptx::mul_f32x2(exp2_pair(x), ptx::fma_f32x2(beta, x, alpha));
+    }
+    return Vec<T>::close(v);
+  }
+  // (zero and nan: the same value everywhere)
+  __device__ __forceinline__ uint4 operator()(const uint4& w) const {
+    if (zero || nan) {
+      uint64_t v[N / 2];
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) v[j] = both(zero ? 0.f : NAN);
+      return Vec<T>::close(v);
+    }
+    return raise ? of<sizeof(T) == 2>(w) : of<false>(w);
+  }
+  __device__ __forceinline__ T at_target(const ProbGradArgs& a, float zy) const {
+    const float ty = (zy - m) / a.temperature, p = __expf(ty - log_sum);
+    const float d = -g * expm1f(ty - log_sum) - (h == 0.f || p == 0.f ? 0.f : h * p * (ty + mean));
+    return from_f32<T>(zero ? 0.f : nan ? NAN : d / a.temperature);
+  }
+};
+
+// Small rows: L lanes each, U granules a lane.
+template <typename T, int L, int U>
+__global__ void __launch_bounds__(128) k_probs_grad_lanes(const T* z, T* dz, const ProbGradArgs a) {
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int64_t t = item / a.parts;
+  const int lane = threadIdx.x & (L - 1);
+  const int64_t t = (int64_t)blockIdx.x * (128 / L) + threadIdx.x / L;
   if (t >= a.tokens) return;
-  const int part = (int)(item - t * a.parts), lane = threadIdx.x & 31;
   const T* zr = z + t * a.ldz;
   T* dr = dz + t * a.ldd;
   const RowSpan<T> row(zr, a.classes);
-  const int y = a.target ? __ldg(a.target + t) : -1;
-  const bool live = y >= 0 && y < a.classes;
-  const float g = live && a.dlogprob ? __ldg(a.dlogprob + t) : 0.f, h = a.dentropy ? __ldg(a.dentropy + t) : 0.f;
-  const float m = __ldg(a.norm + 3 * t), log_sum = __ldg(a.norm + 3 * t + 1), mean = __ldg(a.norm + 3 * t + 2);
-  const bool zero = (g == 0.f && h == 0.f) || m == -INFINITY;
-  const float scale = exp2_of(-log_sum * kLog2e) / a.temperature;
-  const uint64_t alpha = both(-(g + h * mean) * scale), beta = both(-h * kLn2 * scale);
-  const uint64_t minus_m = both(-m), c = both(a.c);
-  const bool raise = sizeof(T) == 2 && has_floor(m);
-  const uint32_t floor = floor_below(m, a.reach);
+  uint4 w[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (u * L + lane < row.count) w[u] = row.granules[u * L + lane];
+  const ProbGradient<T> gradient(a, t);
   const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
-  uint4 w[kGradVecs];
-  const int from = part * 32 * kGradVecs + lane;
 #pragma unroll
-  for (int u = 0; u < kGradVecs; ++u)
-    if (!zero && from + u * 32 < row.count) w[u] = row.granules[from + u * 32];
-#pragma unroll
-  for (int u = 0; u < kGradVecs; ++u) {
-    const int i = from + u * 32, first = row.first(i);
-    if (i >= row.count) break;
-    uint64_t v[N / 2];
-    if (zero) {
-#pragma unroll
-      for (int j = 0; j < N / 2; ++j) v[j] = 0;
-    } else {
-      Vec<T>::open(raise ? raised(w[u], floor) : w[u], v);
-      float at_y = 0.f;
-      if ((uint32_t)(y - first) < (uint32_t)N) {
-        const float ty = (Vec<T>::at(w[u], y - first) - m) / a.temperature, p = __expf(ty - log_sum);
-        at_y = (-g * expm1f(ty - log_sum) - (h == 0.f || p == 0.f ? 0.f : h * p * (ty + mean))) / a.temperature;
-      }
-#pragma unroll
-      for (int j = 0; j < N / 2; ++j) {
-        uint64_t x = shifted(v[j], minus_m, c);
-        if (!raise) x = bounded(x);
-        v[j] = ptx::mul_f32x2(exp2_pair(x), ptx::fma_f32x2(beta, x, alpha));
-      }
-      if ((uint32_t)(y - first) < (uint32_t)N) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (first + j == y)
-            v[j / 2] = j & 1 ? (v[j / 2] & 0xffffffffull) | ((uint64_t)__float_as_uint(at_y) << 32)
-                             : (v[j / 2] & ~0xffffffffull) | __float_as_uint(at_y);
-      }
-      if (isnan(m)) {
-#pragma unroll
-        for (int j = 0; j < N / 2; ++j) v[j] = both(NAN);
-      }
+  for (int u = 0; u < U; ++u)
+    if (u * L + lane < row.count) {
+      const int first = row.first(u * L + lane);
+      put_granule<T>(dr, same, gradient(w[u]), first, a.classes);
+      if ((uint32_t)(gradient.y - first) < (uint32_t)Vec<T>::N)
+        dr[gradient.y] = gradient.at_target(a, Vec<T>::at(w[u], gradient.y - first));
     }
-    put_granule<T>(dr, same, Vec<T>::close(v), first, a.classes);
+}
+
+// Larger rows: 256 threads a part of one, parts of at most kGradPart granules.
+constexpr int kGradPart = 2048;
+template <typename T>
+__global__ void __launch_bounds__(256) k_probs_grad(const T* z, T* dz, const ProbGradArgs a) {
+  ptx::wait_prerequisites();
+  ptx::launch_dependents();
+  const int64_t t = blockIdx.x;
+  const T* zr = z + t * a.ldz;
+  T* dr = dz + t * a.ldd;
+  const RowSpan<T> row(zr, a.classes);
+  const int share = (row.count + gridDim.y - 1) / gridDim.y, begin = blockIdx.y * share, end = min(begin + share, row.count);
+  if (begin >= end) return;
+  const Slice at(row, begin, end, a.classes);
+  const ProbGradient<T> gradient(a, t);
+  const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
+  // the target's class is written by the thread that wrote its granule, after it
+  const int own = gradient.y >= row.first(begin) && gradient.y < row.first(end) ? (gradient.y + row.lead) / Vec<T>::N : -1;
+  const int edge = threadIdx.x == 0 ? at.head : threadIdx.x == 1 ? at.tail : -1;
+  const bool mine = own >= 0 && (own < at.first || own >= at.last ? own == edge : (own - at.first) % 256 == threadIdx.x);
+  float zy = 0.f;
+  if (mine) zy = to_f32<T>(zr[gradient.y]);
+  if (edge >= 0) put_granule<T>(dr, same, gradient(row.granules[edge]), row.first(edge), a.classes);
+  if (same) {
+    uint4* out = reinterpret_cast<uint4*>(dr + row.first(0));
+    auto run = [&](auto raise) {
+#pragma unroll 4
+      for (int i = at.first + threadIdx.x; i < at.last; i += 256)
+        out[i] = gradient.template of<decltype(raise)::value>(row.granules[i]);
+    };
+    if (gradient.zero || gradient.nan) {
+      for (int i = at.first + threadIdx.x; i < at.last; i += 256) out[i] = gradient(uint4{});
+    } else if (gradient.raise) {
+      run(std::integral_constant<bool, sizeof(T) == 2>{});
+    } else {
+      run(std::false_type{});
+    }
+  } else {
+    for (int i = at.first + threadIdx.x; i < at.last; i += 256)
+      put_granule<T>(dr, false, gradient(row.granules[i]), row.first(i), a.classes);
   }
+  if (mine) dr[gradient.y] = gradient.at_target(a, zy);
+}
+
+template <typename T, int L>
+bool probs_grad_lanes(const T* z, T* dz, const ProbGradArgs& a, int granules, cudaStream_t s) {
+  if (granules > L * 8) return false;
+  const dim3 grid((unsigned)ceil_div(a.tokens, 128 / L));
+  if (granules <= L)
+    launch_pdl(k_probs_grad_lanes<T, L, 1>, grid, 128, s, z, dz, a);
+  else if (granules <= 2 * L)
+    launch_pdl(k_probs_grad_lanes<T, L, 2>, grid, 128, s, z, dz, a);
+  else if (granules <= 4 * L)
+    launch_pdl(k_probs_grad_lanes<T, L, 4>, grid, 128, s, z, dz, a);
+  else
+    launch_pdl(k_probs_grad_lanes<T, L, 8>, grid, 128, s, z, dz, a);
+  return true;
 }
 
 template <typename T>
-void launch_probs_grad(const T* z, T* dz, ProbGradArgs a, cudaStream_t s) {
+void launch_probs_grad(const T* z, T* dz, const ProbGradArgs& a, cudaStream_t s) {
   const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
-  a.parts = (int)ceil_div(granules, 32 * kGradVecs);
-  launch_pdl(k_probs_grad<T>, dim3((unsigned)ceil_div(a.tokens * a.parts, 8)), 256, s, z, dz, a);
+  if (!probs_grad_lanes<T, 8>(z, dz, a, granules, s) && !probs_grad_lanes<T, 32>(z, dz, a, granules, s))
+    launch_pdl(k_probs_grad<T>, dim3((unsigned)a.tokens, (unsigned)ceil_div(granules, kGradPart)), 256, s, z, dz, a);
   LC_LAUNCH_CHECK("k_probs_grad");
 }
 
@@ -650,7 +777,7 @@ void log_probs(int type, const void* z, int64_t ldz, int64_t tokens, int classes
 void log_probs_backward(int type, const void* z, int64_t ldz, int64_t tokens, int classes, const float* norm,
                         const int32_t* target, const float* dlogprob, const float* dentropy, double temperature,
                         void* dz, int64_t ldd, cudaStream_t s) {
-  const ProbGradArgs a{ldz, ldd, tokens, classes, 0, (float)temperature, (float)(1.4426950408889634 / temperature),
+  const ProbGradArgs a{ldz, ldd, tokens, classes, (float)temperature, (float)(1.4426950408889634 / temperature),
                        (float)(500.0 / 1.4426950408889634 * temperature), norm, dlogprob, dentropy, target};
   if (type == LIPCACHE_F32)
     launch_probs_grad(static_cast<const float*>(z), static_cast<float*>(dz), a, s);

@@ -189,9 +189,28 @@ __device__ __forceinline__ uint4 raised(uint4 w, uint32_t floor) {
   for (int i = 0; i < 4; ++i) h[i] = __hmax2(h[i], *reinterpret_cast<const __nv_bfloat162*>(&floor));
   return w;
 }
-// t of a pair: differences first, so that logits may stand at any offset.
-__device__ __forceinline__ uint64_t shifted(uint64_t v, uint64_t minus_m, uint64_t c) {
-  return ptx::mul_f32x2(ptx::add_f32x2(v, minus_m), c);
+// v - m of a granule's values: differences first, so that logits may stand at any
+// offset (BF16 ones are opened by the subtraction itself).
+template <typename T>
+__device__ __forceinline__ void differences(const uint4& w, float m, uint64_t (&v)[Vec<T>::N / 2]) {
+  if constexpr (sizeof(T) == 4) {
+    Vec<T>::open(w, v);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::N / 2; ++i) v[i] = ptx::add_f32x2(v[i], both(-m));
+  } else {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      asm("{\n\t.reg .b16 l, h;\n\t"
+          "mov.b32 {l, h}, %2;\n\t"
+          "sub.rn.f32.bf16 %0, l, %3;\n\t"
+          "sub.rn.f32.bf16 %1, h, %3;\n\t}"
+          : "=f"(lo), "=f"(hi)
+          : "r"(x[i]), "f"(m));
+      v[i] = ptx::pack_f32x2(__float_as_uint(lo), __float_as_uint(hi));
+    }
+  }
 }
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t t) {
   return ptx::pack_f32x2(__float_as_uint(exp2_of(lo_f32(t))), __float_as_uint(exp2_of(hi_f32(t))));
@@ -258,14 +277,14 @@ struct RowPart {
   }
   template <bool FLOOR, int U>
   __device__ __forceinline__ void accumulate(const uint4 (&w)[U], float c) {
-    const uint64_t minus_m = both(-m), cc = both(c);
+    const uint64_t cc = both(c);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       uint64_t v[N / 2];
-      Vec<T>::open(FLOOR ? raised(w[u], floor) : w[u], v);
+      differences<T>(FLOOR ? raised(w[u], floor) : w[u], m, v);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
-        uint64_t t = shifted(v[i], minus_m, cc);
+        uint64_t t = ptx::mul_f32x2(v[i], cc);
         if (MEAN && !FLOOR) t = bounded(t);
         const uint64_t e = exp2_pair(t);
         s = ptx::add_f32x2(s, e);
