@@ -651,26 +651,24 @@ struct ProbGradient {
     }
     return Vec<T>::close(v);
   }
-  // (zero and nan: the same value everywhere)
-  __device__ __forceinline__ uint4 operator()(const uint4& w) const {
-    if (zero || nan) {
-      uint64_t v[N / 2];
+  // where the row's gradient is the same value everywhere
+  __device__ __forceinline__ uint4 filled() const {
+    uint64_t v[N / 2];
 #pragma unroll
-      for (int j = 0; j < N / 2; ++j) v[j] = both(zero ? 0.f : NAN);
-      return Vec<T>::close(v);
-    }
-    return raise ? of<sizeof(T) == 2>(w) : of<false>(w);
+    for (int j = 0; j < N / 2; ++j) v[j] = both(zero ? 0.f : NAN);
+    return Vec<T>::close(v);
   }
   __device__ __forceinline__ T at_target(const ProbGradArgs& a, float zy) const {
     const float ty = (zy - m) / a.temperature, p = __expf(ty - log_sum);
     const float d = -g * expm1f(ty - log_sum) - (h == 0.f || p == 0.f ? 0.f : h * p * (ty + mean));
-    return from_f32<T>(zero ? 0.f : nan ? NAN : d / a.temperature);
+    return from_f32<T>(d / a.temperature);
   }
 };
 
-// Small rows: L lanes each, U granules a lane.
+// L lanes a row, or a part of one (blockIdx.y of them, of `share` granules): U
+// granules a lane, all loaded before any is written, which may be to the same array.
 template <typename T, int L, int U>
-__global__ void __launch_bounds__(128) k_probs_grad_lanes(const T* z, T* dz, const ProbGradArgs a) {
+__global__ void __launch_bounds__(128, 8) k_probs_grad(const T* z, T* dz, const ProbGradArgs a, int share) {
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   const int lane = threadIdx.x & (L - 1);
@@ -679,85 +677,54 @@ __global__ void __launch_bounds__(128) k_probs_grad_lanes(const T* z, T* dz, con
   const T* zr = z + t * a.ldz;
   T* dr = dz + t * a.ldd;
   const RowSpan<T> row(zr, a.classes);
+  const int from = blockIdx.y * share + lane, end = min((int)(blockIdx.y + 1) * share, row.count);
   uint4 w[U];
 #pragma unroll
   for (int u = 0; u < U; ++u)
-    if (u * L + lane < row.count) w[u] = row.granules[u * L + lane];
+    if (from + u * L < end) w[u] = row.granules[from + u * L];
   const ProbGradient<T> gradient(a, t);
   const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
+  auto write = [&](auto value) {
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (u * L + lane < row.count) {
-      const int first = row.first(u * L + lane);
-      put_granule<T>(dr, same, gradient(w[u]), first, a.classes);
-      if ((uint32_t)(gradient.y - first) < (uint32_t)Vec<T>::N)
-        dr[gradient.y] = gradient.at_target(a, Vec<T>::at(w[u], gradient.y - first));
-    }
-}
-
-// Larger rows: 256 threads a part of one, parts of at most kGradPart granules.
-constexpr int kGradPart = 2048;
-template <typename T>
-__global__ void __launch_bounds__(256) k_probs_grad(const T* z, T* dz, const ProbGradArgs a) {
-  ptx::wait_prerequisites();
-  ptx::launch_dependents();
-  const int64_t t = blockIdx.x;
-  const T* zr = z + t * a.ldz;
-  T* dr = dz + t * a.ldd;
-  const RowSpan<T> row(zr, a.classes);
-  const int share = (row.count + gridDim.y - 1) / gridDim.y, begin = blockIdx.y * share, end = min(begin + share, row.count);
-  if (begin >= end) return;
-  const Slice at(row, begin, end, a.classes);
-  const ProbGradient<T> gradient(a, t);
-  const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
-  // the target's class is written by the thread that wrote its granule, after it
-  const int own = gradient.y >= row.first(begin) && gradient.y < row.first(end) ? (gradient.y + row.lead) / Vec<T>::N : -1;
-  const int edge = threadIdx.x == 0 ? at.head : threadIdx.x == 1 ? at.tail : -1;
-  const bool mine = own >= 0 && (own < at.first || own >= at.last ? own == edge : (own - at.first) % 256 == threadIdx.x);
-  float zy = 0.f;
-  if (mine) zy = to_f32<T>(zr[gradient.y]);
-  if (edge >= 0) put_granule<T>(dr, same, gradient(row.granules[edge]), row.first(edge), a.classes);
-  if (same) {
-    uint4* out = reinterpret_cast<uint4*>(dr + row.first(0));
-    auto run = [&](auto raise) {
-#pragma unroll 4
-      for (int i = at.first + threadIdx.x; i < at.last; i += 256)
-        out[i] = gradient.template of<decltype(raise)::value>(row.granules[i]);
-    };
-    if (gradient.zero || gradient.nan) {
-      for (int i = at.first + threadIdx.x; i < at.last; i += 256) out[i] = gradient(uint4{});
-    } else if (gradient.raise) {
-      run(std::integral_constant<bool, sizeof(T) == 2>{});
-    } else {
-      run(std::false_type{});
-    }
-  } else {
-    for (int i = at.first + threadIdx.x; i < at.last; i += 256)
-      put_granule<T>(dr, false, gradient(row.granules[i]), row.first(i), a.classes);
+    for (int u = 0; u < U; ++u)
+      if (from + u * L < end) put_granule<T>(dr, same, value(w[u]), row.first(from + u * L), a.classes);
+  };
+  if (gradient.zero || gradient.nan) {
+    write([&](const uint4&) { return gradient.filled(); });
+    return;
   }
-  if (mine) dr[gradient.y] = gradient.at_target(a, zy);
+  if (sizeof(T) == 2 && gradient.raise)
+    write([&](const uint4& x) { return gradient.template of<sizeof(T) == 2>(x); });
+  else
+    write([&](const uint4& x) { return gradient.template of<false>(x); });
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = gradient.y - row.first(from + u * L);
+    if (from + u * L < end && (uint32_t)at < (uint32_t)Vec<T>::N) dr[gradient.y] = gradient.at_target(a, Vec<T>::at(w[u], at));
+  }
 }
 
-template <typename T, int L>
-bool probs_grad_lanes(const T* z, T* dz, const ProbGradArgs& a, int granules, cudaStream_t s) {
-  if (granules > L * 8) return false;
-  const dim3 grid((unsigned)ceil_div(a.tokens, 128 / L));
-  if (granules <= L)
-    launch_pdl(k_probs_grad_lanes<T, L, 1>, grid, 128, s, z, dz, a);
-  else if (granules <= 2 * L)
-    launch_pdl(k_probs_grad_lanes<T, L, 2>, grid, 128, s, z, dz, a);
-  else if (granules <= 4 * L)
-    launch_pdl(k_probs_grad_lanes<T, L, 4>, grid, 128, s, z, dz, a);
-  else
-    launch_pdl(k_probs_grad_lanes<T, L, 8>, grid, 128, s, z, dz, a);
-  return true;
+template <typename T, int L, int U>
+void launch_grad(const T* z, T* dz, const ProbGradArgs& a, int granules, cudaStream_t s) {
+  const int parts = (int)ceil_div(granules, L * U);
+  const dim3 grid((unsigned)ceil_div(a.tokens, 128 / L), (unsigned)parts);
+  launch_pdl(k_probs_grad<T, L, U>, grid, 128, s, z, dz, a, (int)ceil_div(granules, parts));
 }
 
 template <typename T>
 void launch_probs_grad(const T* z, T* dz, const ProbGradArgs& a, cudaStream_t s) {
   const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
-  if (!probs_grad_lanes<T, 8>(z, dz, a, granules, s) && !probs_grad_lanes<T, 32>(z, dz, a, granules, s))
-    launch_pdl(k_probs_grad<T>, dim3((unsigned)a.tokens, (unsigned)ceil_div(granules, kGradPart)), 256, s, z, dz, a);
+  // (at most 2^24 / 4 / 128 parts)
+  if (granules <= 8)
+    launch_grad<T, 8, 1>(z, dz, a, granules, s);
+  else if (granules <= 32)
+    launch_grad<T, 8, 4>(z, dz, a, granules, s);
+  else if (granules <= 64)
+    launch_grad<T, 16, 4>(z, dz, a, granules, s);
+  else if (granules <= 128)
+    launch_grad<T, 32, 4>(z, dz, a, granules, s);
+  else
+    launch_grad<T, 32, sizeof(T) == 4 ? 4 : 8>(z, dz, a, granules, s);
   LC_LAUNCH_CHECK("k_probs_grad");
 }
 
