@@ -176,12 +176,23 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice
   const int live = sh.n_live;
   const uint32_t tau = sh.tau;
   const Reach<T> reach(value_of(tau));
-  for (int l = warp; l < live; l += G / 32)
-    for (int i = at.first + sh.live[l] + lane * G; i < at.last; i += 32 * G) {
-      const uint4 w = get(i);
-      for (uint32_t hits = reach.of(w); hits; hits &= hits - 1) {
-        const int j = reach.index(__ffs(hits) - 1);
-        keep(reach.value(w, j), row.first(i) + j);
+  constexpr int W = G / 32, Q = 4;  // (of Q threads at a time, whose granules come from memory together)
+  for (int base = at.first; base < at.last; base += 32 * G)
+    for (int l = warp; l < live; l += Q * W) {
+      uint4 w[Q];
+      int i[Q];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        i[q] = l + q * W < live ? base + sh.live[l + q * W] + lane * G : at.last;
+        if (i[q] < at.last) w[q] = get(i[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        if (i[q] >= at.last) continue;
+        for (uint32_t hits = reach.of(w[q]); hits; hits &= hits - 1) {
+          const int j = reach.index(__ffs(hits) - 1);
+          keep(reach.value(w[q], j), row.first(i[q]) + j);
+        }
       }
     }
   if (rank == 0 && at.head >= 0) collect(at.head, tau);
@@ -427,7 +438,7 @@ __global__ void __launch_bounds__(128) k_probs_lanes(const T* z, const ProbArgs 
 
 // Large rows: a block of G threads each, or a cluster of CL blocks that split it.
 template <typename T, int G, int CL>
-__global__ void __launch_bounds__(G) k_probs(const T* z, const ProbArgs a) {
+__global__ void __launch_bounds__(G, (CL > 1 ? 768 : 1536) / G) k_probs(const T* z, const ProbArgs a) {
   __shared__ SelectShared<G> select;
   __shared__ JoinShared<G> join;
   __shared__ RowSums part_s;
