@@ -114,29 +114,6 @@ struct Place {
     groups = (n + N - 1) / N;
   }
 };
-template <int W>
-__device__ __forceinline__ uint4 window_at(const uint4& a, const uint4& b, bool half) {
-  const uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  uint4 r{x[W], x[W + 1], x[W + 2], x[W + 3]};
-  if (half) {
-    r.x = __funnelshift_r(x[W], x[W + 1], 16);
-    r.y = __funnelshift_r(x[W + 1], x[W + 2], 16);
-    r.z = __funnelshift_r(x[W + 2], x[W + 3], 16);
-    r.w = __funnelshift_r(x[W + 3], x[W + 4], 16);
-  }
-  return r;
-}
-// The 16 bytes at byte `m` (< 16, the same for the whole row) of granules a, b.
-__device__ __forceinline__ uint4 window(const uint4& a, const uint4& b, int m) {
-  const bool half = m & 2;
-  switch (m >> 2) {
-    case 0: return window_at<0>(a, b, half);
-    case 1: return window_at<1>(a, b, half);
-    case 2: return window_at<2>(a, b, half);
-    default: return window_at<3>(a, b, half);
-  }
-}
-
 // Group g's values join the run, the target's apart.
 template <typename T>
 __device__ __forceinline__ void add_group(Run& r, uint4 w, int g, int classes, int y, float& zy) {

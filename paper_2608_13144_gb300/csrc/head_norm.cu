@@ -27,124 +27,129 @@ struct NormArgs {
 
 constexpr uint32_t kAll = 0xffffffffu;
 
-// A unit of B bytes.
-template <int B>
-struct Unit;
-template <>
-struct Unit<16> {
-  using type = uint4;
-};
-template <>
-struct Unit<8> {
-  using type = uint2;
-};
-template <>
-struct Unit<4> {
-  using type = uint32_t;
-};
-template <>
-struct Unit<2> {
-  using type = uint16_t;
-};
-
-// The columns of a thread: units of B bytes, unit u at G u + rank, so that
-// neighbours read next to each other. Values are held in pairs, for instructions
-// that take two.
-// FULL: the row is as wide as its threads' places.
-template <typename T, int B, int G, int P, bool FULL>
+// The columns of a thread: units of 16 bytes. A warp's units follow one another, each
+// of a thread's 32 after the one before, so that neighbours read next to each other.
+// Values are held in pairs, for instructions
+// that take two. FULL: the row is as wide as its threads' places. SHIFTED: rows start
+// anywhere, and their width is not one of whole units.
+template <typename T, int G, int P, bool FULL, bool SHIFTED>
 struct Columns {
-  static constexpr int E = B / (int)sizeof(T), U = P / E;  // values of a unit, units
-  using Word = typename Unit<B>::type;
+  static constexpr int E = 16 / (int)sizeof(T), U = P / E;  // values of a unit, units
   int d, rank;
-  __device__ __forceinline__ int column(int u) const { return (u * G + rank) * E; }
+  __device__ __forceinline__ int place(int u) const { return G == 32 ? u * 32 + rank : (rank & ~31) * U + u * 32 + (rank & 31); }
+  __device__ __forceinline__ int column(int u) const { return place(u) * E; }
   __device__ __forceinline__ bool inside(int u) const { return FULL || column(u) < d; }
-  // f(pair) for each pair with a column; `whole`: both have one
+  __device__ __forceinline__ bool whole(int u) const { return !SHIFTED || column(u) + E <= d; }
+  // f(pair) for each pair of the units inside
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
 #pragma unroll
     for (int k = 0; k < P / 2; ++k)
       if (inside(2 * k / E)) f(k);
   }
-  __device__ __forceinline__ bool whole(int pair) const { return E > 1 || inside(2 * pair + 1); }
-  // a pair's values, 0 for what has no column
-  __device__ __forceinline__ uint64_t masked(uint64_t v, int pair) const {
-    return whole(pair) ? v : v & 0xffffffffull;
+  // a pair's values, 0 for what is past the row
+  __device__ __forceinline__ uint64_t masked(uint64_t v, int k) const {
+    const int u = 2 * k / E, c = column(u) + 2 * k % E;
+    if (whole(u)) return v;
+    return c + 1 < d ? v : c < d ? v & 0xffffffffull : 0;
   }
-  // values of T, as units
-  __device__ static __forceinline__ void open(const Word& w, int u, uint64_t (&v)[P / 2]) {
-    if constexpr (E == 1) {
-      const uint32_t f = __float_as_uint(to_f32<T>(*reinterpret_cast<const T*>(&w)));
-      v[u / 2] = u & 1 ? (v[u / 2] & 0xffffffffull) | (uint64_t)f << 32 : (uint64_t)f;
-    } else {
+  // how many of the thread's columns the row has
+  __device__ __forceinline__ int count() const {
+    int n = 0;
 #pragma unroll
-      for (int k = 0; k < E / 2; ++k) {
-        if constexpr (sizeof(T) == 4) {
-          const uint32_t* x = reinterpret_cast<const uint32_t*>(&w) + 2 * k;
-          v[u * E / 2 + k] = ptx::pack_f32x2(x[0], x[1]);
-        } else {
-          const uint32_t x = reinterpret_cast<const uint32_t*>(&w)[k];
-          v[u * E / 2 + k] = ptx::pack_f32x2(x << 16, x & 0xffff0000u);
-        }
-      }
-    }
+    for (int u = 0; u < U; ++u) n += FULL ? E : min(max(d - column(u), 0), E);
+    return n;
   }
   // The compiler takes units for new ones from here on.
-  __device__ static __forceinline__ void forget(Word (&w)[U]) {
+  __device__ static __forceinline__ void forget(uint4 (&w)[U]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if constexpr (B == 16)
-        asm volatile("" : "+r"(w[u].x), "+r"(w[u].y), "+r"(w[u].z), "+r"(w[u].w));
-      else if constexpr (B == 4)
-        asm volatile("" : "+r"(w[u]));
-      else
-        asm volatile("" : "+h"(w[u]));
-    }
+    for (int u = 0; u < U; ++u) asm volatile("" : "+r"(w[u].x), "+r"(w[u].y), "+r"(w[u].z), "+r"(w[u].w));
   }
   // a pair of the thread's units
-  __device__ static __forceinline__ uint64_t pair(const Word (&w)[U], int k) {
-    if constexpr (E == 1) {
-      return ptx::pack_f32x2(__float_as_uint(to_f32<T>(*reinterpret_cast<const T*>(&w[2 * k]))),
-                             __float_as_uint(to_f32<T>(*reinterpret_cast<const T*>(&w[2 * k + 1]))));
-    } else if constexpr (sizeof(T) == 4) {
-      const uint32_t* x = reinterpret_cast<const uint32_t*>(&w[2 * k / E]) + 2 * k % E;
-      return ptx::pack_f32x2(x[0], x[1]);
-    } else {
-      const uint32_t x = reinterpret_cast<const uint32_t*>(&w[2 * k / E])[k % (E / 2)];
-      return ptx::pack_f32x2(x << 16, x & 0xffff0000u);
-    }
+  __device__ static __forceinline__ uint64_t pair(const uint4 (&w)[U], int k) {
+    const uint4& x = w[2 * k / E];
+    const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+    if constexpr (sizeof(T) == 4)
+      return ptx::pack_f32x2(v[(2 * k) & 3], v[(2 * k + 1) & 3]);
+    else
+      return ptx::pack_f32x2(v[k & 3] << 16, v[k & 3] & 0xffff0000u);
   }
-  // To a row: f(pair)'s values, a unit (or two of one value) at a time.
+  // To a row: f(pair)'s values, a unit at a time. Where rows are shifted, a thread
+  // writes the granule that its unit's first values lie in, with the last ones of the
+  // unit before it; the ends of the warp's units and of the row go value by value.
   template <typename F>
   __device__ __forceinline__ void put(T* p, F&& f) const {
-    constexpr int S = E > 1 ? 1 : 2;  // units of a step
+    const int lead = SHIFTED ? (int)((uintptr_t)p & 15) / (int)sizeof(T) : 0, lane = threadIdx.x & 31;
+    uint4 w{}, first{}, end{};
+    int end_at = -1;
 #pragma unroll
-    for (int u = 0; u < U; u += S)
+    for (int u = 0; u < U; ++u) {
+      const uint4 last = w;
       if (inside(u)) {
-        Word w[S];
+        uint32_t x[4];
 #pragma unroll
-        for (int k = 0; k < E * S / 2; ++k) {
-          const uint64_t x = f(u * E / 2 + k);
-          if constexpr (E == 1) {
-            *reinterpret_cast<T*>(&w[0]) = from_f32<T>(lo_f32(x));
-            *reinterpret_cast<T*>(&w[1]) = from_f32<T>(hi_f32(x));
-          } else if constexpr (sizeof(T) == 4) {
-            reinterpret_cast<uint32_t*>(&w[0])[2 * k] = (uint32_t)x;
-            reinterpret_cast<uint32_t*>(&w[0])[2 * k + 1] = (uint32_t)(x >> 32);
+        for (int k = 0; k < E / 2; ++k) {
+          const uint64_t v = f(u * E / 2 + k);
+          if constexpr (sizeof(T) == 4) {
+            x[2 * k] = (uint32_t)v;
+            x[2 * k + 1] = (uint32_t)(v >> 32);
           } else {
-            reinterpret_cast<uint32_t*>(&w[0])[k] = pack_bf16(lo_f32(x), hi_f32(x));
+            x[k] = pack_bf16(lo_f32(v), hi_f32(v));
           }
         }
-        *reinterpret_cast<Word*>(p + column(u)) = w[0];
-        if constexpr (S == 2)
-          if (inside(u + 1)) *reinterpret_cast<Word*>(p + column(u + 1)) = w[1];
+        w = uint4{x[0], x[1], x[2], x[3]};
       }
+      const int c = column(u);
+      if constexpr (!SHIFTED) {
+        if (inside(u)) *reinterpret_cast<uint4*>(p + c) = w;
+      } else {
+        uint4 joined = w;
+        if (lead) {
+          const bool over = lane == 31;  // hands on to the first lane's next unit
+          uint4 before;
+          const int from = (lane + 31) & 31;
+          before.x = __shfl_sync(kAll, over ? last.x : w.x, from);
+          before.y = __shfl_sync(kAll, over ? last.y : w.y, from);
+          before.z = __shfl_sync(kAll, over ? last.z : w.z, from);
+          before.w = __shfl_sync(kAll, over ? last.w : w.w, from);
+          joined = window(before, w, 16 - lead * (int)sizeof(T));
+          if (u == 0) first = w;
+        }
+        if (lead == 0 || lane > 0 || u > 0) {
+          if (c - lead + E <= d) {
+            *reinterpret_cast<uint4*>(p + (c - lead)) = joined;
+          } else if (c - lead < d) {
+            end = joined;
+            end_at = c - lead;
+          }
+        }
+      }
+    }
+    if constexpr (SHIFTED) {
+      auto some = [&](const uint4& x, int c, int from, int to) {
+        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e >= from && e < to && c + e < d) {
+            if constexpr (sizeof(T) == 4)
+              p[c + e] = __uint_as_float(v[e & 3]);
+            else
+              p[c + e] = __ushort_as_bfloat16((unsigned short)(v[(e / 2) & 3] >> (e & 1 ? 16 : 0)));
+          }
+      };
+      if (lead && (lane == 0 || lane == 31))
+        some(lane ? w : first, column(lane ? U - 1 : 0), lane ? E - lead : 0, lane ? E : E - lead);
+      if (end_at >= 0) some(end, end_at, 0, E);
+    }
   }
   // f(value of the pair array, column) for each value
   template <typename F>
   __device__ __forceinline__ void each_value(const uint64_t (&v)[P / 2], F&& f) const {
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (inside(i / E)) f(i & 1 ? hi_f32(v[i / 2]) : lo_f32(v[i / 2]), column(i / E) + i % E);
+    for (int i = 0; i < P; ++i) {
+      const int c = column(i / E) + i % E;
+      if (FULL || c < d) f(i & 1 ? hi_f32(v[i / 2]) : lo_f32(v[i / 2]), c);
+    }
   }
   // an FP32 array's values, `other` without one
   __device__ __forceinline__ void floats(const float* p, float other, uint64_t (&v)[P / 2]) const {
@@ -152,52 +157,45 @@ struct Columns {
     for (int k = 0; k < P / 2; ++k) {
       float x[2] = {other, other};
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (p && inside((2 * k + h) / E)) x[h] = __ldg(p + column((2 * k + h) / E) + (2 * k + h) % E);
+      for (int h = 0; h < 2; ++h) {
+        const int c = column((2 * k + h) / E) + (2 * k + h) % E;
+        if (p && (FULL || c < d)) x[h] = __ldg(p + c);
+      }
       v[k] = ptx::pack_f32x2(__float_as_uint(x[0]), __float_as_uint(x[1]));
     }
   }
 };
 
-// Rows on their way to a thread: asynchronous copies of its columns into its own
-// places of a ring in shared memory, D rows ahead, or one row ahead in registers
-// (units of two bytes, which cannot be copied so).
-template <typename T, int B, int G, int P, bool FULL, int D>
+// Rows on their way to a group of threads: asynchronous copies of 16 bytes, D rows
+// ahead, to a ring in shared memory. A thread reads what it copied itself, but of
+// shifted rows also its neighbour's granule: barriers stand before the reading and
+// before the next copy to the same place.
+template <typename T, int G, int P, bool FULL, bool SHIFTED, int D>
 struct Feed {
-  using Cols = Columns<T, B, G, P, FULL>;
-  using Word = typename Cols::Word;
-  static constexpr int U = Cols::U;
-  static constexpr bool kRing = B >= 4;
-  static constexpr int kDepth = kRing ? D : 1;
-  static constexpr int kBytes = kRing ? D * P * G * (int)sizeof(T) : 0;  // of a group
-  Word* ring;
-  Word next[kRing ? 1 : U];
+  using Cols = Columns<T, G, P, FULL, SHIFTED>;
+  static constexpr int U = Cols::U, E = Cols::E;
+  static constexpr int kGranules = U * G + (SHIFTED ? 1 : 0);  // of a row
+  static constexpr int kBytes = D * kGranules * 16;            // of a group
+  uint4* ring;
+  __device__ static __forceinline__ int lead_of(const T* p) { return SHIFTED ? (int)((uintptr_t)p & 15) / (int)sizeof(T) : 0; }
   __device__ __forceinline__ void issue(const Cols& at, int slot, const T* p) {
-    if constexpr (kRing) {
-      if (p) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (at.inside(u)) {
-            const uint32_t to = ptx::smem_u32(ring + (slot * U + u) * G + at.rank);
-            if constexpr (B == 16)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(p + at.column(u)) : "memory");
-            else
-              asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(p + at.column(u)), "n"(B) : "memory");
-          }
-      }
-    } else if (p) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (at.inside(u)) next[u] = *reinterpret_cast<const Word*>(p + at.column(u));
-    }
-  }
-  __device__ __forceinline__ Word word(const Cols& at, int slot, int u) const {
-    return kRing ? ring[(slot * U + u) * G + at.rank] : next[kRing ? 0 : u];
-  }
-  __device__ __forceinline__ void take(const Cols& at, int slot, uint64_t (&v)[P / 2]) const {
+    if (!p || at.d == 0) return;  // (a cluster's block past the row has nothing)
+    const int lead = lead_of(p);
+    const uint4* from = reinterpret_cast<const uint4*>(p - lead);
+    auto copy = [&](int j) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(ring + slot * kGranules + j)), "l"(from + j)
+                   : "memory");
+    };
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (at.inside(u)) Cols::open(word(at, slot, u), u, v);
+      if (FULL || at.column(u) < at.d + lead) copy(at.place(u));
+    if (SHIFTED && at.rank == 0 && U * G * E < at.d + lead) copy(U * G);
+  }
+  __device__ __forceinline__ uint4 word(const Cols& at, int slot, int u, int lead) const {
+    const uint4* in = ring + slot * kGranules + at.place(u);
+    if constexpr (SHIFTED)
+      if (lead) return window(in[0], in[1], lead * (int)sizeof(T));
+    return in[0];
   }
 };
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -256,7 +254,9 @@ constexpr int kBlock = G == 32 ? 256 : G;
 // The barrier of a group of G threads among the block's GROUPS.
 template <int G, int GROUPS>
 __device__ __forceinline__ void group_barrier(int group) {
-  if constexpr (GROUPS == 1)
+  if constexpr (G == 32)
+    __syncwarp();
+  else if constexpr (GROUPS == 1)
     __syncthreads();
   else
     asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(G) : "memory");
@@ -264,11 +264,11 @@ __device__ __forceinline__ void group_barrier(int group) {
 
 // Whose rows a group takes: `first`, then every `step`-th; and its columns, from
 // `base` on. A cluster of CL blocks shares a row.
-template <typename T, int B, int G, int P, bool FULL, int CL, int GROUPS>
+template <typename T, int G, int P, bool FULL, bool SHIFTED, int CL, int GROUPS>
 struct Share {
   int64_t first, step;
   int base, slot;
-  Columns<T, B, G, P, FULL> cols;
+  Columns<T, G, P, FULL, SHIFTED> cols;
   __device__ __forceinline__ explicit Share(int d) {
     slot = GROUPS == 1 ? 0 : threadIdx.x / G;
     first = (int64_t)(blockIdx.x / CL) * GROUPS + slot;
@@ -284,19 +284,21 @@ template <typename T, int G, int P>
 constexpr int kNormDepth = G * P * (int)sizeof(T) > 48 * 1024 ? 3 : 4;
 constexpr int kGradDepth = 3;
 
-template <typename T, int B, int G, int P, bool FULL, int CL>
+template <typename T, int G, int P, bool FULL, bool SHIFTED, int CL>
 __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const NormArgs a) {
   extern __shared__ uint4 ring_s[];
   __shared__ NormShared<G, CL> shared;
-  using Rows = Feed<T, B, G, P, FULL, kNormDepth<T, G, P>>;
+  using Rows = Feed<T, G, P, FULL, SHIFTED, kNormDepth<T, G, P>>;
+  using Cols = typename Rows::Cols;
+  constexpr int D = kNormDepth<T, G, P>;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const Share<T, B, G, P, FULL, CL, kBlock<G> / G> at(a.d);
+  const Share<T, G, P, FULL, SHIFTED, CL, kBlock<G> / G> at(a.d);
   Rows feed;
-  feed.ring = reinterpret_cast<typename Rows::Word*>(reinterpret_cast<char*>(ring_s) + at.slot * Rows::kBytes);
+  feed.ring = ring_s + at.slot * (Rows::kBytes / 16);
   auto row = [&](int64_t t) { return t < a.tokens ? x + t * a.ldx + at.base : nullptr; };
 #pragma unroll
-  for (int i = 0; i < Rows::kDepth; ++i) {
+  for (int i = 0; i < D; ++i) {
     feed.issue(at.cols, i, row(at.first + i * at.step));
     commit_copies();
   }
@@ -305,19 +307,29 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const Norm
   at.cols.floats(a.bias ? a.bias + at.base : nullptr, 0.f, b);
   constexpr int W = G / 32;
   const int warp = G == 32 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int mine = 0;  // the warp's columns
-  at.cols.each([&](int k) { mine += at.cols.whole(k) ? 2 : 1; });
-  mine = __reduce_add_sync(kAll, mine);
+  const int mine = __reduce_add_sync(kAll, at.cols.count());  // the warp's columns
   const float n = (float)mine, over_n = mine ? 1.f / n : 0.f, over = 1.f / (float)a.d;
   int turn = 0, slot = 0;
   T* out = y + at.first * a.ldy + at.base;
   for (int64_t t = at.first; t < a.tokens; t += at.step, out += at.step * a.ldy) {
     uint64_t v[P / 2];
-    wait_copies<Rows::kDepth - 1>();
-    feed.take(at.cols, slot, v);
-    feed.issue(at.cols, slot, row(t + Rows::kDepth * at.step));
-    commit_copies();
-    slot = slot + 1 == Rows::kDepth ? 0 : slot + 1;
+    wait_copies<D - 1>();
+    if (SHIFTED) group_barrier<G, kBlock<G> / G>(at.slot);
+    {
+      const int lead = Rows::lead_of(x + t * a.ldx + at.base);
+      uint4 raw[Cols::U];
+#pragma unroll
+      for (int u = 0; u < Cols::U; ++u)
+        if (at.cols.inside(u)) raw[u] = feed.word(at.cols, slot, u, lead);
+      at.cols.each([&](int k) { v[k] = Cols::pair(raw, k); });
+    }
+    auto refill = [&] {
+      feed.issue(at.cols, slot, row(t + D * at.step));
+      commit_copies();
+      slot = slot + 1 == D ? 0 : slot + 1;
+    };
+    if (SHIFTED && G == 32) __syncwarp();
+    if (!SHIFTED || G == 32) refill();
     // the warp's mean c, and its sums s and m2 of x - c and their squares
     uint64_t p = 0;
     at.cols.each([&](int k) { p = ptx::add_f32x2(p, at.cols.masked(v[k], k)); });
@@ -346,6 +358,7 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const Norm
     } else {
       if (lane == 0) shared.warp[turn][warp] = float4{c, s, m2, n};
       __syncthreads();
+      if (SHIFTED) refill();
       const float4 o = shared.warp[turn][lane % W];
       const float first = __shfl_sync(kAll, o.x, 0), away = o.x - first;
       float sum = away * o.w + o.y, count = o.w;
@@ -394,20 +407,20 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const Norm
 
 // Values wait as they were loaded, not as FP32, between the row's sums and its
 // gradient; GROUPS groups of G threads a block, whose columns' sums join there.
-template <typename T, int B, int G, int P, bool FULL, int CL, int GROUPS>
+template <typename T, int G, int P, bool FULL, bool SHIFTED, int CL, int GROUPS>
 __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x, T* dx, const NormArgs a) {
   extern __shared__ uint4 ring_s[];  // the rows' rings; in the end the groups' columns, 2 x d each
   __shared__ NormShared<G, CL> shared_s[GROUPS];
-  using Rows = Feed<T, B, G, P, FULL, kGradDepth>;
+  constexpr int D = kGradDepth;
+  using Rows = Feed<T, G, P, FULL, SHIFTED, D>;
   using Cols = typename Rows::Cols;
-  using Word = typename Rows::Word;
   ptx::wait_prerequisites();
   ptx::launch_dependents();
-  const Share<T, B, G, P, FULL, CL, GROUPS> at(a.d);
+  const Share<T, G, P, FULL, SHIFTED, CL, GROUPS> at(a.d);
   NormShared<G, CL>& shared = shared_s[at.slot];
   Rows feed_x, feed_dy;
-  feed_x.ring = reinterpret_cast<Word*>(reinterpret_cast<char*>(ring_s) + at.slot * 2 * Rows::kBytes);
-  feed_dy.ring = feed_x.ring + Rows::kBytes / B;
+  feed_x.ring = ring_s + at.slot * 2 * (Rows::kBytes / 16);
+  feed_dy.ring = feed_x.ring + Rows::kBytes / 16;
   float2 ahead[2] = {};  // the statistics of the next two rows
   auto issue = [&](int64_t t, int slot) {
     const bool is = t < a.tokens;
@@ -417,7 +430,7 @@ __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x
   };
   auto stats_of = [&](int64_t t) { return t < a.tokens ? float2{__ldg(a.stats + 2 * t), __ldg(a.stats + 2 * t + 1)} : float2{}; };
 #pragma unroll
-  for (int i = 0; i < Rows::kDepth; ++i) issue(at.first + i * at.step, i);
+  for (int i = 0; i < D; ++i) issue(at.first + i * at.step, i);
   ahead[0] = stats_of(at.first);
   ahead[1] = stats_of(at.first + at.step);
   // Weights in registers; where a thread holds 32 columns, in shared memory, a
@@ -441,16 +454,24 @@ __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x
   const float over = 1.f / (float)a.d;
   int turn = 0, slot = 0;
   for (int64_t t = at.first; t < a.tokens; t += at.step) {
-    Word raw_x[Cols::U], raw_dy[Cols::U];
-    wait_copies<Rows::kDepth - 1>();
+    uint4 raw_x[Cols::U], raw_dy[Cols::U];
+    wait_copies<D - 1>();
+    if (SHIFTED) group_barrier<G, GROUPS>(at.slot);
+    {
+      const int lead_x = Rows::lead_of(x + t * a.ldx + at.base), lead_dy = Rows::lead_of(dy + t * a.lddy + at.base);
 #pragma unroll
-    for (int u = 0; u < Cols::U; ++u)
-      if (at.cols.inside(u)) {
-        raw_x[u] = feed_x.word(at.cols, slot, u);
-        raw_dy[u] = feed_dy.word(at.cols, slot, u);
-      }
-    issue(t + Rows::kDepth * at.step, slot);
-    slot = slot + 1 == Rows::kDepth ? 0 : slot + 1;
+      for (int u = 0; u < Cols::U; ++u)
+        if (at.cols.inside(u)) {
+          raw_x[u] = feed_x.word(at.cols, slot, u, lead_x);
+          raw_dy[u] = feed_dy.word(at.cols, slot, u, lead_dy);
+        }
+    }
+    auto refill = [&] {
+      issue(t + D * at.step, slot);
+      slot = slot + 1 == D ? 0 : slot + 1;
+    };
+    if (SHIFTED && G == 32) __syncwarp();
+    if (!SHIFTED || G == 32) refill();
     const float mean = ahead[0].x, rstd = ahead[0].y;
     ahead[0] = ahead[1];
     ahead[1] = stats_of(t + 2 * at.step);
@@ -472,6 +493,7 @@ __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x
     } else {
       if ((lane & 7) == 0 && lane != 24) reinterpret_cast<float*>(&shared.warp[turn][warp])[lane == 8 ? 2 : lane >> 4] = part;
       group_barrier<G, GROUPS>(at.slot);
+      if (SHIFTED) refill();
       const float4 o = shared.warp[turn][lane % W];
       sum[0] = o.x, sum[1] = o.y, sum[2] = o.z;
 #pragma unroll
@@ -494,7 +516,7 @@ __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x
     const float off = sum[0] * over, mean_g = sum[1] * over, mean_gx = sum[2] * over - off * mean_g;
     const uint64_t less = both(-off), down = both(-mean_g * rstd), along = both(-mean_gx * rstd);
     auto step = [&](int k) {
-      const uint64_t g = Cols::pair(raw_dy, k);
+      const uint64_t g = at.cols.masked(Cols::pair(raw_dy, k), k);
       const uint64_t xh = ptx::add_f32x2(ptx::mul_f32x2(ptx::add_f32x2(Cols::pair(raw_x, k), minus_mean), r), less);
       dw[k] = ptx::fma_f32x2(g, xh, dw[k]);
       db[k] = ptx::add_f32x2(db[k], g);
@@ -609,11 +631,10 @@ void by_width(int d, F&& f) {
     f(Int<512>{}, Int<32>{}, Int<4>{});
 }
 // f(G, P, CL, GROUPS) of the gradient, which holds a thread's columns four times over
-// (FP32 values; packed BF16 ones, not those of single units, take half the
-// registers).
-template <typename T, int B, typename F>
+// (FP32 values; BF16 ones take half the registers).
+template <typename T, typename F>
 void by_width_grad(int d, F&& f) {
-  constexpr bool kPacked = sizeof(T) == 2 && B > 2;
+  constexpr bool kPacked = sizeof(T) == 2;
   if (d <= 256) {
     f(Int<32>{}, Int<8>{}, Int<1>{}, Int<8>{});
   } else if (d <= 512) {
@@ -643,42 +664,31 @@ void by_width_grad(int d, F&& f) {
     f(Int<512>{}, Int<16>{}, Int<8>{}, Int<1>{});
   }
 }
-// f(B) with the largest unit that divides every address and row; f(FULL), which has
-// kernels of its own for the largest unit.
-template <typename T, typename F>
-void by_alignment(uintptr_t bits, F&& f) {
-  if (bits % 16 == 0)
-    f(Int<16>{});
-  else if (sizeof(T) == 2 && bits % 4 == 0)
-    f(Int<4>{});
+// f(FULL, SHIFTED) for `bits`, every address and row in bytes, or'ed.
+template <typename F>
+void by_alignment(uintptr_t bits, bool full, F&& f) {
+  if (bits % 16)
+    f(std::false_type{}, std::true_type{});
+  else if (full)
+    f(std::true_type{}, std::false_type{});
   else
-    f(Int<(int)sizeof(T)>{});
-}
-template <int B, typename F>
-void by_fullness(bool full, F&& f) {
-  if constexpr (B == 16) {
-    if (full) return f(std::true_type{});
-  }
-  f(std::false_type{});
+    f(std::false_type{}, std::false_type{});
 }
 
 template <typename T>
 void launch_norm(const T* x, T* y, const NormArgs& a, cudaStream_t s) {
   const uintptr_t bits = (uintptr_t)x | (uintptr_t)y | (uintptr_t)(a.ldx * sizeof(T)) | (uintptr_t)(a.ldy * sizeof(T)) |
                          (uintptr_t)(a.d * sizeof(T));
-  by_alignment<T>(bits, [&](auto b) {
-    by_width(a.d, [&](auto g, auto p, auto cl) {
-      constexpr int B = decltype(b)::value;
-       by_fullness<B>(a.d == g * p * cl, [&](auto full) {
-          constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value;
-          constexpr bool FULL = decltype(full)::value;
-          constexpr int kSmem = kBlock<G> / G * Feed<T, B, G, P, FULL, kNormDepth<T, G, P>>::kBytes;
-          const auto kernel = k_norm<T, B, G, P, FULL, CL>;
-          if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
-          static const int kResident = resident_blocks(kernel, kBlock<G>, kSmem);
-          const int blocks = (int)std::min<int64_t>(ceil_div(a.tokens, kBlock<G> / G), kResident / CL);
-          launch_cluster<CL>(kernel, blocks, kBlock<G>, kSmem, s, x, y, a);
-        });
+  by_width(a.d, [&](auto g, auto p, auto cl) {
+    by_alignment(bits, a.d == g * p * cl, [&](auto full, auto shifted) {
+      constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value;
+      constexpr bool FULL = decltype(full)::value, SHIFTED = decltype(shifted)::value;
+      constexpr int kSmem = kBlock<G> / G * Feed<T, G, P, FULL, SHIFTED, kNormDepth<T, G, P>>::kBytes;
+      const auto kernel = k_norm<T, G, P, FULL, SHIFTED, CL>;
+      if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
+      static const int kResident = resident_blocks(kernel, kBlock<G>, kSmem);
+      const int blocks = (int)std::min<int64_t>(ceil_div(a.tokens, kBlock<G> / G), kResident / CL);
+      launch_cluster<CL>(kernel, blocks, kBlock<G>, kSmem, s, x, y, a);
     });
   });
   LC_LAUNCH_CHECK("k_norm");
@@ -690,21 +700,18 @@ void launch_norm_grad(const T* dy, const T* x, T* dx, const NormArgs& a, float* 
                          (uintptr_t)(a.lddy * sizeof(T)) | (uintptr_t)(dx ? a.lddx * sizeof(T) : 0) |
                          (uintptr_t)(a.d * sizeof(T));
   int blocks = 0;
-  by_alignment<T>(bits, [&](auto b) {
-    constexpr int B = decltype(b)::value;
-    by_width_grad<T, B>(a.d, [&](auto g, auto p, auto cl, auto groups) {
-      by_fullness<B>(a.d == g * p * cl, [&](auto full) {
-        constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value;
-        constexpr int GROUPS = decltype(groups)::value;
-        constexpr bool FULL = decltype(full)::value;
-        constexpr int kRing = GROUPS * 2 * Feed<T, B, G, P, FULL, kGradDepth>::kBytes;
-        constexpr int kSums = GROUPS > 1 ? GROUPS * 2 * G * P * 4 : 0, kSmem = kRing > kSums ? kRing : kSums;
-        const auto kernel = k_norm_grad<T, B, G, P, FULL, CL, GROUPS>;
-        if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
-        static const int kResident = resident_blocks(kernel, G * GROUPS, kSmem);
-        blocks = (int)std::min<int64_t>(ceil_div(a.tokens, GROUPS), kResident / CL);
-        launch_cluster<CL>(kernel, blocks, G * GROUPS, kSmem, s, dy, x, dx, a);
-      });
+  by_width_grad<T>(a.d, [&](auto g, auto p, auto cl, auto groups) {
+    by_alignment(bits, a.d == g * p * cl, [&](auto full, auto shifted) {
+      constexpr int G = decltype(g)::value, P = decltype(p)::value, CL = decltype(cl)::value;
+      constexpr int GROUPS = decltype(groups)::value;
+      constexpr bool FULL = decltype(full)::value, SHIFTED = decltype(shifted)::value;
+      constexpr int kRing = GROUPS * 2 * Feed<T, G, P, FULL, SHIFTED, kGradDepth>::kBytes;
+      constexpr int kSums = GROUPS > 1 ? GROUPS * 2 * G * P * 4 : 0, kSmem = kRing > kSums ? kRing : kSums;
+      const auto kernel = k_norm_grad<T, G, P, FULL, SHIFTED, CL, GROUPS>;
+      if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
+      static const int kResident = resident_blocks(kernel, G * GROUPS, kSmem);
+      blocks = (int)std::min<int64_t>(ceil_div(a.tokens, GROUPS), kResident / CL);
+      launch_cluster<CL>(kernel, blocks, G * GROUPS, kSmem, s, dy, x, dx, a);
     });
   });
   LC_LAUNCH_CHECK("k_norm_grad");
