@@ -61,6 +61,8 @@ struct Teacher {
     bool out = false, own[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
+      q[i] = 0.f, own[i] = false, log_q[i] = -INFINITY;
+      if (i > 0 && L * i >= a.k) continue;
       const uint32_t b = (__ballot_sync(kAll, v[i] == best) >> base) & (L == 32 ? kAll : (1u << (L & 31)) - 1);
       own[i] = !out && b && __ffs(b) - 1 == lane;
       out = out || b;
@@ -106,6 +108,7 @@ struct Teacher {
     float loss = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
+      if (i > 0 && L * i >= a.k) continue;
       const float lp = sums.none || zj[i] == -INFINITY ? -INFINITY : (zj[i] - sums.m) / a.temperature - log_sum;
       if (q[i] > 0.f) loss += q[i] * (log_q[i] - lp);
       // p - q; where both are near 1, the difference of what they leave to others
@@ -184,12 +187,13 @@ __global__ void __launch_bounds__(128) k_distill_lanes(const T* z, T* dz, const 
     if (live && teacher.first[i]) dr[teacher.index[i]] = from_f32<T>(at[i]);
 }
 
-// Larger rows: a block of G threads each, or a cluster of CL blocks that split it.
-// RESIDENT: a thread copies its granules (16 at most) to shared memory, four at a
-// time, and reads them there twice.
+// Larger rows: a block of G threads each, or a cluster of CL blocks that split it. The
+// last warp has the teacher, the S others the row's granules. RESIDENT: a thread copies
+// its granules (16 at most) to shared memory, four at a time, and reads them there
+// twice.
 template <typename T, int G, int CL, bool RESIDENT>
 __global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(const T* z, T* dz, const DistillArgs a) {
-  constexpr int R = LIPCACHE_MAX_TOP / 32, U = 4;
+  constexpr int R = LIPCACHE_MAX_TOP / 32, U = 4, S = G - 32;
   extern __shared__ uint4 row_s[];
   __shared__ JoinShared<G> join;
   __shared__ int index_s[LIPCACHE_MAX_TOP], live_s, twice_s;
@@ -197,6 +201,7 @@ __global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(con
   ptx::wait_prerequisites();
   ptx::launch_dependents();
   const int rank = threadIdx.x, lane = rank & 31, block = CL > 1 ? (int)ptx::cluster_ctarank() : 0;
+  const bool teaching = rank >= S;
   const int64_t t = blockIdx.x / CL;
   const T* zr = z + t * a.ldz;
   T* dr = dz ? dz + t * a.ldd : nullptr;
@@ -204,25 +209,13 @@ __global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(con
   const int share = (row.count + CL - 1) / CL, begin = min(block * share, row.count), end = min(begin + share, row.count);
   const Slice at(row, begin, end, a.classes);
   auto get = [&](int i) { return row.granules[i]; };
-  if constexpr (RESIDENT) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = at.first + (k * U + u) * G + rank;
-        if (i < at.last) {
-          const uint32_t to = ptx::smem_u32(row_s + (i - begin));
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row.granules + i) : "memory");
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-  }
   const float w = a.weight ? __ldg(a.weight + t) : 1.f;
-  const bool first_warp = rank < 32;
+  const Scale k{a.c, 0.f};
   Teacher<32, R> teacher;
   float zj[R], grad[R];
-  if (first_warp) {
+  // the sums of any row: which have a teacher the other warps know from the join on
+  RowPart<T, false> part;
+  if (teaching) {
     teacher.load(a, t, lane, true);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -233,43 +226,53 @@ __global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(con
       live_s = w == 0.f || !teacher.any ? 0 : teacher.bad ? 2 : 1;
       twice_s = 0;
     }
-  }
-  // the sums of any row: which have a teacher the other warps know from the join on
-  const Scale k{a.c, 0.f};
-  RowPart<T, false> part;
-  if constexpr (RESIDENT) {
+  } else {
+    if constexpr (RESIDENT) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      if (b == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
-      if (b == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
-      if (b == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-      if (b == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
-      int i = at.first + b * U * G + rank;
-      const bool whole = i + (U - 1) * G < at.last;
-      uint4 x[U];
-      if (whole) {
+      for (int b = 0; b < 4; ++b) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = row_s[i + u * G - begin];
+        for (int u = 0; u < U; ++u) {
+          const int i = at.first + (b * U + u) * S + rank;
+          if (i < at.last) {
+            const uint32_t to = ptx::smem_u32(row_s + (i - begin));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row.granules + i) : "memory");
+          }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
-      if (b == 0) part.start(whole ? part.top_of(x) : -INFINITY, k);
-      if (whole) {
-        part.add(x, k);
-      } else {
-        for (; i < at.last && i < at.first + (b + 1) * U * G; i += G) {
-          const uint4 one[1] = {row_s[i - begin]};
-          part.add(one, k);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if (b == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        if (b == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
+        if (b == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+        if (b == 3) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        int i = at.first + b * U * S + rank;
+        const bool whole = i + (U - 1) * S < at.last;
+        uint4 x[U];
+        if (whole) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) x[u] = row_s[i + u * S - begin];
+        }
+        if (b == 0) part.start(whole ? part.top_of(x) : -INFINITY, k);
+        if (whole) {
+          part.add(x, k);
+        } else {
+          for (; i < at.last && i < at.first + (b + 1) * U * S; i += S) {
+            const uint4 one[1] = {row_s[i - begin]};
+            part.add(one, k);
+          }
         }
       }
+      const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
+      if (edge >= 0) {
+        const uint4 one[1] = {masked_outside<T>(get(edge), row.first(edge), a.classes)};
+        part.add(one, k);
+      }
+    } else {
+      part = sum_part<T, S, false, U>(row, at, a.classes, rank, k, get);
     }
-    const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
-    if (edge >= 0) {
-      const uint4 one[1] = {masked_outside<T>(get(edge), row.first(edge), a.classes)};
-      part.add(one, k);
-    }
-  } else {
-    part = sum_part<T, G, false, U>(row, at, a.classes, rank, k, get);
   }
-  RowSums sums = join_block<T, G, false>(part, row, at, a.classes, a.c, get, join, [&] {
+  RowSums sums = join_block<T, G, S, false>(part, row, at, a.classes, a.c, get, join, [&] {
     // whether a class is named twice: four threads an entry
     for (int e = rank; e < 4 * a.k; e += G) {
       const int entry = e >> 2, mine = index_s[entry];
@@ -306,36 +309,47 @@ __global__ void __launch_bounds__(G, RESIDENT && G == 512 ? 2 : 1) k_distill(con
       }
     }
   }
-  float fill = 0.f, loss = 0.f;
   if (live == 1 && isnan(sums.m)) live = 2;
-  if (live == 2) fill = loss = NAN;
-  if (first_warp && live == 1) {
-    if (twice_s) teacher.join_same(a.k, lane);
-    loss = w * a.temperature * a.temperature * warp_sum(teacher.divergence(a, sums, w, zj, grad));
-  }
-  if (a.loss && rank == 0 && block == 0) a.loss[t] = loss;
-  if (dr) {
-    if (live == 1 && sums.none) live = 0;  // masked whole
-    const RowGradient gradient(a, sums, w);
-    const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
-    if (live == 1 && same) {
-      uint4* out = reinterpret_cast<uint4*>(dr + row.first(at.first));
-#pragma unroll 4
-      for (int i = rank; i < at.last - at.first; i += G)
-        out[i] = gradient.of<T>(RESIDENT ? row_s[at.first - begin + i] : get(at.first + i));
-    } else {
-      for (int i = at.first + rank; i < at.last; i += G) {
-        const uint4 x = RESIDENT ? row_s[i - begin] : get(i);
-        put_granule<T>(dr, same, live == 1 ? gradient.of<T>(x) : granule_of<T>(fill), row.first(i), a.classes);
-      }
+  if (teaching) {
+    float loss = live == 2 ? NAN : 0.f;
+    if (live == 1) {
+      if (twice_s) teacher.join_same(a.k, lane);
+      loss = w * a.temperature * a.temperature * warp_sum(teacher.divergence(a, sums, w, zj, grad));
     }
-    const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
-    if (edge >= 0)
-      put_granule<T>(dr, same, live == 1 ? gradient.of<T>(get(edge)) : granule_of<T>(fill), row.first(edge), a.classes);
+    if (a.loss && lane == 0 && block == 0) a.loss[t] = loss;
+  }
+  if (live == 1 && sums.none) live = 0;  // masked whole
+  if (dr) {
+    if (!teaching) {
+      const RowGradient gradient(a, sums, w);
+      const uint4 fill = granule_of<T>(live == 2 ? NAN : 0.f);
+      const bool same = (((uintptr_t)dr ^ (uintptr_t)zr) & 15) == 0;
+      if (live == 1 && same) {
+        uint4* out = reinterpret_cast<uint4*>(dr + row.first(at.first));
+        const int n = at.last - at.first;
+        for (int i = rank; i < n; i += U * S) {
+          // (loads of a batch before its stores, which may be to the same array)
+          uint4 x[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (i + u * S < n) x[u] = RESIDENT ? row_s[at.first - begin + i + u * S] : get(at.first + i + u * S);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (i + u * S < n) out[i + u * S] = gradient.of<T>(x[u]);
+        }
+      } else {
+        for (int i = at.first + rank; i < at.last; i += S) {
+          const uint4 x = RESIDENT ? row_s[i - begin] : get(i);
+          put_granule<T>(dr, same, live == 1 ? gradient.of<T>(x) : fill, row.first(i), a.classes);
+        }
+      }
+      const int edge = rank == 0 ? at.head : rank == 1 ? at.tail : -1;
+      if (edge >= 0) put_granule<T>(dr, same, live == 1 ? gradient.of<T>(get(edge)) : fill, row.first(edge), a.classes);
+    }
     __syncthreads();
     // (each block those of its own classes)
     const int low = row.first(begin), high = row.first(end);
-    if (first_warp && live == 1) {
+    if (teaching && live == 1) {
 #pragma unroll
       for (int i = 0; i < R; ++i)
         if (teacher.first[i] && teacher.index[i] >= low && teacher.index[i] < high) dr[teacher.index[i]] = from_f32<T>(grad[i]);
@@ -361,6 +375,7 @@ bool distill_lanes(const T* z, T* dz, const DistillArgs& a, int granules, cudaSt
 }
 
 constexpr int kResidentBytes = 111 * 1024;  // twice on an SM, beside what is static
+static_assert(16 * 480 * 16 > kResidentBytes, "a thread holds 16 granules");
 
 template <typename T, int G, int CL, bool RESIDENT>
 void launch_blocks(const T* z, T* dz, const DistillArgs& a, int granules, cudaStream_t s) {
@@ -390,7 +405,7 @@ void launch_distill(const T* z, T* dz, const DistillArgs& a, cudaStream_t s) {
   if (distill_lanes<T, 8>(z, dz, a, granules, s) || distill_lanes<T, 16>(z, dz, a, granules, s) ||
       distill_lanes<T, 32>(z, dz, a, granules, s)) {
   } else if (granules <= 2048) {
-    launch_blocks<T, 128, 1, true>(z, dz, a, granules, s);
+    launch_blocks<T, 160, 1, true>(z, dz, a, granules, s);
   } else if (granules <= kMost && a.tokens > 32) {
     launch_blocks<T, 512, 1, true>(z, dz, a, granules, s);
   } else if (granules <= 4 * kMost && a.tokens > 32) {

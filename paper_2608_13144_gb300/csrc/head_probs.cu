@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(G, (CL > 1 ? 768 : 1536) / G) k_probs(const T*
   }
   const auto part = sum_part<T, G, true, 4>(row, at, a.classes, rank, Scale{a.c, a.reach}, get);
   select.key[rank] = part.key();
-  RowSums sums = join_block<T, G, true>(part, row, at, a.classes, a.c, get, join, [&] {
+  RowSums sums = join_block<T, G, G, true>(part, row, at, a.classes, a.c, get, join, [&] {
     if (rank < 32 && a.k) find_threshold<G>(select, a.k);
   });
   if constexpr (CL == 1) {

@@ -374,11 +374,11 @@ struct JoinShared {
   float s[W], q[W], own, again;
 };
 
-// The block's sums from its threads'. Where the row is nearly sure, the sum of the
+// The block's sums from its G threads', of which STRIDE have granules. Where the row is nearly sure, the sum of the
 // thread that holds the maximum has lost the others' last bits beside it: its warp
 // takes that thread's granules again. meanwhile(): what warps do besides, between the
 // two barriers.
-template <typename T, int G, bool MEAN, typename Get, typename F>
+template <typename T, int G, int STRIDE, bool MEAN, typename Get, typename F>
 __device__ __forceinline__ RowSums join_block(const RowPart<T, MEAN>& part, const RowSpan<T>& row, const Slice& at, int n,
                                               float c, Get get, JoinShared<G>& sh, F&& meanwhile) {
   constexpr int W = G / 32;
@@ -433,7 +433,7 @@ __device__ __forceinline__ RowSums join_block(const RowPart<T, MEAN>& part, cons
           if (z < r.m) again += exp2_of((z - r.m) * c);
         }
       };
-      for (int i = at.first + thread + lane * G; i < at.last; i += 32 * G) take(i, false);
+      for (int i = at.first + thread + lane * STRIDE; i < at.last; i += 32 * STRIDE) take(i, false);
       const int edge = thread == 0 ? at.head : thread == 1 ? at.tail : -1;
       if (lane == 0 && edge >= 0) take(edge, true);
       again = warp_sum(again);
