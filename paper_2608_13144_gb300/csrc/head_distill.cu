@@ -406,7 +406,9 @@ void launch_distill(const T* z, T* dz, const DistillArgs& a, cudaStream_t s) {
       distill_lanes<T, 32>(z, dz, a, granules, s)) {
   } else if (granules <= 2048) {
     launch_blocks<T, 160, 1, true>(z, dz, a, granules, s);
-  } else if (granules <= kMost && a.tokens > 32) {
+  } else if (granules <= 4096 || (granules <= kMost && a.tokens > 32)) {
+    // (few rows: of 20,001 BF16 classes 7.5 us in a block, 8.8 in a cluster, of 50,001
+    // 10.2 and 8.9)
     launch_blocks<T, 512, 1, true>(z, dz, a, granules, s);
   } else if (granules <= 4 * kMost && a.tokens > 32) {
     launch_blocks<T, 512, 4, true>(z, dz, a, granules, s);
