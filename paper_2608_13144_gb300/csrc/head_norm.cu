@@ -27,33 +27,32 @@ struct NormArgs {
 
 constexpr uint32_t kAll = 0xffffffffu;
 
-// The columns of a thread: units of 16 bytes. A warp's units follow one another, each
-// of a thread's 32 after the one before, so that neighbours read next to each other.
-// Values are held in pairs, for instructions
-// that take two. FULL: the row is as wide as its threads' places. SHIFTED: rows start
-// anywhere, and their width is not one of whole units.
+// The columns of a thread: units of 16 bytes, or, where rows start anywhere or their
+// width is not one of whole units (SHIFTED), of 4. A warp's units follow one another,
+// each of a thread's 32 after the one before, so that neighbours read next to each
+// other. Values are held in pairs, for instructions that take two. FULL: the row is as
+// wide as its threads' places.
 template <typename T, int G, int P, bool FULL, bool SHIFTED>
 struct Columns {
-  static constexpr int E = 16 / (int)sizeof(T), U = P / E;  // values of a unit, units
+  static constexpr int B = SHIFTED ? 4 : 16, E = B / (int)sizeof(T), U = P / E;  // bytes, values of a unit; units
+  using Word = typename std::conditional<SHIFTED, uint32_t, uint4>::type;
   int d, rank;
-  __device__ __forceinline__ int place(int u) const { return G == 32 ? u * 32 + rank : (rank & ~31) * U + u * 32 + (rank & 31); }
-  __device__ __forceinline__ int column(int u) const { return place(u) * E; }
+  __device__ __forceinline__ int column(int u) const { return ((rank & ~31) * U + u * 32 + (rank & 31)) * E; }
   __device__ __forceinline__ bool inside(int u) const { return FULL || column(u) < d; }
-  __device__ __forceinline__ bool whole(int u) const { return !SHIFTED || column(u) + E <= d; }
-  // f(pair) for each pair of the units inside
+  // f(pair) for each pair with a column
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
 #pragma unroll
     for (int k = 0; k < P / 2; ++k)
       if (inside(2 * k / E)) f(k);
   }
-  // a pair's values, 0 for what is past the row
+  // the column of a pair's second value
+  __device__ __forceinline__ int second(int k) const { return E == 1 ? column(2 * k + 1) : column(2 * k / E) + 2 * k % E + 1; }
+  // a pair with a column; its second value 0 if that has none
   __device__ __forceinline__ uint64_t masked(uint64_t v, int k) const {
-    const int u = 2 * k / E, c = column(u) + 2 * k % E;
-    if (whole(u)) return v;
-    return c + 1 < d ? v : c < d ? v & 0xffffffffull : 0;
+    return !SHIFTED || second(k) < d ? v : v & 0xffffffffull;
   }
-  // how many of the thread's columns the row has
+  // how many columns the thread has
   __device__ __forceinline__ int count() const {
     int n = 0;
 #pragma unroll
@@ -61,85 +60,90 @@ struct Columns {
     return n;
   }
   // The compiler takes units for new ones from here on.
-  __device__ static __forceinline__ void forget(uint4 (&w)[U]) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) asm volatile("" : "+r"(w[u].x), "+r"(w[u].y), "+r"(w[u].z), "+r"(w[u].w));
-  }
-  // a pair of the thread's units
-  __device__ static __forceinline__ uint64_t pair(const uint4 (&w)[U], int k) {
-    const uint4& x = w[2 * k / E];
-    const uint32_t v[4] = {x.x, x.y, x.z, x.w};
-    if constexpr (sizeof(T) == 4)
-      return ptx::pack_f32x2(v[(2 * k) & 3], v[(2 * k + 1) & 3]);
-    else
-      return ptx::pack_f32x2(v[k & 3] << 16, v[k & 3] & 0xffff0000u);
-  }
-  // To a row: f(pair)'s values, a unit at a time. Where rows are shifted, a thread
-  // writes the granule that its unit's first values lie in, with the last ones of the
-  // unit before it; the ends of the warp's units and of the row go value by value.
-  template <typename F>
-  __device__ __forceinline__ void put(T* p, F&& f) const {
-    const int lead = SHIFTED ? (int)((uintptr_t)p & 15) / (int)sizeof(T) : 0, lane = threadIdx.x & 31;
-    uint4 w{}, first{}, end{};
-    int end_at = -1;
+  __device__ static __forceinline__ void forget(Word (&w)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint4 last = w;
-      if (inside(u)) {
-        uint32_t x[4];
-#pragma unroll
-        for (int k = 0; k < E / 2; ++k) {
-          const uint64_t v = f(u * E / 2 + k);
-          if constexpr (sizeof(T) == 4) {
-            x[2 * k] = (uint32_t)v;
-            x[2 * k + 1] = (uint32_t)(v >> 32);
-          } else {
-            x[k] = pack_bf16(lo_f32(v), hi_f32(v));
-          }
-        }
-        w = uint4{x[0], x[1], x[2], x[3]};
-      }
-      const int c = column(u);
-      if constexpr (!SHIFTED) {
-        if (inside(u)) *reinterpret_cast<uint4*>(p + c) = w;
-      } else {
-        uint4 joined = w;
-        if (lead) {
-          const bool over = lane == 31;  // hands on to the first lane's next unit
-          uint4 before;
-          const int from = (lane + 31) & 31;
-          before.x = __shfl_sync(kAll, over ? last.x : w.x, from);
-          before.y = __shfl_sync(kAll, over ? last.y : w.y, from);
-          before.z = __shfl_sync(kAll, over ? last.z : w.z, from);
-          before.w = __shfl_sync(kAll, over ? last.w : w.w, from);
-          joined = window(before, w, 16 - lead * (int)sizeof(T));
-          if (u == 0) first = w;
-        }
-        if (lead == 0 || lane > 0 || u > 0) {
-          if (c - lead + E <= d) {
-            *reinterpret_cast<uint4*>(p + (c - lead)) = joined;
-          } else if (c - lead < d) {
-            end = joined;
-            end_at = c - lead;
-          }
-        }
-      }
+      if constexpr (SHIFTED)
+        asm volatile("" : "+r"(w[u]));
+      else
+        asm volatile("" : "+r"(w[u].x), "+r"(w[u].y), "+r"(w[u].z), "+r"(w[u].w));
     }
-    if constexpr (SHIFTED) {
-      auto some = [&](const uint4& x, int c, int from, int to) {
-        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+  }
+  // a pair of the thread's units
+  __device__ static __forceinline__ uint64_t pair(const Word (&w)[U], int k) {
+    if constexpr (E == 1) {
+      return ptx::pack_f32x2(w[2 * k], w[2 * k + 1]);
+    } else if constexpr (SHIFTED) {
+      return ptx::pack_f32x2(w[k] << 16, w[k] & 0xffff0000u);
+    } else {
+      const uint4& x = w[2 * k / E];
+      const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+      if constexpr (sizeof(T) == 4)
+        return ptx::pack_f32x2(v[(2 * k) & 3], v[(2 * k + 1) & 3]);
+      else
+        return ptx::pack_f32x2(v[k & 3] << 16, v[k & 3] & 0xffff0000u);
+    }
+  }
+  // To a row: f(pair)'s values, a unit (or two of one value) at a time. BF16 rows that
+  // start between two words: a thread writes the word that its unit's first value ends,
+  // with the unit before it; at the ends of the warp's units and of the row single values.
+  template <typename F>
+  __device__ __forceinline__ void put(T* p, F&& f) const {
+    if constexpr (!SHIFTED) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (e >= from && e < to && c + e < d) {
-            if constexpr (sizeof(T) == 4)
-              p[c + e] = __uint_as_float(v[e & 3]);
-            else
-              p[c + e] = __ushort_as_bfloat16((unsigned short)(v[(e / 2) & 3] >> (e & 1 ? 16 : 0)));
+      for (int u = 0; u < U; ++u)
+        if (inside(u)) {
+          uint32_t x[4];
+#pragma unroll
+          for (int k = 0; k < E / 2; ++k) {
+            const uint64_t v = f(u * E / 2 + k);
+            if constexpr (sizeof(T) == 4) {
+              x[2 * k] = (uint32_t)v;
+              x[2 * k + 1] = (uint32_t)(v >> 32);
+            } else {
+              x[k] = pack_bf16(lo_f32(v), hi_f32(v));
+            }
           }
-      };
-      if (lead && (lane == 0 || lane == 31))
-        some(lane ? w : first, column(lane ? U - 1 : 0), lane ? E - lead : 0, lane ? E : E - lead);
-      if (end_at >= 0) some(end, end_at, 0, E);
+          *reinterpret_cast<uint4*>(p + column(u)) = uint4{x[0], x[1], x[2], x[3]};
+        }
+    } else if constexpr (E == 1) {
+#pragma unroll
+      for (int k = 0; k < P / 2; ++k)
+        if (inside(2 * k)) {
+          const uint64_t v = f(k);
+          p[column(2 * k)] = lo_f32(v);
+          if (inside(2 * k + 1)) p[column(2 * k + 1)] = hi_f32(v);
+        }
+    } else {
+      const bool between = (uintptr_t)p & 2;
+      const int lane = threadIdx.x & 31;
+      auto one = [&](int c, uint32_t bits) { p[c] = __ushort_as_bfloat16((unsigned short)bits); };
+      uint32_t x = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t last = x;
+        const int c = column(u);
+        if (inside(u)) {
+          const uint64_t v = f(u);
+          x = pack_bf16(lo_f32(v), hi_f32(v));
+        }
+        if (!between) {
+          if (c + 1 < d)
+            *reinterpret_cast<uint32_t*>(p + c) = x;
+          else if (c < d)
+            one(c, x);
+        } else {
+          // (the first lane's unit follows the last lane's unit before)
+          const uint32_t before = __shfl_sync(kAll, lane == 31 ? last : x, (lane + 31) & 31);
+          if (c < d) {
+            if (u > 0 || lane > 0)
+              *reinterpret_cast<uint32_t*>(p + c - 1) = __funnelshift_r(before, x, 16);
+            else
+              one(c, x);
+            if (c + 1 < d && (c + 2 >= d || (u == U - 1 && lane == 31))) one(c + 1, x >> 16);
+          }
+        }
+      }
     }
   }
   // f(value of the pair array, column) for each value
@@ -167,35 +171,53 @@ struct Columns {
 };
 
 // Rows on their way to a group of threads: asynchronous copies of 16 bytes, D rows
-// ahead, to a ring in shared memory. A thread reads what it copied itself, but of
-// shifted rows also its neighbour's granule: barriers stand before the reading and
-// before the next copy to the same place.
+// ahead, to a ring in shared memory. A thread reads what it copied itself; of shifted
+// rows also others' granules: barriers stand before the reading and before the next
+// copy to the same place.
 template <typename T, int G, int P, bool FULL, bool SHIFTED, int D>
 struct Feed {
   using Cols = Columns<T, G, P, FULL, SHIFTED>;
-  static constexpr int U = Cols::U, E = Cols::E;
-  static constexpr int kGranules = U * G + (SHIFTED ? 1 : 0);  // of a row
-  static constexpr int kBytes = D * kGranules * 16;            // of a group
+  using Word = typename Cols::Word;
+  static constexpr int N = 16 / (int)sizeof(T), C = P / N;  // values of a granule, granules of a thread
+  static constexpr int kGranules = C * G + (SHIFTED ? 1 : 0);
+  static constexpr int kBytes = D * kGranules * 16;  // of a group
   uint4* ring;
-  __device__ static __forceinline__ int lead_of(const T* p) { return SHIFTED ? (int)((uintptr_t)p & 15) / (int)sizeof(T) : 0; }
   __device__ __forceinline__ void issue(const Cols& at, int slot, const T* p) {
     if (!p || at.d == 0) return;  // (a cluster's block past the row has nothing)
-    const int lead = lead_of(p);
+    const int lead = SHIFTED ? (int)((uintptr_t)p & 15) / (int)sizeof(T) : 0;
     const uint4* from = reinterpret_cast<const uint4*>(p - lead);
     auto copy = [&](int j) {
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(ring + slot * kGranules + j)), "l"(from + j)
                    : "memory");
     };
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (FULL || at.column(u) < at.d + lead) copy(at.place(u));
-    if (SHIFTED && at.rank == 0 && U * G * E < at.d + lead) copy(U * G);
+    for (int v = 0; v < C; ++v) {
+      const int j = (at.rank & ~31) * C + v * 32 + (at.rank & 31);
+      if (FULL || j * N < at.d + lead) copy(j);
+    }
+    if (SHIFTED && at.rank == 0 && C * G * N < at.d + lead) copy(C * G);
   }
-  __device__ __forceinline__ uint4 word(const Cols& at, int slot, int u, int lead) const {
-    const uint4* in = ring + slot * kGranules + at.place(u);
-    if constexpr (SHIFTED)
-      if (lead) return window(in[0], in[1], lead * (int)sizeof(T));
-    return in[0];
+  // the thread's units of the row at p
+  __device__ __forceinline__ void take(const Cols& at, int slot, const T* p, Word (&w)[Cols::U]) const {
+    const Word* in = reinterpret_cast<const Word*>(ring + slot * kGranules);
+    if constexpr (!SHIFTED) {
+#pragma unroll
+      for (int u = 0; u < Cols::U; ++u)
+        if (at.inside(u)) w[u] = in[at.column(u) / Cols::E];
+    } else {
+      in += ((uintptr_t)p & 15) / 4;
+      const bool between = sizeof(T) == 2 && ((uintptr_t)p & 2);
+#pragma unroll
+      for (int u = 0; u < Cols::U; ++u) {
+        w[u] = 0;
+        if (at.inside(u)) {
+          const int i = at.column(u) / Cols::E;
+          w[u] = in[i];
+          if (between) w[u] = __funnelshift_r(w[u], in[i + 1], 16);
+          if (sizeof(T) == 2 && at.column(u) + 1 >= at.d) w[u] &= 0xffffu;
+        }
+      }
+    }
   }
 };
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -316,11 +338,8 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const Norm
     wait_copies<D - 1>();
     if (SHIFTED) group_barrier<G, kBlock<G> / G>(at.slot);
     {
-      const int lead = Rows::lead_of(x + t * a.ldx + at.base);
-      uint4 raw[Cols::U];
-#pragma unroll
-      for (int u = 0; u < Cols::U; ++u)
-        if (at.cols.inside(u)) raw[u] = feed.word(at.cols, slot, u, lead);
+      typename Rows::Word raw[Cols::U];
+      feed.take(at.cols, slot, x + t * a.ldx + at.base, raw);
       at.cols.each([&](int k) { v[k] = Cols::pair(raw, k); });
     }
     auto refill = [&] {
@@ -332,7 +351,7 @@ __global__ void __launch_bounds__(kBlock<G>) k_norm(const T* x, T* y, const Norm
     if (!SHIFTED || G == 32) refill();
     // the warp's mean c, and its sums s and m2 of x - c and their squares
     uint64_t p = 0;
-    at.cols.each([&](int k) { p = ptx::add_f32x2(p, at.cols.masked(v[k], k)); });
+    at.cols.each([&](int k) { p = ptx::add_f32x2(p, v[k]); });
     float c = warp_sum(sum_of(p)) * over_n, off = c, s, m2;
     // once, but for rows whose spread is lost in the mean's rounding
     for (int again = 0;; ++again) {
@@ -454,18 +473,11 @@ __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x
   const float over = 1.f / (float)a.d;
   int turn = 0, slot = 0;
   for (int64_t t = at.first; t < a.tokens; t += at.step) {
-    uint4 raw_x[Cols::U], raw_dy[Cols::U];
+    typename Rows::Word raw_x[Cols::U], raw_dy[Cols::U];
     wait_copies<D - 1>();
     if (SHIFTED) group_barrier<G, GROUPS>(at.slot);
-    {
-      const int lead_x = Rows::lead_of(x + t * a.ldx + at.base), lead_dy = Rows::lead_of(dy + t * a.lddy + at.base);
-#pragma unroll
-      for (int u = 0; u < Cols::U; ++u)
-        if (at.cols.inside(u)) {
-          raw_x[u] = feed_x.word(at.cols, slot, u, lead_x);
-          raw_dy[u] = feed_dy.word(at.cols, slot, u, lead_dy);
-        }
-    }
+    feed_x.take(at.cols, slot, x + t * a.ldx + at.base, raw_x);
+    feed_dy.take(at.cols, slot, dy + t * a.lddy + at.base, raw_dy);
     auto refill = [&] {
       issue(t + D * at.step, slot);
       slot = slot + 1 == D ? 0 : slot + 1;
@@ -479,7 +491,7 @@ __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x
     uint64_t s0 = 0, s1 = 0, s2 = 0;
     at.cols.each([&](int k) {
       const uint64_t xh = at.cols.masked(ptx::mul_f32x2(ptx::add_f32x2(Cols::pair(raw_x, k), minus_mean), r), k);
-      const uint64_t gw = ptx::mul_f32x2(at.cols.masked(Cols::pair(raw_dy, k), k), weight(k));
+      const uint64_t gw = ptx::mul_f32x2(Cols::pair(raw_dy, k), weight(k));
       s0 = ptx::add_f32x2(s0, xh);
       s1 = ptx::add_f32x2(s1, gw);
       s2 = ptx::fma_f32x2(gw, xh, s2);
@@ -516,7 +528,7 @@ __global__ void __launch_bounds__(G* GROUPS) k_norm_grad(const T* dy, const T* x
     const float off = sum[0] * over, mean_g = sum[1] * over, mean_gx = sum[2] * over - off * mean_g;
     const uint64_t less = both(-off), down = both(-mean_g * rstd), along = both(-mean_gx * rstd);
     auto step = [&](int k) {
-      const uint64_t g = at.cols.masked(Cols::pair(raw_dy, k), k);
+      const uint64_t g = Cols::pair(raw_dy, k);
       const uint64_t xh = ptx::add_f32x2(ptx::mul_f32x2(ptx::add_f32x2(Cols::pair(raw_x, k), minus_mean), r), less);
       dw[k] = ptx::fma_f32x2(g, xh, dw[k]);
       db[k] = ptx::add_f32x2(db[k], g);
