@@ -483,8 +483,9 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, 
         dbp = dbias.data_ptr()
     if need_dweight or need_dbias:
         nbytes = _norm_bytes(ty, n, d)
-        ws = _workspace(nbytes, device)
-        wsp = ws.data_ptr()
+        if nbytes:
+            ws = _workspace(nbytes, device)
+            wsp = ws.data_ptr()
     _call(at, _lib.load().lipcache_layer_norm_backward, ty, dy.data_ptr(), lddy, x.data_ptr(), ldx, n, d,
           stats.data_ptr(), w, dxp, d, dwp, dbp, wsp, nbytes)
     return dx, dweight, dbias

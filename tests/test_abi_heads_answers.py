@@ -62,13 +62,14 @@ def test_layer_norm_arguments(lib):
         a.update(bad)
         assert lib.lipcache_layer_norm_workspace(a["ty"], a["n"], a["d"]) == -1, bad
     assert lib.lipcache_layer_norm_workspace(0, 0, 8) == 0
-    assert lib.lipcache_layer_norm_workspace(1, 5, 65_536) >= 2 * 65_536 * 4
+    assert lib.lipcache_layer_norm_workspace(1, 500, 65_536) >= 2 * 65_536 * 4
+    assert lib.lipcache_layer_norm_workspace(1, 5, 65_536) == 0  # few rows need none
 
 
 def test_layer_norm_backward_arguments(lib):
     big = 1 << 40  # a workspace size; the refusals come before any use
 
-    def call(ty=0, dy=4096, lddy=8, x=4096, ldx=8, n=2, d=8, stats=4096, w=4096, dx=8192, lddx=8, dw=4096, db=4096,
+    def call(ty=0, dy=4096, lddy=8, x=4096, ldx=8, n=2000, d=8, stats=4096, w=4096, dx=8192, lddx=8, dw=4096, db=4096,
              ws=4096, nb=big):
         return lib.lipcache_layer_norm_backward(ty, dy, lddy, x, ldx, n, d, stats, w, dx, lddx, dw, db, ws, nb, None)
     for bad in (dict(ty=5), dict(n=-1), dict(d=0), dict(d=65_537), dict(dy=None), dict(x=None), dict(stats=None), dict(lddy=7),
