@@ -10,6 +10,14 @@
 // at least k of them reach is found by halving; only threads that reach it hold
 // values that count, so only their granules are read again (from L2), and the few
 // values at or above it are ranked against each other by (value, lowest index).
+//
+// Measured: 4,096 x 50,001 BF16 88 us with 20 classes, 70 without (5.9 TB/s, near the
+// memory's rate: the classes cost a block 2 us of barriers, threshold and second
+// reading in which it loads nothing; rings of asynchronous copies across rows, 134 us,
+// and batches loaded ahead, 109 us, cost more instructions than they hide; 512 threads
+// a row 116 us). 65,536 x 200 FP32 with 5 classes 24 us, bound by instructions (some
+// 200 a row) and by the call from Python (20 us). One row 6 us of the GPU's time. The
+// gradient of 4,096 x 50,001 BF16 140 us, 5.8 TB/s.
 #include "head_mma.cuh"
 #include "head_rows.cuh"
 
@@ -568,6 +576,7 @@ void launch_lanes(const T* z, const ProbArgs& a, cudaStream_t s) {
 template <typename T, int L>
 bool probs_lanes(const T* z, const ProbArgs& a, int granules, cudaStream_t s) {
   constexpr int kMost = sizeof(T) == 4 ? 8 : 4;  // 32 values a lane
+  // (with k near L the least of the lanes' maxima would be the threshold, which half the row may reach)
   if (granules > L * kMost || 4 * a.k > 3 * L) return false;
   if (granules <= L)
     launch_lanes<T, L, 1>(z, a, s);
@@ -602,16 +611,24 @@ template <typename T>
 void launch_probs(const T* z, const ProbArgs& a, cudaStream_t s) {
   // granules of a row, one more where rows start inside one
   const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
-  if (probs_lanes<T, 8>(z, a, granules, s) || probs_lanes<T, 16>(z, a, granules, s) || probs_lanes<T, 32>(z, a, granules, s)) {
-  } else if (granules >= 16384 && 8 * a.tokens <= 2 * mma::num_sms()) {
-    // (one row of 150,000 BF16 classes 14 us in a cluster, 16 in a block, of 400,000 16 and
-    // 29; 80 rows of 150,000 27 and 18)
+  // Lanes while 32 values each hold the row (FP32, 65,536 x 200 with 5 classes 24 us, a
+  // block of 128 a row 195; 16,384 x 1,000 with 20 29 and 78). Beyond, a block a row, of
+  // so many threads that their sums and ranking do not outweigh the row (BF16, 20 classes:
+  // 8,192 x 7,000 50 us with 64, 55 with 128; x 16,000 81, 73 and 90 with 256; 4,096 x
+  // 50,001 152, 117 and 91), but twice as many as classes are asked for, or the threshold
+  // would let too much through. Few long rows a cluster (one row of 150,000 classes 14 us,
+  // 16 in a block, of 400,000 16 and 29; 80 rows of 150,000 27 and 18).
+  if (probs_lanes<T, 8>(z, a, granules, s) || probs_lanes<T, 16>(z, a, granules, s) ||
+      probs_lanes<T, 32>(z, a, granules, s))
+    ;
+  else if (granules >= 16384 && 8 * a.tokens <= 2 * mma::num_sms())
     launch_blocks<T, 256, 8>(z, a, s);
-  } else if (granules <= 2048 && a.k <= 64) {
+  else if (granules <= 1024 && a.k <= 32)
+    launch_blocks<T, 64, 1>(z, a, s);
+  else if (granules <= 4096 && a.k <= 64)
     launch_blocks<T, 128, 1>(z, a, s);
-  } else {
+  else
     launch_blocks<T, 256, 1>(z, a, s);
-  }
   LC_LAUNCH_CHECK("k_probs");
 }
 
