@@ -158,10 +158,10 @@ struct Reach<__nv_bfloat16> {
 
 // The group's k largest unmasked values in granules [begin, end) of a row without
 // NaN or +inf, after find_threshold and a barrier, to emit(rank, candidate), each rank
-// from one thread; returns how many there are (at most k).
+// from one thread; returns how many there are (at most k). m: the largest of them.
 template <typename T, int G, typename Get, typename Emit>
 __device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice& at, int begin, int end, int n, int k,
-                                              Get get, SelectShared<G>& sh, Emit emit) {
+                                              float m, Get get, SelectShared<G>& sh, Emit emit) {
   constexpr uint32_t kAll = 0xffffffffu;
   constexpr int N = Vec<T>::N, kCap = SelectShared<G>::kCap;
   const int rank = group_rank<G>(), lane = threadIdx.x & 31, warp = G == 32 ? 0 : threadIdx.x >> 5;
@@ -212,7 +212,7 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice
     // Many equal values, or large ones crowded into few threads: halve over the whole
     // row until the values from lo up fit, or those above lo are fewer than k and the
     // rest of the k are ties at lo.
-    uint32_t lo = tau, hi = kNanKey;
+    uint32_t lo = tau, hi = ops::key_of(m) + 1;
     int from_lo = found;
     auto count = [&](int i, uint32_t from) {
       const uint4 w = get(i);
@@ -348,7 +348,7 @@ __device__ __forceinline__ void fill_top(const ProbArgs& a, int64_t row, int fro
 // takes the rows of which too much does. k <= L.
 template <typename T, int L, int U>
 __global__ void __launch_bounds__(128) k_probs_lanes(const T* z, const ProbArgs a) {
-  constexpr int N = Vec<T>::N, kRows = 32 / L, kCap = 64;
+  constexpr int N = Vec<T>::N, kRows = 32 / L, kCap = L == 32 ? 128 : 64;
   constexpr uint32_t kAll = 0xffffffffu;
   __shared__ Found found_s[4 * kRows][kCap];
   __shared__ SelectShared<32> select_s[4];
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(128) k_probs_lanes(const T* z, const ProbArgs 
     RowSays other = says;
     other.m = __shfl_sync(kAll, says.m, from);
     other.log_sum = __shfl_sync(kAll, says.log_sum, from);
-    const int have = select_largest<T, 32>(wide, at, 0, wide.count, a.classes, a.k, get, select_s[warp],
+    const int have = select_largest<T, 32>(wide, at, 0, wide.count, a.classes, a.k, other.m, get, select_s[warp],
                                            [&](int r, Found f) { put_top(a, tt, other, r, f); });
     fill_top(a, tt, have, false, threadIdx.x & 31, 32);
     __syncwarp();
@@ -479,14 +479,15 @@ __global__ void __launch_bounds__(G, (CL > 1 ? 768 : 1536) / G) k_probs(const T*
     int have = 0;
     const bool bad = isnan(sums.m);
     if (!bad && !sums.none)
-      have = select_largest<T, G>(row, at, begin, end, a.classes, a.k, get, select,
+      have = select_largest<T, G>(row, at, begin, end, a.classes, a.k, sums.m, get, select,
                                   [&](int r, Found f) { put_top(a, t, RowSays(sums), r, f); });
     if (have < a.k) fill_top(a, t, have, bad, rank, G);
   } else {
     // each block's best, which the first one ranks against each other
     int have = 0;
     if (a.k && !isnan(sums.m) && !sums.none)
-      have = select_largest<T, G>(row, at, begin, end, a.classes, a.k, get, select, [&](int r, Found f) { best_s[r] = f; });
+      have = select_largest<T, G>(row, at, begin, end, a.classes, a.k, sums.m, get, select,
+                                  [&](int r, Found f) { best_s[r] = f; });
     if (rank == 0) {
       part_s = sums;
       have_s = have;

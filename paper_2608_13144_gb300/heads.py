@@ -304,6 +304,7 @@ def log_probs(logits: torch.Tensor, target: torch.Tensor | None = None, top: int
     ty, at, n, c = _logits(logits)
     if logits.requires_grad and _grads():
         _recorded(logits=logits)
+    top = int(top)
     if not 0 <= top <= 128:
         raise ValueError("top must be in [0, 128]")
     z, ldz = _rows(logits)
@@ -318,7 +319,7 @@ def log_probs(logits: torch.Tensor, target: torch.Tensor | None = None, top: int
     if top:
         best, index = _empty((n, top), dtype=F32, device=device), _empty((n, top), dtype=I32, device=device)
         bp, ip = best.data_ptr(), index.data_ptr()
-    _call(at, _lib.load().lipcache_log_probs, ty, z.data_ptr(), ldz, n, c, y, top, temperature, lp, entropy.data_ptr(),
+    _call(at, _lib.load().lipcache_log_probs, ty, z.data_ptr(), ldz, n, c, y, top, float(temperature), lp, entropy.data_ptr(),
           norm.data_ptr(), bp, ip)
     return LogProbs(logprob, entropy, norm, best, index)
 
@@ -360,8 +361,8 @@ def log_probs_backward(logits: torch.Tensor, norm: torch.Tensor, target: torch.T
         dentropy = _entries(dentropy, "dentropy", n, at, F32, "row of logits")
         h = dentropy.data_ptr()
     z, ldz, dz, ldd = _gradient(logits, in_place)
-    _call(at, _lib.load().lipcache_log_probs_backward, ty, z.data_ptr(), ldz, n, c, norm.data_ptr(), y, g, h, temperature,
-          dz.data_ptr(), ldd)
+    _call(at, _lib.load().lipcache_log_probs_backward, ty, z.data_ptr(), ldz, n, c, norm.data_ptr(), y, g, h,
+          float(temperature), dz.data_ptr(), ldd)
     if in_place:
         _written(dz)
     return dz
@@ -398,7 +399,7 @@ def distill(logits: torch.Tensor, top: torch.Tensor, index: torch.Tensor, weight
         ldd = c
     loss = _empty(n, dtype=F32, device=z.device)
     _call(at, _lib.load().lipcache_distill, ty, z.data_ptr(), ldz, n, c, k, top.data_ptr(), index.data_ptr(), w,
-          temperature, loss.data_ptr(), dp, ldd)
+          float(temperature), loss.data_ptr(), dp, ldd)
     if in_place and need_grad:
         _written(dz)
     return loss, dz
@@ -443,7 +444,7 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
         if out.shape != (n, d) or y is not out:
             raise ValueError("out must be n x d with dense rows")
     stats = _empty((n, 2), dtype=F32, device=device)
-    _call(at, _lib.load().lipcache_layer_norm, TYPES[dt], x.data_ptr(), ldx, n, d, w, b, eps, y.data_ptr(), ldy,
+    _call(at, _lib.load().lipcache_layer_norm, TYPES[dt], x.data_ptr(), ldx, n, d, w, b, float(eps), y.data_ptr(), ldy,
           stats.data_ptr())
     if out is not None:
         _written(out)

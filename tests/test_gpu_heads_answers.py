@@ -145,7 +145,8 @@ def logits(dev, dtype, n, c, seed=0, spread=3.0):
 
 SIZES = [(1, 1, 1), (1, 2, 2), (3, 10, 5), (2, 33, 40), (7, 200, 5), (5, 255, 32), (4, 257, 33), (9, 1000, 20),
          (6, 1023, 128), (3, 2047, 8), (5, 2049, 64), (2, 4096, 1), (3, 8200, 128), (2, 16_390, 20), (2, 20_001, 50),
-         (3, 50_001, 20), (1, 131_073, 100), (1, 400_003, 7), (700, 200, 10), (300, 17, 3), (64, 3000, 0), (40, 12_345, 16)]
+         (3, 50_001, 20), (1, 131_073, 100), (1, 400_003, 7), (700, 200, 10), (300, 17, 3), (64, 3000, 0), (40, 12_345, 16),
+         (30, 140_000, 128), (41, 140_001, 30), (200, 7000, 32), (160, 7001, 33), (33, 31_000, 65)]
 
 
 @BOTH
@@ -519,6 +520,32 @@ def test_rows_beyond_32_bits(dev, heads):
     grad = heads.log_probs_backward(z, norm, y, torch.ones(3, device=dev))
     assert torch.equal(heads.log_probs_backward(z, norm, y, torch.ones(3, device=dev), in_place=True), grad)
     del w
+
+
+@BOTH
+def test_arguments_of_any_kind(dev, heads, dtype):
+    """Strided and expanded tensors, numbers of other types, rows of one class."""
+    import numpy as np
+    z, y = logits(dev, dtype, 6, 300, seed=13)
+    want = heads.log_probs(z, y, top=4, temperature=2.0)
+    wide = torch.zeros(6, 2, dtype=torch.int32, device=dev)
+    wide[:, 1] = y
+    got = heads.log_probs(z, wide[:, 1], top=np.int64(4), temperature=torch.tensor(2.0))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    g = torch.ones(1, device=dev).expand(6)
+    a = heads.log_probs_backward(z, want.norm, y, g, g, temperature=2)
+    b = heads.log_probs_backward(z, want.norm.t().contiguous().t(), wide[:, 1], g.contiguous(), g.contiguous(), temperature=2.0)
+    assert torch.equal(a, b)
+    top, index = teacher(dev, z, 5)
+    c = heads.distill(z, top, index, g, temperature=2)
+    d = heads.distill(z, top.t().contiguous().t(), index.t().contiguous().t(), g.contiguous(), temperature=2.0)
+    assert all(torch.equal(p, q) for p, q in zip(c, d))
+    row = z[:1].expand(6, 300)  # one row, six times
+    e, f = heads.log_probs(row, y, top=4), heads.log_probs(row.contiguous(), y, top=4)
+    assert all(torch.equal(p, q) for p, q in zip(e, f))
+    check_answers(heads, z[:, 7:8], torch.zeros(6, dtype=torch.int32, device=dev), 2)
+    with pytest.raises(ValueError):
+        heads.distill(row, top, index, in_place=True)
 
 
 def test_refusals(dev, heads):
