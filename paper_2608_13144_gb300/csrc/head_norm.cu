@@ -649,13 +649,14 @@ __global__ void __launch_bounds__(512) k_norm_columns(const float* parts, int bl
 }
 
 // Blocks (clusters of CL) that take rows in turn: what a GB300's 152 SMs hold at once
-// of the kernel, whose rows are then dealt evenly.
+// of the kernel, whose rows are then dealt evenly (gradients: four an SM at most, whose
+// columns' sums the workspace holds).
 constexpr int kSms = 152, kMostOnSm = 4;
 template <typename K>
 int resident_blocks(K kernel, int threads, int smem) {
   int n = 0;
   LC_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, (size_t)smem));
-  return std::max(1, std::min(n, kMostOnSm)) * kSms;
+  return std::max(1, n) * kSms;
 }
 
 template <int CL, typename K, typename... Args>
@@ -788,7 +789,7 @@ void launch_norm_grad(const T* dy, const T* x, T* dx, const NormArgs& a, cudaStr
         constexpr int kSums = GROUPS > 1 ? GROUPS * 2 * G * P * 4 : 0, kSmem = kRing > kSums ? kRing : kSums;
         const auto kernel = k_norm_grad<T, G, P, decltype(full)::value, SHIFTED, CL, GROUPS>;
         if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
-        static const int kResident = resident_blocks(kernel, G * GROUPS, kSmem);
+        static const int kResident = std::min(resident_blocks(kernel, G * GROUPS, kSmem), kMostOnSm * kSms);
         const bool sums = a.dweight || a.dbias;
         blocks = sums && !a.parts ? 1 : (int)std::min<int64_t>(ceil_div(a.tokens, GROUPS), kResident / CL);
         launch_cluster<CL>(kernel, blocks, G * GROUPS, kSmem, s, dy, x, dx, a);
