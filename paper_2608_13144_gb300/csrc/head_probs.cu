@@ -184,14 +184,19 @@ __device__ __forceinline__ int select_largest(const RowSpan<T>& row, const Slice
   const int live = sh.n_live;
   const uint32_t tau = sh.tau;
   const Reach<T> reach(value_of(tau));
-  constexpr int W = G / 32, Q = 4;  // (of Q threads at a time, whose granules come from memory together)
+  // Of as many threads at a time as their granules fill lanes (a power of two each), Q
+  // such loads before what comes of them.
+  constexpr int W = G / 32, Q = 4;
+  const int rounds = (at.last - at.first + G - 1) / G, bits = rounds > 16 ? 5 : rounds > 1 ? 32 - __clz(rounds - 1) : 0;
+  const int each = 32 >> bits, mine = (warp << (5 - bits)) + (lane >> bits), nth = lane & ((1 << bits) - 1);
   for (int base = at.first; base < at.last; base += 32 * G)
-    for (int l = warp; l < live; l += Q * W) {
+    for (int l = mine; l - (lane >> bits) < live; l += Q * W * each) {
       uint4 w[Q];
       int i[Q];
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        i[q] = l + q * W < live ? base + sh.live[l + q * W] + lane * G : at.last;
+        const int of = l + q * W * each;
+        i[q] = of < live ? base + sh.live[of] + nth * G : at.last;
         if (i[q] < at.last) w[q] = get(i[q]);
       }
 #pragma unroll
