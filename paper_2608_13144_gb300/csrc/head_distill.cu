@@ -151,7 +151,7 @@ __device__ __forceinline__ uint4 granule_of(float fill) {
 
 // Small rows: L lanes each, U granules a lane, up to 2 L classes of the teacher.
 template <typename T, int L, int U>
-__global__ void __launch_bounds__(128) k_distill_lanes(const T* z, T* dz, const DistillArgs a) {
+__global__ void __launch_bounds__(128, 8) k_distill_lanes(const T* z, T* dz, const DistillArgs a) {
   constexpr int kRows = 32 / L, R = 2;
   ptx::wait_prerequisites();
   ptx::launch_dependents();

@@ -352,7 +352,7 @@ __device__ __forceinline__ void fill_top(const ProbArgs& a, int64_t row, int fro
 // maxima is the threshold; what reaches it is ranked as in select_largest, which also
 // takes the rows of which too much does. k <= L.
 template <typename T, int L, int U>
-__global__ void __launch_bounds__(128) k_probs_lanes(const T* z, const ProbArgs a) {
+__global__ void __launch_bounds__(128, 8) k_probs_lanes(const T* z, const ProbArgs a) {
   constexpr int N = Vec<T>::N, kRows = 32 / L, kCap = L == 32 ? 128 : 64;
   constexpr uint32_t kAll = 0xffffffffu;
   __shared__ Found found_s[4 * kRows][kCap];
