@@ -16,7 +16,7 @@
 // reading in which it loads nothing; rings of asynchronous copies across rows, 134 us,
 // and batches loaded ahead, 109 us, cost more instructions than they hide; 512 threads
 // a row 116 us). 65,536 x 200 FP32 with 5 classes 24 us, bound by instructions (some
-// 200 a row) and by the call from Python (20 us). One row 6 us of the GPU's time. The
+// 300 a row) and by the call from Python (20 us). One row 6 us of the GPU's time. The
 // gradient of 4,096 x 50,001 BF16 140 us, 5.8 TB/s.
 #include "head_mma.cuh"
 #include "head_rows.cuh"
@@ -620,8 +620,8 @@ void launch_probs(const T* z, const ProbArgs& a, cudaStream_t s) {
   // Lanes while 32 values each hold the row (FP32, 65,536 x 200 with 5 classes 24 us, a
   // block of 128 a row 195; 16,384 x 1,000 with 20 29 and 78). Beyond, a block a row, of
   // so many threads that their sums and ranking do not outweigh the row (BF16, 20 classes:
-  // 8,192 x 7,000 50 us with 64, 55 with 128; x 16,000 81, 73 and 90 with 256; 4,096 x
-  // 50,001 152, 117 and 91), but twice as many as classes are asked for, or the threshold
+  // 8,192 x 3,000 30 us with 64, 37 with 128, 60 with 256; x 16,000 83, 68 and 82; 4,096 x
+  // 50,001 155, 117 and 90), but twice as many as classes are asked for, or the threshold
   // would let too much through. Few long rows a cluster (one row of 150,000 classes 14 us,
   // 16 in a block, of 400,000 16 and 29; 80 rows of 150,000 27 and 18).
   if (probs_lanes<T, 8>(z, a, granules, s) || probs_lanes<T, 16>(z, a, granules, s) ||
