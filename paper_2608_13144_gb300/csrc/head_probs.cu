@@ -17,7 +17,7 @@
 // and batches loaded ahead, 109 us, cost more instructions than they hide; 512 threads
 // a row 116 us). 65,536 x 200 FP32 with 5 classes 24 us, bound by instructions (some
 // 300 a row) and by the call from Python (20 us). One row 6 us of the GPU's time. The
-// gradient of 4,096 x 50,001 BF16 140 us, 5.8 TB/s.
+// gradient of 4,096 x 50,001 BF16 131 us, 6.3 TB/s.
 #include "head_mma.cuh"
 #include "head_rows.cuh"
 
@@ -750,17 +750,15 @@ void launch_grad(const T* z, T* dz, const ProbGradArgs& a, int granules, cudaStr
 template <typename T>
 void launch_probs_grad(const T* z, T* dz, const ProbGradArgs& a, cudaStream_t s) {
   const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
-  // (at most 2^24 / 4 / 128 parts)
+  // (four granules a lane: 4,096 x 50,001 BF16 133 us of the GPU's time, eight 144; at most 2^24 / 4 / 128 parts)
   if (granules <= 8)
     launch_grad<T, 8, 1>(z, dz, a, granules, s);
   else if (granules <= 32)
     launch_grad<T, 8, 4>(z, dz, a, granules, s);
   else if (granules <= 64)
     launch_grad<T, 16, 4>(z, dz, a, granules, s);
-  else if (granules <= 128)
-    launch_grad<T, 32, 4>(z, dz, a, granules, s);
   else
-    launch_grad<T, 32, sizeof(T) == 4 ? 4 : 8>(z, dz, a, granules, s);
+    launch_grad<T, 32, 4>(z, dz, a, granules, s);
   LC_LAUNCH_CHECK("k_probs_grad");
 }
 
