@@ -6,9 +6,11 @@
 // turn, so that weight, bias and the columns' sums stay with their thread. Columns'
 // sums are written once a block and joined by a second kernel, in a fixed order.
 //
-// A row's moments are taken by warps about the warp's own mean and joined by their
-// distances, which are small: a row far from 0 loses nothing, and one barrier a row
-// is enough. The gradient takes out what the rounded mean that it is given is off by.
+// A row's moments are taken by warps about the warp's own mean, rounded, and joined by
+// their distances, which are small: a row far from 0 loses nothing, and one barrier a row
+// is enough. (No value lies between a mean and the FP32 numbers beside it: the square of
+// what the rounding takes from the mean is at most the variance.) The gradient takes out
+// what the rounded mean that it is given is off by.
 //
 // Bound by memory, then by the latency of the sums' shuffles: 16,384 x 4,096 BF16 48
 // us, 5.6 TB/s, the gradients 72 us, 5.6 TB/s, of which the columns' second kernel is 6;
@@ -406,8 +408,8 @@ __global__ void __launch_bounds__(kBlock<G>, SHIFTED ? kFitting<kBlock<G>, P == 
         const float sq = warp_sum2(sum_of(s2), sum_of(q2)), other = __shfl_xor_sync(kAll, sq, 16);
         s = lane < 16 ? sq : other;
         m2 = lane < 16 ? other : sq;
-        if (!(s * s > m2 * n * 0.00390625f) || again == 7) break;
-        off = s * over_n;
+        off = (c + s * over_n) - c;  // by as much as c moves, so that v stays the distance from c
+        if (!(s * s > m2 * n * 0.00390625f) || off == 0.f || again == 7) break;
         c += off;
       }
       // e: the warp's c less the row's mean

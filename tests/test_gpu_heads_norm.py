@@ -144,6 +144,23 @@ def test_rows_far_from_zero(dev, heads, dtype, d):
     check_norm(heads, x, w, b, eps=1.0)
 
 
+@pytest.mark.parametrize("d", [700, 1500, 2050, 4096, 16_385, 20_000, 40_000])
+@pytest.mark.parametrize("mean", [1000.1234, 3.3, -30_000.0])
+def test_spreads_of_a_few_steps_of_fp32(dev, heads, mean, d):
+    """Rows of values a few steps of FP32 above one far from 0, their level other from each 700 columns to the next: the
+    row's mean and those of its parts lie between two steps."""
+    gen = torch.Generator().manual_seed(d)
+    base = torch.tensor(mean, dtype=F32).double()
+    step = 2.0 ** (math.floor(math.log2(abs(mean))) - 23)
+    steps = torch.randint(0, 3, (5, d), generator=gen) + (torch.arange(d) // 700 * 7 % 4)[None, :]
+    exact = base + step * steps
+    x = exact.float()
+    assert torch.equal(x.double(), exact)
+    _, w, b, dy = case(dev, F32, 5, d, seed=1)
+    _, stats = check_norm(heads, x.to(dev), w, b, eps=1e-30)
+    check_gradient(heads, dy, x.to(dev), w, stats)
+
+
 @BOTH
 @pytest.mark.parametrize("n,d", [(3, 40), (11, 300), (3, 1500), (2, 6000), (2, 9000)])
 def test_strides_and_offsets(dev, heads, dtype, n, d):
