@@ -651,9 +651,8 @@ __global__ void __launch_bounds__(512) k_norm_columns(const float* parts, int bl
 }
 
 // Blocks (clusters of CL) that take rows in turn: what a GB300's 152 SMs hold at once
-// of the kernel, whose rows are then dealt evenly (gradients: four an SM at most, whose
-// columns' sums the workspace holds).
-constexpr int kSms = 152, kMostOnSm = 4;
+// of the kernel, whose rows are then dealt evenly.
+constexpr int kSms = 152;
 template <typename K>
 int resident_blocks(K kernel, int threads, int smem) {
   int n = 0;
@@ -739,6 +738,11 @@ void by_width_grad(int d, F&& f) {
     f(Int<512>{}, Int<16>{}, Int<8>{}, Int<1>{});
   }
 }
+// The gradients' blocks (clusters) at most, each with its columns' sums in the workspace:
+// as many as the registers of by_width_grad's kernels let the SMs hold.
+int most_parts(int d) {
+  return kSms * (d <= 256 ? 3 : d <= 512 ? 2 : 1) / (d <= 8192 ? 1 : d <= 16384 ? 2 : d <= 32768 ? 4 : 8);
+}
 // f(FULL)
 template <bool SHIFTED, typename F>
 void by_fullness(bool full, F&& f) {
@@ -791,9 +795,10 @@ void launch_norm_grad(const T* dy, const T* x, T* dx, const NormArgs& a, cudaStr
         constexpr int kSums = GROUPS > 1 ? GROUPS * 2 * G * P * 4 : 0, kSmem = kRing > kSums ? kRing : kSums;
         const auto kernel = k_norm_grad<T, G, P, decltype(full)::value, SHIFTED, CL, GROUPS>;
         if (kSmem > 40 * 1024) allow_smem(reinterpret_cast<const void*>(kernel), kSmem);
-        static const int kResident = std::min(resident_blocks(kernel, G * GROUPS, kSmem), kMostOnSm * kSms);
+        static const int kResident = resident_blocks(kernel, G * GROUPS, kSmem);
         const bool sums = a.dweight || a.dbias;
-        blocks = sums && !a.parts ? 1 : (int)std::min<int64_t>(ceil_div(a.tokens, GROUPS), kResident / CL);
+        const int most = std::min(kResident / CL, most_parts(a.d));
+        blocks = sums && !a.parts ? 1 : (int)std::min<int64_t>(ceil_div(a.tokens, GROUPS), most);
         launch_cluster<CL>(kernel, blocks, G * GROUPS, kSmem, s, dy, x, dx, a);
       });
     });
@@ -817,7 +822,7 @@ bool one_block(int64_t tokens, int d) { return tokens <= (d <= 512 ? 64 : d <= 4
 }  // namespace
 
 size_t layer_norm_bytes(int64_t tokens, int d) {
-  return one_block(tokens, d) ? 0 : (size_t)std::min<int64_t>(tokens, kSms * kMostOnSm) * 2 * d * 4;
+  return one_block(tokens, d) ? 0 : (size_t)std::min<int64_t>(tokens, most_parts(d)) * 2 * d * 4;
 }
 
 void layer_norm(int type, const void* x, int64_t ldx, int64_t tokens, int d, const float* weight, const float* bias,

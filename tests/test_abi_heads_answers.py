@@ -66,6 +66,15 @@ def test_layer_norm_arguments(lib):
     assert lib.lipcache_layer_norm_workspace(1, 2, 65_536) == 0  # few rows need none
 
 
+def test_layer_norm_workspace_is_what_blocks_write(lib):
+    """Two sums a column of each block: of an SM's blocks, or of clusters that share a wide row, not more."""
+    for d, blocks in ((8, 3 * 152), (256, 3 * 152), (257, 2 * 152), (512, 2 * 152), (1000, 152), (8192, 152), (8193, 76),
+                      (20_000, 38), (40_000, 19), (65_536, 19)):
+        for ty in (0, 1):
+            assert lib.lipcache_layer_norm_workspace(ty, 1 << 20, d) <= blocks * 2 * d * 4, d
+            assert lib.lipcache_layer_norm_workspace(ty, 10, d) in (0, 10 * 2 * d * 4), d
+
+
 def test_layer_norm_backward_arguments(lib):
     big = 1 << 40  # a workspace size; the refusals come before any use
 
