@@ -10,7 +10,8 @@
 // Measured: 4,096 x 50,001 BF16 from 64 classes 144 us, 5.7 TB/s (read and written
 // once; two blocks an SM, whose loads, sums and stores alternate; a teacher's warp
 // beside the others: 175 us while the first of them had it as well). 65,536 x 200 FP32
-// from 10 classes 26 us, 4.3 TB/s, half of it instructions.
+// from 10 classes 25 us, 4.4 TB/s, bound by instructions (309 a row, 71 % of the issue
+// slots). (Below, where launches are compared: times a launch in a graph, 2 to 4 us more.)
 #include "head_mma.cuh"
 #include "head_rows.cuh"
 
@@ -407,11 +408,13 @@ template <typename T>
 void launch_distill(const T* z, T* dz, const DistillArgs& a, cudaStream_t s) {
   const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
   constexpr int kMost = kResidentBytes / 16;
-  // Lanes while 32 values each hold the row (FP32, 65,536 x 200 26 us, a block of 160 a row
-  // 316). Beyond, a block a row of about as many threads as keep 16 granules each (8,192 x
+  // Lanes while 32 values each hold the row and two entries each the teacher (FP32, 65,536 x
+  // 200 from 10 classes 29 us, a block of 160 a row 316; from 64 135, from 65, in blocks of
+  // 96, 299). Beyond, a block a row of about as many threads as keep 16 granules each (8,192 x
   // 3,000 BF16 31 us with 96, 44 with 160, 104 with 512; x 16,000 89 with 160, 146 with
   // 512), a cluster where one block's shared memory does not hold the row, or where rows
-  // are few (30 of 50,001 classes 8.9 us, 10.2 in a block each; of 20,001 8.8 and 7.5).
+  // are few (BF16, 8 of 50,001 classes 8 to 10 us, 10 in a block each, 32 10 and 10, 64 16
+  // and 10; of 20,001 8.8 and 7.5).
   if (distill_lanes<T, 8>(z, dz, a, granules, s) || distill_lanes<T, 16>(z, dz, a, granules, s) ||
       distill_lanes<T, 32>(z, dz, a, granules, s))
     ;

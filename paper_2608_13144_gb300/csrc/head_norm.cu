@@ -12,13 +12,13 @@
 // what the rounding takes from the mean is at most the variance.) The gradient takes out
 // what the rounded mean that it is given is off by.
 //
-// Bound by memory, then by the latency of the sums' shuffles: 16,384 x 4,096 BF16 48
-// us, 5.6 TB/s, the gradients 72 us, 5.6 TB/s, of which the columns' second kernel is 6;
-// 65,536 x 256 FP32 gradients 36 us, 5.6 TB/s. 32 columns a thread where registers hold
+// Bound by memory, then by the latency of the sums' shuffles: 16,384 x 4,096 BF16 47
+// us, 5.7 TB/s, the gradients 71 us, 5.7 TB/s, of which the columns' second kernel is 6;
+// 65,536 x 256 FP32 gradients 35 us, 5.7 TB/s. 32 columns a thread where registers hold
 // them (the gradient of BF16 rows: with weights in shared memory and values kept packed),
 // since what a row costs a warp beside its values weighs less (16 columns: 54 us). Rows
-// that are not aligned take two to three times as long (16,384 x 4,001 BF16 108 us, the
-// gradients 162), bound by instructions: loads and stores of 4 bytes, shifts between them.
+// that are not aligned take two to three times as long (16,384 x 4,001 BF16 105 us, the
+// gradients 165), bound by instructions: loads and stores of 4 bytes, shifts between them.
 #include "head_mma.cuh"
 #include "head_rows.cuh"
 
@@ -815,8 +815,10 @@ void launch_norm_grad(const T* dy, const T* x, T* dx, const NormArgs& a, cudaStr
 }
 
 // Few rows, which one block (or cluster) takes and writes the columns' sums of itself:
-// a second kernel and its workspace cost a call more than the rows one after another
-// (FP32, 64 rows of 256: 17 us a call from Python, 22 with both; 8 of the GPU's and 7).
+// a second kernel and its workspace cost a call more than the rows one after another.
+// Calls from Python take 15 us, 19 to 20 with both, until the rows' time shows; of the
+// GPU's time at the limits (with both): 64 x 256 FP32 8 us (7), 64 x 500 12 (8; BF16 22,
+// a call 20, and 9), 8 x 4,096 13 (10), 2 x 20,000 14 (14); 128 x 256 10 (6).
 bool one_block(int64_t tokens, int d) { return tokens <= (d <= 512 ? 64 : d <= 4096 ? 8 : 2); }
 
 }  // namespace

@@ -11,13 +11,14 @@
 // values that count, so only their granules are read again (from L2), and the few
 // values at or above it are ranked against each other by (value, lowest index).
 //
-// Measured: 4,096 x 50,001 BF16 88 us with 20 classes, 70 without (5.9 TB/s, near the
+// Measured: 4,096 x 50,001 BF16 88 us with 20 classes, 67 without (6.1 TB/s, near the
 // memory's rate: the classes cost a block 2 us of barriers, threshold and second
 // reading in which it loads nothing; rings of asynchronous copies across rows, 134 us,
 // and batches loaded ahead, 109 us, cost more instructions than they hide; 512 threads
-// a row 116 us). 65,536 x 200 FP32 with 5 classes 24 us, bound by instructions (some
-// 300 a row) and by the call from Python (20 us). One row 6 us of the GPU's time. The
-// gradient of 4,096 x 50,001 BF16 131 us, 6.3 TB/s.
+// a row 116 us). 65,536 x 200 FP32 with 5 classes 22 us, bound by instructions (306 a
+// row, 77 % of the issue slots) and by the call from Python (17 us). One row 3 us of the
+// GPU's time, of 50,001 BF16 classes 8. The gradient of 4,096 x 50,001 BF16 130 us, 6.3 TB/s. (Below, where launches
+// are compared: times a launch in a graph, 2 to 4 us more.)
 #include "head_mma.cuh"
 #include "head_rows.cuh"
 
@@ -617,13 +618,15 @@ template <typename T>
 void launch_probs(const T* z, const ProbArgs& a, cudaStream_t s) {
   // granules of a row, one more where rows start inside one
   const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
-  // Lanes while 32 values each hold the row (FP32, 65,536 x 200 with 5 classes 24 us, a
-  // block of 128 a row 195; 16,384 x 1,000 with 20 29 and 78). Beyond, a block a row, of
+  // Lanes while 32 values each hold the row (FP32, 65,536 x 200 with 5 classes 25 us, a
+  // block of 128 a row 195; 16,384 x 1,000 with 20 29 and 78) and maxima of theirs tell the
+  // classes asked for (65,536 x 200 with 24 classes 74 us, with 25, in blocks, 147). Beyond, a block a row, of
   // so many threads that their sums and ranking do not outweigh the row (BF16, 20 classes:
   // 8,192 x 3,000 30 us with 64, 37 with 128, 60 with 256; x 16,000 83, 68 and 82; 4,096 x
   // 50,001 155, 117 and 90), but twice as many as classes are asked for, or the threshold
   // would let too much through. Few long rows a cluster (one row of 150,000 classes 14 us,
-  // 16 in a block, of 400,000 16 and 29; 80 rows of 150,000 27 and 18).
+  // 16 in a block, of 400,000 16 and 29; 38 rows of 150,000 15 and 16, 60 rows 18 and 17, 80
+  // rows 26 and 17).
   if (probs_lanes<T, 8>(z, a, granules, s) || probs_lanes<T, 16>(z, a, granules, s) ||
       probs_lanes<T, 32>(z, a, granules, s))
     ;
@@ -750,7 +753,7 @@ void launch_grad(const T* z, T* dz, const ProbGradArgs& a, int granules, cudaStr
 template <typename T>
 void launch_probs_grad(const T* z, T* dz, const ProbGradArgs& a, cudaStream_t s) {
   const int granules = (int)ceil_div(a.classes, Vec<T>::N) + (a.ldz % Vec<T>::N || ((uintptr_t)z & 15) ? 1 : 0);
-  // (four granules a lane: 4,096 x 50,001 BF16 133 us of the GPU's time, eight 144; at most 2^24 / 4 / 128 parts)
+  // (four granules a lane: 4,096 x 50,001 BF16 133 us, eight 144; at most 2^24 / 4 / 128 parts)
   if (granules <= 8)
     launch_grad<T, 8, 1>(z, dz, a, granules, s);
   else if (granules <= 32)
