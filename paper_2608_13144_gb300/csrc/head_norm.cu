@@ -14,7 +14,7 @@
 //
 // Bound by memory, then by the latency of the sums' shuffles: 16,384 x 4,096 BF16 47
 // us, 5.7 TB/s, the gradients 71 us, 5.7 TB/s, of which the columns' second kernel is 6;
-// 65,536 x 256 FP32 gradients 35 us, 5.7 TB/s. 32 columns a thread where registers hold
+// 65,536 x 256 FP32 gradients 36 us, 5.6 TB/s. 32 columns a thread where registers hold
 // them (the gradient of BF16 rows: with weights in shared memory and values kept packed),
 // since what a row costs a warp beside its values weighs less (16 columns: 54 us). Rows
 // that are not aligned take two to three times as long (16,384 x 4,001 BF16 105 us, the
